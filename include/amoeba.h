@@ -448,6 +448,140 @@ AMOEBA_API amoeba_status amoeba_compact_bytes(const amoeba_plan* plan, const int
 AMOEBA_API amoeba_status amoeba_plan_weight_alias(const amoeba_plan* plan, int32_t dst_rank, int32_t tensor,
                                        int32_t* src_rank, int64_t* src_offset, int64_t* bytes);
 
+/*
+ * Operators on the cache of one running instance
+ *
+ * Between two transformations an instance serves: new tokens' keys and values go into its paged cache, queries attend
+ * over it, and caches that grow too long are cut.  These calls do that on the pools that the calls above re-lay-out, in
+ * either kv_order and at any TP degree, all workers of the instance in one launch.  They interpret the elements, so
+ * they take the element type besides the layout: elem_bytes must be 2 and head_dim 64 or 128 (UNSUPPORTED otherwise;
+ * amoeba_evict_kv moves elements only and takes any layout).
+ *
+ * Per-worker row buffers.  q, k, v, q_out and out are HOST arrays of layout->tp device pointers: worker r's rows of
+ * [heads of r][head_dim] elements, consecutive rows `stride` elements apart (the same for all workers; stride 0 =
+ * dense).  Pointers and strides are multiples of 16 bytes (ALIGNMENT).  So the three members of a worker's fused
+ * projection can be passed where they are, and one logical [rows][all heads][head_dim] tensor is passed as tp pointers
+ * into it.  pools is a HOST array of tp pools; `layer` the layer of the pools the call works on.
+ *
+ * Rows.  The new tokens of sequence s are rows d_q_starts[s] ... d_q_starts[s+1]-1, its last ones: with n rows and
+ * d_seq_lens[s] = len cached tokens, these included, row d_q_starts[s] + j is the token at cache index len - n + j.
+ * Rows that belong to no sequence - before the first, behind the last, as in a padded batch - are neither read nor
+ * written.  The token at cache index i of sequence s is in slot i % block_tokens of block
+ * d_block_table[s][i / block_tokens]; table entries past a sequence's last block are not read.
+ *
+ * Device-detected errors.  INVALID_ARG, and nothing of the sequence is done: a negative length or one that needs more
+ * than max_blocks_per_seq blocks, row numbers that decrease or leave [0, num_rows], more than max_q_len rows.
+ * BAD_BLOCK_ID, and only the tokens of that block are left out: a block id outside the pool.
+ */
+enum { AMOEBA_FP16 = 0, AMOEBA_BF16 = 1 }; /* element type */
+
+typedef struct {
+    const int32_t* d_block_table; /* [num_seqs][max_blocks_per_seq] */
+    const int32_t* d_seq_lens;    /* [num_seqs]: cached tokens, the new ones included */
+    const int32_t* d_q_starts;    /* [num_seqs + 1], or NULL: one new token per sequence, row s */
+    int32_t num_seqs, max_blocks_per_seq;
+    int32_t num_rows;             /* rows of the row buffers */
+    int32_t max_q_len;            /* no sequence has more new tokens than this (it sizes the launch) */
+} amoeba_batch;
+
+/* What amoeba_append_kv does to queries and keys on the way. */
+typedef struct {
+    const void *d_q_norm, *d_k_norm; /* [head_dim] weights of the RMS norm of each query / key head; NULL: no norm */
+    const double* d_inv_freq;        /* [rot_dim / 2] angle per position of each rotated pair; NULL: no rotation */
+    const int32_t* d_positions;      /* [num_rows] position of each row's token; NULL: its cache index */
+    float norm_eps;
+    int32_t rot_dim;     /* leading elements of a head that are rotated: a multiple of 16, at most head_dim */
+    int32_t interleaved; /* pair i is elements 2i, 2i+1 (1) or i, i + rot_dim/2 (0) */
+    int32_t reserved;
+} amoeba_rotation;
+
+/*
+ * amoeba_append_kv
+ *
+ * For every new token and head, in one pass: x = q or k is normalised, x_d / sqrt(mean(x^2) + eps) * w_d, and every
+ * pair (x_a, x_b) of its leading rot_dim elements turned by position * inv_freq[pair],
+ *   (x_a cos - x_b sin, x_b cos + x_a sin);
+ * queries go to q_out, keys and (as they are) values into the cache.  All in 32 bits with one rounding at the end; the
+ * angle and its reduction to [-pi, pi] in 64 bits, since position * inv_freq at position 131071 has lost the low digits
+ * of the angle in 32.
+ * rotation NULL: neither norm nor rotation.  q and q_out both NULL: keys and values only.  q_out may be q.  A sequence
+ * with more new tokens than cached ones is refused (INVALID_ARG).  Several sequences may share a block only if no new
+ * token falls into it.
+ */
+AMOEBA_API amoeba_status amoeba_append_kv(const amoeba_layout* layout, int32_t dtype, int32_t layer, void* const* pools,
+                               const amoeba_batch* batch, const void* const* q, int64_t q_stride,
+                               const void* const* k, int64_t k_stride, const void* const* v, int64_t v_stride,
+                               const amoeba_rotation* rotation, void* const* q_out, int64_t q_out_stride,
+                               int32_t* d_status, void* cuda_stream);
+
+/*
+ * amoeba_attend
+ *
+ * Attention of the new tokens over the cache: query head h of the row at cache index p uses key head h / (Hq/Hkv) and
+ * sees the cached tokens i with p - window < i <= p (window 0: i <= p),
+ *   out = sum_i softmax_i(scale * q . k_i) v_i,   lse = log sum_i exp(scale * q . k_i)
+ * A row that sees nothing (more new tokens than cached ones, an empty cache, only bad blocks) gets out = 0 and
+ * lse = -inf.  d_lse: float [num_rows][num_q_heads], or NULL.  Logits, softmax and sums are held in 32 bits; the
+ * weights are rounded to the element type for the product with the values.
+ * Slots that no query of the call sees may hold anything, infinities and NaN included; the values of the tokens that
+ * some query sees must be finite (a NaN there also reaches earlier rows of the same chunk).
+ * out may not be q.  d_workspace: amoeba_attend_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant before
+ * and after; calls that overlap on the GPU need separate ones.
+ */
+AMOEBA_API amoeba_status amoeba_attend_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
+                                            int64_t* bytes);
+AMOEBA_API amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtype, int32_t layer, const void* const* pools,
+                            const amoeba_batch* batch, const void* const* q, int64_t q_stride, float scale,
+                            int32_t window, void* const* out, int64_t out_stride, float* d_lse, int32_t* d_status,
+                            void* d_workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * amoeba_accumulate_scores
+ *
+ * The attention weight that every cached token received from the rows of the call: for key head g and token i
+ *   score[g][i] = (i < d_scored_lens[s] ? score[g][i] : 0) + sum over rows and query heads h of g that see i of
+ *                 exp(scale * q . k_i - lse[row][h])
+ * with amoeba_attend's lse of the same rows, mask and scale (rows with lse = -inf add nothing).  Every token below
+ * d_seq_lens[s] gets a value, so a score pool needs no clearing.  score_pools: HOST array of tp device pointers, worker
+ * r's float [num_layers][num_blocks][heads of r][block_tokens], addressed by the same block ids as the cache.
+ * d_scored_lens: int32 [num_seqs], or NULL: all sums start from zero.  The order of the additions is fixed: the same
+ * call gives the same bits.  Several sequences may share a block only if they would write the same scores there.
+ */
+AMOEBA_API amoeba_status amoeba_accumulate_scores(const amoeba_layout* layout, int32_t dtype, int32_t layer,
+                                       const void* const* pools, const amoeba_batch* batch, const void* const* q,
+                                       int64_t q_stride, float scale, int32_t window, const float* d_lse,
+                                       const int32_t* d_scored_lens, float* const* score_pools, int32_t* d_status,
+                                       void* cuda_stream);
+
+/*
+ * amoeba_evict_kv
+ *
+ * Cuts every sequence longer than `budget` tokens to budget: its last `recent` tokens stay and, for each layer and key
+ * head, the budget - recent others with the highest scores (equal scores: the lower index; a NaN counts as the lowest
+ * of all).  What stays keeps its order: with kept indices i_0 < i_1 < ... the token at cache index i_j moves, keys,
+ * values and score, to cache index j of the sequence's destination blocks.  Shorter sequences move as they are.  As
+ * every layer and head keeps the same number, the block table and lengths stay shared by all of them.  The elements
+ * are opaque (any elem_bytes, head_dim).
+ *
+ * d_dst_bt: the destination table, [num_seqs][dst_max_blocks_per_seq] - of free blocks (out of place: source blocks,
+ * which may be shared between sequences, keep their contents; no block may be named twice, nor be any sequence's
+ * source block), or the very pointer d_src_bt (in place: the tokens close up in the sequence's first blocks, which no
+ * other sequence may share; the blocks behind are the caller's to free).  d_new_lens: int32 [num_seqs],
+ * min(length, budget), not d_seq_lens itself.  score_pools may be NULL if recent = budget.
+ * 1 <= budget, 0 <= recent <= budget (INVALID_ARG).
+ * Device-detected: a sequence with a bad length, with a source or destination block id outside the pool, or that needs
+ * more destination blocks than dst_max_blocks_per_seq: INVALID_ARG or BAD_BLOCK_ID, nothing of it moves, new length -1.
+ * d_workspace: amoeba_evict_workspace_bytes(...) bytes for that many layers, as in amoeba_attend.
+ */
+AMOEBA_API amoeba_status amoeba_evict_workspace_bytes(const amoeba_layout* layout, int32_t num_layers, int32_t num_seqs,
+                                           int32_t budget, int64_t* bytes);
+AMOEBA_API amoeba_status amoeba_evict_kv(const amoeba_layout* layout, int32_t layer_begin, int32_t layer_end,
+                              void* const* pools, float* const* score_pools, const int32_t* d_src_bt,
+                              const int32_t* d_seq_lens, int32_t num_seqs, int32_t max_blocks_per_seq,
+                              const int32_t* d_dst_bt, int32_t dst_max_blocks_per_seq, int32_t budget, int32_t recent,
+                              int32_t* d_new_lens, int32_t* d_status, void* d_workspace, int64_t workspace_bytes,
+                              void* cuda_stream);
+
 /* Number of kernels the library has launched in this process (for launch accounting in benchmarks). */
 AMOEBA_API int64_t amoeba_launch_count(void);
 

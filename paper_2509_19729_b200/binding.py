@@ -79,6 +79,18 @@ class WeightDesc(C.Structure):
                 ("dst_pitch", C.c_int64), ("n_rows", C.c_int32), ("reserved", C.c_int32)]
 
 
+class Batch(C.Structure):
+    _fields_ = [("d_block_table", C.c_void_p), ("d_seq_lens", C.c_void_p), ("d_q_starts", C.c_void_p),
+                ("num_seqs", C.c_int32), ("max_blocks_per_seq", C.c_int32), ("num_rows", C.c_int32),
+                ("max_q_len", C.c_int32)]
+
+
+class Rotation(C.Structure):
+    _fields_ = [("d_q_norm", C.c_void_p), ("d_k_norm", C.c_void_p), ("d_inv_freq", C.c_void_p),
+                ("d_positions", C.c_void_p), ("norm_eps", C.c_float), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("reserved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -131,6 +143,16 @@ def _load():
         "amoeba_compact_weights_inplace": (I32, [VP, P(LayerWeights), P(I32), I32, I32, VP, VP]),
         "amoeba_compact_bytes": (I32, [VP, P(I32), P(I64)]),
         "amoeba_plan_weight_alias": (I32, [VP, I32, I32, P(I32), P(I64), P(I64)]),
+        "amoeba_append_kv": (I32, [P(Layout), I32, I32, P(VP), P(Batch), P(VP), I64, P(VP), I64, P(VP), I64, P(Rotation),
+                                   P(VP), I64, VP, VP]),
+        "amoeba_attend_workspace_bytes": (I32, [P(Layout), P(Batch), P(I64)]),
+        "amoeba_attend": (I32, [P(Layout), I32, I32, P(VP), P(Batch), P(VP), I64, C.c_float, I32, P(VP), I64, VP, VP, VP,
+                                I64, VP]),
+        "amoeba_accumulate_scores": (I32, [P(Layout), I32, I32, P(VP), P(Batch), P(VP), I64, C.c_float, I32, VP, VP,
+                                           P(VP), VP, VP]),
+        "amoeba_evict_workspace_bytes": (I32, [P(Layout), I32, I32, I32, P(I64)]),
+        "amoeba_evict_kv": (I32, [P(Layout), I32, I32, P(VP), P(VP), VP, VP, I32, I32, VP, I32, I32, I32, VP, VP, VP, I64,
+                                  VP]),
         "amoeba_launch_count": (I64, []),
         "amoeba_status_string": (C.c_char_p, [I32]),
     }
@@ -428,6 +450,222 @@ def amoeba_plan_weight_alias(plan: Plan, dst_rank: int, tensor: int):
 
 
 __all__.append("amoeba_plan_weight_alias")
+
+
+# ---- operators on the cache of a running instance.  Arguments are torch tensors: their types, shapes, strides and device
+# are checked here, the rest by the C library; the calls run on the tensors' device, on its current stream by default.
+DTYPE_FP16, DTYPE_BF16 = 0, 1
+__all__ += ["Batch", "Rotation", "DTYPE_FP16", "DTYPE_BF16", "make_batch", "make_rotation", "amoeba_append_kv",
+            "amoeba_attend_workspace_bytes", "amoeba_attend", "amoeba_accumulate_scores",
+            "amoeba_evict_workspace_bytes", "amoeba_evict_kv"]
+
+
+def _tensor(t, where: str, dtype, numel: int, device) -> int:
+    """Address of a dense tensor of `dtype` on `device` with at least `numel` elements."""
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < numel:
+        raise AmoebaError(ERR_INVALID_ARG, f"{where}: a dense {dtype} tensor on {device} of at least {numel} elements "
+                                           f"is needed, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _torch_dtype(dtype: int, where: str):
+    import torch
+
+    if dtype not in (DTYPE_FP16, DTYPE_BF16):
+        raise AmoebaError(ERR_UNSUPPORTED, where)
+    return torch.float16 if dtype == DTYPE_FP16 else torch.bfloat16
+
+
+def _pools(layout: Layout, pools, nbytes: int, where: str, device):
+    if len(pools) != layout.tp:
+        raise AmoebaError(ERR_INVALID_ARG, f"{where} (pool count != tp)")
+    for p in pools:
+        if p.device != device or not p.is_contiguous() or p.numel() * p.element_size() < nbytes:
+            raise AmoebaError(ERR_INVALID_ARG, f"{where}: a pool is on another device, strided or too small")
+    return (C.c_void_p * layout.tp)(*[p.data_ptr() for p in pools])
+
+
+def _row_buffers(layout: Layout, tensors, rows: int, width: int, dt, where: str, device):
+    """([tp] addresses, row stride) of the workers' [rows, width] (or [rows, heads, head_dim]) buffers."""
+    if len(tensors) != layout.tp:
+        raise AmoebaError(ERR_INVALID_ARG, f"{where} (row buffer count != tp)")
+    stride = None
+    for t in tensors:
+        n = t.dim()
+        ok = t.dtype == dt and t.device == device and n in (2, 3) and t.shape[0] >= rows and t.stride(-1) == 1
+        if ok and n == 3:
+            ok = t.shape[1] * t.shape[2] == width and (t.shape[1] == 1 or t.stride(1) == t.shape[2])
+        elif ok:
+            ok = t.shape[1] == width
+        st = (t.stride(0) if t.shape[0] > 1 else width) if ok else None
+        if not ok or (stride is not None and st != stride):
+            raise AmoebaError(ERR_INVALID_ARG, f"{where}: row buffers are {dt} on {device}, [>= {rows}, {width}], dense "
+                                               "along a row and equally strided")
+        stride = st
+    return (C.c_void_p * layout.tp)(*[t.data_ptr() for t in tensors]), stride
+
+
+def make_batch(block_table, seq_lens, q_starts=None, num_rows: Optional[int] = None, max_q_len: int = 1) -> Batch:
+    """A batch of new tokens: block_table int32 [num_seqs, max_blocks_per_seq], seq_lens int32 [num_seqs], q_starts int32
+    [num_seqs + 1] or None (one token per sequence); num_rows: rows of the row buffers.  Keeps the tensors."""
+    import torch
+
+    S = seq_lens.numel()
+    dev = seq_lens.device
+    if block_table.dim() != 2 or block_table.shape[0] != S:
+        raise AmoebaError(ERR_INVALID_ARG, "make_batch: block_table is [num_seqs, max_blocks_per_seq]")
+    if q_starts is not None and num_rows is None:
+        raise AmoebaError(ERR_INVALID_ARG, "make_batch: num_rows is needed with q_starts")
+    b = Batch(_tensor(block_table, "make_batch", torch.int32, 0, dev), _tensor(seq_lens, "make_batch", torch.int32, S, dev),
+              None if q_starts is None else _tensor(q_starts, "make_batch", torch.int32, S + 1, dev), S,
+              block_table.shape[1], S if num_rows is None else num_rows, max_q_len)
+    b.device, b.keep = dev, (block_table, seq_lens, q_starts)
+    return b
+
+
+def make_rotation(q_norm=None, k_norm=None, norm_eps: float = 1e-6, inv_freq=None, positions=None, rot_dim: int = 0,
+                  interleaved: bool = False) -> Rotation:
+    """q_norm, k_norm: [head_dim] in the element type, or None; inv_freq: float64 [rot_dim / 2], or None; positions:
+    int32 [num_rows], or None (the cache index).  Keeps the tensors."""
+    import torch
+
+    given = [t for t in (q_norm, k_norm, inv_freq, positions) if t is not None]
+    dev = given[0].device if given else None
+    r = Rotation(None if q_norm is None else _tensor(q_norm, "make_rotation", q_norm.dtype, 1, dev),
+                 None if k_norm is None else _tensor(k_norm, "make_rotation", k_norm.dtype, 1, dev),
+                 None if inv_freq is None else _tensor(inv_freq, "make_rotation", torch.float64, rot_dim // 2, dev),
+                 None if positions is None else _tensor(positions, "make_rotation", torch.int32, 0, dev),
+                 norm_eps, rot_dim, int(interleaved), 0)
+    r.device, r.keep = dev, (q_norm, k_norm, inv_freq, positions)
+    return r
+
+
+def _launch(fn, where: str, device, stream, *args) -> None:
+    """Calls fn(*args, stream) with `device` current."""
+    import torch
+
+    if device.type != "cuda":
+        raise AmoebaError(ERR_INVALID_ARG, f"{where}: the tensors are on {device}")
+    handle = torch.cuda.current_stream(device).cuda_stream if stream is None else _stream(stream)
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, handle)
+    _check(status, where)
+
+
+def _layer_bytes(layout: Layout) -> int:
+    m = layout.model
+    return layout.kv_layer_stride_bytes or (layout.num_blocks * (m.num_kv_heads // max(layout.tp, 1)) * 2 *
+                                            layout.block_tokens * m.head_dim * m.elem_bytes)
+
+
+def amoeba_append_kv(layout: Layout, dtype: int, layer: int, pools: Sequence, batch: Batch, q, k: Sequence, v: Sequence,
+                     rotation: Optional[Rotation], q_out, status, stream=None) -> None:
+    """Normalises and turns the new queries (into q_out) and keys and writes keys and values into layer `layer` of the
+    pools.  q, k, v, q_out: one [num_rows, heads of the worker * head_dim] tensor per worker, row strides as they are;
+    q and q_out may both be None."""
+    import torch
+
+    w, dev, m, rows = "amoeba_append_kv", batch.device, layout.model, batch.num_rows
+    dt = _torch_dtype(dtype, w)
+    D, tp = m.head_dim, max(layout.tp, 1)
+    kw, qw = m.num_kv_heads // tp * D, m.num_q_heads // tp * D
+    pp = _pools(layout, pools, _layer_bytes(layout) * (layer + 1), w, dev)
+    kp, ks = _row_buffers(layout, k, rows, kw, dt, w, dev)
+    vp, vs = _row_buffers(layout, v, rows, kw, dt, w, dev)
+    qp = op = None
+    qs = os_ = 0
+    if q is not None:
+        qp, qs = _row_buffers(layout, q, rows, qw, dt, w, dev)
+    if q_out is not None:
+        op, os_ = _row_buffers(layout, q_out, rows, qw, dt, w, dev)
+    if rotation is not None:
+        for t, n, want in zip(rotation.keep, (D, D, 0, rows), (dt, dt, torch.float64, torch.int32)):
+            if t is not None and (t.dtype != want or t.numel() < n or t.device != dev):
+                raise AmoebaError(ERR_INVALID_ARG, f"{w}: norm weights are {dt} [{D}], positions int32 [{rows}], on {dev}")
+    _launch(_load().amoeba_append_kv, w, dev, stream, C.byref(layout), dtype, layer, pp, C.byref(batch), qp, qs, kp, ks,
+            vp, vs, None if rotation is None else C.byref(rotation), op, os_, _tensor(status, w, torch.int32, 1, dev))
+
+
+def amoeba_attend_workspace_bytes(layout: Layout, batch: Batch) -> int:
+    out = C.c_int64()
+    _check(_load().amoeba_attend_workspace_bytes(C.byref(layout), C.byref(batch), C.byref(out)),
+           "amoeba_attend_workspace_bytes")
+    return out.value
+
+
+def amoeba_attend(layout: Layout, dtype: int, layer: int, pools: Sequence, batch: Batch, q: Sequence, scale: float,
+                  window: int, out: Sequence, lse, status, workspace, stream=None) -> None:
+    """Attention of the batch's rows over layer `layer` of the cache.  q, out: one [num_rows, query heads of the worker *
+    head_dim] tensor per worker; lse: float32 [num_rows, num_q_heads] or None; window: 0 = every earlier token."""
+    import torch
+
+    w, dev, m, rows = "amoeba_attend", batch.device, layout.model, batch.num_rows
+    dt = _torch_dtype(dtype, w)
+    width = m.num_q_heads // max(layout.tp, 1) * m.head_dim
+    pp = _pools(layout, pools, _layer_bytes(layout) * (layer + 1), w, dev)
+    qp, qs = _row_buffers(layout, q, rows, width, dt, w, dev)
+    op, os_ = _row_buffers(layout, out, rows, width, dt, w, dev)
+    _launch(_load().amoeba_attend, w, dev, stream, C.byref(layout), dtype, layer, pp, C.byref(batch), qp, qs, scale,
+            window, op, os_, None if lse is None else _tensor(lse, w, torch.float32, rows * m.num_q_heads, dev),
+            _tensor(status, w, torch.int32, 1, dev), _tensor(workspace, w, torch.uint8, 0, dev), workspace.numel())
+
+
+def amoeba_accumulate_scores(layout: Layout, dtype: int, layer: int, pools: Sequence, batch: Batch, q: Sequence,
+                             scale: float, window: int, lse, scored_lens, score_pools: Sequence, status,
+                             stream=None) -> None:
+    """Adds the attention weight that the cached tokens get from the batch's rows to layer `layer` of the score pools
+    (float32, one [num_layers, num_blocks, key heads of the worker, block_tokens] tensor per worker).  lse: amoeba_attend's
+    for the same rows; scored_lens: int32 [num_seqs], how many tokens have a score already, or None."""
+    import torch
+
+    w, dev, m, rows = "amoeba_accumulate_scores", batch.device, layout.model, batch.num_rows
+    dt = _torch_dtype(dtype, w)
+    tp = max(layout.tp, 1)
+    pp = _pools(layout, pools, _layer_bytes(layout) * (layer + 1), w, dev)
+    sp = _score_pools(layout, score_pools, layer + 1, w, dev)
+    qp, qs = _row_buffers(layout, q, rows, m.num_q_heads // tp * m.head_dim, dt, w, dev)
+    _launch(_load().amoeba_accumulate_scores, w, dev, stream, C.byref(layout), dtype, layer, pp, C.byref(batch), qp, qs,
+            scale, window, _tensor(lse, w, torch.float32, rows * m.num_q_heads, dev),
+            None if scored_lens is None else _tensor(scored_lens, w, torch.int32, batch.num_seqs, dev), sp,
+            _tensor(status, w, torch.int32, 1, dev))
+
+
+def _score_pools(layout: Layout, score_pools, layers: int, where: str, device):
+    import torch
+
+    if any(p.dtype != torch.float32 for p in score_pools):
+        raise AmoebaError(ERR_INVALID_ARG, f"{where}: score pools are float32")
+    n = layout.num_blocks * (layout.model.num_kv_heads // max(layout.tp, 1)) * layout.block_tokens * 4
+    return _pools(layout, score_pools, n * layers, where, device)
+
+
+def amoeba_evict_workspace_bytes(layout: Layout, num_layers: int, num_seqs: int, budget: int) -> int:
+    out = C.c_int64()
+    _check(_load().amoeba_evict_workspace_bytes(C.byref(layout), num_layers, num_seqs, budget, C.byref(out)),
+           "amoeba_evict_workspace_bytes")
+    return out.value
+
+
+def amoeba_evict_kv(layout: Layout, layer_begin: int, layer_end: int, pools: Sequence, score_pools, src_bt, seq_lens,
+                    dst_bt, budget: int, recent: int, new_lens, status, workspace, stream=None) -> None:
+    """Cuts the sequences to `budget` tokens, the last `recent` and those with the highest scores, in layers [layer_begin,
+    layer_end) of the pools.  src_bt, dst_bt: int32 [num_seqs, blocks]; dst_bt may be src_bt (in place).  score_pools may
+    be None if recent == budget."""
+    import torch
+
+    w, dev, S = "amoeba_evict_kv", seq_lens.device, seq_lens.numel()
+    if src_bt.dim() != 2 or dst_bt.dim() != 2 or src_bt.shape[0] != S or dst_bt.shape[0] != S:
+        raise AmoebaError(ERR_INVALID_ARG, f"{w}: block tables are [num_seqs, blocks]")
+    pp = _pools(layout, pools, _layer_bytes(layout) * layer_end, w, dev)
+    sp = None if score_pools is None else _score_pools(layout, score_pools, layer_end, w, dev)
+    _launch(_load().amoeba_evict_kv, w, dev, stream, C.byref(layout), layer_begin, layer_end, pp, sp,
+            _tensor(src_bt, w, torch.int32, 0, dev), _tensor(seq_lens, w, torch.int32, S, dev), S, src_bt.shape[1],
+            _tensor(dst_bt, w, torch.int32, 0, dev), dst_bt.shape[1], budget, recent,
+            _tensor(new_lens, w, torch.int32, S, dev), _tensor(status, w, torch.int32, 1, dev),
+            _tensor(workspace, w, torch.uint8, 0, dev), workspace.numel())
 
 
 def amoeba_launch_count() -> int:

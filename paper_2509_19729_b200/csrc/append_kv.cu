@@ -1,0 +1,185 @@
+// amoeba_append_kv: norms of queries and keys per head, rotation by position and the write into the paged cache.
+//
+// Memory-bound: every element of q, k and v is read once and written once, (Hq + 2 Hkv) * head_dim * 4 bytes a token.
+// A head's vector lies in head_dim / 8 neighbouring lanes, 16 bytes each, so that the norm's sum and the partner of a
+// rotated pair are shuffles; the angles of a token are computed once per block, in 64 bits, for all its heads.
+#include "cache_view.cuh"
+
+namespace amoeba {
+
+constexpr int kAppendThreads = 256;
+
+struct AppendParams {
+    CacheView cache;
+    Batch batch;
+    Rows q, k, v, q_out;
+    const void *q_norm, *k_norm;
+    const double* inv_freq;
+    const int32_t* positions;
+    int32_t* status;
+    float eps;
+    int32_t rot, interleaved, q_heads;  // q_heads: query heads per worker, 0 = none are given
+    int32_t tp;
+};
+
+// The sequence that row belongs to (the one s with starts[s] <= row < starts[s+1]), or -1; for the whole block.
+__device__ __forceinline__ int find_sequence(const Batch& b, int row, int* shared) {
+    if (!b.starts) return row < b.num_seqs ? row : -1;
+    if (threadIdx.x == 0) *shared = -1;
+    __syncthreads();
+    for (int s = threadIdx.x; s < b.num_seqs; s += blockDim.x)
+        if (b.starts[s] <= row && row < b.starts[s + 1]) *shared = s;
+    __syncthreads();
+    return *shared;
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kAppendThreads) append_kv(const __grid_constant__ AppendParams p) {
+    constexpr int kLanes = D / 8;  // lanes per head
+    __shared__ float s_cos[64], s_sin[64];
+    __shared__ int s_seq;
+    const int row = blockIdx.x;
+    const int s = find_sequence(p.batch, row, &s_seq);
+    if (s < 0) return;
+    const Seq seq = sequence(p.batch, s, p.cache.block_tokens);
+    if (!seq.ok || seq.qn > seq.len) {
+        if (threadIdx.x == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
+        return;
+    }
+    const int index = seq.len - seq.qn + (row - seq.q0);
+    const int block = p.batch.table[(int64_t)s * p.batch.max_blocks + index / p.cache.block_tokens];
+    const bool cached = block >= 0 && block < p.cache.num_blocks;
+    if (!cached && threadIdx.x == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
+    const int half = p.rot / 2;
+    if (p.inv_freq) {
+        if (threadIdx.x < half) {
+            const double turn = 6.283185307179586476925;
+            double a = (double)(p.positions ? p.positions[row] : index) * p.inv_freq[threadIdx.x];
+            a -= turn * rint(a / turn);
+            sincosf((float)a, &s_sin[threadIdx.x], &s_cos[threadIdx.x]);
+        }
+        __syncthreads();
+    }
+    const int64_t slot = (int64_t)block * p.cache.block_stride + (index % p.cache.block_tokens) * p.cache.tok_stride;
+    const int lane = threadIdx.x % kLanes;
+    const int per_worker = p.q_heads + 2 * p.cache.heads;
+    const int n = p.tp * per_worker;
+    // whole warps go round together: the shuffles below need all their lanes
+    for (int first = threadIdx.x / 32 * (32 / kLanes); first < n; first += kAppendThreads / kLanes) {
+        const int vec = first + threadIdx.x % 32 / kLanes;
+        const bool there = vec < n;
+        const int r = there ? vec / per_worker : 0, h = there ? vec - r * per_worker : 0;
+        const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.cache.heads;
+        const int head = is_q ? h : is_v ? h - p.q_heads - p.cache.heads : h - p.q_heads;
+        const Rows& from = is_q ? p.q : is_v ? p.v : p.k;
+        uint4 raw = make_uint4(0, 0, 0, 0);
+        if (there) raw = *reinterpret_cast<const uint4*>(from.base[r] + row * from.stride + head * (D * 2) + lane * 16);
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = Elem<T>::unpack(w[i]);
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        }
+        const void* norm = is_q ? p.q_norm : p.k_norm;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
+#pragma unroll
+        for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+        if (norm && !is_v) {
+            const float inv = 1.f / sqrtf(sum * (1.f / D) + p.eps);
+            const uint4 nw = reinterpret_cast<const uint4*>(norm)[lane];
+            const uint32_t g[4] = {nw.x, nw.y, nw.z, nw.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = Elem<T>::unpack(g[i]);
+                x[2 * i] *= inv * f.x, x[2 * i + 1] *= inv * f.y;
+            }
+        }
+        if (p.inv_freq) {  // block-uniform
+            if (p.interleaved) {
+                if (lane * 8 < p.rot && !is_v) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float c = s_cos[lane * 4 + i], sn = s_sin[lane * 4 + i], a = x[2 * i], b = x[2 * i + 1];
+                        x[2 * i] = a * c - b * sn, x[2 * i + 1] = b * c + a * sn;
+                    }
+                }
+            } else {
+                const int hl = half / 8;  // lanes per half
+                const bool second = lane >= hl;
+                const int partner = lane >= 2 * hl ? lane : second ? lane - hl : lane + hl;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float other = __shfl_sync(~0u, x[i], partner, kLanes);
+                    if (lane < 2 * hl && !is_v) {
+                        const int j = (second ? lane - hl : lane) * 8 + i;
+                        x[i] = second ? x[i] * s_cos[j] + other * s_sin[j] : x[i] * s_cos[j] - other * s_sin[j];
+                    }
+                }
+            }
+        }
+        if (!there) continue;
+        uint4 out = raw;  // values go as they are
+        if (!is_v)
+            out = make_uint4(Elem<T>::pack(x[0], x[1]), Elem<T>::pack(x[2], x[3]), Elem<T>::pack(x[4], x[5]),
+                             Elem<T>::pack(x[6], x[7]));
+        if (is_q)
+            *reinterpret_cast<uint4*>(p.q_out.base[r] + row * p.q_out.stride + head * (D * 2) + lane * 16) = out;
+        else if (cached)
+            *reinterpret_cast<uint4*>(p.cache.pools[r] + slot + head * p.cache.head_stride +
+                                      (is_v ? p.cache.kv_stride : 0) + lane * 16) = out;
+    }
+}
+
+}  // namespace amoeba
+
+using namespace amoeba;
+
+extern "C" amoeba_status amoeba_append_kv(const amoeba_layout* layout, int32_t dtype, int32_t layer, void* const* pools,
+                                          const amoeba_batch* batch, const void* const* q, int64_t q_stride,
+                                          const void* const* k, int64_t k_stride, const void* const* v,
+                                          int64_t v_stride, const amoeba_rotation* rotation, void* const* q_out,
+                                          int64_t q_out_stride, int32_t* d_status, void* cuda_stream) {
+    AppendParams p{};
+    amoeba_status st;
+    if ((st = check_elements(layout, dtype)) != AMOEBA_OK) return st;
+    if ((st = make_cache_view(layout, layer, pools, &p.cache)) != AMOEBA_OK) return st;
+    if ((st = make_batch(batch, &p.batch)) != AMOEBA_OK) return st;
+    if (!d_status || (q == nullptr) != (q_out == nullptr)) return AMOEBA_ERR_INVALID_ARG;
+    const int D = layout->model.head_dim;
+    p.tp = layout->tp;
+    p.q_heads = q ? layout->model.num_q_heads / layout->tp : 0;
+    if ((st = make_rows(layout, k, k_stride, (int64_t)p.cache.heads * D, &p.k)) != AMOEBA_OK) return st;
+    if ((st = make_rows(layout, v, v_stride, (int64_t)p.cache.heads * D, &p.v)) != AMOEBA_OK) return st;
+    if (q) {
+        if ((st = make_rows(layout, q, q_stride, (int64_t)p.q_heads * D, &p.q)) != AMOEBA_OK) return st;
+        if ((st = make_rows(layout, q_out, q_out_stride, (int64_t)p.q_heads * D, &p.q_out)) != AMOEBA_OK) return st;
+        for (int r = 0; r < layout->tp; ++r)  // in place only row by row
+            if (p.q.base[r] == p.q_out.base[r] && p.q.stride != p.q_out.stride) return AMOEBA_ERR_INVALID_ARG;
+    }
+    p.status = d_status;
+    if (rotation) {
+        p.q_norm = rotation->d_q_norm;
+        p.k_norm = rotation->d_k_norm;
+        p.eps = rotation->norm_eps;
+        if (((uintptr_t)p.q_norm | (uintptr_t)p.k_norm) % 16) return AMOEBA_ERR_ALIGNMENT;
+        if (rotation->d_inv_freq) {
+            if (rotation->rot_dim <= 0 || rotation->rot_dim > D || rotation->rot_dim % 16 ||
+                (rotation->interleaved != 0 && rotation->interleaved != 1))
+                return AMOEBA_ERR_INVALID_ARG;
+            p.inv_freq = rotation->d_inv_freq;
+            p.positions = rotation->d_positions;
+            p.rot = rotation->rot_dim;
+            p.interleaved = rotation->interleaved;
+        }
+    }
+    if (p.batch.num_seqs == 0 || p.batch.num_rows == 0) return AMOEBA_OK;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const int rows = p.batch.starts ? p.batch.num_rows : std::min(p.batch.num_rows, p.batch.num_seqs);
+    auto* kernel = dtype == AMOEBA_FP16 ? (D == 64 ? append_kv<__half, 64> : append_kv<__half, 128>)
+                                        : (D == 64 ? append_kv<__nv_bfloat16, 64> : append_kv<__nv_bfloat16, 128>);
+    kernel<<<rows, kAppendThreads, 0, stream>>>(p);
+    return launch_result();
+}

@@ -1,0 +1,407 @@
+// amoeba_attend: attention of a ragged chunk of new tokens over the paged cache.
+//
+// One unit of work is a (sequence, key head, tile of query rows), the rows of a unit being the new tokens times the
+// query heads that share the key head, so that grouped heads read their keys once.  The softmax runs along the tokens
+// with a running maximum and sum per row; units are cut where the shares of the CTAs end (walk.cuh), and the cut ones
+// are joined by their maxima and sums in a second small launch.
+#include "walk.cuh"
+#include "warp_mma.cuh"
+
+namespace amoeba {
+
+struct AttendParams {
+    CacheView cache;
+    Batch batch;
+    Rows q, out;
+    Shape shape;
+    float* lse;
+    int32_t* status;
+    int64_t* prefix;         // [num_seqs + 1]: first tile of every sequence
+    float *part_o, *part_m, *part_l;  // of the cut units: [2 * CTAs][rows][D], [2 * CTAs][rows]
+    float scale_log2;        // scale * log2(e): the softmax runs in powers of two
+    int32_t q_heads;         // of all workers
+    int32_t whole;           // 1: one CTA per unit, nothing is cut
+    int32_t max_row_tiles;
+};
+
+// Where row r of a unit lies in a row buffer.
+template <int D>
+__device__ __forceinline__ char* row_of(const Rows& rows, const AttendParams& p, const Seq& q, int kv_head, int r) {
+    const int w = kv_head / p.cache.heads, h = kv_head - w * p.cache.heads, g = p.shape.group;
+    const int tok = r / g;
+    return rows.base[w] + (int64_t)(q.q0 + tok) * rows.stride + (h * g + r - tok * g) * (D * 2);
+}
+__device__ __forceinline__ float* lse_of(const AttendParams& p, const Seq& q, int kv_head, int r) {
+    const int g = p.shape.group, tok = r / g;
+    return p.lse + (int64_t)(q.q0 + tok) * p.q_heads + kv_head * g + r - tok * g;
+}
+
+// ------------------------------------------------------------------------------------------------ few rows
+// Up to 8*NT rows a unit.  Bound by the bytes of the cache: 2 * 2 * D a token and key head against at most 32 rows of
+// arithmetic, which warp-level matrix instructions do in a fraction of the time.  Every warp works alone on every
+// fourth run of 16 tokens, with its own ring of asynchronous loads and its own running maximum, sum and output, so
+// that nothing but the end of a unit makes warps wait for one another.  The product is formed the other way round, S^T = K Q^T
+// and O^T = V^T P^T: then 8 rows fill a matrix instruction, where 16 would be needed the usual way.
+constexpr int kFewThreads = 128, kFewWarps = 4, kFewTile = 16 * kFewWarps;
+template <int D, int NT>
+struct FewShape {
+    static constexpr int kStage = 2 * 16 * D * 2;  // 16 tokens' keys and values
+    static constexpr int kMerge = kFewWarps * 8 * NT * (D + 4) * 4;
+    static constexpr int kCtas = NT * D > 128 ? 1 : 2;  // per SM
+    static constexpr int kStages = D == 64 ? 4 : NT == 1 ? 3 : NT == 2 ? 6 : 4;
+    static constexpr int kSmem = kFewWarps * kStages * kStage + kMerge;
+};
+
+template <class T, int D, int NT>
+__global__ void __launch_bounds__(kFewThreads, FewShape<D, NT>::kCtas)
+attend_few(const __grid_constant__ AttendParams p) {
+    using F = FewShape<D, NT>;
+    constexpr int R = 8 * NT, kSteps = D / 16, kPitch = D + 4;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ uint32_t s_mask[kFewWarps][F::kStages];
+    __shared__ float s_m[kFewWarps][R], s_l[kFewWarps][R];
+    float* s_o = reinterpret_cast<float*>(smem + kFewWarps * F::kStages * F::kStage);
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int quad = lane / 4, pair = lane % 4;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * F::kStages * F::kStage;
+    const Shape& sh = p.shape;
+
+    Walk walk;
+    int64_t n;
+    if (p.whole) {
+        const int unit = blockIdx.x, m = unit % p.max_row_tiles, h = unit / p.max_row_tiles % sh.kv_heads;
+        walk.open(sh, p.batch, p.cache.block_tokens, unit / (p.max_row_tiles * sh.kv_heads));
+        if (!walk.seq.ok && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
+        if (m >= walk.nm) return;
+        walk.h = h, walk.m = m;
+        walk.range = row_tile_range(sh, walk.seq, m);
+        n = walk.range.tiles;
+    } else {
+        int64_t total;
+        int ctas;
+        n = take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &total, &ctas, 1, p.prefix, p.status);
+    }
+    if (n == 0) return;
+
+    Walk ahead = walk;
+    int64_t to_load = n;
+    int slot_in = 0, slot = 0;
+    auto load = [&] {
+        if (to_load > 0) {
+            const int key0 = ahead.range.base + ahead.t * kFewTile + warp * 16;
+            const uint32_t mask = load16<D, true>(p.cache, p.batch.table + (int64_t)ahead.s * p.batch.max_blocks,
+                                                  p.cache.head_base(ahead.h), key0, ahead.range.lo, ahead.range.hi,
+                                                  ring + slot_in * F::kStage, p.status);
+            if (lane == 0) s_mask[warp][slot_in] = mask;
+            if (--to_load > 0) ahead.next(sh, p.batch, p.cache.block_tokens);
+        }
+        cp_async_commit();
+        slot_in = slot_in + 1 == F::kStages ? 0 : slot_in + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < F::kStages - 1; ++i) load();
+
+    uint32_t qf[NT][kSteps][2];     // Q^T, the right operand of S^T = K Q^T
+    int see_lo[NT][2], see_hi[NT][2];  // tokens that this lane's rows see: [lo, hi)
+    float m_run[NT][2], l_run[NT][2], o[NT][kSteps][4];
+    bool fresh = true;
+    bool from_start = false;  // of the unit, in this CTA
+
+    for (; n > 0; --n) {
+        if (fresh) {
+            fresh = false;
+            from_start = walk.t == 0;
+            const int rows = walk.seq.qn * sh.group, first = walk.m * R;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int r = first + t * 8 + quad;
+                const bool there = r < rows;
+                const char* src = there ? row_of<D>(p.q, p, walk.seq, walk.h, r) : nullptr;
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        qf[t][j][b] = there ? *reinterpret_cast<const uint32_t*>(src + (j * 16 + b * 8 + pair * 2) * 2) : 0u;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int rr = first + t * 8 + pair * 2 + b;
+                    const int pos = walk.seq.len - walk.seq.qn + rr / sh.group;
+                    see_hi[t][b] = rr < rows ? pos + 1 : 0;
+                    see_lo[t][b] = sh.window > 0 ? pos - sh.window + 1 : 0;
+                    m_run[t][b] = -INFINITY;
+                    l_run[t][b] = 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[t][j][i] = 0.f;
+            }
+        }
+        cp_async_wait<F::kStages - 2>();
+        __syncwarp();
+        load();  // into the slot that the last round has read
+        const uint32_t k_smem = ring + slot * F::kStage, v_smem = k_smem + 16 * D * 2;
+        const uint32_t mask = s_mask[warp][slot];
+        slot = slot + 1 == F::kStages ? 0 : slot + 1;
+
+        float st[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) st[t][0] = st[t][1] = st[t][2] = st[t][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            uint32_t a[4];
+            ldmatrix4(a, k_smem + swizzled<D>(lane % 16, 2 * j + lane / 16));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816<T>(st[t], a, qf[t][j][0], qf[t][j][1]);
+        }
+        // st[t]: tokens quad and quad + 8, rows 2*pair and 2*pair + 1
+        const int key0 = walk.range.base + walk.t * kFewTile + warp * 16 + quad;
+        uint32_t pf[NT][2];
+        bool grew = false;
+        float alpha[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = key0 + (i / 2) * 8;
+                const bool sees = (mask >> (quad + (i / 2) * 8) & 1u) && key < see_hi[t][i % 2] && key >= see_lo[t][i % 2];
+                st[t][i] = sees ? st[t][i] * p.scale_log2 : -INFINITY;
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float top = fmaxf(st[t][b], st[t][b + 2]);
+                top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+                top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+                top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+                const float m_new = fmaxf(m_run[t][b], top);
+                grew |= m_new > m_run[t][b];
+                const float ref = m_new == -INFINITY ? 0.f : m_new;
+                alpha[t][b] = fast_exp2(m_run[t][b] - ref);
+                m_run[t][b] = m_new;
+                st[t][b] = fast_exp2(st[t][b] - ref);
+                st[t][b + 2] = fast_exp2(st[t][b + 2] - ref);
+                l_run[t][b] = l_run[t][b] * alpha[t][b] + st[t][b] + st[t][b + 2];
+            }
+            pf[t][0] = transpose8x8(Elem<T>::pack(st[t][0], st[t][1]));
+            pf[t][1] = transpose8x8(Elem<T>::pack(st[t][2], st[t][3]));
+        }
+        if (__any_sync(~0u, grew)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[t][j][i] *= alpha[t][i % 2];
+        }
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            uint32_t a[4];
+            ldmatrix4_trans(a, v_smem + swizzled<D>(lane % 8 + lane / 16 * 8, 2 * j + lane / 8 % 2));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816<T>(o[t][j], a, pf[t][0], pf[t][1]);
+        }
+
+        const bool unit_ends = walk.t + 1 == walk.range.tiles;
+        if (!unit_ends && n > 1) {
+            ++walk.t;
+            continue;
+        }
+        // The unit, or this CTA's part of it, ends: join the four warps.
+        fresh = true;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float l = l_run[t][b];
+                l += __shfl_xor_sync(~0u, l, 4);
+                l += __shfl_xor_sync(~0u, l, 8);
+                l += __shfl_xor_sync(~0u, l, 16);
+                const int r = t * 8 + pair * 2 + b;
+                if (quad == 0) s_m[warp][r] = m_run[t][b], s_l[warp][r] = l;
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) {
+                    float* to = s_o + (warp * R + r) * kPitch + j * 16 + quad;
+                    to[0] = o[t][j][b];
+                    to[8] = o[t][j][b + 2];
+                }
+            }
+        __syncthreads();
+        const int rows = min(R, walk.seq.qn * sh.group - walk.m * R);
+        const bool direct = from_start && unit_ends;
+        const int64_t part = (int64_t)(2 * blockIdx.x + (from_start ? 1 : 0)) * R;
+        for (int i = tid; i < rows * (D / 4); i += kFewThreads) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4;
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) top = fmaxf(top, s_m[w][r]);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float l = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) {
+                const float f = fast_exp2(s_m[w][r] - ref);
+                const float4 x = *reinterpret_cast<const float4*>(s_o + (w * R + r) * kPitch + d);
+                l += f * s_l[w][r];
+                acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
+            }
+            if (direct) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const int row = walk.m * R + r;
+                *reinterpret_cast<uint2*>(row_of<D>(p.out, p, walk.seq, walk.h, row) + d * 2) =
+                    make_uint2(Elem<T>::pack(acc.x * inv, acc.y * inv), Elem<T>::pack(acc.z * inv, acc.w * inv));
+                if (d == 0 && p.lse) *lse_of(p, walk.seq, walk.h, row) = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+            } else {
+                *reinterpret_cast<float4*>(p.part_o + (part + r) * D + d) = acc;
+                if (d == 0) p.part_m[part + r] = top, p.part_l[part + r] = l;
+            }
+        }
+        __syncthreads();
+        if (n > 1) walk.next(sh, p.batch, p.cache.block_tokens);
+    }
+}
+
+// Joins the parts of the units that were cut: one CTA per unit.
+template <class T, int D>
+__global__ void __launch_bounds__(128) attend_join(const __grid_constant__ AttendParams p, int max_ctas) {
+    const Shape& sh = p.shape;
+    const int unit = blockIdx.x, m = unit % p.max_row_tiles, h = unit / p.max_row_tiles % sh.kv_heads;
+    const int s = unit / (p.max_row_tiles * sh.kv_heads);
+    const Seq q = sequence(p.batch, s, p.cache.block_tokens);
+    if (m >= row_tiles(sh, q)) return;
+    const int64_t total = p.prefix[p.batch.num_seqs];
+    const int ctas = (int)max((int64_t)1, min((int64_t)max_ctas, total));
+    int64_t first = p.prefix[s], per_head = 0;
+    int n = 0;
+    for (int i = 0; i < row_tiles(sh, q); ++i) {
+        const int k = row_tile_range(sh, q, i).tiles;
+        if (i < m) first += k;
+        if (i == m) n = k;
+        per_head += k;
+    }
+    first += h * per_head;
+    const int c0 = share_of(total, ctas, first), c1 = share_of(total, ctas, first + n - 1);
+    if (c0 == c1) return;
+    const int R = sh.rows, rows = min(R, q.qn * sh.group - m * R);
+    for (int i = threadIdx.x; i < rows * (D / 4); i += blockDim.x) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        float top = -INFINITY;
+        for (int c = c0; c <= c1; ++c) top = fmaxf(top, p.part_m[(int64_t)(2 * c + (c == c0)) * R + r]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float l = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c = c0; c <= c1; ++c) {
+            const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
+            const float f = fast_exp2(p.part_m[part] - ref);
+            const float4 x = *reinterpret_cast<const float4*>(p.part_o + part * D + d);
+            l += f * p.part_l[part];
+            acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int row = m * R + r;
+        *reinterpret_cast<uint2*>(row_of<D>(p.out, p, q, h, row) + d * 2) =
+            make_uint2(Elem<T>::pack(acc.x * inv, acc.y * inv), Elem<T>::pack(acc.z * inv, acc.w * inv));
+        if (d == 0 && p.lse) *lse_of(p, q, h, row) = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+    }
+}
+
+constexpr int kMaxFewCtas = 384;  // two for each of up to 192 SMs: bounds the workspace without asking the device
+constexpr int kMaxFewRows = 32;
+
+static int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
+
+struct Workspace {
+    int64_t prefix, part_o, part_m, part_l, bytes;
+};
+static Workspace attend_workspace(const amoeba_layout* l, int32_t num_seqs) {
+    Workspace w;
+    const int64_t parts = 2 * kMaxFewCtas * kMaxFewRows;
+    w.prefix = 0;
+    w.part_o = align16((num_seqs + 1) * 8);
+    w.part_m = w.part_o + parts * l->model.head_dim * 4;
+    w.part_l = w.part_m + parts * 4;
+    w.bytes = w.part_l + parts * 4;
+    return w;
+}
+
+template <class T, int D, int NT>
+static amoeba_status run_few(AttendParams& p, int sms, cudaStream_t stream) {
+    using F = FewShape<D, NT>;
+    p.shape.rows = 8 * NT;
+    p.shape.tile = kFewTile;
+    p.max_row_tiles = (int)(((int64_t)p.batch.max_q_len * p.shape.group + 8 * NT - 1) / (8 * NT));
+    const int64_t units = (int64_t)p.batch.num_seqs * p.shape.kv_heads * p.max_row_tiles;
+    if (units > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
+    if (ensure_dynamic_smem((const void*)attend_few<T, D, NT>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    const int ctas = std::min(F::kCtas * sms, kMaxFewCtas);
+    attend_few<T, D, NT><<<p.whole ? (int)units : ctas, kFewThreads, F::kSmem, stream>>>(p);
+    amoeba_status st = launch_result();
+    if (st != AMOEBA_OK || p.whole) return st;
+    attend_join<T, D><<<(int)units, 128, 0, stream>>>(p, ctas);
+    return launch_result();
+}
+
+template <class T, int D>
+static amoeba_status run_attend(AttendParams& p, int sms, cudaStream_t stream) {
+    const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
+    if (rows <= 8) return run_few<T, D, 1>(p, sms, stream);
+    if (rows <= 16) return run_few<T, D, 2>(p, sms, stream);
+    return run_few<T, D, 4>(p, sms, stream);
+}
+
+}  // namespace amoeba
+
+using namespace amoeba;
+
+extern "C" amoeba_status amoeba_attend_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
+                                                       int64_t* bytes) {
+    int64_t pool = 0;
+    if (!layout || !batch || !bytes || batch->num_seqs < 0) return AMOEBA_ERR_INVALID_ARG;
+    const amoeba_status st = amoeba_layout_kv_pool_bytes(layout, &pool);
+    if (st != AMOEBA_OK) return st;
+    *bytes = attend_workspace(layout, batch->num_seqs).bytes;
+    return AMOEBA_OK;
+}
+
+extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtype, int32_t layer,
+                                       const void* const* pools, const amoeba_batch* batch, const void* const* q,
+                                       int64_t q_stride, float scale, int32_t window, void* const* out,
+                                       int64_t out_stride, float* d_lse, int32_t* d_status, void* d_workspace,
+                                       int64_t workspace_bytes, void* cuda_stream) {
+    AttendParams p{};
+    amoeba_status st;
+    if ((st = check_elements(layout, dtype)) != AMOEBA_OK) return st;
+    if ((st = make_cache_view(layout, layer, pools, &p.cache)) != AMOEBA_OK) return st;
+    if ((st = make_batch(batch, &p.batch)) != AMOEBA_OK) return st;
+    if (!d_status || window < 0) return AMOEBA_ERR_INVALID_ARG;
+    const amoeba_model& m = layout->model;
+    const int64_t row = (int64_t)m.num_q_heads / layout->tp * m.head_dim;
+    if ((st = make_rows(layout, q, q_stride, row, &p.q)) != AMOEBA_OK) return st;
+    if ((st = make_rows(layout, out, out_stride, row, &p.out)) != AMOEBA_OK) return st;
+    for (int r = 0; r < layout->tp; ++r)
+        if (q[r] == out[r]) return AMOEBA_ERR_INVALID_ARG;
+    const Workspace w = attend_workspace(layout, p.batch.num_seqs);
+    if (!d_workspace || workspace_bytes < w.bytes) return AMOEBA_ERR_INVALID_ARG;
+    if ((uintptr_t)d_workspace % 16) return AMOEBA_ERR_ALIGNMENT;
+    if (p.batch.num_seqs == 0 || p.batch.num_rows == 0 || p.batch.max_q_len == 0) return AMOEBA_OK;
+    p.lse = d_lse;
+    p.status = d_status;
+    char* ws = static_cast<char*>(d_workspace);
+    p.prefix = reinterpret_cast<int64_t*>(ws + w.prefix);
+    p.part_o = reinterpret_cast<float*>(ws + w.part_o);
+    p.part_m = reinterpret_cast<float*>(ws + w.part_m);
+    p.part_l = reinterpret_cast<float*>(ws + w.part_l);
+    p.scale_log2 = scale * kLog2e;
+    p.q_heads = m.num_q_heads;
+    p.shape.group = m.num_q_heads / m.num_kv_heads;
+    p.shape.kv_heads = m.num_kv_heads;
+    p.shape.window = std::min(window, 1 << 30);
+    p.shape.min_rows = 0;
+    p.shape.max_rows = INT32_MAX;
+    const DeviceInfo dev = cached_device_info();
+    if (!dev.sms) return AMOEBA_ERR_CUDA;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (dtype == AMOEBA_FP16)
+        return m.head_dim == 64 ? run_attend<__half, 64>(p, dev.sms, stream) : run_attend<__half, 128>(p, dev.sms, stream);
+    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, dev.sms, stream)
+                            : run_attend<__nv_bfloat16, 128>(p, dev.sms, stream);
+}

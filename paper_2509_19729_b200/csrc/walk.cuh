@@ -1,0 +1,175 @@
+// How the operators that read the cache share the work out.
+//
+// A unit is one (sequence, key head, tile of query rows); its work is a run of tiles of consecutive tokens.  All units'
+// tiles are laid end to end in the order (sequence, head, row tile), and every CTA takes an equal run of them, wherever
+// it begins and ends: one very long sequence is spread over as many CTAs as its share of the work, and a batch of any
+// mix finishes together.  The lengths are known only on the device, so every CTA adds them up for itself; there is no
+// planning launch and nothing for the host to know.
+#pragma once
+#include "cache_view.cuh"
+
+namespace amoeba {
+
+struct Shape {  // what the split depends on, besides the batch
+    int32_t group;      // query heads per key head
+    int32_t kv_heads;   // of all workers
+    int32_t window;     // 0 = none
+    int32_t rows;       // query rows per row tile
+    int32_t tile;       // tokens per tile
+    int32_t min_rows, max_rows;  // sequences with more or fewer rows (new tokens * group) are not this launch's
+    int32_t rowless;    // 1: sequences without rows have one row tile all the same
+};
+
+struct Range {
+    int32_t lo, hi;  // tokens that some row of the tile sees
+    int32_t base;    // lo rounded down to a tile
+    int32_t tiles;   // at least 1, so that rows that see nothing are answered too
+};
+
+__device__ __forceinline__ Range row_tile_range(const Shape& p, const Seq& q, int m) {
+    Range r;
+    const int n = q.qn * p.group, last = (int)min((int64_t)n, (int64_t)(m + 1) * p.rows) - 1;
+    const int p0 = q.len - q.qn + m * p.rows / p.group, p1 = q.len - q.qn + last / p.group;
+    r.hi = min(max(p1 + 1, 0), q.len);
+    r.lo = p.window > 0 ? min(max(p0 - p.window + 1, 0), r.hi) : 0;
+    r.base = r.lo / p.tile * p.tile;
+    r.tiles = max(1, (r.hi - r.base + p.tile - 1) / p.tile);
+    return r;
+}
+
+__device__ __forceinline__ int row_tiles(const Shape& p, const Seq& q) {
+    const int n = q.qn * p.group;
+    if (n == 0) return p.rowless && q.ok ? 1 : 0;
+    return n < p.min_rows || n > p.max_rows ? 0 : (n - 1) / p.rows + 1;
+}
+
+// Tiles of one head of a sequence.
+__device__ __forceinline__ int64_t head_tiles(const Shape& p, const Seq& q) {
+    const int nm = row_tiles(p, q);
+    int64_t n = 0;
+    for (int m = 0; m < nm; ++m) n += row_tile_range(p, q, m).tiles;
+    return n;
+}
+
+// First tile of CTA c's share.
+__device__ __forceinline__ int64_t share_begin(int64_t total, int ctas, int c) { return total * c / ctas; }
+__device__ __forceinline__ int share_of(int64_t total, int ctas, int64_t tile) {
+    int c = (int)min((int64_t)ctas - 1, tile * ctas / total);
+    while (share_begin(total, ctas, c + 1) <= tile) ++c;
+    while (share_begin(total, ctas, c) > tile) --c;
+    return c;
+}
+
+struct Walk {
+    int32_t s, h, m, t;  // sequence, key head, row tile, tile of it
+    int32_t nm;
+    Seq seq;
+    Range range;
+
+    __device__ __forceinline__ void open(const Shape& p, const Batch& b, int block_tokens, int seq_index) {
+        s = seq_index;
+        seq = sequence(b, s, block_tokens);
+        nm = row_tiles(p, seq);
+        h = m = t = 0;
+        if (nm) range = row_tile_range(p, seq, 0);
+    }
+    // To the tile `off` tiles into the (non-empty) sequence that is open.
+    __device__ __forceinline__ void seek(const Shape& p, int64_t off) {
+        const int64_t per_head = head_tiles(p, seq);
+        h = (int)(off / per_head);
+        off -= h * per_head;
+        for (m = 0;; ++m) {
+            range = row_tile_range(p, seq, m);
+            if (off < range.tiles) break;
+            off -= range.tiles;
+        }
+        t = (int)off;
+    }
+    // To the next tile; the caller knows that there is one.
+    __device__ __forceinline__ void next(const Shape& p, const Batch& b, int block_tokens) {
+        if (++t < range.tiles) return;
+        t = 0;
+        if (++m < nm) {
+            range = row_tile_range(p, seq, m);
+            return;
+        }
+        m = 0;
+        if (++h < p.kv_heads) {
+            if (nm > 1) range = row_tile_range(p, seq, 0);
+            return;
+        }
+        do open(p, b, block_tokens, s + 1);
+        while (nm == 0 && s + 1 < b.num_seqs);
+    }
+};
+
+// Sum over the block of one value per thread; `shared` holds one value per warp.
+template <int kThreads>
+__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* shared) {
+#pragma unroll
+    for (int o = 16; o; o /= 2) v += __shfl_xor_sync(~0u, v, o);
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) v += shared[w];
+    return v;
+}
+
+// This CTA's share: *total and the number of its tiles, with `walk` at the first of them.  CTA 0 reports bad sequences and
+// writes the first tile of every sequence, and the total behind them, to `prefix` (null: to nowhere).
+template <int kThreads>
+__device__ int64_t take_share(const Shape& p, const Batch& b, int block_tokens, Walk* walk, int64_t* total, int* ctas,
+                              int min_tiles, int64_t* prefix, int32_t* status) {
+    __shared__ int64_t s_warp[kThreads / 32];
+    __shared__ int64_t s_off;
+    __shared__ int32_t s_seq;
+    const int tid = threadIdx.x;
+    int64_t mine = 0, sum = 0;
+    for (int s = tid; s < b.num_seqs; s += kThreads) {
+        const Seq q = sequence(b, s, block_tokens);
+        if (!q.ok && blockIdx.x == 0) report(status, AMOEBA_ERR_INVALID_ARG);
+        mine = p.kv_heads * head_tiles(p, q);
+        sum += mine;
+    }
+    const int64_t all = block_sum<kThreads>(sum, s_warp);
+    *total = all;
+    *ctas = (int)max((int64_t)1, min((int64_t)gridDim.x, all / min_tiles));
+    const int64_t begin = share_begin(all, *ctas, blockIdx.x);
+    const int64_t end = (int)blockIdx.x < *ctas ? share_begin(all, *ctas, blockIdx.x + 1) : begin;
+    const bool writes = blockIdx.x == 0 && prefix;
+    int64_t run = 0;
+    for (int base = 0; base < b.num_seqs; base += kThreads) {
+        const int s = base + tid;
+        if (b.num_seqs > kThreads)
+            mine = s < b.num_seqs ? p.kv_heads * head_tiles(p, sequence(b, s, block_tokens)) : 0;
+        int64_t incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t up = __shfl_up_sync(~0u, incl, o);
+            if (tid % 32 >= o) incl += up;
+        }
+        __syncthreads();
+        if (tid % 32 == 31) s_warp[tid / 32] = incl;
+        __syncthreads();
+        int64_t before = run;
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < tid / 32) before += s_warp[w];
+            run += s_warp[w];
+        }
+        const int64_t first = before + incl - mine;
+        if (writes && s < b.num_seqs) prefix[s] = first;
+        if (begin >= first && begin < first + mine) s_seq = s, s_off = begin - first;
+        if (!writes && run > begin) break;  // block-uniform
+    }
+    if (writes && tid == 0) prefix[b.num_seqs] = all;
+    __syncthreads();
+    if (end > begin) {
+        walk->open(p, b, block_tokens, s_seq);
+        walk->seek(p, s_off);
+    }
+    return end - begin;
+}
+
+}  // namespace amoeba

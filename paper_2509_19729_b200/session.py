@@ -336,3 +336,73 @@ class MergeCopySession:
     def bytes_rw(self) -> int:
         kv, _ = A.amoeba_plan_bytes(self.plan, sum(self.counts))
         return kv * self.kv_layers // self.L
+
+
+class CacheSession:
+    """The paged cache of one serving instance and the operators on it: new tokens in, attention over it, the attention
+    weight its tokens received, and long sequences cut to a budget.
+
+    dtype: "fp16" or "bf16"; kv_layers: layers the pools hold (None = all); scores: hold score pools too.  set_tables()
+    and set_rows() describe the batch of a step; the row buffers q, k, v, out are the caller's, one tensor per worker."""
+
+    def __init__(self, model: dict, tp: int, NB: int, num_seqs: int, max_blocks_per_seq: int, dtype: str = "bf16",
+                 kv_layers: Optional[int] = None, block_tokens: int = 16, kv_order: int = A.KV_HEAD_MAJOR,
+                 device="cuda:0", scores: bool = True):
+        self.model, self.tp = model, tp
+        self.device = dev = torch.device(device)
+        self.dtype = {"fp16": A.DTYPE_FP16, "bf16": A.DTYPE_BF16}[dtype]
+        self.kv_layers = model["L"] if kv_layers is None else kv_layers
+        self.layout = A.make_layout(model, tp, NB, block_tokens, kv_order=kv_order)
+        per_layer = A.amoeba_layout_kv_pool_bytes(self.layout) // model["L"]
+        self.pools = [torch.empty(per_layer * self.kv_layers, dtype=torch.uint8, device=dev) for _ in range(tp)]
+        self.score_pools = [torch.empty(self.kv_layers, NB, model["Hkv"] // tp, block_tokens, device=dev)
+                            for _ in range(tp)] if scores else None
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.block_table = torch.full((num_seqs, max_blocks_per_seq), -1, **i32)
+        self.seq_lens = torch.zeros(num_seqs, **i32)
+        self.new_lens = torch.zeros(num_seqs, **i32)
+        self.q_starts = torch.zeros(num_seqs + 1, **i32)
+        self.status = torch.zeros(1, **i32)
+        self.workspace = torch.empty(0, dtype=torch.uint8, device=dev)
+        self.set_rows(None, num_seqs, 1)
+
+    def set_tables(self, seq_lens, block_table) -> None:
+        self.seq_lens.copy_(torch.as_tensor(seq_lens, dtype=torch.int32))
+        self.block_table.copy_(torch.as_tensor(block_table, dtype=torch.int32))
+
+    def set_rows(self, q_starts, num_rows: int, max_q_len: int) -> None:
+        """q_starts: first row of every sequence's new tokens and the end, or None for one token each."""
+        if q_starts is not None:
+            self.q_starts.copy_(torch.as_tensor(q_starts, dtype=torch.int32))
+        self.batch = A.make_batch(self.block_table, self.seq_lens, None if q_starts is None else self.q_starts, num_rows,
+                                  max_q_len)
+        self._room(A.amoeba_attend_workspace_bytes(self.layout, self.batch))
+
+    def _room(self, nbytes: int) -> None:
+        if self.workspace.numel() < nbytes:
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    def append(self, layer: int, q, k, v, rotation, q_out, stream=None) -> None:
+        A.amoeba_append_kv(self.layout, self.dtype, layer, self.pools, self.batch, q, k, v, rotation, q_out, self.status,
+                           stream)
+
+    def attend(self, layer: int, q, out, lse=None, scale: Optional[float] = None, window: int = 0, stream=None) -> None:
+        A.amoeba_attend(self.layout, self.dtype, layer, self.pools, self.batch, q,
+                        self.model["D"] ** -0.5 if scale is None else scale, window, out, lse, self.status,
+                        self.workspace, stream)
+
+    def accumulate(self, layer: int, q, lse, scored_lens=None, scale: Optional[float] = None, window: int = 0,
+                   stream=None) -> None:
+        A.amoeba_accumulate_scores(self.layout, self.dtype, layer, self.pools, self.batch, q,
+                                   self.model["D"] ** -0.5 if scale is None else scale, window, lse, scored_lens,
+                                   self.score_pools, self.status, stream)
+
+    def evict(self, budget: int, recent: int, dst_table=None, layer_begin: int = 0, layer_end: Optional[int] = None,
+              stream=None) -> None:
+        """Cuts the sequences to `budget` tokens; new_lens has their lengths.  dst_table: free blocks to move to (None: in
+        place)."""
+        layer_end = self.kv_layers if layer_end is None else layer_end
+        self._room(A.amoeba_evict_workspace_bytes(self.layout, layer_end - layer_begin, self.seq_lens.numel(), budget))
+        A.amoeba_evict_kv(self.layout, layer_begin, layer_end, self.pools, self.score_pools, self.block_table,
+                          self.seq_lens, self.block_table if dst_table is None else dst_table, budget, recent,
+                          self.new_lens, self.status, self.workspace, stream)
