@@ -16,9 +16,10 @@ INCLUDE = HERE.parent / "include"
 LIB = HERE / "libamoeba.so"
 LIB_CHECKED = HERE / "libamoeba_checked.so"  # the same sources with -DAMOEBA_CHECK_ITEMS: every work item is tested
 #                                              against the extent of its buffers before it is moved
-SOURCES = ["plan.cpp", "block_tables.cu", "kv_reshard.cu", "weights_reshard.cu", "append_kv.cu", "attend.cu", "scores.cu",
+SOURCES = ["plan.cpp", "block_tables.cu", "kv_reshard.cu", "weights_reshard.cu", "append_kv.cu", "attend.cu", "attend_many.cu",
+           "scores.cu",
            "evict_kv.cu"]
-HEADERS = ["plan.hpp", "launch.hpp", "copy_engine.cuh", "kv_items.cuh", "w_items.cuh", "cache_view.cuh", "walk.cuh",
+HEADERS = ["plan.hpp", "launch.hpp", "copy_engine.cuh", "kv_items.cuh", "w_items.cuh", "cache_view.cuh", "walk.cuh", "attend.cuh",
            "warp_mma.cuh"]
 
 NVCC_FLAGS = [

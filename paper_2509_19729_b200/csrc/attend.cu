@@ -4,37 +4,10 @@
 // query heads that share the key head, so that grouped heads read their keys once.  The softmax runs along the tokens
 // with a running maximum and sum per row; units are cut where the shares of the CTAs end (walk.cuh), and the cut ones
 // are joined by their maxima and sums in a second small launch.
-#include "walk.cuh"
+#include "attend.cuh"
 #include "warp_mma.cuh"
 
 namespace amoeba {
-
-struct AttendParams {
-    CacheView cache;
-    Batch batch;
-    Rows q, out;
-    Shape shape;
-    float* lse;
-    int32_t* status;
-    int64_t* prefix;         // [num_seqs + 1]: first tile of every sequence
-    float *part_o, *part_m, *part_l;  // of the cut units: [2 * CTAs][rows][D], [2 * CTAs][rows]
-    float scale_log2;        // scale * log2(e): the softmax runs in powers of two
-    int32_t q_heads;         // of all workers
-    int32_t whole;           // 1: one CTA per unit, nothing is cut
-    int32_t max_row_tiles;
-};
-
-// Where row r of a unit lies in a row buffer.
-template <int D>
-__device__ __forceinline__ char* row_of(const Rows& rows, const AttendParams& p, const Seq& q, int kv_head, int r) {
-    const int w = kv_head / p.cache.heads, h = kv_head - w * p.cache.heads, g = p.shape.group;
-    const int tok = r / g;
-    return rows.base[w] + (int64_t)(q.q0 + tok) * rows.stride + (h * g + r - tok * g) * (D * 2);
-}
-__device__ __forceinline__ float* lse_of(const AttendParams& p, const Seq& q, int kv_head, int r) {
-    const int g = p.shape.group, tok = r / g;
-    return p.lse + (int64_t)(q.q0 + tok) * p.q_heads + kv_head * g + r - tok * g;
-}
 
 // ------------------------------------------------------------------------------------------------ few rows
 // Up to 8*NT rows a unit.  Bound by the bytes of the cache: 2 * 2 * D a token and key head against at most 32 rows of
@@ -304,23 +277,37 @@ __global__ void __launch_bounds__(128) attend_join(const __grid_constant__ Atten
     }
 }
 
-constexpr int kMaxFewCtas = 384;  // two for each of up to 192 SMs: bounds the workspace without asking the device
+// The workspace holds the parts of cut units, two for each CTA; these bound the grids without asking the device.
+constexpr int kMaxSms = 192, kMaxFewCtas = 2 * kMaxSms;
 constexpr int kMaxFewRows = 32;
 
 static int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
 
-struct Workspace {
-    int64_t prefix, part_o, part_m, part_l, bytes;
-};
-static Workspace attend_workspace(const amoeba_layout* l, int32_t num_seqs) {
-    Workspace w;
-    const int64_t parts = 2 * kMaxFewCtas * kMaxFewRows;
-    w.prefix = 0;
-    w.part_o = align16((num_seqs + 1) * 8);
-    w.part_m = w.part_o + parts * l->model.head_dim * 4;
-    w.part_l = w.part_m + parts * 4;
-    w.bytes = w.part_l + parts * 4;
-    return w;
+// One kernel's part of the workspace: the sequences' first tiles, then the parts.
+static int64_t workspace_part(AttendParams* p, char* ws, int64_t num_seqs, int64_t parts, int64_t rows, int head_dim) {
+    const int64_t o = align16((num_seqs + 1) * 8), m = o + parts * rows * head_dim * 4, l = m + parts * rows * 4;
+    if (p) {
+        p->prefix = reinterpret_cast<int64_t*>(ws);
+        p->part_o = reinterpret_cast<float*>(ws + o);
+        p->part_m = reinterpret_cast<float*>(ws + m);
+        p->part_l = reinterpret_cast<float*>(ws + l);
+    }
+    return l + parts * rows * 4;
+}
+static int64_t few_workspace(AttendParams* p, char* ws, int64_t num_seqs, int head_dim) {
+    return workspace_part(p, ws, num_seqs, 2 * kMaxFewCtas, kMaxFewRows, head_dim);
+}
+static int64_t many_workspace(AttendParams* p, char* ws, int64_t num_seqs, int head_dim) {
+    return workspace_part(p, ws, num_seqs, 2 * kMaxSms, kManyRows, head_dim);
+}
+static int64_t rows_of(const amoeba_layout* l, int32_t max_q_len) {
+    return (int64_t)max_q_len * (l->model.num_q_heads / l->model.num_kv_heads);
+}
+
+template <class T, int D>
+static amoeba_status join(const AttendParams& p, int ctas, cudaStream_t stream) {
+    attend_join<T, D><<<p.batch.num_seqs * p.shape.kv_heads * p.max_row_tiles, 128, 0, stream>>>(p, ctas);
+    return launch_result();
 }
 
 template <class T, int D, int NT>
@@ -328,24 +315,36 @@ static amoeba_status run_few(AttendParams& p, int sms, cudaStream_t stream) {
     using F = FewShape<D, NT>;
     p.shape.rows = 8 * NT;
     p.shape.tile = kFewTile;
-    p.max_row_tiles = (int)(((int64_t)p.batch.max_q_len * p.shape.group + 8 * NT - 1) / (8 * NT));
-    const int64_t units = (int64_t)p.batch.num_seqs * p.shape.kv_heads * p.max_row_tiles;
-    if (units > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
+    p.max_row_tiles = 1;
     if (ensure_dynamic_smem((const void*)attend_few<T, D, NT>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
     const int ctas = std::min(F::kCtas * sms, kMaxFewCtas);
-    attend_few<T, D, NT><<<p.whole ? (int)units : ctas, kFewThreads, F::kSmem, stream>>>(p);
-    amoeba_status st = launch_result();
-    if (st != AMOEBA_OK || p.whole) return st;
-    attend_join<T, D><<<(int)units, 128, 0, stream>>>(p, ctas);
-    return launch_result();
+    attend_few<T, D, NT><<<p.whole ? p.batch.num_seqs * p.shape.kv_heads : ctas, kFewThreads, F::kSmem, stream>>>(p);
+    const amoeba_status st = launch_result();
+    return st != AMOEBA_OK || p.whole ? st : join<T, D>(p, ctas, stream);
 }
 
+// Sequences with at most 32 rows (new tokens times query heads per key head) are read by attend_few, whose time is that of
+// reading the cache; the others by attend_many.  Which there are is known only on the device: a batch that may hold longer
+// ones gets both, and each skips the other's.
 template <class T, int D>
-static amoeba_status run_attend(AttendParams& p, int sms, cudaStream_t stream) {
+static amoeba_status run_attend(AttendParams& p, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
     const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
+    const int64_t few_bytes = few_workspace(&p, ws, p.batch.num_seqs, D);
+    p.shape.min_rows = 0;
+    p.shape.max_rows = kMaxFewRows;
     if (rows <= 8) return run_few<T, D, 1>(p, sms, stream);
     if (rows <= 16) return run_few<T, D, 2>(p, sms, stream);
-    return run_few<T, D, 4>(p, sms, stream);
+    const amoeba_status st = run_few<T, D, 4>(p, sms, stream);
+    if (st != AMOEBA_OK || rows <= kMaxFewRows) return st;
+    many_workspace(&p, ws + few_bytes, p.batch.num_seqs, D);
+    p.shape.min_rows = kMaxFewRows + 1;
+    p.shape.max_rows = INT32_MAX;
+    p.shape.rows = kManyRows;
+    p.shape.tile = kManyTile;
+    p.max_row_tiles = (int)((rows + kManyRows - 1) / kManyRows);
+    const int ctas = std::min(sms, kMaxSms);
+    const amoeba_status many = launch_attend_many(p, dtype, D, ctas, stream);
+    return many != AMOEBA_OK ? many : join<T, D>(p, ctas, stream);
 }
 
 }  // namespace amoeba
@@ -355,10 +354,12 @@ using namespace amoeba;
 extern "C" amoeba_status amoeba_attend_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
                                                        int64_t* bytes) {
     int64_t pool = 0;
-    if (!layout || !batch || !bytes || batch->num_seqs < 0) return AMOEBA_ERR_INVALID_ARG;
+    if (!layout || !batch || !bytes || batch->num_seqs < 0 || batch->max_q_len < 0) return AMOEBA_ERR_INVALID_ARG;
     const amoeba_status st = amoeba_layout_kv_pool_bytes(layout, &pool);
     if (st != AMOEBA_OK) return st;
-    *bytes = attend_workspace(layout, batch->num_seqs).bytes;
+    *bytes = few_workspace(nullptr, nullptr, batch->num_seqs, layout->model.head_dim);
+    if (rows_of(layout, batch->max_q_len) > kMaxFewRows)
+        *bytes += many_workspace(nullptr, nullptr, batch->num_seqs, layout->model.head_dim);
     return AMOEBA_OK;
 }
 
@@ -379,29 +380,27 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     if ((st = make_rows(layout, out, out_stride, row, &p.out)) != AMOEBA_OK) return st;
     for (int r = 0; r < layout->tp; ++r)
         if (q[r] == out[r]) return AMOEBA_ERR_INVALID_ARG;
-    const Workspace w = attend_workspace(layout, p.batch.num_seqs);
-    if (!d_workspace || workspace_bytes < w.bytes) return AMOEBA_ERR_INVALID_ARG;
+    int64_t need = 0;
+    if ((st = amoeba_attend_workspace_bytes(layout, batch, &need)) != AMOEBA_OK) return st;
+    if (!d_workspace || workspace_bytes < need) return AMOEBA_ERR_INVALID_ARG;
     if ((uintptr_t)d_workspace % 16) return AMOEBA_ERR_ALIGNMENT;
     if (p.batch.num_seqs == 0 || p.batch.num_rows == 0 || p.batch.max_q_len == 0) return AMOEBA_OK;
     p.lse = d_lse;
     p.status = d_status;
-    char* ws = static_cast<char*>(d_workspace);
-    p.prefix = reinterpret_cast<int64_t*>(ws + w.prefix);
-    p.part_o = reinterpret_cast<float*>(ws + w.part_o);
-    p.part_m = reinterpret_cast<float*>(ws + w.part_m);
-    p.part_l = reinterpret_cast<float*>(ws + w.part_l);
     p.scale_log2 = scale * kLog2e;
     p.q_heads = m.num_q_heads;
     p.shape.group = m.num_q_heads / m.num_kv_heads;
     p.shape.kv_heads = m.num_kv_heads;
     p.shape.window = std::min(window, 1 << 30);
-    p.shape.min_rows = 0;
-    p.shape.max_rows = INT32_MAX;
+    const int64_t units = (int64_t)p.batch.num_seqs * m.num_kv_heads * (rows_of(layout, p.batch.max_q_len) / kManyRows + 1);
+    if (rows_of(layout, p.batch.max_q_len) > INT32_MAX || units > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    char* ws = static_cast<char*>(d_workspace);
     if (dtype == AMOEBA_FP16)
-        return m.head_dim == 64 ? run_attend<__half, 64>(p, dev.sms, stream) : run_attend<__half, 128>(p, dev.sms, stream);
-    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, dev.sms, stream)
-                            : run_attend<__nv_bfloat16, 128>(p, dev.sms, stream);
+        return m.head_dim == 64 ? run_attend<__half, 64>(p, dtype, ws, dev.sms, stream)
+                                : run_attend<__half, 128>(p, dtype, ws, dev.sms, stream);
+    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, dtype, ws, dev.sms, stream)
+                            : run_attend<__nv_bfloat16, 128>(p, dtype, ws, dev.sms, stream);
 }

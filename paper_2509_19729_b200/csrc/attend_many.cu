@@ -1,0 +1,505 @@
+// amoeba_attend for many rows: the matrix products run on the fifth-generation tensor cores.
+//
+// A unit has 256 query rows, two tiles of 128, and takes 128 tokens at a time.  One thread issues the products: S = Q K^T
+// from shared memory into tensor memory (a row per lane, a token per column), and O += P V with P, the weights in 16
+// bits, read from tensor memory where the softmax threads have written it over S.  Two warpgroups do the softmax, one
+// for each tile, a thread for each row, so that maxima and sums need no exchange between threads; while one works on its
+// S the tensor core has the other's products to do.  Three warps load keys and values, through the block table, 16 bytes
+// at a time into the 128-byte-swizzled layout that the products read.
+//
+// The running maximum of a row is only raised, and O scaled down, when a tile exceeds it by more than 2^8: the weights
+// stay below 2^8 until then and the result is the same, as numerator and sum have the same factor.  That makes the
+// scaling of O, a pass through tensor memory, rare.
+//
+// Tensor memory: columns 0-127 and 128-255 S and P of the two tiles, 256 and 256 + D their O.
+#include "attend.cuh"
+#include "warp_mma.cuh"
+
+namespace amoeba {
+
+constexpr int kManyThreads = 384, kLoadWarps = 3, kLoadThreads = 32 * kLoadWarps;
+constexpr float kRaise = 8.f;
+
+template <int D>
+struct ManyShape {
+    static constexpr int kTileBytes = 128 * D * 2;  // 128 rows of queries, keys or values
+    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;  // up to 1 KiB goes to the alignment
+};
+
+struct ManyBarriers {
+    uint64_t full[8], empty[8];  // ring of tiles: K, V, K, V, ...
+    uint64_t q_full, q_empty;
+    uint64_t s_full[2], p_full[2], o_full[2], o_free[2];
+    uint64_t drain;
+    uint32_t tmem;
+    int32_t abort;
+};
+
+// ---- tensor memory and products
+__device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,"
+        "%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void umma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void umma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// The barrier gets one arrival when all products issued so far are done.
+__device__ __forceinline__ void umma_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// Shared-memory operand in the 128-byte swizzle: groups of eight 128-byte rows 1 KiB apart; `leading` bytes from one
+// 64-element half of a row to the next where the rows run along the product's sum (values).
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading) {
+    return (uint64_t)((addr >> 4) & 0x3fff) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// Product of 16-bit operands into 32 bits, 128 rows, n columns; b_rows: the second operand's rows run along the sum.
+template <class T>
+__device__ constexpr uint32_t product(int n, bool b_rows) {
+    const uint32_t f = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+    return 1u << 4 | f << 7 | f << 10 | (b_rows ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | 8u << 24;
+}
+
+// Byte offset of 16-byte chunk c of row r in a tile: 64-element halves of all rows one behind the other.
+__device__ __forceinline__ int tile_offset(int r, int c) { return c / 8 * (128 * 128) + r * 128 + ((c ^ r) & 7) * 16; }
+
+// The part of a unit that a CTA has in its share.
+struct Part {
+    int tiles, q_tiles, rows;  // rows of the unit, 1 .. 256
+    bool from_start, to_end;
+};
+__device__ __forceinline__ Part part_of(const Shape& sh, const Walk& w, int64_t left) {
+    Part p;
+    p.tiles = (int)min(left, (int64_t)(w.range.tiles - w.t));
+    p.rows = min(kManyRows, w.seq.qn * sh.group - w.m * kManyRows);
+    p.q_tiles = p.rows > 128 ? 2 : 1;
+    p.from_start = w.t == 0;
+    p.to_end = w.t + p.tiles == w.range.tiles;
+    return p;
+}
+
+// ---- loading
+template <int D>
+struct Loader {
+    const AttendParams& p;
+    char* smem;  // two query tiles, then the ring
+    ManyBarriers& b;
+    const int warp, lane;
+    int slot = 0;
+    uint32_t phase = 1;     // of `empty`: the first round waits for nothing
+    int pending = 0;        // started, not yet announced; at most 2 + 1
+    int announce_slot = 0;
+    static constexpr int kChunks = D / 8, kStep = 32 / kChunks;
+
+    // Blocks of the 16 groups of eight tokens of a tile, one per lane; -1: none or a bad one.
+    __device__ __forceinline__ int blocks(const Walk& w) const {
+        const CacheView& v = p.cache;
+        const int key = w.range.base + w.t * kManyTile + lane * 8;
+        if (v.block_tokens % 8 || lane >= 16 || key >= w.range.hi || key + 8 <= w.range.lo) return -1;
+        const int block = p.batch.table[(int64_t)w.s * p.batch.max_blocks + key / v.block_tokens];
+        return block >= 0 && block < v.num_blocks ? block : -1;
+    }
+    // Starts the loads of the tile's keys (kv = 0) or values (1).
+    __device__ __forceinline__ bool tile(const Walk& w, int ids, int kv) {
+        const CacheView& v = p.cache;
+        if (!__all_sync(~0u, mbar_wait_bounded(&b.empty[slot], phase, 0, &b.abort))) return false;
+        const uint32_t dst = smem_u32(smem + (2 + slot) * ManyShape<D>::kTileBytes);
+        const char* head = v.head_base(w.h) + kv * v.kv_stride;
+        const int key0 = w.range.base + w.t * kManyTile, c = lane % kChunks, sub = lane / kChunks;
+        for (int g = warp; g < 16; g += kLoadWarps) {
+            const int block = __shfl_sync(~0u, ids, g);
+#pragma unroll
+            for (int i = 0; i < 8 / kStep; ++i) {
+                const int r = g * 8 + i * kStep + sub, key = key0 + r;
+                bool in = key >= w.range.lo && key < w.range.hi;
+                const char* src = head;
+                if (v.block_tokens % 8 == 0) {
+                    in = in && block >= 0;
+                    if (in) src = head + block * v.block_stride + key % v.block_tokens * v.tok_stride + c * 16;
+                } else if (in) {
+                    const int own = p.batch.table[(int64_t)w.s * p.batch.max_blocks + key / v.block_tokens];
+                    in = own >= 0 && own < v.num_blocks;
+                    if (in) src = head + own * v.block_stride + key % v.block_tokens * v.tok_stride + c * 16;
+                }
+                cp_async16(dst + tile_offset(r, c), src, in ? 16 : 0);
+            }
+        }
+        cp_async_commit();
+        if (++slot == ManyShape<D>::kStages) slot = 0, phase ^= 1;
+        if (++pending > 2) announce<2>();
+        return true;
+    }
+    // Tells the products that the oldest pending tile, and all but kLeft groups, are there.
+    template <int kLeft>
+    __device__ __forceinline__ void announce() {
+        cp_async_wait<kLeft>();
+        fence_async_smem();
+        mbar_arrive(&b.full[announce_slot]);
+        if (++announce_slot == ManyShape<D>::kStages) announce_slot = 0;
+        --pending;
+    }
+    __device__ __forceinline__ void announce_all() {
+        cp_async_wait<0>();
+        fence_async_smem();
+        while (pending > 0) {
+            mbar_arrive(&b.full[announce_slot]);
+            if (++announce_slot == ManyShape<D>::kStages) announce_slot = 0;
+            --pending;
+        }
+    }
+    __device__ __forceinline__ bool queries(const Walk& w, const Part& part, uint32_t q_phase) {
+        announce_all();
+        if (!__all_sync(~0u, mbar_wait_bounded(&b.q_empty, q_phase, 0, &b.abort))) return false;
+        const uint32_t dst = smem_u32(smem);
+        const int c = lane % kChunks, sub = lane / kChunks;
+        for (int r = warp * kStep + sub; r < part.q_tiles * 128; r += kLoadWarps * kStep) {
+            const bool in = r < part.rows;
+            const char* src = in ? row_of<D>(p.q, p, w.seq, w.h, w.m * kManyRows + r) + c * 16 : p.q.base[0];
+            cp_async16(dst + r / 128 * ManyShape<D>::kTileBytes + tile_offset(r % 128, c), src, in ? 16 : 0);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        fence_async_smem();
+        mbar_arrive(&b.q_full);
+        return true;
+    }
+};
+
+template <int D>
+__device__ void load_loop(const AttendParams& p, char* smem, ManyBarriers& b, Walk w, int64_t n) {
+    Loader<D> load{p, smem, b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32};
+    uint32_t q_phase = 1;
+    bool ok = true;
+    while (ok && n > 0) {
+        const Part part = part_of(p.shape, w, n);
+        ok = load.queries(w, part, q_phase);
+        q_phase ^= 1;
+        int ids = load.blocks(w);
+        for (int i = 0; ok && i < part.tiles; ++i) {
+            ok = load.tile(w, ids, 0);
+            Walk next = w;
+            ++next.t;
+            const int next_ids = i + 1 < part.tiles ? load.blocks(next) : -1;
+            if (ok) ok = load.tile(w, ids, 1);
+            ids = next_ids;
+            if (i + 1 < part.tiles) ++w.t;
+        }
+        n -= part.tiles;
+        if (n > 0) w.next(p.shape, p.batch, p.cache.block_tokens);
+    }
+    load.announce_all();
+    if (!ok) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+}
+
+// ---- products: one thread
+template <class T, int D>
+__device__ bool multiply(const AttendParams& p, uint32_t smem, ManyBarriers& b, Walk w, int64_t n) {
+    constexpr int kTile = ManyShape<D>::kTileBytes, kStages = ManyShape<D>::kStages;
+    constexpr uint32_t kS = product<T>(128, false), kO = product<T>(D, true);
+    const uint32_t tmem = b.tmem;
+    int slot = 0;  // of the next K; V is the one behind
+    uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, 0, &b.abort); };
+    auto logits = [&](int t, int k_slot) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const uint32_t step = k / 4 * (128 * 128) + k % 4 * 32;
+            umma_smem(tmem + t * 128, operand(smem + t * kTile + step, 16), operand(smem + (2 + k_slot) * kTile + step, 16), kS, k > 0);
+        }
+    };
+    auto weigh = [&](int t, int v_slot, bool accumulate) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            umma_tmem(tmem + 256 + t * D, tmem + t * 128 + k * 8, operand(smem + (2 + v_slot) * kTile + k * 2048, 128 * 128), kO,
+                      accumulate || k > 0);
+    };
+    while (n > 0) {
+        const Part part = part_of(p.shape, w, n);
+        if (!wait(&b.q_full, q_phase)) return false;
+        q_phase ^= 1;
+        if (!wait(&b.full[slot], phase)) return false;
+        tmem_fence_after();
+        for (int t = 0; t < part.q_tiles; ++t) {
+            logits(t, slot);
+            umma_commit(&b.s_full[t]);
+        }
+        umma_commit(&b.empty[slot]);
+        if (part.tiles == 1) umma_commit(&b.q_empty);
+        for (int i = 0; i < part.tiles; ++i) {
+            int v_slot = slot + 1, k_slot = slot + 2;
+            uint32_t v_phase = phase, k_phase = phase;
+            if (v_slot >= kStages) v_slot -= kStages, v_phase ^= 1;
+            if (k_slot >= kStages) k_slot -= kStages, k_phase ^= 1;
+            if (!wait(&b.full[v_slot], v_phase)) return false;
+            for (int t = 0; t < part.q_tiles; ++t) {
+                if (i == 0) {
+                    if (!wait(&b.o_free[t], o_phase[t])) return false;
+                    o_phase[t] ^= 1;
+                }
+                if (!wait(&b.p_full[t], p_phase[t])) return false;
+                p_phase[t] ^= 1;
+                tmem_fence_after();
+                weigh(t, v_slot, i > 0);
+                umma_commit(&b.o_full[t]);
+                if (i + 1 < part.tiles) {
+                    if (t == 0 && !wait(&b.full[k_slot], k_phase)) return false;
+                    logits(t, k_slot);
+                    umma_commit(&b.s_full[t]);
+                }
+            }
+            umma_commit(&b.empty[v_slot]);
+            if (i + 1 < part.tiles) umma_commit(&b.empty[k_slot]);
+            if (i + 2 == part.tiles) umma_commit(&b.q_empty);
+            slot = k_slot, phase = k_phase;
+        }
+        n -= part.tiles;
+        w.t += part.tiles - 1;
+        if (n > 0) w.next(p.shape, p.batch, p.cache.block_tokens);
+    }
+    return true;
+}
+
+// ---- softmax: a thread per row
+template <class T, int D>
+__device__ bool softmax(const AttendParams& p, ManyBarriers& b, Walk w, int64_t n) {
+    const Shape& sh = p.shape;
+    const int t = threadIdx.x / 128, r = threadIdx.x;  // row of the unit
+    const uint32_t lanes = (uint32_t)(threadIdx.x % 128 / 32 * 32) << 16;
+    const uint32_t s_tmem = b.tmem + lanes + t * 128, o_tmem = b.tmem + lanes + 256 + t * D;
+    const float c = p.scale_log2 == 0.f ? 1e-30f : fabsf(p.scale_log2);  // hidden logits are -infinity: c may not be 0
+    const bool flip = p.scale_log2 < 0.f;
+    uint32_t s_phase = 0, o_phase = 0;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+        return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort));  // and the warp is together again
+    };
+    while (n > 0) {
+        const Part part = part_of(sh, w, n);
+        // a bad block anywhere in the unit: its tokens are looked up one by one below
+        const int32_t* table = p.batch.table + (int64_t)w.s * p.batch.max_blocks;
+        int bad = 0;
+        for (int i = w.range.lo / p.cache.block_tokens + (int)threadIdx.x % 128; i * (int64_t)p.cache.block_tokens < w.range.hi; i += 128)
+            bad |= table[i] < 0 || table[i] >= p.cache.num_blocks;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %0, 0;\n\t"
+            "barrier.cta.red.or.pred q, %1, 128, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+            : "+r"(bad) : "r"(1 + t) : "memory");
+        if (bad && threadIdx.x % 128 == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
+        if (t < part.q_tiles) {
+            const int row = w.m * kManyRows + r;
+            const bool there = r < part.rows;
+            const int pos = w.seq.len - w.seq.qn + row / sh.group;
+            // (rows that are not there see zeros or anything: nothing is written for them)
+            const int see_hi = there ? pos + 1 : INT32_MAX, see_lo = there && sh.window > 0 ? max(pos - sh.window + 1, 0) : 0;
+            float m_ref = -INFINITY, l = 0.f;
+            for (int i = 0; i < part.tiles; ++i) {
+                const int key0 = w.range.base + (w.t + i) * kManyTile;
+                if (!wait(&b.s_full[t], s_phase)) return false;
+                s_phase ^= 1;
+                tmem_fence_after();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) tmem_load32(s[j], s_tmem + j * 32);
+                tmem_load_wait();
+                if (flip) {
+#pragma unroll
+                    for (int j = 0; j < 128; ++j) s[j / 32][j % 32] ^= 0x80000000u;
+                }
+                if (__any_sync(~0u, key0 + kManyTile > see_hi || key0 < see_lo)) {
+#pragma unroll
+                    for (int j = 0; j < 128; ++j)
+                        if (key0 + j >= see_hi || key0 + j < see_lo) s[j / 32][j % 32] = __float_as_uint(-INFINITY);
+                }
+                if (bad) {
+#pragma unroll
+                    for (int j = 0; j < 128; ++j) {
+                        const int key = key0 + j;
+                        if (key < w.range.lo || key >= w.range.hi) continue;
+                        const int block = table[key / p.cache.block_tokens];
+                        if (block < 0 || block >= p.cache.num_blocks) s[j / 32][j % 32] = __float_as_uint(-INFINITY);
+                    }
+                }
+                float top[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    top[j] = __uint_as_float(s[j][0]);
+#pragma unroll
+                    for (int k = 1; k < 32; ++k) top[j] = fmaxf(top[j], __uint_as_float(s[j][k]));
+                }
+                const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
+                const bool raise = m > m_ref + kRaise || (m_ref == -INFINITY && m > -INFINITY);
+                if (__any_sync(~0u, raise)) {
+                    const float m_new = raise ? m : m_ref;
+                    const float f = raise ? fast_exp2(m_ref - m_new) : 1.f;
+                    l *= f;
+                    m_ref = m_new;
+                    if (i > 0) {
+                        if (!wait(&b.o_full[t], o_phase ^ 1)) return false;  // of the tile before
+                        tmem_fence_after();
+#pragma unroll
+                        for (int j = 0; j < D / 32; ++j) {
+                            uint32_t o[32];
+                            tmem_load32(o, o_tmem + j * 32);
+                            tmem_load_wait();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_store32(o_tmem + j * 32, o);
+                        }
+                    }
+                }
+                const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t w16[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        const int e = j * 64 + 2 * k;
+                        const float x = fast_exp2(fmaf(__uint_as_float(s[e / 32][e % 32]), c, -ref));
+                        const float y = fast_exp2(fmaf(__uint_as_float(s[e / 32][e % 32 + 1]), c, -ref));
+                        sum[k % 2 * 2] += x, sum[k % 2 * 2 + 1] += y;
+                        w16[k] = Elem<T>::pack(x, y);
+                    }
+                    tmem_store32(s_tmem + j * 32, w16);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tmem_store_wait();
+                tmem_fence_before();
+                mbar_arrive(&b.p_full[t]);
+                o_phase ^= 1;
+            }
+            if (!wait(&b.o_full[t], o_phase ^ 1)) return false;
+            tmem_fence_after();
+            const bool direct = part.from_start && part.to_end;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const int64_t at = (int64_t)(2 * blockIdx.x + (part.from_start ? 1 : 0)) * kManyRows + r;
+            char* out = there ? row_of<D>(p.out, p, w.seq, w.h, row) : nullptr;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                uint32_t o[32];
+                tmem_load32(o, o_tmem + j * 32);
+                tmem_load_wait();
+                if (!there) continue;
+                if (direct) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            x[i] = Elem<T>::pack(__uint_as_float(o[k + 2 * i]) * inv, __uint_as_float(o[k + 2 * i + 1]) * inv);
+                        *reinterpret_cast<uint4*>(out + (j * 32 + k) * 2) = make_uint4(x[0], x[1], x[2], x[3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        *reinterpret_cast<uint4*>(p.part_o + at * D + j * 32 + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                }
+            }
+            tmem_fence_before();
+            mbar_arrive(&b.o_free[t]);
+            if (there && !direct) p.part_m[at] = m_ref, p.part_l[at] = l;
+            if (there && direct && p.lse)
+                *lse_of(p, w.seq, w.h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
+        }
+        n -= part.tiles;
+        w.t += part.tiles - 1;
+        if (n > 0) w.next(sh, p.batch, p.cache.block_tokens);
+    }
+    return true;
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_constant__ AttendParams p) {
+    extern __shared__ char smem_raw[];
+    __shared__ ManyBarriers b;
+    char* smem = smem_raw + (1024 - smem_u32(smem_raw) % 1024) % 1024;
+    const int warp = threadIdx.x / 32;
+    Walk w;
+    int64_t total;
+    int ctas;
+    const int64_t n = take_share<kManyThreads>(p.shape, p.batch, p.cache.block_tokens, &w, &total, &ctas, 1, p.prefix, p.status);
+    if (n == 0) return;
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&b.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < ManyShape<D>::kStages; ++i) mbar_init(&b.full[i], kLoadThreads), mbar_init(&b.empty[i], 1);
+        mbar_init(&b.q_full, kLoadThreads), mbar_init(&b.q_empty, 1), mbar_init(&b.drain, 1);
+        for (int t = 0; t < 2; ++t)
+            mbar_init(&b.s_full[t], 1), mbar_init(&b.p_full[t], 128), mbar_init(&b.o_full[t], 1), mbar_init(&b.o_free[t], 128);
+        b.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_smem();
+    }
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        if (warp == 8) {
+            if (threadIdx.x % 32 == 0) {
+                if (!multiply<T, D>(p, smem_u32(smem), b, w, n)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+                umma_commit(&b.drain);
+                mbar_drain(&b.drain, 0);
+            }
+            __syncwarp();
+        } else {
+            load_loop<D>(p, smem, b, w, n);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        if (!softmax<T, D>(p, b, w, n)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+    }
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tmem_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(b.tmem));
+    }
+}
+
+template <class T, int D>
+static amoeba_status launch(const AttendParams& p, int ctas, cudaStream_t stream) {
+    if (ensure_dynamic_smem((const void*)attend_many<T, D>, ManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    attend_many<T, D><<<ctas, kManyThreads, ManyShape<D>::kSmem, stream>>>(p);
+    return launch_result();
+}
+
+amoeba_status launch_attend_many(const AttendParams& p, int32_t dtype, int head_dim, int ctas, cudaStream_t stream) {
+    if (dtype == AMOEBA_FP16)
+        return head_dim == 64 ? launch<__half, 64>(p, ctas, stream) : launch<__half, 128>(p, ctas, stream);
+    return head_dim == 64 ? launch<__nv_bfloat16, 64>(p, ctas, stream) : launch<__nv_bfloat16, 128>(p, ctas, stream);
+}
+
+}  // namespace amoeba
