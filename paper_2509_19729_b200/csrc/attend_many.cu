@@ -122,37 +122,54 @@ struct Loader {
     int announce_slot = 0;
     static constexpr int kChunks = D / 8, kStep = 32 / kChunks;
 
-    // Blocks of the 16 groups of eight tokens of a tile, one per lane; -1: none or a bad one.
-    __device__ __forceinline__ int blocks(const Walk& w) const {
+    // Where the 16 groups of eight tokens of a tile lie in a head's part of the pool, one per lane; -1: no token that is
+    // seen, or a bad block.
+    __device__ __forceinline__ int64_t groups(const Walk& w) const {
         const CacheView& v = p.cache;
         const int key = w.range.base + w.t * kManyTile + lane * 8;
         if (v.block_tokens % 8 || lane >= 16 || key >= w.range.hi || key + 8 <= w.range.lo) return -1;
-        const int block = p.batch.table[(int64_t)w.s * p.batch.max_blocks + key / v.block_tokens];
-        return block >= 0 && block < v.num_blocks ? block : -1;
+        const int i = key / v.block_tokens, block = p.batch.table[(int64_t)w.s * p.batch.max_blocks + i];
+        return block >= 0 && block < v.num_blocks ? block * v.block_stride + (key - i * v.block_tokens) * v.tok_stride : -1;
     }
     // Starts the loads of the tile's keys (kv = 0) or values (1).
-    __device__ __forceinline__ bool tile(const Walk& w, int ids, int kv) {
+    __device__ __forceinline__ bool tile(const Walk& w, int64_t at, int kv) {
         const CacheView& v = p.cache;
         if (!__all_sync(~0u, mbar_wait_bounded(&b.empty[slot], phase, 0, &b.abort))) return false;
+        const int c = lane % kChunks, sub = lane / kChunks;
         const uint32_t dst = smem_u32(smem + (2 + slot) * ManyShape<D>::kTileBytes);
         const char* head = v.head_base(w.h) + kv * v.kv_stride;
-        const int key0 = w.range.base + w.t * kManyTile, c = lane % kChunks, sub = lane / kChunks;
-        for (int g = warp; g < 16; g += kLoadWarps) {
-            const int block = __shfl_sync(~0u, ids, g);
+        const int key0 = w.range.base + w.t * kManyTile;
+        const bool whole = key0 >= w.range.lo && key0 + kManyTile <= w.range.hi && __all_sync(~0u, lane >= 16 || at >= 0);
+        if (whole) {
+            const char* from = head + sub * v.tok_stride + c * 16;
+            const int64_t step = kStep * v.tok_stride;
 #pragma unroll
-            for (int i = 0; i < 8 / kStep; ++i) {
-                const int r = g * 8 + i * kStep + sub, key = key0 + r;
-                bool in = key >= w.range.lo && key < w.range.hi;
-                const char* src = head;
-                if (v.block_tokens % 8 == 0) {
-                    in = in && block >= 0;
-                    if (in) src = head + block * v.block_stride + key % v.block_tokens * v.tok_stride + c * 16;
-                } else if (in) {
-                    const int own = p.batch.table[(int64_t)w.s * p.batch.max_blocks + key / v.block_tokens];
-                    in = own >= 0 && own < v.num_blocks;
-                    if (in) src = head + own * v.block_stride + key % v.block_tokens * v.tok_stride + c * 16;
+            for (int j = 0; j < (16 + kLoadWarps - 1) / kLoadWarps; ++j) {
+                const int g = warp + j * kLoadWarps;
+                const char* src = from + __shfl_sync(~0u, at, g & 15);
+                if (g < 16) {
+#pragma unroll
+                    for (int i = 0; i < 8 / kStep; ++i)
+                        cp_async16(dst + g * 1024 + tile_offset(i * kStep + sub, c), src + i * step, 16);
                 }
-                cp_async16(dst + tile_offset(r, c), src, in ? 16 : 0);
+            }
+        } else {
+            for (int g = warp; g < 16; g += kLoadWarps) {
+                const int64_t own = __shfl_sync(~0u, at, g);
+                for (int i = 0; i < 8 / kStep; ++i) {
+                    const int r = g * 8 + i * kStep + sub, key = key0 + r;
+                    bool in = key >= w.range.lo && key < w.range.hi;
+                    const char* src = head;
+                    if (v.block_tokens % 8 == 0) {
+                        in = in && own >= 0;
+                        if (in) src = head + own + r % 8 * v.tok_stride + c * 16;
+                    } else if (in) {
+                        const int block = p.batch.table[(int64_t)w.s * p.batch.max_blocks + key / v.block_tokens];
+                        in = block >= 0 && block < v.num_blocks;
+                        if (in) src = head + block * v.block_stride + key % v.block_tokens * v.tok_stride + c * 16;
+                    }
+                    cp_async16(dst + tile_offset(r, c), src, in ? 16 : 0);
+                }
             }
         }
         cp_async_commit();
@@ -205,14 +222,14 @@ __device__ void load_loop(const AttendParams& p, char* smem, ManyBarriers& b, Wa
         const Part part = part_of(p.shape, w, n);
         ok = load.queries(w, part, q_phase);
         q_phase ^= 1;
-        int ids = load.blocks(w);
+        int64_t at = load.groups(w);
         for (int i = 0; ok && i < part.tiles; ++i) {
-            ok = load.tile(w, ids, 0);
+            ok = load.tile(w, at, 0);
             Walk next = w;
             ++next.t;
-            const int next_ids = i + 1 < part.tiles ? load.blocks(next) : -1;
-            if (ok) ok = load.tile(w, ids, 1);
-            ids = next_ids;
+            const int64_t next_at = i + 1 < part.tiles ? load.groups(next) : -1;
+            if (ok) ok = load.tile(w, at, 1);
+            at = next_at;
             if (i + 1 < part.tiles) ++w.t;
         }
         n -= part.tiles;
