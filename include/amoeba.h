@@ -520,6 +520,7 @@ AMOEBA_API amoeba_status amoeba_append_kv(const amoeba_layout* layout, int32_t d
  * Attention of the new tokens over the cache: query head h of the row at cache index p uses key head h / (Hq/Hkv) and
  * sees the cached tokens i with p - window < i <= p (window 0: i <= p),
  *   out = sum_i softmax_i(scale * q . k_i) v_i,   lse = log sum_i exp(scale * q . k_i)
+ * scale is positive and finite (INVALID_ARG otherwise).
  * A row that sees nothing (more new tokens than cached ones, an empty cache, only bad blocks) gets out = 0 and
  * lse = -inf.  d_lse: float [num_rows][num_q_heads], or NULL.  Logits, softmax and sums are held in 32 bits; the
  * weights are rounded to the element type for the product with the values.

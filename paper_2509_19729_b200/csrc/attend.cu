@@ -373,7 +373,7 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     if ((st = check_elements(layout, dtype)) != AMOEBA_OK) return st;
     if ((st = make_cache_view(layout, layer, pools, &p.cache)) != AMOEBA_OK) return st;
     if ((st = make_batch(batch, &p.batch)) != AMOEBA_OK) return st;
-    if (!d_status || window < 0) return AMOEBA_ERR_INVALID_ARG;
+    if (!d_status || window < 0 || !positive(scale)) return AMOEBA_ERR_INVALID_ARG;
     const amoeba_model& m = layout->model;
     const int64_t row = (int64_t)m.num_q_heads / layout->tp * m.head_dim;
     if ((st = make_rows(layout, q, q_stride, row, &p.q)) != AMOEBA_OK) return st;

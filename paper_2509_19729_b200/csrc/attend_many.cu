@@ -62,21 +62,33 @@ __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-__device__ __forceinline__ void umma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// Issued by the lane whose `leader` is 1; the whole warp comes here together, so that the operands stay in uniform registers.
+__device__ __forceinline__ void umma_smem(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate),
+        "r"(leader)
         : "memory");
 }
-__device__ __forceinline__ void umma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void umma_tmem(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate),
+        "r"(leader)
         : "memory");
 }
 // The barrier gets one arrival when all products issued so far are done.
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+__device__ __forceinline__ void umma_commit(uint32_t leader, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t is;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is;
 }
 
 // Shared-memory operand in the 128-byte swizzle: groups of eight 128-byte rows 1 KiB apart; `leading` bytes from one
@@ -110,43 +122,52 @@ __device__ __forceinline__ Part part_of(const Shape& sh, const Walk& w, int64_t 
 }
 
 // ---- loading
+// One arrival of this thread, when all the asynchronous loads that it has started are done.  The products' warp makes them
+// visible to the tensor core (fence_async_smem after its wait): a fence here would wait for the loads still in flight.
+__device__ __forceinline__ void arrive_when_loaded(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 template <int D>
 struct Loader {
     const AttendParams& p;
-    char* smem;  // two query tiles, then the ring
+    const uint32_t smem;  // two query tiles, then the ring
     ManyBarriers& b;
     const int warp, lane;
     int slot = 0;
-    uint32_t phase = 1;     // of `empty`: the first round waits for nothing
-    int pending = 0;        // started, not yet announced; at most 2 + 1
-    int announce_slot = 0;
-    static constexpr int kChunks = D / 8, kStep = 32 / kChunks;
+    uint32_t phase = 1;  // of `empty`: the first round waits for nothing
+    const char* head = nullptr;        // of the unit: the key head's part of its pool,
+    const int32_t* table = nullptr;    // the sequence's blocks
+    static constexpr int kTile = ManyShape<D>::kTileBytes;
+    static constexpr int kChunks = D / 8, kStep = 32 / kChunks;  // a warp loads kStep rows at a time
 
-    // Where the 16 groups of eight tokens of a tile lie in a head's part of the pool, one per lane; -1: no token that is
-    // seen, or a bad block.
-    __device__ __forceinline__ int64_t groups(const Walk& w) const {
+    __device__ __forceinline__ void open(const Walk& w) {
+        head = p.cache.head_base(w.h);
+        table = p.batch.table + (int64_t)w.s * p.batch.max_blocks;
+    }
+    // Where the 16 groups of eight tokens of the tile at key0 lie in a head's part of the pool, one per lane; -1: no token
+    // that is seen, or a bad block.
+    __device__ __forceinline__ int64_t groups(const Range& range, int key0) const {
         const CacheView& v = p.cache;
-        const int key = w.range.base + w.t * kManyTile + lane * 8;
-        if (v.block_tokens % 8 || lane >= 16 || key >= w.range.hi || key + 8 <= w.range.lo) return -1;
-        const int i = key / v.block_tokens, block = p.batch.table[(int64_t)w.s * p.batch.max_blocks + i];
+        const int key = key0 + lane * 8;
+        if (v.block_tokens % 8 || lane >= 16 || key >= range.hi || key + 8 <= range.lo) return -1;
+        const int i = key / v.block_tokens, block = table[i];
         return block >= 0 && block < v.num_blocks ? block * v.block_stride + (key - i * v.block_tokens) * v.tok_stride : -1;
     }
     // Starts the loads of the tile's keys (kv = 0) or values (1).
-    __device__ __forceinline__ bool tile(const Walk& w, int64_t at, int kv) {
+    __device__ __forceinline__ bool tile(const Range& range, int key0, int64_t at, int kv) {
         const CacheView& v = p.cache;
-        if (!__all_sync(~0u, mbar_wait_bounded(&b.empty[slot], phase, 0, &b.abort))) return false;
         const int c = lane % kChunks, sub = lane / kChunks;
-        const uint32_t dst = smem_u32(smem + (2 + slot) * ManyShape<D>::kTileBytes);
-        const char* head = v.head_base(w.h) + kv * v.kv_stride;
-        const int key0 = w.range.base + w.t * kManyTile;
-        const bool whole = key0 >= w.range.lo && key0 + kManyTile <= w.range.hi && __all_sync(~0u, lane >= 16 || at >= 0);
+        const char* from = head + kv * v.kv_stride + c * 16;
+        const bool whole = key0 >= range.lo && key0 + kManyTile <= range.hi && __all_sync(~0u, lane >= 16 || at >= 0);
+        if (!__all_sync(~0u, mbar_wait_bounded(&b.empty[slot], phase, 0, &b.abort))) return false;
+        const uint32_t dst = smem + (2 + slot) * kTile;
         if (whole) {
-            const char* from = head + sub * v.tok_stride + c * 16;
+            const char* first = from + sub * v.tok_stride;
             const int64_t step = kStep * v.tok_stride;
 #pragma unroll
             for (int j = 0; j < (16 + kLoadWarps - 1) / kLoadWarps; ++j) {
                 const int g = warp + j * kLoadWarps;
-                const char* src = from + __shfl_sync(~0u, at, g & 15);
+                const char* src = first + __shfl_sync(~0u, at, g & 15);
                 if (g < 16) {
 #pragma unroll
                     for (int i = 0; i < 8 / kStep; ++i)
@@ -154,132 +175,128 @@ struct Loader {
                 }
             }
         } else {
+#pragma unroll 1
             for (int g = warp; g < 16; g += kLoadWarps) {
                 const int64_t own = __shfl_sync(~0u, at, g);
+#pragma unroll 1
                 for (int i = 0; i < 8 / kStep; ++i) {
                     const int r = g * 8 + i * kStep + sub, key = key0 + r;
-                    bool in = key >= w.range.lo && key < w.range.hi;
+                    bool in = key >= range.lo && key < range.hi;
                     const char* src = head;
                     if (v.block_tokens % 8 == 0) {
                         in = in && own >= 0;
-                        if (in) src = head + own + r % 8 * v.tok_stride + c * 16;
+                        if (in) src = from + own + r % 8 * v.tok_stride;
                     } else if (in) {
-                        const int block = p.batch.table[(int64_t)w.s * p.batch.max_blocks + key / v.block_tokens];
+                        const int block = table[key / v.block_tokens];
                         in = block >= 0 && block < v.num_blocks;
-                        if (in) src = head + block * v.block_stride + key % v.block_tokens * v.tok_stride + c * 16;
+                        if (in) src = from + block * v.block_stride + key % v.block_tokens * v.tok_stride;
                     }
                     cp_async16(dst + tile_offset(r, c), src, in ? 16 : 0);
                 }
             }
         }
-        cp_async_commit();
+        arrive_when_loaded(&b.full[slot]);
         if (++slot == ManyShape<D>::kStages) slot = 0, phase ^= 1;
-        if (++pending > 2) announce<2>();
         return true;
     }
-    // Tells the products that the oldest pending tile, and all but kLeft groups, are there.
-    template <int kLeft>
-    __device__ __forceinline__ void announce() {
-        cp_async_wait<kLeft>();
-        fence_async_smem();
-        mbar_arrive(&b.full[announce_slot]);
-        if (++announce_slot == ManyShape<D>::kStages) announce_slot = 0;
-        --pending;
-    }
-    __device__ __forceinline__ void announce_all() {
-        cp_async_wait<0>();
-        fence_async_smem();
-        while (pending > 0) {
-            mbar_arrive(&b.full[announce_slot]);
-            if (++announce_slot == ManyShape<D>::kStages) announce_slot = 0;
-            --pending;
-        }
-    }
     __device__ __forceinline__ bool queries(const Walk& w, const Part& part, uint32_t q_phase) {
-        announce_all();
-        if (!__all_sync(~0u, mbar_wait_bounded(&b.q_empty, q_phase, 0, &b.abort))) return false;
-        const uint32_t dst = smem_u32(smem);
         const int c = lane % kChunks, sub = lane / kChunks;
-        for (int r = warp * kStep + sub; r < part.q_tiles * 128; r += kLoadWarps * kStep) {
-            const bool in = r < part.rows;
-            const char* src = in ? row_of<D>(p.q, p, w.seq, w.h, w.m * kManyRows + r) + c * 16 : p.q.base[0];
-            cp_async16(dst + r / 128 * ManyShape<D>::kTileBytes + tile_offset(r % 128, c), src, in ? 16 : 0);
+        const int worker = w.h / p.cache.heads, g = p.shape.group;
+        const char* base = p.q.base[worker] + (int64_t)w.seq.q0 * p.q.stride + (w.h - worker * p.cache.heads) * g * (D * 2) + c * 16;
+        bool waited = false;
+        for (int first = warp * 32; first < part.q_tiles * 128; first += kLoadWarps * 32) {
+            const int r = first + lane, row = w.m * kManyRows + r, tok = row / g;
+            const int64_t mine = r < part.rows ? tok * p.q.stride + (row - tok * g) * (D * 2) : -1;
+            if (!waited && !__all_sync(~0u, mbar_wait_bounded(&b.q_empty, q_phase, 0, &b.abort))) return false;
+            waited = true;
+            const uint32_t dst = smem + first / 128 * kTile;
+#pragma unroll
+            for (int i = 0; i < 32; i += kStep) {
+                const int64_t off = __shfl_sync(~0u, mine, i + sub);
+                cp_async16(dst + tile_offset(first % 128 + i + sub, c), base + max(off, (int64_t)0), off >= 0 ? 16 : 0);
+            }
         }
-        cp_async_commit();
-        cp_async_wait<0>();
-        fence_async_smem();
-        mbar_arrive(&b.q_full);
+        arrive_when_loaded(&b.q_full);
         return true;
     }
 };
 
 template <int D>
 __device__ void load_loop(const AttendParams& p, char* smem, ManyBarriers& b, Walk w, int64_t n) {
-    Loader<D> load{p, smem, b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32};
+    Loader<D> load{p, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32};
     uint32_t q_phase = 1;
     bool ok = true;
     while (ok && n > 0) {
         const Part part = part_of(p.shape, w, n);
+        load.open(w);
+        int key0 = w.range.base + w.t * kManyTile;
+        int64_t at = load.groups(w.range, key0);
         ok = load.queries(w, part, q_phase);
         q_phase ^= 1;
-        int64_t at = load.groups(w);
-        for (int i = 0; ok && i < part.tiles; ++i) {
-            ok = load.tile(w, at, 0);
-            Walk next = w;
-            ++next.t;
-            const int64_t next_at = i + 1 < part.tiles ? load.groups(next) : -1;
-            if (ok) ok = load.tile(w, at, 1);
-            at = next_at;
-            if (i + 1 < part.tiles) ++w.t;
+        for (int i = 0; ok && i < part.tiles; ++i, key0 += kManyTile) {
+            ok = load.tile(w.range, key0, at, 0);
+            const int64_t next = i + 1 < part.tiles ? load.groups(w.range, key0 + kManyTile) : -1;
+            if (ok) ok = load.tile(w.range, key0, at, 1);
+            at = next;
         }
         n -= part.tiles;
+        w.t += part.tiles - 1;
         if (n > 0) w.next(p.shape, p.batch, p.cache.block_tokens);
     }
-    load.announce_all();
+    cp_async_commit();
+    cp_async_wait<0>();
     if (!ok) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
 }
 
-// ---- products: one thread
+// ---- products: one warp, one of its lanes issues
 template <class T, int D>
 __device__ bool multiply(const AttendParams& p, uint32_t smem, ManyBarriers& b, Walk w, int64_t n) {
     constexpr int kTile = ManyShape<D>::kTileBytes, kStages = ManyShape<D>::kStages;
     constexpr uint32_t kS = product<T>(128, false), kO = product<T>(D, true);
-    const uint32_t tmem = b.tmem;
+    const uint32_t tmem = __shfl_sync(~0u, b.tmem, 0), leader = elect_one();
     int slot = 0;  // of the next K; V is the one behind
     uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, 0, &b.abort); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
+    const uint64_t q_op = operand(smem, 16);
     auto logits = [&](int t, int k_slot) {
+        const uint64_t k_op = operand(smem + (2 + __shfl_sync(~0u, k_slot, 0)) * kTile, 16);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-            const uint32_t step = k / 4 * (128 * 128) + k % 4 * 32;
-            umma_smem(tmem + t * 128, operand(smem + t * kTile + step, 16), operand(smem + (2 + k_slot) * kTile + step, 16), kS, k > 0);
+            const uint32_t step = (k / 4 * (128 * 128) + k % 4 * 32) >> 4;
+            umma_smem(leader, tmem + t * 128, q_op + (t * kTile >> 4) + step, k_op + step, kS, k > 0);
         }
     };
     auto weigh = [&](int t, int v_slot, bool accumulate) {
+        const uint64_t v_op = operand(smem + (2 + __shfl_sync(~0u, v_slot, 0)) * kTile, 128 * 128);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            umma_tmem(tmem + 256 + t * D, tmem + t * 128 + k * 8, operand(smem + (2 + v_slot) * kTile + k * 2048, 128 * 128), kO,
-                      accumulate || k > 0);
+            umma_tmem(leader, tmem + 256 + t * D, tmem + t * 128 + k * 8, v_op + (k * 2048 >> 4), kO, accumulate || k > 0);
     };
     while (n > 0) {
         const Part part = part_of(p.shape, w, n);
         if (!wait(&b.q_full, q_phase)) return false;
         q_phase ^= 1;
         if (!wait(&b.full[slot], phase)) return false;
+        fence_async_smem();
         tmem_fence_after();
-        for (int t = 0; t < part.q_tiles; ++t) {
+        #pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if (t >= part.q_tiles) break;
             logits(t, slot);
-            umma_commit(&b.s_full[t]);
+            umma_commit(leader, &b.s_full[t]);
         }
-        umma_commit(&b.empty[slot]);
-        if (part.tiles == 1) umma_commit(&b.q_empty);
+        umma_commit(leader, &b.empty[slot]);
+        if (part.tiles == 1) umma_commit(leader, &b.q_empty);
         for (int i = 0; i < part.tiles; ++i) {
             int v_slot = slot + 1, k_slot = slot + 2;
             uint32_t v_phase = phase, k_phase = phase;
             if (v_slot >= kStages) v_slot -= kStages, v_phase ^= 1;
             if (k_slot >= kStages) k_slot -= kStages, k_phase ^= 1;
             if (!wait(&b.full[v_slot], v_phase)) return false;
-            for (int t = 0; t < part.q_tiles; ++t) {
+            fence_async_smem();
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (t >= part.q_tiles) break;
                 if (i == 0) {
                     if (!wait(&b.o_free[t], o_phase[t])) return false;
                     o_phase[t] ^= 1;
@@ -288,16 +305,19 @@ __device__ bool multiply(const AttendParams& p, uint32_t smem, ManyBarriers& b, 
                 p_phase[t] ^= 1;
                 tmem_fence_after();
                 weigh(t, v_slot, i > 0);
-                umma_commit(&b.o_full[t]);
+                umma_commit(leader, &b.o_full[t]);
                 if (i + 1 < part.tiles) {
-                    if (t == 0 && !wait(&b.full[k_slot], k_phase)) return false;
+                    if (t == 0) {
+                        if (!wait(&b.full[k_slot], k_phase)) return false;
+                        fence_async_smem();
+                    }
                     logits(t, k_slot);
-                    umma_commit(&b.s_full[t]);
+                    umma_commit(leader, &b.s_full[t]);
                 }
             }
-            umma_commit(&b.empty[v_slot]);
-            if (i + 1 < part.tiles) umma_commit(&b.empty[k_slot]);
-            if (i + 2 == part.tiles) umma_commit(&b.q_empty);
+            umma_commit(leader, &b.empty[v_slot]);
+            if (i + 1 < part.tiles) umma_commit(leader, &b.empty[k_slot]);
+            if (i + 2 == part.tiles) umma_commit(leader, &b.q_empty);
             slot = k_slot, phase = k_phase;
         }
         n -= part.tiles;
@@ -306,16 +326,111 @@ __device__ bool multiply(const AttendParams& p, uint32_t smem, ManyBarriers& b, 
     }
     return true;
 }
+// Waits for what `multiply` has issued, also after it gave up.
+__device__ __forceinline__ void drain_products(ManyBarriers& b) {
+    umma_commit(elect_one(), &b.drain);
+    mbar_drain(&b.drain, 0);
+    __syncwarp();
+}
 
 // ---- softmax: a thread per row
+// Bit i of `see`: the row sees token key0 + i.  table: null, or the unit has bad blocks.
+__device__ __noinline__ void visible(uint32_t (&see)[4], int key0, int lo, int hi, const Range& range, const int32_t* table,
+                                     const CacheView& v) {
+    for (int j = 0; j < 4; ++j) {
+        const int first = key0 + j * 32, a = min(max(lo - first, 0), 32), b = min(max(hi - first, 0), 32);
+        uint32_t m = b > a ? (~0u >> (32 - (b - a))) << a : 0u;
+        for (int k = 0; table && k < 32; ++k)
+            if (m >> k & 1u) {
+                const int key = first + k;
+                const int block = key < range.hi ? table[key / v.block_tokens] : -1;
+                if (block < 0 || block >= v.num_blocks) m &= ~(1u << k);
+            }
+        see[j] = m;
+    }
+}
+__device__ __forceinline__ void hide(uint32_t (&s)[32], uint32_t see) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+        if (!(see >> k & 1u)) s[k] = 0xff800000u;  // -infinity
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// Two 32-bit values at a time.
+__device__ __forceinline__ uint64_t pair2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// The largest of the row's logits that it sees.  The row is read once more for the weights: kept, it would fill 128 registers.
+template <bool kCut>
+__device__ __forceinline__ float row_max(uint32_t s_tmem, const uint32_t (&see)[4]) {
+    uint32_t s[4][32];
+    float top[4];
+    tmem_load32(s[0], s_tmem);
+    tmem_load32(s[1], s_tmem + 32);
+    tmem_load_wait();
+    tmem_load32(s[2], s_tmem + 64);
+    tmem_load32(s[3], s_tmem + 96);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (j == 2) tmem_load_wait();
+        if (kCut) hide(s[j], see[j]);
+        top[j] = __uint_as_float(s[j][0]);
+#pragma unroll
+        for (int k = 1; k < 31; k += 2) top[j] = max3(top[j], __uint_as_float(s[j][k]), __uint_as_float(s[j][k + 1]));
+        top[j] = fmaxf(top[j], __uint_as_float(s[j][31]));
+    }
+    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+// Writes the weights 2^(c * logit - ref) over the logits, in 16 bits, and returns their sum in 32.
+template <class T, bool kCut>
+__device__ __forceinline__ float row_weights(uint32_t s_tmem, const uint32_t (&see)[4], float c, float ref) {
+    const uint64_t c2 = pair2(c, c), ref2 = pair2(-ref, -ref);
+    uint64_t sum[2] = {0, 0};
+    uint32_t s[2][32], w16[32];
+    tmem_load32(s[0], s_tmem);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        tmem_load_wait();
+        if (j < 3) tmem_load32(s[(j + 1) % 2], s_tmem + (j + 1) * 32);
+        if (kCut) hide(s[j % 2], see[j]);
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+            float x, y;
+            split2(fma2(pair2(__uint_as_float(s[j % 2][k]), __uint_as_float(s[j % 2][k + 1])), c2, ref2), x, y);
+            x = fast_exp2(x), y = fast_exp2(y);
+            sum[k / 2 % 2] = add2(sum[k / 2 % 2], pair2(x, y));
+            w16[j % 2 * 16 + k / 2] = Elem<T>::pack(x, y);
+        }
+        if (j % 2) tmem_store32(s_tmem + j / 2 * 32, w16);  // over logits that have been read
+    }
+    float a, b;
+    split2(add2(sum[0], sum[1]), a, b);
+    return a + b;
+}
+
 template <class T, int D>
 __device__ bool softmax(const AttendParams& p, ManyBarriers& b, Walk w, int64_t n) {
     const Shape& sh = p.shape;
     const int t = threadIdx.x / 128, r = threadIdx.x;  // row of the unit
     const uint32_t lanes = (uint32_t)(threadIdx.x % 128 / 32 * 32) << 16;
     const uint32_t s_tmem = b.tmem + lanes + t * 128, o_tmem = b.tmem + lanes + 256 + t * D;
-    const float c = p.scale_log2 == 0.f ? 1e-30f : fabsf(p.scale_log2);  // hidden logits are -infinity: c may not be 0
-    const bool flip = p.scale_log2 < 0.f;
+    const float c = p.scale_log2;
     uint32_t s_phase = 0, o_phase = 0;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort));  // and the warp is together again
@@ -344,36 +459,10 @@ __device__ bool softmax(const AttendParams& p, ManyBarriers& b, Walk w, int64_t 
                 if (!wait(&b.s_full[t], s_phase)) return false;
                 s_phase ^= 1;
                 tmem_fence_after();
-                uint32_t s[4][32];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) tmem_load32(s[j], s_tmem + j * 32);
-                tmem_load_wait();
-                if (flip) {
-#pragma unroll
-                    for (int j = 0; j < 128; ++j) s[j / 32][j % 32] ^= 0x80000000u;
-                }
-                if (__any_sync(~0u, key0 + kManyTile > see_hi || key0 < see_lo)) {
-#pragma unroll
-                    for (int j = 0; j < 128; ++j)
-                        if (key0 + j >= see_hi || key0 + j < see_lo) s[j / 32][j % 32] = __float_as_uint(-INFINITY);
-                }
-                if (bad) {
-#pragma unroll
-                    for (int j = 0; j < 128; ++j) {
-                        const int key = key0 + j;
-                        if (key < w.range.lo || key >= w.range.hi) continue;
-                        const int block = table[key / p.cache.block_tokens];
-                        if (block < 0 || block >= p.cache.num_blocks) s[j / 32][j % 32] = __float_as_uint(-INFINITY);
-                    }
-                }
-                float top[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    top[j] = __uint_as_float(s[j][0]);
-#pragma unroll
-                    for (int k = 1; k < 32; ++k) top[j] = fmaxf(top[j], __uint_as_float(s[j][k]));
-                }
-                const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
+                uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
+                const bool cut = __any_sync(~0u, key0 + kManyTile > see_hi || key0 < see_lo) || bad;
+                if (cut) visible(see, key0, see_lo, see_hi, w.range, bad ? table : nullptr, p.cache);
+                const float m = (cut ? row_max<true>(s_tmem, see) : row_max<false>(s_tmem, see)) * c;
                 const bool raise = m > m_ref + kRaise || (m_ref == -INFINITY && m > -INFINITY);
                 if (__any_sync(~0u, raise)) {
                     const float m_new = raise ? m : m_ref;
@@ -395,21 +484,7 @@ __device__ bool softmax(const AttendParams& p, ManyBarriers& b, Walk w, int64_t 
                     }
                 }
                 const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    uint32_t w16[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        const int e = j * 64 + 2 * k;
-                        const float x = fast_exp2(fmaf(__uint_as_float(s[e / 32][e % 32]), c, -ref));
-                        const float y = fast_exp2(fmaf(__uint_as_float(s[e / 32][e % 32 + 1]), c, -ref));
-                        sum[k % 2 * 2] += x, sum[k % 2 * 2 + 1] += y;
-                        w16[k] = Elem<T>::pack(x, y);
-                    }
-                    tmem_store32(s_tmem + j * 32, w16);
-                }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                l += cut ? row_weights<T, true>(s_tmem, see, c, ref) : row_weights<T, false>(s_tmem, see, c, ref);
                 tmem_store_wait();
                 tmem_fence_before();
                 mbar_arrive(&b.p_full[t]);
@@ -485,12 +560,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
         if (warp == 8) {
-            if (threadIdx.x % 32 == 0) {
-                if (!multiply<T, D>(p, smem_u32(smem), b, w, n)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
-                umma_commit(&b.drain);
-                mbar_drain(&b.drain, 0);
-            }
+            if (!multiply<T, D>(p, smem_u32(smem), b, w, n)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
             __syncwarp();
+            drain_products(b);
         } else {
             load_loop<D>(p, smem, b, w, n);
         }

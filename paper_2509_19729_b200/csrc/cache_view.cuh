@@ -1,5 +1,6 @@
 // One layer of an instance's paged cache as the serving operators address it, and the batch of new tokens.
 #pragma once
+#include <cmath>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -155,6 +156,8 @@ inline amoeba_status make_rows(const amoeba_layout* l, const void* const* ptrs, 
     }
     return AMOEBA_OK;
 }
+
+inline bool positive(float x) { return x > 0.f && x < INFINITY; }
 
 inline amoeba_status launch_result() {
     if (cudaGetLastError() != cudaSuccess) return AMOEBA_ERR_CUDA;

@@ -102,6 +102,8 @@ def test_attend_and_scores_refuse():
     assert call("attend", q=q, out=q) == INV and call("attend", out=None) == INV and call("attend", outs=8) == INV
     assert call("attend", window=-1) == INV and call("scores", window=-1) == INV
     assert call("attend", ws=None) == INV and call("attend", ws=PTR + 8) == ALI
+    for scale in (0.0, -1.0, float("inf"), float("nan")):
+        assert call("attend", scale=scale) == INV and call("scores", scale=scale) == INV
     need = C.c_int64()
     assert B._load().amoeba_attend_workspace_bytes(C.byref(A.make_layout(M, 2, 10)), C.byref(batch()), C.byref(need)) == 0
     assert call("attend", ws_bytes=need.value - 1) == INV
