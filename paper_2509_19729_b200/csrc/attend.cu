@@ -52,7 +52,7 @@ attend_few(const __grid_constant__ AttendParams p) {
     } else {
         int64_t total;
         int ctas;
-        n = take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &total, &ctas, 1, p.prefix, p.status);
+        n = take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &total, &ctas, 1, p.prefix, p.begins, p.status);
     }
     if (n == 0) return;
 
@@ -235,14 +235,12 @@ attend_few(const __grid_constant__ AttendParams p) {
 
 // Joins the parts of the units that were cut: one CTA per unit.
 template <class T, int D>
-__global__ void __launch_bounds__(128) attend_join(const __grid_constant__ AttendParams p, int max_ctas) {
+__global__ void __launch_bounds__(128) attend_join(const __grid_constant__ AttendParams p, int ctas) {
     const Shape& sh = p.shape;
     const int unit = blockIdx.x, m = unit % p.max_row_tiles, h = unit / p.max_row_tiles % sh.kv_heads;
     const int s = unit / (p.max_row_tiles * sh.kv_heads);
     const Seq q = sequence(p.batch, s, p.cache.block_tokens);
     if (m >= row_tiles(sh, q)) return;
-    const int64_t total = p.prefix[p.batch.num_seqs];
-    const int ctas = (int)max((int64_t)1, min((int64_t)max_ctas, total));
     int64_t first = p.prefix[s], per_head = 0;
     int n = 0;
     for (int i = 0; i < row_tiles(sh, q); ++i) {
@@ -252,17 +250,20 @@ __global__ void __launch_bounds__(128) attend_join(const __grid_constant__ Atten
         per_head += k;
     }
     first += h * per_head;
-    const int c0 = share_of(total, ctas, first), c1 = share_of(total, ctas, first + n - 1);
+    if (first + n <= p.begins[0]) return;
+    const int c0 = share_of(p.begins, ctas, first), c1 = share_of(p.begins, ctas, first + n - 1);
     if (c0 == c1) return;
     const int R = sh.rows, rows = min(R, q.qn * sh.group - m * R);
     for (int i = threadIdx.x; i < rows * (D / 4); i += blockDim.x) {
         const int r = i / (D / 4), d = i % (D / 4) * 4;
         float top = -INFINITY;
-        for (int c = c0; c <= c1; ++c) top = fmaxf(top, p.part_m[(int64_t)(2 * c + (c == c0)) * R + r]);
+        for (int c = c0; c <= c1; ++c)
+            if (p.begins[c] < p.begins[c + 1]) top = fmaxf(top, p.part_m[(int64_t)(2 * c + (c == c0)) * R + r]);
         const float ref = top == -INFINITY ? 0.f : top;
         float l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int c = c0; c <= c1; ++c) {
+            if (p.begins[c] == p.begins[c + 1]) continue;
             const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
             const float f = fast_exp2(p.part_m[part] - ref);
             const float4 x = *reinterpret_cast<const float4*>(p.part_o + part * D + d);
@@ -278,16 +279,17 @@ __global__ void __launch_bounds__(128) attend_join(const __grid_constant__ Atten
 }
 
 // The workspace holds the parts of cut units, two for each CTA; these bound the grids without asking the device.
-constexpr int kMaxSms = 192, kMaxFewCtas = 2 * kMaxSms;
+constexpr int kMaxFewCtas = 2 * kMaxSms;
 constexpr int kMaxFewRows = 32;
 
 static int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
 
 // One kernel's part of the workspace: the sequences' first tiles, then the parts.
 static int64_t workspace_part(AttendParams* p, char* ws, int64_t num_seqs, int64_t parts, int64_t rows, int head_dim) {
-    const int64_t o = align16((num_seqs + 1) * 8), m = o + parts * rows * head_dim * 4, l = m + parts * rows * 4;
+    const int64_t b = align16((num_seqs + 1) * 8), o = b + align16((kMaxFewCtas + 1) * 8), m = o + parts * rows * head_dim * 4, l = m + parts * rows * 4;
     if (p) {
         p->prefix = reinterpret_cast<int64_t*>(ws);
+        p->begins = reinterpret_cast<int64_t*>(ws + b);
         p->part_o = reinterpret_cast<float*>(ws + o);
         p->part_m = reinterpret_cast<float*>(ws + m);
         p->part_l = reinterpret_cast<float*>(ws + l);

@@ -12,6 +12,7 @@ struct AttendParams {
     float* lse;
     int32_t* status;
     int64_t* prefix;         // [num_seqs + 1]: first tile of every sequence
+    int64_t* begins;         // [CTAs + 1]: first tile of every share; units before the first of all are whole
     float *part_o, *part_m, *part_l;  // of the cut units: [2 * CTAs][rows][D], [2 * CTAs][rows]
     float scale_log2;        // scale * log2(e): the softmax runs in powers of two
     int32_t q_heads;         // of all workers
@@ -33,6 +34,7 @@ __device__ __forceinline__ float* lse_of(const AttendParams& p, const Seq& q, in
 
 // The kernel for many rows (attend_many.cu): 256 rows a unit, 128 tokens a tile.
 constexpr int kManyRows = 256, kManyTile = 128;
+constexpr int kMaxSms = 192;  // bounds the grids, and so the workspace, without asking the device
 amoeba_status launch_attend_many(const AttendParams& p, int32_t dtype, int head_dim, int ctas, cudaStream_t stream);
 
 }  // namespace amoeba

@@ -106,20 +106,188 @@ __device__ constexpr uint32_t product(int n, bool b_rows) {
 // Byte offset of 16-byte chunk c of row r in a tile: 64-element halves of all rows one behind the other.
 __device__ __forceinline__ int tile_offset(int r, int c) { return c / 8 * (128 * 128) + r * 128 + ((c ^ r) & 7) * 16; }
 
-// The part of a unit that a CTA has in its share.
-struct Part {
-    int tiles, q_tiles, rows;  // rows of the unit, 1 .. 256
-    bool from_start, to_end;
+// ---- shares
+// CTAs that work on the same keys at the same time find them in L2 (a batch's cache does not fit there, and every unit reads
+// all of its sequence's).  So the units are dealt out whole and in order as long as there are plenty, and neighbours run through
+// the same keys side by side; the last one or two units per CTA are cut so that all CTAs finish together, whatever the
+// units before have cost each.  With more sequences than the table below holds, all units are cut as in walk.cuh.
+constexpr int kDealtSeqs = 256;
+struct Share {
+    int32_t first_unit[kDealtSeqs + 1];  // of every sequence, and the end
+    int32_t rounds;                      // units dealt to each
+    int64_t begin, end;                  // of this CTA's run of tiles of the cut units
+    int32_t begin_seq;
+    int64_t begin_off;
 };
-__device__ __forceinline__ Part part_of(const Shape& sh, const Walk& w, int64_t left) {
-    Part p;
-    p.tiles = (int)min(left, (int64_t)(w.range.tiles - w.t));
-    p.rows = min(kManyRows, w.seq.qn * sh.group - w.m * kManyRows);
-    p.q_tiles = p.rows > 128 ? 2 : 1;
-    p.from_start = w.t == 0;
-    p.to_end = w.t + p.tiles == w.range.tiles;
-    return p;
+
+// All threads of the block.  False: this CTA has nothing to do.  done: [kMaxSms] for the tiles of the units dealt to every CTA.
+__device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
+    __shared__ int64_t s_warp[kManyThreads / 32];
+    const Shape& shape = p.shape;
+    const Batch& b = p.batch;
+    const int tid = threadIdx.x, ctas = gridDim.x, T = p.cache.block_tokens, S = b.num_seqs;
+    sh.rounds = 0;
+    if (S > kDealtSeqs) {
+        Walk w;
+        int64_t total;
+        int n_ctas;
+        const int64_t n = take_share<kManyThreads>(shape, b, T, &w, &total, &n_ctas, 1, p.prefix, p.begins, p.status);
+        if (tid == 0) {
+            sh.begin = share_begin(total, n_ctas, blockIdx.x), sh.end = sh.begin + n;
+            if (n) {
+                sh.begin_seq = w.s;
+                int64_t off = w.t + w.h * head_tiles(shape, w.seq);
+                for (int m = 0; m < w.m; ++m) off += row_tile_range(shape, w.seq, m).tiles;
+                sh.begin_off = off;
+            }
+        }
+        __syncthreads();
+        return n > 0;
+    }
+    // units and tiles before every sequence
+    int32_t units = 0;
+    int64_t tiles = 0;
+    for (int base = 0; base < S; base += kManyThreads) {
+        const int s = base + tid;
+        int64_t n_units = 0, n_tiles = 0;
+        if (s < S) {
+            const Seq q = sequence(b, s, T);
+            if (!q.ok && blockIdx.x == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
+            n_units = (int64_t)shape.kv_heads * row_tiles(shape, q);
+            n_tiles = shape.kv_heads * head_tiles(shape, q);
+        }
+        int64_t u = n_units, t = n_tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t uu = __shfl_up_sync(~0u, u, o), tt = __shfl_up_sync(~0u, t, o);
+            if (tid % 32 >= o) u += uu, t += tt;
+        }
+        __syncthreads();
+        if (tid % 32 == 31) s_warp[tid / 32] = u;
+        __syncthreads();
+        int64_t before = units;
+        for (int w = 0; w < kManyThreads / 32; ++w) {
+            if (w < tid / 32) before += s_warp[w];
+            units += (int32_t)s_warp[w];
+        }
+        if (s < S) sh.first_unit[s] = (int32_t)(before + u - n_units);
+        __syncthreads();
+        if (tid % 32 == 31) s_warp[tid / 32] = t;
+        __syncthreads();
+        before = tiles;
+        for (int w = 0; w < kManyThreads / 32; ++w) {
+            if (w < tid / 32) before += s_warp[w];
+            tiles += s_warp[w];
+        }
+        if (s < S && blockIdx.x == 0) p.prefix[s] = before + t - n_tiles;
+    }
+    for (int c = tid; c < kMaxSms; c += kManyThreads) done[c] = 0;
+    if (tid == 0) sh.first_unit[S] = units, sh.begin = sh.end = 0;
+    if (blockIdx.x == 0 && tid == 0) p.prefix[S] = tiles;
+    __syncthreads();
+    const int rounds = max(units / ctas - 1, 0), dealt = rounds * ctas;
+    if (tid == 0) sh.rounds = rounds;
+    // tiles of the dealt units, by CTA and in all (row tiles of a sequence cost the same for every head)
+    int64_t mine = 0;
+    int s = 0;
+    for (int u = tid; u < dealt; u += kManyThreads) {
+        while (sh.first_unit[s + 1] <= u) ++s;
+        const Seq q = sequence(b, s, T);
+        const int n = row_tile_range(shape, q, (u - sh.first_unit[s]) % row_tiles(shape, q)).tiles;
+        atomicAdd(&done[u % ctas], n);
+        mine += n;
+    }
+    const int64_t first_cut = block_sum<kManyThreads>(mine, s_warp);  // and the barrier behind the sums by CTA
+    // every CTA gets what it lacks to an even share, in order, until all is given out
+    const int64_t even = (tiles + ctas - 1) / ctas;
+    if (tid < 32) {
+        int64_t run = first_cut;
+        for (int base = 0; base <= ctas; base += 32) {
+            const int c = base + tid;
+            const int64_t want = c < ctas ? max(even - done[c], (int64_t)0) : 0;
+            int64_t incl = want;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int64_t up = __shfl_up_sync(~0u, incl, o);
+                if (tid >= o) incl += up;
+            }
+            const int64_t begin = min(run + incl - want, tiles), end = min(run + incl, tiles);
+            if (c == (int)blockIdx.x) sh.begin = begin, sh.end = end;
+            if (blockIdx.x == 0 && c <= ctas) p.begins[c] = c == ctas ? tiles : begin;
+            run += __shfl_sync(~0u, incl, 31);
+        }
+    }
+    __syncthreads();
+    // the sequence of this CTA's first tile
+    const int64_t at = sh.begin;
+    if (sh.end > at) {
+        int64_t run = 0;
+        for (int base = 0; base < S; base += kManyThreads) {
+            const int i = base + tid;
+            const int64_t n = i < S ? shape.kv_heads * head_tiles(shape, sequence(b, i, T)) : 0;
+            int64_t incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int64_t up = __shfl_up_sync(~0u, incl, o);
+                if (tid % 32 >= o) incl += up;
+            }
+            __syncthreads();
+            if (tid % 32 == 31) s_warp[tid / 32] = incl;
+            __syncthreads();
+            int64_t before = run;
+            for (int w = 0; w < kManyThreads / 32; ++w) {
+                if (w < tid / 32) before += s_warp[w];
+                run += s_warp[w];
+            }
+            const int64_t first = before + incl - n;
+            if (at >= first && at < first + n) sh.begin_seq = i, sh.begin_off = at - first;
+        }
+        __syncthreads();
+    }
+    return rounds > 0 || sh.end > at;
 }
+
+// The parts of units in a CTA's share, one after the other: tiles [w.t, w.t + tiles) of w's unit.
+struct Parts {
+    Walk w;
+    int32_t round = 0, tiles = 0, q_tiles, rows;  // rows of the unit, 1 .. 256
+    bool from_start, to_end, opened = false;
+    int64_t left;
+
+    __device__ __forceinline__ Parts(const Share& sh) : left(sh.end - sh.begin) {}
+    __device__ __forceinline__ bool next(const AttendParams& p, const Share& sh) {
+        const Shape& shape = p.shape;
+        if (round < sh.rounds) {
+            const int u = blockIdx.x + round++ * gridDim.x;
+            int lo = 0, hi = p.batch.num_seqs;  // first_unit[lo] <= u < first_unit[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (sh.first_unit[mid] <= u) lo = mid;
+                else hi = mid;
+            }
+            w.open(shape, p.batch, p.cache.block_tokens, lo);
+            w.to_unit(shape, u - sh.first_unit[lo]);
+            tiles = w.range.tiles;
+        } else {
+            if (left == 0) return false;
+            if (!opened) {
+                opened = true;
+                w.open(shape, p.batch, p.cache.block_tokens, sh.begin_seq);
+                w.seek(shape, sh.begin_off);
+            } else {
+                w.t += tiles - 1;
+                w.next(shape, p.batch, p.cache.block_tokens);
+            }
+            tiles = (int)min(left, (int64_t)(w.range.tiles - w.t));
+            left -= tiles;
+        }
+        rows = min(kManyRows, w.seq.qn * shape.group - w.m * kManyRows);
+        q_tiles = rows > 128 ? 2 : 1;
+        from_start = w.t == 0;
+        to_end = w.t + tiles == w.range.tiles;
+        return true;
+    }
+};
 
 // ---- loading
 // One arrival of this thread, when all the asynchronous loads that it has started are done.  The products' warp makes them
@@ -199,7 +367,8 @@ struct Loader {
         if (++slot == ManyShape<D>::kStages) slot = 0, phase ^= 1;
         return true;
     }
-    __device__ __forceinline__ bool queries(const Walk& w, const Part& part, uint32_t q_phase) {
+    __device__ __forceinline__ bool queries(const Parts& part, uint32_t q_phase) {
+        const Walk& w = part.w;
         const int c = lane % kChunks, sub = lane / kChunks;
         const int worker = w.h / p.cache.heads, g = p.shape.group;
         const char* base = p.q.base[worker] + (int64_t)w.seq.q0 * p.q.stride + (w.h - worker * p.cache.heads) * g * (D * 2) + c * 16;
@@ -222,16 +391,17 @@ struct Loader {
 };
 
 template <int D>
-__device__ void load_loop(const AttendParams& p, char* smem, ManyBarriers& b, Walk w, int64_t n) {
+__device__ void load_loop(const AttendParams& p, const Share& share, char* smem, ManyBarriers& b) {
     Loader<D> load{p, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32};
     uint32_t q_phase = 1;
     bool ok = true;
-    while (ok && n > 0) {
-        const Part part = part_of(p.shape, w, n);
+    Parts part(share);
+    while (ok && part.next(p, share)) {
+        const Walk& w = part.w;
         load.open(w);
         int key0 = w.range.base + w.t * kManyTile;
         int64_t at = load.groups(w.range, key0);
-        ok = load.queries(w, part, q_phase);
+        ok = load.queries(part, q_phase);
         q_phase ^= 1;
         for (int i = 0; ok && i < part.tiles; ++i, key0 += kManyTile) {
             ok = load.tile(w.range, key0, at, 0);
@@ -239,9 +409,6 @@ __device__ void load_loop(const AttendParams& p, char* smem, ManyBarriers& b, Wa
             if (ok) ok = load.tile(w.range, key0, at, 1);
             at = next;
         }
-        n -= part.tiles;
-        w.t += part.tiles - 1;
-        if (n > 0) w.next(p.shape, p.batch, p.cache.block_tokens);
     }
     cp_async_commit();
     cp_async_wait<0>();
@@ -250,7 +417,7 @@ __device__ void load_loop(const AttendParams& p, char* smem, ManyBarriers& b, Wa
 
 // ---- products: one warp, one of its lanes issues
 template <class T, int D>
-__device__ bool multiply(const AttendParams& p, uint32_t smem, ManyBarriers& b, Walk w, int64_t n) {
+__device__ bool multiply(const AttendParams& p, const Share& share, uint32_t smem, ManyBarriers& b) {
     constexpr int kTile = ManyShape<D>::kTileBytes, kStages = ManyShape<D>::kStages;
     constexpr uint32_t kS = product<T>(128, false), kO = product<T>(D, true);
     const uint32_t tmem = __shfl_sync(~0u, b.tmem, 0), leader = elect_one();
@@ -272,8 +439,8 @@ __device__ bool multiply(const AttendParams& p, uint32_t smem, ManyBarriers& b, 
         for (int k = 0; k < 8; ++k)
             umma_tmem(leader, tmem + 256 + t * D, tmem + t * 128 + k * 8, v_op + (k * 2048 >> 4), kO, accumulate || k > 0);
     };
-    while (n > 0) {
-        const Part part = part_of(p.shape, w, n);
+    Parts part(share);
+    while (part.next(p, share)) {
         if (!wait(&b.q_full, q_phase)) return false;
         q_phase ^= 1;
         if (!wait(&b.full[slot], phase)) return false;
@@ -320,9 +487,6 @@ __device__ bool multiply(const AttendParams& p, uint32_t smem, ManyBarriers& b, 
             if (i + 2 == part.tiles) umma_commit(leader, &b.q_empty);
             slot = k_slot, phase = k_phase;
         }
-        n -= part.tiles;
-        w.t += part.tiles - 1;
-        if (n > 0) w.next(p.shape, p.batch, p.cache.block_tokens);
     }
     return true;
 }
@@ -425,7 +589,7 @@ __device__ __forceinline__ float row_weights(uint32_t s_tmem, const uint32_t (&s
 }
 
 template <class T, int D>
-__device__ bool softmax(const AttendParams& p, ManyBarriers& b, Walk w, int64_t n) {
+__device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers& b) {
     const Shape& sh = p.shape;
     const int t = threadIdx.x / 128, r = threadIdx.x;  // row of the unit
     const uint32_t lanes = (uint32_t)(threadIdx.x % 128 / 32 * 32) << 16;
@@ -435,8 +599,9 @@ __device__ bool softmax(const AttendParams& p, ManyBarriers& b, Walk w, int64_t 
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort));  // and the warp is together again
     };
-    while (n > 0) {
-        const Part part = part_of(sh, w, n);
+    Parts part(share);
+    while (part.next(p, share)) {
+        const Walk& w = part.w;
         // a bad block anywhere in the unit: its tokens are looked up one by one below
         const int32_t* table = p.batch.table + (int64_t)w.s * p.batch.max_blocks;
         int bad = 0;
@@ -523,9 +688,6 @@ __device__ bool softmax(const AttendParams& p, ManyBarriers& b, Walk w, int64_t 
             if (there && direct && p.lse)
                 *lse_of(p, w.seq, w.h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
         }
-        n -= part.tiles;
-        w.t += part.tiles - 1;
-        if (n > 0) w.next(sh, p.batch, p.cache.block_tokens);
     }
     return true;
 }
@@ -536,11 +698,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     __shared__ ManyBarriers b;
     char* smem = smem_raw + (1024 - smem_u32(smem_raw) % 1024) % 1024;
     const int warp = threadIdx.x / 32;
-    Walk w;
-    int64_t total;
-    int ctas;
-    const int64_t n = take_share<kManyThreads>(p.shape, p.batch, p.cache.block_tokens, &w, &total, &ctas, 1, p.prefix, p.status);
-    if (n == 0) return;
+    __shared__ Share share;
+    if (!make_share(p, share, reinterpret_cast<int32_t*>(smem))) return;
+    __syncthreads();
     if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&b.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -560,15 +720,15 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
         if (warp == 8) {
-            if (!multiply<T, D>(p, smem_u32(smem), b, w, n)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+            if (!multiply<T, D>(p, share, smem_u32(smem), b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
             __syncwarp();
             drain_products(b);
         } else {
-            load_loop<D>(p, smem, b, w, n);
+            load_loop<D>(p, share, smem, b);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-        if (!softmax<T, D>(p, b, w, n)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+        if (!softmax<T, D>(p, share, b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
     }
     tmem_fence_before();
     __syncthreads();

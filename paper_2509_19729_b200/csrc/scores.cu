@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreCtas) accumulate_scores(c
     Walk walk;
     int64_t total;
     int ctas;
-    int64_t n = take_share<kScoreThreads>(sh, p.batch, p.cache.block_tokens, &walk, &total, &ctas, 1, nullptr, p.status);
+    int64_t n = take_share<kScoreThreads>(sh, p.batch, p.cache.block_tokens, &walk, &total, &ctas, 1, nullptr, nullptr, p.status);
     if (n == 0) return;
 
     Walk ahead = walk;

@@ -53,11 +53,15 @@ __device__ __forceinline__ int64_t head_tiles(const Shape& p, const Seq& q) {
 
 // First tile of CTA c's share.
 __device__ __forceinline__ int64_t share_begin(int64_t total, int ctas, int c) { return total * c / ctas; }
-__device__ __forceinline__ int share_of(int64_t total, int ctas, int64_t tile) {
-    int c = (int)min((int64_t)ctas - 1, tile * ctas / total);
-    while (share_begin(total, ctas, c + 1) <= tile) ++c;
-    while (share_begin(total, ctas, c) > tile) --c;
-    return c;
+// The CTA whose share, of those that begin at begins[0 .. ctas-1], has the tile; begins[ctas] is behind all.
+__device__ __forceinline__ int share_of(const int64_t* begins, int ctas, int64_t tile) {
+    int lo = 0, hi = ctas;  // begins[lo] <= tile < begins[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (begins[mid] <= tile) lo = mid;
+        else hi = mid;
+    }
+    return lo;
 }
 
 struct Walk {
@@ -84,6 +88,13 @@ struct Walk {
             off -= range.tiles;
         }
         t = (int)off;
+    }
+    // To the first tile of the `unit`-th unit of the open sequence.
+    __device__ __forceinline__ void to_unit(const Shape& p, int unit) {
+        h = unit / nm;
+        m = unit - h * nm;
+        t = 0;
+        range = row_tile_range(p, seq, m);
     }
     // To the next tile; the caller knows that there is one.
     __device__ __forceinline__ void next(const Shape& p, const Batch& b, int block_tokens) {
@@ -118,10 +129,11 @@ __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* shared) {
 }
 
 // This CTA's share: *total and the number of its tiles, with `walk` at the first of them.  CTA 0 reports bad sequences and
-// writes the first tile of every sequence, and the total behind them, to `prefix` (null: to nowhere).
+// writes the first tile of every sequence, and the total behind them, to `prefix` (null: to nowhere), and the first tile of
+// every CTA's share, and the total behind them, to `begins`, ended by gridDim.x + 1 entries in all.
 template <int kThreads>
 __device__ int64_t take_share(const Shape& p, const Batch& b, int block_tokens, Walk* walk, int64_t* total, int* ctas,
-                              int min_tiles, int64_t* prefix, int32_t* status) {
+                              int min_tiles, int64_t* prefix, int64_t* begins, int32_t* status) {
     __shared__ int64_t s_warp[kThreads / 32];
     __shared__ int64_t s_off;
     __shared__ int32_t s_seq;
@@ -163,7 +175,10 @@ __device__ int64_t take_share(const Shape& p, const Batch& b, int block_tokens, 
         if (begin >= first && begin < first + mine) s_seq = s, s_off = begin - first;
         if (!writes && run > begin) break;  // block-uniform
     }
-    if (writes && tid == 0) prefix[b.num_seqs] = all;
+    if (writes) {
+        if (tid == 0) prefix[b.num_seqs] = all;
+        for (int c = tid; c <= (int)gridDim.x; c += kThreads) begins[c] = c < *ctas ? share_begin(all, *ctas, c) : all;
+    }
     __syncthreads();
     if (end > begin) {
         walk->open(p, b, block_tokens, s_seq);
