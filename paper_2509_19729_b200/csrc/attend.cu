@@ -39,21 +39,20 @@ attend_few(const __grid_constant__ AttendParams p) {
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * F::kStages * F::kStage;
     const Shape& sh = p.shape;
 
-    Walk walk;
+    Walk walk{};
     int64_t n;
     if (p.whole) {
-        const int unit = blockIdx.x, m = unit % p.max_row_tiles, h = unit / p.max_row_tiles % sh.kv_heads;
-        walk.open(sh, p.batch, p.cache.block_tokens, unit / (p.max_row_tiles * sh.kv_heads));
+        walk.open(sh, p.batch, p.cache.block_tokens, blockIdx.x / sh.kv_heads);
         if (!walk.seq.ok && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
-        if (m >= walk.nm) return;
-        walk.h = h, walk.m = m;
-        walk.range = row_tile_range(sh, walk.seq, m);
-        n = walk.range.tiles;
+        walk.h = blockIdx.x % sh.kv_heads;
+        n = walk.nm ? walk.range.tiles : 0;
     } else {
-        int64_t total;
-        int ctas;
-        n = take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &total, &ctas, 1, p.prefix, p.begins, p.status);
+        int64_t begin, end;
+        take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
+        write_cut(p.cuts, walk, begin, end);
+        n = end - begin;
     }
+    grid_dependency_launch();
     if (n == 0) return;
 
     Walk ahead = walk;
@@ -233,120 +232,154 @@ attend_few(const __grid_constant__ AttendParams p) {
     }
 }
 
-// Joins the parts of the units that were cut: one CTA per unit.
-template <class T, int D>
-__global__ void __launch_bounds__(128) attend_join(const __grid_constant__ AttendParams p, int ctas) {
+// ------------------------------------------------------------------------------------------------ joining
+// Joins the parts of the units that were cut.  kWarps warps to a row: with few rows a unit may be in as many parts as there
+// are CTAs, so its four warps take every fourth part each; with many rows it is in two or three, and a warp does a row.
+template <class T, int D, int kWarps>
+__device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int block) {
     const Shape& sh = p.shape;
-    const int unit = blockIdx.x, m = unit % p.max_row_tiles, h = unit / p.max_row_tiles % sh.kv_heads;
-    const int s = unit / (p.max_row_tiles * sh.kv_heads);
-    const Seq q = sequence(p.batch, s, p.cache.block_tokens);
-    if (m >= row_tiles(sh, q)) return;
-    int64_t first = p.prefix[s], per_head = 0;
-    int n = 0;
-    for (int i = 0; i < row_tiles(sh, q); ++i) {
-        const int k = row_tile_range(sh, q, i).tiles;
-        if (i < m) first += k;
-        if (i == m) n = k;
-        per_head += k;
+    constexpr int kRows = 4 / kWarps;  // per CTA
+    const int groups = sh.rows / kRows;  // blocks for every share: its first unit is joined here if it began in the share before
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int mine = block / groups;
+    const Cut cut = p.cuts[mine];
+    if (cut.begin == cut.end || cut.t == 0) return;
+    const int64_t first = cut.begin - cut.t, last = first + cut.tiles;
+    int c0 = mine - 1;
+    while (p.cuts[c0].begin == p.cuts[c0].end) --c0;
+    if (p.cuts[c0].begin > first) return;
+    const int m = cut.m, h = cut.h, R = sh.rows;
+    const Seq q = sequence(p.batch, cut.s, p.cache.block_tokens);
+    const int rows = min(R, q.qn * sh.group - m * R);
+    const int first_row = block % groups * kRows;
+    if (first_row >= rows) return;
+    int c1 = mine;  // behind the last part
+    for (bool more = true; more; c1 += 32) {
+        const unsigned in = __ballot_sync(~0u, c1 + lane < ctas && p.cuts[c1 + lane].begin < last);
+        more = in == ~0u;
+        if (!more) c1 += __popc(in) - 32;
     }
-    first += h * per_head;
-    if (first + n <= p.begins[0]) return;
-    const int c0 = share_of(p.begins, ctas, first), c1 = share_of(p.begins, ctas, first + n - 1);
-    if (c0 == c1) return;
-    const int R = sh.rows, rows = min(R, q.qn * sh.group - m * R);
-    for (int i = threadIdx.x; i < rows * (D / 4); i += blockDim.x) {
-        const int r = i / (D / 4), d = i % (D / 4) * 4;
-        float top = -INFINITY;
-        for (int c = c0; c <= c1; ++c)
-            if (p.begins[c] < p.begins[c + 1]) top = fmaxf(top, p.part_m[(int64_t)(2 * c + (c == c0)) * R + r]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        float l = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c = c0; c <= c1; ++c) {
-            if (p.begins[c] == p.begins[c + 1]) continue;
+    constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes to a part's row, parts at once
+    const int r = first_row + (kWarps == 1 ? warp : 0), stripe = (kWarps == 1 ? 0 : warp) * kAtOnce + lane / kLanes;
+    float top = -INFINITY, l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < rows) {
+#pragma unroll 4
+        for (int c = c0 + stripe; c < c1; c += kWarps * kAtOnce) {
+            if (p.cuts[c].begin == p.cuts[c].end) continue;  // an empty share
             const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
-            const float f = fast_exp2(p.part_m[part] - ref);
-            const float4 x = *reinterpret_cast<const float4*>(p.part_o + part * D + d);
-            l += f * p.part_l[part];
-            acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
+            const float pm = p.part_m[part], pl = p.part_l[part];
+            const float4 x = *reinterpret_cast<const float4*>(p.part_o + part * D + lane % kLanes * 4);
+            const float up = fmaxf(top, pm), ref = up == -INFINITY ? 0.f : up, f = fast_exp2(top - ref), g = fast_exp2(pm - ref);
+            l = l * f + pl * g;
+            acc.x = acc.x * f + x.x * g, acc.y = acc.y * f + x.y * g, acc.z = acc.z * f + x.z * g, acc.w = acc.w * f + x.w * g;
+            top = up;
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        const int row = m * R + r;
-        *reinterpret_cast<uint2*>(row_of<D>(p.out, p, q, h, row) + d * 2) =
-            make_uint2(Elem<T>::pack(acc.x * inv, acc.y * inv), Elem<T>::pack(acc.z * inv, acc.w * inv));
-        if (d == 0 && p.lse) *lse_of(p, q, h, row) = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
     }
+    // the stripes of a row, in a fixed order
+    auto merge = [&](float top2, float l2, float4 x) {
+        const float up = fmaxf(top, top2), ref = up == -INFINITY ? 0.f : up, f = fast_exp2(top - ref), g = fast_exp2(top2 - ref);
+        l = l * f + l2 * g;
+        acc.x = acc.x * f + x.x * g, acc.y = acc.y * f + x.y * g, acc.z = acc.z * f + x.z * g, acc.w = acc.w * f + x.w * g;
+        top = up;
+    };
+    if (kAtOnce == 2) {
+        const float4 x = make_float4(__shfl_down_sync(~0u, acc.x, 16), __shfl_down_sync(~0u, acc.y, 16),
+                                     __shfl_down_sync(~0u, acc.z, 16), __shfl_down_sync(~0u, acc.w, 16));
+        const float top2 = __shfl_down_sync(~0u, top, 16), l2 = __shfl_down_sync(~0u, l, 16);
+        merge(top2, l2, x);
+    }
+    if (kWarps == 4) {
+        __shared__ float4 s_acc[4][kLanes];
+        __shared__ float s_top[4], s_l[4];
+        if (lane < kLanes) s_acc[warp][lane] = acc;
+        if (lane == 0) s_top[warp] = top, s_l[warp] = l;
+        __syncthreads();
+        if (warp) return;
+        for (int w = 1; w < 4; ++w) merge(s_top[w], s_l[w], s_acc[w][lane % kLanes]);
+    }
+    if (r >= rows || lane >= kLanes) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int row = m * R + r;
+    *reinterpret_cast<uint2*>(row_of<D>(p.out, p, q, h, row) + lane * 8) =
+        make_uint2(Elem<T>::pack(acc.x * inv, acc.y * inv), Elem<T>::pack(acc.z * inv, acc.w * inv));
+    if (lane == 0 && p.lse) *lse_of(p, q, h, row) = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+}
+// Blocks [0, few_blocks) join what attend_few has cut, the others what attend_many has.
+template <class T, int D>
+__global__ void __launch_bounds__(128) attend_join(const __grid_constant__ AttendParams few, int few_ctas, int few_blocks,
+                                                   const __grid_constant__ AttendParams many, int many_ctas) {
+    grid_dependency_wait();
+    if ((int)blockIdx.x < few_blocks) join_rows<T, D, 4>(few, few_ctas, blockIdx.x);
+    else join_rows<T, D, 1>(many, many_ctas, blockIdx.x - few_blocks);
 }
 
 // The workspace holds the parts of cut units, two for each CTA; these bound the grids without asking the device.
 constexpr int kMaxFewCtas = 2 * kMaxSms;
 constexpr int kMaxFewRows = 32;
 
-static int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
-
-// One kernel's part of the workspace: the sequences' first tiles, then the parts.
-static int64_t workspace_part(AttendParams* p, char* ws, int64_t num_seqs, int64_t parts, int64_t rows, int head_dim) {
-    const int64_t b = align16((num_seqs + 1) * 8), o = b + align16((kMaxFewCtas + 1) * 8), m = o + parts * rows * head_dim * 4, l = m + parts * rows * 4;
+// One kernel's part of the workspace: where the shares begin, then the parts.
+static int64_t workspace_part(AttendParams* p, char* ws, int64_t parts, int64_t rows, int head_dim) {
+    const int64_t o = kMaxFewCtas * (int64_t)sizeof(Cut), m = o + parts * rows * head_dim * 4, l = m + parts * rows * 4;
     if (p) {
-        p->prefix = reinterpret_cast<int64_t*>(ws);
-        p->begins = reinterpret_cast<int64_t*>(ws + b);
+        p->cuts = reinterpret_cast<Cut*>(ws);
         p->part_o = reinterpret_cast<float*>(ws + o);
         p->part_m = reinterpret_cast<float*>(ws + m);
         p->part_l = reinterpret_cast<float*>(ws + l);
     }
     return l + parts * rows * 4;
 }
-static int64_t few_workspace(AttendParams* p, char* ws, int64_t num_seqs, int head_dim) {
-    return workspace_part(p, ws, num_seqs, 2 * kMaxFewCtas, kMaxFewRows, head_dim);
+static int64_t few_workspace(AttendParams* p, char* ws, int head_dim) {
+    return workspace_part(p, ws, 2 * kMaxFewCtas, kMaxFewRows, head_dim);
 }
-static int64_t many_workspace(AttendParams* p, char* ws, int64_t num_seqs, int head_dim) {
-    return workspace_part(p, ws, num_seqs, 2 * kMaxSms, kManyRows, head_dim);
+static int64_t many_workspace(AttendParams* p, char* ws, int head_dim) {
+    return workspace_part(p, ws, 2 * kMaxSms, kManyRows, head_dim);
 }
 static int64_t rows_of(const amoeba_layout* l, int32_t max_q_len) {
     return (int64_t)max_q_len * (l->model.num_q_heads / l->model.num_kv_heads);
 }
 
-template <class T, int D>
-static amoeba_status join(const AttendParams& p, int ctas, cudaStream_t stream) {
-    attend_join<T, D><<<p.batch.num_seqs * p.shape.kv_heads * p.max_row_tiles, 128, 0, stream>>>(p, ctas);
-    return launch_result();
-}
-
 template <class T, int D, int NT>
-static amoeba_status run_few(AttendParams& p, int sms, cudaStream_t stream) {
+static amoeba_status run_few(AttendParams& p, int sms, int* ctas, cudaStream_t stream) {
     using F = FewShape<D, NT>;
     p.shape.rows = 8 * NT;
     p.shape.tile = kFewTile;
-    p.max_row_tiles = 1;
     if (ensure_dynamic_smem((const void*)attend_few<T, D, NT>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    const int ctas = std::min(F::kCtas * sms, kMaxFewCtas);
-    attend_few<T, D, NT><<<p.whole ? p.batch.num_seqs * p.shape.kv_heads : ctas, kFewThreads, F::kSmem, stream>>>(p);
-    const amoeba_status st = launch_result();
-    return st != AMOEBA_OK || p.whole ? st : join<T, D>(p, ctas, stream);
+    *ctas = std::min(F::kCtas * sms, kMaxFewCtas);
+    return launch_kernel(attend_few<T, D, NT>, p.whole ? p.batch.num_seqs * p.shape.kv_heads : *ctas, kFewThreads, F::kSmem, stream,
+                         false, p);
 }
 
 // Sequences with at most 32 rows (new tokens times query heads per key head) are read by attend_few, whose time is that of
 // reading the cache; the others by attend_many.  Which there are is known only on the device: a batch that may hold longer
-// ones gets both, and each skips the other's.
+// ones gets both, and each skips the other's.  The launches follow one another closely: a kernel's blocks may be in place
+// before the kernel in front of it ends, and wait there for its results if they read them (attend_join) or end only after
+// it (attend_many).
 template <class T, int D>
 static amoeba_status run_attend(AttendParams& p, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
     const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
-    const int64_t few_bytes = few_workspace(&p, ws, p.batch.num_seqs, D);
+    const int64_t few_bytes = few_workspace(&p, ws, D);
     p.shape.min_rows = 0;
     p.shape.max_rows = kMaxFewRows;
-    if (rows <= 8) return run_few<T, D, 1>(p, sms, stream);
-    if (rows <= 16) return run_few<T, D, 2>(p, sms, stream);
-    const amoeba_status st = run_few<T, D, 4>(p, sms, stream);
-    if (st != AMOEBA_OK || rows <= kMaxFewRows) return st;
-    many_workspace(&p, ws + few_bytes, p.batch.num_seqs, D);
-    p.shape.min_rows = kMaxFewRows + 1;
-    p.shape.max_rows = INT32_MAX;
-    p.shape.rows = kManyRows;
-    p.shape.tile = kManyTile;
-    p.max_row_tiles = (int)((rows + kManyRows - 1) / kManyRows);
-    const int ctas = std::min(sms, kMaxSms);
-    const amoeba_status many = launch_attend_many(p, dtype, D, ctas, stream);
-    return many != AMOEBA_OK ? many : join<T, D>(p, ctas, stream);
+    int few_ctas = 0;
+    amoeba_status st = rows <= 8    ? run_few<T, D, 1>(p, sms, &few_ctas, stream)
+                       : rows <= 16 ? run_few<T, D, 2>(p, sms, &few_ctas, stream)
+                                    : run_few<T, D, 4>(p, sms, &few_ctas, stream);
+    if (st != AMOEBA_OK || (p.whole && rows <= kMaxFewRows)) return st;
+    const int few_blocks = p.whole ? 0 : few_ctas * p.shape.rows;
+    AttendParams many = p;
+    int many_ctas = 0, many_blocks = 0;
+    if (rows > kMaxFewRows) {
+        many_workspace(&many, ws + few_bytes, D);
+        many.shape.min_rows = kMaxFewRows + 1;
+        many.shape.max_rows = INT32_MAX;
+        many.shape.rows = kManyRows;
+        many.shape.tile = kManyTile;
+        many_ctas = std::min(sms, kMaxSms);
+        many_blocks = many_ctas * (kManyRows / 4);
+        if ((st = launch_attend_many(many, dtype, D, many_ctas, stream)) != AMOEBA_OK) return st;
+    }
+    return launch_kernel(attend_join<T, D>, few_blocks + many_blocks, 128, 0, stream, true, p, few_ctas, few_blocks, many, many_ctas);
 }
 
 }  // namespace amoeba
@@ -359,9 +392,9 @@ extern "C" amoeba_status amoeba_attend_workspace_bytes(const amoeba_layout* layo
     if (!layout || !batch || !bytes || batch->num_seqs < 0 || batch->max_q_len < 0) return AMOEBA_ERR_INVALID_ARG;
     const amoeba_status st = amoeba_layout_kv_pool_bytes(layout, &pool);
     if (st != AMOEBA_OK) return st;
-    *bytes = few_workspace(nullptr, nullptr, batch->num_seqs, layout->model.head_dim);
+    *bytes = few_workspace(nullptr, nullptr, layout->model.head_dim);
     if (rows_of(layout, batch->max_q_len) > kMaxFewRows)
-        *bytes += many_workspace(nullptr, nullptr, batch->num_seqs, layout->model.head_dim);
+        *bytes += many_workspace(nullptr, nullptr, layout->model.head_dim);
     return AMOEBA_OK;
 }
 
@@ -394,8 +427,9 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     p.shape.group = m.num_q_heads / m.num_kv_heads;
     p.shape.kv_heads = m.num_kv_heads;
     p.shape.window = std::min(window, 1 << 30);
-    const int64_t units = (int64_t)p.batch.num_seqs * m.num_kv_heads * (rows_of(layout, p.batch.max_q_len) / kManyRows + 1);
-    if (rows_of(layout, p.batch.max_q_len) > INT32_MAX || units > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
+    // (units are numbered in 32 bits)
+    const int64_t rows = rows_of(layout, p.batch.max_q_len);
+    if (rows > INT32_MAX || (int64_t)p.batch.num_seqs * m.num_kv_heads > INT32_MAX / (rows / kManyRows + 1)) return AMOEBA_ERR_UNSUPPORTED;
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);

@@ -11,13 +11,11 @@ struct AttendParams {
     Shape shape;
     float* lse;
     int32_t* status;
-    int64_t* prefix;         // [num_seqs + 1]: first tile of every sequence
-    int64_t* begins;         // [CTAs + 1]: first tile of every share; units before the first of all are whole
+    Cut* cuts;               // [CTAs]
     float *part_o, *part_m, *part_l;  // of the cut units: [2 * CTAs][rows][D], [2 * CTAs][rows]
     float scale_log2;        // scale * log2(e): the softmax runs in powers of two
     int32_t q_heads;         // of all workers
     int32_t whole;           // 1: one CTA per unit, nothing is cut
-    int32_t max_row_tiles;
 };
 
 // Where row r of a unit lies in a row buffer.

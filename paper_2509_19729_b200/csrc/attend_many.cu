@@ -128,21 +128,21 @@ __device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
     const int tid = threadIdx.x, ctas = gridDim.x, T = p.cache.block_tokens, S = b.num_seqs;
     sh.rounds = 0;
     if (S > kDealtSeqs) {
-        Walk w;
-        int64_t total;
-        int n_ctas;
-        const int64_t n = take_share<kManyThreads>(shape, b, T, &w, &total, &n_ctas, 1, p.prefix, p.begins, p.status);
+        Walk w{};
+        int64_t begin, end;
+        take_share<kManyThreads>(shape, b, T, &w, &begin, &end, p.status);
         if (tid == 0) {
-            sh.begin = share_begin(total, n_ctas, blockIdx.x), sh.end = sh.begin + n;
-            if (n) {
+            sh.begin = begin, sh.end = end;
+            if (end > begin) {
                 sh.begin_seq = w.s;
                 int64_t off = w.t + w.h * head_tiles(shape, w.seq);
                 for (int m = 0; m < w.m; ++m) off += row_tile_range(shape, w.seq, m).tiles;
                 sh.begin_off = off;
             }
         }
+        write_cut(p.cuts, w, begin, end);
         __syncthreads();
-        return n > 0;
+        return end > begin;
     }
     // units and tiles before every sequence
     int32_t units = 0;
@@ -174,16 +174,10 @@ __device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
         __syncthreads();
         if (tid % 32 == 31) s_warp[tid / 32] = t;
         __syncthreads();
-        before = tiles;
-        for (int w = 0; w < kManyThreads / 32; ++w) {
-            if (w < tid / 32) before += s_warp[w];
-            tiles += s_warp[w];
-        }
-        if (s < S && blockIdx.x == 0) p.prefix[s] = before + t - n_tiles;
+        for (int w = 0; w < kManyThreads / 32; ++w) tiles += s_warp[w];
     }
     for (int c = tid; c < kMaxSms; c += kManyThreads) done[c] = 0;
     if (tid == 0) sh.first_unit[S] = units, sh.begin = sh.end = 0;
-    if (blockIdx.x == 0 && tid == 0) p.prefix[S] = tiles;
     __syncthreads();
     const int rounds = max(units / ctas - 1, 0), dealt = rounds * ctas;
     if (tid == 0) sh.rounds = rounds;
@@ -202,7 +196,7 @@ __device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
     const int64_t even = (tiles + ctas - 1) / ctas;
     if (tid < 32) {
         int64_t run = first_cut;
-        for (int base = 0; base <= ctas; base += 32) {
+        for (int base = 0; base < ctas; base += 32) {
             const int c = base + tid;
             const int64_t want = c < ctas ? max(even - done[c], (int64_t)0) : 0;
             int64_t incl = want;
@@ -213,7 +207,6 @@ __device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
             }
             const int64_t begin = min(run + incl - want, tiles), end = min(run + incl, tiles);
             if (c == (int)blockIdx.x) sh.begin = begin, sh.end = end;
-            if (blockIdx.x == 0 && c <= ctas) p.begins[c] = c == ctas ? tiles : begin;
             run += __shfl_sync(~0u, incl, 31);
         }
     }
@@ -243,6 +236,14 @@ __device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
             if (at >= first && at < first + n) sh.begin_seq = i, sh.begin_off = at - first;
         }
         __syncthreads();
+    }
+    if (tid == 0) {
+        Walk w{};
+        if (sh.end > at) {
+            w.open(shape, b, T, sh.begin_seq);
+            w.seek(shape, sh.begin_off);
+        }
+        write_cut(p.cuts, w, at, sh.end);
     }
     return rounds > 0 || sh.end > at;
 }
@@ -699,7 +700,12 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     char* smem = smem_raw + (1024 - smem_u32(smem_raw) % 1024) % 1024;
     const int warp = threadIdx.x / 32;
     __shared__ Share share;
-    if (!make_share(p, share, reinterpret_cast<int32_t*>(smem))) return;
+    const bool busy = make_share(p, share, reinterpret_cast<int32_t*>(smem));
+    grid_dependency_launch();
+    if (!busy) {
+        grid_dependency_wait();
+        return;
+    }
     __syncthreads();
     if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&b.tmem)) : "memory");
@@ -730,6 +736,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         if (!softmax<T, D>(p, share, b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
     }
+    grid_dependency_wait();  // attend_few in front is done when this kernel is
     tmem_fence_before();
     __syncthreads();
     if (warp == 8) {
@@ -741,8 +748,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
 template <class T, int D>
 static amoeba_status launch(const AttendParams& p, int ctas, cudaStream_t stream) {
     if (ensure_dynamic_smem((const void*)attend_many<T, D>, ManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    attend_many<T, D><<<ctas, kManyThreads, ManyShape<D>::kSmem, stream>>>(p);
-    return launch_result();
+    return launch_kernel(attend_many<T, D>, ctas, kManyThreads, ManyShape<D>::kSmem, stream, true, p);
 }
 
 amoeba_status launch_attend_many(const AttendParams& p, int32_t dtype, int head_dim, int ctas, cudaStream_t stream) {

@@ -87,6 +87,9 @@ __device__ __forceinline__ float fast_exp2(float x) {
     return y;
 }
 
+__device__ __forceinline__ void grid_dependency_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -154,6 +157,30 @@ inline amoeba_status make_rows(const amoeba_layout* l, const void* const* ptrs, 
         if ((uintptr_t)ptrs[r] % 16) return AMOEBA_ERR_ALIGNMENT;
         out->base[r] = static_cast<char*>(const_cast<void*>(ptrs[r]));
     }
+    return AMOEBA_OK;
+}
+
+// Launches a kernel; early: its blocks may start before the kernel in front of it in the stream has ended (that one has
+// called grid_dependency_launch in all its blocks, or they have ended), and call grid_dependency_wait before they use its
+// results.
+template <class... P, class... A>
+inline amoeba_status launch_kernel(void (*kernel)(P...), int grid, int threads, size_t smem, cudaStream_t stream, bool early,
+                                   const A&... args) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((unsigned)grid);
+    c.blockDim = dim3((unsigned)threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    cudaLaunchAttribute a{};
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &a;
+    c.numAttrs = early ? 1 : 0;
+    if (cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return AMOEBA_ERR_CUDA;
+    }
+    count_launch();
     return AMOEBA_OK;
 }
 

@@ -32,9 +32,9 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreCtas) accumulate_scores(c
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kScoreStages * kStage;
     const Shape& sh = p.shape;
     Walk walk;
-    int64_t total;
-    int ctas;
-    int64_t n = take_share<kScoreThreads>(sh, p.batch, p.cache.block_tokens, &walk, &total, &ctas, 1, nullptr, nullptr, p.status);
+    int64_t begin, end;
+    take_share<kScoreThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
+    int64_t n = end - begin;
     if (n == 0) return;
 
     Walk ahead = walk;

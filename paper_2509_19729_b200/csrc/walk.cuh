@@ -53,17 +53,6 @@ __device__ __forceinline__ int64_t head_tiles(const Shape& p, const Seq& q) {
 
 // First tile of CTA c's share.
 __device__ __forceinline__ int64_t share_begin(int64_t total, int ctas, int c) { return total * c / ctas; }
-// The CTA whose share, of those that begin at begins[0 .. ctas-1], has the tile; begins[ctas] is behind all.
-__device__ __forceinline__ int share_of(const int64_t* begins, int ctas, int64_t tile) {
-    int lo = 0, hi = ctas;  // begins[lo] <= tile < begins[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (begins[mid] <= tile) lo = mid;
-        else hi = mid;
-    }
-    return lo;
-}
-
 struct Walk {
     int32_t s, h, m, t;  // sequence, key head, row tile, tile of it
     int32_t nm;
@@ -128,12 +117,21 @@ __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* shared) {
     return v;
 }
 
-// This CTA's share: *total and the number of its tiles, with `walk` at the first of them.  CTA 0 reports bad sequences and
-// writes the first tile of every sequence, and the total behind them, to `prefix` (null: to nowhere), and the first tile of
-// every CTA's share, and the total behind them, to `begins`, ended by gridDim.x + 1 entries in all.
+// The run of tiles that is a CTA's share, and the unit that it begins in: what the join of cut units goes by.
+struct Cut {
+    int64_t begin, end;  // empty shares: begin = end
+    int32_t s, h, m;     // the first tile's unit,
+    int32_t t, tiles;    // its place in it, and the unit's tiles
+    int32_t pad;
+};
+__device__ __forceinline__ void write_cut(Cut* cuts, const Walk& w, int64_t begin, int64_t end) {
+    if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{begin, end, w.s, w.h, w.m, w.t, w.range.tiles, 0};
+}
+
+// This CTA's share: [*begin, *end) of all tiles, with `walk` at the first of them.  CTA 0 reports bad sequences.
 template <int kThreads>
-__device__ int64_t take_share(const Shape& p, const Batch& b, int block_tokens, Walk* walk, int64_t* total, int* ctas,
-                              int min_tiles, int64_t* prefix, int64_t* begins, int32_t* status) {
+__device__ void take_share(const Shape& p, const Batch& b, int block_tokens, Walk* walk, int64_t* begin_out, int64_t* end_out,
+                           int32_t* status) {
     __shared__ int64_t s_warp[kThreads / 32];
     __shared__ int64_t s_off;
     __shared__ int32_t s_seq;
@@ -146,11 +144,10 @@ __device__ int64_t take_share(const Shape& p, const Batch& b, int block_tokens, 
         sum += mine;
     }
     const int64_t all = block_sum<kThreads>(sum, s_warp);
-    *total = all;
-    *ctas = (int)max((int64_t)1, min((int64_t)gridDim.x, all / min_tiles));
-    const int64_t begin = share_begin(all, *ctas, blockIdx.x);
-    const int64_t end = (int)blockIdx.x < *ctas ? share_begin(all, *ctas, blockIdx.x + 1) : begin;
-    const bool writes = blockIdx.x == 0 && prefix;
+    const int ctas = (int)max((int64_t)1, min((int64_t)gridDim.x, all));
+    const int64_t begin = (int)blockIdx.x < ctas ? share_begin(all, ctas, blockIdx.x) : all;
+    const int64_t end = (int)blockIdx.x < ctas ? share_begin(all, ctas, blockIdx.x + 1) : all;
+    *begin_out = begin, *end_out = end;
     int64_t run = 0;
     for (int base = 0; base < b.num_seqs; base += kThreads) {
         const int s = base + tid;
@@ -171,20 +168,14 @@ __device__ int64_t take_share(const Shape& p, const Batch& b, int block_tokens, 
             run += s_warp[w];
         }
         const int64_t first = before + incl - mine;
-        if (writes && s < b.num_seqs) prefix[s] = first;
         if (begin >= first && begin < first + mine) s_seq = s, s_off = begin - first;
-        if (!writes && run > begin) break;  // block-uniform
-    }
-    if (writes) {
-        if (tid == 0) prefix[b.num_seqs] = all;
-        for (int c = tid; c <= (int)gridDim.x; c += kThreads) begins[c] = c < *ctas ? share_begin(all, *ctas, c) : all;
+        if (run > begin) break;  // block-uniform
     }
     __syncthreads();
     if (end > begin) {
         walk->open(p, b, block_tokens, s_seq);
         walk->seek(p, s_off);
     }
-    return end - begin;
 }
 
 }  // namespace amoeba
