@@ -453,7 +453,7 @@ __all__.append("amoeba_plan_weight_alias")
 
 
 # ---- operators on the cache of a running instance.  Arguments are torch tensors: their types, shapes, strides and device
-# are checked here, the rest by the C library; the calls run on the tensors' device, on its current stream by default.
+# are checked on the way (csrc/torch_calls.cpp), the rest by the C library; the calls run on the tensors' device, on its current stream by default.
 DTYPE_FP16, DTYPE_BF16 = 0, 1
 __all__ += ["Batch", "Rotation", "DTYPE_FP16", "DTYPE_BF16", "make_batch", "make_rotation", "amoeba_append_kv",
             "amoeba_attend_workspace_bytes", "amoeba_attend", "amoeba_accumulate_scores",
@@ -468,41 +468,39 @@ def _tensor(t, where: str, dtype, numel: int, device) -> int:
     return t.data_ptr()
 
 
-def _torch_dtype(dtype: int, where: str):
-    import torch
+def _load_torch_calls():
+    import importlib.util
 
-    if dtype not in (DTYPE_FP16, DTYPE_BF16):
-        raise AmoebaError(ERR_UNSUPPORTED, where)
-    return torch.float16 if dtype == DTYPE_FP16 else torch.bfloat16
+    import torch  # noqa: F401  (its libraries have to be in the process)
+
+    if _build.torch_calls_stale():
+        try:
+            _build.build_torch_calls()
+        except Exception as e:
+            raise ImportError(f"{_build.TORCH_CALLS.name} is missing or stale and could not be built: {e}") from e
+    C.CDLL(str(library_path()), mode=C.RTLD_GLOBAL)  # the functions that the module calls
+    spec = importlib.util.spec_from_file_location("_torch_calls", _build.TORCH_CALLS)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
 
 
-def _pools(layout: Layout, pools, nbytes: int, where: str, device):
-    if len(pools) != layout.tp:
-        raise AmoebaError(ERR_INVALID_ARG, f"{where} (pool count != tp)")
-    for p in pools:
-        if p.device != device or not p.is_contiguous() or p.numel() * p.element_size() < nbytes:
-            raise AmoebaError(ERR_INVALID_ARG, f"{where}: a pool is on another device, strided or too small")
-    return (C.c_void_p * layout.tp)(*[p.data_ptr() for p in pools])
+_torch_calls = None
 
 
-def _row_buffers(layout: Layout, tensors, rows: int, width: int, dt, where: str, device):
-    """([tp] addresses, row stride) of the workers' [rows, width] (or [rows, heads, head_dim]) buffers."""
-    if len(tensors) != layout.tp:
-        raise AmoebaError(ERR_INVALID_ARG, f"{where} (row buffer count != tp)")
-    stride = None
-    for t in tensors:
-        n = t.dim()
-        ok = t.dtype == dt and t.device == device and n in (2, 3) and t.shape[0] >= rows and t.stride(-1) == 1
-        if ok and n == 3:
-            ok = t.shape[1] * t.shape[2] == width and (t.shape[1] == 1 or t.stride(1) == t.shape[2])
-        elif ok:
-            ok = t.shape[1] == width
-        st = (t.stride(0) if t.shape[0] > 1 else width) if ok else None
-        if not ok or (stride is not None and st != stride):
-            raise AmoebaError(ERR_INVALID_ARG, f"{where}: row buffers are {dt} on {device}, [>= {rows}, {width}], dense "
-                                               "along a row and equally strided")
-        stride = st
-    return (C.c_void_p * layout.tp)(*[t.data_ptr() for t in tensors]), stride
+def _call(name: str, where: str, *args) -> None:
+    global _torch_calls
+    if _torch_calls is None:
+        _torch_calls = _load_torch_calls()
+    status = getattr(_torch_calls, name)(*args)
+    if status != OK:
+        if isinstance(status, str):
+            raise AmoebaError(ERR_INVALID_ARG, f"{where}: {status}")
+        raise AmoebaError(status, where)
+
+
+def _handle(stream):
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
 def make_batch(block_table, seq_lens, q_starts=None, num_rows: Optional[int] = None, max_q_len: int = 1) -> Batch:
@@ -519,7 +517,8 @@ def make_batch(block_table, seq_lens, q_starts=None, num_rows: Optional[int] = N
     b = Batch(_tensor(block_table, "make_batch", torch.int32, 0, dev), _tensor(seq_lens, "make_batch", torch.int32, S, dev),
               None if q_starts is None else _tensor(q_starts, "make_batch", torch.int32, S + 1, dev), S,
               block_table.shape[1], S if num_rows is None else num_rows, max_q_len)
-    b.device, b.keep = dev, (block_table, seq_lens, q_starts)
+    b.index = dev.index if dev.type == "cuda" else -1
+    b.address, b.keep = C.addressof(b), (block_table, seq_lens, q_starts)
     return b
 
 
@@ -536,29 +535,8 @@ def make_rotation(q_norm=None, k_norm=None, norm_eps: float = 1e-6, inv_freq=Non
                  None if inv_freq is None else _tensor(inv_freq, "make_rotation", torch.float64, rot_dim // 2, dev),
                  None if positions is None else _tensor(positions, "make_rotation", torch.int32, 0, dev),
                  norm_eps, rot_dim, int(interleaved), 0)
-    r.device, r.keep = dev, (q_norm, k_norm, inv_freq, positions)
+    r.device, r.address, r.keep = dev, C.addressof(r), (q_norm, k_norm, inv_freq, positions)
     return r
-
-
-def _launch(fn, where: str, device, stream, *args) -> None:
-    """Calls fn(*args, stream) with `device` current."""
-    import torch
-
-    if device.type != "cuda":
-        raise AmoebaError(ERR_INVALID_ARG, f"{where}: the tensors are on {device}")
-    handle = torch.cuda.current_stream(device).cuda_stream if stream is None else _stream(stream)
-    if torch.cuda.current_device() == device.index:
-        status = fn(*args, handle)
-    else:
-        with torch.cuda.device(device):
-            status = fn(*args, handle)
-    _check(status, where)
-
-
-def _layer_bytes(layout: Layout) -> int:
-    m = layout.model
-    return layout.kv_layer_stride_bytes or (layout.num_blocks * (m.num_kv_heads // max(layout.tp, 1)) * 2 *
-                                            layout.block_tokens * m.head_dim * m.elem_bytes)
 
 
 def amoeba_append_kv(layout: Layout, dtype: int, layer: int, pools: Sequence, batch: Batch, q, k: Sequence, v: Sequence,
@@ -566,27 +544,23 @@ def amoeba_append_kv(layout: Layout, dtype: int, layer: int, pools: Sequence, ba
     """Normalises and turns the new queries (into q_out) and keys and writes keys and values into layer `layer` of the
     pools.  q, k, v, q_out: one [num_rows, heads of the worker * head_dim] tensor per worker, row strides as they are;
     q and q_out may both be None."""
+    if rotation is not None:
+        _check_rotation(rotation, layout, dtype, batch)
+    _call("append_kv", "amoeba_append_kv", C.addressof(layout), dtype, layer, pools, batch.address, batch.index, q, k, v,
+          None if rotation is None else rotation.address, q_out, status, _handle(stream))
+
+
+def _check_rotation(rotation: Rotation, layout: Layout, dtype: int, batch: Batch) -> None:
     import torch
 
-    w, dev, m, rows = "amoeba_append_kv", batch.device, layout.model, batch.num_rows
-    dt = _torch_dtype(dtype, w)
-    D, tp = m.head_dim, max(layout.tp, 1)
-    kw, qw = m.num_kv_heads // tp * D, m.num_q_heads // tp * D
-    pp = _pools(layout, pools, _layer_bytes(layout) * (layer + 1), w, dev)
-    kp, ks = _row_buffers(layout, k, rows, kw, dt, w, dev)
-    vp, vs = _row_buffers(layout, v, rows, kw, dt, w, dev)
-    qp = op = None
-    qs = os_ = 0
-    if q is not None:
-        qp, qs = _row_buffers(layout, q, rows, qw, dt, w, dev)
-    if q_out is not None:
-        op, os_ = _row_buffers(layout, q_out, rows, qw, dt, w, dev)
-    if rotation is not None:
-        for t, n, want in zip(rotation.keep, (D, D, 0, rows), (dt, dt, torch.float64, torch.int32)):
-            if t is not None and (t.dtype != want or t.numel() < n or t.device != dev):
-                raise AmoebaError(ERR_INVALID_ARG, f"{w}: norm weights are {dt} [{D}], positions int32 [{rows}], on {dev}")
-    _launch(_load().amoeba_append_kv, w, dev, stream, C.byref(layout), dtype, layer, pp, C.byref(batch), qp, qs, kp, ks,
-            vp, vs, None if rotation is None else C.byref(rotation), op, os_, _tensor(status, w, torch.int32, 1, dev))
+    D, dt = layout.model.head_dim, torch.float16 if dtype == DTYPE_FP16 else torch.bfloat16
+    q_norm, k_norm, inv_freq, positions = rotation.keep
+    dev = rotation.device
+    if (dev is not None and dev.index != batch.index) or any(
+            w is not None and (w.dtype is not dt or w.numel() < D) for w in (q_norm, k_norm)) or (
+            positions is not None and positions.numel() < batch.num_rows):
+        raise AmoebaError(ERR_INVALID_ARG, f"amoeba_append_kv: norm weights are {dt} [{D}], positions int32 "
+                                           f"[{batch.num_rows}], on the batch's device")
 
 
 def amoeba_attend_workspace_bytes(layout: Layout, batch: Batch) -> int:
@@ -600,17 +574,8 @@ def amoeba_attend(layout: Layout, dtype: int, layer: int, pools: Sequence, batch
                   window: int, out: Sequence, lse, status, workspace, stream=None) -> None:
     """Attention of the batch's rows over layer `layer` of the cache.  q, out: one [num_rows, query heads of the worker *
     head_dim] tensor per worker; lse: float32 [num_rows, num_q_heads] or None; window: 0 = every earlier token."""
-    import torch
-
-    w, dev, m, rows = "amoeba_attend", batch.device, layout.model, batch.num_rows
-    dt = _torch_dtype(dtype, w)
-    width = m.num_q_heads // max(layout.tp, 1) * m.head_dim
-    pp = _pools(layout, pools, _layer_bytes(layout) * (layer + 1), w, dev)
-    qp, qs = _row_buffers(layout, q, rows, width, dt, w, dev)
-    op, os_ = _row_buffers(layout, out, rows, width, dt, w, dev)
-    _launch(_load().amoeba_attend, w, dev, stream, C.byref(layout), dtype, layer, pp, C.byref(batch), qp, qs, scale,
-            window, op, os_, None if lse is None else _tensor(lse, w, torch.float32, rows * m.num_q_heads, dev),
-            _tensor(status, w, torch.int32, 1, dev), _tensor(workspace, w, torch.uint8, 0, dev), workspace.numel())
+    _call("attend", "amoeba_attend", C.addressof(layout), dtype, layer, pools, batch.address, batch.index, q, scale, window,
+          out, lse, status, workspace, _handle(stream))
 
 
 def amoeba_accumulate_scores(layout: Layout, dtype: int, layer: int, pools: Sequence, batch: Batch, q: Sequence,
@@ -619,27 +584,8 @@ def amoeba_accumulate_scores(layout: Layout, dtype: int, layer: int, pools: Sequ
     """Adds the attention weight that the cached tokens get from the batch's rows to layer `layer` of the score pools
     (float32, one [num_layers, num_blocks, key heads of the worker, block_tokens] tensor per worker).  lse: amoeba_attend's
     for the same rows; scored_lens: int32 [num_seqs], how many tokens have a score already, or None."""
-    import torch
-
-    w, dev, m, rows = "amoeba_accumulate_scores", batch.device, layout.model, batch.num_rows
-    dt = _torch_dtype(dtype, w)
-    tp = max(layout.tp, 1)
-    pp = _pools(layout, pools, _layer_bytes(layout) * (layer + 1), w, dev)
-    sp = _score_pools(layout, score_pools, layer + 1, w, dev)
-    qp, qs = _row_buffers(layout, q, rows, m.num_q_heads // tp * m.head_dim, dt, w, dev)
-    _launch(_load().amoeba_accumulate_scores, w, dev, stream, C.byref(layout), dtype, layer, pp, C.byref(batch), qp, qs,
-            scale, window, _tensor(lse, w, torch.float32, rows * m.num_q_heads, dev),
-            None if scored_lens is None else _tensor(scored_lens, w, torch.int32, batch.num_seqs, dev), sp,
-            _tensor(status, w, torch.int32, 1, dev))
-
-
-def _score_pools(layout: Layout, score_pools, layers: int, where: str, device):
-    import torch
-
-    if any(p.dtype != torch.float32 for p in score_pools):
-        raise AmoebaError(ERR_INVALID_ARG, f"{where}: score pools are float32")
-    n = layout.num_blocks * (layout.model.num_kv_heads // max(layout.tp, 1)) * layout.block_tokens * 4
-    return _pools(layout, score_pools, n * layers, where, device)
+    _call("accumulate_scores", "amoeba_accumulate_scores", C.addressof(layout), dtype, layer, pools, batch.address,
+          batch.index, q, scale, window, lse, scored_lens, score_pools, status, _handle(stream))
 
 
 def amoeba_evict_workspace_bytes(layout: Layout, num_layers: int, num_seqs: int, budget: int) -> int:
@@ -654,18 +600,8 @@ def amoeba_evict_kv(layout: Layout, layer_begin: int, layer_end: int, pools: Seq
     """Cuts the sequences to `budget` tokens, the last `recent` and those with the highest scores, in layers [layer_begin,
     layer_end) of the pools.  src_bt, dst_bt: int32 [num_seqs, blocks]; dst_bt may be src_bt (in place).  score_pools may
     be None if recent == budget."""
-    import torch
-
-    w, dev, S = "amoeba_evict_kv", seq_lens.device, seq_lens.numel()
-    if src_bt.dim() != 2 or dst_bt.dim() != 2 or src_bt.shape[0] != S or dst_bt.shape[0] != S:
-        raise AmoebaError(ERR_INVALID_ARG, f"{w}: block tables are [num_seqs, blocks]")
-    pp = _pools(layout, pools, _layer_bytes(layout) * layer_end, w, dev)
-    sp = None if score_pools is None else _score_pools(layout, score_pools, layer_end, w, dev)
-    _launch(_load().amoeba_evict_kv, w, dev, stream, C.byref(layout), layer_begin, layer_end, pp, sp,
-            _tensor(src_bt, w, torch.int32, 0, dev), _tensor(seq_lens, w, torch.int32, S, dev), S, src_bt.shape[1],
-            _tensor(dst_bt, w, torch.int32, 0, dev), dst_bt.shape[1], budget, recent,
-            _tensor(new_lens, w, torch.int32, S, dev), _tensor(status, w, torch.int32, 1, dev),
-            _tensor(workspace, w, torch.uint8, 0, dev), workspace.numel())
+    _call("evict_kv", "amoeba_evict_kv", C.addressof(layout), layer_begin, layer_end, pools, score_pools, src_bt, seq_lens,
+          dst_bt, budget, recent, new_lens, status, workspace, _handle(stream))
 
 
 def amoeba_launch_count() -> int:

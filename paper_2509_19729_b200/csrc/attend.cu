@@ -432,6 +432,12 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     if (rows > INT32_MAX || (int64_t)p.batch.num_seqs * m.num_kv_heads > INT32_MAX / (rows / kManyRows + 1)) return AMOEBA_ERR_UNSUPPORTED;
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
+    // Short sequences are not worth cutting: what the shares and the join take, about 5 us, is what a CTA needs for 512
+    // tokens, or for 1024 when there are units enough to fill the GPU (one sequence of 256 tokens, 8 key heads: 7.9 us whole,
+    // 9.5 cut; of 1024: 20.5 and 11.3; 32 sequences of 1024: 24 and 29; of 2048: 41 and 47, but there one long one would
+    // hold up all).
+    const int64_t tokens = (int64_t)p.batch.max_blocks * layout->block_tokens;
+    p.whole = tokens <= 512 || (tokens <= 1024 && p.batch.num_seqs * m.num_kv_heads >= dev.sms);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(d_workspace);
     if (dtype == AMOEBA_FP16)

@@ -1,9 +1,10 @@
 // amoeba_evict_kv: long sequences cut to a budget by their tokens' scores.
 //
-// Two launches: which tokens stay (one CTA per layer, sequence and key head: a radix selection of the budget-th largest
-// score and an ordered list of the kept indices), and the move of their keys, values and scores.  Memory-bound: the
-// scores are read once, what stays is read and written once.
+// Two launches: which tokens stay (for each layer, sequence and key head, by the budget-th largest score: an ordered list of
+// the kept indices), and the move of their keys, values and scores.  Memory-bound: the scores are read once, what stays is
+// read and written once.
 #include "cache_view.cuh"
+#include "copy_engine.cuh"
 
 namespace amoeba {
 
@@ -46,171 +47,299 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kSelectThreads = 512;
+// ------------------------------------------------------------------------------------------------ which tokens stay
+// A cluster of CTAs for each (layer, sequence, key head): each takes a run of the tokens, its scores as ordered whole numbers
+// in shared memory.  The smallest score that stays is found from the top, 11, 11 and 10 bits at a time, from counts of the
+// digits that all CTAs of the cluster add up; then every warp lists the kept ones of its own run of tokens in order.
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectKeys = 12288, kMaxCluster = 8;  // keys that a CTA holds, unless eight CTAs need to hold more
+constexpr int kDigits = 2048;
 
-__global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_constant__ EvictParams p) {
-    __shared__ int32_t s_hist[256];
-    __shared__ int64_t s_warp[kSelectThreads / 32];
-    __shared__ uint32_t s_key;
-    __shared__ int32_t s_need;
-    const int tid = threadIdx.x;
-    const int h = blockIdx.x % p.kv_heads, s = blockIdx.x / p.kv_heads % p.num_seqs;
-    const int l = blockIdx.x / p.kv_heads / p.num_seqs;
-    const bool first = l == 0 && h == 0;
+struct SelectShared {
+    int32_t count[kDigits];   // of this CTA's tokens, by digit
+    int32_t total[kDigits];   // of the cluster's
+    int32_t warp[kSelectWarps];
+    int32_t more, equal;      // this CTA's tokens above the limit, and at it
+    int32_t found[2];         // digit, and how many at it stay
+    int32_t before[kSelectWarps][2];
+};
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm("mov.u32 %0, %cluster_nctarank;" : "=r"(r));
+    return r;
+}
+// A 32-bit value at the same place in another CTA's shared memory.
+__device__ __forceinline__ int32_t load_remote(const int32_t* p, uint32_t rank) {
+    uint32_t addr = (uint32_t)__cvta_generic_to_shared(p), remote;
+    int32_t v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_constant__ EvictParams p, int room) {
+    extern __shared__ __align__(16) uint32_t s_keys[];
+    __shared__ SelectShared sh;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const uint32_t rank = cluster_rank(), size = cluster_size();
+    const int unit = blockIdx.x / size;
+    const int h = unit % p.kv_heads, s = unit / p.kv_heads % p.num_seqs, l = unit / p.kv_heads / p.num_seqs;
+    const bool first = l == 0 && h == 0 && rank == 0;
     const int len = checked_len(p, s, first);
     if (first && tid == 0) p.new_lens[s] = min(len, p.budget);
-    if (len <= p.budget) return;
+    if (len <= p.budget) return;  // the whole cluster
     const int free = len - p.recent, need = p.budget - p.recent;
     const int w = h / p.cache.heads, hw = h - w * p.cache.heads, T = p.cache.block_tokens;
     int32_t* kept = p.kept + ((int64_t)(l * p.num_seqs + s) * p.kv_heads + h) * p.budget;
-    for (int i = tid; i < p.recent; i += kSelectThreads) kept[need + i] = free + i;
+    for (int i = rank * kSelectThreads + tid; i < p.recent; i += size * kSelectThreads) kept[need + i] = free + i;
     if (need == 0) return;
+
+    const int run = (free + size * 32 - 1) / (size * 32) * 32;  // tokens of a CTA
+    const int begin = min(free, (int)rank * run), n = min(free - begin, run);
     const float* scores = p.scores[w] + l * p.layer_scores;
     const int32_t* table = p.src_bt + (int64_t)s * p.max_blocks;
-    auto key_of = [&](int i) {
-        return order_of(scores[((int64_t)table[i / T] * p.cache.heads + hw) * T + i % T]);
-    };
-    // The need-th largest key, eight bits at a time; s_need of the tokens that have exactly that key stay.
-    uint32_t prefix = 0;
-    int left = need;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kSelectThreads) s_hist[i] = 0;
-        __syncthreads();
-        const uint32_t above = shift == 24 ? 0 : ~0u << (shift + 8);
-        for (int i = tid; i < free; i += kSelectThreads) {
-            const uint32_t k = key_of(i);
-            if ((k & above) == prefix) atomicAdd(&s_hist[k >> shift & 255], 1);
-        }
-        __syncthreads();
-        if (tid < 32) {  // from the largest digit down
-            int mine[8], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) mine[i] = s_hist[255 - tid * 8 - i], sum += mine[i];
-            int before = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int up = __shfl_up_sync(~0u, before, o);
-                if (tid >= o) before += up;
+    auto score_at = [&](int i) { return scores + ((int64_t)table[i / T] * p.cache.heads + hw) * T + i % T; };
+    const bool held = n <= room;
+    if (held) {
+        if (T % 4 == 0) {
+            for (int i = tid * 4; i < n; i += kSelectThreads * 4) {  // (run is a multiple of 32: i is in one block)
+                const float4 x = *reinterpret_cast<const float4*>(score_at(begin + i));
+                *reinterpret_cast<uint4*>(s_keys + i) = make_uint4(order_of(x.x), order_of(x.y), order_of(x.z), order_of(x.w));
             }
-            before -= sum;
-            if (before < left && left <= before + sum) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (before < left && left <= before + mine[i]) {
-                        s_key = prefix | (uint32_t)(255 - tid * 8 - i) << shift;
-                        s_need = left - before;
-                    }
-                    before += mine[i];
-                }
+        } else {
+            for (int i = tid; i < n; i += kSelectThreads) s_keys[i] = order_of(*score_at(begin + i));
+        }
+    }
+    auto key_of = [&](int i) { return held ? s_keys[i] : order_of(*score_at(begin + i)); };
+
+    uint32_t limit = 0;  // found so far, from the top
+    int left = need;     // how many of the tokens that agree with it stay
+    for (int round = 0; round < 3; ++round) {
+        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
+        const uint32_t above = round == 0 ? 0u : ~0u << (shift + bits);
+        for (int i = tid; i < kDigits; i += kSelectThreads) sh.count[i] = 0;
+        __syncthreads();
+        for (int i = tid; i - lane < n; i += kSelectThreads) {
+            const uint32_t k = i < n ? key_of(i) : 0;
+            const bool counts = i < n && (k & above) == limit;
+            const uint32_t those = __ballot_sync(~0u, counts);
+            if (counts) {  // equal digits of a warp are added once: scores of many tokens are the same
+                const uint32_t digit = k >> shift & ((1u << bits) - 1);
+                const uint32_t same = __match_any_sync(those, digit);
+                if (__ffs(same) - 1 == lane) atomicAdd(&sh.count[digit], __popc(same));
             }
         }
         __syncthreads();
-        prefix = s_key;
-        left = s_need;
-    }
-    // In order: thread t lists the kept ones of its run of consecutive tokens.
-    const int per = (free + kSelectThreads - 1) / kSelectThreads, begin = min(free, tid * per), end = min(free, begin + per);
-    int32_t more = 0, equal = 0;
-    for (int i = begin; i < end; ++i) {
-        const uint32_t k = key_of(i);
-        more += k > prefix;
-        equal += k == prefix;
-    }
-    int64_t incl = (int64_t)more << 32 | (uint32_t)equal;
-    const int64_t mine = incl;
+        if (size > 1) cluster_sync();
+        // from the largest digit down: thread t has digits 2047 - 4t ... 2044 - 4t
+        int mine[4], sum = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        const int64_t up = __shfl_up_sync(~0u, incl, o);
-        if (tid % 32 >= o) incl += up;
+        for (int j = 0; j < 4; ++j) {
+            const int d = kDigits - 1 - tid * 4 - j;
+            mine[j] = sh.count[d];
+            for (uint32_t r = 1; r < size; ++r) mine[j] += load_remote(&sh.count[d], (rank + r) % size);
+            sum += mine[j];
+        }
+        int before = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int up = __shfl_up_sync(~0u, before, o);
+            if (lane >= o) before += up;
+        }
+        if (lane == 31) sh.warp[warp] = before;
+        __syncthreads();
+        before -= sum;
+        for (int i = 0; i < warp; ++i) before += sh.warp[i];
+        if (before < left && left <= before + sum) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (before < left && left <= before + mine[j])
+                    sh.found[0] = kDigits - 1 - tid * 4 - j, sh.found[1] = left - before;
+                before += mine[j];
+            }
+        }
+        if (size > 1) cluster_sync();  // before the counts are cleared
+        else __syncthreads();
+        limit |= (uint32_t)sh.found[0] << shift;
+        left = sh.found[1];
     }
-    if (tid % 32 == 31) s_warp[tid / 32] = incl;
+
+    // Every warp's run of tokens, counted, and then listed behind those of the warps and CTAs before.
+    const int per = (n + kSelectThreads - 1) / kSelectThreads * 32;
+    const int from = min(n, warp * per), to = min(n, from + per);
+    int more = 0, equal = 0;
+    for (int i = from + lane; i - lane < to; i += 32) {
+        const uint32_t k = i < to ? key_of(i) : 0;
+        more += i < to && k > limit;
+        equal += i < to && k == limit;
+    }
+    more = __reduce_add_sync(~0u, more), equal = __reduce_add_sync(~0u, equal);
+    if (lane == 0) sh.before[warp][0] = more, sh.before[warp][1] = equal;
     __syncthreads();
-    for (int i = 0; i < tid / 32; ++i) incl += s_warp[i];
-    incl -= mine;
-    int rank_eq = (int)(uint32_t)incl, at = (int)(incl >> 32) + min(rank_eq, left);
-    for (int i = begin; i < end; ++i) {
-        const uint32_t k = key_of(i);
-        if (k > prefix || (k == prefix && rank_eq++ < left)) kept[at++] = i;
+    if (tid == 0) {
+        int a = 0, b = 0;
+        for (int i = 0; i < kSelectWarps; ++i) a += sh.before[i][0], b += sh.before[i][1];
+        sh.more = a, sh.equal = b;
+    }
+    if (size > 1) cluster_sync();
+    else __syncthreads();
+    more = equal = 0;
+    for (uint32_t r = 0; r < rank; ++r) more += load_remote(&sh.more, r), equal += load_remote(&sh.equal, r);
+    for (int i = 0; i < warp; ++i) more += sh.before[i][0], equal += sh.before[i][1];
+    const uint32_t lower = (1u << lane) - 1;
+    for (int i = from + lane; i - lane < to; i += 32) {
+        const uint32_t k = i < to ? key_of(i) : 0;
+        const uint32_t is_more = __ballot_sync(~0u, i < to && k > limit), is_equal = __ballot_sync(~0u, i < to && k == limit);
+        const int rank_equal = equal + __popc(is_equal & lower);
+        const bool stays = (is_more >> lane & 1u) || ((is_equal >> lane & 1u) && rank_equal < left);
+        if (stays) kept[more + __popc(is_more & lower) + min(rank_equal, left)] = begin + i;
+        more += __popc(is_more), equal += __popc(is_equal);
+    }
+    if (size > 1) cluster_sync();  // no CTA ends while another reads its counts
+}
+
+// ------------------------------------------------------------------------------------------------ the move
+// Rows are tokens: a key and a value of `vec` bytes each.  The offsets of a chunk of rows are worked out once, a thread a row,
+// and the rows then copied 16 bytes a lane with as many loads in flight as a lane has stores.
+constexpr int kMoveThreads = 256, kMoveRows = 64;
+
+struct MoveUnit {
+    int s, h, l, n, w, hw;
+    bool cut;
+    const int32_t *src_bt, *dst_bt, *kept;
+    char* pool;
+    float* scores;
+};
+__device__ __forceinline__ MoveUnit move_unit(const EvictParams& p, int u) {
+    MoveUnit m;
+    m.h = u % p.kv_heads, m.s = u / p.kv_heads % p.num_seqs, m.l = u / p.kv_heads / p.num_seqs;
+    m.n = p.new_lens[m.s];
+    m.cut = p.seq_lens[m.s] > m.n;
+    m.w = m.h / p.cache.heads, m.hw = m.h - m.w * p.cache.heads;
+    m.src_bt = p.src_bt + (int64_t)m.s * p.max_blocks, m.dst_bt = p.dst_bt + (int64_t)m.s * p.dst_max_blocks;
+    m.kept = p.kept + ((int64_t)(m.l * p.num_seqs + m.s) * p.kv_heads + m.h) * p.budget;
+    m.pool = p.cache.pools[m.w] + m.l * p.layer_stride + m.hw * p.cache.head_stride;
+    m.scores = p.has_scores ? p.scores[m.w] + m.l * p.layer_scores : nullptr;
+    return m;
+}
+struct RowPlace {
+    int64_t bytes;   // of the token's key in the head's part of the pool
+    int64_t score;
+};
+__device__ __forceinline__ RowPlace place(const EvictParams& p, const MoveUnit& m, const int32_t* bt, int i) {
+    const int T = p.cache.block_tokens, b = i / T, t = i - b * T;
+    const int64_t block = bt[b];
+    return RowPlace{block * p.cache.block_stride + t * p.cache.tok_stride, (block * p.cache.heads + m.hw) * T + t};
+}
+
+// Out of place: a CTA takes chunks of destination rows of one unit.
+template <int kVecs>  // 16-byte pieces of a key, or 0: any number
+__global__ void __launch_bounds__(kMoveThreads) evict_move(const __grid_constant__ EvictParams p, int chunks) {
+    __shared__ int64_t s_from[kMoveRows], s_to[kMoveRows];
+    const MoveUnit m = move_unit(p, blockIdx.x / chunks);
+    const int begin = blockIdx.x % chunks * kMoveRows;
+    if (begin >= m.n) return;
+    const int count = min(kMoveRows, m.n - begin), tid = threadIdx.x;
+    if (tid < count) {
+        const int j = begin + tid;
+        const RowPlace to = place(p, m, m.dst_bt, j), from = place(p, m, m.src_bt, m.cut ? m.kept[j] : j);
+        s_from[tid] = from.bytes, s_to[tid] = to.bytes;
+        if (m.scores) m.scores[to.score] = m.scores[from.score];
+    }
+    __syncthreads();
+    const int vecs = kVecs ? kVecs : p.vec / 16;
+    const int all = count * vecs * 2;  // piece i: row i / (2 vecs), key or value, 16 bytes of it
+    constexpr int kUnroll = 8;
+    for (int base = tid; base < all; base += kMoveThreads * kUnroll) {
+        uint4 x[kUnroll];
+        int64_t to[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int i = base + u * kMoveThreads, row = i / (2 * vecs), c = i - row * 2 * vecs, kv = c >= vecs;
+            if (i < all) {
+                const int64_t off = kv * p.cache.kv_stride + (c - kv * vecs) * 16;
+                to[u] = s_to[row] + off;
+                x[u] = ld_stream(reinterpret_cast<const uint4*>(m.pool + s_from[row] + off));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (base + u * kMoveThreads < all) st_stream(reinterpret_cast<uint4*>(m.pool + to[u]), x[u]);
     }
 }
 
-constexpr int kMoveThreads = 256;
-
-// Out of place: CTA (chunk of destination rows, layer, sequence, head); a row is a token's key and value.
-__global__ void __launch_bounds__(kMoveThreads) evict_move(const __grid_constant__ EvictParams p, int rows, int chunks) {
-    int u = blockIdx.x;
-    const int chunk = u % chunks;
-    u /= chunks;
-    const int h = u % p.kv_heads, s = u / p.kv_heads % p.num_seqs, l = u / p.kv_heads / p.num_seqs;
-    const int n = p.new_lens[s], begin = chunk * rows, T = p.cache.block_tokens;
-    if (begin >= n) return;
-    const bool cut = p.seq_lens[s] > n;
-    const int w = h / p.cache.heads, hw = h - w * p.cache.heads;
-    const int32_t *src_bt = p.src_bt + (int64_t)s * p.max_blocks, *dst_bt = p.dst_bt + (int64_t)s * p.dst_max_blocks;
-    const int32_t* kept = p.kept + ((int64_t)(l * p.num_seqs + s) * p.kv_heads + h) * p.budget;
-    char* pool = p.cache.pools[w] + l * p.layer_stride + hw * p.cache.head_stride;
-    const int count = min(rows, n - begin), vecs = p.vec / 16;
-    for (int i = threadIdx.x; i < count * vecs; i += kMoveThreads) {
-        const int j = begin + i / vecs, c = i % vecs * 16, from = cut ? kept[j] : j;
-        const char* a = pool + src_bt[from / T] * p.cache.block_stride + from % T * p.cache.tok_stride + c;
-        char* b = pool + dst_bt[j / T] * p.cache.block_stride + j % T * p.cache.tok_stride + c;
-        const uint4 key = *reinterpret_cast<const uint4*>(a), value = *reinterpret_cast<const uint4*>(a + p.cache.kv_stride);
-        *reinterpret_cast<uint4*>(b) = key;
-        *reinterpret_cast<uint4*>(b + p.cache.kv_stride) = value;
-    }
-    if (p.has_scores) {
-        float* scores = p.scores[w] + l * p.layer_scores;
-        for (int i = threadIdx.x; i < count; i += kMoveThreads) {
-            const int j = begin + i, from = cut ? kept[j] : j;
-            scores[((int64_t)dst_bt[j / T] * p.cache.heads + hw) * T + j % T] =
-                scores[((int64_t)src_bt[from / T] * p.cache.heads + hw) * T + from % T];
+// In place: a cluster of CTAs takes the kept tokens of one unit in order, a chunk at a time.  Token j of the new order
+// comes from index kept[j] >= j, so what a chunk overwrites has been read with it or with an earlier one: all of the chunk
+// is read into registers before any of it is written.
+constexpr int kCloseThreads = 512, kCloseHeld = 8;  // 16-byte pieces that a thread holds
+template <int kVecs>
+__global__ void __launch_bounds__(kCloseThreads) evict_close_up(const __grid_constant__ EvictParams p, int rows) {
+    extern __shared__ __align__(16) char smem[];  // [rows] from, [rows] to, and the scores
+    int64_t *s_from = reinterpret_cast<int64_t*>(smem), *s_to = s_from + rows;
+    const uint32_t rank = cluster_rank(), size = cluster_size();
+    const MoveUnit m = move_unit(p, blockIdx.x / size);
+    if (m.n < 0 || !m.cut) return;  // the whole cluster
+    const int vecs = kVecs ? kVecs : p.vec / 16, tid = threadIdx.x;
+    for (int base = 0; base < m.n; base += rows * size) {
+        const int begin = base + rank * rows, count = max(0, min(rows, m.n - begin)), all = count * vecs * 2;
+        // rows <= kCloseThreads: a thread holds one row's score
+        float score = 0.f;
+        int64_t score_to = -1;
+        if (tid < count) {
+            const RowPlace to = place(p, m, m.src_bt, begin + tid), from = place(p, m, m.src_bt, m.kept[begin + tid]);
+            s_from[tid] = from.bytes, s_to[tid] = to.bytes;
+            if (m.scores) score = m.scores[from.score], score_to = to.score;
         }
+        __syncthreads();
+        uint4 x[kCloseHeld];
+#pragma unroll
+        for (int u = 0; u < kCloseHeld; ++u) {
+            const int i = tid + u * kCloseThreads, row = i / (2 * vecs), c = i - row * 2 * vecs, kv = c >= vecs;
+            if (i < all)
+                x[u] = *reinterpret_cast<const uint4*>(m.pool + s_from[row] + kv * p.cache.kv_stride + (c - kv * vecs) * 16);
+        }
+        if (size > 1) cluster_sync();
+        else __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kCloseHeld; ++u) {
+            const int i = tid + u * kCloseThreads, row = i / (2 * vecs), c = i - row * 2 * vecs, kv = c >= vecs;
+            if (i < all) *reinterpret_cast<uint4*>(m.pool + s_to[row] + kv * p.cache.kv_stride + (c - kv * vecs) * 16) = x[u];
+        }
+        if (score_to >= 0) m.scores[score_to] = score;
+        __syncthreads();  // the offsets are used up
     }
 }
 
-// In place: one CTA per (layer, sequence, head) takes the kept tokens in order, a chunk at a time.  Token j of the new
-// order comes from index kept[j] >= j, so what a chunk overwrites has been read by it or by an earlier one.
-__global__ void __launch_bounds__(kMoveThreads) evict_close_up(const __grid_constant__ EvictParams p, int rows) {
-    extern __shared__ __align__(16) char smem[];
-    const int u = blockIdx.x;
-    const int h = u % p.kv_heads, s = u / p.kv_heads % p.num_seqs, l = u / p.kv_heads / p.num_seqs;
-    const int n = p.new_lens[s], T = p.cache.block_tokens;
-    if (n < 0 || p.seq_lens[s] <= n) return;
-    const int w = h / p.cache.heads, hw = h - w * p.cache.heads;
-    const int32_t* bt = p.src_bt + (int64_t)s * p.max_blocks;
-    const int32_t* kept = p.kept + ((int64_t)(l * p.num_seqs + s) * p.kv_heads + h) * p.budget;
-    char* pool = p.cache.pools[w] + l * p.layer_stride + hw * p.cache.head_stride;
-    float* scores = p.has_scores ? p.scores[w] + l * p.layer_scores : nullptr;
-    const int vecs = p.vec / 16;
-    uint4* buf = reinterpret_cast<uint4*>(smem);
-    float* sbuf = reinterpret_cast<float*>(smem + (int64_t)rows * 2 * p.vec);
-    for (int begin = 0; begin < n; begin += rows) {
-        const int count = min(rows, n - begin);
-        for (int i = threadIdx.x; i < count * vecs; i += kMoveThreads) {
-            const int from = kept[begin + i / vecs];
-            const char* a = pool + bt[from / T] * p.cache.block_stride + from % T * p.cache.tok_stride + i % vecs * 16;
-            buf[2 * i] = *reinterpret_cast<const uint4*>(a);
-            buf[2 * i + 1] = *reinterpret_cast<const uint4*>(a + p.cache.kv_stride);
-        }
-        if (scores)
-            for (int i = threadIdx.x; i < count; i += kMoveThreads) {
-                const int from = kept[begin + i];
-                sbuf[i] = scores[((int64_t)bt[from / T] * p.cache.heads + hw) * T + from % T];
-            }
-        __syncthreads();
-        for (int i = threadIdx.x; i < count * vecs; i += kMoveThreads) {
-            const int j = begin + i / vecs;
-            char* b = pool + bt[j / T] * p.cache.block_stride + j % T * p.cache.tok_stride + i % vecs * 16;
-            *reinterpret_cast<uint4*>(b) = buf[2 * i];
-            *reinterpret_cast<uint4*>(b + p.cache.kv_stride) = buf[2 * i + 1];
-        }
-        if (scores)
-            for (int i = threadIdx.x; i < count; i += kMoveThreads) {
-                const int j = begin + i;
-                scores[((int64_t)bt[j / T] * p.cache.heads + hw) * T + j % T] = sbuf[i];
-            }
-        __syncthreads();
+template <class... P, class... A>
+static amoeba_status launch_clusters(void (*kernel)(P...), int64_t grid, int threads, size_t smem, int cluster, cudaStream_t stream,
+                                     const A&... args) {
+    if (smem > 16 * 1024 && ensure_dynamic_smem((const void*)kernel, (int)smem) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((unsigned)grid);
+    c.blockDim = dim3((unsigned)threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    cudaLaunchAttribute a{};
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = (unsigned)cluster;
+    a.val.clusterDim.y = a.val.clusterDim.z = 1;
+    c.attrs = &a;
+    c.numAttrs = cluster > 1 ? 1 : 0;
+    if (cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return AMOEBA_ERR_CUDA;
     }
+    count_launch();
+    return AMOEBA_OK;
 }
 
 }  // namespace amoeba
@@ -267,19 +396,29 @@ extern "C" amoeba_status amoeba_evict_kv(const amoeba_layout* layout, int32_t la
     p.vec = layout->model.head_dim * layout->model.elem_bytes;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const int64_t units = (int64_t)p.layers * num_seqs * p.kv_heads;
-    // rows of a chunk: 64 KiB of keys and values
-    const int rows = 65536 / (2 * p.vec);
-    const int64_t most = std::min<int64_t>(budget, (int64_t)max_blocks_per_seq * layout->block_tokens);
-    const int64_t chunks = rows ? (most + rows - 1) / rows : 0;
-    if (rows < 1 || units > INT32_MAX || units * std::max<int64_t>(chunks, 1) > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
-    evict_select<<<(int)units, kSelectThreads, 0, stream>>>(p);
-    if ((st = launch_result()) != AMOEBA_OK || chunks == 0) return st;
+    const int64_t tokens = (int64_t)max_blocks_per_seq * layout->block_tokens, most = std::min<int64_t>(budget, tokens);
+    const int64_t chunks = std::max<int64_t>((most + kMoveRows - 1) / kMoveRows, 1);
+    const int pieces = p.vec / 16 * 2;
+    // in place: a row's pieces have to fit into what a CTA's threads hold
+    const int rows = std::min(kCloseThreads, kCloseThreads * kCloseHeld / pieces);
+    if (rows < 1 || units * std::max<int64_t>(chunks, kMaxCluster) > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
+    const DeviceInfo dev = cached_device_info();
+    if (!dev.sms) return AMOEBA_ERR_CUDA;
+    // CTAs to a unit: as many as hold its scores; a CTA of a full cluster may hold more, and reads them anew past that.
+    int cluster = 1;
+    while (cluster < kMaxCluster && tokens > (int64_t)cluster * kSelectKeys) cluster *= 2;
+    const int64_t slice = (tokens + cluster * 32 - 1) / (cluster * 32) * 32;
+    const int room = (int)std::min<int64_t>(slice, (dev.smem_optin - (int)sizeof(SelectShared) - 1024) / 4 / 32 * 32);
+    if ((st = launch_clusters(evict_select, units * cluster, kSelectThreads, (size_t)room * 4, cluster, stream, p, room)) != AMOEBA_OK ||
+        tokens == 0)
+        return st;
     if (p.in_place) {
-        const int smem = rows * (2 * p.vec + 4);
-        if (ensure_dynamic_smem((const void*)evict_close_up, smem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-        evict_close_up<<<(int)units, kMoveThreads, smem, stream>>>(p, rows);
-    } else {
-        evict_move<<<(int)(units * chunks), kMoveThreads, 0, stream>>>(p, rows, (int)chunks);
+        // One CTA moves about 100 GB/s; with few units, several CTAs to each.
+        int group = 1;
+        while (group < kMaxCluster && units * group * 2 <= 2 * dev.sms && (int64_t)group * rows < most) group *= 2;
+        auto* kernel = p.vec == 256 ? evict_close_up<16> : p.vec == 128 ? evict_close_up<8> : evict_close_up<0>;
+        return launch_clusters(kernel, units * group, kCloseThreads, (size_t)rows * 16, group, stream, p, rows);
     }
-    return launch_result();
+    auto* kernel = p.vec == 256 ? evict_move<16> : p.vec == 128 ? evict_move<8> : evict_move<0>;
+    return launch_clusters(kernel, units * chunks, kMoveThreads, 0, 1, stream, p, (int)chunks);
 }
