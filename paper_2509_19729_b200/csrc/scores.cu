@@ -2,8 +2,7 @@
 //
 // exp(scale * q . k - lse) needs no running statistics, so a token's sum is finished by the warp that has read its key:
 // every key is read once, the rows are walked in order for it, and no two warps add to the same score.
-#include "walk.cuh"
-#include "warp_mma.cuh"
+#include "umma.cuh"
 
 namespace amoeba {
 
@@ -20,21 +19,33 @@ struct ScoreParams {
     int32_t q_heads, window;
 };
 
-// A warp takes 16 tokens of every tile of 64; S^T = K Q^T as in attend.cu, so that a token's sum runs along the columns.
-constexpr int kScoreThreads = 128, kScoreWarps = 4, kScoreTile = 16 * kScoreWarps, kScoreStages = 6, kScoreCtas = 2;
+// ------------------------------------------------------------------------------------------------ few rows
+// Up to 8*NT rows a sequence.  Bound by the bytes of the keys.  A warp takes 16 tokens of every tile of 64; S^T = K Q^T as in
+// attend.cu, so that a token's sum runs along the columns.
+constexpr int kScoreThreads = 128, kScoreWarps = 4, kScoreTile = 16 * kScoreWarps;
+template <int D, int NT>
+struct ScoreShape {
+    static constexpr int kStage = 16 * D * 2, kStages = 6, kCtas = NT == 4 ? 2 : 3;  // CTAs per SM
+    static constexpr int kSmem = kScoreWarps * kStages * kStage;
+};
 
-template <class T, int D>
-__global__ void __launch_bounds__(kScoreThreads, kScoreCtas) accumulate_scores(const __grid_constant__ ScoreParams p) {
-    constexpr int kSteps = D / 16, kStage = 16 * D * 2;
+template <class T, int D, int NT>
+__global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score_few(const __grid_constant__ ScoreParams p) {
+    using F = ScoreShape<D, NT>;
+    constexpr int kSteps = D / 16;
     extern __shared__ __align__(128) char smem[];
-    __shared__ uint32_t s_mask[kScoreWarps][kScoreStages];
+    __shared__ uint32_t s_mask[kScoreWarps][F::kStages];
+    __shared__ int64_t s_slot[kScoreWarps][F::kStages];  // of the 16 tokens' first score, where they lie in one block
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, quad = lane / 4, pair = lane % 4;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kScoreStages * kStage;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * F::kStages * F::kStage;
     const Shape& sh = p.shape;
+    const int bt = p.cache.block_tokens;
+    const bool one_block = bt % 16 == 0;
     Walk walk;
     int64_t begin, end;
-    take_share<kScoreThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
+    take_share<kScoreThreads>(sh, p.batch, bt, &walk, &begin, &end, p.status);
     int64_t n = end - begin;
+    grid_dependency_launch();
     if (n == 0) return;
 
     Walk ahead = walk;
@@ -43,84 +54,421 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreCtas) accumulate_scores(c
     auto load = [&] {
         if (to_load > 0) {
             const int key0 = ahead.t * kScoreTile + warp * 16;
-            const uint32_t mask = load16<D, false>(p.cache, p.batch.table + (int64_t)ahead.s * p.batch.max_blocks,
-                                                   p.cache.head_base(ahead.h), key0, 0, ahead.range.hi,
-                                                   ring + slot_in * kStage, p.status);
-            if (lane == 0) s_mask[warp][slot_in] = mask;
-            if (--to_load > 0) ahead.next(sh, p.batch, p.cache.block_tokens);
+            const int32_t* table = p.batch.table + (int64_t)ahead.s * p.batch.max_blocks;
+            const uint32_t mask = load16<D, false>(p.cache, table, p.cache.head_base(ahead.h), key0, 0, ahead.range.hi,
+                                                   ring + slot_in * F::kStage, p.status);
+            if (lane == 0) {
+                s_mask[warp][slot_in] = mask;
+                if (one_block && mask)
+                    s_slot[warp][slot_in] = ((int64_t)table[key0 / bt] * p.cache.heads + ahead.h % p.cache.heads) * bt + key0 % bt;
+            }
+            if (--to_load > 0) ahead.next(sh, p.batch, bt);
         }
         cp_async_commit();
-        slot_in = slot_in + 1 == kScoreStages ? 0 : slot_in + 1;
+        slot_in = slot_in + 1 == F::kStages ? 0 : slot_in + 1;
     };
 #pragma unroll
-    for (int i = 0; i < kScoreStages - 1; ++i) load();
+    for (int i = 0; i < F::kStages - 1; ++i) load();
 
+    uint32_t qf[NT][kSteps][2];
+    int see_lo[NT][2], see_hi[NT][2];
+    float lse[NT][2];
+    int scored = 0, rows = 0;
+    bool fresh = true;
     for (; n > 0; --n) {
-        cp_async_wait<kScoreStages - 2>();
-        __syncwarp();
-        load();
-        const uint32_t k_smem = ring + slot * kStage;
-        const uint32_t mask = s_mask[warp][slot];
-        slot = slot + 1 == kScoreStages ? 0 : slot + 1;
-        uint32_t a[kSteps][4];
+        if (fresh) {
+            fresh = false;
+            const Seq& q = walk.seq;
+            const int g = sh.group, w = walk.h / p.cache.heads, h = walk.h - w * p.cache.heads;
+            rows = q.qn * g;
+            scored = p.scored ? p.scored[walk.s] : 0;
 #pragma unroll
-        for (int j = 0; j < kSteps; ++j) ldmatrix4(a[j], k_smem + swizzled<D>(lane % 16, 2 * j + lane / 16));
-
-        const Seq& q = walk.seq;
-        const int g = sh.group, rows = q.qn * g, w = walk.h / p.cache.heads, h = walk.h - w * p.cache.heads;
-        const int key0 = walk.t * kScoreTile + warp * 16 + quad;
-        float sum[2] = {0.f, 0.f};
-        if (mask)
-            for (int first = 0; first < rows; first += 8) {
-                const int r = first + quad;
-                const bool there = r < rows;
-                const int tok = r / g;
+            for (int t = 0; t < NT; ++t) {
+                const int r = t * 8 + quad, tok = r / g;
                 const char* src = p.q.base[w] + (int64_t)(q.q0 + tok) * p.q.stride + (h * g + r - tok * g) * (D * 2);
-                float st[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) {
-                    uint32_t b[2];
+                for (int j = 0; j < kSteps; ++j)
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
-                        b[i] = there ? *reinterpret_cast<const uint32_t*>(src + (j * 16 + i * 8 + pair * 2) * 2) : 0u;
-                    mma16816<T>(st, a[j], b[0], b[1]);
-                }
+                        qf[t][j][i] = r < rows ? *reinterpret_cast<const uint32_t*>(src + (j * 16 + i * 8 + pair * 2) * 2) : 0u;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const int rr = first + pair * 2 + b;
-                    if (rr >= rows) continue;
-                    const int t = rr / g, pos = q.len - q.qn + t;
-                    const float lse = p.lse[(int64_t)(q.q0 + t) * p.q_heads + walk.h * g + rr - t * g];
-                    if (lse == -INFINITY) continue;
-                    const int lo = p.window > 0 ? pos - p.window + 1 : 0;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int key = key0 + i * 8;
-                        if (key <= pos && key >= lo) sum[i] += fast_exp2(st[2 * i + b] * p.scale_log2 - lse * kLog2e);
-                    }
+                    const int rr = t * 8 + pair * 2 + b, token = rr / g, pos = q.len - q.qn + token;
+                    const float x = rr < rows ? p.lse[(int64_t)(q.q0 + token) * p.q_heads + walk.h * g + rr - token * g] : -INFINITY;
+                    lse[t][b] = x * kLog2e;
+                    see_hi[t][b] = x == -INFINITY ? 0 : pos + 1;  // a row that saw nothing adds nothing
+                    see_lo[t][b] = p.window > 0 ? pos - p.window + 1 : 0;
                 }
             }
+        }
+        cp_async_wait<F::kStages - 2>();
+        __syncwarp();
+        const uint32_t k_smem = ring + slot * F::kStage, mask = s_mask[warp][slot];
+        const int64_t first = s_slot[warp][slot];
+        load();  // into the slot that the last round has read
+        slot = slot + 1 == F::kStages ? 0 : slot + 1;
+        const int key0 = walk.t * kScoreTile + warp * 16 + quad;
+        float sum[2] = {0.f, 0.f};
+        if (mask) {
+            float st[NT][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) st[t][0] = st[t][1] = st[t][2] = st[t][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {
+                uint32_t a[4];
+                ldmatrix4(a, k_smem + swizzled<D>(lane % 16, 2 * j + lane / 16));
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma16816<T>(st[t], a, qf[t][j][0], qf[t][j][1]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = key0 + i / 2 * 8;
+                    if (key < see_hi[t][i % 2] && key >= see_lo[t][i % 2])
+                        sum[i / 2] += fast_exp2(st[t][i] * p.scale_log2 - lse[t][i % 2]);
+                }
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             sum[i] += __shfl_xor_sync(~0u, sum[i], 1);
             sum[i] += __shfl_xor_sync(~0u, sum[i], 2);
-            if (pair == 0 && (mask >> (quad + i * 8) & 1u)) {
-                const int key = key0 + i * 8, bt = p.cache.block_tokens;
-                const int block = p.batch.table[(int64_t)walk.s * p.batch.max_blocks + key / bt];
-                float* to = p.scores[w] + ((int64_t)block * p.cache.heads + h) * bt + key % bt;
-                *to = (p.scored && key < p.scored[walk.s] ? *to : 0.f) + sum[i];
+            if (pair == i && (mask >> (quad + i * 8) & 1u)) {
+                const int key = key0 + i * 8, w = walk.h / p.cache.heads, h = walk.h - w * p.cache.heads;
+                int64_t at = first + quad + i * 8;
+                if (!one_block) {
+                    const int block = p.batch.table[(int64_t)walk.s * p.batch.max_blocks + key / bt];
+                    at = ((int64_t)block * p.cache.heads + h) * bt + key % bt;
+                }
+                float* to = p.scores[w] + at;
+                *to = (key < scored ? *to : 0.f) + sum[i];
             }
         }
-        if (n > 1) walk.next(sh, p.batch, p.cache.block_tokens);
+        if (n > 1) {
+            const int h = walk.h, s = walk.s;
+            walk.next(sh, p.batch, bt);
+            fresh = walk.h != h || walk.s != s;
+        }
     }
 }
 
+// ------------------------------------------------------------------------------------------------ many rows
+// The products on the fifth-generation tensor cores, 128 tokens by 128 query rows: S^T = K Q^T, so that a thread has a token
+// and sums along its own columns.  A CTA keeps 128 rows in shared memory and runs through its tokens, 128 at a time, then the
+// next 128 rows of the same sequence and head, then its next head; the tokens of a head are dealt out to CTAs in tiles, all
+// rows with them, so a score has one thread.  Bound by the exponentials, 16 a clock and SM; two warpgroups take the tiles in
+// turn, each with two logit tiles in tensor memory, so that the products run ahead.
+constexpr int kScoreManyThreads = 384, kScoreLoadWarps = 3;
+template <int D>
+struct ScoreManyShape {
+    static constexpr int kTileBytes = 128 * D * 2, kStages = D == 128 ? 4 : 8;
+    static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
+};
+struct ScoreBarriers {
+    uint64_t k_full[8], k_empty[8], q_full[2], q_empty[2], s_full[4], s_empty[4], drain;
+    uint32_t tmem;
+    int32_t abort;
+};
+
+__device__ __forceinline__ int score_passes(const Shape& sh, const Seq& q) {  // of 128 rows
+    const int n = q.qn * sh.group;
+    return n < sh.min_rows ? 0 : (n + 127) / 128;
+}
+// Tiles times passes of one head: what it costs.
+__device__ __forceinline__ int64_t score_cost(const Shape& sh, const Seq& q) {
+    return (int64_t)((q.len + 127) / 128) * score_passes(sh, q);
+}
+
+// The runs of tiles [t0, t1) of heads that a CTA has: its share of the cost, each end moved up to a whole tile.
+struct Runs {
+    Walk w;
+    int32_t t0, t1, passes, rows;
+    int64_t off, left;  // cost in front of this CTA in its sequence, and what is left of its share
+    bool opened = false;
+
+    __device__ __forceinline__ bool next(const ScoreParams& p) {
+        const Shape& sh = p.shape;
+        while (left > 0) {
+            if (opened) {
+                ++w.h, off = 0;
+                if (w.h == sh.kv_heads) {
+                    do w.open(sh, p.batch, p.cache.block_tokens, w.s + 1);
+                    while (score_cost(sh, w.seq) == 0);
+                }
+            }
+            const int64_t cost = score_cost(sh, w.seq);
+            if (!opened) w.h = (int)(off / cost), off %= cost;
+            opened = true;
+            passes = score_passes(sh, w.seq);
+            rows = w.seq.qn * sh.group;
+            const int64_t stop = min(cost, off + left);
+            t0 = (int)((off + passes - 1) / passes), t1 = (int)((stop + passes - 1) / passes);
+            left -= stop - off;
+            if (t0 < t1) return true;
+        }
+        return false;
+    }
+};
+
+__device__ void take_runs(const ScoreParams& p, Runs* r, int32_t* status) {
+    __shared__ int64_t s_warp[kScoreManyThreads / 32], s_off;
+    __shared__ int32_t s_seq;
+    const Shape& sh = p.shape;
+    const int tid = threadIdx.x, S = p.batch.num_seqs, T = p.cache.block_tokens;
+    int64_t sum = 0;
+    for (int s = tid; s < S; s += kScoreManyThreads) sum += sh.kv_heads * score_cost(sh, sequence(p.batch, s, T));
+    const int64_t all = block_sum<kScoreManyThreads>(sum, s_warp);
+    const int64_t begin = share_begin(all, gridDim.x, blockIdx.x), end = share_begin(all, gridDim.x, blockIdx.x + 1);
+    int64_t run = 0;
+    for (int base = 0; base < S && run <= begin; base += kScoreManyThreads) {
+        const int s = base + tid;
+        const int64_t mine = s < S ? sh.kv_heads * score_cost(sh, sequence(p.batch, s, T)) : 0;
+        int64_t incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t up = __shfl_up_sync(~0u, incl, o);
+            if (tid % 32 >= o) incl += up;
+        }
+        __syncthreads();
+        if (tid % 32 == 31) s_warp[tid / 32] = incl;
+        __syncthreads();
+        int64_t before = run;
+        for (int w = 0; w < kScoreManyThreads / 32; ++w) {
+            if (w < tid / 32) before += s_warp[w];
+            run += s_warp[w];
+        }
+        const int64_t first = before + incl - mine;
+        if (begin >= first && begin < first + mine) s_seq = s, s_off = begin - first;
+    }
+    __syncthreads();
+    r->left = end - begin;
+    if (r->left > 0) {
+        r->w.open(sh, p.batch, T, s_seq);
+        r->off = s_off;
+    }
+}
+
+template <int D>
+__device__ bool score_load(const ScoreParams& p, uint32_t smem, ScoreBarriers& b, Runs run) {
+    using S = ScoreManyShape<D>;
+    TileLoader<D, kScoreLoadWarps> load(p.cache, ((int)threadIdx.x - 288) / 32, threadIdx.x % 32);
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
+    int slot = 0, qb = 0;
+    uint32_t phase = 1, q_phase = 1;
+    while (run.next(p)) {
+        load.open(run.w, p.batch);
+        const int len = run.w.seq.len;
+        for (int j = 0; j < run.passes; ++j) {
+            if (!wait(&b.q_empty[qb], q_phase)) return false;
+            load.queries(p.q, run.w, p.shape.group, j * 128, min(128, run.rows - j * 128), smem + qb * S::kTileBytes);
+            arrive_when_loaded(&b.q_full[qb]);
+            if (qb ^= 1, qb == 0) q_phase ^= 1;
+            int64_t at = load.groups(0, len, run.t0 * 128);
+            for (int t = run.t0; t < run.t1; ++t) {
+                if (!wait(&b.k_empty[slot], phase)) return false;
+                load.tokens(0, len, t * 128, at, 0, smem + (2 + slot) * S::kTileBytes);
+                arrive_when_loaded(&b.k_full[slot]);
+                if (++slot == S::kStages) slot = 0, phase ^= 1;
+                at = t + 1 < run.t1 ? load.groups(0, len, (t + 1) * 128) : -1;
+            }
+        }
+    }
+    return true;
+}
+
 template <class T, int D>
-static amoeba_status run_scores(const ScoreParams& p, int sms, cudaStream_t stream) {
-    constexpr int smem = kScoreWarps * kScoreStages * 16 * D * 2;
-    if (ensure_dynamic_smem((const void*)accumulate_scores<T, D>, smem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    accumulate_scores<T, D><<<kScoreCtas * sms, kScoreThreads, smem, stream>>>(p);
-    return launch_result();
+__device__ bool score_multiply(const ScoreParams& p, uint32_t smem, ScoreBarriers& b, Runs run) {
+    using S = ScoreManyShape<D>;
+    constexpr uint32_t kIdesc = product<T>(128, false);
+    const uint32_t tmem = __shfl_sync(~0u, b.tmem, 0), leader = elect_one();
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
+    int slot = 0, qb = 0, done[2] = {0, 0};  // tiles of each warpgroup
+    uint32_t phase = 0, q_phase = 0;
+    while (run.next(p)) {
+        for (int j = 0; j < run.passes; ++j) {
+            if (!wait(&b.q_full[qb], q_phase)) return false;
+            for (int i = 0; i < run.t1 - run.t0; ++i) {
+                const int g = i & 1, buf = g * 2 + (done[g] & 1);
+                if (!wait(&b.k_full[slot], phase)) return false;
+                if (!wait(&b.s_empty[buf], (done[g] >> 1 & 1) ^ 1)) return false;
+                ++done[g];
+                fence_async_smem();
+                tmem_fence_after();
+                const uint64_t k_op = operand(smem + (2 + __shfl_sync(~0u, slot, 0)) * S::kTileBytes, 16);
+                const uint64_t q_op = operand(smem + __shfl_sync(~0u, qb, 0) * S::kTileBytes, 16);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t step = (k / 4 * (128 * 128) + k % 4 * 32) >> 4;
+                    umma_smem(leader, tmem + buf * 128, k_op + step, q_op + step, kIdesc, k > 0);
+                }
+                umma_commit(leader, &b.s_full[buf]);
+                umma_commit(leader, &b.k_empty[slot]);
+                if (++slot == S::kStages) slot = 0, phase ^= 1;
+            }
+            umma_commit(leader, &b.q_empty[qb]);
+            if (qb ^= 1, qb == 0) q_phase ^= 1;
+        }
+    }
+    return true;
+}
+
+// s_row: [2][128] of this warpgroup, -lse * log2(e) of the pass's rows; s_pos: their cache indices.
+__device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, float (*s_row)[128], int32_t (*s_pos)[128]) {
+    const int g = threadIdx.x / 128, tid = threadIdx.x % 128, G = p.shape.group, T = p.cache.block_tokens;
+    const uint32_t lanes = (uint32_t)(tid / 32 * 32) << 16;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
+    const float c = p.scale_log2;
+    int done = 0, pass = 0;
+    while (run.next(p)) {
+        const Seq& q = run.w.seq;
+        const int w = run.w.h / p.cache.heads, hw = run.w.h - w * p.cache.heads;
+        const int32_t* table = p.batch.table + (int64_t)run.w.s * p.batch.max_blocks;
+        const int scored = p.scored ? p.scored[run.w.s] : 0;
+        for (int j = 0; j < run.passes; ++j, pass ^= 1) {
+            const int row = j * 128 + tid, tok = row / G;
+            float lse = -INFINITY;
+            int pos = -1;
+            if (row < run.rows) {
+                lse = p.lse[(int64_t)(q.q0 + tok) * p.q_heads + run.w.h * G + row - tok * G];
+                pos = q.len - q.qn + tok;
+            }
+            s_row[pass][tid] = lse == -INFINITY ? -INFINITY : -lse * kLog2e;  // a row that saw nothing adds nothing
+            s_pos[pass][tid] = pos;
+            asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + g) : "memory");
+            // what the pass's first row and its last one see, if they are there
+            const int first_pos = q.len - q.qn + j * 128 / G;
+            const int last_pos = q.len - q.qn + (min(run.rows, j * 128 + 128) - 1) / G;
+            for (int t = run.t0 + g; t < run.t1; t += 2, ++done) {
+                const int key0 = t * 128, key = key0 + tid, buf = g * 2 + (done & 1);
+                float* to = nullptr;
+                float old = 0.f;
+                if (key < q.len) {
+                    const int block = table[key / T];
+                    if (block >= 0 && block < p.cache.num_blocks) {
+                        to = p.scores[w] + ((int64_t)block * p.cache.heads + hw) * T + key % T;
+                        if (j > 0 || key < scored) old = *to;
+                    } else {
+                        report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
+                    }
+                }
+                const bool cut = key0 + 127 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
+                if (!wait(&b.s_full[buf], done >> 1 & 1)) return false;
+                tmem_fence_after();
+                const uint32_t from = b.tmem + lanes + buf * 128;
+                uint32_t s[2][32];
+                uint64_t sum[2] = {0, 0};
+                const uint64_t c2 = pair2(c, c);
+                tmem_load32(s[0], from);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    tmem_load_wait();
+                    if (i < 3) {
+                        tmem_load32(s[(i + 1) % 2], from + (i + 1) * 32);
+                    } else {
+                        tmem_fence_before();
+                        mbar_arrive(&b.s_empty[buf]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) {
+                        const float4 r = *reinterpret_cast<const float4*>(&s_row[pass][i * 32 + k]);
+                        float x[4];
+                        split2(fma2(pair2(__uint_as_float(s[i % 2][k]), __uint_as_float(s[i % 2][k + 1])), c2, pair2(r.x, r.y)), x[0], x[1]);
+                        split2(fma2(pair2(__uint_as_float(s[i % 2][k + 2]), __uint_as_float(s[i % 2][k + 3])), c2, pair2(r.z, r.w)), x[2], x[3]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = fast_exp2(x[e]);
+                        if (cut) {
+                            const int4 at = *reinterpret_cast<const int4*>(&s_pos[pass][i * 32 + k]);
+                            const int seen[4] = {at.x, at.y, at.z, at.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (key > seen[e] || (p.window > 0 && key <= seen[e] - p.window)) x[e] = 0.f;
+                        }
+                        sum[0] = add2(sum[0], pair2(x[0], x[1]));
+                        sum[1] = add2(sum[1], pair2(x[2], x[3]));
+                    }
+                }
+                float lo, hi;
+                split2(add2(sum[0], sum[1]), lo, hi);
+                if (to) *to = old + (lo + hi);
+            }
+        }
+    }
+    return true;
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_constant__ ScoreParams p) {
+    extern __shared__ char smem_raw[];
+    __shared__ ScoreBarriers b;
+    __shared__ __align__(16) float s_row[2][2][128];
+    __shared__ __align__(16) int32_t s_pos[2][2][128];
+    using S = ScoreManyShape<D>;
+    char* smem = smem_raw + (1024 - smem_u32(smem_raw) % 1024) % 1024;
+    const int warp = threadIdx.x / 32;
+    Runs run;
+    take_runs(p, &run, p.status);
+    if (run.left == 0) {
+        grid_dependency_wait();
+        return;
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&b.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) mbar_init(&b.k_full[i], 32 * kScoreLoadWarps), mbar_init(&b.k_empty[i], 1);
+        for (int i = 0; i < 2; ++i) mbar_init(&b.q_full[i], 32 * kScoreLoadWarps), mbar_init(&b.q_empty[i], 1);
+        for (int i = 0; i < 4; ++i) mbar_init(&b.s_full[i], 1), mbar_init(&b.s_empty[i], 128);
+        mbar_init(&b.drain, 1);
+        b.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_smem();
+    }
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    bool ok;
+    if (warp < 8) {
+        ok = score_sum(p, b, run, s_row[warp / 4], s_pos[warp / 4]);
+    } else if (warp == 8) {
+        ok = score_multiply<T, D>(p, smem_u32(smem), b, run);
+        __syncwarp();
+        umma_commit(elect_one(), &b.drain);
+        mbar_drain(&b.drain, 0);
+    } else {
+        ok = score_load<D>(p, smem_u32(smem), b, run);
+        cp_async_commit();
+        cp_async_wait<0>();
+    }
+    if (!ok) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+    grid_dependency_wait();  // score_few in front is done when this kernel is
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tmem_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(b.tmem));
+    }
+}
+
+template <class T, int D, int NT>
+static amoeba_status run_score_few(const ScoreParams& p, int sms, cudaStream_t stream) {
+    using F = ScoreShape<D, NT>;
+    if (ensure_dynamic_smem((const void*)score_few<T, D, NT>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    return launch_kernel(score_few<T, D, NT>, F::kCtas * sms, kScoreThreads, F::kSmem, stream, false, p);
+}
+
+// As in attend.cu: up to 32 rows, or none, by the kernel that only reads; more by the tensor cores'.
+template <class T, int D>
+static amoeba_status run_scores(ScoreParams& p, int sms, cudaStream_t stream) {
+    const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
+    p.shape.max_rows = 32;
+    const amoeba_status st = rows <= 8    ? run_score_few<T, D, 1>(p, sms, stream)
+                             : rows <= 16 ? run_score_few<T, D, 2>(p, sms, stream)
+                                          : run_score_few<T, D, 4>(p, sms, stream);
+    if (st != AMOEBA_OK || rows <= 32) return st;
+    p.shape.min_rows = 33;
+    if (ensure_dynamic_smem((const void*)score_many<T, D>, ScoreManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    return launch_kernel(score_many<T, D>, sms, kScoreManyThreads, ScoreManyShape<D>::kSmem, stream, true, p);
 }
 
 }  // namespace amoeba
@@ -155,10 +503,10 @@ extern "C" amoeba_status amoeba_accumulate_scores(const amoeba_layout* layout, i
     p.q_heads = m.num_q_heads;
     p.shape.group = m.num_q_heads / m.num_kv_heads;
     p.shape.kv_heads = m.num_kv_heads;
-    p.shape.rows = INT32_MAX;  // all rows of a sequence in one unit; its tiles run over the whole sequence
+    p.shape.rows = INT32_MAX;  // all rows of a sequence in one unit, whose tiles run over the whole sequence
     p.shape.tile = kScoreTile;
-    p.shape.max_rows = INT32_MAX;
     p.shape.rowless = 1;
+    if (((int64_t)p.batch.max_q_len + 128) * p.shape.group > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);

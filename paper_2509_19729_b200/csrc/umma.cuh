@@ -1,0 +1,184 @@
+// Fifth-generation tensor core pieces (tcgen05) shared by the operators with many query rows: products of 128-row tiles in the
+// 128-byte-swizzled layout, tensor memory, and the warps that load such tiles through the block table.
+#pragma once
+#include "walk.cuh"
+#include "warp_mma.cuh"
+
+namespace amoeba {
+
+// ---- tensor memory and products
+__device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,"
+        "%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Issued by the lane whose `leader` is 1; the whole warp comes here together, so that the operands stay in uniform registers.
+__device__ __forceinline__ void umma_smem(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate),
+        "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void umma_tmem(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate),
+        "r"(leader)
+        : "memory");
+}
+// The barrier gets one arrival when all products issued so far are done.
+__device__ __forceinline__ void umma_commit(uint32_t leader, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t is;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is;
+}
+
+// Shared-memory operand in the 128-byte swizzle: groups of eight 128-byte rows 1 KiB apart; `leading` bytes from one
+// 64-element half of a row to the next where the rows run along the product's sum (values).
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading) {
+    return (uint64_t)((addr >> 4) & 0x3fff) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// Product of 16-bit operands into 32 bits, 128 rows, n columns; b_rows: the second operand's rows run along the sum.
+template <class T>
+__device__ constexpr uint32_t product(int n, bool b_rows) {
+    const uint32_t f = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+    return 1u << 4 | f << 7 | f << 10 | (b_rows ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | 8u << 24;
+}
+
+// Byte offset of 16-byte chunk c of row r in a tile: 64-element halves of all rows one behind the other.
+__device__ __forceinline__ int tile_offset(int r, int c) { return c / 8 * (128 * 128) + r * 128 + ((c ^ r) & 7) * 16; }
+
+// ---- two 32-bit values at a time
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// ---- loading
+// One arrival of this thread, when all the asynchronous loads that it has started are done.  The products' warp makes them
+// visible to the tensor core (fence_async_smem after its wait): a fence here would wait for the loads still in flight.
+__device__ __forceinline__ void arrive_when_loaded(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// The tiles that kWarps warps load together, each lane 16 bytes at a time.
+template <int D, int kWarps>
+struct TileLoader {
+    const CacheView& v;
+    const int warp, lane;
+    const char* head = nullptr;        // the key head's part of its pool,
+    const int32_t* table = nullptr;    // the sequence's blocks
+    static constexpr int kChunks = D / 8, kStep = 32 / kChunks;  // a warp loads kStep rows at a time
+
+    __device__ __forceinline__ TileLoader(const CacheView& v_, int warp_, int lane_) : v(v_), warp(warp_), lane(lane_) {}
+    __device__ __forceinline__ void open(const Walk& w, const Batch& b) {
+        head = v.head_base(w.h);
+        table = b.table + (int64_t)w.s * b.max_blocks;
+    }
+    // Where the 16 groups of eight tokens of the tile at key0 lie in the head's part of the pool, one per lane; -1: no token
+    // in [lo, hi), or a bad block.
+    __device__ __forceinline__ int64_t groups(int lo, int hi, int key0) const {
+        const int key = key0 + lane * 8;
+        if (v.block_tokens % 8 || lane >= 16 || key >= hi || key + 8 <= lo) return -1;
+        const int i = key / v.block_tokens, block = table[i];
+        return block >= 0 && block < v.num_blocks ? block * v.block_stride + (key - i * v.block_tokens) * v.tok_stride : -1;
+    }
+    // Starts the loads of the keys (kv = 0) or values (1) of 128 tokens; zeros outside [lo, hi) and for bad blocks.
+    __device__ __forceinline__ void tokens(int lo, int hi, int key0, int64_t at, int kv, uint32_t dst) const {
+        const int c = lane % kChunks, sub = lane / kChunks;
+        const char* from = head + kv * v.kv_stride + c * 16;
+        if (key0 >= lo && key0 + 128 <= hi && __all_sync(~0u, lane >= 16 || at >= 0)) {
+            const char* first = from + sub * v.tok_stride;
+            const int64_t step = kStep * v.tok_stride;
+#pragma unroll
+            for (int j = 0; j < (16 + kWarps - 1) / kWarps; ++j) {
+                const int g = warp + j * kWarps;
+                const char* src = first + __shfl_sync(~0u, at, g & 15);
+                if (g < 16) {
+#pragma unroll
+                    for (int i = 0; i < 8 / kStep; ++i)
+                        cp_async16(dst + g * 1024 + tile_offset(i * kStep + sub, c), src + i * step, 16);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int g = warp; g < 16; g += kWarps) {
+                const int64_t own = __shfl_sync(~0u, at, g);
+#pragma unroll 1
+                for (int i = 0; i < 8 / kStep; ++i) {
+                    const int r = g * 8 + i * kStep + sub, key = key0 + r;
+                    bool in = key >= lo && key < hi;
+                    const char* src = head;
+                    if (v.block_tokens % 8 == 0) {
+                        in = in && own >= 0;
+                        if (in) src = from + own + r % 8 * v.tok_stride;
+                    } else if (in) {
+                        const int block = table[key / v.block_tokens];
+                        in = block >= 0 && block < v.num_blocks;
+                        if (in) src = from + block * v.block_stride + key % v.block_tokens * v.tok_stride;
+                    }
+                    cp_async16(dst + tile_offset(r, c), src, in ? 16 : 0);
+                }
+            }
+        }
+    }
+    // Starts the loads of `count` (at most 128) query rows of w's sequence and key head, from row `row` on; zeros behind.
+    __device__ __forceinline__ void queries(const Rows& q, const Walk& w, int group, int row, int count, uint32_t dst) const {
+        const int c = lane % kChunks, sub = lane / kChunks, worker = w.h / v.heads;
+        const char* base = q.base[worker] + (int64_t)w.seq.q0 * q.stride + (w.h - worker * v.heads) * group * (D * 2) + c * 16;
+        for (int first = warp * 32; first < 128; first += kWarps * 32) {
+            const int r = row + first + lane, tok = r / group;
+            const int64_t mine = first + lane < count ? tok * q.stride + (r - tok * group) * (D * 2) : -1;
+#pragma unroll
+            for (int i = 0; i < 32; i += kStep) {
+                const int64_t off = __shfl_sync(~0u, mine, i + sub);
+                cp_async16(dst + tile_offset(first + i + sub, c), off >= 0 ? base + off : v.pools[0], off >= 0 ? 16 : 0);
+            }
+        }
+    }
+};
+
+}  // namespace amoeba
