@@ -55,17 +55,13 @@ attend_few(const __grid_constant__ AttendParams p) {
     grid_dependency_launch();
     if (n == 0) return;
 
-    Walk ahead = walk;
-    int64_t to_load = n;
+    Ahead<D, true, kFewTile> ahead(p.cache, p.batch, sh, p.status, walk, n, warp * 16);
     int slot_in = 0, slot = 0;
     auto load = [&] {
-        if (to_load > 0) {
-            const int key0 = ahead.range.base + ahead.t * kFewTile + warp * 16;
-            const uint32_t mask = load16<D, true>(p.cache, p.batch.table + (int64_t)ahead.s * p.batch.max_blocks,
-                                                  p.cache.head_base(ahead.h), key0, ahead.range.lo, ahead.range.hi,
-                                                  ring + slot_in * F::kStage, p.status);
+        if (ahead.left > 0) {
+            int64_t first;
+            const uint32_t mask = ahead.load(ring + slot_in * F::kStage, &first);
             if (lane == 0) s_mask[warp][slot_in] = mask;
-            if (--to_load > 0) ahead.next(sh, p.batch, p.cache.block_tokens);
         }
         cp_async_commit();
         slot_in = slot_in + 1 == F::kStages ? 0 : slot_in + 1;

@@ -48,21 +48,13 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
     grid_dependency_launch();
     if (n == 0) return;
 
-    Walk ahead = walk;
-    int64_t to_load = n;
+    Ahead<D, false, kScoreTile> ahead(p.cache, p.batch, sh, p.status, walk, n, warp * 16);
     int slot_in = 0, slot = 0;
     auto load = [&] {
-        if (to_load > 0) {
-            const int key0 = ahead.t * kScoreTile + warp * 16;
-            const int32_t* table = p.batch.table + (int64_t)ahead.s * p.batch.max_blocks;
-            const uint32_t mask = load16<D, false>(p.cache, table, p.cache.head_base(ahead.h), key0, 0, ahead.range.hi,
-                                                   ring + slot_in * F::kStage, p.status);
-            if (lane == 0) {
-                s_mask[warp][slot_in] = mask;
-                if (one_block && mask)
-                    s_slot[warp][slot_in] = ((int64_t)table[key0 / bt] * p.cache.heads + ahead.h % p.cache.heads) * bt + key0 % bt;
-            }
-            if (--to_load > 0) ahead.next(sh, p.batch, bt);
+        if (ahead.left > 0) {
+            int64_t first;
+            const uint32_t mask = ahead.load(ring + slot_in * F::kStage, &first);
+            if (lane == 0) s_mask[warp][slot_in] = mask, s_slot[warp][slot_in] = first;
         }
         cp_async_commit();
         slot_in = slot_in + 1 == F::kStages ? 0 : slot_in + 1;
@@ -74,6 +66,7 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
     int see_lo[NT][2], see_hi[NT][2];
     float lse[NT][2];
     int scored = 0, rows = 0;
+    float* scores = nullptr;
     bool fresh = true;
     for (; n > 0; --n) {
         if (fresh) {
@@ -81,6 +74,7 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
             const Seq& q = walk.seq;
             const int g = sh.group, w = walk.h / p.cache.heads, h = walk.h - w * p.cache.heads;
             rows = q.qn * g;
+            scores = p.scores[w];
             scored = p.scored ? p.scored[walk.s] : 0;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -134,13 +128,13 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
             sum[i] += __shfl_xor_sync(~0u, sum[i], 1);
             sum[i] += __shfl_xor_sync(~0u, sum[i], 2);
             if (pair == i && (mask >> (quad + i * 8) & 1u)) {
-                const int key = key0 + i * 8, w = walk.h / p.cache.heads, h = walk.h - w * p.cache.heads;
+                const int key = key0 + i * 8;
                 int64_t at = first + quad + i * 8;
                 if (!one_block) {
                     const int block = p.batch.table[(int64_t)walk.s * p.batch.max_blocks + key / bt];
-                    at = ((int64_t)block * p.cache.heads + h) * bt + key % bt;
+                    at = ((int64_t)block * p.cache.heads + walk.h % p.cache.heads) * bt + key % bt;
                 }
-                float* to = p.scores[w] + at;
+                float* to = scores + at;
                 *to = (key < scored ? *to : 0.f) + sum[i];
             }
         }

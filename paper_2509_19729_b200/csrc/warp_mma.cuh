@@ -1,7 +1,7 @@
 // Warp-level pieces shared by the operators that read the cache with few query rows: asynchronous 16-byte loads into
 // swizzled shared memory, 8x8 matrix loads and the 16x8x16 matrix instruction.
 #pragma once
-#include "cache_view.cuh"
+#include "walk.cuh"
 
 namespace amoeba {
 
@@ -52,57 +52,109 @@ __device__ __forceinline__ int swizzled(int r, int c) {
     return r * (D * 2) + ((c & 8) | ((c ^ r) & 7)) * 16;
 }
 
-// Starts the loads of 16 consecutive tokens' keys (and, with_values, values) of one head into `dst`, [K][V][16][D]
-// swizzled, by one warp; tokens outside [lo, hi) and of bad blocks become zeros.  Returns the mask of the others.
-// table: the sequence's row of the block table; head: the head's base address in its pool.
-template <int D, bool kValues>
-__device__ __forceinline__ uint32_t load16(const CacheView& v, const int32_t* table, const char* head, int key0, int lo,
-                                           int hi, uint32_t dst, int32_t* status) {
-    constexpr int kChunks = D / 8, kStep = 32 / kChunks, kRows = 16 / kStep;
-    const int lane = threadIdx.x & 31, c = lane % kChunks, r0 = lane / kChunks;
-    uint32_t mask = 0;
-    bool bad = false;
-    if (v.block_tokens % 16 == 0) {  // key0 is a multiple of 16: all in one block
-        int block = -1;
-        if (key0 < hi && key0 + 16 > lo) {
-            block = table[key0 / v.block_tokens];
-            bad = block < 0 || block >= v.num_blocks;
-        }
-        const bool ok = block >= 0 && !bad;
-        const char* src = head + (ok ? block * v.block_stride + (key0 % v.block_tokens) * v.tok_stride : 0) + c * 16;
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int r = r0 + i * kStep;
-            const bool in = ok && key0 + r >= lo && key0 + r < hi;
-            const char* s = in ? src + r * v.tok_stride : head;
-            cp_async16(dst + swizzled<D>(r, c), s, in ? 16 : 0);
-            if (kValues) cp_async16(dst + 16 * D * 2 + swizzled<D>(r, c), in ? s + v.kv_stride : s, in ? 16 : 0);
-        }
-        if (ok) {
-            const int a = max(lo - key0, 0), b = min(hi - key0, 16);
-            mask = ((1u << b) - 1) & ~((1u << a) - 1);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int r = r0 + i * kStep, key = key0 + r;
-            bool in = key >= lo && key < hi;
-            const char* s = head;
-            if (in) {
-                const int block = table[key / v.block_tokens];
-                in = block >= 0 && block < v.num_blocks;
-                bad |= !in;
-                if (in) s = head + block * v.block_stride + (key % v.block_tokens) * v.tok_stride + c * 16;
-            }
-            cp_async16(dst + swizzled<D>(r, c), s, in ? 16 : 0);
-            if (kValues) cp_async16(dst + 16 * D * 2 + swizzled<D>(r, c), in ? s + v.kv_stride : s, in ? 16 : 0);
-            const uint32_t there = __ballot_sync(~0u, in);
-#pragma unroll
-            for (int j = 0; j < kStep; ++j) mask |= (there >> (j * kChunks) & 1u) << (i * kStep + j);
+// One warp's loads of 16 consecutive tokens' keys (and, kValues, values) of one head at a time, [K][V][16][D] swizzled, ahead
+// of the warp's own walk over the tiles (kTile tokens each, the warp's 16 at `offset` in every tile).  The block that the
+// next tokens lie in is looked up one step early.
+template <int D, bool kValues, int kTile>
+struct Ahead {
+    const CacheView& v;
+    const Batch& b;
+    const Shape& shape;
+    int32_t* status;
+    const int lane, offset;
+    const bool one_block;  // 16 tokens lie in one block
+    Walk w;
+    int64_t left;          // tiles to go
+    const int32_t* table;
+    const char* head;
+    int32_t hw, block = -1, in_block = 0;
+
+    __device__ __forceinline__ Ahead(const CacheView& v_, const Batch& b_, const Shape& s_, int32_t* status_, const Walk& w_, int64_t n,
+                                     int offset_)
+        : v(v_), b(b_), shape(s_), status(status_), lane(threadIdx.x & 31), offset(offset_), one_block(v_.block_tokens % 16 == 0), w(w_),
+          left(n) {
+        if (left > 0) {
+            open();
+            look_up();
         }
     }
-    if (bad) report(status, AMOEBA_ERR_BAD_BLOCK_ID);
-    return mask;
-}
+    __device__ __forceinline__ void open() {
+        table = b.table + (int64_t)w.s * b.max_blocks;
+        const int r = w.h / v.heads;
+        hw = w.h - r * v.heads;
+        head = v.pools[r] + hw * v.head_stride;
+    }
+    __device__ __forceinline__ int key0() const { return w.range.base + w.t * kTile + offset; }
+    __device__ __forceinline__ void look_up() {
+        const int k = key0();
+        block = -1;
+        if (one_block && k < w.range.hi && k + 16 > w.range.lo) {
+            const int i = k / v.block_tokens;
+            in_block = k - i * v.block_tokens;
+            block = table[i];
+        }
+    }
+    // Starts the loads into `dst`; tokens outside [lo, hi) of the unit and of bad blocks become zeros.  Returns the mask of
+    // the others; *slot: of the 16 tokens' first score in the worker's score pool, where they lie in one block.
+    __device__ __forceinline__ uint32_t load(uint32_t dst, int64_t* slot) {
+        constexpr int kChunks = D / 8, kStep = 32 / kChunks, kRows = 16 / kStep;
+        const int c = lane % kChunks, r0 = lane / kChunks, lo = w.range.lo, hi = w.range.hi, k0 = key0();
+        uint32_t mask = 0;
+        bool bad = false;
+        if (one_block) {
+            const bool ok = block >= 0 && block < v.num_blocks;
+            bad = !ok && k0 < hi && k0 + 16 > lo;
+            if (ok) {
+                const int a = max(lo - k0, 0), z = min(hi - k0, 16);
+                mask = ((1u << z) - 1) & ~((1u << a) - 1);
+            }
+            *slot = ((int64_t)block * v.heads + hw) * v.block_tokens + in_block;
+            const char* src = head + (ok ? block * v.block_stride + in_block * v.tok_stride : 0) + r0 * v.tok_stride + c * 16;
+            if (mask == 0xffffu) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    const char* s = src + i * kStep * v.tok_stride;
+                    cp_async16(dst + swizzled<D>(r0 + i * kStep, c), s, 16);
+                    if (kValues) cp_async16(dst + 16 * D * 2 + swizzled<D>(r0 + i * kStep, c), s + v.kv_stride, 16);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    const int r = r0 + i * kStep;
+                    const bool in = mask >> r & 1u;
+                    const char* s = in ? src + i * kStep * v.tok_stride : head;
+                    cp_async16(dst + swizzled<D>(r, c), s, in ? 16 : 0);
+                    if (kValues) cp_async16(dst + 16 * D * 2 + swizzled<D>(r, c), in ? s + v.kv_stride : s, in ? 16 : 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int r = r0 + i * kStep, key = k0 + r;
+                bool in = key >= lo && key < hi;
+                const char* s = head;
+                if (in) {
+                    const int own = table[key / v.block_tokens];
+                    in = own >= 0 && own < v.num_blocks;
+                    bad |= !in;
+                    if (in) s = head + own * v.block_stride + (key % v.block_tokens) * v.tok_stride + c * 16;
+                }
+                cp_async16(dst + swizzled<D>(r, c), s, in ? 16 : 0);
+                if (kValues) cp_async16(dst + 16 * D * 2 + swizzled<D>(r, c), in ? s + v.kv_stride : s, in ? 16 : 0);
+                const uint32_t there = __ballot_sync(~0u, in);
+#pragma unroll
+                for (int j = 0; j < kStep; ++j) mask |= (there >> (j * kChunks) & 1u) << (i * kStep + j);
+            }
+        }
+        if (bad) report(status, AMOEBA_ERR_BAD_BLOCK_ID);
+        if (--left > 0) {
+            const int h = w.h, s = w.s;
+            w.next(shape, b, v.block_tokens);
+            if (w.h != h || w.s != s) open();
+            look_up();
+        }
+        return mask;
+    }
+};
 
 }  // namespace amoeba
