@@ -4,6 +4,7 @@
 // A head's vector lies in head_dim / 8 neighbouring lanes, 16 bytes each, so that the norm's sum and the partner of a
 // rotated pair are shuffles; the angles of a token are computed once per block, in 64 bits, for all its heads.
 #include "cache_view.cuh"
+#include "copy_engine.cuh"
 
 namespace amoeba {
 
@@ -36,9 +37,30 @@ __device__ __forceinline__ int find_sequence(const Batch& b, int row, int* share
 template <class T, int D>
 __global__ void __launch_bounds__(kAppendThreads) append_kv(const __grid_constant__ AppendParams p) {
     constexpr int kLanes = D / 8;  // lanes per head
+    constexpr int kBatch = 6;      // heads that a thread holds a piece of at a time
+    constexpr int kStride = kAppendThreads / kLanes;
     __shared__ float s_cos[64], s_sin[64];
     __shared__ int s_seq;
-    const int row = blockIdx.x;
+    const int row = blockIdx.x, lane = threadIdx.x % kLanes;
+    const int per_worker = p.q_heads + 2 * p.cache.heads, n = p.tp * per_worker;
+    // The row's vectors do not depend on where the token goes: they are under way while that is looked up.
+    uint4 raw[kBatch];
+    auto load = [&](int first) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int vec = first + i * kStride;
+            raw[i] = make_uint4(0, 0, 0, 0);
+            if (vec < n) {
+                const int r = vec / per_worker, h = vec - r * per_worker;
+                const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.cache.heads;
+                const int head = is_q ? h : is_v ? h - p.q_heads - p.cache.heads : h - p.q_heads;
+                const Rows& from = is_q ? p.q : is_v ? p.v : p.k;
+                raw[i] = ld_stream(reinterpret_cast<const uint4*>(from.base[r] + row * from.stride + head * (D * 2) + lane * 16));
+            }
+        }
+    };
+    int first = threadIdx.x / kLanes;
+    load(first);
     const int s = find_sequence(p.batch, row, &s_seq);
     if (s < 0) return;
     const Seq seq = sequence(p.batch, s, p.cache.block_tokens);
@@ -48,88 +70,91 @@ __global__ void __launch_bounds__(kAppendThreads) append_kv(const __grid_constan
     }
     const int index = seq.len - seq.qn + (row - seq.q0);
     const int block = p.batch.table[(int64_t)s * p.batch.max_blocks + index / p.cache.block_tokens];
-    const bool cached = block >= 0 && block < p.cache.num_blocks;
-    if (!cached && threadIdx.x == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
     const int half = p.rot / 2;
     if (p.inv_freq) {
         if (threadIdx.x < half) {
             const double turn = 6.283185307179586476925;
             double a = (double)(p.positions ? p.positions[row] : index) * p.inv_freq[threadIdx.x];
-            a -= turn * rint(a / turn);
+            a -= turn * rint(a * (1. / turn));
             sincosf((float)a, &s_sin[threadIdx.x], &s_cos[threadIdx.x]);
         }
         __syncthreads();
     }
+    const bool cached = block >= 0 && block < p.cache.num_blocks;
+    if (!cached && threadIdx.x == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
     const int64_t slot = (int64_t)block * p.cache.block_stride + (index % p.cache.block_tokens) * p.cache.tok_stride;
-    const int lane = threadIdx.x % kLanes;
-    const int per_worker = p.q_heads + 2 * p.cache.heads;
-    const int n = p.tp * per_worker;
-    // whole warps go round together: the shuffles below need all their lanes
-    for (int first = threadIdx.x / 32 * (32 / kLanes); first < n; first += kAppendThreads / kLanes) {
-        const int vec = first + threadIdx.x % 32 / kLanes;
-        const bool there = vec < n;
-        const int r = there ? vec / per_worker : 0, h = there ? vec - r * per_worker : 0;
-        const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.cache.heads;
-        const int head = is_q ? h : is_v ? h - p.q_heads - p.cache.heads : h - p.q_heads;
-        const Rows& from = is_q ? p.q : is_v ? p.v : p.k;
-        uint4 raw = make_uint4(0, 0, 0, 0);
-        if (there) raw = *reinterpret_cast<const uint4*>(from.base[r] + row * from.stride + head * (D * 2) + lane * 16);
-        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-        float x[8];
+    for (;;) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = Elem<T>::unpack(w[i]);
-            x[2 * i] = f.x, x[2 * i + 1] = f.y;
-        }
-        const void* norm = is_q ? p.q_norm : p.k_norm;
-        float sum = 0.f;
+        for (int i = 0; i < kBatch; ++i) {
+            const int vec = first + i * kStride;
+            // whole warps go on together: the shuffles below need all their lanes
+            if (first - threadIdx.x % 32 / kLanes + i * kStride >= n) break;
+            const bool there = vec < n;
+            const int r = there ? vec / per_worker : 0, h = there ? vec - r * per_worker : 0;
+            const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.cache.heads;
+            const int head = is_q ? h : is_v ? h - p.q_heads - p.cache.heads : h - p.q_heads;
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
-#pragma unroll
-        for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-        if (norm && !is_v) {
-            const float inv = 1.f / sqrtf(sum * (1.f / D) + p.eps);
-            const uint4 nw = reinterpret_cast<const uint4*>(norm)[lane];
-            const uint32_t g[4] = {nw.x, nw.y, nw.z, nw.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = Elem<T>::unpack(g[i]);
-                x[2 * i] *= inv * f.x, x[2 * i + 1] *= inv * f.y;
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = Elem<T>::unpack(w[j]);
+                x[2 * j] = f.x, x[2 * j + 1] = f.y;
             }
-        }
-        if (p.inv_freq) {  // block-uniform
-            if (p.interleaved) {
-                if (lane * 8 < p.rot && !is_v) {
+            const void* norm = is_q ? p.q_norm : p.k_norm;
+            if (p.q_norm || p.k_norm) {
+                float sum = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float c = s_cos[lane * 4 + i], sn = s_sin[lane * 4 + i], a = x[2 * i], b = x[2 * i + 1];
-                        x[2 * i] = a * c - b * sn, x[2 * i + 1] = b * c + a * sn;
-                    }
-                }
-            } else {
-                const int hl = half / 8;  // lanes per half
-                const bool second = lane >= hl;
-                const int partner = lane >= 2 * hl ? lane : second ? lane - hl : lane + hl;
+                for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float other = __shfl_sync(~0u, x[i], partner, kLanes);
-                    if (lane < 2 * hl && !is_v) {
-                        const int j = (second ? lane - hl : lane) * 8 + i;
-                        x[i] = second ? x[i] * s_cos[j] + other * s_sin[j] : x[i] * s_cos[j] - other * s_sin[j];
+                for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+                if (norm && !is_v) {
+                    const float inv = 1.f / sqrtf(sum * (1.f / D) + p.eps);
+                    const uint4 nw = reinterpret_cast<const uint4*>(norm)[lane];
+                    const uint32_t g[4] = {nw.x, nw.y, nw.z, nw.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 f = Elem<T>::unpack(g[j]);
+                        x[2 * j] *= inv * f.x, x[2 * j + 1] *= inv * f.y;
                     }
                 }
             }
+            if (p.inv_freq) {  // block-uniform
+                if (p.interleaved) {
+                    if (lane * 8 < p.rot && !is_v) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float c = s_cos[lane * 4 + j], sn = s_sin[lane * 4 + j], a = x[2 * j], b = x[2 * j + 1];
+                            x[2 * j] = a * c - b * sn, x[2 * j + 1] = b * c + a * sn;
+                        }
+                    }
+                } else {
+                    const int hl = half / 8;  // lanes per half
+                    const bool second = lane >= hl;
+                    const int partner = lane >= 2 * hl ? lane : second ? lane - hl : lane + hl;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float other = __shfl_sync(~0u, x[j], partner, kLanes);
+                        if (lane < 2 * hl && !is_v) {
+                            const int k = (second ? lane - hl : lane) * 8 + j;
+                            x[j] = second ? x[j] * s_cos[k] + other * s_sin[k] : x[j] * s_cos[k] - other * s_sin[k];
+                        }
+                    }
+                }
+            }
+            if (!there) continue;
+            uint4 out = raw[i];  // values go as they are
+            if (!is_v)
+                out = make_uint4(Elem<T>::pack(x[0], x[1]), Elem<T>::pack(x[2], x[3]), Elem<T>::pack(x[4], x[5]),
+                                 Elem<T>::pack(x[6], x[7]));
+            if (is_q)
+                *reinterpret_cast<uint4*>(p.q_out.base[r] + row * p.q_out.stride + head * (D * 2) + lane * 16) = out;
+            else if (cached)
+                *reinterpret_cast<uint4*>(p.cache.pools[r] + slot + head * p.cache.head_stride +
+                                          (is_v ? p.cache.kv_stride : 0) + lane * 16) = out;
         }
-        if (!there) continue;
-        uint4 out = raw;  // values go as they are
-        if (!is_v)
-            out = make_uint4(Elem<T>::pack(x[0], x[1]), Elem<T>::pack(x[2], x[3]), Elem<T>::pack(x[4], x[5]),
-                             Elem<T>::pack(x[6], x[7]));
-        if (is_q)
-            *reinterpret_cast<uint4*>(p.q_out.base[r] + row * p.q_out.stride + head * (D * 2) + lane * 16) = out;
-        else if (cached)
-            *reinterpret_cast<uint4*>(p.cache.pools[r] + slot + head * p.cache.head_stride +
-                                      (is_v ? p.cache.kv_stride : 0) + lane * 16) = out;
+        first += kBatch * kStride;
+        if (first - threadIdx.x % 32 / kLanes >= n) break;
+        load(first);
     }
 }
 

@@ -230,11 +230,12 @@ attend_few(const __grid_constant__ AttendParams p) {
 
 // ------------------------------------------------------------------------------------------------ joining
 // Joins the parts of the units that were cut.  kWarps warps to a row: with few rows a unit may be in as many parts as there
-// are CTAs, so its four warps take every fourth part each; with many rows it is in two or three, and a warp does a row.
+// are CTAs, so its eight warps take every eighth part each; with many rows it is in two or three, and a warp does a row.
+constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 template <class T, int D, int kWarps>
 __device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int block) {
     const Shape& sh = p.shape;
-    constexpr int kRows = 4 / kWarps;  // per CTA
+    constexpr int kRows = kJoinWarps / kWarps;  // per CTA
     const int groups = sh.rows / kRows;  // blocks for every share: its first unit is joined here if it began in the share before
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int mine = block / groups;
@@ -260,7 +261,7 @@ __device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int b
     float top = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < rows) {
-#pragma unroll 4
+#pragma unroll 8
         for (int c = c0 + stripe; c < c1; c += kWarps * kAtOnce) {
             if (p.cuts[c].begin == p.cuts[c].end) continue;  // an empty share
             const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
@@ -285,14 +286,14 @@ __device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int b
         const float top2 = __shfl_down_sync(~0u, top, 16), l2 = __shfl_down_sync(~0u, l, 16);
         merge(top2, l2, x);
     }
-    if (kWarps == 4) {
-        __shared__ float4 s_acc[4][kLanes];
-        __shared__ float s_top[4], s_l[4];
+    if (kWarps > 1) {
+        __shared__ float4 s_acc[kWarps][kLanes];
+        __shared__ float s_top[kWarps], s_l[kWarps];
         if (lane < kLanes) s_acc[warp][lane] = acc;
         if (lane == 0) s_top[warp] = top, s_l[warp] = l;
         __syncthreads();
         if (warp) return;
-        for (int w = 1; w < 4; ++w) merge(s_top[w], s_l[w], s_acc[w][lane % kLanes]);
+        for (int w = 1; w < kWarps; ++w) merge(s_top[w], s_l[w], s_acc[w][lane % kLanes]);
     }
     if (r >= rows || lane >= kLanes) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -303,10 +304,10 @@ __device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int b
 }
 // Blocks [0, few_blocks) join what attend_few has cut, the others what attend_many has.
 template <class T, int D>
-__global__ void __launch_bounds__(128) attend_join(const __grid_constant__ AttendParams few, int few_ctas, int few_blocks,
+__global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constant__ AttendParams few, int few_ctas, int few_blocks,
                                                    const __grid_constant__ AttendParams many, int many_ctas) {
     grid_dependency_wait();
-    if ((int)blockIdx.x < few_blocks) join_rows<T, D, 4>(few, few_ctas, blockIdx.x);
+    if ((int)blockIdx.x < few_blocks) join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x);
     else join_rows<T, D, 1>(many, many_ctas, blockIdx.x - few_blocks);
 }
 
@@ -346,8 +347,8 @@ static amoeba_status run_few(AttendParams& p, int sms, int* ctas, cudaStream_t s
                          false, p);
 }
 
-// Sequences with at most 32 rows (new tokens times query heads per key head) are read by attend_few, whose time is that of
-// reading the cache; the others by attend_many.  Which there are is known only on the device: a batch that may hold longer
+// Sequences with few rows (new tokens times query heads per key head) are read by attend_few, whose time is that of reading
+// the cache; the others by attend_many.  Which there are is known only on the device: a batch that may hold longer
 // ones gets both, and each skips the other's.  The launches follow one another closely: a kernel's blocks may be in place
 // before the kernel in front of it ends, and wait there for its results if they read them (attend_join) or end only after
 // it (attend_many).
@@ -355,11 +356,14 @@ template <class T, int D>
 static amoeba_status run_attend(AttendParams& p, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
     const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
     const int64_t few_bytes = few_workspace(&p, ws, D);
+    // In a batch with longer pieces attend_few gets the single tokens (and what has as few rows): its rows cost registers.
+    const int64_t few_rows = rows <= kMaxFewRows ? rows : p.shape.group;
+    const int most = few_rows <= 8 ? 8 : few_rows <= 16 ? 16 : kMaxFewRows;
     p.shape.min_rows = 0;
-    p.shape.max_rows = kMaxFewRows;
+    p.shape.max_rows = most;
     int few_ctas = 0;
-    amoeba_status st = rows <= 8    ? run_few<T, D, 1>(p, sms, &few_ctas, stream)
-                       : rows <= 16 ? run_few<T, D, 2>(p, sms, &few_ctas, stream)
+    amoeba_status st = most == 8    ? run_few<T, D, 1>(p, sms, &few_ctas, stream)
+                       : most == 16 ? run_few<T, D, 2>(p, sms, &few_ctas, stream)
                                     : run_few<T, D, 4>(p, sms, &few_ctas, stream);
     if (st != AMOEBA_OK || (p.whole && rows <= kMaxFewRows)) return st;
     const int few_blocks = p.whole ? 0 : few_ctas * p.shape.rows;
@@ -367,15 +371,15 @@ static amoeba_status run_attend(AttendParams& p, int32_t dtype, char* ws, int sm
     int many_ctas = 0, many_blocks = 0;
     if (rows > kMaxFewRows) {
         many_workspace(&many, ws + few_bytes, D);
-        many.shape.min_rows = kMaxFewRows + 1;
+        many.shape.min_rows = most + 1;
         many.shape.max_rows = INT32_MAX;
         many.shape.rows = kManyRows;
         many.shape.tile = kManyTile;
         many_ctas = std::min(sms, kMaxSms);
-        many_blocks = many_ctas * (kManyRows / 4);
+        many_blocks = many_ctas * (kManyRows / kJoinWarps);
         if ((st = launch_attend_many(many, dtype, D, many_ctas, stream)) != AMOEBA_OK) return st;
     }
-    return launch_kernel(attend_join<T, D>, few_blocks + many_blocks, 128, 0, stream, true, p, few_ctas, few_blocks, many, many_ctas);
+    return launch_kernel(attend_join<T, D>, few_blocks + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_blocks, many, many_ctas);
 }
 
 }  // namespace amoeba

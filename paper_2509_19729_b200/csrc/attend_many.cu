@@ -234,7 +234,7 @@ struct Loader : TileLoader<D, kLoadWarps> {
     __device__ __forceinline__ Loader(const AttendParams& p_, uint32_t smem_, ManyBarriers& b_, int warp, int lane)
         : Base(p_.cache, warp, lane), p(p_), smem(smem_), b(b_) {}
     // Starts the loads of the tile's keys (kv = 0) or values (1).
-    __device__ __forceinline__ bool tile(const Range& range, int key0, int64_t at, int kv) {
+    __device__ __forceinline__ bool tile(const Range& range, int key0, const typename Base::Group& at, int kv) {
         if (!__all_sync(~0u, mbar_wait_bounded(&b.empty[slot], phase, 0, &b.abort))) return false;
         Base::tokens(range.lo, range.hi, key0, at, kv, smem + (2 + slot) * kTile);
         arrive_when_loaded(&b.full[slot]);
@@ -260,14 +260,14 @@ __device__ void load_loop(const AttendParams& p, const Share& share, char* smem,
         const Walk& w = part.w;
         load.open(w, p.batch);
         int key0 = w.range.base + w.t * kManyTile;
-        int64_t at = load.groups(w.range.lo, w.range.hi, key0);
+        auto at = load.groups(w.range.lo, w.range.hi, key0), next = load.groups(w.range.lo, w.range.hi, key0 + kManyTile);
         ok = load.queries(part, q_phase);
         q_phase ^= 1;
         for (int i = 0; ok && i < part.tiles; ++i, key0 += kManyTile) {
             ok = load.tile(w.range, key0, at, 0);
-            const int64_t next = i + 1 < part.tiles ? load.groups(w.range.lo, w.range.hi, key0 + kManyTile) : -1;
             if (ok) ok = load.tile(w.range, key0, at, 1);
             at = next;
+            if (i + 2 < part.tiles) next = load.groups(w.range.lo, w.range.hi, key0 + 2 * kManyTile);
         }
     }
     cp_async_commit();

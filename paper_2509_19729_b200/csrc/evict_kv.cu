@@ -56,8 +56,8 @@ constexpr int kSelectKeys = 12288, kMaxCluster = 8;  // keys that a CTA holds, u
 constexpr int kDigits = 2048;
 
 struct SelectShared {
-    int32_t count[kDigits];   // of this CTA's tokens, by digit
-    int32_t total[kDigits];   // of the cluster's
+    alignas(16) int32_t count[kDigits];  // of this CTA's tokens, by digit
+    alignas(16) int32_t total[kDigits];  // of the cluster's
     int32_t warp[kSelectWarps];
     int32_t more, equal;      // this CTA's tokens above the limit, and at it
     int32_t found[2];         // digit, and how many at it stay
@@ -86,6 +86,12 @@ __device__ __forceinline__ int32_t load_remote(const int32_t* p, uint32_t rank) 
     return v;
 }
 
+__device__ __forceinline__ void store_remote(int32_t* p, uint32_t rank, int32_t v) {
+    uint32_t addr = (uint32_t)__cvta_generic_to_shared(p), remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(remote), "r"(v) : "memory");
+}
+
 __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_constant__ EvictParams p, int room) {
     extern __shared__ __align__(16) uint32_t s_keys[];
     __shared__ SelectShared sh;
@@ -107,19 +113,33 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
     const int begin = min(free, (int)rank * run), n = min(free - begin, run);
     const float* scores = p.scores[w] + l * p.layer_scores;
     const int32_t* table = p.src_bt + (int64_t)s * p.max_blocks;
-    auto score_at = [&](int i) { return scores + ((int64_t)table[i / T] * p.cache.heads + hw) * T + i % T; };
+    auto score_at = [&](int i) { return ((int64_t)table[i / T] * p.cache.heads + hw) * T + i % T; };
     const bool held = n <= room;
     if (held) {
-        if (T % 4 == 0) {
-            for (int i = tid * 4; i < n; i += kSelectThreads * 4) {  // (run is a multiple of 32: i is in one block)
-                const float4 x = *reinterpret_cast<const float4*>(score_at(begin + i));
-                *reinterpret_cast<uint4*>(s_keys + i) = make_uint4(order_of(x.x), order_of(x.y), order_of(x.z), order_of(x.w));
+        if (T % 4 == 0) {  // (run is a multiple of 32: four tokens from a multiple of four on are in one block)
+            constexpr int kAtOnce = 4;
+            for (int base = tid * 4; base < n; base += kSelectThreads * 4 * kAtOnce) {
+                int64_t at[kAtOnce];
+                float4 x[kAtOnce];
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const int i = base + u * kSelectThreads * 4;
+                    if (i < n) at[u] = score_at(begin + i);
+                }
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+                    if (base + u * kSelectThreads * 4 < n) x[u] = *reinterpret_cast<const float4*>(scores + at[u]);
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+                    if (base + u * kSelectThreads * 4 < n)
+                        *reinterpret_cast<uint4*>(s_keys + base + u * kSelectThreads * 4) =
+                            make_uint4(order_of(x[u].x), order_of(x[u].y), order_of(x[u].z), order_of(x[u].w));
             }
         } else {
-            for (int i = tid; i < n; i += kSelectThreads) s_keys[i] = order_of(*score_at(begin + i));
+            for (int i = tid; i < n; i += kSelectThreads) s_keys[i] = order_of(scores[score_at(begin + i)]);
         }
     }
-    auto key_of = [&](int i) { return held ? s_keys[i] : order_of(*score_at(begin + i)); };
+    auto key_of = [&](int i) { return held ? s_keys[i] : order_of(scores[score_at(begin + i)]); };
 
     uint32_t limit = 0;  // found so far, from the top
     int left = need;     // how many of the tokens that agree with it stay
@@ -139,16 +159,25 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
             }
         }
         __syncthreads();
-        if (size > 1) cluster_sync();
-        // from the largest digit down: thread t has digits 2047 - 4t ... 2044 - 4t
-        int mine[4], sum = 0;
+        const int32_t* total = sh.count;
+        if (size > 1) {  // every CTA adds up its part of the digits and hands the sums to all
+            cluster_sync();
+            const int part = kDigits / size;
+            for (int d = rank * part + tid; d < (int)(rank + 1) * part; d += kSelectThreads) {
+                int v[kMaxCluster], sum = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int d = kDigits - 1 - tid * 4 - j;
-            mine[j] = sh.count[d];
-            for (uint32_t r = 1; r < size; ++r) mine[j] += load_remote(&sh.count[d], (rank + r) % size);
-            sum += mine[j];
+                for (uint32_t r = 0; r < kMaxCluster; ++r) v[r] = r < size ? load_remote(&sh.count[d], r) : 0;
+#pragma unroll
+                for (uint32_t r = 0; r < kMaxCluster; ++r) sum += v[r];
+                for (uint32_t r = 0; r < size; ++r) store_remote(&sh.total[d], r, sum);
+            }
+            cluster_sync();
+            total = sh.total;
         }
+        // from the largest digit down: thread t has digits 2047 - 4t ... 2044 - 4t
+        const int4 four = *reinterpret_cast<const int4*>(&total[kDigits - 4 - tid * 4]);
+        const int mine[4] = {four.w, four.z, four.y, four.x};
+        int sum = mine[0] + mine[1] + mine[2] + mine[3];
         int before = sum;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -167,8 +196,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
                 before += mine[j];
             }
         }
-        if (size > 1) cluster_sync();  // before the counts are cleared
-        else __syncthreads();
+        __syncthreads();
         limit |= (uint32_t)sh.found[0] << shift;
         left = sh.found[1];
     }
@@ -210,7 +238,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
 // ------------------------------------------------------------------------------------------------ the move
 // Rows are tokens: a key and a value of `vec` bytes each.  The offsets of a chunk of rows are worked out once, a thread a row,
 // and the rows then copied 16 bytes a lane with as many loads in flight as a lane has stores.
-constexpr int kMoveThreads = 256, kMoveRows = 64;
+constexpr int kMoveThreads = 256, kMoveRows = 256;  // rows: at most, a thread each
 
 struct MoveUnit {
     int s, h, l, n, w, hw;
@@ -243,12 +271,12 @@ __device__ __forceinline__ RowPlace place(const EvictParams& p, const MoveUnit& 
 
 // Out of place: a CTA takes chunks of destination rows of one unit.
 template <int kVecs>  // 16-byte pieces of a key, or 0: any number
-__global__ void __launch_bounds__(kMoveThreads) evict_move(const __grid_constant__ EvictParams p, int chunks) {
+__global__ void __launch_bounds__(kMoveThreads) evict_move(const __grid_constant__ EvictParams p, int chunks, int rows) {
     __shared__ int64_t s_from[kMoveRows], s_to[kMoveRows];
     const MoveUnit m = move_unit(p, blockIdx.x / chunks);
-    const int begin = blockIdx.x % chunks * kMoveRows;
+    const int begin = blockIdx.x % chunks * rows;
     if (begin >= m.n) return;
-    const int count = min(kMoveRows, m.n - begin), tid = threadIdx.x;
+    const int count = min(rows, m.n - begin), tid = threadIdx.x;
     if (tid < count) {
         const int j = begin + tid;
         const RowPlace to = place(p, m, m.dst_bt, j), from = place(p, m, m.src_bt, m.cut ? m.kept[j] : j);
@@ -397,11 +425,10 @@ extern "C" amoeba_status amoeba_evict_kv(const amoeba_layout* layout, int32_t la
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const int64_t units = (int64_t)p.layers * num_seqs * p.kv_heads;
     const int64_t tokens = (int64_t)max_blocks_per_seq * layout->block_tokens, most = std::min<int64_t>(budget, tokens);
-    const int64_t chunks = std::max<int64_t>((most + kMoveRows - 1) / kMoveRows, 1);
     const int pieces = p.vec / 16 * 2;
     // in place: a row's pieces have to fit into what a CTA's threads hold
     const int rows = std::min(kCloseThreads, kCloseThreads * kCloseHeld / pieces);
-    if (rows < 1 || units * std::max<int64_t>(chunks, kMaxCluster) > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
+    if (rows < 1 || units * std::max<int64_t>((most + 31) / 32, kMaxCluster) > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
     // CTAs to a unit: as many as hold its scores; a CTA of a full cluster may hold more, and reads them anew past that.
@@ -420,5 +447,9 @@ extern "C" amoeba_status amoeba_evict_kv(const amoeba_layout* layout, int32_t la
         return launch_clusters(kernel, units * group, kCloseThreads, (size_t)rows * 16, group, stream, p, rows);
     }
     auto* kernel = p.vec == 256 ? evict_move<16> : p.vec == 128 ? evict_move<8> : evict_move<0>;
-    return launch_clusters(kernel, units * chunks, kMoveThreads, 0, 1, stream, p, (int)chunks);
+    // Out of place: long chunks, in which looking up the rows counts for little, if that leaves four CTAs to an SM.
+    int chunk = kMoveRows;
+    while (chunk > 32 && units * ((most + chunk - 1) / chunk) < 4 * dev.sms) chunk /= 2;
+    const int64_t chunks = std::max<int64_t>((most + chunk - 1) / chunk, 1);
+    return launch_clusters(kernel, units * chunks, kMoveThreads, 0, 1, stream, p, (int)chunks, chunk);
 }

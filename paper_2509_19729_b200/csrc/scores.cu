@@ -25,7 +25,7 @@ struct ScoreParams {
 constexpr int kScoreThreads = 128, kScoreWarps = 4, kScoreTile = 16 * kScoreWarps;
 template <int D, int NT>
 struct ScoreShape {
-    static constexpr int kStage = 16 * D * 2, kStages = 6, kCtas = NT == 4 ? 2 : 3;  // CTAs per SM
+    static constexpr int kStage = 16 * D * 2, kStages = NT == 4 ? 4 : 2, kCtas = NT == 1 ? 5 : NT == 2 ? 3 : 2;  // CTAs per SM
     static constexpr int kSmem = kScoreWarps * kStages * kStage;
 };
 
@@ -257,13 +257,14 @@ __device__ bool score_load(const ScoreParams& p, uint32_t smem, ScoreBarriers& b
             load.queries(p.q, run.w, p.shape.group, j * 128, min(128, run.rows - j * 128), smem + qb * S::kTileBytes);
             arrive_when_loaded(&b.q_full[qb]);
             if (qb ^= 1, qb == 0) q_phase ^= 1;
-            int64_t at = load.groups(0, len, run.t0 * 128);
+            auto at = load.groups(0, len, run.t0 * 128), next = load.groups(0, len, run.t0 * 128 + 128);
             for (int t = run.t0; t < run.t1; ++t) {
                 if (!wait(&b.k_empty[slot], phase)) return false;
                 load.tokens(0, len, t * 128, at, 0, smem + (2 + slot) * S::kTileBytes);
                 arrive_when_loaded(&b.k_full[slot]);
                 if (++slot == S::kStages) slot = 0, phase ^= 1;
-                at = t + 1 < run.t1 ? load.groups(0, len, (t + 1) * 128) : -1;
+                at = next;
+                if (t + 2 < run.t1) next = load.groups(0, len, (t + 2) * 128);
             }
         }
     }
@@ -318,6 +319,7 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
         const int w = run.w.h / p.cache.heads, hw = run.w.h - w * p.cache.heads;
         const int32_t* table = p.batch.table + (int64_t)run.w.s * p.batch.max_blocks;
         const int scored = p.scored ? p.scored[run.w.s] : 0;
+        float* scores = p.scores[w];
         for (int j = 0; j < run.passes; ++j, pass ^= 1) {
             const int row = j * 128 + tid, tok = row / G;
             float lse = -INFINITY;
@@ -332,18 +334,25 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
             // what the pass's first row and its last one see, if they are there
             const int first_pos = q.len - q.qn + j * 128 / G;
             const int last_pos = q.len - q.qn + (min(run.rows, j * 128 + 128) - 1) / G;
+            // the block of the next tile's token is asked for a tile early
+            int at = (run.t0 + g) * 128 + tid, i_block = at / T, in_block = at - i_block * T, block = -1;
+            if (run.t0 + g < run.t1 && at < q.len) block = table[i_block];
             for (int t = run.t0 + g; t < run.t1; t += 2, ++done) {
                 const int key0 = t * 128, key = key0 + tid, buf = g * 2 + (done & 1);
                 float* to = nullptr;
                 float old = 0.f;
                 if (key < q.len) {
-                    const int block = table[key / T];
                     if (block >= 0 && block < p.cache.num_blocks) {
-                        to = p.scores[w] + ((int64_t)block * p.cache.heads + hw) * T + key % T;
+                        to = scores + ((int64_t)block * p.cache.heads + hw) * T + in_block;
                         if (j > 0 || key < scored) old = *to;
                     } else {
                         report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
                     }
+                }
+                at = key + 256;
+                if (t + 2 < run.t1 && at < q.len) {
+                    i_block = at / T, in_block = at - i_block * T;
+                    block = table[i_block];
                 }
                 const bool cut = key0 + 127 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
                 if (!wait(&b.s_full[buf], done >> 1 & 1)) return false;
@@ -451,16 +460,17 @@ static amoeba_status run_score_few(const ScoreParams& p, int sms, cudaStream_t s
     return launch_kernel(score_few<T, D, NT>, F::kCtas * sms, kScoreThreads, F::kSmem, stream, false, p);
 }
 
-// As in attend.cu: up to 32 rows, or none, by the kernel that only reads; more by the tensor cores'.
+// As in attend.cu: few rows, or none, by the kernel that only reads; more by the tensor cores'.
 template <class T, int D>
 static amoeba_status run_scores(ScoreParams& p, int sms, cudaStream_t stream) {
-    const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
-    p.shape.max_rows = 32;
-    const amoeba_status st = rows <= 8    ? run_score_few<T, D, 1>(p, sms, stream)
-                             : rows <= 16 ? run_score_few<T, D, 2>(p, sms, stream)
+    const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group, few_rows = rows <= 32 ? rows : p.shape.group;
+    const int most = few_rows <= 8 ? 8 : few_rows <= 16 ? 16 : 32;
+    p.shape.max_rows = most;
+    const amoeba_status st = most == 8    ? run_score_few<T, D, 1>(p, sms, stream)
+                             : most == 16 ? run_score_few<T, D, 2>(p, sms, stream)
                                           : run_score_few<T, D, 4>(p, sms, stream);
     if (st != AMOEBA_OK || rows <= 32) return st;
-    p.shape.min_rows = 33;
+    p.shape.min_rows = most + 1;
     if (ensure_dynamic_smem((const void*)score_many<T, D>, ScoreManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
     return launch_kernel(score_many<T, D>, sms, kScoreManyThreads, ScoreManyShape<D>::kSmem, stream, true, p);
 }

@@ -118,16 +118,25 @@ struct TileLoader {
         head = v.head_base(w.h);
         table = b.table + (int64_t)w.s * b.max_blocks;
     }
-    // Where the 16 groups of eight tokens of the tile at key0 lie in the head's part of the pool, one per lane; -1: no token
-    // in [lo, hi), or a bad block.
-    __device__ __forceinline__ int64_t groups(int lo, int hi, int key0) const {
+    // The blocks that the 16 groups of eight tokens of the tile at key0 lie in, one per lane; -1: no token in [lo, hi).  Asked
+    // for well ahead: nothing here waits for the answer.
+    struct Group {
+        int32_t block, in_block;
+    };
+    __device__ __forceinline__ Group groups(int lo, int hi, int key0) const {
         const int key = key0 + lane * 8;
-        if (v.block_tokens % 8 || lane >= 16 || key >= hi || key + 8 <= lo) return -1;
-        const int i = key / v.block_tokens, block = table[i];
-        return block >= 0 && block < v.num_blocks ? block * v.block_stride + (key - i * v.block_tokens) * v.tok_stride : -1;
+        Group g{-1, 0};
+        if (v.block_tokens % 8 == 0 && lane < 16 && key < hi && key + 8 > lo) {
+            const int i = key / v.block_tokens;
+            g.in_block = key - i * v.block_tokens;
+            g.block = table[i];
+        }
+        return g;
     }
     // Starts the loads of the keys (kv = 0) or values (1) of 128 tokens; zeros outside [lo, hi) and for bad blocks.
-    __device__ __forceinline__ void tokens(int lo, int hi, int key0, int64_t at, int kv, uint32_t dst) const {
+    __device__ __forceinline__ void tokens(int lo, int hi, int key0, const Group& group, int kv, uint32_t dst) const {
+        const int64_t at = group.block >= 0 && group.block < v.num_blocks
+                               ? group.block * v.block_stride + group.in_block * v.tok_stride : -1;
         const int c = lane % kChunks, sub = lane / kChunks;
         const char* from = head + kv * v.kv_stride + c * 16;
         if (key0 >= lo && key0 + 128 <= hi && __all_sync(~0u, lane >= 16 || at >= 0)) {
