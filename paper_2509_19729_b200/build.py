@@ -18,9 +18,9 @@ LIB_CHECKED = HERE / "libamoeba_checked.so"  # the same sources with -DAMOEBA_CH
 #                                              against the extent of its buffers before it is moved
 TORCH_CALLS = HERE / "_torch_calls.so"  # the serving operators' Python calls on torch tensors
 SOURCES = ["plan.cpp", "block_tables.cu", "kv_reshard.cu", "weights_reshard.cu", "append_kv.cu", "attend.cu", "attend_many.cu",
-           "scores.cu", "evict_kv.cu"]
+           "scores.cu", "evict_kv.cu", "cache_maps.cu"]
 HEADERS = ["plan.hpp", "launch.hpp", "copy_engine.cuh", "kv_items.cuh", "w_items.cuh", "cache_view.cuh", "walk.cuh", "attend.cuh",
-           "warp_mma.cuh", "umma.cuh"]
+           "warp_mma.cuh", "umma.cuh", "cache_maps.hpp"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",

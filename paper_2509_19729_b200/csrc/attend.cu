@@ -353,7 +353,7 @@ static amoeba_status run_few(AttendParams& p, int sms, int* ctas, cudaStream_t s
 // before the kernel in front of it ends, and wait there for its results if they read them (attend_join) or end only after
 // it (attend_many).
 template <class T, int D>
-static amoeba_status run_attend(AttendParams& p, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
+static amoeba_status run_attend(AttendParams& p, int tp, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
     const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
     const int64_t few_bytes = few_workspace(&p, ws, D);
     // In a batch with longer pieces attend_few gets the single tokens (and what has as few rows): its rows cost registers.
@@ -377,7 +377,7 @@ static amoeba_status run_attend(AttendParams& p, int32_t dtype, char* ws, int sm
         many.shape.tile = kManyTile;
         many_ctas = std::min(sms, kMaxSms);
         many_blocks = many_ctas * (kManyRows / kJoinWarps);
-        if ((st = launch_attend_many(many, dtype, D, many_ctas, stream)) != AMOEBA_OK) return st;
+        if ((st = launch_attend_many(many, tp, dtype, D, many_ctas, stream)) != AMOEBA_OK) return st;
     }
     return launch_kernel(attend_join<T, D>, few_blocks + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_blocks, many, many_ctas);
 }
@@ -441,8 +441,8 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(d_workspace);
     if (dtype == AMOEBA_FP16)
-        return m.head_dim == 64 ? run_attend<__half, 64>(p, dtype, ws, dev.sms, stream)
-                                : run_attend<__half, 128>(p, dtype, ws, dev.sms, stream);
-    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, dtype, ws, dev.sms, stream)
-                            : run_attend<__nv_bfloat16, 128>(p, dtype, ws, dev.sms, stream);
+        return m.head_dim == 64 ? run_attend<__half, 64>(p, layout->tp, dtype, ws, dev.sms, stream)
+                                : run_attend<__half, 128>(p, layout->tp, dtype, ws, dev.sms, stream);
+    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, layout->tp, dtype, ws, dev.sms, stream)
+                            : run_attend<__nv_bfloat16, 128>(p, layout->tp, dtype, ws, dev.sms, stream);
 }

@@ -33,6 +33,6 @@ __device__ __forceinline__ float* lse_of(const AttendParams& p, const Seq& q, in
 // The kernel for many rows (attend_many.cu): 256 rows a unit, 128 tokens a tile.
 constexpr int kManyRows = 256, kManyTile = 128;
 constexpr int kMaxSms = 192;  // bounds the grids, and so the workspace, without asking the device
-amoeba_status launch_attend_many(const AttendParams& p, int32_t dtype, int head_dim, int ctas, cudaStream_t stream);
+amoeba_status launch_attend_many(const AttendParams& p, int tp, int32_t dtype, int head_dim, int ctas, cudaStream_t stream);
 
 }  // namespace amoeba

@@ -231,13 +231,13 @@ struct Loader : TileLoader<D, kLoadWarps> {
     uint32_t phase = 1;  // of `empty`: the first round waits for nothing
     static constexpr int kTile = ManyShape<D>::kTileBytes;
 
-    __device__ __forceinline__ Loader(const AttendParams& p_, uint32_t smem_, ManyBarriers& b_, int warp, int lane)
-        : Base(p_.cache, warp, lane), p(p_), smem(smem_), b(b_) {}
+    __device__ __forceinline__ Loader(const AttendParams& p_, const CacheMaps& maps, int box_rows, uint32_t smem_, ManyBarriers& b_, int warp,
+                                      int lane)
+        : Base(p_.cache, maps, box_rows, warp, lane), p(p_), smem(smem_), b(b_) {}
     // Starts the loads of the tile's keys (kv = 0) or values (1).
     __device__ __forceinline__ bool tile(const Range& range, int key0, const typename Base::Group& at, int kv) {
         if (!__all_sync(~0u, mbar_wait_bounded(&b.empty[slot], phase, 0, &b.abort))) return false;
-        Base::tokens(range.lo, range.hi, key0, at, kv, smem + (2 + slot) * kTile);
-        arrive_when_loaded(&b.full[slot]);
+        Base::tokens(range.lo, range.hi, key0, at, kv, smem + (2 + slot) * kTile, &b.full[slot]);
         if (++slot == ManyShape<D>::kStages) slot = 0, phase ^= 1;
         return true;
     }
@@ -251,8 +251,8 @@ struct Loader : TileLoader<D, kLoadWarps> {
 };
 
 template <int D>
-__device__ void load_loop(const AttendParams& p, const Share& share, char* smem, ManyBarriers& b) {
-    Loader<D> load{p, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32};
+__device__ void load_loop(const AttendParams& p, const CacheMaps& maps, int box_rows, const Share& share, char* smem, ManyBarriers& b) {
+    Loader<D> load(p, maps, box_rows, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32);
     uint32_t q_phase = 1;
     bool ok = true;
     Parts part(share);
@@ -531,7 +531,8 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
 }
 
 template <class T, int D>
-__global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_constant__ AttendParams p) {
+__global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_constant__ AttendParams p, const __grid_constant__ CacheMaps maps,
+                                                            int box_rows) {
     extern __shared__ char smem_raw[];
     __shared__ ManyBarriers b;
     char* smem = smem_raw + (1024 - smem_u32(smem_raw) % 1024) % 1024;
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
             __syncwarp();
             drain_products(b);
         } else {
-            load_loop<D>(p, share, smem, b);
+            load_loop<D>(p, maps, box_rows, share, smem, b);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
@@ -583,15 +584,17 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
 }
 
 template <class T, int D>
-static amoeba_status launch(const AttendParams& p, int ctas, cudaStream_t stream) {
+static amoeba_status launch(const AttendParams& p, const CacheMaps& maps, int box_rows, int ctas, cudaStream_t stream) {
     if (ensure_dynamic_smem((const void*)attend_many<T, D>, ManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    return launch_kernel(attend_many<T, D>, ctas, kManyThreads, ManyShape<D>::kSmem, stream, true, p);
+    return launch_kernel(attend_many<T, D>, ctas, kManyThreads, ManyShape<D>::kSmem, stream, true, p, maps, box_rows);
 }
 
-amoeba_status launch_attend_many(const AttendParams& p, int32_t dtype, int head_dim, int ctas, cudaStream_t stream) {
+amoeba_status launch_attend_many(const AttendParams& p, int tp, int32_t dtype, int head_dim, int ctas, cudaStream_t stream) {
+    CacheMaps maps;
+    const int rows = make_cache_maps(&maps, p.cache, tp, head_dim, dtype);
     if (dtype == AMOEBA_FP16)
-        return head_dim == 64 ? launch<__half, 64>(p, ctas, stream) : launch<__half, 128>(p, ctas, stream);
-    return head_dim == 64 ? launch<__nv_bfloat16, 64>(p, ctas, stream) : launch<__nv_bfloat16, 128>(p, ctas, stream);
+        return head_dim == 64 ? launch<__half, 64>(p, maps, rows, ctas, stream) : launch<__half, 128>(p, maps, rows, ctas, stream);
+    return head_dim == 64 ? launch<__nv_bfloat16, 64>(p, maps, rows, ctas, stream) : launch<__nv_bfloat16, 128>(p, maps, rows, ctas, stream);
 }
 
 }  // namespace amoeba

@@ -243,9 +243,9 @@ __device__ void take_runs(const ScoreParams& p, Runs* r, int32_t* status) {
 }
 
 template <int D>
-__device__ bool score_load(const ScoreParams& p, uint32_t smem, ScoreBarriers& b, Runs run) {
+__device__ bool score_load(const ScoreParams& p, const CacheMaps& maps, int box_rows, uint32_t smem, ScoreBarriers& b, Runs run) {
     using S = ScoreManyShape<D>;
-    TileLoader<D, kScoreLoadWarps> load(p.cache, ((int)threadIdx.x - 288) / 32, threadIdx.x % 32);
+    TileLoader<D, kScoreLoadWarps> load(p.cache, maps, box_rows, ((int)threadIdx.x - 288) / 32, threadIdx.x % 32);
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
     int slot = 0, qb = 0;
     uint32_t phase = 1, q_phase = 1;
@@ -260,8 +260,7 @@ __device__ bool score_load(const ScoreParams& p, uint32_t smem, ScoreBarriers& b
             auto at = load.groups(0, len, run.t0 * 128), next = load.groups(0, len, run.t0 * 128 + 128);
             for (int t = run.t0; t < run.t1; ++t) {
                 if (!wait(&b.k_empty[slot], phase)) return false;
-                load.tokens(0, len, t * 128, at, 0, smem + (2 + slot) * S::kTileBytes);
-                arrive_when_loaded(&b.k_full[slot]);
+                load.tokens(0, len, t * 128, at, 0, smem + (2 + slot) * S::kTileBytes, &b.k_full[slot]);
                 if (++slot == S::kStages) slot = 0, phase ^= 1;
                 at = next;
                 if (t + 2 < run.t1) next = load.groups(0, len, (t + 2) * 128);
@@ -400,7 +399,8 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
 }
 
 template <class T, int D>
-__global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_constant__ ScoreParams p) {
+__global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_constant__ ScoreParams p, const __grid_constant__ CacheMaps maps,
+                                                                int box_rows) {
     extern __shared__ char smem_raw[];
     __shared__ ScoreBarriers b;
     __shared__ __align__(16) float s_row[2][2][128];
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_
         umma_commit(elect_one(), &b.drain);
         mbar_drain(&b.drain, 0);
     } else {
-        ok = score_load<D>(p, smem_u32(smem), b, run);
+        ok = score_load<D>(p, maps, box_rows, smem_u32(smem), b, run);
         cp_async_commit();
         cp_async_wait<0>();
     }
@@ -462,7 +462,7 @@ static amoeba_status run_score_few(const ScoreParams& p, int sms, cudaStream_t s
 
 // As in attend.cu: few rows, or none, by the kernel that only reads; more by the tensor cores'.
 template <class T, int D>
-static amoeba_status run_scores(ScoreParams& p, int sms, cudaStream_t stream) {
+static amoeba_status run_scores(ScoreParams& p, const amoeba_layout* layout, int32_t dtype, int sms, cudaStream_t stream) {
     const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group, few_rows = rows <= 32 ? rows : p.shape.group;
     const int most = few_rows <= 8 ? 8 : few_rows <= 16 ? 16 : 32;
     p.shape.max_rows = most;
@@ -472,7 +472,9 @@ static amoeba_status run_scores(ScoreParams& p, int sms, cudaStream_t stream) {
     if (st != AMOEBA_OK || rows <= 32) return st;
     p.shape.min_rows = most + 1;
     if (ensure_dynamic_smem((const void*)score_many<T, D>, ScoreManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    return launch_kernel(score_many<T, D>, sms, kScoreManyThreads, ScoreManyShape<D>::kSmem, stream, true, p);
+    CacheMaps maps;
+    const int box_rows = make_cache_maps(&maps, p.cache, layout->tp, D, dtype);
+    return launch_kernel(score_many<T, D>, sms, kScoreManyThreads, ScoreManyShape<D>::kSmem, stream, true, p, maps, box_rows);
 }
 
 }  // namespace amoeba
@@ -516,7 +518,7 @@ extern "C" amoeba_status amoeba_accumulate_scores(const amoeba_layout* layout, i
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     p.window = std::min(window, 1 << 30);  // not the shape's: every token gets a value, zero if no row sees it
     if (dtype == AMOEBA_FP16)
-        return m.head_dim == 64 ? run_scores<__half, 64>(p, dev.sms, stream) : run_scores<__half, 128>(p, dev.sms, stream);
-    return m.head_dim == 64 ? run_scores<__nv_bfloat16, 64>(p, dev.sms, stream)
-                            : run_scores<__nv_bfloat16, 128>(p, dev.sms, stream);
+        return m.head_dim == 64 ? run_scores<__half, 64>(p, layout, dtype, dev.sms, stream) : run_scores<__half, 128>(p, layout, dtype, dev.sms, stream);
+    return m.head_dim == 64 ? run_scores<__nv_bfloat16, 64>(p, layout, dtype, dev.sms, stream)
+                            : run_scores<__nv_bfloat16, 128>(p, layout, dtype, dev.sms, stream);
 }

@@ -1,6 +1,8 @@
 // Fifth-generation tensor core pieces (tcgen05) shared by the operators with many query rows: products of 128-row tiles in the
 // 128-byte-swizzled layout, tensor memory, and the warps that load such tiles through the block table.
 #pragma once
+#include "cache_maps.hpp"
+#include "copy_engine.cuh"
 #include "walk.cuh"
 #include "warp_mma.cuh"
 
@@ -104,18 +106,34 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 __device__ __forceinline__ void arrive_when_loaded(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-// The tiles that kWarps warps load together, each lane 16 bytes at a time.
+// A box of a worker's pool (cache_maps.hpp) into shared memory, by the TMA unit.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int dim, int token, int kv, int head, int block,
+                                         uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
+            "r"(dst), "l"(map), "r"(dim), "r"(token), "r"(kv), "r"(head), "r"(block), "r"(smem_u32(bar))
+        : "memory");
+}
+// The tiles that kWarps warps load together: by boxes where all 128 tokens are wanted and the blocks have a box's shape, else
+// each lane 16 bytes at a time.
 template <int D, int kWarps>
 struct TileLoader {
     const CacheView& v;
-    const int warp, lane;
+    const CacheMaps& maps;
+    const int box_rows, warp, lane;    // box_rows 0: no maps
     const char* head = nullptr;        // the key head's part of its pool,
     const int32_t* table = nullptr;    // the sequence's blocks
+    const CUtensorMap* map = nullptr;
+    int hw = 0;                        // head of the worker
     static constexpr int kChunks = D / 8, kStep = 32 / kChunks;  // a warp loads kStep rows at a time
 
-    __device__ __forceinline__ TileLoader(const CacheView& v_, int warp_, int lane_) : v(v_), warp(warp_), lane(lane_) {}
+    __device__ __forceinline__ TileLoader(const CacheView& v_, const CacheMaps& maps_, int box_rows_, int warp_, int lane_)
+        : v(v_), maps(maps_), box_rows(box_rows_), warp(warp_), lane(lane_) {}
     __device__ __forceinline__ void open(const Walk& w, const Batch& b) {
-        head = v.head_base(w.h);
+        const int r = w.h / v.heads;
+        hw = w.h - r * v.heads;
+        head = v.pools[r] + hw * v.head_stride;
+        map = &maps.worker[r];
         table = b.table + (int64_t)w.s * b.max_blocks;
     }
     // The blocks that the 16 groups of eight tokens of the tile at key0 lie in, one per lane; -1: no token in [lo, hi).  Asked
@@ -133,13 +151,27 @@ struct TileLoader {
         }
         return g;
     }
-    // Starts the loads of the keys (kv = 0) or values (1) of 128 tokens; zeros outside [lo, hi) and for bad blocks.
-    __device__ __forceinline__ void tokens(int lo, int hi, int key0, const Group& group, int kv, uint32_t dst) const {
-        const int64_t at = group.block >= 0 && group.block < v.num_blocks
-                               ? group.block * v.block_stride + group.in_block * v.tok_stride : -1;
+    // Starts the loads of the keys (kv = 0) or values (1) of 128 tokens, which arrive at `bar` with one arrival of each thread;
+    // zeros outside [lo, hi) and for bad blocks.
+    __device__ __forceinline__ void tokens(int lo, int hi, int key0, const Group& group, int kv, uint32_t dst, uint64_t* bar) const {
+        const bool good = group.block >= 0 && group.block < v.num_blocks;
+        const bool whole = key0 >= lo && key0 + 128 <= hi && __all_sync(~0u, lane >= 16 || good);
+        if (whole && box_rows) {
+            constexpr int kHalves = D / 64;
+            const int i = warp + lane * kWarps, row = i / kHalves * box_rows, half = i % kHalves;
+            const int block = __shfl_sync(~0u, group.block, row / 8 & 15), token = __shfl_sync(~0u, group.in_block, row / 8 & 15);
+            if (row < 128) {
+                mbar_arrive_expect_tx(bar, box_rows * 128);
+                load_box(dst + half * (128 * 128) + row * 128, map, half * 64, token, kv, hw, block, bar);
+            } else {
+                mbar_arrive(bar);
+            }
+            return;
+        }
+        const int64_t at = good ? group.block * v.block_stride + group.in_block * v.tok_stride : -1;
         const int c = lane % kChunks, sub = lane / kChunks;
         const char* from = head + kv * v.kv_stride + c * 16;
-        if (key0 >= lo && key0 + 128 <= hi && __all_sync(~0u, lane >= 16 || at >= 0)) {
+        if (whole) {
             const char* first = from + sub * v.tok_stride;
             const int64_t step = kStep * v.tok_stride;
 #pragma unroll
@@ -173,6 +205,7 @@ struct TileLoader {
                 }
             }
         }
+        arrive_when_loaded(bar);
     }
     // Starts the loads of `count` (at most 128) query rows of w's sequence and key head, from row `row` on; zeros behind.
     __device__ __forceinline__ void queries(const Rows& q, const Walk& w, int group, int row, int count, uint32_t dst) const {
