@@ -45,13 +45,16 @@ __global__ void __launch_bounds__(kAppendThreads) append_kv(const __grid_constan
     const int per_worker = p.q_heads + 2 * p.cache.heads, n = p.tp * per_worker;
     // The row's vectors do not depend on where the token goes: they are under way while that is looked up.
     uint4 raw[kBatch];
-    auto load = [&](int first) {
+    // (worker and head of a vector: counted on rather than divided out, the kernel is bound by its instructions)
+    auto onward = [&](int& r, int& h) {
+        h += kStride;
+        while (h >= per_worker) h -= per_worker, ++r;
+    };
+    auto load = [&](int first, int r, int h) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int vec = first + i * kStride;
+        for (int i = 0; i < kBatch; ++i, onward(r, h)) {
             raw[i] = make_uint4(0, 0, 0, 0);
-            if (vec < n) {
-                const int r = vec / per_worker, h = vec - r * per_worker;
+            if (first + i * kStride < n) {
                 const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.cache.heads;
                 const int head = is_q ? h : is_v ? h - p.q_heads - p.cache.heads : h - p.q_heads;
                 const Rows& from = is_q ? p.q : is_v ? p.v : p.k;
@@ -59,8 +62,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kv(const __grid_constan
             }
         }
     };
-    int first = threadIdx.x / kLanes;
-    load(first);
+    int first = threadIdx.x / kLanes, r = first / per_worker, h = first - r * per_worker;
+    load(first, r, h);
     const int s = find_sequence(p.batch, row, &s_seq);
     if (s < 0) return;
     const Seq seq = sequence(p.batch, s, p.cache.block_tokens);
@@ -83,78 +86,89 @@ __global__ void __launch_bounds__(kAppendThreads) append_kv(const __grid_constan
     const bool cached = block >= 0 && block < p.cache.num_blocks;
     if (!cached && threadIdx.x == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
     const int64_t slot = (int64_t)block * p.cache.block_stride + (index % p.cache.block_tokens) * p.cache.tok_stride;
-    for (;;) {
+    // The angles of this lane's elements, the sine's sign with them; lanes past the rotated part keep their elements.
+    float cs[8], sn[8];
+    const int hl = half / 8;  // lanes per half
+    const bool turns = p.inv_freq && lane * 8 < p.rot, second = lane >= hl;
+    const int partner = !turns ? lane : second ? lane - hl : lane + hl;
+    if (turns) {
+        const int k = p.interleaved ? lane * 4 : (second ? lane - hl : lane) * 8;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int vec = first + i * kStride;
+        for (int j = 0; j < 8; ++j) {
+            if (p.interleaved && j >= 4) break;
+            cs[j] = s_cos[k + j];
+            sn[j] = p.interleaved || second ? s_sin[k + j] : -s_sin[k + j];
+        }
+    }
+    const bool norms = p.q_norm || p.k_norm;
+    for (;;) {
+        int br = r, bh = h;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i, onward(br, bh)) {
             // whole warps go on together: the shuffles below need all their lanes
             if (first - threadIdx.x % 32 / kLanes + i * kStride >= n) break;
-            const bool there = vec < n;
-            const int r = there ? vec / per_worker : 0, h = there ? vec - r * per_worker : 0;
-            const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.cache.heads;
-            const int head = is_q ? h : is_v ? h - p.q_heads - p.cache.heads : h - p.q_heads;
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-            float x[8];
+            const bool there = first + i * kStride < n;
+            const bool is_q = bh < p.q_heads, is_v = bh >= p.q_heads + p.cache.heads;
+            const int head = is_q ? bh : is_v ? bh - p.q_heads - p.cache.heads : bh - p.q_heads;
+            uint4 out = raw[i];
+            if (__any_sync(~0u, there && !is_v)) {  // values go as they are
+                const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                float x[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 f = Elem<T>::unpack(w[j]);
-                x[2 * j] = f.x, x[2 * j + 1] = f.y;
-            }
-            const void* norm = is_q ? p.q_norm : p.k_norm;
-            if (p.q_norm || p.k_norm) {
-                float sum = 0.f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
-#pragma unroll
-                for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-                if (norm && !is_v) {
-                    const float inv = 1.f / sqrtf(sum * (1.f / D) + p.eps);
-                    const uint4 nw = reinterpret_cast<const uint4*>(norm)[lane];
-                    const uint32_t g[4] = {nw.x, nw.y, nw.z, nw.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 f = Elem<T>::unpack(g[j]);
-                        x[2 * j] *= inv * f.x, x[2 * j + 1] *= inv * f.y;
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    const float2 f = Elem<T>::unpack(w[j]);
+                    x[2 * j] = f.x, x[2 * j + 1] = f.y;
                 }
-            }
-            if (p.inv_freq) {  // block-uniform
-                if (p.interleaved) {
-                    if (lane * 8 < p.rot && !is_v) {
+                if (norms) {
+                    const void* norm = is_q ? p.q_norm : p.k_norm;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
+#pragma unroll
+                    for (int o = kLanes / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+                    if (norm) {
+                        const float inv = 1.f / sqrtf(sum * (1.f / D) + p.eps);
+                        const uint4 nw = reinterpret_cast<const uint4*>(norm)[lane];
+                        const uint32_t g[4] = {nw.x, nw.y, nw.z, nw.w};
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const float c = s_cos[lane * 4 + j], sn = s_sin[lane * 4 + j], a = x[2 * j], b = x[2 * j + 1];
-                            x[2 * j] = a * c - b * sn, x[2 * j + 1] = b * c + a * sn;
-                        }
-                    }
-                } else {
-                    const int hl = half / 8;  // lanes per half
-                    const bool second = lane >= hl;
-                    const int partner = lane >= 2 * hl ? lane : second ? lane - hl : lane + hl;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float other = __shfl_sync(~0u, x[j], partner, kLanes);
-                        if (lane < 2 * hl && !is_v) {
-                            const int k = (second ? lane - hl : lane) * 8 + j;
-                            x[j] = second ? x[j] * s_cos[k] + other * s_sin[k] : x[j] * s_cos[k] - other * s_sin[k];
+                            const float2 f = Elem<T>::unpack(g[j]);
+                            x[2 * j] *= inv * f.x, x[2 * j + 1] *= inv * f.y;
                         }
                     }
                 }
+                if (p.inv_freq) {  // block-uniform, as is the next
+                    if (p.interleaved) {
+                        if (turns) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float a = x[2 * j], b = x[2 * j + 1];
+                                x[2 * j] = a * cs[j] - b * sn[j], x[2 * j + 1] = b * cs[j] + a * sn[j];
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float other = __shfl_sync(~0u, x[j], partner, kLanes);
+                            if (turns) x[j] = x[j] * cs[j] + other * sn[j];
+                        }
+                    }
+                }
+                if (!is_v)
+                    out = make_uint4(Elem<T>::pack(x[0], x[1]), Elem<T>::pack(x[2], x[3]), Elem<T>::pack(x[4], x[5]),
+                                     Elem<T>::pack(x[6], x[7]));
             }
             if (!there) continue;
-            uint4 out = raw[i];  // values go as they are
-            if (!is_v)
-                out = make_uint4(Elem<T>::pack(x[0], x[1]), Elem<T>::pack(x[2], x[3]), Elem<T>::pack(x[4], x[5]),
-                                 Elem<T>::pack(x[6], x[7]));
             if (is_q)
-                *reinterpret_cast<uint4*>(p.q_out.base[r] + row * p.q_out.stride + head * (D * 2) + lane * 16) = out;
+                *reinterpret_cast<uint4*>(p.q_out.base[br] + row * p.q_out.stride + head * (D * 2) + lane * 16) = out;
             else if (cached)
-                *reinterpret_cast<uint4*>(p.cache.pools[r] + slot + head * p.cache.head_stride +
+                *reinterpret_cast<uint4*>(p.cache.pools[br] + slot + head * p.cache.head_stride +
                                           (is_v ? p.cache.kv_stride : 0) + lane * 16) = out;
         }
         first += kBatch * kStride;
         if (first - threadIdx.x % 32 / kLanes >= n) break;
-        load(first);
+        r = br, h = bh;
+        load(first, r, h);
     }
 }
 

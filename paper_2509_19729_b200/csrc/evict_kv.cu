@@ -27,10 +27,12 @@ __device__ __forceinline__ int checked_len(const EvictParams& p, int s, bool rep
     if (len < 0 || len > (int64_t)p.max_blocks * T) return reports && threadIdx.x == 0 ? (report(p.status, AMOEBA_ERR_INVALID_ARG), -1) : -1;
     const int keep = min(len, p.budget), n_src = (len + T - 1) / T, n_dst = (keep + T - 1) / T;
     if (n_dst > p.dst_max_blocks) return reports && threadIdx.x == 0 ? (report(p.status, AMOEBA_ERR_INVALID_ARG), -1) : -1;
+#pragma unroll 8
     for (int i = threadIdx.x; i < n_src; i += blockDim.x) {
         const int b = p.src_bt[(int64_t)s * p.max_blocks + i];
         if (b < 0 || b >= p.cache.num_blocks) code = 1;
     }
+#pragma unroll 8
     for (int i = threadIdx.x; i < n_dst; i += blockDim.x) {
         const int b = p.dst_bt[(int64_t)s * p.dst_max_blocks + i];
         if (b < 0 || b >= p.cache.num_blocks) code = 1;
@@ -148,15 +150,11 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
         const uint32_t above = round == 0 ? 0u : ~0u << (shift + bits);
         for (int i = tid; i < kDigits; i += kSelectThreads) sh.count[i] = 0;
         __syncthreads();
-        for (int i = tid; i - lane < n; i += kSelectThreads) {
-            const uint32_t k = i < n ? key_of(i) : 0;
-            const bool counts = i < n && (k & above) == limit;
-            const uint32_t those = __ballot_sync(~0u, counts);
-            if (counts) {  // equal digits of a warp are added once: scores of many tokens are the same
-                const uint32_t digit = k >> shift & ((1u << bits) - 1);
-                const uint32_t same = __match_any_sync(those, digit);
-                if (__ffs(same) - 1 == lane) atomicAdd(&sh.count[digit], __popc(same));
-            }
+        // (plain additions: gathering a warp's equal digits first takes longer than adding them one by one)
+#pragma unroll 4
+        for (int i = tid; i < n; i += kSelectThreads) {
+            const uint32_t k = key_of(i);
+            if ((k & above) == limit) atomicAdd(&sh.count[k >> shift & ((1u << bits) - 1)], 1);
         }
         __syncthreads();
         const int32_t* total = sh.count;
@@ -205,6 +203,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
     const int per = (n + kSelectThreads - 1) / kSelectThreads * 32;
     const int from = min(n, warp * per), to = min(n, from + per);
     int more = 0, equal = 0;
+#pragma unroll 4
     for (int i = from + lane; i - lane < to; i += 32) {
         const uint32_t k = i < to ? key_of(i) : 0;
         more += i < to && k > limit;
@@ -224,6 +223,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
     for (uint32_t r = 0; r < rank; ++r) more += load_remote(&sh.more, r), equal += load_remote(&sh.equal, r);
     for (int i = 0; i < warp; ++i) more += sh.before[i][0], equal += sh.before[i][1];
     const uint32_t lower = (1u << lane) - 1;
+#pragma unroll 4
     for (int i = from + lane; i - lane < to; i += 32) {
         const uint32_t k = i < to ? key_of(i) : 0;
         const uint32_t is_more = __ballot_sync(~0u, i < to && k > limit), is_equal = __ballot_sync(~0u, i < to && k == limit);
@@ -271,7 +271,7 @@ __device__ __forceinline__ RowPlace place(const EvictParams& p, const MoveUnit& 
 
 // Out of place: a CTA takes chunks of destination rows of one unit.
 template <int kVecs>  // 16-byte pieces of a key, or 0: any number
-__global__ void __launch_bounds__(kMoveThreads) evict_move(const __grid_constant__ EvictParams p, int chunks, int rows) {
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move(const __grid_constant__ EvictParams p, int chunks, int rows) {
     __shared__ int64_t s_from[kMoveRows], s_to[kMoveRows];
     const MoveUnit m = move_unit(p, blockIdx.x / chunks);
     const int begin = blockIdx.x % chunks * rows;
@@ -289,19 +289,17 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move(const __grid_constant
     constexpr int kUnroll = 8;
     for (int base = tid; base < all; base += kMoveThreads * kUnroll) {
         uint4 x[kUnroll];
-        int64_t to[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int i = base + u * kMoveThreads, row = i / (2 * vecs), c = i - row * 2 * vecs, kv = c >= vecs;
-            if (i < all) {
-                const int64_t off = kv * p.cache.kv_stride + (c - kv * vecs) * 16;
-                to[u] = s_to[row] + off;
-                x[u] = ld_stream(reinterpret_cast<const uint4*>(m.pool + s_from[row] + off));
-            }
+            if (i < all)
+                x[u] = ld_stream(reinterpret_cast<const uint4*>(m.pool + s_from[row] + kv * p.cache.kv_stride + (c - kv * vecs) * 16));
         }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-            if (base + u * kMoveThreads < all) st_stream(reinterpret_cast<uint4*>(m.pool + to[u]), x[u]);
+        for (int u = 0; u < kUnroll; ++u) {
+            const int i = base + u * kMoveThreads, row = i / (2 * vecs), c = i - row * 2 * vecs, kv = c >= vecs;
+            if (i < all) st_stream(reinterpret_cast<uint4*>(m.pool + s_to[row] + kv * p.cache.kv_stride + (c - kv * vecs) * 16), x[u]);
+        }
     }
 }
 

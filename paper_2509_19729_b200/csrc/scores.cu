@@ -306,6 +306,48 @@ __device__ bool score_multiply(const ScoreParams& p, uint32_t smem, ScoreBarrier
     return true;
 }
 
+// Sum over the 128 rows of 2^(c * logit + row) for one token; kCut: of those rows that see it.  `empty` gets this thread's
+// arrival when the logits are read.
+template <bool kCut>
+__device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[128], const int32_t (&pos)[128], int key, int window, float c,
+                                            uint64_t* empty) {
+    const uint64_t c2 = pair2(c, c);
+    uint64_t sum[2] = {0, 0};
+    uint32_t s[2][32];
+    tmem_load32(s[0], from);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        tmem_load_wait();
+        if (i < 3) {
+            tmem_load32(s[(i + 1) % 2], from + (i + 1) * 32);
+        } else {
+            tmem_fence_before();
+            mbar_arrive(empty);
+        }
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+            const float4 r = *reinterpret_cast<const float4*>(&row[i * 32 + k]);
+            float x[4];
+            split2(fma2(pair2(__uint_as_float(s[i % 2][k]), __uint_as_float(s[i % 2][k + 1])), c2, pair2(r.x, r.y)), x[0], x[1]);
+            split2(fma2(pair2(__uint_as_float(s[i % 2][k + 2]), __uint_as_float(s[i % 2][k + 3])), c2, pair2(r.z, r.w)), x[2], x[3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = fast_exp2(x[e]);
+            if (kCut) {
+                const int4 at = *reinterpret_cast<const int4*>(&pos[i * 32 + k]);
+                const int seen[4] = {at.x, at.y, at.z, at.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (key > seen[e] || (window > 0 && key <= seen[e] - window)) x[e] = 0.f;
+            }
+            sum[0] = add2(sum[0], pair2(x[0], x[1]));
+            sum[1] = add2(sum[1], pair2(x[2], x[3]));
+        }
+    }
+    float lo, hi;
+    split2(add2(sum[0], sum[1]), lo, hi);
+    return lo + hi;
+}
+
 // s_row: [2][128] of this warpgroup, -lse * log2(e) of the pass's rows; s_pos: their cache indices.
 __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, float (*s_row)[128], int32_t (*s_pos)[128]) {
     const int g = threadIdx.x / 128, tid = threadIdx.x % 128, G = p.shape.group, T = p.cache.block_tokens;
@@ -357,41 +399,9 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
                 if (!wait(&b.s_full[buf], done >> 1 & 1)) return false;
                 tmem_fence_after();
                 const uint32_t from = b.tmem + lanes + buf * 128;
-                uint32_t s[2][32];
-                uint64_t sum[2] = {0, 0};
-                const uint64_t c2 = pair2(c, c);
-                tmem_load32(s[0], from);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    tmem_load_wait();
-                    if (i < 3) {
-                        tmem_load32(s[(i + 1) % 2], from + (i + 1) * 32);
-                    } else {
-                        tmem_fence_before();
-                        mbar_arrive(&b.s_empty[buf]);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 32; k += 4) {
-                        const float4 r = *reinterpret_cast<const float4*>(&s_row[pass][i * 32 + k]);
-                        float x[4];
-                        split2(fma2(pair2(__uint_as_float(s[i % 2][k]), __uint_as_float(s[i % 2][k + 1])), c2, pair2(r.x, r.y)), x[0], x[1]);
-                        split2(fma2(pair2(__uint_as_float(s[i % 2][k + 2]), __uint_as_float(s[i % 2][k + 3])), c2, pair2(r.z, r.w)), x[2], x[3]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] = fast_exp2(x[e]);
-                        if (cut) {
-                            const int4 at = *reinterpret_cast<const int4*>(&s_pos[pass][i * 32 + k]);
-                            const int seen[4] = {at.x, at.y, at.z, at.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (key > seen[e] || (p.window > 0 && key <= seen[e] - p.window)) x[e] = 0.f;
-                        }
-                        sum[0] = add2(sum[0], pair2(x[0], x[1]));
-                        sum[1] = add2(sum[1], pair2(x[2], x[3]));
-                    }
-                }
-                float lo, hi;
-                split2(add2(sum[0], sum[1]), lo, hi);
-                if (to) *to = old + (lo + hi);
+                const float sum = cut ? column_sum<true>(from, s_row[pass], s_pos[pass], key, p.window, c, &b.s_empty[buf])
+                                      : column_sum<false>(from, s_row[pass], s_pos[pass], key, p.window, c, &b.s_empty[buf]);
+                if (to) *to = old + sum;
             }
         }
     }
