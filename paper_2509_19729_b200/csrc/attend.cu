@@ -232,11 +232,13 @@ attend_few(const __grid_constant__ AttendParams p) {
 // Joins the parts of the units that were cut.  kWarps warps to a row: with few rows a unit may be in as many parts as there
 // are CTAs, so its eight warps take every eighth part each; with many rows it is in two or three, and a warp does a row.
 constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
+template <int kWarps>
+constexpr int kJoinRows = kWarps == 1 ? 4 * kJoinWarps : 1;  // of a block: four to a warp, or one to all
 template <class T, int D, int kWarps>
-__device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int block) {
+__device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int block, int rows_most) {
     const Shape& sh = p.shape;
-    constexpr int kRows = kJoinWarps / kWarps;  // per CTA
-    const int groups = sh.rows / kRows;  // blocks for every share: its first unit is joined here if it began in the share before
+    constexpr int kRows = kJoinRows<kWarps>;
+    const int groups = (rows_most + kRows - 1) / kRows;  // blocks for every share: its first unit is joined here if it began in the share before
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int mine = block / groups;
     const Cut cut = p.cuts[mine];
@@ -257,11 +259,14 @@ __device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int b
         if (!more) c1 += __popc(in) - 32;
     }
     constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes to a part's row, parts at once
-    const int r = first_row + (kWarps == 1 ? warp : 0), stripe = (kWarps == 1 ? 0 : warp) * kAtOnce + lane / kLanes;
+    const int stripe = (kWarps == 1 ? 0 : warp) * kAtOnce + lane / kLanes;
+#pragma unroll
+    for (int i = 0; i < (kWarps == 1 ? 4 : 1); ++i) {
+    const int r = first_row + (kWarps == 1 ? i * kJoinWarps + warp : 0);
     float top = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < rows) {
-#pragma unroll 8
+#pragma unroll (kWarps == 1 ? 2 : 8)
         for (int c = c0 + stripe; c < c1; c += kWarps * kAtOnce) {
             if (p.cuts[c].begin == p.cuts[c].end) continue;  // an empty share
             const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
@@ -295,20 +300,21 @@ __device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int b
         if (warp) return;
         for (int w = 1; w < kWarps; ++w) merge(s_top[w], s_l[w], s_acc[w][lane % kLanes]);
     }
-    if (r >= rows || lane >= kLanes) return;
+    if (r >= rows || lane >= kLanes) continue;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int row = m * R + r;
     *reinterpret_cast<uint2*>(row_of<D>(p.out, p, q, h, row) + lane * 8) =
         make_uint2(Elem<T>::pack(acc.x * inv, acc.y * inv), Elem<T>::pack(acc.z * inv, acc.w * inv));
     if (lane == 0 && p.lse) *lse_of(p, q, h, row) = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+    }
 }
 // Blocks [0, few_blocks) join what attend_few has cut, the others what attend_many has.
 template <class T, int D>
-__global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constant__ AttendParams few, int few_ctas, int few_blocks,
-                                                   const __grid_constant__ AttendParams many, int many_ctas) {
+__global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constant__ AttendParams few, int few_ctas, int few_rows, int few_blocks,
+                                                            const __grid_constant__ AttendParams many, int many_ctas) {
     grid_dependency_wait();
-    if ((int)blockIdx.x < few_blocks) join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x);
-    else join_rows<T, D, 1>(many, many_ctas, blockIdx.x - few_blocks);
+    if ((int)blockIdx.x < few_blocks) join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x, few_rows);
+    else join_rows<T, D, 1>(many, many_ctas, blockIdx.x - few_blocks, kManyRows);
 }
 
 // The workspace holds the parts of cut units, two for each CTA; these bound the grids without asking the device.
@@ -366,7 +372,7 @@ static amoeba_status run_attend(AttendParams& p, int tp, int32_t dtype, char* ws
                        : most == 16 ? run_few<T, D, 2>(p, sms, &few_ctas, stream)
                                     : run_few<T, D, 4>(p, sms, &few_ctas, stream);
     if (st != AMOEBA_OK || (p.whole && rows <= kMaxFewRows)) return st;
-    const int few_blocks = p.whole ? 0 : few_ctas * p.shape.rows;
+    const int few_most = (int)std::min<int64_t>(rows, most), few_blocks = p.whole ? 0 : few_ctas * few_most;
     AttendParams many = p;
     int many_ctas = 0, many_blocks = 0;
     if (rows > kMaxFewRows) {
@@ -376,10 +382,10 @@ static amoeba_status run_attend(AttendParams& p, int tp, int32_t dtype, char* ws
         many.shape.rows = kManyRows;
         many.shape.tile = kManyTile;
         many_ctas = std::min(sms, kMaxSms);
-        many_blocks = many_ctas * (kManyRows / kJoinWarps);
+        many_blocks = many_ctas * (kManyRows / kJoinRows<1>);
         if ((st = launch_attend_many(many, tp, dtype, D, many_ctas, stream)) != AMOEBA_OK) return st;
     }
-    return launch_kernel(attend_join<T, D>, few_blocks + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_blocks, many, many_ctas);
+    return launch_kernel(attend_join<T, D>, few_blocks + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_most, few_blocks, many, many_ctas);
 }
 
 }  // namespace amoeba

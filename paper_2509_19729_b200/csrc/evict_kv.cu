@@ -20,51 +20,7 @@ struct EvictParams {
     int32_t vec;            // bytes of one token's key
 };
 
-// The sequence's length, or -1 if it is refused; the whole block asks together.
-__device__ __forceinline__ int checked_len(const EvictParams& p, int s, bool reports) {
-    const int len = p.seq_lens[s], T = p.cache.block_tokens;
-    int code = 0;
-    if (len < 0 || len > (int64_t)p.max_blocks * T) return reports && threadIdx.x == 0 ? (report(p.status, AMOEBA_ERR_INVALID_ARG), -1) : -1;
-    const int keep = min(len, p.budget), n_src = (len + T - 1) / T, n_dst = (keep + T - 1) / T;
-    if (n_dst > p.dst_max_blocks) return reports && threadIdx.x == 0 ? (report(p.status, AMOEBA_ERR_INVALID_ARG), -1) : -1;
-#pragma unroll 8
-    for (int i = threadIdx.x; i < n_src; i += blockDim.x) {
-        const int b = p.src_bt[(int64_t)s * p.max_blocks + i];
-        if (b < 0 || b >= p.cache.num_blocks) code = 1;
-    }
-#pragma unroll 8
-    for (int i = threadIdx.x; i < n_dst; i += blockDim.x) {
-        const int b = p.dst_bt[(int64_t)s * p.dst_max_blocks + i];
-        if (b < 0 || b >= p.cache.num_blocks) code = 1;
-    }
-    if (!__syncthreads_or(code)) return len;
-    if (reports && threadIdx.x == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
-    return -1;
-}
-
-// Scores as whole numbers of the same order: a NaN is 0, below -infinity; -0 is 0.
-__device__ __forceinline__ uint32_t order_of(float x) {
-    if (x != x) return 0;
-    const uint32_t u = __float_as_uint(x + 0.f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
-// ------------------------------------------------------------------------------------------------ which tokens stay
-// A cluster of CTAs for each (layer, sequence, key head): each takes a run of the tokens, its scores as ordered whole numbers
-// in shared memory.  The smallest score that stays is found from the top, 11, 11 and 10 bits at a time, from counts of the
-// digits that all CTAs of the cluster add up; then every warp lists the kept ones of its own run of tokens in order.
-constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
-constexpr int kSelectKeys = 12288, kMaxCluster = 8;  // keys that a CTA holds, unless eight CTAs need to hold more
-constexpr int kDigits = 2048;
-
-struct SelectShared {
-    alignas(16) int32_t count[kDigits];  // of this CTA's tokens, by digit
-    alignas(16) int32_t total[kDigits];  // of the cluster's
-    int32_t warp[kSelectWarps];
-    int32_t more, equal;      // this CTA's tokens above the limit, and at it
-    int32_t found[2];         // digit, and how many at it stay
-    int32_t before[kSelectWarps][2];
-};
+constexpr int kMaxCluster = 8;
 
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -94,6 +50,60 @@ __device__ __forceinline__ void store_remote(int32_t* p, uint32_t rank, int32_t 
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(remote), "r"(v) : "memory");
 }
 
+// The sequence's length, or -1 if it is refused.  The whole cluster asks together, each CTA looking at its part of the tables;
+// bad: [kMaxCluster] in shared memory.
+__device__ __forceinline__ int checked_len(const EvictParams& p, int s, bool reports, uint32_t rank, uint32_t size, int32_t* bad) {
+    const int len = p.seq_lens[s], T = p.cache.block_tokens;
+    int code = 0;
+    if (len < 0 || len > (int64_t)p.max_blocks * T) return reports && threadIdx.x == 0 ? (report(p.status, AMOEBA_ERR_INVALID_ARG), -1) : -1;
+    const int keep = min(len, p.budget), n_src = (len + T - 1) / T, n_dst = (keep + T - 1) / T;
+    if (n_dst > p.dst_max_blocks) return reports && threadIdx.x == 0 ? (report(p.status, AMOEBA_ERR_INVALID_ARG), -1) : -1;
+#pragma unroll 4
+    for (int i = rank * blockDim.x + threadIdx.x; i < n_src; i += blockDim.x * size) {
+        const int b = p.src_bt[(int64_t)s * p.max_blocks + i];
+        if (b < 0 || b >= p.cache.num_blocks) code = 1;
+    }
+#pragma unroll 4
+    for (int i = rank * blockDim.x + threadIdx.x; i < n_dst; i += blockDim.x * size) {
+        const int b = p.dst_bt[(int64_t)s * p.dst_max_blocks + i];
+        if (b < 0 || b >= p.cache.num_blocks) code = 1;
+    }
+    code = __syncthreads_or(code);
+    if (size > 1) {
+        if (threadIdx.x < size) store_remote(&bad[rank], threadIdx.x, code);
+        cluster_sync();
+        for (uint32_t r = 0; r < size; ++r) code |= bad[r];
+    }
+    if (!code) return len;
+    if (reports && threadIdx.x == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
+    return -1;
+}
+
+// Scores as whole numbers of the same order: a NaN is 0, below -infinity; -0 is 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    if (x != x) return 0;
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// ------------------------------------------------------------------------------------------------ which tokens stay
+// A cluster of CTAs for each (layer, sequence, key head): each takes a run of the tokens, its scores as ordered whole numbers
+// in shared memory.  The smallest score that stays is found from the top, 11, 11 and 10 bits at a time, from counts of the
+// digits that all CTAs of the cluster add up; then every warp lists the kept ones of its own run of tokens in order.
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectKeys = 12288;  // keys that a CTA holds, unless eight CTAs need to hold more
+constexpr int kDigits = 2048;
+
+struct SelectShared {
+    alignas(16) int32_t count[kDigits];  // of this CTA's tokens, by digit
+    alignas(16) int32_t total[kDigits];  // of the cluster's
+    int32_t warp[kSelectWarps];
+    int32_t more, equal;      // this CTA's tokens above the limit, and at it
+    int32_t found[2];         // digit, and how many at it stay
+    int32_t before[kSelectWarps][2];
+    int32_t bad[kMaxCluster];
+};
+
 __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_constant__ EvictParams p, int room) {
     extern __shared__ __align__(16) uint32_t s_keys[];
     __shared__ SelectShared sh;
@@ -102,7 +112,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
     const int unit = blockIdx.x / size;
     const int h = unit % p.kv_heads, s = unit / p.kv_heads % p.num_seqs, l = unit / p.kv_heads / p.num_seqs;
     const bool first = l == 0 && h == 0 && rank == 0;
-    const int len = checked_len(p, s, first);
+    const int len = checked_len(p, s, first, rank, size, sh.bad);
     if (first && tid == 0) p.new_lens[s] = min(len, p.budget);
     if (len <= p.budget) return;  // the whole cluster
     const int free = len - p.recent, need = p.budget - p.recent;
@@ -151,10 +161,21 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
         for (int i = tid; i < kDigits; i += kSelectThreads) sh.count[i] = 0;
         __syncthreads();
         // (plain additions: gathering a warp's equal digits first takes longer than adding them one by one)
-#pragma unroll 4
-        for (int i = tid; i < n; i += kSelectThreads) {
-            const uint32_t k = key_of(i);
-            if ((k & above) == limit) atomicAdd(&sh.count[k >> shift & ((1u << bits) - 1)], 1);
+        const uint32_t ones = (1u << bits) - 1;
+        if (held) {
+#pragma unroll 2
+            for (int i = tid * 4; i < n; i += kSelectThreads * 4) {
+                const uint4 k = *reinterpret_cast<const uint4*>(s_keys + i);
+                if ((k.x & above) == limit) atomicAdd(&sh.count[k.x >> shift & ones], 1);
+                if ((k.y & above) == limit && i + 1 < n) atomicAdd(&sh.count[k.y >> shift & ones], 1);
+                if ((k.z & above) == limit && i + 2 < n) atomicAdd(&sh.count[k.z >> shift & ones], 1);
+                if ((k.w & above) == limit && i + 3 < n) atomicAdd(&sh.count[k.w >> shift & ones], 1);
+            }
+        } else {
+            for (int i = tid; i < n; i += kSelectThreads) {
+                const uint32_t k = order_of(scores[score_at(begin + i)]);
+                if ((k & above) == limit) atomicAdd(&sh.count[k >> shift & ones], 1);
+            }
         }
         __syncthreads();
         const int32_t* total = sh.count;
@@ -199,15 +220,29 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
         left = sh.found[1];
     }
 
-    // Every warp's run of tokens, counted, and then listed behind those of the warps and CTAs before.
-    const int per = (n + kSelectThreads - 1) / kSelectThreads * 32;
+    // Every warp's run of tokens, counted, and then listed behind those of the warps and CTAs before; four tokens a lane.
+    const int per = (n + kSelectThreads * 4 - 1) / (kSelectThreads * 4) * 128;
     const int from = min(n, warp * per), to = min(n, from + per);
+    auto four = [&](int i, uint32_t (&k)[4]) {  // keys from i on; behind the end 0, which is below any limit but a NaN's
+        if (held && i + 3 < to) {
+            const uint4 x = *reinterpret_cast<const uint4*>(s_keys + i);
+            k[0] = x.x, k[1] = x.y, k[2] = x.z, k[3] = x.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = i + j < to ? key_of(i + j) : 0;
+        }
+    };
     int more = 0, equal = 0;
-#pragma unroll 4
-    for (int i = from + lane; i - lane < to; i += 32) {
-        const uint32_t k = i < to ? key_of(i) : 0;
-        more += i < to && k > limit;
-        equal += i < to && k == limit;
+#pragma unroll 2
+    for (int base = from; base < to; base += 128) {
+        const int i = base + lane * 4;
+        uint32_t k[4];
+        four(i, k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            more += k[j] > limit;
+            equal += k[j] == limit && i + j < to;
+        }
     }
     more = __reduce_add_sync(~0u, more), equal = __reduce_add_sync(~0u, equal);
     if (lane == 0) sh.before[warp][0] = more, sh.before[warp][1] = equal;
@@ -222,15 +257,28 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
     more = equal = 0;
     for (uint32_t r = 0; r < rank; ++r) more += load_remote(&sh.more, r), equal += load_remote(&sh.equal, r);
     for (int i = 0; i < warp; ++i) more += sh.before[i][0], equal += sh.before[i][1];
-    const uint32_t lower = (1u << lane) - 1;
-#pragma unroll 4
-    for (int i = from + lane; i - lane < to; i += 32) {
-        const uint32_t k = i < to ? key_of(i) : 0;
-        const uint32_t is_more = __ballot_sync(~0u, i < to && k > limit), is_equal = __ballot_sync(~0u, i < to && k == limit);
-        const int rank_equal = equal + __popc(is_equal & lower);
-        const bool stays = (is_more >> lane & 1u) || ((is_equal >> lane & 1u) && rank_equal < left);
-        if (stays) kept[more + __popc(is_more & lower) + min(rank_equal, left)] = begin + i;
-        more += __popc(is_more), equal += __popc(is_equal);
+    for (int base = from; base < to; base += 128) {
+        const int i = base + lane * 4;
+        uint32_t k[4];
+        four(i, k);
+        int mine = 0;  // above the limit in the low half, at it in the high one
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mine += (k[j] > limit) + (k[j] == limit && i + j < to ? 0x10000 : 0);
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int up = __shfl_up_sync(~0u, incl, o);
+            if (lane >= o) incl += up;
+        }
+        int m = more + ((incl - mine) & 0xffff), e = equal + ((incl - mine) >> 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool is_more = k[j] > limit, is_equal = k[j] == limit && i + j < to;
+            if (is_more || (is_equal && e < left)) kept[m + min(e, left)] = begin + i + j;
+            m += is_more, e += is_equal;
+        }
+        const int all = __shfl_sync(~0u, incl, 31);
+        more += all & 0xffff, equal += all >> 16;
     }
     if (size > 1) cluster_sync();  // no CTA ends while another reads its counts
 }
