@@ -90,24 +90,26 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 // A cluster of CTAs for each (layer, sequence, key head): each takes a run of the tokens, its scores as ordered whole numbers
 // in shared memory.  The smallest score that stays is found from the top, 11, 11 and 10 bits at a time, from counts of the
 // digits that all CTAs of the cluster add up; then every warp lists the kept ones of its own run of tokens in order.
-constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
 constexpr int kSelectKeys = 12288;  // keys that a CTA holds, unless eight CTAs need to hold more
-constexpr int kDigits = 2048;
+constexpr int kDigits = 2048, kDigitThreads = kDigits / 4;
 
 struct SelectShared {
     alignas(16) int32_t count[kDigits];  // of this CTA's tokens, by digit
     alignas(16) int32_t total[kDigits];  // of the cluster's
-    int32_t warp[kSelectWarps];
+    int32_t warp[kDigitThreads / 32];
     int32_t more, equal;      // this CTA's tokens above the limit, and at it
     int32_t found[2];         // digit, and how many at it stay
-    int32_t before[kSelectWarps][2];
+    int32_t before[32][2];
     int32_t bad[kMaxCluster];
 };
 
+template <int kSelectThreads>
 __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_constant__ EvictParams p, int room) {
+    constexpr int kSelectWarps = kSelectThreads / 32;
     extern __shared__ __align__(16) uint32_t s_keys[];
     __shared__ SelectShared sh;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    grid_dependency_launch();
     const uint32_t rank = cluster_rank(), size = cluster_size();
     const int unit = blockIdx.x / size;
     const int h = unit % p.kv_heads, s = unit / p.kv_heads % p.num_seqs, l = unit / p.kv_heads / p.num_seqs;
@@ -193,26 +195,30 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
             cluster_sync();
             total = sh.total;
         }
-        // from the largest digit down: thread t has digits 2047 - 4t ... 2044 - 4t
-        const int4 four = *reinterpret_cast<const int4*>(&total[kDigits - 4 - tid * 4]);
-        const int mine[4] = {four.w, four.z, four.y, four.x};
-        int sum = mine[0] + mine[1] + mine[2] + mine[3];
-        int before = sum;
+        // from the largest digit down: thread t < 512 has digits 2047 - 4t ... 2044 - 4t
+        int mine[4] = {0, 0, 0, 0}, before = 0, sum = 0;
+        if (tid < kDigitThreads) {
+            const int4 four = *reinterpret_cast<const int4*>(&total[kDigits - 4 - tid * 4]);
+            mine[0] = four.w, mine[1] = four.z, mine[2] = four.y, mine[3] = four.x;
+            before = sum = mine[0] + mine[1] + mine[2] + mine[3];
 #pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int up = __shfl_up_sync(~0u, before, o);
-            if (lane >= o) before += up;
+            for (int o = 1; o < 32; o *= 2) {
+                const int up = __shfl_up_sync(~0u, before, o);
+                if (lane >= o) before += up;
+            }
+            if (lane == 31) sh.warp[warp] = before;
         }
-        if (lane == 31) sh.warp[warp] = before;
         __syncthreads();
-        before -= sum;
-        for (int i = 0; i < warp; ++i) before += sh.warp[i];
-        if (before < left && left <= before + sum) {
+        if (tid < kDigitThreads) {
+            before -= sum;
+            for (int i = 0; i < warp; ++i) before += sh.warp[i];
+            if (before < left && left <= before + sum) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (before < left && left <= before + mine[j])
-                    sh.found[0] = kDigits - 1 - tid * 4 - j, sh.found[1] = left - before;
-                before += mine[j];
+                for (int j = 0; j < 4; ++j) {
+                    if (before < left && left <= before + mine[j])
+                        sh.found[0] = kDigits - 1 - tid * 4 - j, sh.found[1] = left - before;
+                    before += mine[j];
+                }
             }
         }
         __syncthreads();
@@ -321,6 +327,7 @@ __device__ __forceinline__ RowPlace place(const EvictParams& p, const MoveUnit& 
 template <int kVecs>  // 16-byte pieces of a key, or 0: any number
 __global__ void __launch_bounds__(kMoveThreads, 4) evict_move(const __grid_constant__ EvictParams p, int chunks, int rows) {
     __shared__ int64_t s_from[kMoveRows], s_to[kMoveRows];
+    grid_dependency_wait();
     const MoveUnit m = move_unit(p, blockIdx.x / chunks);
     const int begin = blockIdx.x % chunks * rows;
     if (begin >= m.n) return;
@@ -359,6 +366,7 @@ template <int kVecs>
 __global__ void __launch_bounds__(kCloseThreads) evict_close_up(const __grid_constant__ EvictParams p, int rows) {
     extern __shared__ __align__(16) char smem[];  // [rows] from, [rows] to, and the scores
     int64_t *s_from = reinterpret_cast<int64_t*>(smem), *s_to = s_from + rows;
+    grid_dependency_wait();
     const uint32_t rank = cluster_rank(), size = cluster_size();
     const MoveUnit m = move_unit(p, blockIdx.x / size);
     if (m.n < 0 || !m.cut) return;  // the whole cluster
@@ -394,20 +402,27 @@ __global__ void __launch_bounds__(kCloseThreads) evict_close_up(const __grid_con
 }
 
 template <class... P, class... A>
-static amoeba_status launch_clusters(void (*kernel)(P...), int64_t grid, int threads, size_t smem, int cluster, cudaStream_t stream,
-                                     const A&... args) {
+static amoeba_status launch_clusters(void (*kernel)(P...), int64_t grid, int threads, size_t smem, int cluster, bool early,
+                                     cudaStream_t stream, const A&... args) {
     if (smem > 16 * 1024 && ensure_dynamic_smem((const void*)kernel, (int)smem) != cudaSuccess) return AMOEBA_ERR_CUDA;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)grid);
     c.blockDim = dim3((unsigned)threads);
     c.dynamicSmemBytes = smem;
     c.stream = stream;
-    cudaLaunchAttribute a{};
-    a.id = cudaLaunchAttributeClusterDimension;
-    a.val.clusterDim.x = (unsigned)cluster;
-    a.val.clusterDim.y = a.val.clusterDim.z = 1;
-    c.attrs = &a;
-    c.numAttrs = cluster > 1 ? 1 : 0;
+    cudaLaunchAttribute a[2] = {};
+    if (cluster > 1) {
+        a[c.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        a[c.numAttrs].val.clusterDim.x = (unsigned)cluster;
+        a[c.numAttrs].val.clusterDim.y = a[c.numAttrs].val.clusterDim.z = 1;
+        ++c.numAttrs;
+    }
+    if (early) {
+        a[c.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        a[c.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++c.numAttrs;
+    }
+    c.attrs = a;
     if (cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...) != cudaSuccess) {
         (void)cudaGetLastError();
         return AMOEBA_ERR_CUDA;
@@ -482,20 +497,21 @@ extern "C" amoeba_status amoeba_evict_kv(const amoeba_layout* layout, int32_t la
     while (cluster < kMaxCluster && tokens > (int64_t)cluster * kSelectKeys) cluster *= 2;
     const int64_t slice = (tokens + cluster * 32 - 1) / (cluster * 32) * 32;
     const int room = (int)std::min<int64_t>(slice, (dev.smem_optin - (int)sizeof(SelectShared) - 1024) / 4 / 32 * 32);
-    if ((st = launch_clusters(evict_select, units * cluster, kSelectThreads, (size_t)room * 4, cluster, stream, p, room)) != AMOEBA_OK ||
-        tokens == 0)
-        return st;
+    // (few and long units: as many threads as a CTA may have)
+    st = cluster == kMaxCluster ? launch_clusters(evict_select<1024>, units * cluster, 1024, (size_t)room * 4, cluster, false, stream, p, room)
+                                : launch_clusters(evict_select<512>, units * cluster, 512, (size_t)room * 4, cluster, false, stream, p, room);
+    if (st != AMOEBA_OK || tokens == 0) return st;
     if (p.in_place) {
         // One CTA moves about 100 GB/s; with few units, several CTAs to each.
         int group = 1;
         while (group < kMaxCluster && units * group * 2 <= 2 * dev.sms && (int64_t)group * rows < most) group *= 2;
         auto* kernel = p.vec == 256 ? evict_close_up<16> : p.vec == 128 ? evict_close_up<8> : evict_close_up<0>;
-        return launch_clusters(kernel, units * group, kCloseThreads, (size_t)rows * 16, group, stream, p, rows);
+        return launch_clusters(kernel, units * group, kCloseThreads, (size_t)rows * 16, group, true, stream, p, rows);
     }
     auto* kernel = p.vec == 256 ? evict_move<16> : p.vec == 128 ? evict_move<8> : evict_move<0>;
     // Out of place: long chunks, in which looking up the rows counts for little, if that leaves four CTAs to an SM.
     int chunk = kMoveRows;
     while (chunk > 32 && units * ((most + chunk - 1) / chunk) < 4 * dev.sms) chunk /= 2;
     const int64_t chunks = std::max<int64_t>((most + chunk - 1) / chunk, 1);
-    return launch_clusters(kernel, units * chunks, kMoveThreads, 0, 1, stream, p, (int)chunks, chunk);
+    return launch_clusters(kernel, units * chunks, kMoveThreads, 0, 1, true, stream, p, (int)chunks, chunk);
 }
