@@ -49,7 +49,7 @@ attend_few(const __grid_constant__ AttendParams p) {
     } else {
         int64_t begin, end;
         take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
-        write_cut(p.cuts, walk, begin, end);
+        write_cut(sh, p.cuts, walk, begin, end);
         n = end - begin;
     }
     grid_dependency_launch();
@@ -240,18 +240,15 @@ __device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int b
     constexpr int kRows = kJoinRows<kWarps>;
     const int groups = (rows_most + kRows - 1) / kRows;  // blocks for every share: its first unit is joined here if it began in the share before
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int mine = block / groups;
+    const int mine = block / groups, first_row = block % groups * kRows;
     const Cut cut = p.cuts[mine];
-    if (cut.begin == cut.end || cut.t == 0) return;
+    if (cut.begin == cut.end || cut.t == 0 || first_row >= cut.rows) return;
     const int64_t first = cut.begin - cut.t, last = first + cut.tiles;
+    const int m = cut.m, h = cut.h, R = sh.rows, rows = cut.rows;
+    const Seq q = sequence(p.batch, cut.s, p.cache.block_tokens);
     int c0 = mine - 1;
     while (p.cuts[c0].begin == p.cuts[c0].end) --c0;
     if (p.cuts[c0].begin > first) return;
-    const int m = cut.m, h = cut.h, R = sh.rows;
-    const Seq q = sequence(p.batch, cut.s, p.cache.block_tokens);
-    const int rows = min(R, q.qn * sh.group - m * R);
-    const int first_row = block % groups * kRows;
-    if (first_row >= rows) return;
     int c1 = mine;  // behind the last part
     for (bool more = true; more; c1 += 32) {
         const unsigned in = __ballot_sync(~0u, c1 + lane < ctas && p.cuts[c1 + lane].begin < last);

@@ -70,7 +70,7 @@ __device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
                 sh.begin_off = off;
             }
         }
-        write_cut(p.cuts, w, begin, end);
+        write_cut(shape, p.cuts, w, begin, end);
         __syncthreads();
         return end > begin;
     }
@@ -173,7 +173,7 @@ __device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
             w.open(shape, b, T, sh.begin_seq);
             w.seek(shape, sh.begin_off);
         }
-        write_cut(p.cuts, w, at, sh.end);
+        write_cut(shape, p.cuts, w, at, sh.end);
     }
     return rounds > 0 || sh.end > at;
 }
@@ -358,25 +358,25 @@ __device__ __forceinline__ void drain_products(ManyBarriers& b) {
 }
 
 // ---- softmax: a thread per row
-// Bit i of `see`: the row sees token key0 + i.  table: null, or the unit has bad blocks.
-__device__ __noinline__ void visible(uint32_t (&see)[4], int key0, int lo, int hi, const Range& range, const int32_t* table,
-                                     const CacheView& v) {
+// Bit i of `see`: the row sees token key0 + i, of those in [lo, hi).
+__device__ __forceinline__ void visible(uint32_t (&see)[4], int key0, int lo, int hi) {
+#pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int first = key0 + j * 32, a = min(max(lo - first, 0), 32), b = min(max(hi - first, 0), 32);
-        uint32_t m = b > a ? (~0u >> (32 - (b - a))) << a : 0u;
-        for (int k = 0; table && k < 32; ++k)
-            if (m >> k & 1u) {
-                const int key = first + k;
-                const int block = key < range.hi ? table[key / v.block_tokens] : -1;
-                if (block < 0 || block >= v.num_blocks) m &= ~(1u << k);
-            }
-        see[j] = m;
+        const int a = min(max(lo - key0 - j * 32, 0), 32), b = min(max(hi - key0 - j * 32, a), 32);
+        see[j] = (uint32_t)((1ull << b) - (1ull << a));
+    }
+}
+// Takes out the tokens of bad blocks.
+__device__ __noinline__ void take_out_bad(uint32_t (&see)[4], int key0, int hi, const int32_t* table, const CacheView& v) {
+    for (int i = 0; i < 128 && key0 + i < hi; ++i) {
+        const int block = table[(key0 + i) / v.block_tokens];
+        if (block < 0 || block >= v.num_blocks) see[i / 32] &= ~(1u << i % 32);
     }
 }
 __device__ __forceinline__ void hide(uint32_t (&s)[32], uint32_t see) {
 #pragma unroll
     for (int k = 0; k < 32; ++k)
-        if (!(see >> k & 1u)) s[k] = 0xff800000u;  // -infinity
+        if (!(see & 1u << k)) s[k] = 0xff800000u;  // -infinity
 }
 // The largest of the row's logits that it sees.  The row is read once more for the weights: kept, it would fill 128 registers.
 template <bool kCut>
@@ -464,7 +464,14 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
                 tmem_fence_after();
                 uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
                 const bool cut = __any_sync(~0u, key0 + kManyTile > see_hi || key0 < see_lo) || bad;
-                if (cut) visible(see, key0, see_lo, see_hi, w.range, bad ? table : nullptr, p.cache);
+                if (cut) {
+                    visible(see, key0, see_lo, see_hi);
+                    if (bad) {
+                        uint32_t good[4] = {see[0], see[1], see[2], see[3]};  // (in memory)
+                        take_out_bad(good, key0, w.range.hi, table, p.cache);
+                        see[0] = good[0], see[1] = good[1], see[2] = good[2], see[3] = good[3];
+                    }
+                }
                 const float m = (cut ? row_max<true>(s_tmem, see) : row_max<false>(s_tmem, see)) * c;
                 const bool raise = m > m_ref + kRaise || (m_ref == -INFINITY && m > -INFINITY);
                 if (__any_sync(~0u, raise)) {

@@ -155,8 +155,7 @@ struct TileLoader {
     // zeros outside [lo, hi) and for bad blocks.
     __device__ __forceinline__ void tokens(int lo, int hi, int key0, const Group& group, int kv, uint32_t dst, uint64_t* bar) const {
         const bool good = group.block >= 0 && group.block < v.num_blocks;
-        const bool whole = key0 >= lo && key0 + 128 <= hi && __all_sync(~0u, lane >= 16 || good);
-        if (whole && box_rows) {
+        if (box_rows && key0 >= lo && key0 + 128 <= hi && __all_sync(~0u, lane >= 16 || good)) {
             constexpr int kHalves = D / 64;
             const int i = warp + lane * kWarps, row = i / kHalves * box_rows, half = i % kHalves;
             const int block = __shfl_sync(~0u, group.block, row / 8 & 15), token = __shfl_sync(~0u, group.in_block, row / 8 & 15);
@@ -168,35 +167,32 @@ struct TileLoader {
             }
             return;
         }
-        const int64_t at = good ? group.block * v.block_stride + group.in_block * v.tok_stride : -1;
         const int c = lane % kChunks, sub = lane / kChunks;
         const char* from = head + kv * v.kv_stride + c * 16;
-        if (whole) {
-            const char* first = from + sub * v.tok_stride;
+        if (v.block_tokens % 8 == 0) {
+            const int64_t at = good ? group.block * v.block_stride + group.in_block * v.tok_stride : -1;
             const int64_t step = kStep * v.tok_stride;
 #pragma unroll
             for (int j = 0; j < (16 + kWarps - 1) / kWarps; ++j) {
-                const int g = warp + j * kWarps;
-                const char* src = first + __shfl_sync(~0u, at, g & 15);
+                const int g = warp + j * kWarps, r0 = g * 8 + sub;
+                const int64_t own = __shfl_sync(~0u, at, g & 15);
+                const char* src = from + (own >= 0 ? own : 0) + sub * v.tok_stride;
+                const int l = own >= 0 ? lo - key0 - r0 : 128, h = hi - key0 - r0;  // rows [l, h) of r0, r0 + kStep, ... are wanted
                 if (g < 16) {
 #pragma unroll
                     for (int i = 0; i < 8 / kStep; ++i)
-                        cp_async16(dst + g * 1024 + tile_offset(i * kStep + sub, c), src + i * step, 16);
+                        cp_async16(dst + g * 1024 + tile_offset(i * kStep + sub, c), src + i * step, i * kStep >= l && i * kStep < h ? 16 : 0);
                 }
             }
         } else {
 #pragma unroll 1
             for (int g = warp; g < 16; g += kWarps) {
-                const int64_t own = __shfl_sync(~0u, at, g);
 #pragma unroll 1
                 for (int i = 0; i < 8 / kStep; ++i) {
                     const int r = g * 8 + i * kStep + sub, key = key0 + r;
                     bool in = key >= lo && key < hi;
                     const char* src = head;
-                    if (v.block_tokens % 8 == 0) {
-                        in = in && own >= 0;
-                        if (in) src = from + own + r % 8 * v.tok_stride;
-                    } else if (in) {
+                    if (in) {
                         const int block = table[key / v.block_tokens];
                         in = block >= 0 && block < v.num_blocks;
                         if (in) src = from + block * v.block_stride + key % v.block_tokens * v.tok_stride;

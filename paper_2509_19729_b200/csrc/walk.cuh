@@ -122,10 +122,11 @@ struct Cut {
     int64_t begin, end;  // empty shares: begin = end
     int32_t s, h, m;     // the first tile's unit,
     int32_t t, tiles;    // its place in it, and the unit's tiles
-    int32_t pad;
+    int32_t rows;        // of the unit
 };
-__device__ __forceinline__ void write_cut(Cut* cuts, const Walk& w, int64_t begin, int64_t end) {
-    if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{begin, end, w.s, w.h, w.m, w.t, w.range.tiles, 0};
+__device__ __forceinline__ void write_cut(const Shape& p, Cut* cuts, const Walk& w, int64_t begin, int64_t end) {
+    if (threadIdx.x == 0)
+        cuts[blockIdx.x] = Cut{begin, end, w.s, w.h, w.m, w.t, w.range.tiles, min(p.rows, w.seq.qn * p.group - w.m * p.rows)};
 }
 
 // This CTA's share: [*begin, *end) of all tiles, with `walk` at the first of them.  CTA 0 reports bad sequences.
