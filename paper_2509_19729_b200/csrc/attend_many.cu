@@ -30,7 +30,7 @@ struct ManyShape {
 struct ManyBarriers {
     uint64_t full[8], empty[8];  // ring of tiles: K, V, K, V, ...
     uint64_t q_full, q_empty;
-    uint64_t s_full[2], p_full[2], o_full[2], o_free[2];
+    uint64_t s_full[2], p_half[2], p_full[2], o_full[2], o_free[2];
     uint64_t drain;
     uint32_t tmem;
     int32_t abort;
@@ -293,10 +293,10 @@ __device__ bool multiply(const AttendParams& p, const Share& share, uint32_t sme
             umma_smem(leader, tmem + t * 128, q_op + (t * kTile >> 4) + step, k_op + step, kS, k > 0);
         }
     };
-    auto weigh = [&](int t, int v_slot, bool accumulate) {
+    auto weigh = [&](int t, int v_slot, int half, bool accumulate) {
         const uint64_t v_op = operand(smem + (2 + __shfl_sync(~0u, v_slot, 0)) * kTile, 128 * 128);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = half * 4; k < half * 4 + 4; ++k)
             umma_tmem(leader, tmem + 256 + t * D, tmem + t * 128 + k * 8, v_op + (k * 2048 >> 4), kO, accumulate || k > 0);
     };
     Parts part(share);
@@ -328,10 +328,14 @@ __device__ bool multiply(const AttendParams& p, const Share& share, uint32_t sme
                     if (!wait(&b.o_free[t], o_phase[t])) return false;
                     o_phase[t] ^= 1;
                 }
+                // the first half of the weights is multiplied while the second is formed
+                if (!wait(&b.p_half[t], p_phase[t])) return false;
+                tmem_fence_after();
+                weigh(t, v_slot, 0, i > 0);
                 if (!wait(&b.p_full[t], p_phase[t])) return false;
                 p_phase[t] ^= 1;
                 tmem_fence_after();
-                weigh(t, v_slot, i > 0);
+                weigh(t, v_slot, 1, true);
                 umma_commit(leader, &b.o_full[t]);
                 if (i + 1 < part.tiles) {
                     if (t == 0) {
@@ -399,9 +403,10 @@ __device__ __forceinline__ float row_max(uint32_t s_tmem, const uint32_t (&see)[
     }
     return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
-// Writes the weights 2^(c * logit - ref) over the logits, in 16 bits, and returns their sum in 32.
+// Writes the weights 2^(c * logit - ref) over the logits, in 16 bits, and returns their sum in 32; `half` gets
+// this thread's arrival when the first 64 are there.
 template <class T, bool kCut>
-__device__ __forceinline__ float row_weights(uint32_t s_tmem, const uint32_t (&see)[4], float c, float ref) {
+__device__ __forceinline__ float row_weights(uint32_t s_tmem, const uint32_t (&see)[4], float c, float ref, uint64_t* half) {
     const uint64_t c2 = pair2(c, c), ref2 = pair2(-ref, -ref);
     uint64_t sum[2] = {0, 0};
     uint32_t s[2][32], w16[32];
@@ -415,11 +420,17 @@ __device__ __forceinline__ float row_weights(uint32_t s_tmem, const uint32_t (&s
         for (int k = 0; k < 32; k += 2) {
             float x, y;
             split2(fma2(pair2(__uint_as_float(s[j % 2][k]), __uint_as_float(s[j % 2][k + 1])), c2, ref2), x, y);
-            x = fast_exp2(x), y = fast_exp2(y);
+            if (!kCut && k / 2 % kPolyOf == 0) poly_exp2(x, y);
+            else x = fast_exp2(x), y = fast_exp2(y);
             sum[k / 2 % 2] = add2(sum[k / 2 % 2], pair2(x, y));
             w16[j % 2 * 16 + k / 2] = Elem<T>::pack(x, y);
         }
         if (j % 2) tmem_store32(s_tmem + j / 2 * 32, w16);  // over logits that have been read
+        if (j == 1) {
+            tmem_store_wait();
+            tmem_fence_before();
+            mbar_arrive(half);
+        }
     }
     float a, b;
     split2(add2(sum[0], sum[1]), a, b);
@@ -494,7 +505,7 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
                     }
                 }
                 const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-                l += cut ? row_weights<T, true>(s_tmem, see, c, ref) : row_weights<T, false>(s_tmem, see, c, ref);
+                l += cut ? row_weights<T, true>(s_tmem, see, c, ref, &b.p_half[t]) : row_weights<T, false>(s_tmem, see, c, ref, &b.p_half[t]);
                 tmem_store_wait();
                 tmem_fence_before();
                 mbar_arrive(&b.p_full[t]);
@@ -560,7 +571,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
         for (int i = 0; i < ManyShape<D>::kStages; ++i) mbar_init(&b.full[i], kLoadThreads), mbar_init(&b.empty[i], 1);
         mbar_init(&b.q_full, kLoadThreads), mbar_init(&b.q_empty, 1), mbar_init(&b.drain, 1);
         for (int t = 0; t < 2; ++t)
-            mbar_init(&b.s_full[t], 1), mbar_init(&b.p_full[t], 128), mbar_init(&b.o_full[t], 1), mbar_init(&b.o_free[t], 128);
+            mbar_init(&b.s_full[t], 1), mbar_init(&b.p_half[t], 128), mbar_init(&b.p_full[t], 128), mbar_init(&b.o_full[t], 1), mbar_init(&b.o_free[t], 128);
         b.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();

@@ -154,6 +154,26 @@ def test_attend_ignores_what_no_row_sees(q, window, bad):
     check_attend(c, window)
 
 
+@pytest.mark.parametrize("q", [1, 6, 200])
+def test_attend_hands_on_a_nan_key(q):
+    """A NaN in a key that a row sees makes that row's outputs NaN, whichever token it is, and no other row's."""
+    c = Case(2, 2, 128, lens=[400], qlens=[q], seed=15).up()
+    clean = None
+    for token in [None, *range(0, 399, 7), 399]:
+        if token is not None:
+            b, t = int(c.bt[0, token // 16]), token % 16
+            keep = c.dpools[0][0, b, 1, 0, t, 5].clone()
+            c.dpools[0][0, b, 1, 0, t, 5] = float("nan")
+        c.attend()
+        got, lse = c.result()
+        sees = np.arange(q) + 400 - q >= (400 if token is None else token)
+        assert np.isnan(got[sees, 1]).all() and np.isnan(lse[sees, 1]).all() and np.isfinite(got[~sees]).all()
+        clean = got if clean is None else clean
+        assert np.array_equal(got[:, 0], clean[:, 0]) and np.array_equal(got[~sees], clean[~sees])
+        if token is not None:
+            c.dpools[0][0, b, 1, 0, t, 5] = keep
+
+
 def test_attend_large_logits_and_one_hot_rows():
     """Logits of several hundred: the maximum moves, all weight on one token."""
     for dtype in ("fp16", "bf16"):
