@@ -15,7 +15,7 @@ struct Shape {  // what the split depends on, besides the batch
     int32_t kv_heads;   // of all workers
     int32_t window;     // 0 = none
     int32_t rows;       // query rows per row tile
-    int32_t tile;       // tokens per tile
+    int32_t tile;       // tokens per tile, a power of two
     int32_t min_rows, max_rows;  // sequences with more or fewer rows (new tokens * group) are not this launch's
     int32_t rowless;    // 1: sequences without rows have one row tile all the same
 };
@@ -28,12 +28,17 @@ struct Range {
 
 __device__ __forceinline__ Range row_tile_range(const Shape& p, const Seq& q, int m) {
     Range r;
-    const int n = q.qn * p.group, last = (int)min((int64_t)n, (int64_t)(m + 1) * p.rows) - 1;
-    const int p0 = q.len - q.qn + m * p.rows / p.group, p1 = q.len - q.qn + last / p.group;
+    const int n = q.qn * p.group;
+    int p0 = q.len - q.qn, p1 = q.len - 1;  // cache indices of the tile's first and last rows
+    if (n > p.rows) {
+        const int last = (int)min((int64_t)n, (int64_t)(m + 1) * p.rows) - 1;
+        p1 = p0 + last / p.group;
+        p0 += m * p.rows / p.group;
+    }
     r.hi = min(max(p1 + 1, 0), q.len);
     r.lo = p.window > 0 ? min(max(p0 - p.window + 1, 0), r.hi) : 0;
-    r.base = r.lo / p.tile * p.tile;
-    r.tiles = max(1, (r.hi - r.base + p.tile - 1) / p.tile);
+    r.base = r.lo & -p.tile;  // (a power of two)
+    r.tiles = max(1, (r.hi - r.base + p.tile - 1) >> __ffs(p.tile) - 1);
     return r;
 }
 
@@ -52,7 +57,9 @@ __device__ __forceinline__ int64_t head_tiles(const Shape& p, const Seq& q) {
 }
 
 // First tile of CTA c's share.
-__device__ __forceinline__ int64_t share_begin(int64_t total, int ctas, int c) { return total * c / ctas; }
+__device__ __forceinline__ int64_t share_begin(int64_t total, int ctas, int c) {
+    return total < (1 << 20) ? (uint32_t)total * (uint32_t)c / (uint32_t)ctas : total * c / ctas;  // (ctas < 4096)
+}
 struct Walk {
     int32_t s, h, m, t;  // sequence, key head, row tile, tile of it
     int32_t nm;
@@ -69,7 +76,7 @@ struct Walk {
     // To the tile `off` tiles into the (non-empty) sequence that is open.
     __device__ __forceinline__ void seek(const Shape& p, int64_t off) {
         const int64_t per_head = head_tiles(p, seq);
-        h = (int)(off / per_head);
+        h = (off | per_head) >> 31 == 0 ? (int)((uint32_t)off / (uint32_t)per_head) : (int)(off / per_head);
         off -= h * per_head;
         for (m = 0;; ++m) {
             range = row_tile_range(p, seq, m);
