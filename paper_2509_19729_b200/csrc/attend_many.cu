@@ -488,9 +488,11 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
                 if (__any_sync(~0u, raise)) {
                     const float m_new = raise ? m : m_ref;
                     const float f = raise ? fast_exp2(m_ref - m_new) : 1.f;
+                    // (a row that has seen nothing yet has O = 0)
+                    const bool scales = __any_sync(~0u, raise && m_ref > -INFINITY);
                     l *= f;
                     m_ref = m_new;
-                    if (i > 0) {
+                    if (i > 0 && scales) {
                         if (!wait(&b.o_full[t], o_phase ^ 1)) return false;  // of the tile before
                         tmem_fence_after();
 #pragma unroll

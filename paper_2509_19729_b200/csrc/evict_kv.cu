@@ -91,12 +91,12 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 // in shared memory.  The smallest score that stays is found from the top, 11, 11 and 10 bits at a time, from counts of the
 // digits that all CTAs of the cluster add up; then every warp lists the kept ones of its own run of tokens in order.
 constexpr int kSelectKeys = 12288;  // keys that a CTA holds, unless eight CTAs need to hold more
-constexpr int kDigits = 2048, kDigitThreads = kDigits / 4;
+constexpr int kDigits = 2048;
 
 struct SelectShared {
     alignas(16) int32_t count[kDigits];  // of this CTA's tokens, by digit
     alignas(16) int32_t total[kDigits];  // of the cluster's
-    int32_t warp[kDigitThreads / 32];
+    int32_t warp[32];
     int32_t more, equal;      // this CTA's tokens above the limit, and at it
     int32_t found[2];         // digit, and how many at it stay
     int32_t before[32][2];
@@ -106,6 +106,7 @@ struct SelectShared {
 template <int kSelectThreads>
 __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_constant__ EvictParams p, int room) {
     constexpr int kSelectWarps = kSelectThreads / 32;
+    constexpr int kOwn = kSelectThreads < 512 ? kDigits / kSelectThreads : 4, kDigitThreads = kDigits / kOwn;  // digits of a thread
     extern __shared__ __align__(16) uint32_t s_keys[];
     __shared__ SelectShared sh;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -195,12 +196,16 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
             cluster_sync();
             total = sh.total;
         }
-        // from the largest digit down: thread t < 512 has digits 2047 - 4t ... 2044 - 4t
-        int mine[4] = {0, 0, 0, 0}, before = 0, sum = 0;
+        // from the largest digit down: thread t has kOwn of them, from 2047 - kOwn * t on
+        int mine[kOwn] = {}, before = 0, sum = 0;
         if (tid < kDigitThreads) {
-            const int4 four = *reinterpret_cast<const int4*>(&total[kDigits - 4 - tid * 4]);
-            mine[0] = four.w, mine[1] = four.z, mine[2] = four.y, mine[3] = four.x;
-            before = sum = mine[0] + mine[1] + mine[2] + mine[3];
+#pragma unroll
+            for (int j = 0; j < kOwn; j += 4) {
+                const int4 four = *reinterpret_cast<const int4*>(&total[kDigits - 4 - tid * kOwn - j]);
+                mine[j] = four.w, mine[j + 1] = four.z, mine[j + 2] = four.y, mine[j + 3] = four.x;
+                sum += four.x + four.y + four.z + four.w;
+            }
+            before = sum;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
                 const int up = __shfl_up_sync(~0u, before, o);
@@ -214,9 +219,9 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select(const __grid_cons
             for (int i = 0; i < warp; ++i) before += sh.warp[i];
             if (before < left && left <= before + sum) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < kOwn; ++j) {
                     if (before < left && left <= before + mine[j])
-                        sh.found[0] = kDigits - 1 - tid * 4 - j, sh.found[1] = left - before;
+                        sh.found[0] = kDigits - 1 - tid * kOwn - j, sh.found[1] = left - before;
                     before += mine[j];
                 }
             }
@@ -499,7 +504,8 @@ extern "C" amoeba_status amoeba_evict_kv(const amoeba_layout* layout, int32_t la
     const int room = (int)std::min<int64_t>(slice, (dev.smem_optin - (int)sizeof(SelectShared) - 1024) / 4 / 32 * 32);
     // (few and long units: as many threads as a CTA may have)
     st = cluster == kMaxCluster ? launch_clusters(evict_select<1024>, units * cluster, 1024, (size_t)room * 4, cluster, false, stream, p, room)
-                                : launch_clusters(evict_select<512>, units * cluster, 512, (size_t)room * 4, cluster, false, stream, p, room);
+         : units > 2 * dev.sms ? launch_clusters(evict_select<256>, units * cluster, 256, (size_t)room * 4, cluster, false, stream, p, room)
+                               : launch_clusters(evict_select<512>, units * cluster, 512, (size_t)room * 4, cluster, false, stream, p, room);
     if (st != AMOEBA_OK || tokens == 0) return st;
     if (p.in_place) {
         // One CTA moves about 100 GB/s; with few units, several CTAs to each.
