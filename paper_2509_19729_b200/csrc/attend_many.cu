@@ -362,29 +362,29 @@ __device__ __forceinline__ void drain_products(ManyBarriers& b) {
 }
 
 // ---- softmax: a thread per row
-// Bit i of `see`: the row sees token key0 + i, of those in [lo, hi).
-__device__ __forceinline__ void visible(uint32_t (&see)[4], int key0, int lo, int hi) {
-#pragma unroll
+// Hides the logits of tokens outside [lo, hi), and of bad blocks (table: null, or the unit has some), from the row: -infinity.
+__device__ __noinline__ void hide(uint32_t s_tmem, int key0, int lo, int hi, const int32_t* table, int unit_hi, const CacheView& v) {
+#pragma unroll 1
     for (int j = 0; j < 4; ++j) {
-        const int a = min(max(lo - key0 - j * 32, 0), 32), b = min(max(hi - key0 - j * 32, a), 32);
-        see[j] = (uint32_t)((1ull << b) - (1ull << a));
-    }
-}
-// Takes out the tokens of bad blocks.
-__device__ __noinline__ void take_out_bad(uint32_t (&see)[4], int key0, int hi, const int32_t* table, const CacheView& v) {
-    for (int i = 0; i < 128 && key0 + i < hi; ++i) {
-        const int block = table[(key0 + i) / v.block_tokens];
-        if (block < 0 || block >= v.num_blocks) see[i / 32] &= ~(1u << i % 32);
-    }
-}
-__device__ __forceinline__ void hide(uint32_t (&s)[32], uint32_t see) {
+        const int first = key0 + j * 32, a = min(max(lo - first, 0), 32), b = min(max(hi - first, a), 32);
+        uint32_t see = (uint32_t)((1ull << b) - (1ull << a));
+        for (int k = 0; table && k < 32 && first + k < unit_hi; ++k) {
+            const int block = table[(first + k) / v.block_tokens];
+            if (block < 0 || block >= v.num_blocks) see &= ~(1u << k);
+        }
+        __syncwarp();
+        uint32_t s[32];
+        tmem_load32(s, s_tmem + j * 32);
+        tmem_load_wait();
 #pragma unroll
-    for (int k = 0; k < 32; ++k)
-        if (!(see & 1u << k)) s[k] = 0xff800000u;  // -infinity
+        for (int k = 0; k < 32; ++k)
+            if (!(see & 1u << k)) s[k] = 0xff800000u;
+        tmem_store32(s_tmem + j * 32, s);
+    }
+    tmem_store_wait();
 }
-// The largest of the row's logits that it sees.  The row is read once more for the weights: kept, it would fill 128 registers.
-template <bool kCut>
-__device__ __forceinline__ float row_max(uint32_t s_tmem, const uint32_t (&see)[4]) {
+// The largest of the row's logits.  The row is read once more for the weights: kept, it would fill 128 registers.
+__device__ __forceinline__ float row_max(uint32_t s_tmem) {
     uint32_t s[4][32];
     float top[4];
     tmem_load32(s[0], s_tmem);
@@ -395,7 +395,6 @@ __device__ __forceinline__ float row_max(uint32_t s_tmem, const uint32_t (&see)[
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         if (j == 2) tmem_load_wait();
-        if (kCut) hide(s[j], see[j]);
         top[j] = __uint_as_float(s[j][0]);
 #pragma unroll
         for (int k = 1; k < 31; k += 2) top[j] = max3(top[j], __uint_as_float(s[j][k]), __uint_as_float(s[j][k + 1]));
@@ -405,8 +404,8 @@ __device__ __forceinline__ float row_max(uint32_t s_tmem, const uint32_t (&see)[
 }
 // Writes the weights 2^(c * logit - ref) over the logits, in 16 bits, and returns their sum in 32; `half` gets
 // this thread's arrival when the first 64 are there.
-template <class T, bool kCut>
-__device__ __forceinline__ float row_weights(uint32_t s_tmem, const uint32_t (&see)[4], float c, float ref, uint64_t* half) {
+template <class T>
+__device__ __forceinline__ float row_weights(uint32_t s_tmem, float c, float ref, uint64_t* half) {
     const uint64_t c2 = pair2(c, c), ref2 = pair2(-ref, -ref);
     uint64_t sum[2] = {0, 0};
     uint32_t s[2][32], w16[32];
@@ -415,13 +414,11 @@ __device__ __forceinline__ float row_weights(uint32_t s_tmem, const uint32_t (&s
     for (int j = 0; j < 4; ++j) {
         tmem_load_wait();
         if (j < 3) tmem_load32(s[(j + 1) % 2], s_tmem + (j + 1) * 32);
-        if (kCut) hide(s[j % 2], see[j]);
 #pragma unroll
         for (int k = 0; k < 32; k += 2) {
             float x, y;
             split2(fma2(pair2(__uint_as_float(s[j % 2][k]), __uint_as_float(s[j % 2][k + 1])), c2, ref2), x, y);
-            if (!kCut && k / 2 % kPolyOf == 0) poly_exp2(x, y);
-            else x = fast_exp2(x), y = fast_exp2(y);
+            x = fast_exp2(x), y = fast_exp2(y);
             sum[k / 2 % 2] = add2(sum[k / 2 % 2], pair2(x, y));
             w16[j % 2 * 16 + k / 2] = Elem<T>::pack(x, y);
         }
@@ -473,17 +470,9 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
                 if (!wait(&b.s_full[t], s_phase)) return false;
                 s_phase ^= 1;
                 tmem_fence_after();
-                uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
-                const bool cut = __any_sync(~0u, key0 + kManyTile > see_hi || key0 < see_lo) || bad;
-                if (cut) {
-                    visible(see, key0, see_lo, see_hi);
-                    if (bad) {
-                        uint32_t good[4] = {see[0], see[1], see[2], see[3]};  // (in memory)
-                        take_out_bad(good, key0, w.range.hi, table, p.cache);
-                        see[0] = good[0], see[1] = good[1], see[2] = good[2], see[3] = good[3];
-                    }
-                }
-                const float m = (cut ? row_max<true>(s_tmem, see) : row_max<false>(s_tmem, see)) * c;
+                if (__any_sync(~0u, key0 + kManyTile > see_hi || key0 < see_lo) || bad)
+                    hide(s_tmem, key0, see_lo, see_hi, bad ? table : nullptr, w.range.hi, p.cache);
+                const float m = row_max(s_tmem) * c;
                 const bool raise = m > m_ref + kRaise || (m_ref == -INFINITY && m > -INFINITY);
                 if (__any_sync(~0u, raise)) {
                     const float m_new = raise ? m : m_ref;
@@ -507,7 +496,7 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
                     }
                 }
                 const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-                l += cut ? row_weights<T, true>(s_tmem, see, c, ref, &b.p_half[t]) : row_weights<T, false>(s_tmem, see, c, ref, &b.p_half[t]);
+                l += row_weights<T>(s_tmem, c, ref, &b.p_half[t]);
                 tmem_store_wait();
                 tmem_fence_before();
                 mbar_arrive(&b.p_full[t]);
@@ -582,7 +571,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     __syncthreads();
     tmem_fence_after();
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == 8) {
             if (!multiply<T, D>(p, share, smem_u32(smem), b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
             __syncwarp();
@@ -591,7 +580,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
             load_loop<D>(p, maps, box_rows, share, smem, b);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         if (!softmax<T, D>(p, share, b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
     }
     grid_dependency_wait();  // attend_few in front is done when this kernel is

@@ -100,32 +100,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// One pair in kPolyOf has its powers of two formed on the multiply-add units, beside the others on the special-function unit,
-// which is what the softmax of many rows waits for most (of a chunk of 4 x 2048 tokens: none 976 us, one in eight 956, two 970).
-constexpr int kPolyOf = 8;
-// 2^x of two values, for x up to 16: the whole part goes to the exponent, 2^f of the rest, f in [-1/2, 1/2], is a polynomial (the
-// one of degree 5 with the least relative error, by the Remez exchange: 7.5e-8, 2.2e-7 as evaluated).  Below 2^-125 it stays
-// there, which counts as nothing beside a largest weight of 1 or more.
-__device__ __forceinline__ void poly_exp2(float& lo, float& hi) {
-    const uint64_t x = pair2(fmaxf(lo, -125.f), fmaxf(hi, -125.f));
-    const float round = 12582912.f;  // 1.5 * 2^23: the sum's last bits are the whole part
-    const uint64_t t = add2(x, pair2(round, round));
-    const uint64_t f = fma2(add2(t, pair2(-round, -round)), pair2(-1.f, -1.f), x);
-    uint64_t r = pair2(1.3276475e-3f, 1.3276475e-3f);
-    r = fma2(r, f, pair2(9.675541e-3f, 9.675541e-3f));
-    r = fma2(r, f, pair2(5.5507131e-2f, 5.5507131e-2f));
-    r = fma2(r, f, pair2(0.24022120f, 0.24022120f));
-    r = fma2(r, f, pair2(0.69314694f, 0.69314694f));
-    r = fma2(r, f, pair2(1.0000001f, 1.0000001f));
-    float a, b, n, m;
-    split2(r, a, b);
-    split2(t, n, m);
-    a = __uint_as_float(__float_as_uint(a) + (__float_as_uint(n) << 23));
-    b = __uint_as_float(__float_as_uint(b) + (__float_as_uint(m) << 23));
-    lo = lo == lo ? a : lo;  // a NaN stays one
-    hi = hi == hi ? b : hi;
-}
-
 // ---- loading
 // One arrival of this thread, when all the asynchronous loads that it has started are done.  The products' warp makes them
 // visible to the tensor core (fence_async_smem after its wait): a fence here would wait for the loads still in flight.
