@@ -465,8 +465,8 @@ AMOEBA_API amoeba_status amoeba_plan_weight_alias(const amoeba_plan* plan, int32
  *
  * Rows.  The new tokens of sequence s are rows d_q_starts[s] ... d_q_starts[s+1]-1, its last ones: with n rows and
  * d_seq_lens[s] = len cached tokens, these included, row d_q_starts[s] + j is the token at cache index len - n + j.
- * Rows that belong to no sequence - before the first, behind the last, as in a padded batch - are neither read nor
- * written.  The token at cache index i of sequence s is in slot i % block_tokens of block
+ * Rows that belong to no sequence - before the first, behind the last, as in a padded batch - may hold anything and are
+ * not written.  The token at cache index i of sequence s is in slot i % block_tokens of block
  * d_block_table[s][i / block_tokens]; table entries past a sequence's last block are not read.
  *
  * Device-detected errors.  INVALID_ARG, and nothing of the sequence is done: a negative length or one that needs more
@@ -502,8 +502,8 @@ typedef struct {
  * pair (x_a, x_b) of its leading rot_dim elements turned by position * inv_freq[pair],
  *   (x_a cos - x_b sin, x_b cos + x_a sin);
  * queries go to q_out, keys and (as they are) values into the cache.  All in 32 bits with one rounding at the end; the
- * angle and its reduction to [-pi, pi] in 64 bits, since position * inv_freq at position 131071 has lost the low digits
- * of the angle in 32.
+ * angle and its reduction to [-pi, pi] in 64 bits, since in 32 position * inv_freq has lost its last digits long before
+ * position 131071.
  * rotation NULL: neither norm nor rotation.  q and q_out both NULL: keys and values only.  q_out may be q.  A sequence
  * with more new tokens than cached ones is refused (INVALID_ARG).  Several sequences may share a block only if no new
  * token falls into it.

@@ -150,16 +150,17 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
 // The products on the fifth-generation tensor cores, 128 tokens by 128 query rows: S^T = K Q^T, so that a thread has a token
 // and sums along its own columns.  A CTA keeps 128 rows in shared memory and runs through its tokens, 128 at a time, then the
 // next 128 rows of the same sequence and head, then its next head; the tokens of a head are dealt out to CTAs in tiles, all
-// rows with them, so a score has one thread.  Bound by the exponentials, 16 a clock and SM; two warpgroups take the tiles in
-// turn, each with two logit tiles in tensor memory, so that the products run ahead.
-constexpr int kScoreManyThreads = 384, kScoreLoadWarps = 3;
+// rows with them, so a score has one thread.  Four warpgroups take the tiles in turn, each with its own logits in tensor
+// memory: a tile's 16384 exponentials take the special-function units 1024 clocks, and four warps to each keep them busy
+// where two left them idle half the time.
+constexpr int kScoreGroups = 4, kScoreManyThreads = 128 * (kScoreGroups + 1), kScoreLoadWarps = 3;
 template <int D>
 struct ScoreManyShape {
     static constexpr int kTileBytes = 128 * D * 2, kStages = D == 128 ? 4 : 8;
     static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
 };
 struct ScoreBarriers {
-    uint64_t k_full[8], k_empty[8], q_full[2], q_empty[2], s_full[4], s_empty[4], drain;
+    uint64_t k_full[8], k_empty[8], q_full[2], q_empty[2], s_full[kScoreGroups], s_empty[kScoreGroups], drain;
     uint32_t tmem;
     int32_t abort;
 };
@@ -245,7 +246,8 @@ __device__ void take_runs(const ScoreParams& p, Runs* r, int32_t* status) {
 template <int D>
 __device__ bool score_load(const ScoreParams& p, const CacheMaps& maps, int box_rows, uint32_t smem, ScoreBarriers& b, Runs run) {
     using S = ScoreManyShape<D>;
-    TileLoader<D, kScoreLoadWarps> load(p.cache, maps, box_rows, ((int)threadIdx.x - 288) / 32, threadIdx.x % 32);
+    TileLoader<D, kScoreLoadWarps> load(p.cache, maps, box_rows, (int)(threadIdx.x - (kScoreManyThreads - 32 * kScoreLoadWarps)) / 32,
+                                         threadIdx.x % 32);
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
     int slot = 0, qb = 0;
     uint32_t phase = 1, q_phase = 1;
@@ -276,16 +278,16 @@ __device__ bool score_multiply(const ScoreParams& p, uint32_t smem, ScoreBarrier
     constexpr uint32_t kIdesc = product<T>(128, false);
     const uint32_t tmem = __shfl_sync(~0u, b.tmem, 0), leader = elect_one();
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
-    int slot = 0, qb = 0, done[2] = {0, 0};  // tiles of each warpgroup
-    uint32_t phase = 0, q_phase = 0;
+    int slot = 0, qb = 0;
+    uint32_t phase = 0, q_phase = 0, free = (1u << kScoreGroups) - 1;  // bit g: parity to wait for at s_empty[g]
     while (run.next(p)) {
         for (int j = 0; j < run.passes; ++j) {
             if (!wait(&b.q_full[qb], q_phase)) return false;
             for (int i = 0; i < run.t1 - run.t0; ++i) {
-                const int g = i & 1, buf = g * 2 + (done[g] & 1);
+                const int g = i % kScoreGroups;
                 if (!wait(&b.k_full[slot], phase)) return false;
-                if (!wait(&b.s_empty[buf], (done[g] >> 1 & 1) ^ 1)) return false;
-                ++done[g];
+                if (!wait(&b.s_empty[g], free >> g & 1)) return false;
+                free ^= 1u << g;
                 fence_async_smem();
                 tmem_fence_after();
                 const uint64_t k_op = operand(smem + (2 + __shfl_sync(~0u, slot, 0)) * S::kTileBytes, 16);
@@ -293,9 +295,9 @@ __device__ bool score_multiply(const ScoreParams& p, uint32_t smem, ScoreBarrier
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint32_t step = (k / 4 * (128 * 128) + k % 4 * 32) >> 4;
-                    umma_smem(leader, tmem + buf * 128, k_op + step, q_op + step, kIdesc, k > 0);
+                    umma_smem(leader, tmem + __shfl_sync(~0u, g, 0) * 128, k_op + step, q_op + step, kIdesc, k > 0);
                 }
-                umma_commit(leader, &b.s_full[buf]);
+                umma_commit(leader, &b.s_full[g]);
                 umma_commit(leader, &b.k_empty[slot]);
                 if (++slot == S::kStages) slot = 0, phase ^= 1;
             }
@@ -313,14 +315,12 @@ __device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[12
                                             uint64_t* empty) {
     const uint64_t c2 = pair2(c, c);
     uint64_t sum[2] = {0, 0};
-    uint32_t s[2][32];
-    tmem_load32(s[0], from);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        uint32_t s[32];
+        tmem_load32(s, from + i * 32);
         tmem_load_wait();
-        if (i < 3) {
-            tmem_load32(s[(i + 1) % 2], from + (i + 1) * 32);
-        } else {
+        if (i == 3) {
             tmem_fence_before();
             mbar_arrive(empty);
         }
@@ -328,8 +328,8 @@ __device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[12
         for (int k = 0; k < 32; k += 4) {
             const float4 r = *reinterpret_cast<const float4*>(&row[i * 32 + k]);
             float x[4];
-            split2(fma2(pair2(__uint_as_float(s[i % 2][k]), __uint_as_float(s[i % 2][k + 1])), c2, pair2(r.x, r.y)), x[0], x[1]);
-            split2(fma2(pair2(__uint_as_float(s[i % 2][k + 2]), __uint_as_float(s[i % 2][k + 3])), c2, pair2(r.z, r.w)), x[2], x[3]);
+            split2(fma2(pair2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, pair2(r.x, r.y)), x[0], x[1]);
+            split2(fma2(pair2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, pair2(r.z, r.w)), x[2], x[3]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = fast_exp2(x[e]);
             if (kCut) {
@@ -354,7 +354,8 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
     const uint32_t lanes = (uint32_t)(tid / 32 * 32) << 16;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
     const float c = p.scale_log2;
-    int done = 0, pass = 0;
+    int pass = 0;
+    uint32_t full = 0;  // parity to wait for at s_full[g]
     while (run.next(p)) {
         const Seq& q = run.w.seq;
         const int w = run.w.h / p.cache.heads, hw = run.w.h - w * p.cache.heads;
@@ -378,8 +379,8 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
             // the block of the next tile's token is asked for a tile early
             int at = (run.t0 + g) * 128 + tid, i_block = at / T, in_block = at - i_block * T, block = -1;
             if (run.t0 + g < run.t1 && at < q.len) block = table[i_block];
-            for (int t = run.t0 + g; t < run.t1; t += 2, ++done) {
-                const int key0 = t * 128, key = key0 + tid, buf = g * 2 + (done & 1);
+            for (int t = run.t0 + g; t < run.t1; t += kScoreGroups, full ^= 1) {
+                const int key0 = t * 128, key = key0 + tid;
                 float* to = nullptr;
                 float old = 0.f;
                 if (key < q.len) {
@@ -390,17 +391,17 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
                         report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
                     }
                 }
-                at = key + 256;
-                if (t + 2 < run.t1 && at < q.len) {
+                at = key + 128 * kScoreGroups;
+                if (t + kScoreGroups < run.t1 && at < q.len) {
                     i_block = at / T, in_block = at - i_block * T;
                     block = table[i_block];
                 }
                 const bool cut = key0 + 127 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
-                if (!wait(&b.s_full[buf], done >> 1 & 1)) return false;
+                if (!wait(&b.s_full[g], full)) return false;
                 tmem_fence_after();
-                const uint32_t from = b.tmem + lanes + buf * 128;
-                const float sum = cut ? column_sum<true>(from, s_row[pass], s_pos[pass], key, p.window, c, &b.s_empty[buf])
-                                      : column_sum<false>(from, s_row[pass], s_pos[pass], key, p.window, c, &b.s_empty[buf]);
+                const uint32_t from = b.tmem + lanes + g * 128;
+                const float sum = cut ? column_sum<true>(from, s_row[pass], s_pos[pass], key, p.window, c, &b.s_empty[g])
+                                      : column_sum<false>(from, s_row[pass], s_pos[pass], key, p.window, c, &b.s_empty[g]);
                 if (to) *to = old + sum;
             }
         }
@@ -413,8 +414,8 @@ __global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_
                                                                 int box_rows) {
     extern __shared__ char smem_raw[];
     __shared__ ScoreBarriers b;
-    __shared__ __align__(16) float s_row[2][2][128];
-    __shared__ __align__(16) int32_t s_pos[2][2][128];
+    __shared__ __align__(16) float s_row[kScoreGroups][2][128];
+    __shared__ __align__(16) int32_t s_pos[kScoreGroups][2][128];
     using S = ScoreManyShape<D>;
     char* smem = smem_raw + (1024 - smem_u32(smem_raw) % 1024) % 1024;
     const int warp = threadIdx.x / 32;
@@ -424,14 +425,14 @@ __global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_
         grid_dependency_wait();
         return;
     }
-    if (warp == 8) {
+    if (warp == 4 * kScoreGroups) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&b.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) mbar_init(&b.k_full[i], 32 * kScoreLoadWarps), mbar_init(&b.k_empty[i], 1);
         for (int i = 0; i < 2; ++i) mbar_init(&b.q_full[i], 32 * kScoreLoadWarps), mbar_init(&b.q_empty[i], 1);
-        for (int i = 0; i < 4; ++i) mbar_init(&b.s_full[i], 1), mbar_init(&b.s_empty[i], 128);
+        for (int i = 0; i < kScoreGroups; ++i) mbar_init(&b.s_full[i], 1), mbar_init(&b.s_empty[i], 128);
         mbar_init(&b.drain, 1);
         b.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -441,9 +442,9 @@ __global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_
     __syncthreads();
     tmem_fence_after();
     bool ok;
-    if (warp < 8) {
+    if (warp < 4 * kScoreGroups) {
         ok = score_sum(p, b, run, s_row[warp / 4], s_pos[warp / 4]);
-    } else if (warp == 8) {
+    } else if (warp == 4 * kScoreGroups) {
         ok = score_multiply<T, D>(p, smem_u32(smem), b, run);
         __syncwarp();
         umma_commit(elect_one(), &b.drain);
@@ -457,7 +458,7 @@ __global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_
     grid_dependency_wait();  // score_few in front is done when this kernel is
     tmem_fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 4 * kScoreGroups) {
         tmem_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(b.tmem));
     }

@@ -99,10 +99,11 @@ def test_attend_single_tokens(Hq, Hkv, D, tp, dtype, order):
     check_attend(c)
 
 
-@pytest.mark.parametrize("T", [1, 5, 8, 16, 24, 32, 48, 64, 100])
+@pytest.mark.parametrize("T", [1, 5, 8, 16, 24, 32, 48, 64, 72, 100, 128, 256, 1000])
 @pytest.mark.parametrize("D", [64, 128])
-def test_attend_block_sizes(T, D):
-    c = Case(4, 2, D, 2, T=T, order=T % 2, lens=[1, 70, 129, 31], qlens=[1, 3, 40, 0], seed=T).up()
+@pytest.mark.parametrize("order", [0, 1])
+def test_attend_block_sizes(T, D, order):
+    c = Case(4, 2, D, 2, T=T, order=order, lens=[1, 70, 129, 31, 290], qlens=[1, 3, 40, 0, 60], seed=T).up()
     c.attend()
     check_attend(c)
 
@@ -309,6 +310,20 @@ def test_attend_long_sequence_beside_short_ones():
             assert (np.abs(lse[lo:hi] - L) <= ref.tolerance_lse(128, int(n), L, size)).all()
 
 
+@pytest.mark.parametrize("S,Hkv", [(40, 8), (300, 1)])
+def test_attend_pieces_of_many_sequences(S, Hkv):
+    """Units enough to be dealt out whole before the last are cut; and more sequences than that is kept for."""
+    g = np.random.default_rng(S)
+    q = g.integers(33, 42, S)
+    q[::7] = 1
+    c = Case(Hkv, Hkv, 64, lens=q + g.integers(0, 200, S), qlens=q, seed=16).up()
+    c.attend()
+    check_attend(c)
+    first = [o.clone() for o in c.out]
+    c.attend()
+    assert all(torch.equal(x, y) for x, y in zip(first, c.out))  # the same bits again
+
+
 def test_attend_many_sequences_and_nothing_to_do():
     a = A()
     n = np.random.default_rng(1).integers(0, 40, 700)
@@ -475,6 +490,33 @@ def test_scores_bad_blocks():
     c = Case(4, 2, 64, lens=[60, 20], qlens=[3, 1], seed=32)
     c.bt[0, 1] = -7
     check_scores(c.up(), status=A().ERR_BAD_BLOCK_ID)
+
+
+def test_scores_of_long_sequences():
+    """Several passes of 128 rows over many tiles, a window, and a share that ends inside a head; against torch in 64 bits."""
+    for window in (0, 700):
+        c = Case(8, 2, 128, 2, order=1, lens=[2900, 40, 1111], qlens=[100, 40, 1], seed=34).up()
+        c.attend(window)
+        prior = [2800, 0, 1200]
+        old, got = run_scores(c, window, prior)
+        for s, n in enumerate(c.lens):
+            n = int(n)
+            i = torch.arange(n, device=DEV)
+            b, t = c.dbt[s].long()[i // 16], i % 16
+            lo, hi = int(c.starts[s]), int(c.starts[s + 1])
+            pos = n - (hi - lo) + torch.arange(hi - lo, device=DEV)[:, None]
+            sees = (i[None] <= pos) & ((i[None] > pos - window) if window else True)
+            for h in range(2):
+                K = c.dpools[h][0, 0, b, t, 0].double()
+                q = c.q[lo:hi, h * 4:h * 4 + 4].double().to(DEV)
+                x = torch.einsum("rgd,kd->rgk", q, K) * c.scale
+                L = c.lse[lo:hi, h * 4:h * 4 + 4].double()[..., None]
+                p = torch.where(sees[:, None], (x - L).exp(), 0.0)
+                was = old[h][0].to(DEV)[b, 0, t].double() * (i < prior[s])
+                size = torch.einsum("rgd,kd->rgk", q.abs(), K.abs()) * c.scale
+                e = (128 + 4) * 2.0 ** -23 * size + 3 * 2.0 ** -23 * (x.abs() + L.abs()) + 2.0 ** -20 + (4 * (hi - lo) + 4) * 2.0 ** -23
+                off = (got[h][0][b, 0, t].double() - (was + p.sum((0, 1)))).abs()
+                assert (off <= (p * e).sum((0, 1)) + was.abs() * 2.0 ** -22 + 1e-37).all()
 
 
 def test_scores_sum_to_the_rows():
@@ -655,6 +697,31 @@ def test_evict_long_sequences():
                 assert torch.equal(p[0, db, h, :, j % T], pool[0, sb, h, :, f % T])
                 assert torch.equal(sc[0, db, h, j % T], scores[0, sb, h, f % T])
             assert int(new.item()) == budget and int(status.item()) == 0
+
+
+def test_evict_more_scores_than_fit_on_chip():
+    """Half a million tokens of one small head: the scores are read anew in every pass."""
+    a = A()
+    T, n, budget = 32, 500001, 70000
+    nb = -(-n // T)
+    layout = a.make_layout(model(1, 1, 8), 1, nb, T)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    pool = torch.randn(1, nb, 1, 2, T, 8, generator=g, device=DEV).to(torch.bfloat16)
+    scores = torch.randn(1, nb, 1, T, generator=g, device=DEV).mul(1000).round()
+    bt = torch.randperm(nb, generator=g, device=DEV).to(torch.int32).view(1, nb)
+    lens, new = torch.tensor([n], dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(a.amoeba_evict_workspace_bytes(layout, 1, 1, budget), dtype=torch.uint8, device=DEV)
+    i = torch.arange(n, device=DEV)
+    x = scores[0, bt[0].long()[i // T], 0, i % T].clone()
+    x[n - 100:] = math.inf
+    f = x.sort(descending=True, stable=True).indices[:budget].sort().values
+    p, sc = pool.clone(), scores.clone()
+    a.amoeba_evict_kv(layout, 0, 1, [p], [sc], bt, lens, bt, budget, 100, new, status, ws)
+    j = torch.arange(budget, device=DEV)
+    sb, db = bt[0].long()[f // T], bt[0].long()[j // T]
+    assert torch.equal(p[0, db, 0, :, j % T], pool[0, sb, 0, :, f % T]) and torch.equal(sc[0, db, 0, j % T], scores[0, sb, 0, f % T])
+    assert int(new.item()) == budget and int(status.item()) == 0
 
 
 # ------------------------------------------------------------------------------------------------- streams, graphs, together
