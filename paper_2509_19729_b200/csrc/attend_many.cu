@@ -11,8 +11,8 @@
 // The first half of a tile's weights is handed on while the second is formed.  A row's logits are read from tensor memory twice,
 // for the maximum and for the weights: kept in between they would fill 128 registers.
 //
-// Measured: four sequences, 1807 to 2017 new tokens each, 6 to 12 thousand cached, 32 query heads on 8 key heads of 128: 973 us
-// (1.09 PFLOP/s) in short runs, 1.13 ms (0.95) when it runs on and the power limit takes the clock from 1965 to 1700 MHz.  Of a
+// Measured: four sequences, about 1830 new tokens each, 9 to 12 thousand cached, 32 query heads on 8 key heads of 128: 965 us
+// (1.10 PFLOP/s) in short runs, 1.12 ms (0.95) when it runs on and the power limit takes the clock from 1965 to 1700 MHz.  Of a
 // tile's 3.4 thousand clocks the tensor core is busy about 2.5; the rest is a row's softmax, 310 clocks for the maximum and 1500
 // for the weights, whose 128 exponentials take 1024 on the special-function unit that two rows of the other tile use as well.  (A
 // polynomial on the multiply-add units in place of every eighth exponential made it slower, 1010 us.)

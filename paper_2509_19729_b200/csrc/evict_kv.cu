@@ -2,7 +2,9 @@
 //
 // Two launches: which tokens stay (for each layer, sequence and key head, by the budget-th largest score: an ordered list of
 // the kept indices), and the move of their keys, values and scores.  Memory-bound: the scores are read once, what stays is
-// read and written once.
+// read and written once.  Measured: 32 sequences of 700 to 8192 tokens cut to 1024, two layers, 8 key heads of 128: 118 us, of
+// which the selection is 25 (latency: one unit takes a CTA 10 to 20 us) and the move 84 (5.6 TB/s of rows of 256 bytes); one of
+// 131072 cut to 16384: 51 us, 25 and 22.  (Both in one kernel took 117 and 67 us.)
 #include "cache_view.cuh"
 #include "copy_engine.cuh"
 
