@@ -480,7 +480,7 @@ typedef struct {
     const int32_t* d_seq_lens;    /* [num_seqs]: cached tokens, the new ones included */
     const int32_t* d_q_starts;    /* [num_seqs + 1], or NULL: one new token per sequence, row s */
     int32_t num_seqs, max_blocks_per_seq;
-    int32_t num_rows;             /* rows of the row buffers */
+    int32_t num_rows;             /* rows of the row buffers; with 0 these, and lse, may be NULL */
     int32_t max_q_len;            /* no sequence has more new tokens than this (it sizes the launch) */
 } amoeba_batch;
 

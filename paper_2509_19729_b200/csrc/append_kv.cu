@@ -199,13 +199,13 @@ extern "C" amoeba_status amoeba_append_kv(const amoeba_layout* layout, int32_t d
     const int D = layout->model.head_dim;
     p.tp = layout->tp;
     p.q_heads = q ? layout->model.num_q_heads / layout->tp : 0;
-    if ((st = make_rows(layout, k, k_stride, (int64_t)p.cache.heads * D, &p.k)) != AMOEBA_OK) return st;
-    if ((st = make_rows(layout, v, v_stride, (int64_t)p.cache.heads * D, &p.v)) != AMOEBA_OK) return st;
+    if ((st = make_rows(layout, p.batch, k, k_stride, (int64_t)p.cache.heads * D, &p.k)) != AMOEBA_OK) return st;
+    if ((st = make_rows(layout, p.batch, v, v_stride, (int64_t)p.cache.heads * D, &p.v)) != AMOEBA_OK) return st;
     if (q) {
-        if ((st = make_rows(layout, q, q_stride, (int64_t)p.q_heads * D, &p.q)) != AMOEBA_OK) return st;
-        if ((st = make_rows(layout, q_out, q_out_stride, (int64_t)p.q_heads * D, &p.q_out)) != AMOEBA_OK) return st;
+        if ((st = make_rows(layout, p.batch, q, q_stride, (int64_t)p.q_heads * D, &p.q)) != AMOEBA_OK) return st;
+        if ((st = make_rows(layout, p.batch, q_out, q_out_stride, (int64_t)p.q_heads * D, &p.q_out)) != AMOEBA_OK) return st;
         for (int r = 0; r < layout->tp; ++r)  // in place only row by row
-            if (p.q.base[r] == p.q_out.base[r] && p.q.stride != p.q_out.stride) return AMOEBA_ERR_INVALID_ARG;
+            if (p.q.base[r] && p.q.base[r] == p.q_out.base[r] && p.q.stride != p.q_out.stride) return AMOEBA_ERR_INVALID_ARG;
     }
     p.status = d_status;
     if (rotation) {

@@ -417,11 +417,11 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     if (!d_status || window < 0 || !positive(scale)) return AMOEBA_ERR_INVALID_ARG;
     const amoeba_model& m = layout->model;
     const int64_t row = (int64_t)m.num_q_heads / layout->tp * m.head_dim;
-    if ((st = make_rows(layout, q, q_stride, row, &p.q)) != AMOEBA_OK) return st;
-    if ((st = make_rows(layout, out, out_stride, row, &p.out)) != AMOEBA_OK) return st;
+    if ((st = make_rows(layout, p.batch, q, q_stride, row, &p.q)) != AMOEBA_OK) return st;
+    if ((st = make_rows(layout, p.batch, out, out_stride, row, &p.out)) != AMOEBA_OK) return st;
     for (int r = 0; r < layout->tp; ++r)  // other CTAs may still read the rows that one has answered
         for (int o = 0; o < layout->tp; ++o)
-            if (q[r] == out[o]) return AMOEBA_ERR_INVALID_ARG;
+            if (q[r] && q[r] == out[o]) return AMOEBA_ERR_INVALID_ARG;
     int64_t need = 0;
     if ((st = amoeba_attend_workspace_bytes(layout, batch, &need)) != AMOEBA_OK) return st;
     if (!d_workspace || workspace_bytes < need) return AMOEBA_ERR_INVALID_ARG;

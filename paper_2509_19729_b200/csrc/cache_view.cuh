@@ -145,7 +145,8 @@ inline amoeba_status make_batch(const amoeba_batch* b, Batch* out) {
     return AMOEBA_OK;
 }
 
-inline amoeba_status make_rows(const amoeba_layout* l, const void* const* ptrs, int64_t stride, int64_t row_elems,
+// The workers' row buffers; without rows their addresses do not matter.
+inline amoeba_status make_rows(const amoeba_layout* l, const Batch& b, const void* const* ptrs, int64_t stride, int64_t row_elems,
                                Rows* out) {
     if (!ptrs) return AMOEBA_ERR_INVALID_ARG;
     if (stride == 0) stride = row_elems;
@@ -153,7 +154,7 @@ inline amoeba_status make_rows(const amoeba_layout* l, const void* const* ptrs, 
     out->stride = stride * l->model.elem_bytes;
     if (out->stride % 16) return AMOEBA_ERR_ALIGNMENT;
     for (int r = 0; r < l->tp; ++r) {
-        if (!ptrs[r]) return AMOEBA_ERR_INVALID_ARG;
+        if (!ptrs[r] && b.num_rows) return AMOEBA_ERR_INVALID_ARG;
         if ((uintptr_t)ptrs[r] % 16) return AMOEBA_ERR_ALIGNMENT;
         out->base[r] = static_cast<char*>(const_cast<void*>(ptrs[r]));
     }

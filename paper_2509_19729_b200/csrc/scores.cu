@@ -505,9 +505,9 @@ extern "C" amoeba_status amoeba_accumulate_scores(const amoeba_layout* layout, i
     if ((st = check_elements(layout, dtype)) != AMOEBA_OK) return st;
     if ((st = make_cache_view(layout, layer, pools, &p.cache)) != AMOEBA_OK) return st;
     if ((st = make_batch(batch, &p.batch)) != AMOEBA_OK) return st;
-    if (!d_status || !d_lse || !score_pools || window < 0 || !positive(scale)) return AMOEBA_ERR_INVALID_ARG;
+    if (!d_status || (!d_lse && p.batch.num_rows) || !score_pools || window < 0 || !positive(scale)) return AMOEBA_ERR_INVALID_ARG;
     const amoeba_model& m = layout->model;
-    if ((st = make_rows(layout, q, q_stride, (int64_t)m.num_q_heads / layout->tp * m.head_dim, &p.q)) != AMOEBA_OK)
+    if ((st = make_rows(layout, p.batch, q, q_stride, (int64_t)m.num_q_heads / layout->tp * m.head_dim, &p.q)) != AMOEBA_OK)
         return st;
     const int64_t layer_scores = (int64_t)layout->num_blocks * p.cache.heads * layout->block_tokens;
     for (int r = 0; r < layout->tp; ++r) {

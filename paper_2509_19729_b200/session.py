@@ -343,7 +343,8 @@ class CacheSession:
     weight its tokens received, and long sequences cut to a budget.
 
     dtype: "fp16" or "bf16"; kv_layers: layers the pools hold (None = all); scores: hold score pools too.  set_tables()
-    and set_rows() describe the batch of a step; the row buffers q, k, v, out are the caller's, one tensor per worker."""
+    and set_rows() describe the batch of a step; the row buffers q, k, v, out are the caller's, one tensor per worker.
+    All calls share one workspace, so they run one after another, on one stream or on streams that wait for each other."""
 
     def __init__(self, model: dict, tp: int, NB: int, num_seqs: int, max_blocks_per_seq: int, dtype: str = "bf16",
                  kv_layers: Optional[int] = None, block_tokens: int = 16, kv_order: int = A.KV_HEAD_MAJOR,
@@ -363,7 +364,7 @@ class CacheSession:
         self.new_lens = torch.zeros(num_seqs, **i32)
         self.q_starts = torch.zeros(num_seqs + 1, **i32)
         self.status = torch.zeros(1, **i32)
-        self.workspace = torch.empty(0, dtype=torch.uint8, device=dev)
+        self.workspace, self._outgrown = torch.empty(0, dtype=torch.uint8, device=dev), []
         self.set_rows(None, num_seqs, 1)
 
     def set_tables(self, seq_lens, block_table) -> None:
@@ -380,7 +381,9 @@ class CacheSession:
 
     def _room(self, nbytes: int) -> None:
         if self.workspace.numel() < nbytes:
-            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            # Calls on any stream, or captured ones, may still use the old one; doubling bounds what they keep.
+            self._outgrown.append(self.workspace)
+            self.workspace = torch.empty(max(nbytes, 2 * self.workspace.numel()), dtype=torch.uint8, device=self.device)
 
     def append(self, layer: int, q, k, v, rotation, q_out, stream=None) -> None:
         A.amoeba_append_kv(self.layout, self.dtype, layer, self.pools, self.batch, q, k, v, rotation, q_out, self.status,

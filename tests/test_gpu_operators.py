@@ -757,6 +757,64 @@ def test_other_streams_and_captured_graphs_that_share_a_workspace():
         check_attend(d)
 
 
+def test_two_calls_at_once():
+    """Two streams, two workspaces, the same cache."""
+    c = Case(8, 2, 128, 2, lens=[3000, 40, 800], qlens=[1, 1, 1], seed=52).up()
+    d = Case(8, 2, 128, 2, lens=[3000, 40, 800], qlens=[90, 30, 1], seed=52).up()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for x, st in zip((c, d), streams):
+            x.attend(stream=st)
+    torch.cuda.synchronize()
+    check_attend(c)
+    check_attend(d)
+
+
+def test_batches_without_rows():
+    """No new tokens: nothing to attend or append, and new tokens' scores start at zero."""
+    a = A()
+    c = Case(4, 2, 64, lens=[40, 20], qlens=[0, 0], seed=53).up()
+    assert c.rows == 0
+    c.attend()
+    a.amoeba_append_kv(c.layout, 1, 0, c.dpools, c.batch, c.dq, [x[:, :128] for x in c.dq], [x[:, :128] for x in c.dq], None, c.out,
+                       c.status)
+    old, got = run_scores(c, scored=[10, 20])
+    torch.cuda.synchronize()
+    for s, (n, k) in enumerate(((40, 10), (20, 20))):
+        i = torch.arange(n)
+        b, t = torch.from_numpy(c.bt[s]).long()[i // 16], i % 16
+        want = torch.where(i[:, None] < k, old[0][0][b, :, t], torch.zeros(()))
+        assert torch.equal(got[0][0].cpu()[b, :, t], want)
+    assert int(c.status.item()) == 0
+
+
+def test_a_captured_call_outlives_a_larger_workspace():
+    """A call captured before the session's workspace grew still has its own to work in."""
+    from paper_2509_19729_b200.session import CacheSession
+
+    s = CacheSession(model(4, 2, 64), 1, 80, 2, 40, device=DEV)
+    g = torch.Generator().manual_seed(61)
+    for pool in s.pools:
+        n = pool.numel() // 2
+        pool.view(torch.bfloat16).copy_(torch.randn(n, generator=g).to(torch.bfloat16))
+    s.set_tables([640, 600], torch.arange(80, dtype=torch.int32).view(2, 40))
+    q = torch.randn(2, 256, generator=g).to(torch.bfloat16).to(DEV)
+    want, out = torch.empty_like(q), torch.zeros_like(q)
+    s.attend(0, [q], [want])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.attend(0, [q], [out])
+    before = s.workspace.data_ptr()
+    s._room(4 * s.workspace.numel())
+    assert s.workspace.data_ptr() != before
+    taken = [torch.full((1 << 16,), -1, dtype=torch.int32, device=DEV) for _ in range(64)]
+    graph.replay()
+    assert torch.equal(out, want) and int(s.status.item()) == 0
+    assert all(bool((t == -1).all()) for t in taken)
+
+
 def test_a_generation_with_eviction_and_a_transformation():
     """Append, attend, accumulate and evict in turn, two layers, as a serving loop calls them; then the instance is split
     TP 1 -> 2 -> its attention is the same to the bit."""
