@@ -24,8 +24,17 @@ struct EvictParams {
 
 constexpr int kMaxCluster = 8;
 
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -53,22 +62,33 @@ __device__ __forceinline__ void store_remote(int32_t* p, uint32_t rank, int32_t 
 }
 
 // The sequence's length, or -1 if it is refused.  The whole cluster asks together, each CTA looking at its part of the tables;
-// bad: [kMaxCluster] in shared memory.
+// bad: [kMaxCluster] in shared memory.  Another CTA's shared memory may be written once that CTA runs: every CTA arrives at the
+// cluster's barrier before it looks at the tables and waits there after, in front of its first remote store.
 __device__ __forceinline__ int checked_len(const EvictParams& p, int s, bool reports, uint32_t rank, uint32_t size, int32_t* bad) {
+    if (size > 1) cluster_arrive();
     const int len = p.seq_lens[s], T = p.cache.block_tokens;
     int code = 0;
-    if (len < 0 || len > (int64_t)p.max_blocks * T) return reports && threadIdx.x == 0 ? (report(p.status, AMOEBA_ERR_INVALID_ARG), -1) : -1;
-    const int keep = min(len, p.budget), n_src = (len + T - 1) / T, n_dst = (keep + T - 1) / T;
-    if (n_dst > p.dst_max_blocks) return reports && threadIdx.x == 0 ? (report(p.status, AMOEBA_ERR_INVALID_ARG), -1) : -1;
+    bool fits = len >= 0 && len <= (int64_t)p.max_blocks * T;
+    if (fits) {
+        const int keep = min(len, p.budget), n_src = (len + T - 1) / T, n_dst = (keep + T - 1) / T;
+        fits = n_dst <= p.dst_max_blocks;
+        if (fits) {
 #pragma unroll 4
-    for (int i = rank * blockDim.x + threadIdx.x; i < n_src; i += blockDim.x * size) {
-        const int b = p.src_bt[(int64_t)s * p.max_blocks + i];
-        if (b < 0 || b >= p.cache.num_blocks) code = 1;
+            for (int i = rank * blockDim.x + threadIdx.x; i < n_src; i += blockDim.x * size) {
+                const int b = p.src_bt[(int64_t)s * p.max_blocks + i];
+                if (b < 0 || b >= p.cache.num_blocks) code = 1;
+            }
+#pragma unroll 4
+            for (int i = rank * blockDim.x + threadIdx.x; i < n_dst; i += blockDim.x * size) {
+                const int b = p.dst_bt[(int64_t)s * p.dst_max_blocks + i];
+                if (b < 0 || b >= p.cache.num_blocks) code = 1;
+            }
+        }
     }
-#pragma unroll 4
-    for (int i = rank * blockDim.x + threadIdx.x; i < n_dst; i += blockDim.x * size) {
-        const int b = p.dst_bt[(int64_t)s * p.dst_max_blocks + i];
-        if (b < 0 || b >= p.cache.num_blocks) code = 1;
+    if (size > 1) cluster_wait();
+    if (!fits) {  // all threads of the cluster alike
+        if (reports && threadIdx.x == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
+        return -1;
     }
     code = __syncthreads_or(code);
     if (size > 1) {
