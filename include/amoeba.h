@@ -469,8 +469,8 @@ AMOEBA_API amoeba_status amoeba_plan_weight_alias(const amoeba_plan* plan, int32
  * not written.  The token at cache index i of sequence s is in slot i % block_tokens of block
  * d_block_table[s][i / block_tokens]; table entries past a sequence's last block are not read.
  *
- * Device-detected errors.  INVALID_ARG, and nothing of the sequence is done: a negative length or one that needs more
- * than max_blocks_per_seq blocks, row numbers that decrease or leave [0, num_rows], more than max_q_len rows.
+ * Device-detected errors.  INVALID_ARG, and nothing of the sequence is done: a negative length, one above 2^30 or one that
+ * needs more than max_blocks_per_seq blocks, row numbers that decrease or leave [0, num_rows], more than max_q_len rows.
  * BAD_BLOCK_ID, and only the tokens of that block are left out: a block id outside the pool.
  */
 enum { AMOEBA_FP16 = 0, AMOEBA_BF16 = 1 }; /* element type */

@@ -33,6 +33,9 @@ struct Batch {
     int32_t num_seqs, max_blocks, num_rows, max_q_len;
 };
 
+// Cached tokens of a sequence at most: their indices, rounded up to tiles and blocks or moved by a window, stay below 2^31.
+constexpr int32_t kMaxTokens = 1 << 30;
+
 // One sequence of the batch: its rows q0 .. q0+qn-1 are the tokens at cache indices len-qn .. len-1.
 struct Seq {
     int32_t q0, qn, len;
@@ -51,7 +54,7 @@ __device__ __forceinline__ Seq sequence(const Batch& b, int s, int block_tokens)
     }
     q.len = b.lens[s];
     q.ok = q.q0 >= 0 && q1 >= q.q0 && q1 <= b.num_rows && q1 - q.q0 <= b.max_q_len && q.len >= 0 &&
-           q.len <= (int64_t)b.max_blocks * block_tokens;
+           q.len <= min((int64_t)b.max_blocks * block_tokens, (int64_t)kMaxTokens);
     q.qn = q.ok ? q1 - q.q0 : 0;
     return q;
 }
@@ -101,6 +104,7 @@ inline amoeba_status make_cache_view(const amoeba_layout* l, int32_t layer, cons
     if (st != AMOEBA_OK) return st;
     const amoeba_model& m = l->model;
     if (layer < 0 || layer >= m.num_layers) return AMOEBA_ERR_INVALID_ARG;
+    if (l->block_tokens > kMaxTokens) return AMOEBA_ERR_UNSUPPORTED;
     const int64_t vec = (int64_t)m.head_dim * m.elem_bytes;
     const int64_t layer_stride = bytes / m.num_layers;
     if (vec % 16 || layer_stride % 16) return AMOEBA_ERR_ALIGNMENT;

@@ -68,7 +68,7 @@ __device__ __forceinline__ int checked_len(const EvictParams& p, int s, bool rep
     if (size > 1) cluster_arrive();
     const int len = p.seq_lens[s], T = p.cache.block_tokens;
     int code = 0;
-    bool fits = len >= 0 && len <= (int64_t)p.max_blocks * T;
+    bool fits = len >= 0 && len <= min((int64_t)p.max_blocks * T, (int64_t)kMaxTokens);
     if (fits) {
         const int keep = min(len, p.budget), n_src = (len + T - 1) / T, n_dst = (keep + T - 1) / T;
         fits = n_dst <= p.dst_max_blocks;

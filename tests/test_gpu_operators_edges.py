@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import cache_reference as ref
-from test_gpu_operators import A, DEV, model
+from test_gpu_operators import A, DEV, Case, model
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,46 @@ def test_evict_refuses_one_by_one_across_a_cluster(room):
             want[0, b[j // T], h, :, j % T] = pool[0, b[f // T], h, :, f % T]
             ws[0, b[j // T], h, j % T] = scores[0, b[f // T], h, f % T]
     assert torch.equal(dpool.cpu(), want) and torch.equal(dscores.cpu(), ws)
+
+
+# ------------------------------------------------------------------------------------------------------ lengths past 2^30
+
+@pytest.mark.parametrize("length", [2 ** 30 + 1, 2 ** 31 - 100, 2 ** 31 - 1])
+def test_lengths_past_2_to_the_30_are_refused(length):
+    """A table that would hold them, of blocks of 65536 tokens: INVALID_ARG, nothing of that sequence is done, and the
+    sequence beside it is."""
+    a = A()
+    T, width = 1 << 16, 1 << 15
+    c = Case(1, 1, 64, T=T, lens=[100], seed=70, spare=1)
+    c.bt = np.zeros((2, width), np.int32)
+    c.bt[0, 0] = 1
+    c.lens, c.qlens = np.array([100, 5], np.int32), np.array([1, 1])
+    c.starts, c.rows = np.array([0, 1, 2], np.int32), 2
+    c.q = torch.cat([c.q, c.q])
+    c.up()
+    c.dlens.copy_(torch.tensor([100, length], dtype=torch.int32))
+
+    def refused():
+        torch.cuda.synchronize()
+        code, _ = int(c.status.item()), c.status.zero_()
+        return code == a.ERR_INVALID_ARG
+
+    for maxq in (1, 40):  # the kernels for few rows, and for many beside them
+        c.batch = a.make_batch(c.dbt, c.dlens, c.dstarts, 2, maxq)
+        c.ws = torch.full((a.amoeba_attend_workspace_bytes(c.layout, c.batch),), 0x7F, dtype=torch.uint8, device=DEV)
+        c.out[0].fill_(7.0)
+        c.attend()
+        assert refused() and (c.out[0][1] == 7).all() and (c.out[0][0] != 7).any()
+        scores = torch.full((1, c.NB, 1, T), 3.0, device=DEV)
+        a.amoeba_accumulate_scores(c.layout, 1, 0, c.dpools, c.batch, c.dq, c.scale, 0, c.lse, None, [scores], c.status)
+        assert refused() and (scores[0, 0] == 3).all() and (scores[0, 1, 0, :100] != 3).all() and (scores[0, 1, 0, 100:] == 3).all()
+        pool, q_out = c.dpools[0].clone(), torch.full_like(c.dq[0], 7.0)
+        a.amoeba_append_kv(c.layout, 1, 0, [pool], c.batch, c.dq, c.dq, c.dq, None, [q_out], c.status)
+        assert refused() and torch.equal(pool[0, 0], c.dpools[0][0, 0]) and (q_out[1] == 7).all()
+        assert torch.equal(pool[0, 1, 0, 0, 99], c.dq[0][0]) and torch.equal(q_out[0], c.dq[0][0])
+    pool, scores, new = c.dpools[0].clone(), torch.rand(1, c.NB, 1, T, device=DEV), torch.full((2,), 99, dtype=torch.int32, device=DEV)
+    before = scores.clone()
+    ws = torch.empty(a.amoeba_evict_workspace_bytes(c.layout, 1, 2, 40), dtype=torch.uint8, device=DEV)
+    a.amoeba_evict_kv(c.layout, 0, 1, [pool], [scores], c.dbt, c.dlens, c.dbt, 40, 8, new, c.status, ws)
+    assert refused() and new.tolist() == [40, -1]
+    assert torch.equal(pool[0, 0], c.dpools[0][0, 0]) and torch.equal(scores[0, 0], before[0, 0])

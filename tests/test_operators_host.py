@@ -185,3 +185,9 @@ def test_reference_on_a_case_worked_by_hand():
     assert ref.kept([np.nan, -np.inf, 1.0], 3, 2, 0).tolist() == [1, 2]
     y, _ = ref.turned(np.array([[[1.0, 0.0]]]), None, 0, np.array([np.pi / 2]), np.array([1]), 2, False)
     assert np.allclose(y, [[[0.0, 1.0]]])
+
+
+@pytest.mark.parametrize("name", ROWS + ["evict"])
+def test_blocks_longer_than_any_sequence_are_refused(name):
+    layout = A.make_layout(dict(M, D=64), 2, 1, (1 << 30) + 16)
+    assert call(name, layout=layout) == UNS
