@@ -2,7 +2,8 @@
 // and devices of the tensors are checked and the C functions called, in well under a microsecond.  A CPython module; the
 // C library itself knows nothing of torch.
 //
-// Every function returns the C status, or a text that says which tensor does not fit.
+// Every function returns the C status, or a text that says which tensor does not fit.  Tensors on the host are checked like those
+// on a GPU, and refused last.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/core/Tensor.h>
@@ -36,7 +37,8 @@ const at::Tensor& tensor(PyObject* o) {
     if (!THPVariable_Check(o)) throw Refused{"a tensor is needed"};
     return THPVariable_Unpack(o);
 }
-bool on(const at::Tensor& t, int64_t device) { return t.is_cuda() && t.device().index() == device; }
+// device: of a GPU, or -1 for the host.
+bool on(const at::Tensor& t, int64_t device) { return device < 0 ? t.is_cpu() : t.is_cuda() && t.device().index() == device; }
 
 // Address of a dense tensor with at least n elements.
 void* dense(PyObject* o, at::ScalarType type, int64_t n, int64_t device, const char* why) {
@@ -104,16 +106,15 @@ const amoeba_layout& layout_of(PyObject* o) {
     if (!l || l->tp < 1 || l->tp > AMOEBA_MAX_TP) throw Refused{"the layout's tp"};
     return *l;
 }
-int64_t cuda_device(PyObject* o) {
-    const int64_t d = whole(o);
-    if (d < 0) throw Refused{"the tensors are not on a GPU"};
-    return d;
-}
 // The stream to launch on, with its device current while the object lives.
 struct On {
     c10::cuda::CUDAGuard guard;
     void* stream;
-    On(int64_t device, PyObject* given) : guard((c10::DeviceIndex)device) {
+    static c10::DeviceIndex gpu(int64_t device) {
+        if (device < 0) throw Refused{"the tensors are not on a GPU"};
+        return (c10::DeviceIndex)device;
+    }
+    On(int64_t device, PyObject* given) : guard(gpu(device)) {
         stream = given == Py_None ? (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream() : PyLong_AsVoidPtr(given);
     }
 };
@@ -141,7 +142,7 @@ PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const amoeba_layout& l = layout_of(a[0]);
         const int32_t dtype = whole32(a[1]), layer = whole32(a[2]);
         const amoeba_batch* b = at_address<amoeba_batch>(a[4]);
-        const int64_t dev = cuda_device(a[5]), D = l.model.head_dim;
+        const int64_t dev = whole(a[5]), D = l.model.head_dim;
         const at::ScalarType type = element(dtype);
         Pointers pool, q, k, v, out;
         pools(a[3], l, layer_bytes(l) * (layer + 1), false, dev, &pool);
@@ -163,7 +164,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const amoeba_layout& l = layout_of(a[0]);
         const int32_t dtype = whole32(a[1]), layer = whole32(a[2]);
         const amoeba_batch* b = at_address<amoeba_batch>(a[4]);
-        const int64_t dev = cuda_device(a[5]), width = (int64_t)l.model.num_q_heads / l.tp * l.model.head_dim;
+        const int64_t dev = whole(a[5]), width = (int64_t)l.model.num_q_heads / l.tp * l.model.head_dim;
         const at::ScalarType type = element(dtype);
         Pointers pool, q, out;
         pools(a[3], l, layer_bytes(l) * (layer + 1), false, dev, &pool);
@@ -187,7 +188,7 @@ PyObject* accumulate_scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const amoeba_layout& l = layout_of(a[0]);
         const int32_t dtype = whole32(a[1]), layer = whole32(a[2]);
         const amoeba_batch* b = at_address<amoeba_batch>(a[4]);
-        const int64_t dev = cuda_device(a[5]);
+        const int64_t dev = whole(a[5]);
         const at::ScalarType type = element(dtype);
         Pointers pool, q, scores;
         pools(a[3], l, layer_bytes(l) * (layer + 1), false, dev, &pool);
@@ -210,8 +211,7 @@ PyObject* evict_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const amoeba_layout& l = layout_of(a[0]);
         const int32_t l0 = whole32(a[1]), l1 = whole32(a[2]);
         const at::Tensor &lens = tensor(a[6]), &src = tensor(a[5]), &dst = tensor(a[7]);
-        if (!lens.is_cuda()) throw Refused{"the tensors are not on a GPU"};
-        const int64_t dev = lens.device().index(), S = lens.numel();
+        const int64_t dev = lens.is_cuda() ? lens.device().index() : -1, S = lens.numel();
         if (src.dim() != 2 || dst.dim() != 2 || src.size(0) != S || dst.size(0) != S) throw Refused{"block tables are [num_seqs, blocks]"};
         if (S > INT32_MAX || src.size(1) > INT32_MAX || dst.size(1) > INT32_MAX) throw Refused{"too many sequences or blocks"};
         Pointers pool, scores;

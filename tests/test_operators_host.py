@@ -191,3 +191,97 @@ def test_reference_on_a_case_worked_by_hand():
 def test_blocks_longer_than_any_sequence_are_refused(name):
     layout = A.make_layout(dict(M, D=64), 2, 1, (1 << 30) + 16)
     assert call(name, layout=layout) == UNS
+
+
+# ---- the Python calls' own checks, each refused for its own reason.  Tensors on the host are checked like those on a GPU and
+# refused last, so that none of this needs one.
+
+class Calls:
+    """The four Python calls with host tensors that are in order but for their device, and arguments in their place."""
+
+    def __init__(self):
+        i32, f16 = dict(dtype=torch.int32), dict(dtype=torch.float16)
+        self.layout = A.make_layout(M, 2, 10)
+        self.pools = [torch.zeros(2, 10, 2, 2, 16, 64, **f16) for _ in range(2)]
+        self.scores = [torch.zeros(2, 10, 2, 16) for _ in range(2)]
+        self.bt, self.lens = torch.zeros(3, 4, **i32), torch.zeros(3, **i32)
+        self.batch = A.make_batch(self.bt, self.lens)
+        self.wide = [torch.zeros(3, 256, **f16) for _ in range(2)]  # rows of 4 query heads of 64
+        self.slim = [torch.zeros(3, 128, **f16) for _ in range(2)]  # of 2 key heads
+        self.status, self.ws = torch.zeros(1, **i32), torch.zeros(1 << 26, dtype=torch.uint8)
+        self.lse = torch.zeros(3, 8)
+
+    def __call__(self, name, **kw):
+        g = lambda k, d: kw.get(k, d)  # noqa: E731
+        pools, q, st = g("pools", self.pools), g("q", self.wide), g("status", self.status)
+        dtype, layer, batch = g("dtype", A.DTYPE_FP16), g("layer", 0), g("batch", self.batch)
+        out, scores, scale, stream = g("out", [x.clone() for x in self.wide]), g("scores", self.scores), g("scale", 1.0), g("stream", None)
+        if name == "append":
+            A.amoeba_append_kv(self.layout, dtype, layer, pools, batch, q, g("k", self.slim), g("v", self.slim), g("rotation", None),
+                               out, st, stream)
+        elif name == "attend":
+            A.amoeba_attend(self.layout, dtype, layer, pools, batch, q, scale, g("window", 0), out, g("lse", self.lse), st,
+                            g("ws", self.ws), stream)
+        elif name == "scores":
+            A.amoeba_accumulate_scores(self.layout, dtype, layer, pools, batch, q, scale, g("window", 0), g("lse", self.lse),
+                                       g("scored", None), scores, st, stream)
+        else:
+            A.amoeba_evict_kv(self.layout, g("l0", 0), g("l1", 2), pools, scores, g("src", self.bt), g("lens", self.lens),
+                              g("dst", self.bt), g("budget", 10), 2, g("new", self.lens.clone()), st, g("ws", self.ws), stream)
+
+
+ALL = ROWS + ["evict"]
+POOL, ROW, LSE = "a pool is on another device, strided or too small", "row buffers are", "lse is float32"
+
+
+@pytest.mark.parametrize("name", ALL)
+def test_calls_in_order_are_refused_for_the_device_alone(name):
+    with pytest.raises(A.AmoebaError, match="not on a GPU"):
+        Calls()(name)
+
+
+@pytest.mark.parametrize("names,bad,why", [
+    (ALL, lambda c: dict(pools=c.pools[:1]), "pool count != tp"),
+    (ALL, lambda c: dict(pools=c.pools[0]), "as a list or tuple"),
+    (ALL, lambda c: dict(pools=[None, None]), "a tensor is needed"),
+    (ALL, lambda c: dict(pools=[p[:, :9] for p in c.pools]), POOL),
+    (ALL, lambda c: dict(pools=[p.transpose(3, 4) for p in c.pools]), POOL),
+    (ALL, lambda c: dict(pools=[p.to("meta") for p in c.pools]), POOL),
+    (ROWS, lambda c: dict(pools=[p[:1] for p in c.pools], layer=1), POOL),
+    (["evict"], lambda c: dict(pools=[p[:1] for p in c.pools]), POOL),
+    (ROWS, lambda c: dict(dtype=2), "dtype is"),
+    (ROWS, lambda c: dict(layer=1 << 40), "does not fit 32 bits"),
+    (ROWS, lambda c: dict(q=c.wide[:1]), "row buffer count != tp"),
+    (ROWS, lambda c: dict(q=[x[:2] for x in c.wide]), ROW),
+    (ROWS, lambda c: dict(q=c.slim), ROW),
+    (ROWS, lambda c: dict(q=[x.float() for x in c.wide]), ROW),
+    (ROWS, lambda c: dict(q=[x.t().contiguous().t() for x in c.wide]), ROW),
+    (ROWS, lambda c: dict(q=[x.view(3, 4, 64).transpose(1, 2).reshape(3, 4, 64).transpose(1, 2) for x in c.wide]), ROW),
+    (ROWS, lambda c: dict(q=[torch.zeros(3, 8, 64, dtype=torch.float16)[:, ::2] for _ in c.wide]), ROW),
+    (ROWS, lambda c: dict(q=[c.wide[0], torch.zeros(3, 512, dtype=torch.float16)[:, :256]]), ROW),
+    (ROWS, lambda c: dict(q=[x.flatten() for x in c.wide]), ROW),
+    (["append"], lambda c: dict(k=c.wide), ROW), (["append"], lambda c: dict(v=[x[:2] for x in c.slim]), ROW),
+    (["append", "attend"], lambda c: dict(out=c.slim), ROW),
+    (["attend", "scores"], lambda c: dict(lse=torch.zeros(3, 7)), LSE),
+    (["attend", "scores"], lambda c: dict(lse=torch.zeros(3, 8, dtype=torch.float64)), LSE),
+    (["attend", "scores"], lambda c: dict(lse=torch.zeros(8, 3).t()), LSE),
+    (["attend", "scores"], lambda c: dict(window=1 << 31), "does not fit 32 bits"),
+    (["scores"], lambda c: dict(scored=torch.zeros(2, dtype=torch.int32)), "scored_lens is int32"),
+    (["scores"], lambda c: dict(scored=torch.zeros(3, dtype=torch.int64)), "scored_lens is int32"),
+    (["scores", "evict"], lambda c: dict(scores=[x.double() for x in c.scores]), "score pools are float32"),
+    (["scores", "evict"], lambda c: dict(scores=[x[:, :9] for x in c.scores]), POOL),
+    (["scores", "evict"], lambda c: dict(scores=c.scores[:1]), "score pool count != tp"),
+    (["scores"], lambda c: dict(scores=None), "as a list or tuple"),
+    (["evict"], lambda c: dict(src=c.bt[:2]), "block tables are"), (["evict"], lambda c: dict(dst=c.bt.long()), "block tables are int32"),
+    (["evict"], lambda c: dict(src=c.bt.t().contiguous().t()), "block tables are int32"),
+    (["evict"], lambda c: dict(dst=c.bt[0]), "block tables are"),
+    (["evict"], lambda c: dict(new=c.lens[:2]), "lengths are int32"), (["evict"], lambda c: dict(new=c.lens.long()), "lengths are int32"),
+    (["evict"], lambda c: dict(lens=c.lens.long()), "lengths are int32"),
+    (ALL, lambda c: dict(status=torch.zeros(1)), "status is int32"), (ALL, lambda c: dict(status=c.status[:0]), "status is int32"),
+    (["attend", "evict"], lambda c: dict(ws=c.ws.view(torch.int32)), "the workspace is uint8"),
+])
+def test_calls_say_which_tensor_does_not_fit(names, bad, why):
+    c = Calls()
+    for name in names:
+        with pytest.raises(A.AmoebaError, match=why):
+            c(name, **bad(c))
