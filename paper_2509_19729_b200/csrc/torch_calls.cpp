@@ -68,12 +68,14 @@ void pools(PyObject* list, const amoeba_layout& l, int64_t bytes, bool scores, i
         out->p[r] = t.data_ptr();
     }
 }
-// [>= rows, width] or [>= rows, heads, head_dim] row buffers, dense along a row, equally strided.
+// [>= rows, width] or [>= rows, heads, head_dim] row buffers, dense along a row, equally strided; rows may not overlap (a
+// broadcast row has stride 0, which means dense rows to the C call).  A tensor of one row fits beside any stride.
 void rows(PyObject* list, const amoeba_layout& l, int64_t n_rows, int64_t width, at::ScalarType type, int64_t device, Pointers* out) {
     static const char* why =
         "row buffers are [>= num_rows, heads of the worker * head_dim] of the element type, on the batch's device, dense along a "
-        "row and equally strided";
+        "row, equally strided and without rows that overlap";
     PyObject** items = workers(list, l.tp, "row buffer count != tp");
+    out->stride = 0;
     for (int r = 0; r < l.tp; ++r) {
         const at::Tensor& t = tensor(items[r]);
         const int64_t dim = t.dim();
@@ -81,9 +83,10 @@ void rows(PyObject* list, const amoeba_layout& l, int64_t n_rows, int64_t width,
             throw Refused{why};
         if (dim == 3 ? t.size(1) * t.size(2) != width || (t.size(1) > 1 && t.stride(1) != t.size(2)) : t.size(1) != width)
             throw Refused{why};
-        const int64_t stride = t.size(0) > 1 ? t.stride(0) : width;
-        if (r && stride != out->stride) throw Refused{why};
-        out->stride = stride;
+        if (t.size(0) > 1) {
+            if (t.stride(0) < width || (out->stride && t.stride(0) != out->stride)) throw Refused{why};
+            out->stride = t.stride(0);
+        }
         out->p[r] = t.data_ptr();
     }
 }

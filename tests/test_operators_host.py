@@ -285,3 +285,30 @@ def test_calls_say_which_tensor_does_not_fit(names, bad, why):
     for name in names:
         with pytest.raises(A.AmoebaError, match=why):
             c(name, **bad(c))
+
+
+@pytest.mark.parametrize("name", ROWS)
+def test_rows_that_share_storage_are_refused(name):
+    """A broadcast row, or rows that overlap: the kernels would read and write behind the storage, or on other rows."""
+    c = Calls()
+    one = torch.zeros(1, 256, dtype=torch.float16)
+    flat = torch.zeros(4096, dtype=torch.float16)
+    for q in (one.expand(3, 256), flat.as_strided((3, 256), (128, 1)), one.view(1, 4, 64).expand(3, 4, 64)):
+        with pytest.raises(A.AmoebaError, match=ROW):
+            c(name, q=[q, q])
+        if name != "scores":
+            with pytest.raises(A.AmoebaError, match=ROW):
+                c(name, out=[q, q])
+    if name == "append":
+        with pytest.raises(A.AmoebaError, match=ROW):
+            c(name, v=[one[:, :128].expand(3, 128)] * 2)
+
+
+def test_a_tensor_of_one_row_fits_beside_any_stride():
+    """Its row stride says nothing: one worker's row may be a tensor of its own, another's part of a wider one."""
+    c = Calls()
+    c.batch = A.make_batch(c.bt[:1], c.lens[:1])
+    alone, part = torch.zeros(1, 256, dtype=torch.float16), torch.zeros(3, 512, dtype=torch.float16)[:, :256]
+    for q in ([alone, part], [part, alone], [alone, part[:1]], [alone, alone]):
+        with pytest.raises(A.AmoebaError, match="not on a GPU"):
+            c("attend", q=q)
