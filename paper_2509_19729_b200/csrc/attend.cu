@@ -429,6 +429,9 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     if (p.batch.num_seqs == 0 || p.batch.num_rows == 0 || p.batch.max_q_len == 0) return AMOEBA_OK;
     p.lse = d_lse;
     p.status = d_status;
+#ifdef AMOEBA_CHECK_ITEMS
+    p.polls = operator_wait_polls();
+#endif
     p.scale_log2 = scale * kLog2e;
     p.q_heads = m.num_q_heads;
     p.shape.group = m.num_q_heads / m.num_kv_heads;

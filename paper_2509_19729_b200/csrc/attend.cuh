@@ -16,6 +16,9 @@ struct AttendParams {
     float scale_log2;        // scale * log2(e): the softmax runs in powers of two
     int32_t q_heads;         // of all workers
     int32_t whole;           // 1: one CTA per unit, nothing is cut
+#ifdef AMOEBA_CHECK_ITEMS
+    int32_t polls;           // of every wait in attend_many
+#endif
 };
 
 // Where row r of a unit lies in a row buffer.

@@ -237,22 +237,21 @@ struct Loader : TileLoader<D, kLoadWarps> {
     const AttendParams& p;
     const uint32_t smem;  // two query tiles, then the ring
     ManyBarriers& b;
-    int slot = 0;
-    uint32_t phase = 1;  // of `empty`: the first round waits for nothing
+    RingPlace at;
     static constexpr int kTile = ManyShape<D>::kTileBytes;
 
     __device__ __forceinline__ Loader(const AttendParams& p_, const CacheMaps& maps, int box_rows, uint32_t smem_, ManyBarriers& b_, int warp,
                                       int lane)
         : Base(p_.cache, maps, box_rows, warp, lane), p(p_), smem(smem_), b(b_) {}
     // Starts the loads of the tile's keys (kv = 0) or values (1).
-    __device__ __forceinline__ bool tile(const Range& range, int key0, const typename Base::Group& at, int kv) {
-        if (!__all_sync(~0u, mbar_wait_bounded(&b.empty[slot], phase, 0, &b.abort))) return false;
-        Base::tokens(range.lo, range.hi, key0, at, kv, smem + (2 + slot) * kTile, &b.full[slot]);
-        if (++slot == ManyShape<D>::kStages) slot = 0, phase ^= 1;
+    __device__ __forceinline__ bool tile(const Range& range, int key0, const typename Base::Group& group, int kv) {
+        if (!__all_sync(~0u, mbar_wait_bounded(&b.empty[at.slot], at.phase, polls(p), &b.abort))) return false;
+        Base::tokens(range.lo, range.hi, key0, group, kv, smem + (2 + at.slot) * kTile, &b.full[at.slot]);
+        if (++at.slot == ManyShape<D>::kStages) at.slot = 0, at.phase ^= 1;
         return true;
     }
     __device__ __forceinline__ bool queries(const Parts& part, uint32_t q_phase) {
-        if (!__all_sync(~0u, mbar_wait_bounded(&b.q_empty, q_phase, 0, &b.abort))) return false;
+        if (!__all_sync(~0u, mbar_wait_bounded(&b.q_empty, q_phase, polls(p), &b.abort))) return false;
         for (int t = 0; t < part.q_tiles; ++t)
             Base::queries(p.q, part.w, p.shape.group, part.w.m * kManyRows + t * 128, min(128, part.rows - t * 128), smem + t * kTile);
         arrive_when_loaded(&b.q_full);
@@ -261,7 +260,7 @@ struct Loader : TileLoader<D, kLoadWarps> {
 };
 
 template <int D>
-__device__ void load_loop(const AttendParams& p, const CacheMaps& maps, int box_rows, const Share& share, char* smem, ManyBarriers& b) {
+__device__ RingPlace load_loop(const AttendParams& p, const CacheMaps& maps, int box_rows, const Share& share, char* smem, ManyBarriers& b) {
     Loader<D> load(p, maps, box_rows, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32);
     uint32_t q_phase = 1;
     bool ok = true;
@@ -283,6 +282,7 @@ __device__ void load_loop(const AttendParams& p, const CacheMaps& maps, int box_
     cp_async_commit();
     cp_async_wait<0>();
     if (!ok) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+    return load.at;
 }
 
 // ---- products: one warp, one of its lanes issues
@@ -293,7 +293,7 @@ __device__ bool multiply(const AttendParams& p, const Share& share, uint32_t sme
     const uint32_t tmem = __shfl_sync(~0u, b.tmem, 0), leader = elect_one();
     int slot = 0;  // of the next K; V is the one behind
     uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort)); };
     const uint64_t q_op = operand(smem, 16);
     auto logits = [&](int t, int k_slot) {
         const uint64_t k_op = operand(smem + (2 + __shfl_sync(~0u, k_slot, 0)) * kTile, 16);
@@ -453,8 +453,9 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
     const float c = p.scale_log2;
     uint32_t s_phase = 0, o_phase = 0;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-        return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort));  // and the warp is together again
+        return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort));  // and the warp is together again
     };
+    bool ok = true;  // a warp that gives up goes on to the barriers below, where the others of its warpgroup wait for it
     Parts part(share);
     while (part.next(p, share)) {
         const Walk& w = part.w;
@@ -468,7 +469,7 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
             "barrier.cta.red.or.pred q, %1, 128, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
             : "+r"(bad) : "r"(1 + t) : "memory");
         if (bad && threadIdx.x % 128 == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
-        if (t < part.q_tiles) {
+        if (ok && t < part.q_tiles) ok = [&] {
             const int row = w.m * kManyRows + r;
             const bool there = r < part.rows;
             const int pos = w.seq.len - w.seq.qn + row / sh.group;
@@ -544,9 +545,11 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
             if (there && !direct) p.part_m[at] = m_ref, p.part_l[at] = l;
             if (there && direct && p.lse)
                 *lse_of(p, w.seq, w.h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
-        }
+            return true;
+        }();
+        if (!ok) b.abort = 1;
     }
-    return true;
+    return ok;
 }
 
 template <class T, int D>
@@ -580,6 +583,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
+    RingPlace loaded;
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == 8) {
@@ -587,7 +591,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
             __syncwarp();
             drain_products(b);
         } else {
-            load_loop<D>(p, maps, box_rows, share, smem, b);
+            loaded = load_loop<D>(p, maps, box_rows, share, smem, b);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
@@ -600,6 +604,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
         tmem_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(b.tmem));
     }
+    if (warp > 8 && b.abort) drain_ring<ManyShape<D>::kStages>(b.full, loaded);
 }
 
 template <class T, int D>

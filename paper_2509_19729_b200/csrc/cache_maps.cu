@@ -2,7 +2,16 @@
 // link against the driver.
 #include "cache_maps.hpp"
 
+#include <atomic>
 #include <mutex>
+
+#ifdef AMOEBA_CHECK_ITEMS
+static std::atomic<int32_t> g_wait_polls{0};
+namespace amoeba {
+int32_t operator_wait_polls() { return g_wait_polls; }
+}  // namespace amoeba
+extern "C" AMOEBA_API void amoeba_checked_set_wait_polls(int32_t polls) { g_wait_polls = polls < 0 ? 0 : polls; }
+#endif
 
 namespace amoeba {
 

@@ -189,6 +189,10 @@ inline amoeba_status launch_kernel(void (*kernel)(P...), int grid, int threads, 
     return AMOEBA_OK;
 }
 
+#ifdef AMOEBA_CHECK_ITEMS
+int32_t operator_wait_polls();  // what a test has set (cache_maps.cu)
+#endif
+
 inline bool positive(float x) { return x > 0.f && x < INFINITY; }
 
 inline amoeba_status launch_result() {

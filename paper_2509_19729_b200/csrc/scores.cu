@@ -17,6 +17,9 @@ struct ScoreParams {
     int32_t* status;
     float scale_log2;
     int32_t q_heads, window;
+#ifdef AMOEBA_CHECK_ITEMS
+    int32_t polls;  // of every wait in score_many
+#endif
 };
 
 // ------------------------------------------------------------------------------------------------ few rows
@@ -247,32 +250,38 @@ __device__ void take_runs(const ScoreParams& p, Runs* r, int32_t* status) {
 }
 
 template <int D>
-__device__ bool score_load(const ScoreParams& p, const CacheMaps& maps, int box_rows, uint32_t smem, ScoreBarriers& b, Runs run) {
+__device__ bool score_load(const ScoreParams& p, const CacheMaps& maps, int box_rows, uint32_t smem, ScoreBarriers& b, Runs run,
+                           RingPlace* loaded) {
     using S = ScoreManyShape<D>;
     TileLoader<D, kScoreLoadWarps> load(p.cache, maps, box_rows, (int)(threadIdx.x - (kScoreManyThreads - 32 * kScoreLoadWarps)) / 32,
                                          threadIdx.x % 32);
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
-    int slot = 0, qb = 0;
-    uint32_t phase = 1, q_phase = 1;
-    while (run.next(p)) {
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort)); };
+    RingPlace ring;
+    int qb = 0;
+    uint32_t q_phase = 1;
+    bool ok = true;
+    while (ok && run.next(p)) {
         load.open(run.w, p.batch);
         const int len = run.w.seq.len;
-        for (int j = 0; j < run.passes; ++j) {
-            if (!wait(&b.q_empty[qb], q_phase)) return false;
+        for (int j = 0; ok && j < run.passes; ++j) {
+            if (!(ok = wait(&b.q_empty[qb], q_phase))) break;
             load.queries(p.q, run.w, p.shape.group, j * 128, min(128, run.rows - j * 128), smem + qb * S::kTileBytes);
             arrive_when_loaded(&b.q_full[qb]);
             if (qb ^= 1, qb == 0) q_phase ^= 1;
             auto at = load.groups(0, len, run.t0 * 128), next = load.groups(0, len, run.t0 * 128 + 128);
             for (int t = run.t0; t < run.t1; ++t) {
-                if (!wait(&b.k_empty[slot], phase)) return false;
-                load.tokens(0, len, t * 128, at, 0, smem + (2 + slot) * S::kTileBytes, &b.k_full[slot]);
-                if (++slot == S::kStages) slot = 0, phase ^= 1;
+                if (!(ok = wait(&b.k_empty[ring.slot], ring.phase))) break;
+                load.tokens(0, len, t * 128, at, 0, smem + (2 + ring.slot) * S::kTileBytes, &b.k_full[ring.slot]);
+                if (++ring.slot == S::kStages) ring.slot = 0, ring.phase ^= 1;
                 at = next;
                 if (t + 2 < run.t1) next = load.groups(0, len, (t + 2) * 128);
             }
         }
     }
-    return true;
+    cp_async_commit();
+    cp_async_wait<0>();
+    *loaded = ring;
+    return ok;
 }
 
 template <class T, int D>
@@ -280,7 +289,7 @@ __device__ bool score_multiply(const ScoreParams& p, uint32_t smem, ScoreBarrier
     using S = ScoreManyShape<D>;
     constexpr uint32_t kIdesc = product<T>(128, false);
     const uint32_t tmem = __shfl_sync(~0u, b.tmem, 0), leader = elect_one();
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort)); };
     int slot = 0, qb = 0;
     uint32_t phase = 0, q_phase = 0, free = (1u << kScoreGroups) - 1;  // bit g: parity to wait for at s_empty[g]
     while (run.next(p)) {
@@ -355,10 +364,11 @@ __device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[12
 __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, float (*s_row)[128], int32_t (*s_pos)[128]) {
     const int g = threadIdx.x / 128, tid = threadIdx.x % 128, G = p.shape.group, T = p.cache.block_tokens;
     const uint32_t lanes = (uint32_t)(tid / 32 * 32) << 16;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, 0, &b.abort)); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort)); };
     const float c = p.scale_log2;
     int pass = 0;
     uint32_t full = 0;  // parity to wait for at s_full[g]
+    bool ok = true;     // a warp that gives up goes on to the barriers below, where the others of its warpgroup wait for it
     while (run.next(p)) {
         const Seq& q = run.w.seq;
         const int w = run.w.h / p.cache.heads, hw = run.w.h - w * p.cache.heads;
@@ -382,7 +392,7 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
             // the block of the next tile's token is asked for a tile early
             int at = (run.t0 + g) * 128 + tid, i_block = at / T, in_block = at - i_block * T, block = -1;
             if (run.t0 + g < run.t1 && at < q.len) block = table[i_block];
-            for (int t = run.t0 + g; t < run.t1; t += kScoreGroups, full ^= 1) {
+            for (int t = run.t0 + g; ok && t < run.t1; t += kScoreGroups, full ^= 1) {
                 const int key0 = t * 128, key = key0 + tid;
                 float* to = nullptr;
                 float old = 0.f;
@@ -400,7 +410,10 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
                     block = table[i_block];
                 }
                 const bool cut = key0 + 127 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
-                if (!wait(&b.s_full[g], full)) return false;
+                if (!wait(&b.s_full[g], full)) {
+                    ok = false, b.abort = 1;
+                    break;
+                }
                 tmem_fence_after();
                 const uint32_t from = b.tmem + lanes + g * 128;
                 const float sum = cut ? column_sum<true>(from, s_row[pass], s_pos[pass], key, p.window, c, &b.s_empty[g])
@@ -409,7 +422,7 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
             }
         }
     }
-    return true;
+    return ok;
 }
 
 template <class T, int D>
@@ -445,6 +458,7 @@ __global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_
     __syncthreads();
     tmem_fence_after();
     bool ok;
+    RingPlace loaded;
     if (warp < 4 * kScoreGroups) {
         ok = score_sum(p, b, run, s_row[warp / 4], s_pos[warp / 4]);
     } else if (warp == 4 * kScoreGroups) {
@@ -453,9 +467,7 @@ __global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_
         umma_commit(elect_one(), &b.drain);
         mbar_drain(&b.drain, 0);
     } else {
-        ok = score_load<D>(p, maps, box_rows, smem_u32(smem), b, run);
-        cp_async_commit();
-        cp_async_wait<0>();
+        ok = score_load<D>(p, maps, box_rows, smem_u32(smem), b, run, &loaded);
     }
     if (!ok) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
     grid_dependency_wait();  // score_few in front is done when this kernel is
@@ -465,6 +477,7 @@ __global__ void __launch_bounds__(kScoreManyThreads, 1) score_many(const __grid_
         tmem_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(b.tmem));
     }
+    if (warp > 4 * kScoreGroups && b.abort) drain_ring<S::kStages>(b.k_full, loaded);
 }
 
 template <class T, int D, int NT>
@@ -519,6 +532,9 @@ extern "C" amoeba_status amoeba_accumulate_scores(const amoeba_layout* layout, i
     p.lse = d_lse;
     p.scored = d_scored_lens;
     p.status = d_status;
+#ifdef AMOEBA_CHECK_ITEMS
+    p.polls = operator_wait_polls();
+#endif
     p.scale_log2 = scale * kLog2e;
     p.q_heads = m.num_q_heads;
     p.shape.group = m.num_q_heads / m.num_kv_heads;

@@ -8,6 +8,17 @@
 
 namespace amoeba {
 
+// Polls of a wait before it gives up, for mbar_wait_bounded: 0, its own budget.  The checked build lets a test set fewer, so that the
+// give-up paths run.
+template <class P>
+__device__ __forceinline__ uint32_t polls(const P& p) {
+#ifdef AMOEBA_CHECK_ITEMS
+    return p.polls;
+#else
+    return 0;
+#endif
+}
+
 // ---- tensor memory and products
 __device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr) {
     asm volatile(
@@ -113,6 +124,19 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
         "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
             "r"(dst), "l"(map), "r"(dim), "r"(token), "r"(kv), "r"(head), "r"(block), "r"(smem_u32(bar))
         : "memory");
+}
+// Where a loading thread is in its ring of tiles: the next one, and the parity that it waits for at its `empty` (the first round
+// waits for nothing).
+struct RingPlace {
+    int slot = 0;
+    uint32_t phase = 1;
+};
+// After some warp has given up: waits until the boxes that this thread has started are there, as the block may not end before.
+// Bounded: a tile that not all warps got to never fills.
+template <int kStages>
+__device__ __forceinline__ void drain_ring(uint64_t* full, RingPlace at) {
+    for (int i = 0; i < kStages; ++i)  // (a tile that was never loaded counts as filled in the round before)
+        for (uint32_t n = 0; n < kDrainWaitTries && !mbar_test_wait(&full[i], i < at.slot ? at.phase ^ 1 : at.phase); ++n) __nanosleep(64);
 }
 // The tiles that kWarps warps load together: by boxes where all 128 tokens are wanted and the blocks have a box's shape, else
 // each lane 16 bytes at a time.

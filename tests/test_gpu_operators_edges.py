@@ -1,4 +1,8 @@
 """The serving operators at the edges of what their documentation allows, and what they refuse there."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -93,3 +97,16 @@ def test_lengths_past_2_to_the_30_are_refused(length):
     a.amoeba_evict_kv(c.layout, 0, 1, [pool], [scores], c.dbt, c.dlens, c.dbt, 40, 8, new, c.status, ws)
     assert refused() and new.tolist() == [40, -1]
     assert torch.equal(pool[0, 0], c.dpools[0][0, 0]) and torch.equal(scores[0, 0], before[0, 0])
+
+
+# ---------------------------------------------------------------------------------------------------------- waits that run out
+
+def test_waits_that_run_out_end_the_call_with_a_status():
+    """In the checked build, whose waits can be told to give up after a few polls (give_up_check.py)."""
+    import paper_2509_19729_b200.build as b
+
+    b.build(checked=True)
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, os.path.join(here, "give_up_check.py")], cwd=os.path.dirname(here), timeout=300,
+                       env=dict(os.environ, AMOEBA_BINDING_BUILD="checked", PYTHONPATH=os.path.dirname(here)), capture_output=True, text=True)
+    assert r.returncode == 0 and "gave up and came back" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
