@@ -111,6 +111,7 @@ attend_few(const __grid_constant__ AttendParams p) {
         cp_async_wait<F::kStages - 2>();
         __syncwarp();
         load();  // into the slot that the last round has read
+        __syncwarp();  // the matrix instructions want the warp together
         const uint32_t k_smem = ring + slot * F::kStage, v_smem = k_smem + 16 * D * 2;
         const uint32_t mask = s_mask[warp][slot];
         slot = slot + 1 == F::kStages ? 0 : slot + 1;

@@ -389,6 +389,7 @@ __device__ __noinline__ void hide(uint32_t s_tmem, int key0, int lo, int hi, con
 #pragma unroll
         for (int k = 0; k < 32; ++k)
             if (!(see & 1u << k)) s[k] = 0xff800000u;
+        __syncwarp();
         tmem_store32(s_tmem + j * 32, s);
     }
     tmem_store_wait();
@@ -522,6 +523,7 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 uint32_t o[32];
+                __syncwarp();  // (rows that are not there have parted from the others)
                 tmem_load32(o, o_tmem + j * 32);
                 tmem_load_wait();
                 if (!there) continue;

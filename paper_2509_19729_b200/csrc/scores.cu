@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
         const uint32_t k_smem = ring + slot * F::kStage, mask = s_mask[warp][slot];
         const int64_t first = s_slot[warp][slot];
         load();  // into the slot that the last round has read
+        __syncwarp();  // the matrix instructions want the warp together
         slot = slot + 1 == F::kStages ? 0 : slot + 1;
         const int key0 = walk.t * kScoreTile + warp * 16 + quad;
         float sum[2] = {0.f, 0.f};
@@ -330,6 +331,7 @@ __device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[12
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t s[32];
+        if (kCut) __syncwarp();
         tmem_load32(s, from + i * 32);
         tmem_load_wait();
         if (i == 3) {
