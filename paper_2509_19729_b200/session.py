@@ -5,6 +5,7 @@ tables, and issues the three C-ABI calls of one transformation in order.  No re-
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Optional
 
 import torch
@@ -338,13 +339,23 @@ class MergeCopySession:
         return kv * self.kv_layers // self.L
 
 
+def _on(stream, device):
+    """Makes `stream` (a torch stream, its handle, or None) the current one of the device."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
 class CacheSession:
     """The paged cache of one serving instance and the operators on it: new tokens in, attention over it, the attention
     weight its tokens received, and long sequences cut to a budget.
 
     dtype: "fp16" or "bf16"; kv_layers: layers the pools hold (None = all); scores: hold score pools too.  set_tables()
     and set_rows() describe the batch of a step; the row buffers q, k, v, out are the caller's, one tensor per worker.
-    All calls share one workspace, so they run one after another, on one stream or on streams that wait for each other."""
+    All calls share one workspace, so they run one after another, on one stream or on streams that wait for each other;
+    set_tables() and set_rows() work on the current stream."""
 
     def __init__(self, model: dict, tp: int, NB: int, num_seqs: int, max_blocks_per_seq: int, dtype: str = "bf16",
                  kv_layers: Optional[int] = None, block_tokens: int = 16, kv_order: int = A.KV_HEAD_MAJOR,
@@ -379,11 +390,13 @@ class CacheSession:
                                   max_q_len)
         self._room(A.amoeba_attend_workspace_bytes(self.layout, self.batch))
 
-    def _room(self, nbytes: int) -> None:
+    def _room(self, nbytes: int, stream=None) -> None:
+        """A workspace of nbytes, for calls on `stream` (None: the current one) and on what waits for it."""
         if self.workspace.numel() < nbytes:
             # Calls on any stream, or captured ones, may still use the old one; doubling bounds what they keep.
             self._outgrown.append(self.workspace)
-            self.workspace = torch.empty(max(nbytes, 2 * self.workspace.numel()), dtype=torch.uint8, device=self.device)
+            with _on(stream, self.device):  # what the allocator hands out may still be in use on the stream that freed it
+                self.workspace = torch.empty(max(nbytes, 2 * self.workspace.numel()), dtype=torch.uint8, device=self.device)
 
     def append(self, layer: int, q, k, v, rotation, q_out, stream=None) -> None:
         A.amoeba_append_kv(self.layout, self.dtype, layer, self.pools, self.batch, q, k, v, rotation, q_out, self.status,
@@ -405,7 +418,7 @@ class CacheSession:
         """Cuts the sequences to `budget` tokens; new_lens has their lengths.  dst_table: free blocks to move to (None: in
         place)."""
         layer_end = self.kv_layers if layer_end is None else layer_end
-        self._room(A.amoeba_evict_workspace_bytes(self.layout, layer_end - layer_begin, self.seq_lens.numel(), budget))
+        self._room(A.amoeba_evict_workspace_bytes(self.layout, layer_end - layer_begin, self.seq_lens.numel(), budget), stream)
         A.amoeba_evict_kv(self.layout, layer_begin, layer_end, self.pools, self.score_pools, self.block_table,
                           self.seq_lens, self.block_table if dst_table is None else dst_table, budget, recent,
                           self.new_lens, self.status, self.workspace, stream)

@@ -110,3 +110,42 @@ def test_waits_that_run_out_end_the_call_with_a_status():
     r = subprocess.run([sys.executable, os.path.join(here, "give_up_check.py")], cwd=os.path.dirname(here), timeout=300,
                        env=dict(os.environ, AMOEBA_BINDING_BUILD="checked", PYTHONPATH=os.path.dirname(here)), capture_output=True, text=True)
     assert r.returncode == 0 and "gave up and came back" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
+
+
+# -------------------------------------------------------------------------------------------------------------------- sessions
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_a_workspace_is_taken_from_the_stream_that_uses_it(as_handle):
+    """An eviction on another stream, which has to grow the workspace, beside a kernel on the current stream that still writes
+    to memory freed there."""
+    from paper_2509_19729_b200.session import CacheSession
+
+    m, budget, recent = model(2, 2, 64), 100, 10
+    s = CacheSession(m, 1, 60, 3, 20, device=DEV)
+    g = torch.Generator().manual_seed(90)
+    pool = torch.randn(1, 60, 2, 2, 16, 64, generator=g).to(torch.bfloat16)
+    scores = torch.randn(1, 60, 2, 16, generator=g)
+    s.pools[0].copy_(pool.flatten().view(torch.uint8))
+    s.score_pools[0].copy_(scores)
+    lens, bt = [320, 120, 50], torch.arange(60, dtype=torch.int32).view(3, 20)
+    s.set_tables(lens, bt)
+    s.workspace = torch.empty(0, dtype=torch.uint8, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    freed = torch.empty(A().amoeba_evict_workspace_bytes(s.layout, 1, 3, budget), dtype=torch.uint8, device=DEV)
+    at = freed.data_ptr()
+    torch.cuda._sleep(200_000_000)
+    freed.fill_(0x7F)
+    del freed
+    s.evict(budget, recent, stream=side.cuda_stream if as_handle else side)
+    assert s.workspace.data_ptr() != at
+    torch.cuda.synchronize()
+    want, ws = pool.clone(), scores.clone()
+    for q, n in enumerate(lens[:2]):
+        i, j, b = torch.arange(n), torch.arange(budget), bt[q].long()
+        for h in range(2):
+            f = torch.from_numpy(ref.kept(scores[0, b[i // 16], h, i % 16].double().numpy(), n, budget, recent))
+            want[0, b[j // 16], h, :, j % 16] = pool[0, b[f // 16], h, :, f % 16]
+            ws[0, b[j // 16], h, j % 16] = scores[0, b[f // 16], h, f % 16]
+    assert s.new_lens.tolist() == [100, 100, 50] and int(s.status.item()) == 0
+    assert torch.equal(s.pools[0].cpu(), want.flatten().view(torch.uint8)) and torch.equal(s.score_pools[0].cpu(), ws)
