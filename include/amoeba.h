@@ -472,6 +472,8 @@ AMOEBA_API amoeba_status amoeba_plan_weight_alias(const amoeba_plan* plan, int32
  * Device-detected errors.  INVALID_ARG, and nothing of the sequence is done: a negative length, one above 2^30 or one that
  * needs more than max_blocks_per_seq blocks, row numbers that decrease or leave [0, num_rows], more than max_q_len rows.
  * BAD_BLOCK_ID, and only the tokens of that block are left out: a block id outside the pool.
+ * Rows that several sequences name (some row number between theirs decreases): amoeba_append_kv gives them to the
+ * first of these, amoeba_attend the result of one of them.  With num_rows 0 these two look at nothing.
  */
 enum { AMOEBA_FP16 = 0, AMOEBA_BF16 = 1 }; /* element type */
 

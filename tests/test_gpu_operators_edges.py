@@ -149,3 +149,53 @@ def test_a_workspace_is_taken_from_the_stream_that_uses_it(as_handle):
             ws[0, b[j // 16], h, j % 16] = scores[0, b[f // 16], h, f % 16]
     assert s.new_lens.tolist() == [100, 100, 50] and int(s.status.item()) == 0
     assert torch.equal(s.pools[0].cpu(), want.flatten().view(torch.uint8)) and torch.equal(s.score_pools[0].cpu(), ws)
+
+
+# ---------------------------------------------------------------------------------------------------------------------- append
+
+def append_beside_bad(lens, starts, rows, maxq, left, S=3, T=16):
+    """Appends; sequences `left` must be left out, the others' tokens written; a row that two name is the first one's."""
+    a = A()
+    c = Case(2, 1, 64, T=T, lens=[40] * S, seed=91).up()
+    c.dlens.copy_(torch.tensor(lens, dtype=torch.int32))
+    c.dstarts.copy_(torch.tensor(starts, dtype=torch.int32))
+    c.batch = a.make_batch(c.dbt, c.dlens, c.dstarts, rows, maxq)
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn(rows, w, generator=g).to(torch.bfloat16).to(DEV) for w in (128, 64, 64))
+    out, want = torch.full_like(q, 7.0), torch.full_like(q, 7.0)
+    pool, host = c.dpools[0].clone(), c.dpools[0].clone()
+    a.amoeba_append_kv(c.layout, 1, 0, [pool], c.batch, [q], [k], [v], None, [out], c.status)
+    torch.cuda.synchronize()
+    owners = [[s for s in range(S) if starts[s] <= r < starts[s + 1]] for r in range(rows)]
+    for r, o in enumerate(owners):
+        if o and o[0] not in left:
+            s = o[0]
+            i = lens[s] - (starts[s + 1] - starts[s]) + r - starts[s]
+            b = int(c.bt[s, i // T])
+            host[0, b, 0, 0, i % T], host[0, b, 0, 1, i % T], want[r] = k[r], v[r], q[r]
+    assert torch.equal(pool, host) and torch.equal(out, want)
+    return int(c.status.item())
+
+
+@pytest.mark.parametrize("lens,starts,rows,maxq,left", [
+    ([40, 40, 40], [0, 1, 0, 1], 1, 1, [1]),          # a decreasing row number: no row is the second's, row 0 two others'
+    ([40, 40, 40], [0, 3, 1, 4], 4, 3, [1]),          # rows 1 and 2 are two sequences', 0 and 3 one's
+    ([40, 40, 40], [0, 2, 2, 4], 4, 1, [0, 2]),       # more rows than announced
+    ([40, -1, 40], [0, 1, 1, 3], 3, 2, [1]),          # bad lengths of sequences without rows
+    ([40, 49, 40], [0, 1, 1, 3], 3, 2, [1]),
+    ([40, 2 ** 31 - 1, 40], [0, 1, 1, 3], 3, 2, [1]),
+    ([40, 40, 40], [0, 1, 2, 9], 2, 9, [2]),          # rows that leave the buffers
+    ([40, 40, 40], [0, 1, 7, 9], 1, 9, [1, 2]),
+    ([40, 40, 40], [-3, 1, 2, 3], 3, 9, [0]),
+    ([40, 40, 1], [0, 1, 2, 4], 4, 2, [2]),           # more new tokens than cached ones
+])
+def test_append_reports_every_bad_sequence(lens, starts, rows, maxq, left):
+    assert append_beside_bad(lens, starts, rows, maxq, left) == A().ERR_INVALID_ARG
+
+
+def test_append_reports_the_last_of_many_sequences():
+    lens, S = [40] * 1500, 1500
+    starts = [min(s, 7) for s in range(S + 1)]
+    assert append_beside_bad(lens, starts, 7, 1, [], S) == 0
+    lens[-1] = -5
+    assert append_beside_bad(lens, starts, 7, 1, [], S) == A().ERR_INVALID_ARG
