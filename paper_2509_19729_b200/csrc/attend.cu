@@ -427,7 +427,7 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     if ((st = amoeba_attend_workspace_bytes(layout, batch, &need)) != AMOEBA_OK) return st;
     if (!d_workspace || workspace_bytes < need) return AMOEBA_ERR_INVALID_ARG;
     if ((uintptr_t)d_workspace % 16) return AMOEBA_ERR_ALIGNMENT;
-    if (p.batch.num_seqs == 0 || p.batch.num_rows == 0 || p.batch.max_q_len == 0) return AMOEBA_OK;
+    if (p.batch.num_seqs == 0 || p.batch.num_rows == 0) return AMOEBA_OK;
     p.lse = d_lse;
     p.status = d_status;
 #ifdef AMOEBA_CHECK_ITEMS
@@ -446,9 +446,9 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     // Short sequences are not worth cutting: what the shares and the join take, about 5 us, is what a CTA needs for 512
     // tokens, or for 1024 when there are units enough to fill the GPU (one sequence of 256 tokens, 8 key heads: 7.9 us whole,
     // 9.5 cut; of 1024: 20.5 and 11.3; 32 sequences of 1024: 24 and 29; of 2048: 41 and 47, but there one long one would
-    // hold up all).
+    // hold up all).  With max_q_len 0 sequences are only looked at.
     const int64_t tokens = (int64_t)p.batch.max_blocks * layout->block_tokens;
-    p.whole = tokens <= 512 || (tokens <= 1024 && p.batch.num_seqs * m.num_kv_heads >= dev.sms);
+    p.whole = rows == 0 || tokens <= 512 || (tokens <= 1024 && p.batch.num_seqs * m.num_kv_heads >= dev.sms);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(d_workspace);
     if (dtype == AMOEBA_FP16)

@@ -199,3 +199,29 @@ def test_append_reports_the_last_of_many_sequences():
     assert append_beside_bad(lens, starts, 7, 1, [], S) == 0
     lens[-1] = -5
     assert append_beside_bad(lens, starts, 7, 1, [], S) == A().ERR_INVALID_ARG
+
+
+# ---------------------------------------------------------------------------------------------------------------------- attend
+
+@pytest.mark.parametrize("lens", [(20, 30, 40), (900, 30, 400)])
+def test_rows_where_none_are_announced(lens):
+    """max_q_len 0: sequences with rows are refused by every call, those without are fine."""
+    a = A()
+    for starts, lengths, status in (([0, 0, 0, 0], lens, 0), ([0, 0, 1, 1], lens, a.ERR_INVALID_ARG),
+                                    ([0, 0, 0, 0], (lens[0], -1, lens[2]), a.ERR_INVALID_ARG)):
+        c = Case(4, 2, 64, lens=lens, seed=92).up()
+        c.dlens.copy_(torch.tensor(lengths, dtype=torch.int32))
+        c.dstarts.copy_(torch.tensor(starts, dtype=torch.int32))
+        c.batch = a.make_batch(c.dbt, c.dlens, c.dstarts, c.rows, 0)
+        c.attend()
+        torch.cuda.synchronize()
+        assert int(c.status.item()) == status and (c.out[0] == 7).all() and (c.lse == 7).all()
+        c.status.zero_()
+        pool, k = c.dpools[0].clone(), torch.zeros(c.rows, 128, dtype=torch.bfloat16, device=DEV)
+        a.amoeba_append_kv(c.layout, 1, 0, [pool], c.batch, c.dq, [k], [k], None, c.out, c.status)
+        torch.cuda.synchronize()
+        assert int(c.status.item()) == status and (c.out[0] == 7).all() and torch.equal(pool, c.dpools[0])
+        c.status.zero_()
+        a.amoeba_accumulate_scores(c.layout, 1, 0, c.dpools, c.batch, c.dq, c.scale, 0, c.lse, None,
+                                   [torch.zeros(1, c.NB, 2, 16, device=DEV)], c.status)
+        assert int(c.status.item()) == status
