@@ -266,7 +266,7 @@ __device__ bool score_load(const ScoreParams& p, const CacheMaps& maps, int box_
         const int len = run.w.seq.len;
         for (int j = 0; ok && j < run.passes; ++j) {
             if (!(ok = wait(&b.q_empty[qb], q_phase))) break;
-            load.queries(p.q, run.w, p.shape.group, j * 128, min(128, run.rows - j * 128), smem + qb * S::kTileBytes);
+            load.template queries<true>(p.q, run.w, p.shape.group, j * 128, min(128, run.rows - j * 128), smem + qb * S::kTileBytes);
             arrive_when_loaded(&b.q_full[qb]);
             if (qb ^= 1, qb == 0) q_phase ^= 1;
             auto at = load.groups(0, len, run.t0 * 128), next = load.groups(0, len, run.t0 * 128 + 128);
@@ -362,7 +362,9 @@ __device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[12
     return lo + hi;
 }
 
-// s_row: [2][128] of this warpgroup, -lse * log2(e) of the pass's rows; s_pos: their cache indices.
+// s_row: [2][128] of this warpgroup, -lse * log2(e) of the pass's rows; s_pos: their cache indices.  A pass has rows that add nothing:
+// those behind its last row, which repeat that one (their logits are infinite or NaN only where its own are), and those with
+// lse -infinity, whose queries may be anything, so that with one of them all tiles are summed with a look at who sees them.
 __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, float (*s_row)[128], int32_t (*s_pos)[128]) {
     const int g = threadIdx.x / 128, tid = threadIdx.x % 128, G = p.shape.group, T = p.cache.block_tokens;
     const uint32_t lanes = (uint32_t)(tid / 32 * 32) << 16;
@@ -385,9 +387,13 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
                 lse = p.lse[(int64_t)(q.q0 + tok) * p.q_heads + run.w.h * G + row - tok * G];
                 pos = q.len - q.qn + tok;
             }
-            s_row[pass][tid] = lse == -INFINITY ? -INFINITY : -lse * kLog2e;  // a row that saw nothing adds nothing
-            s_pos[pass][tid] = pos;
-            asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + g) : "memory");
+            int mute = row < run.rows && lse == -INFINITY;
+            s_row[pass][tid] = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+            s_pos[pass][tid] = mute ? -1 : pos;
+            asm volatile(
+                "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %0, 0;\n\t"
+                "barrier.cta.red.or.pred q, %1, 128, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+                : "+r"(mute) : "r"(1 + g) : "memory");
             // what the pass's first row and its last one see, if they are there
             const int first_pos = q.len - q.qn + j * 128 / G;
             const int last_pos = q.len - q.qn + (min(run.rows, j * 128 + 128) - 1) / G;
@@ -411,7 +417,7 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
                     i_block = at / T, in_block = at - i_block * T;
                     block = table[i_block];
                 }
-                const bool cut = key0 + 127 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
+                const bool cut = mute || key0 + 127 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
                 if (!wait(&b.s_full[g], full)) {
                     ok = false, b.abort = 1;
                     break;

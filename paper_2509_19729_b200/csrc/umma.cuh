@@ -227,13 +227,15 @@ struct TileLoader {
         }
         arrive_when_loaded(bar);
     }
-    // Starts the loads of `count` (at most 128) query rows of w's sequence and key head, from row `row` on; zeros behind.
+    // Starts the loads of `count` (at most 128) query rows of w's sequence and key head, from row `row` on; behind them zeros, or
+    // (kRepeat) the last of them over and over.
+    template <bool kRepeat = false>
     __device__ __forceinline__ void queries(const Rows& q, const Walk& w, int group, int row, int count, uint32_t dst) const {
         const int c = lane % kChunks, sub = lane / kChunks, worker = w.h / v.heads;
         const char* base = q.base[worker] + (int64_t)w.seq.q0 * q.stride + (w.h - worker * v.heads) * group * (D * 2) + c * 16;
         for (int first = warp * 32; first < 128; first += kWarps * 32) {
-            const int r = row + first + lane, tok = r / group;
-            const int64_t mine = first + lane < count ? tok * q.stride + (r - tok * group) * (D * 2) : -1;
+            const int r = row + (kRepeat ? min(first + lane, count - 1) : first + lane), tok = r / group;
+            const int64_t mine = kRepeat || first + lane < count ? tok * q.stride + (r - tok * group) * (D * 2) : -1;
 #pragma unroll
             for (int i = 0; i < 32; i += kStep) {
                 const int64_t off = __shfl_sync(~0u, mine, i + sub);

@@ -225,3 +225,43 @@ def test_rows_where_none_are_announced(lens):
         a.amoeba_accumulate_scores(c.layout, 1, 0, c.dpools, c.batch, c.dq, c.scale, 0, c.lse, None,
                                    [torch.zeros(1, c.NB, 2, 16, device=DEV)], c.status)
         assert int(c.status.item()) == status
+
+
+# ---------------------------------------------------------------------------------------------------------------------- scores
+
+def scores_of(c, lse):
+    got = [torch.zeros(1, c.NB, c.m["Hkv"] // c.tp, c.T, device=DEV) for _ in range(c.tp)]
+    A().amoeba_accumulate_scores(c.layout, 1, 0, c.dpools, c.batch, c.dq, c.scale, 0, lse, None, got, c.status)
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == 0
+    return got
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,q", [(4, 2, 64, 3), (8, 2, 128, 33), (8, 2, 64, 40), (6, 2, 128, 100), (2, 2, 64, 300)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 0.0])
+def test_scores_rows_that_add_nothing_may_hold_anything(Hq, Hkv, D, q, bad):
+    """Rows with lse -infinity, first and last of their sequences among them: the others' sums, to the bit."""
+    c = Case(Hq, Hkv, D, lens=[700, q, 300], qlens=[q, q, 1], seed=100 + q).up()
+    c.attend()
+    lse = c.lse.clone()
+    mute = torch.zeros(c.rows, dtype=torch.bool)
+    mute[[0, q // 2, q - 1, q]] = True
+    lse[mute.to(DEV)] = -np.inf
+    want = scores_of(c, lse)
+    for x in c.dq:
+        x[mute.to(DEV)] = bad
+    got = scores_of(c, lse)
+    assert all(torch.equal(x, y) for x, y in zip(got, want)) and all(torch.isfinite(x).all() for x in got)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,q", [(4, 2, 64, 3), (8, 2, 128, 33), (8, 2, 64, 40), (6, 2, 128, 100), (2, 2, 64, 300)])
+def test_scores_of_a_key_that_no_row_wants(Hq, Hkv, D, q):
+    """A key of -infinity that every row sees with a logit of -infinity: its score is 0, in passes that are not full too."""
+    c = Case(Hq, Hkv, D, lens=[700, q], qlens=[q, q], seed=120 + q).up()
+    at = 5
+    for x in c.dq:
+        x.view(c.rows, Hq, D)[..., at] = x.view(c.rows, Hq, D)[..., at].abs() + 0.5
+    c.dpools[0][0, int(c.bt[0, 9]), :, 0, 7, at] = -np.inf  # token 151 of the first sequence
+    c.attend()
+    got = scores_of(c, c.lse)[0][0, int(c.bt[0, 9])]
+    assert (got[:, 7] == 0).all() and torch.isfinite(got).all() and (got[:, 6] > 0).all()
