@@ -1,7 +1,8 @@
 // amoeba_accumulate_scores: the attention weight that every cached token received, summed over the rows.
 //
 // exp(scale * q . k - lse) needs no running statistics, so a token's sum is finished by the warp that has read its key:
-// every key is read once, the rows are walked in order for it, and no two warps add to the same score.
+// every key is read once, the rows are walked in order for it, and no two warps add to the same score.  The exponent is formed as
+// (scale * q . k - lse) * log2(e): logit and lse may be large and near each other, so only their difference is rounded.
 #include "umma.cuh"
 
 namespace amoeba {
@@ -15,7 +16,7 @@ struct ScoreParams {
     const float* lse;
     const int32_t* scored;
     int32_t* status;
-    float scale_log2;
+    float scale;
     int32_t q_heads, window;
 #ifdef AMOEBA_CHECK_ITEMS
     int32_t polls;  // of every wait in score_many
@@ -94,7 +95,7 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
                 for (int b = 0; b < 2; ++b) {
                     const int rr = t * 8 + pair * 2 + b, token = rr / g, pos = q.len - q.qn + token;
                     const float x = rr < rows ? p.lse[(int64_t)(q.q0 + token) * p.q_heads + walk.h * g + rr - token * g] : -INFINITY;
-                    lse[t][b] = x * kLog2e;
+                    lse[t][b] = x;
                     see_hi[t][b] = x == -INFINITY ? 0 : pos + 1;  // a row that saw nothing adds nothing
                     see_lo[t][b] = p.window > 0 ? pos - p.window + 1 : 0;
                 }
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
                 for (int i = 0; i < 4; ++i) {
                     const int key = key0 + i / 2 * 8;
                     if (key < see_hi[t][i % 2] && key >= see_lo[t][i % 2])
-                        sum[i / 2] += fast_exp2(st[t][i] * p.scale_log2 - lse[t][i % 2]);
+                        sum[i / 2] += fast_exp2(fmaf(st[t][i], p.scale, -lse[t][i % 2]) * kLog2e);
                 }
         }
 #pragma unroll
@@ -321,12 +322,12 @@ __device__ bool score_multiply(const ScoreParams& p, uint32_t smem, ScoreBarrier
     return true;
 }
 
-// Sum over the 128 rows of 2^(c * logit + row) for one token; kCut: of those rows that see it.  `empty` gets this thread's
+// Sum over the 128 rows of e^(c * logit + row) for one token; kCut: of those rows that see it.  `empty` gets this thread's
 // arrival when the logits are read.
 template <bool kCut>
 __device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[128], const int32_t (&pos)[128], int key, int window, float c,
                                             uint64_t* empty) {
-    const uint64_t c2 = pair2(c, c);
+    const uint64_t c2 = pair2(c, c), e2 = pair2(kLog2e, kLog2e);
     uint64_t sum[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -342,8 +343,8 @@ __device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[12
         for (int k = 0; k < 32; k += 4) {
             const float4 r = *reinterpret_cast<const float4*>(&row[i * 32 + k]);
             float x[4];
-            split2(fma2(pair2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, pair2(r.x, r.y)), x[0], x[1]);
-            split2(fma2(pair2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, pair2(r.z, r.w)), x[2], x[3]);
+            split2(mul2(fma2(pair2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, pair2(r.x, r.y)), e2), x[0], x[1]);
+            split2(mul2(fma2(pair2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, pair2(r.z, r.w)), e2), x[2], x[3]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = fast_exp2(x[e]);
             if (kCut) {
@@ -362,14 +363,14 @@ __device__ __forceinline__ float column_sum(uint32_t from, const float (&row)[12
     return lo + hi;
 }
 
-// s_row: [2][128] of this warpgroup, -lse * log2(e) of the pass's rows; s_pos: their cache indices.  A pass has rows that add nothing:
+// s_row: [2][128] of this warpgroup, -lse of the pass's rows; s_pos: their cache indices.  A pass has rows that add nothing:
 // those behind its last row, which repeat that one (their logits are infinite or NaN only where its own are), and those with
 // lse -infinity, whose queries may be anything, so that with one of them all tiles are summed with a look at who sees them.
 __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, float (*s_row)[128], int32_t (*s_pos)[128]) {
     const int g = threadIdx.x / 128, tid = threadIdx.x % 128, G = p.shape.group, T = p.cache.block_tokens;
     const uint32_t lanes = (uint32_t)(tid / 32 * 32) << 16;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort)); };
-    const float c = p.scale_log2;
+    const float c = p.scale;
     int pass = 0;
     uint32_t full = 0;  // parity to wait for at s_full[g]
     bool ok = true;     // a warp that gives up goes on to the barriers below, where the others of its warpgroup wait for it
@@ -388,7 +389,7 @@ __device__ bool score_sum(const ScoreParams& p, ScoreBarriers& b, Runs run, floa
                 pos = q.len - q.qn + tok;
             }
             int mute = row < run.rows && lse == -INFINITY;
-            s_row[pass][tid] = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+            s_row[pass][tid] = lse == -INFINITY ? -INFINITY : -lse;
             s_pos[pass][tid] = mute ? -1 : pos;
             asm volatile(
                 "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %0, 0;\n\t"
@@ -543,7 +544,7 @@ extern "C" amoeba_status amoeba_accumulate_scores(const amoeba_layout* layout, i
 #ifdef AMOEBA_CHECK_ITEMS
     p.polls = operator_wait_polls();
 #endif
-    p.scale_log2 = scale * kLog2e;
+    p.scale = scale;
     p.q_heads = m.num_q_heads;
     p.shape.group = m.num_q_heads / m.num_kv_heads;
     p.shape.kv_heads = m.num_kv_heads;

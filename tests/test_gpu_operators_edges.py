@@ -265,3 +265,34 @@ def test_scores_of_a_key_that_no_row_wants(Hq, Hkv, D, q):
     c.attend()
     got = scores_of(c, c.lse)[0][0, int(c.bt[0, 9])]
     assert (got[:, 7] == 0).all() and torch.isfinite(got).all() and (got[:, 6] > 0).all()
+
+
+@pytest.mark.parametrize("D,T,dtype", [(64, 16, "fp16"), (128, 8, "bf16"), (128, 5, "fp16")])
+@pytest.mark.parametrize("q", [1, 8, 40])
+def test_scores_of_large_logits(D, T, dtype, q):
+    """Logits around a thousand, whose products and sums are exact: what is left is one rounding of the difference to lse and one
+    of its product with log2(e), itself off by 2^-26 (3 half steps of 2^-24 of the exponent, with room for that), the exponential's
+    2^-22 and the additions' 2^-24 each."""
+    c = Case(8, 2, D, T=T, dtype=dtype, lens=[q + 200], qlens=[q], seed=140)
+    n = q + 200
+    g = np.random.default_rng(q)
+    u, v = g.integers(120, 129, n).astype(float), g.integers(60, 65, (q, 8)).astype(float)  # whole numbers of 8 bits at most
+    scale = np.float32(0.125 if D == 64 else 0.1)
+    c.q.zero_()
+    c.q[:, :, 3] = torch.from_numpy(v).to(c.q.dtype)
+    for i in range(n):
+        for h in range(2):
+            k = c.cache.at(0, int(c.bt[0, i // T]), h, 0, i % T)
+            k.zero_()
+            k[3] = u[i]
+    c.up()
+    lse = (np.float64(scale) * v * 128 + 0.3 * v / 60).astype(np.float32)
+    got = [torch.zeros(1, c.NB, 2, T, device=DEV)]
+    A().amoeba_accumulate_scores(c.layout, int(dtype == "bf16"), 0, c.dpools, c.batch, c.dq, float(scale), 0,
+                                 torch.from_numpy(lse).to(DEV), None, got, c.status)
+    host = got[0].cpu().double().numpy()
+    for i in range(n):
+        x = np.float64(scale) * v * u[i] - lse.astype(np.float64)  # [q, 8]
+        w = np.where((i <= n - q + np.arange(q))[:, None], np.exp(x), 0.0).reshape(q, 2, 4)
+        tol = (w * (4 * 2.0 ** -24 * np.abs(x).reshape(q, 2, 4) + 2.0 ** -22 + 4 * q * 2.0 ** -24)).sum((0, 2))
+        assert (np.abs(host[0, c.bt[0, i // T], :, i % T] - w.sum((0, 2))) <= tol).all()
