@@ -548,7 +548,8 @@ AMOEBA_API amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
  * d_seq_lens[s] gets a value, so a score pool needs no clearing.  score_pools: HOST array of tp device pointers, worker
  * r's float [num_layers][num_blocks][heads of r][block_tokens], addressed by the same block ids as the cache.
  * d_scored_lens: int32 [num_seqs], or NULL: all sums start from zero.  The order of the additions is fixed: the same
- * call gives the same bits.  Several sequences may share a block only if they would write the same scores there.
+ * call gives the same bits.  Sequences of a call may not share a block, not even with the same scores there: a sum may be
+ * written and read again between its rows.
  */
 AMOEBA_API amoeba_status amoeba_accumulate_scores(const amoeba_layout* layout, int32_t dtype, int32_t layer,
                                        const void* const* pools, const amoeba_batch* batch, const void* const* q,
