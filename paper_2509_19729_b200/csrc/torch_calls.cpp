@@ -33,6 +33,11 @@ int32_t whole32(PyObject* o) {
     if (v < INT32_MIN || v > INT32_MAX) throw Refused{"a number does not fit 32 bits"};
     return (int32_t)v;
 }
+double real(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1. && PyErr_Occurred()) throw Refused{nullptr};
+    return v;
+}
 const at::Tensor& tensor(PyObject* o) {
     if (!THPVariable_Check(o)) throw Refused{"a tensor is needed"};
     return THPVariable_Unpack(o);
@@ -111,14 +116,19 @@ const amoeba_layout& layout_of(PyObject* o) {
 }
 // The stream to launch on, with its device current while the object lives.
 struct On {
-    c10::cuda::CUDAGuard guard;
     void* stream;
+    c10::cuda::CUDAGuard guard;
     static c10::DeviceIndex gpu(int64_t device) {
         if (device < 0) throw Refused{"the tensors are not on a GPU"};
         return (c10::DeviceIndex)device;
     }
-    On(int64_t device, PyObject* given) : guard(gpu(device)) {
-        stream = given == Py_None ? (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream() : PyLong_AsVoidPtr(given);
+    static void* handle(PyObject* o) {
+        void* p = o == Py_None ? nullptr : PyLong_AsVoidPtr(o);
+        if (!p && PyErr_Occurred()) throw Refused{nullptr};
+        return p;
+    }
+    On(int64_t device, PyObject* given) : stream(handle(given)), guard(gpu(device)) {
+        if (given == Py_None) stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
     }
 };
 
@@ -148,7 +158,7 @@ PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t dev = whole(a[5]), D = l.model.head_dim;
         const at::ScalarType type = element(dtype);
         Pointers pool, q, k, v, out;
-        pools(a[3], l, layer_bytes(l) * (layer + 1), false, dev, &pool);
+        pools(a[3], l, layer_bytes(l) * ((int64_t)layer + 1), false, dev, &pool);
         const bool has_q = a[6] != Py_None, has_out = a[10] != Py_None;
         if (has_q) rows(a[6], l, b->num_rows, l.model.num_q_heads / l.tp * D, type, dev, &q);
         rows(a[7], l, b->num_rows, l.model.num_kv_heads / l.tp * D, type, dev, &k);
@@ -170,10 +180,10 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t dev = whole(a[5]), width = (int64_t)l.model.num_q_heads / l.tp * l.model.head_dim;
         const at::ScalarType type = element(dtype);
         Pointers pool, q, out;
-        pools(a[3], l, layer_bytes(l) * (layer + 1), false, dev, &pool);
+        pools(a[3], l, layer_bytes(l) * ((int64_t)layer + 1), false, dev, &pool);
         rows(a[6], l, b->num_rows, width, type, dev, &q);
         rows(a[9], l, b->num_rows, width, type, dev, &out);
-        const double scale = PyFloat_AsDouble(a[7]);
+        const double scale = real(a[7]);
         const int32_t window = whole32(a[8]);
         void* lse = a[10] == Py_None ? nullptr
                                      : dense(a[10], at::kFloat, (int64_t)b->num_rows * l.model.num_q_heads, dev,
@@ -194,10 +204,10 @@ PyObject* accumulate_scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t dev = whole(a[5]);
         const at::ScalarType type = element(dtype);
         Pointers pool, q, scores;
-        pools(a[3], l, layer_bytes(l) * (layer + 1), false, dev, &pool);
-        pools(a[11], l, layer_scores(l) * (layer + 1), true, dev, &scores);
+        pools(a[3], l, layer_bytes(l) * ((int64_t)layer + 1), false, dev, &pool);
+        pools(a[11], l, layer_scores(l) * ((int64_t)layer + 1), true, dev, &scores);
         rows(a[6], l, b->num_rows, (int64_t)l.model.num_q_heads / l.tp * l.model.head_dim, type, dev, &q);
-        const double scale = PyFloat_AsDouble(a[7]);
+        const double scale = real(a[7]);
         const int32_t window = whole32(a[8]);
         void* lse = dense(a[9], at::kFloat, (int64_t)b->num_rows * l.model.num_q_heads, dev, "lse is float32 [num_rows, num_q_heads]");
         void* scored = a[10] == Py_None ? nullptr : dense(a[10], at::kInt, b->num_seqs, dev, "scored_lens is int32 [num_seqs]");
@@ -212,7 +222,7 @@ PyObject* accumulate_scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* evict_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return answer(n, 14, [&] {
         const amoeba_layout& l = layout_of(a[0]);
-        const int32_t l0 = whole32(a[1]), l1 = whole32(a[2]);
+        const int32_t l0 = whole32(a[1]), l1 = whole32(a[2]), budget = whole32(a[8]), recent = whole32(a[9]);
         const at::Tensor &lens = tensor(a[6]), &src = tensor(a[5]), &dst = tensor(a[7]);
         const int64_t dev = lens.is_cuda() ? lens.device().index() : -1, S = lens.numel();
         if (src.dim() != 2 || dst.dim() != 2 || src.size(0) != S || dst.size(0) != S) throw Refused{"block tables are [num_seqs, blocks]"};
@@ -229,7 +239,7 @@ PyObject* evict_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* ws = dense(a[12], at::kByte, 0, dev, "the workspace is uint8");
         const On here(dev, a[13]);
         return amoeba_evict_kv(&l, l0, l1, pool, has_scores ? (float* const*)scores.p : nullptr, (int32_t*)src_p, (int32_t*)lens_p,
-                               (int32_t)S, (int32_t)src.size(1), (int32_t*)dst_p, (int32_t)dst.size(1), whole32(a[8]), whole32(a[9]),
+                               (int32_t)S, (int32_t)src.size(1), (int32_t*)dst_p, (int32_t)dst.size(1), budget, recent,
                                (int32_t*)new_p, (int32_t*)status, ws, tensor(a[12]).numel(), here.stream);
     });
 }

@@ -312,3 +312,29 @@ def test_a_tensor_of_one_row_fits_beside_any_stride():
     for q in ([alone, part], [part, alone], [alone, part[:1]], [alone, alone]):
         with pytest.raises(A.AmoebaError, match="not on a GPU"):
             c("attend", q=q)
+
+
+class NoStream:
+    cuda_stream = "7"
+
+
+@pytest.mark.parametrize("names,bad", [
+    (["attend", "scores"], dict(scale="1")), (["attend", "scores"], dict(scale=None)), (["attend", "scores"], dict(window=1.5)),
+    (ROWS, dict(dtype="fp16")), (ROWS, dict(layer=None)), (["evict"], dict(l0=0.0)), (["evict"], dict(budget="10")),
+    (ALL, dict(stream=NoStream())), (ALL, dict(stream=NoStream)),
+])
+def test_what_is_no_number_is_a_type_error(names, bad):
+    for name in names:
+        with pytest.raises(TypeError):
+            Calls()(name, **bad)
+
+
+def test_the_largest_numbers_are_refused():
+    c = Calls()
+    for bad in (dict(layer=2 ** 31 - 1), dict(layer=-1), dict(layer=-2 ** 31)):
+        for name in ROWS:
+            with pytest.raises(A.AmoebaError):
+                c(name, **bad)
+    for bad in (dict(l1=2 ** 31 - 1), dict(l0=-1), dict(budget=2 ** 31)):
+        with pytest.raises(A.AmoebaError):
+            c("evict", **bad)
