@@ -477,9 +477,9 @@ def _load_torch_calls():
         try:
             _build.build_torch_calls()
         except Exception as e:
-            raise ImportError(f"{_build.TORCH_CALLS.name} is missing or stale and could not be built: {e}") from e
+            raise ImportError(f"{_build.torch_calls_path().name} is missing or stale and could not be built: {e}") from e
     C.CDLL(str(library_path()), mode=C.RTLD_GLOBAL)  # the functions that the module calls
-    spec = importlib.util.spec_from_file_location("_torch_calls", _build.TORCH_CALLS)
+    spec = importlib.util.spec_from_file_location("_torch_calls", _build.torch_calls_path())
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
     return module

@@ -16,7 +16,6 @@ INCLUDE = HERE.parent / "include"
 LIB = HERE / "libamoeba.so"
 LIB_CHECKED = HERE / "libamoeba_checked.so"  # the same sources with -DAMOEBA_CHECK_ITEMS: every work item is tested
 #                                              against the extent of its buffers before it is moved
-TORCH_CALLS = HERE / "_torch_calls.so"  # the serving operators' Python calls on torch tensors
 SOURCES = ["plan.cpp", "block_tables.cu", "kv_reshard.cu", "weights_reshard.cu", "append_kv.cu", "attend.cu", "attend_many.cu",
            "scores.cu", "evict_kv.cu", "cache_maps.cu"]
 HEADERS = ["plan.hpp", "launch.hpp", "copy_engine.cuh", "kv_items.cuh", "w_items.cuh", "cache_view.cuh", "walk.cuh", "attend.cuh",
@@ -60,29 +59,38 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     return lib
 
 
+def torch_calls_path() -> Path:
+    """The serving operators' Python calls on torch tensors.  The module reads tensors by the C++ layout of the Python and the torch
+    that it was built for, so it is named after them: another version builds its own."""
+    import torch
+
+    return HERE / f"_torch_calls.{sys.implementation.cache_tag}-torch{torch.__version__}-abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}.so"
+
+
 def torch_calls_stale() -> bool:
-    deps = [CSRC / "torch_calls.cpp", INCLUDE / "amoeba.h"]
-    return not TORCH_CALLS.exists() or any(d.stat().st_mtime > TORCH_CALLS.stat().st_mtime for d in deps)
+    lib, deps = torch_calls_path(), [CSRC / "torch_calls.cpp", INCLUDE / "amoeba.h"]
+    return not lib.exists() or any(d.stat().st_mtime > lib.stat().st_mtime for d in deps)
 
 
 def build_torch_calls(force: bool = False) -> Path:
     """The CPython module between torch tensors and the C library.  It binds the library's functions when it is loaded,
     by then in the process, so that the checked build can stand in for the normal one."""
+    lib = torch_calls_path()
     if not force and not torch_calls_stale():
-        return TORCH_CALLS
+        return lib
     import sysconfig
 
     import torch
     from torch.utils.cpp_extension import include_paths, library_paths
 
-    tmp = TORCH_CALLS.with_suffix(f".tmp{os.getpid()}.so")
+    tmp = lib.with_suffix(f".tmp{os.getpid()}.so")
     cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-fvisibility=hidden", f"-I{INCLUDE}",
            f"-I{sysconfig.get_path('include')}", *[f"-I{p}" for p in include_paths("cuda")],
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", str(CSRC / "torch_calls.cpp"),
            *[f"-L{p}" for p in library_paths()], "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", str(tmp)]
     subprocess.run(cmd, check=True)
-    os.replace(tmp, TORCH_CALLS)
-    return TORCH_CALLS
+    os.replace(tmp, lib)
+    return lib
 
 
 if __name__ == "__main__":

@@ -338,3 +338,18 @@ def test_the_largest_numbers_are_refused():
     for bad in (dict(l1=2 ** 31 - 1), dict(l0=-1), dict(budget=2 ** 31)):
         with pytest.raises(A.AmoebaError):
             c("evict", **bad)
+
+
+def test_another_torch_does_not_load_this_one_s_module(monkeypatch):
+    """The module that reads tensors by their C++ layout is built anew for another version of torch or of Python's interface."""
+    import sys
+
+    from paper_2509_19729_b200 import build
+
+    here = build.torch_calls_path()
+    assert here.exists() and not build.torch_calls_stale()
+    for target, name, value in ((torch, "__version__", "0.0.1"), (sys.implementation, "cache_tag", "cpython-300"),
+                                (torch._C, "_GLIBCXX_USE_CXX11_ABI", not torch._C._GLIBCXX_USE_CXX11_ABI)):
+        with monkeypatch.context() as m:
+            m.setattr(target, name, value)
+            assert build.torch_calls_path() != here and build.torch_calls_stale()
