@@ -16,11 +16,6 @@ struct CacheView {
     char* pools[AMOEBA_MAX_TP];  // worker pools, advanced to the layer
     int64_t block_stride, head_stride, kv_stride, tok_stride;
     int32_t num_blocks, block_tokens, heads;  // heads: key heads per worker
-
-    __device__ __forceinline__ const char* head_base(int kv_head) const {
-        const int r = kv_head / heads;
-        return pools[r] + (kv_head - r * heads) * head_stride;
-    }
 };
 
 struct Rows {
@@ -194,11 +189,5 @@ int32_t operator_wait_polls();  // what a test has set (cache_maps.cu)
 #endif
 
 inline bool positive(float x) { return x > 0.f && x < INFINITY; }
-
-inline amoeba_status launch_result() {
-    if (cudaGetLastError() != cudaSuccess) return AMOEBA_ERR_CUDA;
-    count_launch();
-    return AMOEBA_OK;
-}
 
 }  // namespace amoeba

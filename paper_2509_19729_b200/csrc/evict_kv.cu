@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move(const __grid_const
 constexpr int kCloseThreads = 512, kCloseHeld = 8;  // 16-byte pieces that a thread holds
 template <int kVecs>
 __global__ void __launch_bounds__(kCloseThreads) evict_close_up(const __grid_constant__ EvictParams p, int rows) {
-    extern __shared__ __align__(16) char smem[];  // [rows] from, [rows] to, and the scores
+    extern __shared__ __align__(16) char smem[];  // [rows] from, [rows] to
     int64_t *s_from = reinterpret_cast<int64_t*>(smem), *s_to = s_from + rows;
     grid_dependency_wait();
     const uint32_t rank = cluster_rank(), size = cluster_size();
