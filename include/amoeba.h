@@ -547,6 +547,10 @@ AMOEBA_API amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
  * with amoeba_attend's lse of the same rows, mask and scale (rows with lse = -inf add nothing).  Every token below
  * d_seq_lens[s] gets a value, so a score pool needs no clearing.  score_pools: HOST array of tp device pointers, worker
  * r's float [num_layers][num_blocks][heads of r][block_tokens], addressed by the same block ids as the cache.
+ * Score pools do not go along with a transformation of the cache by themselves; amoeba_reshard_kv moves them when it is called
+ * for them too, with the same pair list and a plan between the two layouts that have heads of 8 elements of 2 bytes, blocks of
+ * block_tokens / 8 tokens and the header-centric order, whatever the cache's: a block's scores of a head, 4 * block_tokens
+ * bytes, are then one unit of it (block_tokens a multiple of 8).
  * d_scored_lens: int32 [num_seqs], or NULL: all sums start from zero.  The order of the additions is fixed: the same
  * call gives the same bits.  Sequences of a call may not share a block, not even with the same scores there: a sum may be
  * written and read again between its rows.

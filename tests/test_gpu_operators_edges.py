@@ -296,3 +296,47 @@ def test_scores_of_large_logits(D, T, dtype, q):
         w = np.where((i <= n - q + np.arange(q))[:, None], np.exp(x), 0.0).reshape(q, 2, 4)
         tol = (w * (4 * 2.0 ** -24 * np.abs(x).reshape(q, 2, 4) + 2.0 ** -22 + 4 * q * 2.0 ** -24)).sum((0, 2))
         assert (np.abs(host[0, c.bt[0, i // T], :, i % T] - w.sum((0, 2))) <= tol).all()
+
+
+@pytest.mark.parametrize("tp,to,T,order", [(1, 2, 16, 0), (4, 1, 8, 1), (2, 4, 32, 0)])
+def test_scores_go_along_with_a_transformation(tp, to, T, order):
+    """Scores of one layout, moved by a second call for the same pairs: the eviction that follows keeps the same tokens."""
+    from paper_2509_19729_b200.session import Session
+
+    a = A()
+    L, Hkv, D, lens, budget, recent = 2, 4, 64, [200, 90, 33], 64, 8
+    m = model(4, Hkv, D, L=L)
+    c = Case(4, Hkv, D, tp, T=T, order=order, lens=lens, L=L, seed=150)
+    c.up()
+    g = torch.Generator().manual_seed(2)
+    scores = [torch.randn(L, c.NB, Hkv // tp, T, generator=g).to(DEV) for _ in range(tp)]
+    t = Session(m, tp, to, c.NB, c.NB + 5, 3, c.bt.shape[1], c.bt.size, weights=False, block_tokens=T, device=DEV,
+                src_kv_order=order, dst_kv_order=order)
+    t.set_tables(lens, c.bt, free_list=np.random.default_rng(1).permutation(c.NB + 5))
+    for x, y in zip(t.src_pools, c.dpools):
+        x.copy_(y.flatten().view(torch.uint8))
+    t.step()
+    layout = lambda n, nb: a.make_layout(dict(m, D=8), n, nb, T // 8)  # noqa: E731
+    plan = a.amoeba_plan_create(layout(tp, c.NB), layout(to, c.NB + 5))
+    assert a.amoeba_layout_kv_pool_bytes(plan.src) == scores[0].nbytes
+    moved = [torch.full((L, c.NB + 5, Hkv // to, T), -9.0, device=DEV) for _ in range(to)]
+    a.amoeba_reshard_kv(plan, scores, moved, t.pairs, t.num_pairs, t.pairs_cap, 0, L, t.status)
+    db = t.dst_bt.cpu().numpy()
+    for s, n in enumerate(lens):
+        i = np.arange(-(-n // T) * T)
+        for h in range(Hkv):
+            x = scores[h // (Hkv // tp)][:, c.bt[s, i // T], h % (Hkv // tp), i % T]
+            y = moved[h // (Hkv // to)][:, db[s, i // T], h % (Hkv // to), i % T]
+            assert torch.equal(x, y)
+    kept = []
+    for lay, pools, sc, bt in ((c.layout, c.dpools, scores, c.dbt), (t.dst_layout, t.dst_pools, moved, t.dst_bt)):
+        new = torch.zeros(3, dtype=torch.int32, device=DEV)
+        ws = torch.empty(a.amoeba_evict_workspace_bytes(lay, L, 3, budget), dtype=torch.uint8, device=DEV)
+        a.amoeba_evict_kv(lay, 0, L, pools, sc, bt, c.dlens, bt, budget, recent, new, t.status, ws)
+        hb = bt.cpu().numpy()
+        n = len(pools)
+        shape = (L, -1, Hkv // n, 2, T, D) if order == 0 else (L, 2, -1, T, Hkv // n, D)
+        p = [x.view(torch.uint8).view(torch.bfloat16).view(*shape) for x in (y.flatten() for y in pools)]
+        p = [x if order == 0 else x.permute(0, 2, 4, 1, 3, 5) for x in p]
+        kept.append([torch.cat([x[:, hb[s, i // T], :, :, i % T] for x in p], 2) for s, i in ((s, np.arange(min(k, budget))) for s, k in enumerate(lens))])
+    assert all(torch.equal(x, y) for x, y in zip(*kept)) and int(t.status.item()) == 0
