@@ -506,8 +506,8 @@ typedef struct {
  * queries go to q_out, keys and (as they are) values into the cache.  All in 32 bits with one rounding at the end; the
  * angle and its reduction to [-pi, pi] in 64 bits, since in 32 position * inv_freq has lost its last digits long before
  * position 131071.
- * rotation NULL: neither norm nor rotation.  q and q_out both NULL: keys and values only.  q_out may be q.  A sequence
- * with more new tokens than cached ones is refused (INVALID_ARG).  Several sequences may share a block only if no new
+ * rotation NULL: neither norm nor rotation.  q and q_out both NULL: keys and values only.  q_out may be q (the same pointers and
+ * stride); otherwise it may not overlap q, k or v.  A sequence with more new tokens than cached ones is refused (INVALID_ARG).  Several sequences may share a block only if no new
  * token falls into it.
  */
 AMOEBA_API amoeba_status amoeba_append_kv(const amoeba_layout* layout, int32_t dtype, int32_t layer, void* const* pools,
@@ -528,7 +528,7 @@ AMOEBA_API amoeba_status amoeba_append_kv(const amoeba_layout* layout, int32_t d
  * weights are rounded to the element type for the product with the values.
  * Slots that no query of the call sees may hold anything, infinities and NaN included; the values of the tokens that
  * some query sees must be finite (a NaN there also reaches earlier rows of the same chunk).
- * out may not be q.  d_workspace: amoeba_attend_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant before
+ * out may not overlap q.  d_workspace: amoeba_attend_workspace_bytes(...) bytes, 16-byte aligned, contents irrelevant before
  * and after; calls that overlap on the GPU need separate ones.
  */
 AMOEBA_API amoeba_status amoeba_attend_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
@@ -577,6 +577,7 @@ AMOEBA_API amoeba_status amoeba_accumulate_scores(const amoeba_layout* layout, i
  * other sequence may share; the blocks behind are the caller's to free).  d_new_lens: int32 [num_seqs],
  * min(length, budget), not d_seq_lens itself.  score_pools may be NULL if recent = budget.
  * 1 <= budget, 0 <= recent <= budget (INVALID_ARG).
+ * An empty range of layers: nothing is done, d_new_lens is not written.
  * Device-detected: a sequence with a bad length, with a source or destination block id outside the pool, or that needs
  * more destination blocks than dst_max_blocks_per_seq: INVALID_ARG or BAD_BLOCK_ID, nothing of it moves, new length -1.
  * d_workspace: amoeba_evict_workspace_bytes(...) bytes for that many layers, as in amoeba_attend.

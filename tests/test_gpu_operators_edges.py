@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import cache_reference as ref
-from test_gpu_operators import A, DEV, Case, model
+from test_gpu_operators import A, DEV, Case, check_attend, check_evict, check_scores, draw_scores, model
 
 pytestmark = pytest.mark.gpu
 
@@ -340,3 +340,30 @@ def test_scores_go_along_with_a_transformation(tp, to, T, order):
         p = [x if order == 0 else x.permute(0, 2, 4, 1, 3, 5) for x in p]
         kept.append([torch.cat([x[:, hb[s, i // T], :, :, i % T] for x in p], 2) for s, i in ((s, np.arange(min(k, budget))) for s, k in enumerate(lens))])
     assert all(torch.equal(x, y) for x, y in zip(*kept)) and int(t.status.item()) == 0
+
+
+# ------------------------------------------------------------------------------------------- tables much wider than the lengths
+
+@pytest.mark.parametrize("extra", [0, 100, 5000])
+@pytest.mark.parametrize("T", [8, 16])
+def test_tables_wider_than_the_lengths(extra, T):
+    """Launch shapes go by the table's width: short sequences in the tables of a session with room for long ones."""
+    for qlens in ([1, 1, 1, 0, 1], [1, 20, 70, 0, 3]):
+        c = Case(8, 2, 64, 2, T=T, lens=[5, 40, 130, 0, 300], qlens=qlens, seed=160, extra=extra).up()
+        c.attend()
+        check_attend(c)
+        check_scores(c, scored=[4, 20, 60, 0, 297])
+
+
+@pytest.mark.parametrize("extra", [100, 1000, 5000])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_in_tables_wider_than_the_lengths(extra, in_place):
+    lens = [5, 64, 65, 130, 0, 301]
+    c = Case(4, 2, 64, 2, T=16, lens=lens, L=2, seed=161, spare=60, extra=extra).up()
+    free = np.setdiff1d(np.arange(c.NB), c.bt).astype(np.int32)
+    dst, k = np.full((len(lens), 4), -1, np.int32), 0
+    for s, n in enumerate(lens):
+        m = -(-min(n, 64) // 16)
+        dst[s, :m] = free[k:k + m]
+        k += m
+    check_evict(c, draw_scores(c, "ties"), 64, 10, in_place, dst_blocks=dst)
