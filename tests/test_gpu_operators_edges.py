@@ -298,6 +298,33 @@ def test_scores_of_large_logits(D, T, dtype, q):
         assert (np.abs(host[0, c.bt[0, i // T], :, i % T] - w.sum((0, 2))) <= tol).all()
 
 
+@pytest.mark.parametrize("q", [1, 8, 12, 30])
+def test_scores_of_logits_whose_sums_are_cut(q):
+    """One product of 512 beside eight of 0.9 steps of it, one to each matrix instruction, which may cut what does not reach a
+    step (2^-14).  Up to 8 rows there are four sums of two instructions: two steps cut and three half steps of rounding; up to 32
+    two of four: four steps and a half.  One sum would lose seven steps.  Beside that the roundings of the exponent (as above)."""
+    c = Case(2, 2, 128, lens=[q + 64], qlens=[q], seed=170)
+    n = q + 64
+    c.q.zero_()
+    c.q[:, :, 0], c.q[:, :, 1::16] = 32.0, 2.0 ** -7
+    for i in range(n):
+        for h in range(2):
+            k = c.cache.at(0, int(c.bt[0, i // 16]), h, 0, i % 16)
+            k.zero_()
+            k[0], k[1::16] = 16.0, 115 * 2.0 ** -14
+    c.up()
+    logit, lse = (512 + 8 * 115 * 2.0 ** -21) / 64, 8.5
+    got = [torch.zeros(1, c.NB, 2, 16, device=DEV)]
+    A().amoeba_accumulate_scores(c.layout, 1, 0, c.dpools, c.batch, c.dq, 1 / 64, 0, torch.full((q, 2), lse, device=DEV), None, got,
+                                 c.status)
+    host = got[0].cpu().double().numpy()
+    off = (3.5 if q <= 8 else 4.5) * 2.0 ** -14 / 64 + 4 * 2.0 ** -24 * abs(logit - lse) + 2.0 ** -22 + q * 2.0 ** -24
+    for i in range(n):
+        rows = q if i <= n - q else n - i
+        want = rows * np.exp(logit - lse)
+        assert (np.abs(host[0, c.bt[0, i // 16], :, i % 16] - want) <= want * off).all(), (i, host[0, c.bt[0, i // 16], :, i % 16] / want - 1, off)
+
+
 @pytest.mark.parametrize("tp,to,T,order", [(1, 2, 16, 0), (4, 1, 8, 1), (2, 4, 32, 0)])
 def test_scores_go_along_with_a_transformation(tp, to, T, order):
     """Scores of one layout, moved by a second call for the same pairs: the eviction that follows keeps the same tokens."""
