@@ -394,3 +394,67 @@ def test_evict_in_tables_wider_than_the_lengths(extra, in_place):
         dst[s, :m] = free[k:k + m]
         k += m
     check_evict(c, draw_scores(c, "ties"), 64, 10, in_place, dst_blocks=dst)
+
+
+# ------------------------------------------------------------------------------------------------------------ captured calls
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("wide", [0, 1000])  # one CTA, and a cluster, to each selection
+def test_a_captured_step_with_an_eviction(in_place, wide):
+    """Append, attend, accumulate and evict in one graph, replayed with other rows, lengths and tables: the same bits as the calls
+    one by one, on another stream."""
+    a = A()
+    L, budget, recent, S, NB = 2, 40, 8, 3, 120
+    layout = a.make_layout(model(8, 2, 64, L), 2, NB, 16)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    bt, dst = torch.full((S, 12 + wide), -1, **i32), torch.full((S, 12 + wide), -1, **i32)
+    lens, starts, new = torch.zeros(S, **i32), torch.zeros(S + 1, **i32), torch.zeros(S, **i32)
+    status = torch.zeros(1, **i32)
+    q, k, v = ([torch.zeros(60, w, dtype=torch.bfloat16, device=DEV) for _ in range(2)] for w in (256, 64, 64))
+    q_out, out = ([torch.zeros_like(x) for x in q] for _ in range(2))
+    lse = torch.zeros(60, 8, device=DEV)
+    pools = [torch.zeros(L, NB, 1, 2, 16, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    scores = [torch.zeros(L, NB, 1, 16, device=DEV) for _ in range(2)]
+    freq = (10000.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64) / 64)).to(DEV)
+    rotation = a.make_rotation(inv_freq=freq, rot_dim=64)
+    batch = a.make_batch(bt, lens, starts, 60, 50)
+    ws = torch.zeros(a.amoeba_attend_workspace_bytes(layout, batch), dtype=torch.uint8, device=DEV)
+    ews = torch.zeros(a.amoeba_evict_workspace_bytes(layout, L, S, budget), dtype=torch.uint8, device=DEV)
+
+    def step(stream=None):
+        for l in range(L):
+            a.amoeba_append_kv(layout, 1, l, pools, batch, q, k, v, rotation, q_out, status, stream)
+            a.amoeba_attend(layout, 1, l, pools, batch, q_out, 0.125, 0, out, lse, status, ws, stream)
+            a.amoeba_accumulate_scores(layout, 1, l, pools, batch, q_out, 0.125, 0, lse, None, scores, status, stream)
+        a.amoeba_evict_kv(layout, 0, L, pools, scores, bt, lens, bt if in_place else dst, budget, recent, new, status, ews, stream)
+
+    def fill(seed, n, rows):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        for t in q + k + v + pools + scores:
+            t.copy_(torch.randn(t.shape, generator=g, device=DEV))
+        ids = torch.randperm(NB, generator=g, device=DEV).to(torch.int32).view(S, 40)
+        bt[:, :12], dst[:, :12] = ids[:, :12], ids[:, 12:24]
+        lens.copy_(torch.tensor(n))
+        starts.copy_(torch.tensor([0, *np.cumsum(rows).tolist()]))
+
+    def state():
+        return [t.clone() for t in (*q_out, *out, lse, *pools, *scores, new)]
+
+    fill(0, [5, 6, 7], [1, 1, 1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed, n, rows in ((1, [150, 41, 30], [50, 1, 9]), (2, [30, 40, 192], [1, 1, 1]), (3, [100, 60, 50], [0, 33, 20])):
+        fill(seed, n, rows)
+        side.wait_stream(torch.cuda.current_stream())
+        step(side)
+        side.synchronize()
+        want = state()
+        fill(seed, n, rows)
+        graph.replay()
+        assert all(torch.equal(x, y) for x, y in zip(state(), want))
+        assert int(status.item()) == 0 and new.tolist() == [min(x, budget) for x in n]
