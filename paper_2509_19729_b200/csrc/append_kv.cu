@@ -4,7 +4,7 @@
 // A head's vector lies in head_dim / 8 neighbouring lanes, 16 bytes each, so that the norm's sum and the partner of a
 // rotated pair are shuffles; the angles of a token are computed once per block, in 64 bits, for all its heads.  A head's norm,
 // rotation and rounding are in 32 bits, with one rounding to the element type at the end.
-// Measured: 9443 rows of 32 + 2*32 heads of 128, pairs rotated: 87.5 us, 5.3 TB/s (81 % of a copy's rate); the instructions, about
+// Measured: 9443 rows of 32 + 2*32 heads of 128, pairs rotated: 91 us, 5.1 TB/s (78 % of a copy's rate); the instructions, about
 // 130 for the 512 bytes that a warp turns at a time, take as long as the bytes.
 #include "cache_view.cuh"
 #include "copy_engine.cuh"
@@ -40,7 +40,7 @@ __device__ __forceinline__ int find_sequence(const Batch& b, int row, int* share
 }
 
 // kThreads to a row: with rows enough to fill the GPU, 128 (9443 rows of 96 heads: 87.5 us, with 256 94, with 512 111); with
-// fewer the time is that of one row, and 512 (128 rows of 48 heads: 7.6 us, with 128 10.8).  Three pieces at a time and ten
+// fewer the time is that of one row, and 512 (128 rows of 48 heads: 7.0 us, with 128 10.8).  Three pieces at a time and ten
 // blocks an SM, against two and twelve: 87.5 and 89.7 us; loading the next pieces ahead of these: 88 to 90.5 us.
 template <class T, int D, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 128 ? 10 : 1536 / kThreads) append_kv(const __grid_constant__ AppendParams p) {

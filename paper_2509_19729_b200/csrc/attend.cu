@@ -235,8 +235,9 @@ attend_few(const __grid_constant__ AttendParams p) {
 // ------------------------------------------------------------------------------------------------ joining
 // Joins the parts of the units that were cut, by their maxima and sums; in order, so the same call gives the same bits.  kWarps
 // warps to a row: with few rows a unit may be in as many parts as there are CTAs, so eight warps take every eighth part each;
-// with many rows it is in two or three, and a warp does four rows.  Bound by its few dependent loads: 9 us by itself for
-// 296 shares of 8 rows, of which the launch in front hides a part.
+// with many rows a warp does four rows, and walks all parts of each: two or three, as long as there are units enough, but up to
+// one for each CTA where a few units of many rows run over a long cache.  Bound by its few dependent loads: 9 us by itself for 296
+// shares of 8 rows, of which the launch in front hides a part.
 constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 template <int kWarps>
 constexpr int kJoinRows = kWarps == 1 ? 4 * kJoinWarps : 1;  // of a block

@@ -27,7 +27,7 @@ struct ScoreParams {
 // Up to 8*NT rows a sequence.  Bound by the bytes of the keys.  A warp takes 16 tokens of every tile of 64; S^T = K Q^T as in
 // attend.cu, so that a token's sum runs along the columns.  The loads of 16 tokens are half of attend_few's and the arithmetic
 // on them nearly as long, so it takes many warps rather than deep rings: 5 CTAs an SM with two stages 93 us, 4 with three 98, 2
-// with six 172 (64 sequences of 512 to 8192 tokens, 8 key heads of 128; now 95 us, 5.8 TB/s, 89 % of a copy's rate).
+// with six 172 (64 sequences of 512 to 8192 tokens, 8 key heads of 128; now 98 us, 5.7 TB/s, 86 % of a copy's rate).
 constexpr int kScoreThreads = 128, kScoreWarps = 4, kScoreTile = 16 * kScoreWarps;
 template <int D, int NT>
 struct ScoreShape {
@@ -167,8 +167,10 @@ __global__ void __launch_bounds__(kScoreThreads, ScoreShape<D, NT>::kCtas) score
 // next 128 rows of the same sequence and head, then its next head; the tokens of a head are dealt out to CTAs in tiles, all
 // rows with them, so a score has one thread.  Four warpgroups take the tiles in turn, each with its own logits in tensor
 // memory, so that the products run ahead.  Six prompts of 4 to 32 thousand tokens, 32 queries of each, 32 query heads on 8 key
-// heads of 128: 79 us; without the loads it would take 60 (a tile's 16384 exponentials are 1024 of the 2 thousand clocks that
-// it takes), without the sums 59 (the keys at a copy's rate, and about 12 us to start, to share the work out and to end).
+// heads of 128: 81 us; without the loads it would take about 60 (a tile's 16384 exponentials are 1024 of the 2 thousand clocks that
+// it takes), without the sums as much (the keys at a copy's rate, and about 12 us to start, to share the work out and to end).
+// A logit is one sum of D / 16 instructions, each of which cuts it (ScoreShape::kSums): the scores are 7.6e-7 off, against 3.5e-7
+// in plain torch.  All 512 columns of tensor memory hold logits, so there is no room for second sums.
 constexpr int kScoreGroups = 4, kScoreManyThreads = 128 * (kScoreGroups + 1), kScoreLoadWarps = 3;
 template <int D>
 struct ScoreManyShape {
