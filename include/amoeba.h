@@ -474,6 +474,8 @@ AMOEBA_API amoeba_status amoeba_plan_weight_alias(const amoeba_plan* plan, int32
  * BAD_BLOCK_ID, and only the tokens of that block are left out: a block id outside the pool.
  * Rows that several sequences name (some row number between theirs decreases): amoeba_append_kv gives them to the
  * first of these, amoeba_attend the result of one of them.  With num_rows 0 these two look at nothing.
+ * On the host, UNSUPPORTED: blocks of more than 2^30 tokens; a batch with more rows times heads, or more pieces of work (num_seqs
+ * times key heads times tiles of max_q_len rows), than 32 bits number.
  */
 enum { AMOEBA_FP16 = 0, AMOEBA_BF16 = 1 }; /* element type */
 
@@ -506,9 +508,9 @@ typedef struct {
  * queries go to q_out, keys and (as they are) values into the cache.  All in 32 bits with one rounding at the end; the
  * angle and its reduction to [-pi, pi] in 64 bits, since in 32 position * inv_freq has lost its last digits long before
  * position 131071.
- * rotation NULL: neither norm nor rotation.  q and q_out both NULL: keys and values only.  q_out may be q (the same pointers and
- * stride); otherwise it may not overlap q, k or v.  A sequence with more new tokens than cached ones is refused (INVALID_ARG).  Several sequences may share a block only if no new
- * token falls into it.
+ * rotation NULL: neither norm nor rotation.  q and q_out both NULL: keys and values only.  q_out may be q (the same pointers
+ * and stride); otherwise it may not overlap q, k or v.  A sequence with more new tokens than cached ones is refused
+ * (INVALID_ARG).  Several sequences may share a block only if no new token falls into it.
  */
 AMOEBA_API amoeba_status amoeba_append_kv(const amoeba_layout* layout, int32_t dtype, int32_t layer, void* const* pools,
                                const amoeba_batch* batch, const void* const* q, int64_t q_stride,
