@@ -593,6 +593,98 @@ AMOEBA_API amoeba_status amoeba_evict_kv(const amoeba_layout* layout, int32_t la
                               int32_t* d_new_lens, int32_t* d_status, void* d_workspace, int64_t workspace_bytes,
                               void* cuda_stream);
 
+/*
+ * amoeba_attend_shared
+ *
+ * amoeba_attend (without a window) for sequences that share prefixes: group g is the sequences d_group_starts[g] ...
+ * d_group_starts[g + 1] - 1 of the batch, whose caches hold the same first d_prefix_lens[g] tokens - in the same blocks or in
+ * copies: the prefix is read once for the group, through the block table of its first sequence with rows, and not looked at in the
+ * others' blocks.  Which tokens are the same is the caller's to know; a length need not be a multiple of block_tokens.  The results
+ * are amoeba_attend's but for the order of the sums.
+ * A group shares at most as many tokens as its shortest sequence has cached in front of its new ones.  It shares nothing, and its
+ * sequences attend by themselves, if fewer than two have rows, if one is bad (reported as by amoeba_attend), if d_prefix_lens[g] is
+ * negative or if it has more than max_group_rows rows (INVALID_ARG is reported).  So do sequences in front of the first group and
+ * behind the last, and all of them if d_group_starts decreases or leaves [0, num_seqs] (INVALID_ARG).
+ * The rows of the prefix's bad blocks are left out for the whole group.
+ * d_workspace: amoeba_attend_shared_workspace_bytes(...) bytes, as in amoeba_attend; it grows with num_rows (32-bit sums of every row and
+ * query head).
+ */
+typedef struct {
+    const int32_t* d_group_starts; /* [num_groups + 1] sequences */
+    const int32_t* d_prefix_lens;  /* [num_groups] tokens */
+    int32_t num_groups;
+    int32_t max_group_rows;        /* no group has more new tokens than this (it sizes the launch) */
+} amoeba_prefixes;
+AMOEBA_API amoeba_status amoeba_attend_shared_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
+                                                   const amoeba_prefixes* prefixes, int64_t* bytes);
+AMOEBA_API amoeba_status amoeba_attend_shared(const amoeba_layout* layout, int32_t dtype, int32_t layer, const void* const* pools,
+                                   const amoeba_batch* batch, const amoeba_prefixes* prefixes, const void* const* q,
+                                   int64_t q_stride, float scale, void* const* out, int64_t out_stride, float* d_lse,
+                                   int32_t* d_status, void* d_workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * amoeba_advance_tables
+ *
+ * Takes an instance's sequences from the lengths they have to those they are to have: blocks are handed out, given back and shared,
+ * and what the step's new tokens need is written.  d_block_refs[b] counts the table entries, below the sequences' lengths, that
+ * name block b; 0 is free.  With T = block_tokens, for sequence s from old = d_seq_lens[s] to now = d_new_lens[s]:
+ *   now > old   blocks are taken for the tokens behind old.  If old ends inside a block that is counted more than once, the first
+ *               one taken replaces it in the table and is to be a copy of it (a pair, see below).
+ *   now < old   the blocks behind ceil(now / T) are given back: counted down, their entries -1.  now = 0: the sequence is finished.
+ *   d_parents[s] >= 0 (old = 0)   the sequence is forked: it shares the first d_shared_lens[s] tokens of sequence d_parents[s], as
+ *               the table has them before the call.  The whole blocks among these are named by both and counted; where they end
+ *               inside a block, the first block taken is to be a copy of it.  now >= d_shared_lens[s]: the rest are new tokens.
+ * Sequences get their blocks in order, the free ids in ascending order.  Blocks that the call itself frees are not handed out.
+ * New tokens: now less old, or less d_shared_lens[s].  Their rows are numbered in order of the sequences: d_q_starts[s] is the first of
+ * sequence s, as amoeba_batch wants it.  For every row r < num_rows d_positions[r] is the position of its token, d_first_positions[s]
+ * plus its place among the new ones (NULL: its cache index), and d_slots[r] = block * T + place in the block; rows behind the
+ * last get position 0 and slot -1.  d_q_starts NULL: rows are not numbered.
+ * d_pairs: (source, destination) blocks to be copied by amoeba_copy_blocks before the new tokens are appended, in order of the sequences,
+ * *d_num_pairs of them; the entries behind are not written.  pairs_cap 0: both may be NULL.
+ * d_lens_out: the lengths afterwards (it may be d_seq_lens).  *d_free_count: the free blocks afterwards.
+ *
+ * Device-detected errors.  INVALID_ARG, and the sequence stays as it is: a length that is negative, above 2^30 or needs more than
+ * max_blocks_per_seq blocks; d_parents[s] >= num_seqs, a fork with old != 0, with d_shared_lens[s] negative, above its parent's length
+ * or above now.  NO_FREE_BLOCKS: the first growing or forked sequence that there are not blocks enough for, and every growing or forked one
+ * behind it, stays as it is; d_lens_out tells which.  The same, with INVALID_ARG, where the rows exceed num_rows or the copies
+ * pairs_cap.  BAD_BLOCK_ID: a block id outside the pool, or one counted 0, that was to be shared, copied or given back; such an id
+ * is shared as it is, its pair's source is -1, and nothing is counted for it.  One code is reported, the first of these in this order.
+ * What is in the counts is the caller's to keep right: with wrong ones blocks may be handed out twice.
+ * TOO_LARGE: 20 bytes for each sequence and a bit for each of the pool's blocks / 8 do not fit in shared memory (11 000 sequences with
+ * 30 000 blocks, 1 000 with 13 million).
+ */
+typedef struct {
+    int32_t* d_block_table;           /* [num_seqs][max_blocks_per_seq], in and out */
+    int32_t* d_block_refs;            /* [num_blocks], in and out */
+    const int32_t* d_seq_lens;        /* [num_seqs] */
+    const int32_t* d_new_lens;        /* [num_seqs] */
+    const int32_t* d_parents;         /* [num_seqs], negative: none; or NULL: no forks */
+    const int32_t* d_shared_lens;     /* [num_seqs], read where there is a parent; NULL with d_parents */
+    int32_t* d_lens_out;              /* [num_seqs] */
+    int32_t* d_q_starts;              /* [num_seqs + 1], or NULL */
+    const int32_t* d_first_positions; /* [num_seqs], or NULL */
+    int32_t* d_positions;             /* [num_rows], or NULL */
+    int64_t* d_slots;                 /* [num_rows], or NULL */
+    int32_t* d_pairs;                 /* [pairs_cap][2] */
+    int32_t* d_num_pairs;
+    int32_t* d_free_count;            /* or NULL */
+    int32_t num_seqs, max_blocks_per_seq, num_rows, pairs_cap;
+} amoeba_table_step;
+AMOEBA_API amoeba_status amoeba_advance_tables(const amoeba_layout* layout, const amoeba_table_step* step, int32_t* d_status,
+                                    void* cuda_stream);
+
+/*
+ * amoeba_copy_blocks
+ *
+ * Copies blocks to other blocks of the same pools: for every pair k < min(*d_num_pairs, pairs_cap), in layers [layer_begin, layer_end) of
+ * all workers, block d_pairs[k][0] to block d_pairs[k][1].  Pairs with a negative id, or twice the same, are left out; so are those
+ * with an id outside the pool (BAD_BLOCK_ID).  A block may be the source of several pairs; none may be written twice, nor be both
+ * source and destination.  The elements are opaque (any elem_bytes, head_dim whose vectors are a multiple of 16 bytes).
+ */
+AMOEBA_API amoeba_status amoeba_copy_blocks(const amoeba_layout* layout, void* const* pools, const int32_t* d_pairs,
+                                 const int32_t* d_num_pairs, int32_t pairs_cap, int32_t layer_begin, int32_t layer_end,
+                                 int32_t* d_status, void* cuda_stream);
+
 /* Number of kernels the library has launched in this process (for launch accounting in benchmarks). */
 AMOEBA_API int64_t amoeba_launch_count(void);
 

@@ -85,6 +85,18 @@ class Batch(C.Structure):
                 ("max_q_len", C.c_int32)]
 
 
+class Prefixes(C.Structure):
+    _fields_ = [("d_group_starts", C.c_void_p), ("d_prefix_lens", C.c_void_p), ("num_groups", C.c_int32),
+                ("max_group_rows", C.c_int32)]
+
+
+class TableStep(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in (
+        "d_block_table", "d_block_refs", "d_seq_lens", "d_new_lens", "d_parents", "d_shared_lens", "d_lens_out", "d_q_starts",
+        "d_first_positions", "d_positions", "d_slots", "d_pairs", "d_num_pairs", "d_free_count")] + [
+        (n, C.c_int32) for n in ("num_seqs", "max_blocks_per_seq", "num_rows", "pairs_cap")]
+
+
 class Rotation(C.Structure):
     _fields_ = [("d_q_norm", C.c_void_p), ("d_k_norm", C.c_void_p), ("d_inv_freq", C.c_void_p),
                 ("d_positions", C.c_void_p), ("norm_eps", C.c_float), ("rot_dim", C.c_int32),
@@ -153,6 +165,11 @@ def _load():
         "amoeba_evict_workspace_bytes": (I32, [P(Layout), I32, I32, I32, P(I64)]),
         "amoeba_evict_kv": (I32, [P(Layout), I32, I32, P(VP), P(VP), VP, VP, I32, I32, VP, I32, I32, I32, VP, VP, VP, I64,
                                   VP]),
+        "amoeba_attend_shared_workspace_bytes": (I32, [P(Layout), P(Batch), P(Prefixes), P(I64)]),
+        "amoeba_attend_shared": (I32, [P(Layout), I32, I32, P(VP), P(Batch), P(Prefixes), P(VP), I64, C.c_float, P(VP), I64, VP, VP,
+                                       VP, I64, VP]),
+        "amoeba_advance_tables": (I32, [P(Layout), P(TableStep), VP, VP]),
+        "amoeba_copy_blocks": (I32, [P(Layout), P(VP), VP, VP, I32, I32, I32, VP, VP]),
         "amoeba_launch_count": (I64, []),
         "amoeba_status_string": (C.c_char_p, [I32]),
     }
@@ -602,6 +619,56 @@ def amoeba_evict_kv(layout: Layout, layer_begin: int, layer_end: int, pools: Seq
     be None if recent == budget."""
     _call("evict_kv", "amoeba_evict_kv", C.addressof(layout), layer_begin, layer_end, pools, score_pools, src_bt, seq_lens,
           dst_bt, budget, recent, new_lens, status, workspace, _handle(stream))
+
+
+def make_prefixes(group_starts, prefix_lens, max_group_rows: int) -> Prefixes:
+    """What groups of a batch's sequences share: group g is the sequences group_starts[g] .. group_starts[g + 1] - 1 (int32
+    [groups + 1]) and shares its first prefix_lens[g] tokens (int32 [groups]); max_group_rows: no group has more new tokens.
+    Keeps the tensors."""
+    import torch
+
+    dev, G = prefix_lens.device, prefix_lens.numel()
+    x = Prefixes(_tensor(group_starts, "make_prefixes", torch.int32, G + 1, dev), _tensor(prefix_lens, "make_prefixes", torch.int32, G, dev),
+                 G, max_group_rows)
+    x.index = dev.index if dev.type == "cuda" else -1
+    x.address, x.keep = C.addressof(x), (group_starts, prefix_lens)
+    return x
+
+
+def amoeba_attend_shared_workspace_bytes(layout: Layout, batch: Batch, prefixes: Prefixes) -> int:
+    out = C.c_int64()
+    _check(_load().amoeba_attend_shared_workspace_bytes(C.byref(layout), C.byref(batch), C.byref(prefixes), C.byref(out)),
+           "amoeba_attend_shared_workspace_bytes")
+    return out.value
+
+
+def amoeba_attend_shared(layout: Layout, dtype: int, layer: int, pools: Sequence, batch: Batch, prefixes: Prefixes, q: Sequence,
+                         scale: float, out: Sequence, lse, status, workspace, stream=None) -> None:
+    """amoeba_attend of sequences that share prefixes, each of which is read once."""
+    _call("attend_shared", "amoeba_attend_shared", C.addressof(layout), dtype, layer, pools, batch.address, batch.index,
+          prefixes.address, prefixes.index, q, scale, out, lse, status, workspace, _handle(stream))
+
+
+def amoeba_advance_tables(layout: Layout, block_table, block_refs, seq_lens, new_lens, parents, shared_lens, lens_out, q_starts,
+                          num_rows: int, first_positions, positions, slots, pairs, num_pairs, free_count, status, stream=None) -> None:
+    """Block table int32 [num_seqs, blocks] and counts int32 [num_blocks] from lengths seq_lens to new_lens (int32 [num_seqs]);
+    parents, shared_lens: forks, or both None; lens_out: the lengths afterwards.  For the new tokens, each of them or None: q_starts
+    int32 [num_seqs + 1], positions int32 [num_rows] (from first_positions, int32 [num_seqs], or the cache index), slots int64
+    [num_rows]; pairs int32 [most, 2] and num_pairs: blocks to be copied; free_count."""
+    _call("advance_tables", "amoeba_advance_tables", C.addressof(layout), block_table, block_refs, seq_lens, new_lens, parents,
+          shared_lens, lens_out, q_starts, num_rows, first_positions, positions, slots, pairs, num_pairs, free_count, status,
+          _handle(stream))
+
+
+def amoeba_copy_blocks(layout: Layout, pools: Sequence, pairs, num_pairs, layer_begin: int, layer_end: int, status,
+                       stream=None) -> None:
+    """Copies the first num_pairs (int32, on the device) of pairs (int32 [most, 2]: source, destination) inside the pools."""
+    _call("copy_blocks", "amoeba_copy_blocks", C.addressof(layout), pools, pairs, num_pairs, layer_begin, layer_end, status,
+          _handle(stream))
+
+
+__all__ += ["Prefixes", "TableStep", "make_prefixes", "amoeba_attend_shared_workspace_bytes", "amoeba_attend_shared",
+            "amoeba_advance_tables", "amoeba_copy_blocks"]
 
 
 def amoeba_launch_count() -> int:

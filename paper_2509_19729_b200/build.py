@@ -17,9 +17,9 @@ LIB = HERE / "libamoeba.so"
 LIB_CHECKED = HERE / "libamoeba_checked.so"  # the same sources with -DAMOEBA_CHECK_ITEMS: every work item is tested
 #                                              against the extent of its buffers before it is moved
 SOURCES = ["plan.cpp", "block_tables.cu", "kv_reshard.cu", "weights_reshard.cu", "append_kv.cu", "attend.cu", "attend_many.cu",
-           "scores.cu", "evict_kv.cu", "cache_maps.cu"]
+           "scores.cu", "evict_kv.cu", "cache_maps.cu", "advance_tables.cu", "copy_blocks.cu"]
 HEADERS = ["plan.hpp", "launch.hpp", "copy_engine.cuh", "kv_items.cuh", "w_items.cuh", "cache_view.cuh", "walk.cuh", "attend.cuh",
-           "warp_mma.cuh", "umma.cuh", "cache_maps.hpp"]
+           "warp_mma.cuh", "umma.cuh", "cache_maps.hpp", "cluster.cuh"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",

@@ -28,9 +28,9 @@ struct FewShape {
     static constexpr int kSmem = kFewWarps * kStages * kStage + kMerge;
 };
 
-template <class T, int D, int NT>
+template <class T, int D, int NT, class B>
 __global__ void __launch_bounds__(kFewThreads, FewShape<D, NT>::kCtas)
-attend_few(const __grid_constant__ AttendParams p) {
+attend_few(const __grid_constant__ AttendParams<B> p) {
     using F = FewShape<D, NT>;
     constexpr int R = 8 * NT, kSteps = D / 16, kPitch = D + 4;
     extern __shared__ __align__(128) char smem[];
@@ -58,7 +58,7 @@ attend_few(const __grid_constant__ AttendParams p) {
     grid_dependency_launch();
     if (n == 0) return;
 
-    Ahead<D, true, kFewTile> ahead(p.cache, p.batch, sh, p.status, walk, n, warp * 16);
+    Ahead<D, true, kFewTile, B> ahead(p.cache, p.batch, sh, p.status, walk, n, warp * 16);
     int slot_in = 0, slot = 0;
     auto load = [&] {
         if (ahead.left > 0) {
@@ -96,7 +96,7 @@ attend_few(const __grid_constant__ AttendParams p) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const int rr = first + t * 8 + pair * 2 + b;
-                    const int pos = walk.seq.len - walk.seq.qn + rr / sh.group;
+                    const int pos = last_seen(walk.seq, rr / sh.group);
                     see_hi[t][b] = rr < rows ? pos + 1 : 0;
                     see_lo[t][b] = sh.window > 0 ? pos - sh.window + 1 : 0;
                     m_run[t][b] = -INFINITY;
@@ -207,24 +207,20 @@ attend_few(const __grid_constant__ AttendParams p) {
 #pragma unroll
             for (int w = 0; w < kFewWarps; ++w) top = fmaxf(top, s_m[w][r]);
             const float ref = top == -INFINITY ? 0.f : top;
-            float l = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            Joined j;
+            j.top = top;
 #pragma unroll
             for (int w = 0; w < kFewWarps; ++w) {
                 const float f = fast_exp2(s_m[w][r] - ref);
                 const float4 x = *reinterpret_cast<const float4*>(s_o + (w * R + r) * kPitch + d);
-                l += f * s_l[w][r];
-                acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
+                j.l += f * s_l[w][r];
+                j.acc.x += f * x.x, j.acc.y += f * x.y, j.acc.z += f * x.z, j.acc.w += f * x.w;
             }
             if (direct) {
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                const int row = walk.m * R + r;
-                *reinterpret_cast<uint2*>(row_of<D>(p.out, p, walk.seq, walk.h, row) + d * 2) =
-                    make_uint2(Elem<T>::pack(acc.x * inv, acc.y * inv), Elem<T>::pack(acc.z * inv, acc.w * inv));
-                if (d == 0 && p.lse) *lse_of(p, walk.seq, walk.h, row) = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+                finish<T, D>(p, walk.seq, walk.h, walk.m * R + r, d, j);
             } else {
-                *reinterpret_cast<float4*>(p.part_o + (part + r) * D + d) = acc;
-                if (d == 0) p.part_m[part + r] = top, p.part_l[part + r] = l;
+                *reinterpret_cast<float4*>(p.part_o + (part + r) * D + d) = j.acc;
+                if (d == 0) p.part_m[part + r] = top, p.part_l[part + r] = j.l;
             }
         }
         __syncthreads();
@@ -242,20 +238,9 @@ constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 template <int kWarps>
 constexpr int kJoinRows = kWarps == 1 ? 4 * kJoinWarps : 1;  // of a block
 
-struct Joined {
-    float top = -INFINITY, l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    __device__ __forceinline__ void add(float top2, float l2, const float4& x) {
-        const float up = fmaxf(top, top2), ref = up == -INFINITY ? 0.f : up, f = fast_exp2(top - ref), g = fast_exp2(top2 - ref);
-        l = l * f + l2 * g;
-        acc.x = acc.x * f + x.x * g, acc.y = acc.y * f + x.y * g, acc.z = acc.z * f + x.z * g, acc.w = acc.w * f + x.w * g;
-        top = up;
-    }
-};
-
 // `groups` blocks to every share: the unit that it begins in is joined there, if that began in the share before.
-template <class T, int D, int kWarps>
-__device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int block, int groups) {
+template <class T, int D, int kWarps, class B>
+__device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, int block, int groups) {
     constexpr int kRows = kJoinRows<kWarps>, kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes to a part's row, parts at once
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int mine = block / groups, first_row = block % groups * kRows, R = p.shape.rows;
@@ -300,17 +285,13 @@ __device__ __forceinline__ void join_rows(const AttendParams& p, int ctas, int b
             for (int w = 1; w < kWarps; ++w) j.add(s_top[w], s_l[w], s_acc[w][lane % kLanes]);
         }
         if (r >= cut.rows || lane >= kLanes) continue;
-        const float inv = j.l == 0.f ? 0.f : 1.f / j.l;
-        const int row = cut.m * R + r;
-        *reinterpret_cast<uint2*>(row_of<D>(p.out, p, q, cut.h, row) + lane * 8) =
-            make_uint2(Elem<T>::pack(j.acc.x * inv, j.acc.y * inv), Elem<T>::pack(j.acc.z * inv, j.acc.w * inv));
-        if (lane == 0 && p.lse) *lse_of(p, q, cut.h, row) = j.l == 0.f ? -INFINITY : (j.top + log2f(j.l)) * kLn2;
+        finish<T, D>(p, q, cut.h, cut.m * R + r, lane * 4, j);
     }
 }
 // Blocks [0, few_ctas * few_rows) join what attend_few has cut, the others what attend_many has.
-template <class T, int D>
-__global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constant__ AttendParams few, int few_ctas, int few_rows,
-                                                            const __grid_constant__ AttendParams many, int many_ctas) {
+template <class T, int D, class B>
+__global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constant__ AttendParams<B> few, int few_ctas, int few_rows,
+                                                            const __grid_constant__ AttendParams<B> many, int many_ctas) {
     grid_dependency_wait();
     const int block = (int)blockIdx.x - few_ctas * few_rows;
     if (block < 0) join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x, few_rows);
@@ -322,7 +303,8 @@ constexpr int kMaxFewCtas = 2 * kMaxSms;
 constexpr int kMaxFewRows = 32;
 
 // One kernel's part of the workspace: where the shares begin, then the parts.
-static int64_t workspace_part(AttendParams* p, char* ws, int64_t parts, int64_t rows, int head_dim) {
+template <class B>
+static int64_t workspace_part(AttendParams<B>* p, char* ws, int64_t parts, int64_t rows, int head_dim) {
     const int64_t o = kMaxFewCtas * (int64_t)sizeof(Cut), m = o + parts * rows * head_dim * 4, l = m + parts * rows * 4;
     if (p) {
         p->cuts = reinterpret_cast<Cut*>(ws);
@@ -332,24 +314,26 @@ static int64_t workspace_part(AttendParams* p, char* ws, int64_t parts, int64_t 
     }
     return l + parts * rows * 4;
 }
-static int64_t few_workspace(AttendParams* p, char* ws, int head_dim) {
+template <class B>
+static int64_t few_workspace(AttendParams<B>* p, char* ws, int head_dim) {
     return workspace_part(p, ws, 2 * kMaxFewCtas, kMaxFewRows, head_dim);
 }
-static int64_t many_workspace(AttendParams* p, char* ws, int head_dim) {
+template <class B>
+static int64_t many_workspace(AttendParams<B>* p, char* ws, int head_dim) {
     return workspace_part(p, ws, 2 * kMaxSms, kManyRows, head_dim);
 }
 static int64_t rows_of(const amoeba_layout* l, int32_t max_q_len) {
     return (int64_t)max_q_len * (l->model.num_q_heads / l->model.num_kv_heads);
 }
 
-template <class T, int D, int NT>
-static amoeba_status run_few(AttendParams& p, int sms, int* ctas, cudaStream_t stream) {
+template <class T, int D, int NT, class B>
+static amoeba_status run_few(AttendParams<B>& p, int sms, int* ctas, cudaStream_t stream) {
     using F = FewShape<D, NT>;
     p.shape.rows = 8 * NT;
     p.shape.tile = kFewTile;
-    if (ensure_dynamic_smem((const void*)attend_few<T, D, NT>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    if (ensure_dynamic_smem((const void*)attend_few<T, D, NT, B>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
     *ctas = std::min(F::kCtas * sms, kMaxFewCtas);
-    return launch_kernel(attend_few<T, D, NT>, p.whole ? p.batch.num_seqs * p.shape.kv_heads : *ctas, kFewThreads, F::kSmem, stream,
+    return launch_kernel(attend_few<T, D, NT, B>, p.whole ? p.batch.num_seqs * p.shape.kv_heads : *ctas, kFewThreads, F::kSmem, stream,
                          false, p);
 }
 
@@ -358,23 +342,26 @@ static amoeba_status run_few(AttendParams& p, int sms, int* ctas, cudaStream_t s
 // ones gets both, and each skips the other's.  The launches follow one another closely: a kernel's blocks may be in place
 // before the kernel in front of it ends, and wait there for its results if they read them (attend_join) or end only after
 // it (attend_many).
-template <class T, int D>
-static amoeba_status run_attend(AttendParams& p, int tp, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
+template <class T, int D, class B>
+static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
     const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
     const int64_t few_bytes = few_workspace(&p, ws, D);
-    // In a batch with longer pieces attend_few gets the single tokens (and what has as few rows): its rows cost registers.
+    // In a batch with longer pieces attend_few gets the single tokens (and what has as few rows): its rows cost registers.  Groups
+    // all go to one kernel: small ones beside large ones are not worth a launch.
+    const bool groups = p.batch.by_groups(), few = !groups || rows <= kMaxFewRows;
     const int64_t few_rows = rows <= kMaxFewRows ? rows : p.shape.group;
-    const int most = few_rows <= 8 ? 8 : few_rows <= 16 ? 16 : kMaxFewRows;
+    const int most = !few ? 0 : few_rows <= 8 ? 8 : few_rows <= 16 ? 16 : kMaxFewRows;
     p.shape.min_rows = 0;
     p.shape.max_rows = most;
     int few_ctas = 0;
-    amoeba_status st = most == 8    ? run_few<T, D, 1>(p, sms, &few_ctas, stream)
+    amoeba_status st = !few         ? AMOEBA_OK
+                       : most == 8  ? run_few<T, D, 1>(p, sms, &few_ctas, stream)
                        : most == 16 ? run_few<T, D, 2>(p, sms, &few_ctas, stream)
                                     : run_few<T, D, 4>(p, sms, &few_ctas, stream);
     if (st != AMOEBA_OK || (p.whole && rows <= kMaxFewRows)) return st;
     if (p.whole) few_ctas = 0;  // nothing is cut
     const int few_most = (int)std::min<int64_t>(rows, most);
-    AttendParams many = p;
+    AttendParams<B> many = p;
     int many_ctas = 0, many_blocks = 0;
     if (rows > kMaxFewRows) {
         many_workspace(&many, ws + few_bytes, D);
@@ -386,7 +373,7 @@ static amoeba_status run_attend(AttendParams& p, int tp, int32_t dtype, char* ws
         many_blocks = many_ctas * (kManyRows / kJoinRows<1>);
         if ((st = launch_attend_many(many, tp, dtype, D, many_ctas, stream)) != AMOEBA_OK) return st;
     }
-    return launch_kernel(attend_join<T, D>, few_ctas * few_most + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_most, many,
+    return launch_kernel(attend_join<T, D, B>, few_ctas * few_most + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_most, many,
                          many_ctas);
 }
 
@@ -400,10 +387,61 @@ extern "C" amoeba_status amoeba_attend_workspace_bytes(const amoeba_layout* layo
     if (!layout || !batch || !bytes || batch->num_seqs < 0 || batch->max_q_len < 0) return AMOEBA_ERR_INVALID_ARG;
     const amoeba_status st = amoeba_layout_kv_pool_bytes(layout, &pool);
     if (st != AMOEBA_OK) return st;
-    *bytes = few_workspace(nullptr, nullptr, layout->model.head_dim);
+    *bytes = few_workspace<Batch>(nullptr, nullptr, layout->model.head_dim);
     if (rows_of(layout, batch->max_q_len) > kMaxFewRows)
-        *bytes += many_workspace(nullptr, nullptr, layout->model.head_dim);
+        *bytes += many_workspace<Batch>(nullptr, nullptr, layout->model.head_dim);
     return AMOEBA_OK;
+}
+
+// Checks the arguments that both calls have and fills in all but the workspace.
+template <class B>
+static amoeba_status make_params(const amoeba_layout* layout, int32_t dtype, int32_t layer, const void* const* pools,
+                                 const amoeba_batch* batch, const void* const* q, int64_t q_stride, float scale, int32_t window,
+                                 void* const* out, int64_t out_stride, float* d_lse, int32_t* d_status, AttendParams<B>* p) {
+    amoeba_status st;
+    if ((st = check_elements(layout, dtype)) != AMOEBA_OK) return st;
+    if ((st = make_cache_view(layout, layer, pools, &p->cache)) != AMOEBA_OK) return st;
+    if ((st = make_batch(batch, &p->batch)) != AMOEBA_OK) return st;
+    if (!d_status || window < 0 || !positive(scale)) return AMOEBA_ERR_INVALID_ARG;
+    const amoeba_model& m = layout->model;
+    const int64_t row = (int64_t)m.num_q_heads / layout->tp * m.head_dim;
+    if ((st = make_rows(layout, p->batch, q, q_stride, row, &p->q)) != AMOEBA_OK) return st;
+    if ((st = make_rows(layout, p->batch, out, out_stride, row, &p->out)) != AMOEBA_OK) return st;
+    for (int r = 0; r < layout->tp; ++r)  // other CTAs may still read the rows that one has answered
+        for (int o = 0; o < layout->tp; ++o)
+            if (q[r] && q[r] == out[o]) return AMOEBA_ERR_INVALID_ARG;
+    p->lse = d_lse;
+    p->status = d_status;
+#ifdef AMOEBA_CHECK_ITEMS
+    p->polls = operator_wait_polls();
+#endif
+    p->scale_log2 = scale * kLog2e;
+    p->q_heads = m.num_q_heads;
+    p->shape.group = m.num_q_heads / m.num_kv_heads;
+    p->shape.kv_heads = m.num_kv_heads;
+    p->shape.window = std::min(window, 1 << 30);
+    return AMOEBA_OK;
+}
+
+// (units are numbered in 32 bits)
+static bool units_fit(const amoeba_layout* l, int64_t num_seqs, int64_t rows) {
+    return rows <= INT32_MAX && num_seqs * l->model.num_kv_heads <= INT32_MAX / (rows / kManyRows + 1);
+}
+
+// Short sequences are not worth cutting: what the shares and the join take, about 5 us, is what a CTA needs for 512
+// tokens, or for 1024 when there are units enough to fill the GPU (one sequence of 256 tokens, 8 key heads: 7.9 us whole,
+// 9.5 cut; of 1024: 20.5 and 11.3; 32 sequences of 1024: 24 and 29; of 2048: 41 and 47, but there one long one would
+// hold up all).  With max_q_len 0 sequences are only looked at.
+template <class B>
+static amoeba_status attend_pass(const amoeba_layout* layout, int32_t dtype, AttendParams<B>& p, char* ws, int sms, cudaStream_t stream) {
+    const amoeba_model& m = layout->model;
+    const int64_t tokens = (int64_t)p.batch.max_blocks * layout->block_tokens;
+    p.whole = rows_of(layout, p.batch.max_q_len) == 0 || tokens <= 512 || (tokens <= 1024 && p.batch.num_seqs * m.num_kv_heads >= sms);
+    if (dtype == AMOEBA_FP16)
+        return m.head_dim == 64 ? run_attend<__half, 64>(p, layout->tp, dtype, ws, sms, stream)
+                                : run_attend<__half, 128>(p, layout->tp, dtype, ws, sms, stream);
+    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, layout->tp, dtype, ws, sms, stream)
+                            : run_attend<__nv_bfloat16, 128>(p, layout->tp, dtype, ws, sms, stream);
 }
 
 extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtype, int32_t layer,
@@ -411,50 +449,147 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
                                        int64_t q_stride, float scale, int32_t window, void* const* out,
                                        int64_t out_stride, float* d_lse, int32_t* d_status, void* d_workspace,
                                        int64_t workspace_bytes, void* cuda_stream) {
-    AttendParams p{};
-    amoeba_status st;
-    if ((st = check_elements(layout, dtype)) != AMOEBA_OK) return st;
-    if ((st = make_cache_view(layout, layer, pools, &p.cache)) != AMOEBA_OK) return st;
-    if ((st = make_batch(batch, &p.batch)) != AMOEBA_OK) return st;
-    if (!d_status || window < 0 || !positive(scale)) return AMOEBA_ERR_INVALID_ARG;
-    const amoeba_model& m = layout->model;
-    const int64_t row = (int64_t)m.num_q_heads / layout->tp * m.head_dim;
-    if ((st = make_rows(layout, p.batch, q, q_stride, row, &p.q)) != AMOEBA_OK) return st;
-    if ((st = make_rows(layout, p.batch, out, out_stride, row, &p.out)) != AMOEBA_OK) return st;
-    for (int r = 0; r < layout->tp; ++r)  // other CTAs may still read the rows that one has answered
-        for (int o = 0; o < layout->tp; ++o)
-            if (q[r] && q[r] == out[o]) return AMOEBA_ERR_INVALID_ARG;
+    AttendParams<Batch> p{};
+    amoeba_status st = make_params(layout, dtype, layer, pools, batch, q, q_stride, scale, window, out, out_stride, d_lse, d_status, &p);
+    if (st != AMOEBA_OK) return st;
     int64_t need = 0;
     if ((st = amoeba_attend_workspace_bytes(layout, batch, &need)) != AMOEBA_OK) return st;
     if (!d_workspace || workspace_bytes < need) return AMOEBA_ERR_INVALID_ARG;
     if ((uintptr_t)d_workspace % 16) return AMOEBA_ERR_ALIGNMENT;
     if (p.batch.num_seqs == 0 || p.batch.num_rows == 0) return AMOEBA_OK;
-    p.lse = d_lse;
-    p.status = d_status;
-#ifdef AMOEBA_CHECK_ITEMS
-    p.polls = operator_wait_polls();
-#endif
-    p.scale_log2 = scale * kLog2e;
-    p.q_heads = m.num_q_heads;
-    p.shape.group = m.num_q_heads / m.num_kv_heads;
-    p.shape.kv_heads = m.num_kv_heads;
-    p.shape.window = std::min(window, 1 << 30);
-    // (units are numbered in 32 bits)
-    const int64_t rows = rows_of(layout, p.batch.max_q_len);
-    if (rows > INT32_MAX || (int64_t)p.batch.num_seqs * m.num_kv_heads > INT32_MAX / (rows / kManyRows + 1)) return AMOEBA_ERR_UNSUPPORTED;
+    if (!units_fit(layout, p.batch.num_seqs, rows_of(layout, p.batch.max_q_len))) return AMOEBA_ERR_UNSUPPORTED;
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
-    // Short sequences are not worth cutting: what the shares and the join take, about 5 us, is what a CTA needs for 512
-    // tokens, or for 1024 when there are units enough to fill the GPU (one sequence of 256 tokens, 8 key heads: 7.9 us whole,
-    // 9.5 cut; of 1024: 20.5 and 11.3; 32 sequences of 1024: 24 and 29; of 2048: 41 and 47, but there one long one would
-    // hold up all).  With max_q_len 0 sequences are only looked at.
-    const int64_t tokens = (int64_t)p.batch.max_blocks * layout->block_tokens;
-    p.whole = rows == 0 || tokens <= 512 || (tokens <= 1024 && p.batch.num_seqs * m.num_kv_heads >= dev.sms);
+    return attend_pass(layout, dtype, p, static_cast<char*>(d_workspace), dev.sms, static_cast<cudaStream_t>(cuda_stream));
+}
+
+// ------------------------------------------------------------------------------------------------ shared prefixes
+// amoeba_attend_shared is two passes of the above.  The softmax's sums over disjoint sets of tokens join by their maxima:
+//   m = max(m1, m2),   l = l1 2^(m1 - m) + l2 2^(m2 - m),   o = o1 2^(m1 - m) + o2 2^(m2 - m),   out = o / l.
+// First the groups as if each were one sequence with all rows of its sequences, every row seeing the whole prefix: that reads the
+// prefix once, and has rows enough for the tensor cores where a sequence by itself has a few.  Its sums stay in 32 bits, not yet
+// divided, in the workspace (the carry); the pass over the sequences' own tokens takes them up where it ends a row.
+
+struct PrefixParams {
+    Batch batch;
+    const int32_t *group_starts, *prefix_lens;
+    Group* groups;
+    int32_t *first, *status;
+    int32_t num_groups, max_group_rows, block_tokens;
+};
+
+// What a group shares: no more than its shortest sequence has in front of its new tokens, and nothing where fewer than two have
+// rows or one is bad; then its sequences attend by themselves.  One block, a warp to a group.
+constexpr int kPrefixThreads = 1024;
+__global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_constant__ PrefixParams p) {
+    const int tid = threadIdx.x, lane = tid % 32, S = p.batch.num_seqs;
+    bool bad = false;
+    for (int g = tid; g < p.num_groups; g += kPrefixThreads) {
+        const int a = p.group_starts[g], z = p.group_starts[g + 1];
+        bad |= a < 0 || z < a || z > S;
+    }
+    for (int s = tid; s < S; s += kPrefixThreads) p.first[s] = 0;
+    bad = __syncthreads_or(bad);
+    if (bad && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
+    for (int g = tid / 32; g < p.num_groups; g += kPrefixThreads / 32) {
+        const int a = bad ? 0 : p.group_starts[g], z = bad ? 0 : p.group_starts[g + 1];
+        int least = INT32_MAX, row = INT32_MAX, with_rows = 0, q0 = INT32_MAX, q1 = 0;
+        bool ok = true;
+        for (int s = a + lane; s < z; s += 32) {
+            const Seq q = sequence(p.batch, s, p.block_tokens);
+            ok &= q.ok;
+            if (q.qn == 0) continue;
+            least = min(least, q.len - q.qn);
+            row = min(row, s);
+            q0 = min(q0, q.q0);
+            q1 = max(q1, q.q0 + q.qn);
+            ++with_rows;
+        }
+        ok = __all_sync(~0u, ok);
+        least = __reduce_min_sync(~0u, least);
+        row = __reduce_min_sync(~0u, row);
+        with_rows = __reduce_add_sync(~0u, with_rows);
+        q0 = __reduce_min_sync(~0u, q0);
+        q1 = __reduce_max_sync(~0u, q1);
+        Group out{0, 0, 0, 0};
+        if (z > a) {
+            const int len = p.prefix_lens[g];
+            const bool wrong = len < 0 || (with_rows && q1 - q0 > p.max_group_rows);
+            if (wrong && lane == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
+            if (!wrong && ok && with_rows > 1 && min(len, least) > 0) {
+                out = Group{q0, q1 - q0, min(len, least), row};
+                for (int s = a + lane; s < z; s += 32) p.first[s] = out.len;
+            }
+        }
+        if (lane == 0) p.groups[g] = out;
+    }
+}
+
+// Where the parts of the workspace begin: both passes' own, the carry, the groups and the sequences' first tokens.
+struct SharedSpace {
+    int64_t groups_pass, rest_pass, carry_o, carry_m, carry_l, groups, first, end;
+};
+static SharedSpace shared_space(const amoeba_layout* l, const amoeba_batch* b, const amoeba_prefixes* x) {
+    const int D = l->model.head_dim;
+    const int64_t few = few_workspace<Batch>(nullptr, nullptr, D), many = many_workspace<Batch>(nullptr, nullptr, D);
+    const int64_t heads = ((int64_t)b->num_rows * l->model.num_q_heads + 3) / 4 * 4;
+    SharedSpace s;
+    s.groups_pass = 0;
+    s.rest_pass = few + (rows_of(l, x->max_group_rows) > kMaxFewRows ? many : 0);
+    s.carry_o = s.rest_pass + few + (rows_of(l, b->max_q_len) > kMaxFewRows ? many : 0);
+    s.carry_m = s.carry_o + heads * D * 4;
+    s.carry_l = s.carry_m + heads * 4;
+    s.groups = s.carry_l + heads * 4;
+    s.first = s.groups + (int64_t)x->num_groups * sizeof(Group);
+    s.end = s.first + ((int64_t)b->num_seqs * 4 + 15) / 16 * 16;
+    return s;
+}
+
+extern "C" amoeba_status amoeba_attend_shared_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
+                                                              const amoeba_prefixes* prefixes, int64_t* bytes) {
+    int64_t pool = 0;
+    if (!layout || !batch || !prefixes || !bytes || batch->num_seqs < 0 || batch->max_q_len < 0 || batch->num_rows < 0 ||
+        prefixes->num_groups < 0 || prefixes->max_group_rows < 0)
+        return AMOEBA_ERR_INVALID_ARG;
+    const amoeba_status st = amoeba_layout_kv_pool_bytes(layout, &pool);
+    if (st != AMOEBA_OK) return st;
+    *bytes = shared_space(layout, batch, prefixes).end;
+    return AMOEBA_OK;
+}
+
+extern "C" amoeba_status amoeba_attend_shared(const amoeba_layout* layout, int32_t dtype, int32_t layer, const void* const* pools,
+                                              const amoeba_batch* batch, const amoeba_prefixes* prefixes, const void* const* q,
+                                              int64_t q_stride, float scale, void* const* out, int64_t out_stride, float* d_lse,
+                                              int32_t* d_status, void* d_workspace, int64_t workspace_bytes, void* cuda_stream) {
+    AttendParams<SharedBatch> p{};
+    amoeba_status st = make_params(layout, dtype, layer, pools, batch, q, q_stride, scale, 0, out, out_stride, d_lse, d_status, &p);
+    if (st != AMOEBA_OK) return st;
+    int64_t need = 0;
+    if ((st = amoeba_attend_shared_workspace_bytes(layout, batch, prefixes, &need)) != AMOEBA_OK) return st;
+    if (prefixes->num_groups && (!prefixes->d_group_starts || !prefixes->d_prefix_lens)) return AMOEBA_ERR_INVALID_ARG;
+    if (!d_workspace || workspace_bytes < need) return AMOEBA_ERR_INVALID_ARG;
+    if ((uintptr_t)d_workspace % 16) return AMOEBA_ERR_ALIGNMENT;
+    if (p.batch.num_seqs == 0 || p.batch.num_rows == 0) return AMOEBA_OK;
+    const int32_t group_rows = std::min(prefixes->max_group_rows, p.batch.num_rows);
+    if (!units_fit(layout, p.batch.num_seqs, rows_of(layout, p.batch.max_q_len)) ||
+        !units_fit(layout, prefixes->num_groups, rows_of(layout, group_rows)))
+        return AMOEBA_ERR_UNSUPPORTED;
+    const DeviceInfo dev = cached_device_info();
+    if (!dev.sms) return AMOEBA_ERR_CUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(d_workspace);
-    if (dtype == AMOEBA_FP16)
-        return m.head_dim == 64 ? run_attend<__half, 64>(p, layout->tp, dtype, ws, dev.sms, stream)
-                                : run_attend<__half, 128>(p, layout->tp, dtype, ws, dev.sms, stream);
-    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, layout->tp, dtype, ws, dev.sms, stream)
-                            : run_attend<__nv_bfloat16, 128>(p, layout->tp, dtype, ws, dev.sms, stream);
+    const SharedSpace at = shared_space(layout, batch, prefixes);
+    p.carry = Carry{reinterpret_cast<float*>(ws + at.carry_o), reinterpret_cast<float*>(ws + at.carry_m), reinterpret_cast<float*>(ws + at.carry_l)};
+    PrefixParams x{p.batch, prefixes->d_group_starts, prefixes->d_prefix_lens, reinterpret_cast<Group*>(ws + at.groups),
+                   reinterpret_cast<int32_t*>(ws + at.first), d_status, prefixes->num_groups, group_rows, layout->block_tokens};
+    if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, false, x)) != AMOEBA_OK) return st;
+    p.batch.first = x.first;
+    if (prefixes->num_groups && group_rows) {
+        AttendParams<SharedBatch> g = p;
+        g.batch.groups = x.groups;
+        g.batch.num_seqs = prefixes->num_groups;
+        g.batch.max_q_len = group_rows;
+        if ((st = attend_pass(layout, dtype, g, ws + at.groups_pass, dev.sms, stream)) != AMOEBA_OK) return st;
+    }
+    return attend_pass(layout, dtype, p, ws + at.rest_pass, dev.sms, stream);
 }

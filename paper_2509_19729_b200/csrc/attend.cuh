@@ -4,9 +4,17 @@
 
 namespace amoeba {
 
+// What a row has from its sequence's prefix, for every query head, before it is divided: sums of weights times values, the largest
+// logit in powers of two and the sum of the weights.
+struct Carry {
+    float *o, *m, *l;  // [num_rows][query heads][D], [num_rows][query heads]
+};
+
+// B: Batch, or SharedBatch: then the groups' pass writes the carry and the sequences' pass takes it up.
+template <class B>
 struct AttendParams {
     CacheView cache;
-    Batch batch;
+    B batch;
     Rows q, out;
     Shape shape;
     float* lse;
@@ -16,26 +24,63 @@ struct AttendParams {
     float scale_log2;        // scale * log2(e): the softmax runs in powers of two
     int32_t q_heads;         // of all workers
     int32_t whole;           // 1: one CTA per unit, nothing is cut
+    Carry carry;             // of a SharedBatch
 #ifdef AMOEBA_CHECK_ITEMS
     int32_t polls;           // of every wait in attend_many
 #endif
 };
 
 // Where row r of a unit lies in a row buffer.
-template <int D>
-__device__ __forceinline__ char* row_of(const Rows& rows, const AttendParams& p, const Seq& q, int kv_head, int r) {
+template <int D, class B>
+__device__ __forceinline__ char* row_of(const Rows& rows, const AttendParams<B>& p, const Seq& q, int kv_head, int r) {
     const int w = kv_head / p.cache.heads, h = kv_head - w * p.cache.heads, g = p.shape.group;
     const int tok = r / g;
     return rows.base[w] + (int64_t)(q.q0 + tok) * rows.stride + (h * g + r - tok * g) * (D * 2);
 }
-__device__ __forceinline__ float* lse_of(const AttendParams& p, const Seq& q, int kv_head, int r) {
+// Its place among the rows and query heads of all workers.
+template <class B>
+__device__ __forceinline__ int64_t head_of(const AttendParams<B>& p, const Seq& q, int kv_head, int r) {
     const int g = p.shape.group, tok = r / g;
-    return p.lse + (int64_t)(q.q0 + tok) * p.q_heads + kv_head * g + r - tok * g;
+    return (int64_t)(q.q0 + tok) * p.q_heads + kv_head * g + r - tok * g;
+}
+template <class B>
+__device__ __forceinline__ float* lse_of(const AttendParams<B>& p, const Seq& q, int kv_head, int r) {
+    return p.lse + head_of(p, q, kv_head, r);
+}
+
+// Sums of one or more parts of a row, four of its values.
+struct Joined {
+    float top = -INFINITY, l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    __device__ __forceinline__ void add(float top2, float l2, const float4& x) {
+        const float up = fmaxf(top, top2), ref = up == -INFINITY ? 0.f : up, f = fast_exp2(top - ref), g = fast_exp2(top2 - ref);
+        l = l * f + l2 * g;
+        acc.x = acc.x * f + x.x * g, acc.y = acc.y * f + x.y * g, acc.z = acc.z * f + x.z * g, acc.w = acc.w * f + x.w * g;
+        top = up;
+    }
+};
+// What a unit's row comes to, its values d .. d + 3: into the carry, or with what is carried to the output.
+template <class T, int D, class B>
+__device__ __forceinline__ void finish(const AttendParams<B>& p, const Seq& q, int kv_head, int row, int d, Joined& j) {
+    if (B::kShared && (q.level || q.first > 0)) {
+        const int64_t at = head_of(p, q, kv_head, row);
+        if (q.level) {
+            *reinterpret_cast<float4*>(p.carry.o + at * D + d) = j.acc;
+            if (d == 0) p.carry.m[at] = j.top, p.carry.l[at] = j.l;
+            return;
+        }
+        j.add(p.carry.m[at], p.carry.l[at], *reinterpret_cast<const float4*>(p.carry.o + at * D + d));
+    }
+    const float inv = j.l == 0.f ? 0.f : 1.f / j.l;
+    *reinterpret_cast<uint2*>(row_of<D>(p.out, p, q, kv_head, row) + d * 2) =
+        make_uint2(Elem<T>::pack(j.acc.x * inv, j.acc.y * inv), Elem<T>::pack(j.acc.z * inv, j.acc.w * inv));
+    if (d == 0 && p.lse) *lse_of(p, q, kv_head, row) = j.l == 0.f ? -INFINITY : (j.top + log2f(j.l)) * kLn2;
 }
 
 // The kernel for many rows (attend_many.cu): 256 rows a unit, 128 tokens a tile.
 constexpr int kManyRows = 256, kManyTile = 128;
 constexpr int kMaxSms = 192;  // bounds the grids, and so the workspace, without asking the device
-amoeba_status launch_attend_many(const AttendParams& p, int tp, int32_t dtype, int head_dim, int ctas, cudaStream_t stream);
+template <class B>
+amoeba_status launch_attend_many(const AttendParams<B>& p, int tp, int32_t dtype, int head_dim, int ctas, cudaStream_t stream);
 
 }  // namespace amoeba

@@ -61,10 +61,11 @@ struct Share {
 };
 
 // All threads of the block.  False: this CTA has nothing to do.  done: [kMaxSms] for the tiles of the units dealt to every CTA.
-__device__ bool make_share(const AttendParams& p, Share& sh, int32_t* done) {
+template <class B>
+__device__ bool make_share(const AttendParams<B>& p, Share& sh, int32_t* done) {
     __shared__ int64_t s_warp[kManyThreads / 32];
     const Shape& shape = p.shape;
-    const Batch& b = p.batch;
+    const B& b = p.batch;
     const int tid = threadIdx.x, ctas = gridDim.x, T = p.cache.block_tokens, S = b.num_seqs;
     sh.rounds = 0;
     if (S > kDealtSeqs) {
@@ -196,7 +197,8 @@ struct Parts {
     int64_t left;
 
     __device__ __forceinline__ Parts(const Share& sh) : left(sh.end - sh.begin) {}
-    __device__ __forceinline__ bool next(const AttendParams& p, const Share& sh) {
+    template <class B>
+    __device__ __forceinline__ bool next(const AttendParams<B>& p, const Share& sh) {
         const Shape& shape = p.shape;
         if (round < sh.rounds) {
             const int u = blockIdx.x + round++ * gridDim.x;
@@ -231,16 +233,16 @@ struct Parts {
 };
 
 // ---- loading
-template <int D>
+template <int D, class B>
 struct Loader : TileLoader<D, kLoadWarps> {
     using Base = TileLoader<D, kLoadWarps>;
-    const AttendParams& p;
+    const AttendParams<B>& p;
     const uint32_t smem;  // two query tiles, then the ring
     ManyBarriers& b;
     RingPlace at;
     static constexpr int kTile = ManyShape<D>::kTileBytes;
 
-    __device__ __forceinline__ Loader(const AttendParams& p_, const CacheMaps& maps, int box_rows, uint32_t smem_, ManyBarriers& b_, int warp,
+    __device__ __forceinline__ Loader(const AttendParams<B>& p_, const CacheMaps& maps, int box_rows, uint32_t smem_, ManyBarriers& b_, int warp,
                                       int lane)
         : Base(p_.cache, maps, box_rows, warp, lane), p(p_), smem(smem_), b(b_) {}
     // Starts the loads of the tile's keys (kv = 0) or values (1).
@@ -259,9 +261,9 @@ struct Loader : TileLoader<D, kLoadWarps> {
     }
 };
 
-template <int D>
-__device__ RingPlace load_loop(const AttendParams& p, const CacheMaps& maps, int box_rows, const Share& share, char* smem, ManyBarriers& b) {
-    Loader<D> load(p, maps, box_rows, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32);
+template <int D, class B>
+__device__ RingPlace load_loop(const AttendParams<B>& p, const CacheMaps& maps, int box_rows, const Share& share, char* smem, ManyBarriers& b) {
+    Loader<D, B> load(p, maps, box_rows, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32);
     uint32_t q_phase = 1;
     bool ok = true;
     Parts part(share);
@@ -286,8 +288,8 @@ __device__ RingPlace load_loop(const AttendParams& p, const CacheMaps& maps, int
 }
 
 // ---- products: one warp, one of its lanes issues
-template <class T, int D>
-__device__ bool multiply(const AttendParams& p, const Share& share, uint32_t smem, ManyBarriers& b) {
+template <class T, int D, class B>
+__device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t smem, ManyBarriers& b) {
     constexpr int kTile = ManyShape<D>::kTileBytes, kStages = ManyShape<D>::kStages;
     constexpr uint32_t kS = product<T>(128, false), kO = product<T>(D, true);
     const uint32_t tmem = __shfl_sync(~0u, b.tmem, 0), leader = elect_one();
@@ -445,8 +447,8 @@ __device__ __forceinline__ float row_weights(uint32_t s_tmem, float c, float ref
     return a + b;
 }
 
-template <class T, int D>
-__device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers& b) {
+template <class T, int D, class B>
+__device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarriers& b) {
     const Shape& sh = p.shape;
     const int t = threadIdx.x / 128, r = threadIdx.x;  // row of the unit
     const uint32_t lanes = (uint32_t)(threadIdx.x % 128 / 32 * 32) << 16;
@@ -461,7 +463,7 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
     while (part.next(p, share)) {
         const Walk& w = part.w;
         // a bad block anywhere in the unit: its tokens are looked up one by one below
-        const int32_t* table = p.batch.table + (int64_t)w.s * p.batch.max_blocks;
+        const int32_t* table = p.batch.table + (int64_t)w.seq.row * p.batch.max_blocks;
         int bad = 0;
         for (int i = w.range.lo / p.cache.block_tokens + (int)threadIdx.x % 128; i * (int64_t)p.cache.block_tokens < w.range.hi; i += 128)
             bad |= table[i] < 0 || table[i] >= p.cache.num_blocks;
@@ -473,9 +475,10 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
         if (ok && t < part.q_tiles) ok = [&] {
             const int row = w.m * kManyRows + r;
             const bool there = r < part.rows;
-            const int pos = w.seq.len - w.seq.qn + row / sh.group;
+            const int pos = last_seen(w.seq, row / sh.group);
             // (rows that are not there see zeros or anything: nothing is written for them)
-            const int see_hi = there ? pos + 1 : INT32_MAX, see_lo = there && sh.window > 0 ? max(pos - sh.window + 1, 0) : 0;
+            const int see_hi = there ? pos + 1 : INT32_MAX,
+                      see_lo = !there ? 0 : sh.window > 0 ? max(pos - sh.window + 1, 0) : B::kShared ? w.seq.first : 0;
             float m_ref = -INFINITY, l = 0.f;
             for (int i = 0; i < part.tiles; ++i) {
                 const int key0 = w.range.base + (w.t + i) * kManyTile;
@@ -517,9 +520,21 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
             if (!wait(&b.o_full[t], o_phase ^ 1)) return false;
             tmem_fence_after();
             const bool direct = part.from_start && part.to_end;
+            // With a carry: into it (a group's rows), or taken up, own sums by `keep` and the carried ones by `take`.
+            const bool into = B::kShared && w.seq.level, takes = B::kShared && direct && there && w.seq.first > 0;
+            const int64_t head = B::kShared && there ? head_of(p, w.seq, w.h, row) : 0;
+            float keep = 1.f, take = 0.f;
+            if (takes) {
+                const float m2 = p.carry.m[head], up = fmaxf(m_ref, m2), ref = up == -INFINITY ? 0.f : up;
+                keep = fast_exp2(m_ref - ref), take = fast_exp2(m2 - ref);
+                l = l * keep + p.carry.l[head] * take;
+                m_ref = up;
+            }
             const float inv = l == 0.f ? 0.f : 1.f / l;
+            keep *= inv, take *= inv;
             const int64_t at = (int64_t)(2 * blockIdx.x + (part.from_start ? 1 : 0)) * kManyRows + r;
             char* out = there ? row_of<D>(p.out, p, w.seq, w.h, row) : nullptr;
+            float* const raw = direct ? p.carry.o + head * D : p.part_o + at * D;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 uint32_t o[32];
@@ -527,26 +542,37 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
                 tmem_load32(o, o_tmem + j * 32);
                 tmem_load_wait();
                 if (!there) continue;
-                if (direct) {
+                if (direct && !into) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
+                    if (takes)
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4) {
+                            const float4 c4 = *reinterpret_cast<const float4*>(p.carry.o + head * D + j * 32 + k);
+                            o[k] = __float_as_uint(__uint_as_float(o[k]) + c4.x * take);
+                            o[k + 1] = __float_as_uint(__uint_as_float(o[k + 1]) + c4.y * take);
+                            o[k + 2] = __float_as_uint(__uint_as_float(o[k + 2]) + c4.z * take);
+                            o[k + 3] = __float_as_uint(__uint_as_float(o[k + 3]) + c4.w * take);
+                        }
 #pragma unroll
                     for (int k = 0; k < 32; k += 8) {
                         uint32_t x[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            x[i] = Elem<T>::pack(__uint_as_float(o[k + 2 * i]) * inv, __uint_as_float(o[k + 2 * i + 1]) * inv);
+                            x[i] = Elem<T>::pack(__uint_as_float(o[k + 2 * i]), __uint_as_float(o[k + 2 * i + 1]));
                         *reinterpret_cast<uint4*>(out + (j * 32 + k) * 2) = make_uint4(x[0], x[1], x[2], x[3]);
                     }
                 } else {
 #pragma unroll
                     for (int k = 0; k < 32; k += 4)
-                        *reinterpret_cast<uint4*>(p.part_o + at * D + j * 32 + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                        *reinterpret_cast<uint4*>(raw + j * 32 + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                 }
             }
             tmem_fence_before();
             mbar_arrive(&b.o_free[t]);
             if (there && !direct) p.part_m[at] = m_ref, p.part_l[at] = l;
-            if (there && direct && p.lse)
-                *lse_of(p, w.seq, w.h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
+            else if (there && into) p.carry.m[head] = m_ref, p.carry.l[head] = l;
+            else if (there && p.lse) *lse_of(p, w.seq, w.h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
             return true;
         }();
         if (!ok) b.abort = 1;
@@ -554,14 +580,15 @@ __device__ bool softmax(const AttendParams& p, const Share& share, ManyBarriers&
     return ok;
 }
 
-template <class T, int D>
-__global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_constant__ AttendParams p, const __grid_constant__ CacheMaps maps,
+template <class T, int D, class B>
+__global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_constant__ AttendParams<B> p, const __grid_constant__ CacheMaps maps,
                                                             int box_rows) {
     extern __shared__ char smem_raw[];
     __shared__ ManyBarriers b;
     char* smem = smem_raw + (1024 - smem_u32(smem_raw) % 1024) % 1024;
     const int warp = threadIdx.x / 32;
     __shared__ Share share;
+    if (B::kShared) grid_dependency_wait();  // the groups are there
     const bool busy = make_share(p, share, reinterpret_cast<int32_t*>(smem));
     grid_dependency_launch();
     if (!busy) {
@@ -609,18 +636,21 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     if (warp > 8 && b.abort) drain_ring<ManyShape<D>::kStages>(b.full, loaded);
 }
 
-template <class T, int D>
-static amoeba_status launch(const AttendParams& p, const CacheMaps& maps, int box_rows, int ctas, cudaStream_t stream) {
-    if (ensure_dynamic_smem((const void*)attend_many<T, D>, ManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    return launch_kernel(attend_many<T, D>, ctas, kManyThreads, ManyShape<D>::kSmem, stream, true, p, maps, box_rows);
+template <class T, int D, class B>
+static amoeba_status launch(const AttendParams<B>& p, const CacheMaps& maps, int box_rows, int ctas, cudaStream_t stream) {
+    if (ensure_dynamic_smem((const void*)attend_many<T, D, B>, ManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    return launch_kernel(attend_many<T, D, B>, ctas, kManyThreads, ManyShape<D>::kSmem, stream, true, p, maps, box_rows);
 }
 
-amoeba_status launch_attend_many(const AttendParams& p, int tp, int32_t dtype, int head_dim, int ctas, cudaStream_t stream) {
+template <class B>
+amoeba_status launch_attend_many(const AttendParams<B>& p, int tp, int32_t dtype, int head_dim, int ctas, cudaStream_t stream) {
     CacheMaps maps;
     const int rows = make_cache_maps(&maps, p.cache, tp, head_dim, dtype);
     if (dtype == AMOEBA_FP16)
         return head_dim == 64 ? launch<__half, 64>(p, maps, rows, ctas, stream) : launch<__half, 128>(p, maps, rows, ctas, stream);
     return head_dim == 64 ? launch<__nv_bfloat16, 64>(p, maps, rows, ctas, stream) : launch<__nv_bfloat16, 128>(p, maps, rows, ctas, stream);
 }
+template amoeba_status launch_attend_many(const AttendParams<Batch>&, int, int32_t, int, int, cudaStream_t);
+template amoeba_status launch_attend_many(const AttendParams<SharedBatch>&, int, int32_t, int, int, cudaStream_t);
 
 }  // namespace amoeba

@@ -6,6 +6,7 @@
 // which the selection is 25 (latency: one unit takes a CTA 10 to 20 us) and the move 84 (5.6 TB/s of rows of 256 bytes); one of
 // 131072 cut to 16384: 51 us, 25 and 22.  (Both in one kernel took 117 and 67 us.)
 #include "cache_view.cuh"
+#include "cluster.cuh"
 #include "copy_engine.cuh"
 
 namespace amoeba {
@@ -21,45 +22,6 @@ struct EvictParams {
     int32_t num_seqs, max_blocks, dst_max_blocks, budget, recent, kv_heads, layers, has_scores, in_place;
     int32_t vec;            // bytes of one token's key
 };
-
-constexpr int kMaxCluster = 8;
-
-__device__ __forceinline__ void cluster_arrive() {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() {
-    __syncwarp();
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_sync() {
-    cluster_arrive();
-    cluster_wait();
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm("mov.u32 %0, %cluster_nctarank;" : "=r"(r));
-    return r;
-}
-// A 32-bit value at the same place in another CTA's shared memory.
-__device__ __forceinline__ int32_t load_remote(const int32_t* p, uint32_t rank) {
-    uint32_t addr = (uint32_t)__cvta_generic_to_shared(p), remote;
-    int32_t v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
-    return v;
-}
-
-__device__ __forceinline__ void store_remote(int32_t* p, uint32_t rank, int32_t v) {
-    uint32_t addr = (uint32_t)__cvta_generic_to_shared(p), remote;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(remote), "r"(v) : "memory");
-}
 
 // The sequence's length, or -1 if it is refused.  The whole cluster asks together, each CTA looking at its part of the tables;
 // bad: [kMaxCluster] in shared memory.  Another CTA's shared memory may be written once that CTA runs: every CTA arrives at the
@@ -426,36 +388,6 @@ __global__ void __launch_bounds__(kCloseThreads) evict_close_up(const __grid_con
         if (score_to >= 0) m.scores[score_to] = score;
         __syncthreads();  // the offsets are used up
     }
-}
-
-template <class... P, class... A>
-static amoeba_status launch_clusters(void (*kernel)(P...), int64_t grid, int threads, size_t smem, int cluster, bool early,
-                                     cudaStream_t stream, const A&... args) {
-    if (smem > 16 * 1024 && ensure_dynamic_smem((const void*)kernel, (int)smem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)grid);
-    c.blockDim = dim3((unsigned)threads);
-    c.dynamicSmemBytes = smem;
-    c.stream = stream;
-    cudaLaunchAttribute a[2] = {};
-    if (cluster > 1) {
-        a[c.numAttrs].id = cudaLaunchAttributeClusterDimension;
-        a[c.numAttrs].val.clusterDim.x = (unsigned)cluster;
-        a[c.numAttrs].val.clusterDim.y = a[c.numAttrs].val.clusterDim.z = 1;
-        ++c.numAttrs;
-    }
-    if (early) {
-        a[c.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        a[c.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-        ++c.numAttrs;
-    }
-    c.attrs = a;
-    if (cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return AMOEBA_ERR_CUDA;
-    }
-    count_launch();
-    return AMOEBA_OK;
 }
 
 }  // namespace amoeba

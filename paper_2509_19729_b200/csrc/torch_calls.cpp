@@ -244,10 +244,94 @@ PyObject* evict_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// (layout, dtype, layer, pools, batch, device, prefixes, prefixes' device, q, scale, out, lse, status, workspace, stream)
+PyObject* attend_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return answer(n, 15, [&] {
+        const amoeba_layout& l = layout_of(a[0]);
+        const int32_t dtype = whole32(a[1]), layer = whole32(a[2]);
+        const amoeba_batch* b = at_address<amoeba_batch>(a[4]);
+        const int64_t dev = whole(a[5]), width = (int64_t)l.model.num_q_heads / l.tp * l.model.head_dim;
+        if (whole(a[7]) != dev) throw Refused{"the prefixes are on another device than the batch"};
+        const at::ScalarType type = element(dtype);
+        Pointers pool, q, out;
+        pools(a[3], l, layer_bytes(l) * ((int64_t)layer + 1), false, dev, &pool);
+        rows(a[8], l, b->num_rows, width, type, dev, &q);
+        rows(a[10], l, b->num_rows, width, type, dev, &out);
+        const double scale = real(a[9]);
+        void* lse = a[11] == Py_None ? nullptr
+                                     : dense(a[11], at::kFloat, (int64_t)b->num_rows * l.model.num_q_heads, dev,
+                                             "lse is float32 [num_rows, num_q_heads]");
+        void* status = dense(a[12], at::kInt, 1, dev, "status is int32");
+        void* ws = dense(a[13], at::kByte, 0, dev, "the workspace is uint8");
+        const On here(dev, a[14]);
+        return amoeba_attend_shared(&l, dtype, layer, pool, b, at_address<amoeba_prefixes>(a[6]), q, q.stride, (float)scale, out,
+                                    out.stride, (float*)lse, (int32_t*)status, ws, tensor(a[13]).numel(), here.stream);
+    });
+}
+// (layout, block_table, block_refs, seq_lens, new_lens, parents, shared_lens, lens_out, q_starts, num_rows, first_positions, positions,
+//  slots, pairs, num_pairs, free_count, status, stream)
+PyObject* advance_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return answer(n, 18, [&] {
+        const amoeba_layout& l = layout_of(a[0]);
+        const at::Tensor &table = tensor(a[1]), &lens = tensor(a[3]);
+        const int64_t dev = lens.is_cuda() ? lens.device().index() : -1, S = lens.numel();
+        if (table.dim() != 2 || table.size(0) != S) throw Refused{"block tables are [num_seqs, blocks]"};
+        if (S > INT32_MAX || table.size(1) > INT32_MAX) throw Refused{"too many sequences or blocks"};
+        amoeba_table_step s{};
+        auto ints = [&](int i, int64_t count, const char* why) {
+            return a[i] == Py_None ? nullptr : (int32_t*)dense(a[i], at::kInt, count, dev, why);
+        };
+        s.num_seqs = (int32_t)S, s.max_blocks_per_seq = (int32_t)table.size(1), s.num_rows = whole32(a[9]);
+        s.d_block_table = ints(1, 0, "block tables are int32");
+        s.d_block_refs = ints(2, l.num_blocks, "block counts are int32 [num_blocks]");
+        s.d_seq_lens = ints(3, S, "lengths are int32 [num_seqs]");
+        s.d_new_lens = ints(4, S, "lengths are int32 [num_seqs]");
+        s.d_parents = ints(5, S, "parents are int32 [num_seqs]");
+        s.d_shared_lens = ints(6, S, "shared lengths are int32 [num_seqs]");
+        s.d_lens_out = ints(7, S, "lengths are int32 [num_seqs]");
+        s.d_q_starts = ints(8, S + 1, "row starts are int32 [num_seqs + 1]");
+        s.d_first_positions = ints(10, S, "first positions are int32 [num_seqs]");
+        s.d_positions = ints(11, s.num_rows, "positions are int32 [num_rows]");
+        s.d_slots = a[12] == Py_None ? nullptr : (int64_t*)dense(a[12], at::kLong, s.num_rows, dev, "slots are int64 [num_rows]");
+        s.d_pairs = ints(13, 0, "pairs are int32 [pairs, 2]");
+        if (s.d_pairs) {
+            const at::Tensor& t = tensor(a[13]);
+            if (t.dim() != 2 || t.size(1) != 2 || t.size(0) > INT32_MAX) throw Refused{"pairs are int32 [pairs, 2]"};
+            s.pairs_cap = (int32_t)t.size(0);
+        }
+        s.d_num_pairs = ints(14, 1, "the number of pairs is int32");
+        s.d_free_count = ints(15, 1, "the free count is int32");
+        void* status = dense(a[16], at::kInt, 1, dev, "status is int32");
+        const On here(dev, a[17]);
+        return amoeba_advance_tables(&l, &s, (int32_t*)status, here.stream);
+    });
+}
+// (layout, pools, pairs, num_pairs, layer_begin, layer_end, status, stream)
+PyObject* copy_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return answer(n, 8, [&] {
+        const amoeba_layout& l = layout_of(a[0]);
+        const int32_t l0 = whole32(a[4]), l1 = whole32(a[5]);
+        const at::Tensor& pairs = tensor(a[2]);
+        const int64_t dev = pairs.is_cuda() ? pairs.device().index() : -1;
+        if (pairs.dim() != 2 || pairs.size(1) != 2 || pairs.size(0) > INT32_MAX) throw Refused{"pairs are int32 [pairs, 2]"};
+        Pointers pool;
+        pools(a[1], l, layer_bytes(l) * l1, false, dev, &pool);
+        void* pairs_p = dense(a[2], at::kInt, 0, dev, "pairs are int32 [pairs, 2]");
+        void* count = dense(a[3], at::kInt, 1, dev, "the number of pairs is int32");
+        void* status = dense(a[6], at::kInt, 1, dev, "status is int32");
+        const On here(dev, a[7]);
+        return amoeba_copy_blocks(&l, pool, (int32_t*)pairs_p, (int32_t*)count, (int32_t)pairs.size(0), l0, l1, (int32_t*)status,
+                                  here.stream);
+    });
+}
+
 PyMethodDef kMethods[] = {
     {"append_kv", (PyCFunction)(void (*)())append_kv, METH_FASTCALL, nullptr},
     {"attend", (PyCFunction)(void (*)())attend, METH_FASTCALL, nullptr},
     {"accumulate_scores", (PyCFunction)(void (*)())accumulate_scores, METH_FASTCALL, nullptr},
+    {"attend_shared", (PyCFunction)(void (*)())attend_shared, METH_FASTCALL, nullptr},
+    {"advance_tables", (PyCFunction)(void (*)())advance_tables, METH_FASTCALL, nullptr},
+    {"copy_blocks", (PyCFunction)(void (*)())copy_blocks, METH_FASTCALL, nullptr},
     {"evict_kv", (PyCFunction)(void (*)())evict_kv, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

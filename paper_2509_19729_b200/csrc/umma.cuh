@@ -163,7 +163,7 @@ struct TileLoader {
         hw = w.h - r * v.heads;
         head = v.pools[r] + hw * v.head_stride;
         map = &maps.worker[r];
-        table = b.table + (int64_t)w.s * b.max_blocks;
+        table = b.table + (int64_t)w.seq.row * b.max_blocks;
     }
     // The blocks that the 16 groups of eight tokens of the tile at key0 lie in, one per lane; -1: no token in [lo, hi).  Asked
     // for well ahead: nothing here waits for the answer.

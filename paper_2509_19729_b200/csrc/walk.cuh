@@ -30,13 +30,13 @@ __device__ __forceinline__ Range row_tile_range(const Shape& p, const Seq& q, in
     Range r;
     const int n = q.qn * p.group;
     int p0 = q.len - q.qn, p1 = q.len - 1;  // cache indices of the tile's first and last rows
-    if (n > p.rows) {
+    if (n > p.rows && !q.level) {
         const int last = (int)min((int64_t)n, (int64_t)(m + 1) * p.rows) - 1;
         p1 = p0 + last / p.group;
         p0 += m * p.rows / p.group;
     }
     r.hi = min(max(p1 + 1, 0), q.len);
-    r.lo = p.window > 0 ? min(max(p0 - p.window + 1, 0), r.hi) : 0;
+    r.lo = p.window > 0 ? min(max(p0 - p.window + 1, 0), r.hi) : min(q.first, r.hi);
     r.base = r.lo & -p.tile;  // (a power of two)
     r.tiles = max(1, (r.hi - r.base + p.tile - 1) >> __ffs(p.tile) - 1);
     return r;
@@ -66,7 +66,8 @@ struct Walk {
     Seq seq;
     Range range;
 
-    __device__ __forceinline__ void open(const Shape& p, const Batch& b, int block_tokens, int seq_index) {
+    template <class B>
+    __device__ __forceinline__ void open(const Shape& p, const B& b, int block_tokens, int seq_index) {
         s = seq_index;
         seq = sequence(b, s, block_tokens);
         nm = row_tiles(p, seq);
@@ -93,7 +94,8 @@ struct Walk {
         range = row_tile_range(p, seq, m);
     }
     // To the next tile; the caller knows that there is one.
-    __device__ __forceinline__ void next(const Shape& p, const Batch& b, int block_tokens) {
+    template <class B>
+    __device__ __forceinline__ void next(const Shape& p, const B& b, int block_tokens) {
         if (++t < range.tiles) return;
         t = 0;
         if (++m < nm) {
@@ -137,8 +139,8 @@ __device__ __forceinline__ void write_cut(const Shape& p, Cut* cuts, const Walk&
 }
 
 // This CTA's share: [*begin, *end) of all tiles, with `walk` at the first of them.  CTA 0 reports bad sequences.
-template <int kThreads>
-__device__ void take_share(const Shape& p, const Batch& b, int block_tokens, Walk* walk, int64_t* begin_out, int64_t* end_out,
+template <int kThreads, class B>
+__device__ void take_share(const Shape& p, const B& b, int block_tokens, Walk* walk, int64_t* begin_out, int64_t* end_out,
                            int32_t* status) {
     __shared__ int64_t s_warp[kThreads / 32];
     __shared__ int64_t s_off;

@@ -55,10 +55,10 @@ __device__ __forceinline__ int swizzled(int r, int c) {
 // One warp's loads of 16 consecutive tokens' keys (and, kValues, values) of one head at a time, [K][V][16][D] swizzled, ahead
 // of the warp's own walk over the tiles (kTile tokens each, the warp's 16 at `offset` in every tile).  The block that the
 // next tokens lie in is looked up one step early.
-template <int D, bool kValues, int kTile>
+template <int D, bool kValues, int kTile, class B = Batch>
 struct Ahead {
     const CacheView& v;
-    const Batch& b;
+    const B& b;
     const Shape& shape;
     int32_t* status;
     const int lane, offset;
@@ -69,7 +69,7 @@ struct Ahead {
     const char* head;
     int32_t hw, block = -1, in_block = 0;
 
-    __device__ __forceinline__ Ahead(const CacheView& v_, const Batch& b_, const Shape& s_, int32_t* status_, const Walk& w_, int64_t n,
+    __device__ __forceinline__ Ahead(const CacheView& v_, const B& b_, const Shape& s_, int32_t* status_, const Walk& w_, int64_t n,
                                      int offset_)
         : v(v_), b(b_), shape(s_), status(status_), lane(threadIdx.x & 31), offset(offset_), one_block(v_.block_tokens % 16 == 0), w(w_),
           left(n) {
@@ -79,7 +79,7 @@ struct Ahead {
         }
     }
     __device__ __forceinline__ void open() {
-        table = b.table + (int64_t)w.s * b.max_blocks;
+        table = b.table + (int64_t)w.seq.row * b.max_blocks;
         const int r = w.h / v.heads;
         hw = w.h - r * v.heads;
         head = v.pools[r] + hw * v.head_stride;
