@@ -235,13 +235,13 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
 // one for each CTA where a few units of many rows run over a long cache.  Bound by its few dependent loads: 9 us by itself for 296
 // shares of 8 rows, of which the launch in front hides a part.
 constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
-template <int kWarps>
-constexpr int kJoinRows = kWarps == 1 ? 4 * kJoinWarps : 1;  // of a block
+template <int kWarps, class B>
+constexpr int kJoinRows = kWarps > 1 ? 1 : B::kShared ? kJoinWarps : 4 * kJoinWarps;  // of a block
 
 // `groups` blocks to every share: the unit that it begins in is joined there, if that began in the share before.
 template <class T, int D, int kWarps, class B>
 __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, int block, int groups) {
-    constexpr int kRows = kJoinRows<kWarps>, kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes to a part's row, parts at once
+    constexpr int kRows = kJoinRows<kWarps, B>, kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes to a part's row, parts at once
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int mine = block / groups, first_row = block % groups * kRows, R = p.shape.rows;
     const Cut cut = p.cuts[mine];
@@ -262,7 +262,7 @@ __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, in
         const int r = first_row + (kWarps == 1 ? i + warp : 0);
         Joined j;
         if (r < cut.rows) {
-#pragma unroll (kWarps == 1 ? 2 : 8)
+#pragma unroll (kWarps > 1 ? 8 : B::kShared ? 6 : 2)
             for (int c = c0 + (kWarps == 1 ? 0 : warp) * kAtOnce + lane / kLanes; c < c1; c += kWarps * kAtOnce) {
                 if (p.cuts[c].begin == p.cuts[c].end) continue;
                 const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
@@ -295,12 +295,13 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constan
     grid_dependency_wait();
     const int block = (int)blockIdx.x - few_ctas * few_rows;
     if (block < 0) join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x, few_rows);
-    else join_rows<T, D, 1>(many, many_ctas, block, kManyRows / kJoinRows<1>);
+    else join_rows<T, D, 1>(many, many_ctas, block, kManyRows / kJoinRows<1, B>);
 }
 
 // The workspace holds the parts of cut units, two for each CTA; these bound the grids without asking the device.
 constexpr int kMaxFewCtas = 2 * kMaxSms;
 constexpr int kMaxFewRows = 32;
+constexpr int kMaxGroupRows = 8;  // of a group by attend_few
 
 // One kernel's part of the workspace: where the shares begin, then the parts.
 template <class B>
@@ -348,7 +349,7 @@ static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char*
     const int64_t few_bytes = few_workspace(&p, ws, D);
     // In a batch with longer pieces attend_few gets the single tokens (and what has as few rows): its rows cost registers.  Groups
     // all go to one kernel: small ones beside large ones are not worth a launch.
-    const bool groups = p.batch.by_groups(), few = !groups || rows <= kMaxFewRows;
+    const bool groups = p.batch.by_groups(), few = !groups || rows <= kMaxGroupRows;
     const int64_t few_rows = rows <= kMaxFewRows ? rows : p.shape.group;
     const int most = !few ? 0 : few_rows <= 8 ? 8 : few_rows <= 16 ? 16 : kMaxFewRows;
     p.shape.min_rows = 0;
@@ -358,19 +359,19 @@ static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char*
                        : most == 8  ? run_few<T, D, 1>(p, sms, &few_ctas, stream)
                        : most == 16 ? run_few<T, D, 2>(p, sms, &few_ctas, stream)
                                     : run_few<T, D, 4>(p, sms, &few_ctas, stream);
-    if (st != AMOEBA_OK || (p.whole && rows <= kMaxFewRows)) return st;
+    if (st != AMOEBA_OK || (p.whole && few && rows <= kMaxFewRows)) return st;
     if (p.whole) few_ctas = 0;  // nothing is cut
     const int few_most = (int)std::min<int64_t>(rows, most);
     AttendParams<B> many = p;
     int many_ctas = 0, many_blocks = 0;
-    if (rows > kMaxFewRows) {
+    if (!few || rows > kMaxFewRows) {
         many_workspace(&many, ws + few_bytes, D);
         many.shape.min_rows = most + 1;
         many.shape.max_rows = INT32_MAX;
         many.shape.rows = kManyRows;
         many.shape.tile = kManyTile;
         many_ctas = std::min(sms, kMaxSms);
-        many_blocks = many_ctas * (kManyRows / kJoinRows<1>);
+        many_blocks = many_ctas * (kManyRows / kJoinRows<1, B>);
         if ((st = launch_attend_many(many, tp, dtype, D, many_ctas, stream)) != AMOEBA_OK) return st;
     }
     return launch_kernel(attend_join<T, D, B>, few_ctas * few_most + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_most, many,
@@ -535,7 +536,7 @@ static SharedSpace shared_space(const amoeba_layout* l, const amoeba_batch* b, c
     const int64_t heads = ((int64_t)b->num_rows * l->model.num_q_heads + 3) / 4 * 4;
     SharedSpace s;
     s.groups_pass = 0;
-    s.rest_pass = few + (rows_of(l, x->max_group_rows) > kMaxFewRows ? many : 0);
+    s.rest_pass = few + (rows_of(l, x->max_group_rows) > kMaxGroupRows ? many : 0);
     s.carry_o = s.rest_pass + few + (rows_of(l, b->max_q_len) > kMaxFewRows ? many : 0);
     s.carry_m = s.carry_o + heads * D * 4;
     s.carry_l = s.carry_m + heads * 4;

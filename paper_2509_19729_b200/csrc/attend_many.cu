@@ -21,6 +21,10 @@
 // stay below 2^8 until then and the result is the same, as numerator and sum have the same factor.  That makes the
 // scaling of O, a pass through tensor memory, rare.
 //
+// Units of at most 128 rows (of a SharedBatch, whose groups are often that small) would leave one warpgroup idle and every product
+// waiting for a softmax.  There both warpgroups have the same rows and take the tiles in turn, each with its own maximum, sum and O;
+// the first reads the other's O from tensor memory, whose lanes both reach, and joins the two.
+//
 // Tensor memory: columns 0-127 and 128-255 S and P of the two tiles, 256 and 256 + D their O.
 #include "attend.cuh"
 #include "umma.cuh"
@@ -193,7 +197,7 @@ __device__ bool make_share(const AttendParams<B>& p, Share& sh, int32_t* done) {
 struct Parts {
     Walk w;
     int32_t round = 0, tiles = 0, q_tiles, rows;  // rows of the unit, 1 .. 256
-    bool from_start, to_end, opened = false;
+    bool from_start, to_end, in_turn, opened = false;  // in_turn: the warpgroups take the tiles in turn
     int64_t left;
 
     __device__ __forceinline__ Parts(const Share& sh) : left(sh.end - sh.begin) {}
@@ -226,6 +230,7 @@ struct Parts {
         }
         rows = min(kManyRows, w.seq.qn * shape.group - w.m * kManyRows);
         q_tiles = rows > 128 ? 2 : 1;
+        in_turn = B::kShared && q_tiles == 1 && tiles > 1;
         from_start = w.t == 0;
         to_end = w.t + tiles == w.range.tiles;
         return true;
@@ -297,12 +302,12 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
     uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort)); };
     const uint64_t q_op = operand(smem, 16);
-    auto logits = [&](int t, int k_slot) {
+    auto logits = [&](int q_tile, int t, int k_slot) {
         const uint64_t k_op = operand(smem + (2 + __shfl_sync(~0u, k_slot, 0)) * kTile, 16);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
             const uint32_t step = (k / 4 * (128 * 128) + k % 4 * 32) >> 4;
-            umma_smem(leader, tmem + t * 128, q_op + (t * kTile >> 4) + step, k_op + step, kS, k > 0);
+            umma_smem(leader, tmem + t * 128, q_op + (q_tile * kTile >> 4) + step, k_op + step, kS, k > 0);
         }
     };
     auto weigh = [&](int t, int v_slot, int half, bool accumulate) {
@@ -311,17 +316,71 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
         for (int k = half * 4; k < half * 4 + 4; ++k)
             umma_tmem(leader, tmem + 256 + t * D, tmem + t * 128 + k * 8, v_op + (k * 2048 >> 4), kO, accumulate || k > 0);
     };
+    // The place `n` slots on in the ring.
+    auto onward = [&](int n, int& at, uint32_t& parity) {
+        at = slot + n, parity = phase;
+        if (at >= kStages) at -= kStages, parity ^= 1;
+    };
+    // The products of a part whose tiles the warpgroups take in turn: the logits run two tiles ahead of the weights.
+    auto in_turn = [&](const Parts& part) {
+        int at;
+        uint32_t parity;
+        for (int t = 0; t < 2; ++t) {
+            onward(2 * t, at, parity);
+            if (!wait(&b.full[at], parity)) return false;
+            fence_async_smem();
+            tmem_fence_after();
+            logits(0, t, at);
+            umma_commit(leader, &b.s_full[t]);
+            umma_commit(leader, &b.empty[at]);
+        }
+        if (part.tiles == 2) umma_commit(leader, &b.q_empty);
+        for (int i = 0; i < part.tiles; ++i) {
+            const int t = i % 2;
+            onward(1, at, parity);
+            if (!wait(&b.full[at], parity)) return false;
+            fence_async_smem();
+            if (i < 2) {
+                if (!wait(&b.o_free[t], o_phase[t])) return false;
+                o_phase[t] ^= 1;
+            }
+            if (!wait(&b.p_half[t], p_phase[t])) return false;
+            tmem_fence_after();
+            weigh(t, at, 0, i > 1);
+            if (!wait(&b.p_full[t], p_phase[t])) return false;
+            p_phase[t] ^= 1;
+            tmem_fence_after();
+            weigh(t, at, 1, true);
+            umma_commit(leader, &b.o_full[t]);
+            umma_commit(leader, &b.empty[at]);
+            if (i + 2 < part.tiles) {
+                onward(4, at, parity);
+                if (!wait(&b.full[at], parity)) return false;
+                fence_async_smem();
+                logits(0, t, at);
+                umma_commit(leader, &b.s_full[t]);
+                umma_commit(leader, &b.empty[at]);
+            }
+            if (i + 3 == part.tiles) umma_commit(leader, &b.q_empty);
+            onward(2, slot, phase);
+        }
+        return true;
+    };
     Parts part(share);
     while (part.next(p, share)) {
         if (!wait(&b.q_full, q_phase)) return false;
         q_phase ^= 1;
+        if (B::kShared && part.in_turn) {
+            if (!in_turn(part)) return false;
+            continue;
+        }
         if (!wait(&b.full[slot], phase)) return false;
         fence_async_smem();
         tmem_fence_after();
         #pragma unroll
         for (int t = 0; t < 2; ++t) {
             if (t >= part.q_tiles) break;
-            logits(t, slot);
+            logits(t, t, slot);
             umma_commit(leader, &b.s_full[t]);
         }
         umma_commit(leader, &b.empty[slot]);
@@ -354,7 +413,7 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
                         if (!wait(&b.full[k_slot], k_phase)) return false;
                         fence_async_smem();
                     }
-                    logits(t, k_slot);
+                    logits(t, t, k_slot);
                     umma_commit(leader, &b.s_full[t]);
                 }
             }
@@ -450,7 +509,7 @@ __device__ __forceinline__ float row_weights(uint32_t s_tmem, float c, float ref
 template <class T, int D, class B>
 __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarriers& b) {
     const Shape& sh = p.shape;
-    const int t = threadIdx.x / 128, r = threadIdx.x;  // row of the unit
+    const int t = threadIdx.x / 128;
     const uint32_t lanes = (uint32_t)(threadIdx.x % 128 / 32 * 32) << 16;
     const uint32_t s_tmem = b.tmem + lanes + t * 128, o_tmem = b.tmem + lanes + 256 + t * D;
     const float c = p.scale_log2;
@@ -462,25 +521,28 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
     Parts part(share);
     while (part.next(p, share)) {
         const Walk& w = part.w;
-        // a bad block anywhere in the unit: its tokens are looked up one by one below
+        const bool in_turn = B::kShared && part.in_turn;
+        // a bad block anywhere in the part: its tokens are looked up one by one below
         const int32_t* table = p.batch.table + (int64_t)w.seq.row * p.batch.max_blocks;
         int bad = 0;
-        for (int i = w.range.lo / p.cache.block_tokens + (int)threadIdx.x % 128; i * (int64_t)p.cache.block_tokens < w.range.hi; i += 128)
+        const int part_lo = max(w.range.lo, w.range.base + w.t * kManyTile), part_hi = min(w.range.hi, w.range.base + (w.t + part.tiles) * kManyTile);
+        for (int i = part_lo / p.cache.block_tokens + (int)threadIdx.x % 128; i * (int64_t)p.cache.block_tokens < part_hi; i += 128)
             bad |= table[i] < 0 || table[i] >= p.cache.num_blocks;
         asm volatile(
             "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %0, 0;\n\t"
             "barrier.cta.red.or.pred q, %1, 128, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
             : "+r"(bad) : "r"(1 + t) : "memory");
         if (bad && threadIdx.x % 128 == 0) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
-        if (ok && t < part.q_tiles) ok = [&] {
-            const int row = w.m * kManyRows + r;
-            const bool there = r < part.rows;
-            const int pos = last_seen(w.seq, row / sh.group);
-            // (rows that are not there see zeros or anything: nothing is written for them)
-            const int see_hi = there ? pos + 1 : INT32_MAX,
-                      see_lo = !there ? 0 : sh.window > 0 ? max(pos - sh.window + 1, 0) : B::kShared ? w.seq.first : 0;
-            float m_ref = -INFINITY, l = 0.f;
-            for (int i = 0; i < part.tiles; ++i) {
+        const int r = in_turn ? (int)threadIdx.x % 128 : (int)threadIdx.x, row = w.m * kManyRows + r;  // row of the unit
+        const bool there = r < part.rows;
+        const int pos = last_seen(w.seq, row / sh.group);
+        // (rows that are not there see zeros or anything: nothing is written for them)
+        const int see_hi = there ? pos + 1 : INT32_MAX,
+                  see_lo = !there ? 0 : sh.window > 0 ? max(pos - sh.window + 1, 0) : B::kShared ? w.seq.first : 0;
+        const int first_tile = in_turn ? t : 0, step = in_turn ? 2 : 1;
+        float m_ref = -INFINITY, l = 0.f;
+        if (ok && (in_turn || t < part.q_tiles)) ok = [&] {
+            for (int i = first_tile; i < part.tiles; i += step) {
                 const int key0 = w.range.base + (w.t + i) * kManyTile;
                 if (!wait(&b.s_full[t], s_phase)) return false;
                 s_phase ^= 1;
@@ -496,7 +558,7 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
                     const bool scales = __any_sync(~0u, raise && m_ref > -INFINITY);
                     l *= f;
                     m_ref = m_new;
-                    if (i > 0 && scales) {
+                    if (i > first_tile && scales) {
                         if (!wait(&b.o_full[t], o_phase ^ 1)) return false;  // of the tile before
                         tmem_fence_after();
 #pragma unroll
@@ -519,20 +581,41 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
             }
             if (!wait(&b.o_full[t], o_phase ^ 1)) return false;
             tmem_fence_after();
+            return true;
+        }();
+        const int64_t at = (int64_t)(2 * blockIdx.x + (part.from_start ? 1 : 0)) * kManyRows + r;
+        if (in_turn) {
+            // The first warpgroup ends the part for both; the second's maxima and sums go through the part's rows 128 to 255, of which
+            // there are none.  (It comes to its next ones only after o_free.)
+            if (t == 1) p.part_m[at + 128] = m_ref, p.part_l[at + 128] = l;
+            tmem_fence_before();
+            __syncwarp();
+            asm volatile("barrier.cta.sync 3, 256;" ::: "memory");
+            tmem_fence_after();
+        }
+        if (ok && t < part.q_tiles) {
             const bool direct = part.from_start && part.to_end;
-            // With a carry: into it (a group's rows), or taken up, own sums by `keep` and the carried ones by `take`.
+            // A row's sum is `keep` of its own O, `other` of the second warpgroup's, `take` of the carried one.
             const bool into = B::kShared && w.seq.level, takes = B::kShared && direct && there && w.seq.first > 0;
             const int64_t head = B::kShared && there ? head_of(p, w.seq, w.h, row) : 0;
-            float keep = 1.f, take = 0.f;
-            if (takes) {
-                const float m2 = p.carry.m[head], up = fmaxf(m_ref, m2), ref = up == -INFINITY ? 0.f : up;
-                keep = fast_exp2(m_ref - ref), take = fast_exp2(m2 - ref);
-                l = l * keep + p.carry.l[head] * take;
+            float keep = 1.f, other = 0.f, take = 0.f;
+            if (in_turn) {
+                const float m2 = p.part_m[at + 128], up = fmaxf(m_ref, m2), ref = up == -INFINITY ? 0.f : up;
+                keep = fast_exp2(m_ref - ref), other = fast_exp2(m2 - ref);
+                l = l * keep + p.part_l[at + 128] * other;
                 m_ref = up;
             }
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            keep *= inv, take *= inv;
-            const int64_t at = (int64_t)(2 * blockIdx.x + (part.from_start ? 1 : 0)) * kManyRows + r;
+            if (takes) {
+                const float m2 = p.carry.m[head], up = fmaxf(m_ref, m2), ref = up == -INFINITY ? 0.f : up, f = fast_exp2(m_ref - ref);
+                take = fast_exp2(m2 - ref);
+                l = l * f + p.carry.l[head] * take;
+                keep *= f, other *= f;
+                m_ref = up;
+            }
+            if (direct && !into) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                keep *= inv, other *= inv, take *= inv;
+            }
             char* out = there ? row_of<D>(p.out, p, w.seq, w.h, row) : nullptr;
             float* const raw = direct ? p.carry.o + head * D : p.part_o + at * D;
 #pragma unroll
@@ -540,11 +623,19 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
                 uint32_t o[32];
                 __syncwarp();  // (rows that are not there have parted from the others)
                 tmem_load32(o, o_tmem + j * 32);
-                tmem_load_wait();
-                if (!there) continue;
-                if (direct && !into) {
+                if (in_turn) {
+                    uint32_t o2[32];
+                    tmem_load32(o2, o_tmem + D + j * 32);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep + __uint_as_float(o2[k]) * other);
+                } else {
+                    tmem_load_wait();
 #pragma unroll
                     for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
+                }
+                if (!there) continue;
+                if (direct && !into) {
                     if (takes)
 #pragma unroll
                         for (int k = 0; k < 32; k += 4) {
@@ -570,11 +661,11 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
             }
             tmem_fence_before();
             mbar_arrive(&b.o_free[t]);
+            if (in_turn) mbar_arrive(&b.o_free[1]);
             if (there && !direct) p.part_m[at] = m_ref, p.part_l[at] = l;
             else if (there && into) p.carry.m[head] = m_ref, p.carry.l[head] = l;
             else if (there && p.lse) *lse_of(p, w.seq, w.h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
-            return true;
-        }();
+        }
         if (!ok) b.abort = 1;
     }
     return ok;
