@@ -20,284 +20,284 @@ struct StepParams {
     int64_t* slots;
     int2* pairs;
     int32_t num_seqs, max_blocks, num_rows, pairs_cap, num_blocks, block_tokens;
+    int32_t shift;          // block_tokens = 2^shift, or -1
     int32_t max_len;        // tokens that a row of the table has room for
     int32_t warp_words;     // words of 32 blocks that a warp looks at
+
+    __device__ __forceinline__ int whole(int tokens) const { return shift >= 0 ? tokens >> shift : tokens / block_tokens; }
+    __device__ __forceinline__ int blocks_of(int tokens) const { return whole(tokens + block_tokens - 1); }
+    __device__ __forceinline__ bool inside(int b) const { return b >= 0 && b < num_blocks; }
 };
 
 constexpr int kStepThreads = 1024, kStepWarps = kStepThreads / 32;
-constexpr int kEntryRun = 128;  // table entries that a warp takes at a time
+constexpr int kStepIds = 4096;  // free ids that a CTA lists at a time
 constexpr uint32_t kBadArg = 1, kBadBlock = 2;
 
-// Per sequence, in dynamic shared memory; then the bits of the free blocks that the CTA looks at.
+// In dynamic shared memory: sums over the sequences in front of every one, and at [num_seqs] over all; then the bits of the free
+// blocks that the CTA looks at.
 struct StepShared {
-    int32_t *blocks, *rows, *copies;  // [num_seqs + 1] before every sequence
-    int32_t* first;                   // [num_seqs] cache index of the first new token; -1: refused
-    int32_t* touched;                 // [num_seqs] the forked and the shortened ones, in any order
-    uint32_t* free;                   // [kStepWarps * warp_words]
-};
-__device__ __forceinline__ StepShared step_shared(char* smem, const StepParams& p) {
-    StepShared sh;
-    sh.blocks = reinterpret_cast<int32_t*>(smem);
-    sh.rows = sh.blocks + p.num_seqs + 1;
-    sh.copies = sh.rows + p.num_seqs + 1;
-    sh.first = sh.copies + p.num_seqs + 1;
-    sh.touched = sh.first + p.num_seqs;
-    sh.free = reinterpret_cast<uint32_t*>(sh.touched + p.num_seqs);
-    return sh;
-}
-static int64_t step_smem(int64_t num_seqs, int64_t warp_words) { return (5 * num_seqs + 3 + kStepWarps * warp_words) * 4; }
+    int32_t *blocks, *rows, *copies;
+    int32_t* entries;  // entries of the table that are shared with a parent's or given back
+    int32_t* first;    // cache index of the first new token; -1: refused
+    int32_t* ids;      // [kStepIds] free blocks, counted from the CTA's first
+    uint32_t* free;    // [kStepWarps * warp_words]
 
-// What a sequence asks for.
-struct Need {
-    int32_t blocks, rows, copy, first;
-    bool touched;
-};
-__device__ __forceinline__ Need need_of(const StepParams& p, int s, uint32_t* bad) {
-    const int T = p.block_tokens, old = p.lens[s], now = p.new_lens[s], parent = p.parents ? p.parents[s] : -1;
-    Need n{0, 0, 0, -1, false};
-    bool ok = old >= 0 && old <= p.max_len && now >= 0 && now <= p.max_len && parent < p.num_seqs;
-    int share = 0;
-    if (ok && parent >= 0) {
-        const int from = p.lens[parent];
-        share = p.shared[s];
-        ok = old == 0 && from <= p.max_len && share >= 0 && share <= from && share <= now;
+    __device__ __forceinline__ StepShared(char* smem, const StepParams& p) {
+        const int n = p.num_seqs + 1;
+        blocks = reinterpret_cast<int32_t*>(smem);
+        rows = blocks + n, copies = rows + n, entries = copies + n, first = entries + n, ids = first + n;
+        free = reinterpret_cast<uint32_t*>(ids + kStepIds);
     }
-    if (!ok) {
-        *bad |= kBadArg;
+};
+static int64_t step_smem(int64_t num_seqs, int64_t warp_words) { return (5 * (num_seqs + 1) + kStepIds + kStepWarps * warp_words) * 4; }
+
+// What a sequence asks for.  The loads come in two steps, so that others can be started in between.
+struct Need {
+    int32_t blocks = 0, rows = 0, copies = 0, entries = 0, first = -1;
+};
+struct Ask {
+    int32_t old = 0, now = 0, parent = -1, share = 0, from = 0, last = -1;
+    bool ok = false;
+
+    __device__ __forceinline__ void lengths(const StepParams& p, int s) {
+        old = p.lens[s], now = p.new_lens[s];
+        if (p.parents) parent = p.parents[s];
+        ok = old >= 0 && old <= p.max_len && now >= 0 && now <= p.max_len && parent < p.num_seqs;
+    }
+    __device__ __forceinline__ void more(const StepParams& p, int s) {
+        if (!ok) return;
+        if (parent >= 0) share = p.shared[s], from = p.lens[parent];
+        else if (now > old && p.whole(old) * p.block_tokens != old) last = p.table[(int64_t)s * p.max_blocks + p.whole(old)];
+    }
+    __device__ __forceinline__ Need need(const StepParams& p, uint32_t* bad) const {
+        Need n;
+        if (!ok || (parent >= 0 && (old != 0 || from > p.max_len || share < 0 || share > from || share > now))) {
+            *bad |= kBadArg;
+            return n;
+        }
+        n.first = parent >= 0 ? share : old;
+        if (now < old) {
+            n.entries = p.blocks_of(old) - p.blocks_of(now);
+            return n;
+        }
+        int have = p.whole(n.first);
+        if (parent >= 0) n.entries = have;
+        if (have * p.block_tokens != n.first) {
+            // The last block is not full: a fork gets a copy of its parent's, and a sequence one of a block that others name too.
+            n.copies = parent >= 0;
+            if (parent < 0 && now > old) {
+                const int count = p.inside(last) ? p.refs[last] : 0;
+                if (count < 1) *bad |= kBadBlock;
+                n.copies = count > 1;
+            }
+            if (!n.copies) ++have;
+        }
+        n.blocks = max(p.blocks_of(now) - have, 0);
+        n.rows = p.starts ? now - n.first : 0;
         return n;
     }
-    n.first = parent >= 0 ? share : old;
-    n.touched = parent >= 0 || now < old;
-    if (now < old) return n;
-    int have = n.first / T;
-    if (have * T != n.first) {
-        // The last block is not full: a fork gets a copy of its parent's, and a sequence one of a block that others name too.
-        n.copy = parent >= 0;
-        if (parent < 0 && now > old) {
-            const int b = p.table[(int64_t)s * p.max_blocks + have];
-            const int count = b >= 0 && b < p.num_blocks ? p.refs[b] : 0;
-            if (count < 1) *bad |= kBadBlock;
-            n.copy = count > 1;
-        }
-        if (!n.copy) ++have;
-    }
-    n.blocks = max((now + T - 1) / T - have, 0);
-    n.rows = p.starts ? now - n.first : 0;
-    return n;
-}
+};
 
 // The last s in [0, n) with before[s] <= at; before[0] = 0.
 __device__ __forceinline__ int last_at_most(const int32_t* before, int n, int at) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (before[mid] <= at) lo = mid;
-        else hi = mid;
+    int lo = 0;
+    while (n > 1) {
+        const int half = n / 2;
+        if (before[lo + half] <= at) lo += half, n -= half;
+        else n = half;
     }
     return lo;
 }
+
+// Sums do not pass 2^31 - 1.
+__device__ __forceinline__ uint32_t add_up(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }
 
 __device__ __forceinline__ void step_sync(uint32_t size) {
     if (size > 1) cluster_sync();
     else __syncthreads();
 }
 
-// Calls entry(s, place in the table, column) for the columns [begin(s), end(s)) of the touched sequences, whose warps all share them.
-// A lane looks at one sequence each first, so that their loads overlap.
-template <class Range, class Entry>
-__device__ __forceinline__ void for_entries(const StepParams& p, const StepShared& sh, int n_touched, uint32_t rank, uint32_t size,
-                                            Range range, Entry entry) {
-    const int lane = threadIdx.x % 32, warps = size * kStepWarps, mine = rank * kStepWarps + threadIdx.x / 32;
-    for (int base = 0; base < n_touched; base += 32) {
-        const int s_own = base + lane < n_touched ? sh.touched[base + lane] : -1;
-        int2 r_own = make_int2(0, 0);
-        if (s_own >= 0) r_own = range(s_own);
-        for (int i = 0; i < min(32, n_touched - base); ++i) {
-            const int s = __shfl_sync(~0u, s_own, i), lo = __shfl_sync(~0u, r_own.x, i), hi = __shfl_sync(~0u, r_own.y, i);
-            const int turn = (int)((uint32_t)s * 37u % (uint32_t)warps), at = mine >= turn ? mine - turn : mine - turn + warps;
-            for (int64_t j = lo + (int64_t)at * kEntryRun + lane; j - lane < hi; j += (int64_t)warps * kEntryRun)
-#pragma unroll
-                for (int k = 0; k < kEntryRun; k += 32)
-                    if (j + k < hi) entry(s, (int64_t)s * p.max_blocks + j + k, (int)j + k);
-        }
-    }
-}
-
 __global__ void __launch_bounds__(kStepThreads, 1) advance_tables(const __grid_constant__ StepParams p) {
     extern __shared__ __align__(16) char smem[];
-    __shared__ int64_t s_sum[3][kStepWarps];
+    __shared__ uint32_t s_sum[4][kStepWarps];
     __shared__ int32_t s_free[kStepWarps];   // of every warp, then before it
     __shared__ int32_t s_count;              // free blocks that this CTA looks at
-    __shared__ int32_t s_touched, s_freed;
+    __shared__ int32_t s_freed;
     __shared__ uint32_t s_bad;
     __shared__ int32_t s_all_bad[kMaxCluster], s_all_freed[kMaxCluster];  // in the first CTA
     const uint32_t rank = cluster_rank(), size = cluster_size();
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.num_seqs, T = p.block_tokens;
-    const StepShared sh = step_shared(smem, p);
-    if (tid == 0) s_touched = s_freed = 0, s_bad = 0;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.num_seqs;
+    const StepShared sh(smem, p);
+    if (tid == 0) s_freed = 0, s_bad = 0;
+    grid_dependency_launch();
+    grid_dependency_wait();
 
-    // ---- the free blocks
-    const int64_t first_block = ((int64_t)rank * kStepWarps + warp) * p.warp_words * 32;
+    // ---- the free blocks, and what the first sequences ask for
+    Ask ask;
+    if (tid < S) ask.lengths(p, tid);
+    const int64_t cta_block = (int64_t)rank * kStepWarps * p.warp_words * 32;
     uint32_t* const words = sh.free + warp * p.warp_words;
     int found = 0;
-#pragma unroll 8
-    for (int w = 0; w < p.warp_words; ++w) {
-        const int64_t b = first_block + w * 32 + lane;
-        const uint32_t word = __ballot_sync(~0u, b < p.num_blocks && p.refs[b] == 0);
-        if (lane == 0) words[w] = word;
-        found += __popc(word);
+    constexpr int kAtOnce = 8;
+    for (int w0 = 0; w0 < p.warp_words; w0 += kAtOnce) {
+        bool is[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int64_t b = cta_block + ((int64_t)warp * p.warp_words + w0 + i) * 32 + lane;
+            is[i] = w0 + i < p.warp_words && b < p.num_blocks && p.refs[b] == 0;
+        }
+        if (w0 == 0 && tid < S) ask.more(p, tid);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const uint32_t word = __ballot_sync(~0u, is[i]);
+            if (w0 + i < p.warp_words) {
+                if (lane == 0) words[w0 + i] = word;
+                found += __popc(word);
+            }
+        }
     }
     if (lane == 0) s_free[warp] = found;
-    __syncthreads();
 
-    // ---- what the sequences ask for, and the sums before each
-    uint32_t bad = 0;
-    int64_t run[3] = {0, 0, 0};
-    for (int base = 0; base < S; base += kStepThreads) {
+    // ---- the sums in front of every sequence
+    uint32_t bad = 0, run[4] = {0, 0, 0, 0};
+    for (int base = 0; base < S || base == 0; base += kStepThreads) {
         const int s = base + tid;
-        Need n{0, 0, 0, 0, false};
+        Need n;
         if (s < S) {
-            n = need_of(p, s, &bad);
+            if (base > 0) {
+                ask = Ask();
+                ask.lengths(p, s);
+                ask.more(p, s);
+            }
+            n = ask.need(p, &bad);
             sh.first[s] = n.first;
-            if (n.touched) sh.touched[atomicAdd(&s_touched, 1)] = s;
         }
-        const int64_t own[3] = {n.blocks, n.rows, n.copy};
-        int64_t incl[3] = {own[0], own[1], own[2]};
+        uint32_t incl[4] = {(uint32_t)n.blocks, (uint32_t)n.rows, (uint32_t)n.copies, (uint32_t)n.entries}, before[4];
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < 4; ++k) {
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
-                const int64_t up = __shfl_up_sync(~0u, incl[k], o);
-                if (lane >= o) incl[k] += up;
+                const uint32_t up = __shfl_up_sync(~0u, incl[k], o);
+                if (lane >= o) incl[k] = add_up(incl[k], up);
             }
+            before[k] = __shfl_up_sync(~0u, incl[k], 1);
+            if (lane == 0) before[k] = 0;
             if (lane == 31) s_sum[k][warp] = incl[k];
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            int64_t warps = s_sum[k][lane];  // (as many warps as lanes)
+        for (int k = 0; k < 4; ++k) {
+            uint32_t all = s_sum[k][lane];  // (as many warps as lanes)
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
-                const int64_t up = __shfl_up_sync(~0u, warps, o);
-                if (lane >= o) warps += up;
+                const uint32_t up = __shfl_up_sync(~0u, all, o);
+                if (lane >= o) all = add_up(all, up);
             }
-            const int64_t total = __shfl_sync(~0u, warps, 31), before = __shfl_sync(~0u, warps, max(warp - 1, 0));
-            if (s < S) (k == 0 ? sh.blocks : k == 1 ? sh.rows : sh.copies)[s] =
-                (int32_t)min(run[k] + (warp ? before : 0) + incl[k] - own[k], (int64_t)INT32_MAX);
-            run[k] += total;
+            const uint32_t total = __shfl_sync(~0u, all, 31), warps = __shfl_sync(~0u, all, max(warp - 1, 0));
+            if (s < S) (sh.blocks + k * (S + 1))[s] = (int32_t)add_up(run[k], add_up(warp ? warps : 0, before[k]));
+            run[k] = add_up(run[k], total);
         }
-        __syncthreads();
-    }
-    if (tid == 0) {
-        sh.blocks[S] = (int32_t)min(run[0], (int64_t)INT32_MAX);
-        sh.rows[S] = (int32_t)min(run[1], (int64_t)INT32_MAX);
-        sh.copies[S] = (int32_t)min(run[2], (int64_t)INT32_MAX);
-    }
-    if (warp == 0) {
-        const int own = s_free[lane];
-        int incl = own;
+        if (base == 0 && warp == 0) {
+            const int own = s_free[lane];
+            int sum = own;
 #pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int up = __shfl_up_sync(~0u, incl, o);
-            if (lane >= o) incl += up;
+            for (int o = 1; o < 32; o *= 2) {
+                const int up = __shfl_up_sync(~0u, sum, o);
+                if (lane >= o) sum += up;
+            }
+            s_free[lane] = sum - own;
+            if (lane == 31) s_count = sum;
         }
-        s_free[lane] = incl - own;
-        if (lane == 31) s_count = incl;
+        if (base + kStepThreads < S) __syncthreads();
     }
+    if (tid < 4) (sh.blocks + tid * (S + 1))[S] = (int32_t)(tid == 0 ? run[0] : tid == 1 ? run[1] : tid == 2 ? run[2] : run[3]);
     if (bad) atomicOr(&s_bad, bad);
     step_sync(size);
 
-    // ---- who gets it: the sequences before the first that does not fit
+    // ---- who gets it: the sequences in front of the first that does not fit
     int n_free = 0, rank_before = 0;
     for (uint32_t r = 0; r < size; ++r) {
         const int n = size > 1 ? load_remote(&s_count, r) : s_count;
         if (r < rank) rank_before += n;
         n_free += n;
     }
-    int fits = 0;
-    for (int hi = S + 1; hi - fits > 1;) {  // the largest number of sequences that fits
-        const int mid = (fits + hi) / 2;
-        if (sh.blocks[mid] <= n_free && sh.rows[mid] <= p.num_rows && sh.copies[mid] <= p.pairs_cap) fits = mid;
-        else hi = mid;
+    int fits = S;
+    if (sh.blocks[S] > n_free || sh.rows[S] > p.num_rows || sh.copies[S] > p.pairs_cap) {
+        fits = 0;
+        for (int hi = S; hi - fits > 1;) {
+            const int mid = (fits + hi) / 2;
+            if (sh.blocks[mid] <= n_free && sh.rows[mid] <= p.num_rows && sh.copies[mid] <= p.pairs_cap) fits = mid;
+            else hi = mid;
+        }
     }
-    const int n_taken = sh.blocks[fits], n_rows = sh.rows[fits], n_copies = sh.copies[fits], n_touched = s_touched;
+    const int n_taken = sh.blocks[fits], n_rows = sh.rows[fits], n_copies = sh.copies[fits], n_entries = sh.entries[S];
     const int all = size * kStepThreads, me = rank * kStepThreads + tid;
-    auto have = [&](int s) {  // blocks that a growing sequence keeps or shares
-        const bool copy = sh.copies[s + 1] > sh.copies[s];
-        return copy ? sh.first[s] / T : (sh.first[s] + T - 1) / T;
-    };
-    // Counts down: a block with no count left was not this table's to give back.
+    auto copies = [&](int s) { return sh.copies[s + 1] > sh.copies[s]; };
+    auto parent_of = [&](int s) { return p.parents ? p.parents[s] : -1; };
     int freed = 0;
     auto give_back = [&](int b) {
-        if (b < 0 || b >= p.num_blocks) {
-            bad |= kBadBlock;
+        const int count = p.inside(b) ? atomicAdd(&p.refs[b], -1) : 0;
+        if (count > 0) {
+            freed += count == 1;
             return;
         }
-        const int count = atomicAdd(&p.refs[b], -1);
-        if (count <= 0) {
-            atomicAdd(&p.refs[b], 1);
-            bad |= kBadBlock;
-        }
-        freed += count == 1;
+        bad |= kBadBlock;  // no count left: it was not this table's to give back
+        if (p.inside(b)) atomicAdd(&p.refs[b], 1);
     };
 
     // ---- shared and given back blocks, sources of copies: everything that reads other sequences' rows of the table
-    for_entries(
-        p, sh, n_touched, rank, size,
-        [&](int s) {
-            if (p.parents && p.parents[s] >= 0) return make_int2(0, s < fits ? sh.first[s] / T : 0);
-            return make_int2((p.new_lens[s] + T - 1) / T, (p.lens[s] + T - 1) / T);
-        },
-        [&](int s, int64_t place, int col) {
-            const int parent = p.parents ? p.parents[s] : -1;
-            if (parent < 0) {
-                give_back(p.table[place]);
-                return;
-            }
-            const int b = p.table[(int64_t)parent * p.max_blocks + col];
-            p.table[place] = b;
-            if (b < 0 || b >= p.num_blocks) bad |= kBadBlock;
+    for (int e = me; e < n_entries; e += all) {
+        const int s = last_at_most(sh.entries, S, e), j = e - sh.entries[s], parent = parent_of(s);
+        int32_t* const row = p.table + (int64_t)s * p.max_blocks;
+        if (parent < 0) {
+            give_back(row[p.blocks_of(p.new_lens[s]) + j]);
+        } else if (s < fits) {
+            const int b = p.table[(int64_t)parent * p.max_blocks + j];
+            row[j] = b;
+            if (!p.inside(b)) bad |= kBadBlock;
             else freed -= atomicAdd(&p.refs[b], 1) == 0;  // (its last other user has just given it back)
-        });
-    if (n_copies > 0)
-        for (int s = me; s < fits; s += all) {
-            if (sh.copies[s + 1] == sh.copies[s]) continue;
-            const int parent = p.parents ? p.parents[s] : -1;
-            const int b = p.table[(int64_t)(parent >= 0 ? parent : s) * p.max_blocks + sh.first[s] / T];
-            const bool there = b >= 0 && b < p.num_blocks;
-            p.pairs[sh.copies[s]].x = there ? b : -1;
-            if (!there) bad |= kBadBlock;
-            if (parent < 0) give_back(b);
         }
+    }
+    for (int s = me; n_copies > 0 && s < fits; s += all) {
+        if (!copies(s)) continue;
+        const int parent = parent_of(s), b = p.table[(int64_t)(parent >= 0 ? parent : s) * p.max_blocks + p.whole(sh.first[s])];
+        p.pairs[sh.copies[s]].x = p.inside(b) ? b : -1;
+        if (parent < 0) give_back(b);
+        else if (!p.inside(b)) bad |= kBadBlock;
+    }
     if (p.parents || p.pairs_cap > 0) step_sync(size);  // (without these no row is read that is not the reader's own)
 
     // ---- the free blocks to their sequences
-    for_entries(
-        p, sh, n_touched, rank, size,
-        [&](int s) {
-            if (p.parents && p.parents[s] >= 0) return make_int2(0, 0);
-            return make_int2((p.new_lens[s] + T - 1) / T, (p.lens[s] + T - 1) / T);
-        },
-        [&](int, int64_t place, int) { p.table[place] = -1; });
-    int r0 = rank_before + s_free[warp];
-    for (int w = 0; w < p.warp_words && r0 < n_taken; ++w) {
-        const uint32_t word = words[w];
-        const int r = r0 + __popc(word & ((1u << lane) - 1));
-        if (word >> lane & 1u && r < n_taken) {
-            const int b = (int)(first_block + w * 32 + lane), s = last_at_most(sh.blocks, fits, r), j = r - sh.blocks[s];
-            p.table[(int64_t)s * p.max_blocks + have(s) + j] = b;
-            p.refs[b] = 1;
-            if (j == 0 && sh.copies[s + 1] > sh.copies[s]) p.pairs[sh.copies[s]].y = b;
+    for (int e = me; e < n_entries; e += all) {
+        const int s = last_at_most(sh.entries, S, e);
+        if (parent_of(s) < 0) p.table[(int64_t)s * p.max_blocks + p.blocks_of(p.new_lens[s]) + e - sh.entries[s]] = -1;
+    }
+    const int mine = min(s_count, n_taken - rank_before);  // of the free blocks that this CTA looks at
+    for (int base = 0; base < mine; base += kStepIds) {
+        const int end = min(mine, base + kStepIds);
+        int r0 = s_free[warp];
+        for (int w = 0; w < p.warp_words && r0 < end; ++w) {
+            const uint32_t word = words[w];
+            const int r = r0 + __popc(word & ((1u << lane) - 1));
+            if (word >> lane & 1u && r >= base && r < end) sh.ids[r - base] = (warp * p.warp_words + w) * 32 + lane;
+            r0 += __popc(word);
         }
-        r0 += __popc(word);
+        __syncthreads();
+        for (int i = tid; i < end - base; i += kStepThreads) {
+            const int b = (int)cta_block + sh.ids[i], r = rank_before + base + i, s = last_at_most(sh.blocks, fits, r), j = r - sh.blocks[s];
+            const int have = copies(s) ? p.whole(sh.first[s]) : p.blocks_of(sh.first[s]);
+            p.table[(int64_t)s * p.max_blocks + have + j] = b;
+            p.refs[b] = 1;
+            if (j == 0 && copies(s)) p.pairs[sh.copies[s]].y = b;
+        }
+        if (end < mine) __syncthreads();
     }
     if (bad) atomicOr(&s_bad, bad);
     if (freed) atomicAdd(&s_freed, freed);
     __syncthreads();
-    if (size > 1) {
-        if (tid == 0) store_remote(&s_all_bad[rank], 0, (int32_t)s_bad), store_remote(&s_all_freed[rank], 0, s_freed);
-    } else if (tid == 0) {
-        s_all_bad[0] = (int32_t)s_bad, s_all_freed[0] = s_freed;
+    if (tid == 0) {
+        if (size > 1) store_remote(&s_all_bad[rank], 0, (int32_t)s_bad), store_remote(&s_all_freed[rank], 0, s_freed);
+        else s_all_bad[0] = (int32_t)s_bad, s_all_freed[0] = s_freed;
     }
     step_sync(size);
 
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) advance_tables(const __grid_c
         for (int s = me; s <= S; s += all) p.starts[s] = sh.rows[min(s, fits)];
     for (int s = me; s < S; s += all) {
         const int old = p.lens[s], now = p.new_lens[s];
-        const bool grows = now > old || (p.parents && p.parents[s] >= 0);
+        const bool grows = now > old || parent_of(s) >= 0;
         p.lens_out[s] = sh.first[s] < 0 || (grows && s >= fits) ? old : now;
     }
     if (p.positions || p.slots)
@@ -317,8 +317,8 @@ __global__ void __launch_bounds__(kStepThreads, 1) advance_tables(const __grid_c
                 const int s = last_at_most(sh.rows, fits, r), j = r - sh.rows[s], index = sh.first[s] + j;
                 position = p.first_pos ? p.first_pos[s] + j : index;
                 if (p.slots) {
-                    const int b = __ldcg(&p.table[(int64_t)s * p.max_blocks + index / T]);
-                    if (b >= 0 && b < p.num_blocks) slot = (int64_t)b * T + index % T;
+                    const int n = p.whole(index), b = __ldcg(&p.table[(int64_t)s * p.max_blocks + n]);
+                    if (p.inside(b)) slot = ((int64_t)b - n) * p.block_tokens + index;
                 }
             }
             if (p.positions) p.positions[r] = position;
@@ -365,12 +365,13 @@ extern "C" amoeba_status amoeba_advance_tables(const amoeba_layout* layout, cons
     p.status = d_status;
     p.num_seqs = a.num_seqs, p.max_blocks = a.max_blocks_per_seq, p.num_rows = a.num_rows, p.pairs_cap = a.pairs_cap;
     p.num_blocks = layout->num_blocks, p.block_tokens = layout->block_tokens;
+    p.shift = (p.block_tokens & (p.block_tokens - 1)) == 0 ? __builtin_ctz((unsigned)p.block_tokens) : -1;
     p.max_len = (int32_t)std::min<int64_t>((int64_t)a.max_blocks_per_seq * layout->block_tokens, kMaxTokens);
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
-    const int cluster = p.num_blocks <= 4096 && p.num_seqs <= kStepThreads && p.num_rows <= 4 * kStepThreads ? 1 : kMaxCluster;
+    const int cluster = p.num_blocks <= 8192 && p.num_seqs <= kStepThreads && p.num_rows <= 4 * kStepThreads ? 1 : kMaxCluster;
     p.warp_words = (int32_t)(((int64_t)p.num_blocks + cluster * kStepThreads - 1) / (cluster * kStepThreads));
     const int64_t smem = step_smem(p.num_seqs, p.warp_words);
     if (smem > dev.smem_optin - 2048) return AMOEBA_ERR_TOO_LARGE;
-    return launch_clusters(advance_tables, cluster, kStepThreads, (size_t)smem, cluster, false, static_cast<cudaStream_t>(cuda_stream), p);
+    return launch_clusters(advance_tables, cluster, kStepThreads, (size_t)smem, cluster, true, static_cast<cudaStream_t>(cuda_stream), p);
 }
