@@ -2,12 +2,13 @@
 //
 // One launch of one cluster.  With n = ceil(length / block_tokens) blocks before and after,
 //   blocks(s) = what a growing or forked sequence lacks,  rows(s) = its new tokens,  copies(s) = 1 if its first new block is a copy,
-// and their prefix sums over the sequences, the r-th free id overall (ascending) goes to the sequence with
-// blocks[s] <= r < blocks[s + 1], and row r to the one with rows[s] <= r < rows[s + 1].  The free ids are counted warp by warp in
-// contiguous runs, so that an id's rank needs one exchange of counts between the CTAs; the prefix sums every CTA makes for itself.
+// and their sums over the sequences in front of s, the r-th free id overall (ascending) goes to the sequence with
+// blocks[s] <= r < blocks[s + 1], as its entry r - blocks[s] of the new ones, and who hands it out knows the rows and slots of the tokens
+// that it holds.  So nothing has to be read back from the table.  The sums every CTA makes for itself; the pool's counts are dealt
+// to the CTAs in tiles of 1024, whose free blocks are exchanged once.
 //
-// What bounds it is latency: a launch, the dependent loads of a look at a sequence's last block, two or three barriers of the
-// cluster and a search for every block and row.  The counts (4 bytes a block) are read once.
+// What bounds it is latency: a launch, the dependent loads of a look at a sequence's last block, one or two barriers of the
+// cluster, a search for every block.  The counts (4 bytes a block) are read once.
 #include "cache_view.cuh"
 #include "cluster.cuh"
 
@@ -22,34 +23,38 @@ struct StepParams {
     int32_t num_seqs, max_blocks, num_rows, pairs_cap, num_blocks, block_tokens;
     int32_t shift;          // block_tokens = 2^shift, or -1
     int32_t max_len;        // tokens that a row of the table has room for
-    int32_t warp_words;     // words of 32 blocks that a warp looks at
+    int32_t tiles;          // of kTileBlocks blocks, in the pool
 
     __device__ __forceinline__ int whole(int tokens) const { return shift >= 0 ? tokens >> shift : tokens / block_tokens; }
     __device__ __forceinline__ int blocks_of(int tokens) const { return whole(tokens + block_tokens - 1); }
     __device__ __forceinline__ bool inside(int b) const { return b >= 0 && b < num_blocks; }
 };
 
-constexpr int kStepThreads = 1024, kStepWarps = kStepThreads / 32;
-constexpr int kStepIds = 4096;  // free ids that a CTA lists at a time
+constexpr int kStepMost = 1024;    // threads
+constexpr int kStepCluster = 16;   // CTAs
 constexpr uint32_t kBadArg = 1, kBadBlock = 2;
 
-// In dynamic shared memory: sums over the sequences in front of every one, and at [num_seqs] over all; then the bits of the free
-// blocks that the CTA looks at.
+// In dynamic shared memory: sums over the sequences in front of every one, and at [num_seqs] over all; then what the CTA knows of
+// its tiles, every size-th of the pool's.  A tile has a word of 32 blocks for each warp.
 struct StepShared {
-    int32_t *blocks, *rows, *copies;
-    int32_t* entries;  // entries of the table that are shared with a parent's or given back
-    int32_t* first;    // cache index of the first new token; -1: refused
-    int32_t* ids;      // [kStepIds] free blocks, counted from the CTA's first
-    uint32_t* free;    // [kStepWarps * warp_words]
+    int32_t* sums[4];   // blocks, rows, copies; entries of the table that are shared with a parent's or given back
+    int32_t* first;     // cache index of the first new token; -1: refused
+    int32_t* count;     // free blocks of a tile,
+    int32_t* start;     // and of all tiles of the pool in front of it
+    uint32_t* free;     // [warps] a tile: the free blocks' bits
+    int32_t* before;    // [warps] a tile: free blocks of the tile in front of a word
 
-    __device__ __forceinline__ StepShared(char* smem, const StepParams& p) {
+    __device__ __forceinline__ StepShared(char* smem, const StepParams& p, int tiles, int warps) {
         const int n = p.num_seqs + 1;
-        blocks = reinterpret_cast<int32_t*>(smem);
-        rows = blocks + n, copies = rows + n, entries = copies + n, first = entries + n, ids = first + n;
-        free = reinterpret_cast<uint32_t*>(ids + kStepIds);
+        sums[0] = reinterpret_cast<int32_t*>(smem);
+        sums[1] = sums[0] + n, sums[2] = sums[1] + n, sums[3] = sums[2] + n, first = sums[3] + n;
+        count = first + n, start = count + tiles;
+        free = reinterpret_cast<uint32_t*>(start + tiles);
+        before = reinterpret_cast<int32_t*>(free + warps * tiles);
     }
 };
-static int64_t step_smem(int64_t num_seqs, int64_t warp_words) { return (5 * (num_seqs + 1) + kStepIds + kStepWarps * warp_words) * 4; }
+static int64_t step_smem(int64_t num_seqs, int64_t tiles, int warps) { return (5 * (num_seqs + 1) + (2 + 2 * warps) * tiles) * 4; }
+constexpr int kStepStatic = 26 * 1024;  // bytes of shared memory beside those
 
 // What a sequence asks for.  The loads come in two steps, so that others can be started in between.
 struct Need {
@@ -117,17 +122,69 @@ __device__ __forceinline__ void step_sync(uint32_t size) {
     else __syncthreads();
 }
 
-__global__ void __launch_bounds__(kStepThreads, 1) advance_tables(const __grid_constant__ StepParams p) {
+// Sums over the block in front of every thread of N values a thread, none above 2^31 - 1; total: of all.  Only the first `busy` warps
+// have any.  shared: [N][32], not in use since the last barrier.
+template <int N, int kWarps>
+__device__ __forceinline__ void sum_before(uint32_t (&v)[N], uint32_t (&total)[N], uint32_t (*shared)[32], int busy) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (warp < busy) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            uint32_t incl = v[k];
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t up = __shfl_up_sync(~0u, incl, o);
+                if (lane >= o) incl = add_up(incl, up);
+            }
+            if (lane == 31) shared[k][warp] = incl;
+            v[k] = __shfl_up_sync(~0u, incl, 1);
+            if (lane == 0) v[k] = 0;
+        }
+    }
+    __syncthreads();
+    if (busy > 1) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            if (warp != k % kWarps) continue;
+            uint32_t incl = lane < busy ? shared[k][lane] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t up = __shfl_up_sync(~0u, incl, o);
+                if (lane >= o) incl = add_up(incl, up);
+            }
+            shared[k][lane] = incl;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if (warp > 0 && warp < busy) v[k] = add_up(v[k], shared[k][warp - 1]);
+        total[k] = shared[k][busy - 1];
+    }
+}
+
+// A block that gets new tokens, with what the rows of its tokens need.
+struct Handed {
+    int64_t slot;       // of the sequence's cache index 0, were all its blocks in a row with this one
+    int32_t lo, hi;     // cache indices of the new tokens in the block
+    int32_t row, pos;   // row and position of cache index 0
+};
+constexpr int64_t kNoSlot = INT64_MIN;
+
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_constant__ StepParams p) {
+    constexpr int kWarps = kThreads / 32;
     extern __shared__ __align__(16) char smem[];
-    __shared__ uint32_t s_sum[4][kStepWarps];
-    __shared__ int32_t s_free[kStepWarps];   // of every warp, then before it
-    __shared__ int32_t s_count;              // free blocks that this CTA looks at
+    __shared__ uint32_t s_sum[4][32];
+    __shared__ Handed s_block[kWarps][32];
     __shared__ int32_t s_freed;
     __shared__ uint32_t s_bad;
-    __shared__ int32_t s_all_bad[kMaxCluster], s_all_freed[kMaxCluster];  // in the first CTA
+    __shared__ int32_t s_all_bad[kStepCluster], s_all_freed[kStepCluster];  // in the first CTA
     const uint32_t rank = cluster_rank(), size = cluster_size();
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.num_seqs;
-    const StepShared sh(smem, p);
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.num_seqs, T = p.block_tokens;
+    const int tiles = (p.tiles + (int)size - 1) / (int)size;  // of this CTA; the last may lie behind the pool
+    const StepShared sh(smem, p, tiles, kWarps);
+    const int32_t *const blocks = sh.sums[0], *const rows = sh.sums[1], *const copied = sh.sums[2], *const entries = sh.sums[3];
     if (tid == 0) s_freed = 0, s_bad = 0;
     grid_dependency_launch();
     grid_dependency_wait();
@@ -135,32 +192,26 @@ __global__ void __launch_bounds__(kStepThreads, 1) advance_tables(const __grid_c
     // ---- the free blocks, and what the first sequences ask for
     Ask ask;
     if (tid < S) ask.lengths(p, tid);
-    const int64_t cta_block = (int64_t)rank * kStepWarps * p.warp_words * 32;
-    uint32_t* const words = sh.free + warp * p.warp_words;
-    int found = 0;
-    constexpr int kAtOnce = 8;
-    for (int w0 = 0; w0 < p.warp_words; w0 += kAtOnce) {
-        bool is[kAtOnce];
+    auto first_block = [&](int tile) { return ((uint32_t)tile * size + rank) * kThreads + warp * 32; };  // of this warp's word
+    constexpr int kAtOnce = kThreads == kStepMost ? 16 : 8;
+    for (int t0 = 0; t0 < tiles || t0 == 0; t0 += kAtOnce) {
+        int count[kAtOnce];  // loaded without a question, so that the loads overlap
+        const uint32_t b0 = first_block(t0) + lane, step = size * kThreads, last = (uint32_t)p.num_blocks - 1;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) count[i] = p.refs[min(b0 + i * step, last)];
+        if (t0 == 0 && tid < S) ask.more(p, tid);
+        uint32_t mine = 0;  // lane i keeps word i
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-            const int64_t b = cta_block + ((int64_t)warp * p.warp_words + w0 + i) * 32 + lane;
-            is[i] = w0 + i < p.warp_words && b < p.num_blocks && p.refs[b] == 0;
+            const uint32_t word = __ballot_sync(~0u, count[i] == 0 && b0 + i * step <= last);
+            if (lane == i) mine = word;
         }
-        if (w0 == 0 && tid < S) ask.more(p, tid);
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const uint32_t word = __ballot_sync(~0u, is[i]);
-            if (w0 + i < p.warp_words) {
-                if (lane == 0) words[w0 + i] = word;
-                found += __popc(word);
-            }
-        }
+        if (lane < min(kAtOnce, tiles - t0)) sh.free[(t0 + lane) * kWarps + warp] = mine;
     }
-    if (lane == 0) s_free[warp] = found;
 
     // ---- the sums in front of every sequence
     uint32_t bad = 0, run[4] = {0, 0, 0, 0};
-    for (int base = 0; base < S || base == 0; base += kStepThreads) {
+    for (int base = 0; base < S; base += kThreads) {
         const int s = base + tid;
         Need n;
         if (s < S) {
@@ -172,67 +223,60 @@ __global__ void __launch_bounds__(kStepThreads, 1) advance_tables(const __grid_c
             n = ask.need(p, &bad);
             sh.first[s] = n.first;
         }
-        uint32_t incl[4] = {(uint32_t)n.blocks, (uint32_t)n.rows, (uint32_t)n.copies, (uint32_t)n.entries}, before[4];
+        uint32_t v[4] = {(uint32_t)n.blocks, (uint32_t)n.rows, (uint32_t)n.copies, (uint32_t)n.entries}, total[4];
+        if (base > 0) __syncthreads();
+        sum_before<4, kWarps>(v, total, s_sum, min(kWarps, (S - base + 31) / 32));
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const uint32_t up = __shfl_up_sync(~0u, incl[k], o);
-                if (lane >= o) incl[k] = add_up(incl[k], up);
-            }
-            before[k] = __shfl_up_sync(~0u, incl[k], 1);
-            if (lane == 0) before[k] = 0;
-            if (lane == 31) s_sum[k][warp] = incl[k];
+            if (s < S) sh.sums[k][s] = (int32_t)add_up(run[k], v[k]);
+            run[k] = add_up(run[k], total[k]);
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t all = s_sum[k][lane];  // (as many warps as lanes)
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const uint32_t up = __shfl_up_sync(~0u, all, o);
-                if (lane >= o) all = add_up(all, up);
-            }
-            const uint32_t total = __shfl_sync(~0u, all, 31), warps = __shfl_sync(~0u, all, max(warp - 1, 0));
-            if (s < S) (sh.blocks + k * (S + 1))[s] = (int32_t)add_up(run[k], add_up(warp ? warps : 0, before[k]));
-            run[k] = add_up(run[k], total);
-        }
-        if (base == 0 && warp == 0) {
-            const int own = s_free[lane];
-            int sum = own;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int up = __shfl_up_sync(~0u, sum, o);
-                if (lane >= o) sum += up;
-            }
-            s_free[lane] = sum - own;
-            if (lane == 31) s_count = sum;
-        }
-        if (base + kStepThreads < S) __syncthreads();
     }
-    if (tid < 4) (sh.blocks + tid * (S + 1))[S] = (int32_t)(tid == 0 ? run[0] : tid == 1 ? run[1] : tid == 2 ? run[2] : run[3]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (tid == 0) sh.sums[k][S] = (int32_t)run[k];
     if (bad) atomicOr(&s_bad, bad);
+    __syncthreads();
+    for (int t = warp; t < tiles; t += kWarps) {  // words of a tile
+        const int own = lane < kWarps ? __popc(sh.free[t * kWarps + lane]) : 0;
+        int sum = own;
+#pragma unroll
+        for (int o = 1; o < kWarps; o *= 2) {
+            const int up = __shfl_up_sync(~0u, sum, o);
+            if (lane >= o) sum += up;
+        }
+        if (lane < kWarps) sh.before[t * kWarps + lane] = sum - own;
+        if (lane == kWarps - 1) sh.count[t] = sum;
+    }
     step_sync(size);
 
-    // ---- who gets it: the sequences in front of the first that does not fit
-    int n_free = 0, rank_before = 0;
-    for (uint32_t r = 0; r < size; ++r) {
-        const int n = size > 1 ? load_remote(&s_count, r) : s_count;
-        if (r < rank) rank_before += n;
-        n_free += n;
+    // ---- the tiles of all CTAs, and who gets what: the sequences in front of the first that does not fit
+    uint32_t n_free = 0;
+    for (int base = 0; base < p.tiles; base += kThreads) {
+        const int t = base + tid;
+        uint32_t v[1] = {t >= p.tiles ? 0u : (uint32_t)(size > 1 ? load_remote(&sh.count[(uint32_t)t / size], (uint32_t)t % size) : sh.count[t])}, total[1];
+        if (base > 0) __syncthreads();
+        sum_before<1, kWarps>(v, total, s_sum, min(kWarps, (p.tiles - base + 31) / 32));
+        if (t < p.tiles && (uint32_t)t % size == rank) sh.start[(uint32_t)t / size] = (int32_t)(n_free + v[0]);
+        n_free += total[0];
     }
+    for (int t = tid; t < tiles; t += kThreads)
+        if ((int64_t)t * size + rank >= p.tiles) sh.start[t] = INT32_MAX;
+    // No CTA ends while another reads its counts: the barrier that all arrive at here, or behind the reads of other sequences' rows.
+    const bool reads_others = p.parents || p.pairs_cap > 0;
+    if (size > 1 && !reads_others) cluster_arrive();
     int fits = S;
-    if (sh.blocks[S] > n_free || sh.rows[S] > p.num_rows || sh.copies[S] > p.pairs_cap) {
+    if (blocks[S] > (int)n_free || rows[S] > p.num_rows || copied[S] > p.pairs_cap) {
         fits = 0;
         for (int hi = S; hi - fits > 1;) {
             const int mid = (fits + hi) / 2;
-            if (sh.blocks[mid] <= n_free && sh.rows[mid] <= p.num_rows && sh.copies[mid] <= p.pairs_cap) fits = mid;
+            if (blocks[mid] <= (int)n_free && rows[mid] <= p.num_rows && copied[mid] <= p.pairs_cap) fits = mid;
             else hi = mid;
         }
     }
-    const int n_taken = sh.blocks[fits], n_rows = sh.rows[fits], n_copies = sh.copies[fits], n_entries = sh.entries[S];
-    const int all = size * kStepThreads, me = rank * kStepThreads + tid;
-    auto copies = [&](int s) { return sh.copies[s + 1] > sh.copies[s]; };
+    const int n_taken = blocks[fits], n_rows = rows[fits], n_copies = copied[fits], n_entries = entries[S];
+    const int all = size * kThreads, me = (warp * size + rank) * 32 + lane;
+    auto copies = [&](int s) { return copied[s + 1] > copied[s]; };
     auto parent_of = [&](int s) { return p.parents ? p.parents[s] : -1; };
     int freed = 0;
     auto give_back = [&](int b) {
@@ -247,7 +291,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) advance_tables(const __grid_c
 
     // ---- shared and given back blocks, sources of copies: everything that reads other sequences' rows of the table
     for (int e = me; e < n_entries; e += all) {
-        const int s = last_at_most(sh.entries, S, e), j = e - sh.entries[s], parent = parent_of(s);
+        const int s = last_at_most(entries, S, e), j = e - entries[s], parent = parent_of(s);
         int32_t* const row = p.table + (int64_t)s * p.max_blocks;
         if (parent < 0) {
             give_back(row[p.blocks_of(p.new_lens[s]) + j]);
@@ -261,77 +305,111 @@ __global__ void __launch_bounds__(kStepThreads, 1) advance_tables(const __grid_c
     for (int s = me; n_copies > 0 && s < fits; s += all) {
         if (!copies(s)) continue;
         const int parent = parent_of(s), b = p.table[(int64_t)(parent >= 0 ? parent : s) * p.max_blocks + p.whole(sh.first[s])];
-        p.pairs[sh.copies[s]].x = p.inside(b) ? b : -1;
+        p.pairs[copied[s]].x = p.inside(b) ? b : -1;
         if (parent < 0) give_back(b);
         else if (!p.inside(b)) bad |= kBadBlock;
     }
-    if (p.parents || p.pairs_cap > 0) step_sync(size);  // (without these no row is read that is not the reader's own)
+    if (size > 1 && reads_others) cluster_sync();
+    else __syncthreads();
 
-    // ---- the free blocks to their sequences
-    for (int e = me; e < n_entries; e += all) {
-        const int s = last_at_most(sh.entries, S, e);
-        if (parent_of(s) < 0) p.table[(int64_t)s * p.max_blocks + p.blocks_of(p.new_lens[s]) + e - sh.entries[s]] = -1;
-    }
-    const int mine = min(s_count, n_taken - rank_before);  // of the free blocks that this CTA looks at
-    for (int base = 0; base < mine; base += kStepIds) {
-        const int end = min(mine, base + kStepIds);
-        int r0 = s_free[warp];
-        for (int w = 0; w < p.warp_words && r0 < end; ++w) {
-            const uint32_t word = words[w];
-            const int r = r0 + __popc(word & ((1u << lane) - 1));
-            if (word >> lane & 1u && r >= base && r < end) sh.ids[r - base] = (warp * p.warp_words + w) * 32 + lane;
-            r0 += __popc(word);
-        }
-        __syncthreads();
-        for (int i = tid; i < end - base; i += kStepThreads) {
-            const int b = (int)cta_block + sh.ids[i], r = rank_before + base + i, s = last_at_most(sh.blocks, fits, r), j = r - sh.blocks[s];
-            const int have = copies(s) ? p.whole(sh.first[s]) : p.blocks_of(sh.first[s]);
-            p.table[(int64_t)s * p.max_blocks + have + j] = b;
+    // ---- the free blocks to their sequences, a warp's word of every tile; rows, positions and slots of the tokens in them
+    const bool writes_rows = p.positions || p.slots;
+    auto write_row = [&](int row, int position, int64_t slot) {
+        if (p.positions) p.positions[row] = position;
+        if (p.slots) p.slots[row] = slot;
+    };
+    auto end_of = [&](int s) { return sh.first[s] + rows[s + 1] - rows[s]; };
+    for (int t = 0; t < tiles && sh.start[t] < n_taken; ++t) {
+        const uint32_t word = sh.free[t * kWarps + warp];
+        const int r0 = sh.start[t] + sh.before[t * kWarps + warp], n = min(__popc(word), n_taken - r0);
+        const int k = __popc(word & ((1u << lane) - 1)), r = r0 + k;
+        if (n <= 0) continue;
+        if (word >> lane & 1u && k < n) {
+            const int b = (int)(first_block(t) + lane), s = last_at_most(blocks, fits, r), j = r - blocks[s], first = sh.first[s];
+            const bool copy = copies(s);
+            const int column = (copy ? p.whole(first) : p.blocks_of(first)) + j;
+            p.table[(int64_t)s * p.max_blocks + column] = b;
             p.refs[b] = 1;
-            if (j == 0 && copies(s)) p.pairs[sh.copies[s]].y = b;
+            if (j == 0 && copy) p.pairs[copied[s]].y = b;
+            const int64_t begin = (int64_t)column * T;
+            s_block[warp][k] = Handed{(int64_t)b * T - begin, (int)max(begin, (int64_t)first), (int)min(begin + T, (int64_t)end_of(s)),
+                                      rows[s] - first, p.first_pos ? p.first_pos[s] - first : 0};
         }
-        if (end < mine) __syncthreads();
+        __syncwarp();
+        if (writes_rows) {
+            if (T >= 32) {
+                for (int i = 0; i < n; ++i) {
+                    const Handed x = s_block[warp][i];
+                    for (int index = x.lo + lane; index < x.hi; index += 32) write_row(x.row + index, x.pos + index, x.slot + index);
+                }
+            } else {
+                const int at_once = 32 / T, part = lane / T;  // blocks at a time
+                for (int i = part; i < n && part < at_once; i += at_once) {
+                    const Handed x = s_block[warp][i];
+                    const int index = x.lo + lane - part * T;
+                    if (index < x.hi) write_row(x.row + index, x.pos + index, x.slot + index);
+                }
+            }
+        }
+        __syncwarp();
     }
+    for (int e = me; e < n_entries; e += all) {
+        const int s = last_at_most(entries, S, e);
+        if (parent_of(s) < 0) p.table[(int64_t)s * p.max_blocks + p.blocks_of(p.new_lens[s]) + e - entries[s]] = -1;
+    }
+
+    // ---- lengths, row starts, and the rows in blocks that were there: what is left of a last block
+    for (int base = (warp * size + rank) * 32; base <= S; base += all) {
+        const int s = base + lane;
+        Handed x{0, 0, 0, 0, 0};
+        if (s < S) {
+            const int old = p.lens[s], now = p.new_lens[s], first = sh.first[s];
+            const bool grows = now > old || parent_of(s) >= 0, stays = first < 0 || (grows && s >= fits);
+            p.lens_out[s] = stays ? old : now;
+            const int n = stays ? 0 : p.whole(first);
+            if (writes_rows && !stays && n * T != first && !copies(s) && rows[s + 1] > rows[s]) {
+                const int b = p.table[(int64_t)s * p.max_blocks + n];
+                x = Handed{p.inside(b) ? ((int64_t)b - n) * T : kNoSlot, first, (int)min((int64_t)end_of(s), ((int64_t)n + 1) * T), rows[s] - first,
+                           p.first_pos ? p.first_pos[s] - first : 0};
+                if (T < 128)
+                    for (int index = x.lo; index < x.hi; ++index) write_row(x.row + index, x.pos + index, x.slot == kNoSlot ? -1 : x.slot + index);
+            }
+        }
+        if (p.starts && s <= S) p.starts[s] = rows[min(s, fits)];
+        for (unsigned more = T < 128 ? 0 : __ballot_sync(~0u, x.hi > x.lo); more; more &= more - 1) {
+            const int of = __ffs(more) - 1, lo = __shfl_sync(~0u, x.lo, of), hi = __shfl_sync(~0u, x.hi, of);
+            const int row = __shfl_sync(~0u, x.row, of), pos = __shfl_sync(~0u, x.pos, of);
+            const int64_t slot = __shfl_sync(~0u, x.slot, of);
+            for (int index = lo + lane; index < hi; index += 32) write_row(row + index, pos + index, slot == kNoSlot ? -1 : slot + index);
+        }
+    }
+    if (writes_rows)
+        for (int r = n_rows + me; r < p.num_rows; r += all) {
+            if (p.positions) p.positions[r] = 0;
+            if (p.slots) p.slots[r] = -1;
+        }
+
+    // ---- one code, always the same for the same call, and the counts
     if (bad) atomicOr(&s_bad, bad);
     if (freed) atomicAdd(&s_freed, freed);
     __syncthreads();
+    if (size > 1 && !reads_others) cluster_wait();
     if (tid == 0) {
         if (size > 1) store_remote(&s_all_bad[rank], 0, (int32_t)s_bad), store_remote(&s_all_freed[rank], 0, s_freed);
         else s_all_bad[0] = (int32_t)s_bad, s_all_freed[0] = s_freed;
     }
-    step_sync(size);
-
-    // ---- rows, lengths, counts
-    if (p.starts)
-        for (int s = me; s <= S; s += all) p.starts[s] = sh.rows[min(s, fits)];
-    for (int s = me; s < S; s += all) {
-        const int old = p.lens[s], now = p.new_lens[s];
-        const bool grows = now > old || parent_of(s) >= 0;
-        p.lens_out[s] = sh.first[s] < 0 || (grows && s >= fits) ? old : now;
+    if (size > 1) {
+        cluster_arrive();
+        if (rank > 0) return;
+        cluster_wait();
     }
-    if (p.positions || p.slots)
-        for (int r = me; r < p.num_rows; r += all) {
-            int position = 0;
-            int64_t slot = -1;
-            if (r < n_rows) {
-                const int s = last_at_most(sh.rows, fits, r), j = r - sh.rows[s], index = sh.first[s] + j;
-                position = p.first_pos ? p.first_pos[s] + j : index;
-                if (p.slots) {
-                    const int n = p.whole(index), b = __ldcg(&p.table[(int64_t)s * p.max_blocks + n]);
-                    if (p.inside(b)) slot = ((int64_t)b - n) * p.block_tokens + index;
-                }
-            }
-            if (p.positions) p.positions[r] = position;
-            if (p.slots) p.slots[r] = slot;
-        }
-    if (rank == 0 && tid == 0) {
+    if (tid == 0) {
         uint32_t all_bad = 0;
         int all_freed = 0;
         for (uint32_t r = 0; r < size; ++r) all_bad |= (uint32_t)s_all_bad[r], all_freed += s_all_freed[r];
         if (p.num_pairs) *p.num_pairs = n_copies;
-        if (p.free_count) *p.free_count = n_free - n_taken + all_freed;
-        // One code, always the same for the same call.
-        if ((all_bad & kBadArg) || (fits < S && sh.blocks[fits + 1] <= n_free)) report(p.status, AMOEBA_ERR_INVALID_ARG);
+        if (p.free_count) *p.free_count = (int)n_free - n_taken + all_freed;
+        if ((all_bad & kBadArg) || (fits < S && blocks[fits + 1] <= (int)n_free)) report(p.status, AMOEBA_ERR_INVALID_ARG);
         else if (fits < S) report(p.status, AMOEBA_ERR_NO_FREE_BLOCKS);
         else if (all_bad & kBadBlock) report(p.status, AMOEBA_ERR_BAD_BLOCK_ID);
     }
@@ -369,9 +447,14 @@ extern "C" amoeba_status amoeba_advance_tables(const amoeba_layout* layout, cons
     p.max_len = (int32_t)std::min<int64_t>((int64_t)a.max_blocks_per_seq * layout->block_tokens, kMaxTokens);
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
-    const int cluster = p.num_blocks <= 8192 && p.num_seqs <= kStepThreads && p.num_rows <= 4 * kStepThreads ? 1 : kMaxCluster;
-    p.warp_words = (int32_t)(((int64_t)p.num_blocks + cluster * kStepThreads - 1) / (cluster * kStepThreads));
-    const int64_t smem = step_smem(p.num_seqs, p.warp_words);
-    if (smem > dev.smem_optin - 2048) return AMOEBA_ERR_TOO_LARGE;
-    return launch_clusters(advance_tables, cluster, kStepThreads, (size_t)smem, cluster, true, static_cast<cudaStream_t>(cuda_stream), p);
+    // A few sequences and blocks are soonest done by one small CTA; then a cluster's loads and stores count, then its bytes.
+    const bool large = p.num_blocks > 131072 || p.num_seqs > 512 || p.num_rows > 8192;
+    const bool small = p.num_blocks <= 8192 && p.num_seqs <= 256 && p.num_rows <= 1024;
+    const int cluster = small ? 1 : large ? kStepCluster : kMaxCluster, threads = large ? kStepMost : 256;
+    p.tiles = (int32_t)(((int64_t)p.num_blocks + threads - 1) / threads);
+    const int64_t smem = step_smem(p.num_seqs, (p.tiles + cluster - 1) / cluster, threads / 32);
+    if (smem > dev.smem_optin - kStepStatic) return AMOEBA_ERR_TOO_LARGE;
+    if (large && allow_large_clusters((const void*)advance_tables<kStepMost>) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    return launch_clusters(large ? advance_tables<kStepMost> : advance_tables<256>, cluster, threads, (size_t)smem, cluster, true,
+                           static_cast<cudaStream_t>(cuda_stream), p);
 }

@@ -43,6 +43,23 @@ __device__ __forceinline__ void store_remote(int32_t* p, uint32_t rank, int32_t 
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(remote), "r"(v) : "memory");
 }
 
+// Lets a kernel have clusters of up to 16 CTAs, once per device.
+inline cudaError_t allow_large_clusters(const void* kernel) {
+    static std::mutex mutex;
+    static const void* known[kMaxDevices][8];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(mutex);
+    int i = 0;
+    if (dev >= 0 && dev < kMaxDevices) {
+        while (i < 8 && known[dev][i] && known[dev][i] != kernel) ++i;
+        if (i < 8 && known[dev][i]) return cudaSuccess;
+    }
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && dev >= 0 && dev < kMaxDevices && i < 8) known[dev][i] = kernel;
+    return e;
+}
+
 template <class... P, class... A>
 inline amoeba_status launch_clusters(void (*kernel)(P...), int64_t grid, int threads, size_t smem, int cluster, bool early,
                                      cudaStream_t stream, const A&... args) {
