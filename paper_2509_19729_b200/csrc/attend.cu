@@ -44,6 +44,7 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
 
     Walk walk{};
     int64_t n;
+    if (B::kShared && p.batch.by_groups()) grid_dependency_wait();  // the groups are there
     if (p.whole) {
         walk.open(sh, p.batch, p.cache.block_tokens, blockIdx.x / sh.kv_heads);
         if (!walk.seq.ok && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
@@ -56,7 +57,10 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
         n = end - begin;
     }
     grid_dependency_launch();
-    if (n == 0) return;
+    if (n == 0) {
+        if (B::kShared) grid_dependency_wait();  // (what ends behind this kernel ends behind those in front of it too)
+        return;
+    }
 
     Ahead<D, true, kFewTile, B> ahead(p.cache, p.batch, sh, p.status, walk, n, warp * 16);
     int slot_in = 0, slot = 0;
@@ -201,6 +205,12 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
         const int rows = min(R, walk.seq.qn * sh.group - walk.m * R);
         const bool direct = from_start && unit_ends;
         const int64_t part = (int64_t)(2 * blockIdx.x + (from_start ? 1 : 0)) * R;
+        Own own{};
+        if constexpr (B::kShared)
+            if (direct && walk.seq.first > 0) {
+                own = own_of(p, walk.s);
+                grid_dependency_wait();  // the groups' pass is done
+            }
         for (int i = tid; i < rows * (D / 4); i += kFewThreads) {
             const int r = i / (D / 4), d = i % (D / 4) * 4;
             float top = -INFINITY;
@@ -217,7 +227,7 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
                 j.acc.x += f * x.x, j.acc.y += f * x.y, j.acc.z += f * x.z, j.acc.w += f * x.w;
             }
             if (direct) {
-                finish<T, D>(p, walk.seq, walk.h, walk.m * R + r, d, j);
+                finish<T, D>(p, walk.seq, own, walk.h, walk.m * R + r, d, j);
             } else {
                 *reinterpret_cast<float4*>(p.part_o + (part + r) * D + d) = j.acc;
                 if (d == 0) p.part_m[part + r] = top, p.part_l[part + r] = j.l;
@@ -226,6 +236,7 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
         __syncthreads();
         if (n > 1) walk.next(sh, p.batch, p.cache.block_tokens);
     }
+    if (B::kShared) grid_dependency_wait();
 }
 
 // ------------------------------------------------------------------------------------------------ joining
@@ -248,6 +259,9 @@ __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, in
     if (cut.begin == cut.end || cut.t == 0 || first_row >= cut.rows) return;
     const int64_t first = cut.begin - cut.t, last = first + cut.tiles;
     const Seq q = sequence(p.batch, cut.s, p.cache.block_tokens);
+    Own own{};
+    if constexpr (B::kShared)
+        if (q.first > 0) own = own_of(p, cut.s);
     int c0 = mine - 1;
     while (p.cuts[c0].begin == p.cuts[c0].end) --c0;  // (empty shares)
     if (p.cuts[c0].begin > first) return;
@@ -285,7 +299,7 @@ __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, in
             for (int w = 1; w < kWarps; ++w) j.add(s_top[w], s_l[w], s_acc[w][lane % kLanes]);
         }
         if (r >= cut.rows || lane >= kLanes) continue;
-        finish<T, D>(p, q, cut.h, cut.m * R + r, lane * 4, j);
+        finish<T, D>(p, q, own, cut.h, cut.m * R + r, lane * 4, j);
     }
 }
 // Blocks [0, few_ctas * few_rows) join what attend_few has cut, the others what attend_many has.
@@ -335,7 +349,7 @@ static amoeba_status run_few(AttendParams<B>& p, int sms, int* ctas, cudaStream_
     if (ensure_dynamic_smem((const void*)attend_few<T, D, NT, B>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
     *ctas = std::min(F::kCtas * sms, kMaxFewCtas);
     return launch_kernel(attend_few<T, D, NT, B>, p.whole ? p.batch.num_seqs * p.shape.kv_heads : *ctas, kFewThreads, F::kSmem, stream,
-                         false, p);
+                         B::kShared, p);
 }
 
 // Sequences with few rows (new tokens times query heads per key head) are read by attend_few, whose time is that of reading
@@ -372,7 +386,7 @@ static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char*
         many.shape.tile = kManyTile;
         many_ctas = std::min(sms, kMaxSms);
         many_blocks = many_ctas * (kManyRows / kJoinRows<1, B>);
-        if ((st = launch_attend_many(many, tp, dtype, D, many_ctas, stream)) != AMOEBA_OK) return st;
+        if ((st = launch_attend_many(many, tp, dtype, D, many_ctas, stream)) != AMOEBA_OK || groups) return st;
     }
     return launch_kernel(attend_join<T, D, B>, few_ctas * few_most + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_most, many,
                          many_ctas);
@@ -475,35 +489,47 @@ struct PrefixParams {
     Batch batch;
     const int32_t *group_starts, *prefix_lens;
     Group* groups;
-    int32_t *first, *status;
+    int64_t* tile0;
+    Own* own;
+    int32_t* status;
     int32_t num_groups, max_group_rows, block_tokens;
+    int32_t kv_heads, group;  // query heads per key head
+    int32_t many_ctas;        // of the groups' pass, if it is attend_many's
 };
 
 // What a group shares: no more than its shortest sequence has in front of its new tokens, and nothing where fewer than two have
-// rows or one is bad; then its sequences attend by themselves.  One block, a warp to a group.
+// rows, one is bad, or it does not pay; then its sequences attend by themselves.  One block, a warp to a group.
+//
+// Whether it pays is counted in tiles of 128 tokens (a tile of a sequence with few rows costs about as much as one of 256 rows): every
+// tile of rows reads the prefix, of each sequence by itself or of the group's rows together; a group's unit costs its start and end, about
+// four tiles, and taking up the sums half a tile for a few rows, six for 256.
 constexpr int kPrefixThreads = 1024;
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_constant__ PrefixParams p) {
-    const int tid = threadIdx.x, lane = tid % 32, S = p.batch.num_seqs;
+    __shared__ int64_t s_warp[kPrefixThreads / 32];
+    const int tid = threadIdx.x, lane = tid % 32, S = p.batch.num_seqs, G = p.num_groups;
     bool bad = false;
-    for (int g = tid; g < p.num_groups; g += kPrefixThreads) {
+    for (int g = tid; g < G; g += kPrefixThreads) {
         const int a = p.group_starts[g], z = p.group_starts[g + 1];
         bad |= a < 0 || z < a || z > S;
     }
-    for (int s = tid; s < S; s += kPrefixThreads) p.first[s] = 0;
+    for (int s = tid; s < S; s += kPrefixThreads) p.own[s] = Own{};
     bad = __syncthreads_or(bad);
     if (bad && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
-    for (int g = tid / 32; g < p.num_groups; g += kPrefixThreads / 32) {
+    for (int g = tid / 32; g < G; g += kPrefixThreads / 32) {
         const int a = bad ? 0 : p.group_starts[g], z = bad ? 0 : p.group_starts[g + 1];
-        int least = INT32_MAX, row = INT32_MAX, with_rows = 0, q0 = INT32_MAX, q1 = 0;
+        int least = INT32_MAX, row = INT32_MAX, with_rows = 0, q0 = INT32_MAX, q1 = 0, alone = 0, taking = 0;
         bool ok = true;
         for (int s = a + lane; s < z; s += 32) {
             const Seq q = sequence(p.batch, s, p.block_tokens);
             ok &= q.ok;
             if (q.qn == 0) continue;
+            const int tiles = (q.qn * p.group - 1) / kManyRows + 1;
             least = min(least, q.len - q.qn);
             row = min(row, s);
             q0 = min(q0, q.q0);
             q1 = max(q1, q.q0 + q.qn);
+            alone += tiles;
+            taking += q.qn * p.group <= kMaxFewRows ? 1 : 12 * tiles;  // half tiles
             ++with_rows;
         }
         ok = __all_sync(~0u, ok);
@@ -512,23 +538,58 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_
         with_rows = __reduce_add_sync(~0u, with_rows);
         q0 = __reduce_min_sync(~0u, q0);
         q1 = __reduce_max_sync(~0u, q1);
+        alone = __reduce_add_sync(~0u, alone);
+        taking = __reduce_add_sync(~0u, taking);
         Group out{0, 0, 0, 0};
+        int64_t tiles = 0;
         if (z > a) {
-            const int len = p.prefix_lens[g];
-            const bool wrong = len < 0 || (with_rows && q1 - q0 > p.max_group_rows);
+            const int given = p.prefix_lens[g];
+            const bool wrong = given < 0 || (with_rows && q1 - q0 > p.max_group_rows);
             if (wrong && lane == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
-            if (!wrong && ok && with_rows > 1 && min(len, least) > 0) {
-                out = Group{q0, q1 - q0, min(len, least), row};
-                for (int s = a + lane; s < z; s += 32) p.first[s] = out.len;
+            const int len = min(given, least), key_tiles = (len - 1) / kManyTile + 1;
+            if (!wrong && ok && with_rows > 1 && len > 0) {
+                const int row_tiles = (int)(((int64_t)(q1 - q0) * p.group - 1) / kManyRows) + 1;
+                if (2 * (int64_t)(alone - row_tiles) * key_tiles > 8 * (int64_t)row_tiles + taking) {
+                    out = Group{q0, q1 - q0, len, row};
+                    tiles = (int64_t)p.kv_heads * row_tiles * key_tiles;
+                    for (int s = a + lane; s < z; s += 32) p.own[s] = Own{len, q0, key_tiles, row_tiles, g, 0};
+                }
             }
         }
-        if (lane == 0) p.groups[g] = out;
+        if (lane == 0) p.groups[g] = out, p.tile0[g] = tiles;
     }
+    if (p.many_ctas == 0) return;
+    // the first tile of every group, and every CTA's share
+    __syncthreads();
+    int64_t run = 0;
+    for (int base = 0; base < G; base += kPrefixThreads) {
+        const int g = base + tid;
+        const int64_t own = g < G ? p.tile0[g] : 0;
+        int64_t incl = own;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t up = __shfl_up_sync(~0u, incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 31) s_warp[tid / 32] = incl;
+        __syncthreads();
+        int64_t before = run;
+        for (int w = 0; w < kPrefixThreads / 32; ++w) {
+            if (w < tid / 32) before += s_warp[w];
+            run += s_warp[w];
+        }
+        if (g < G) p.tile0[g] = before + incl - own;
+        __syncthreads();
+    }
+    if (tid == 0) p.tile0[G] = run;
+    const int64_t even = divide(run + p.many_ctas - 1, p.many_ctas);
+    for (int s = tid; s < S; s += kPrefixThreads)
+        if (p.own[s].first > 0) p.own[s].tile0 = p.tile0[p.own[s].tile0], p.own[s].even = even;
 }
 
 // Where the parts of the workspace begin: both passes' own, the carry, the groups and the sequences' first tokens.
 struct SharedSpace {
-    int64_t groups_pass, rest_pass, carry_o, carry_m, carry_l, groups, first, end;
+    int64_t groups_pass, rest_pass, carry_o, carry_m, carry_l, groups, tile0, own, end;
 };
 static SharedSpace shared_space(const amoeba_layout* l, const amoeba_batch* b, const amoeba_prefixes* x) {
     const int D = l->model.head_dim;
@@ -541,8 +602,9 @@ static SharedSpace shared_space(const amoeba_layout* l, const amoeba_batch* b, c
     s.carry_m = s.carry_o + heads * D * 4;
     s.carry_l = s.carry_m + heads * 4;
     s.groups = s.carry_l + heads * 4;
-    s.first = s.groups + (int64_t)x->num_groups * sizeof(Group);
-    s.end = s.first + ((int64_t)b->num_seqs * 4 + 15) / 16 * 16;
+    s.tile0 = s.groups + (int64_t)x->num_groups * sizeof(Group);
+    s.own = s.tile0 + ((int64_t)x->num_groups / 2 + 1) * 16;
+    s.end = s.own + (int64_t)b->num_seqs * sizeof(Own);
     return s;
 }
 
@@ -581,16 +643,28 @@ extern "C" amoeba_status amoeba_attend_shared(const amoeba_layout* layout, int32
     char* ws = static_cast<char*>(d_workspace);
     const SharedSpace at = shared_space(layout, batch, prefixes);
     p.carry = Carry{reinterpret_cast<float*>(ws + at.carry_o), reinterpret_cast<float*>(ws + at.carry_m), reinterpret_cast<float*>(ws + at.carry_l)};
-    PrefixParams x{p.batch, prefixes->d_group_starts, prefixes->d_prefix_lens, reinterpret_cast<Group*>(ws + at.groups),
-                   reinterpret_cast<int32_t*>(ws + at.first), d_status, prefixes->num_groups, group_rows, layout->block_tokens};
+    const int32_t num_groups = group_rows ? prefixes->num_groups : 0;
+    const bool many = rows_of(layout, group_rows) > kMaxGroupRows;
+    PrefixParams x{};
+    x.batch = p.batch;
+    x.group_starts = prefixes->d_group_starts, x.prefix_lens = prefixes->d_prefix_lens;
+    x.groups = reinterpret_cast<Group*>(ws + at.groups), x.tile0 = reinterpret_cast<int64_t*>(ws + at.tile0);
+    x.own = reinterpret_cast<Own*>(ws + at.own);
+    x.status = d_status;
+    x.num_groups = prefixes->num_groups, x.max_group_rows = group_rows, x.block_tokens = layout->block_tokens;
+    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group;
+    x.many_ctas = many ? std::min(dev.sms, kMaxSms) : 0;
     if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, false, x)) != AMOEBA_OK) return st;
-    p.batch.first = x.first;
-    if (prefixes->num_groups && group_rows) {
+    p.batch.own = x.own;
+    if (num_groups) {
         AttendParams<SharedBatch> g = p;
-        g.batch.groups = x.groups;
-        g.batch.num_seqs = prefixes->num_groups;
+        g.batch.groups = x.groups, g.batch.tile0 = x.tile0;
+        g.batch.num_seqs = num_groups;
         g.batch.max_q_len = group_rows;
         if ((st = attend_pass(layout, dtype, g, ws + at.groups_pass, dev.sms, stream)) != AMOEBA_OK) return st;
+        AttendParams<SharedBatch> cut{};  // where the parts of its units are
+        many_workspace(&cut, ws + at.groups_pass + few_workspace<Batch>(nullptr, nullptr, layout->model.head_dim), layout->model.head_dim);
+        p.cut = Carry{cut.part_o, cut.part_m, cut.part_l};
     }
     return attend_pass(layout, dtype, p, ws + at.rest_pass, dev.sms, stream);
 }

@@ -62,7 +62,36 @@ struct Share {
     int64_t begin, end;                  // of this CTA's run of tiles of the cut units
     int32_t begin_seq;
     int64_t begin_off;
+    Walk walk;                           // of groups: at the first tile
 };
+
+// Groups: all rows of one see the same tokens, so a unit's place in the end-to-end order of all tiles is a product, and the first tile of
+// every group is in memory.  Every CTA has `even` of them, the last ones fewer, without a look at the others; what is cut is joined where
+// it is taken up (attend.cuh).
+template <class B>
+__device__ bool make_group_share(const AttendParams<B>& p, Share& sh) {
+    const B& b = p.batch;
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        const int64_t all = __ldcg(b.tile0 + b.num_seqs), even = divide(all + gridDim.x - 1, gridDim.x);
+        const int64_t begin = min(blockIdx.x * even, all), end = min(begin + even, all);
+        int group = 0;  // the last that does not begin behind
+        for (int base = 0; base < b.num_seqs; base += 32) {
+            const unsigned in = __ballot_sync(~0u, base + lane < b.num_seqs && __ldcg(b.tile0 + base + lane) <= begin);
+            group = base + __popc(in) - 1;
+            if (in != ~0u) break;
+        }
+        if (end > begin) {
+            Walk w{};
+            w.open(p.shape, b, p.cache.block_tokens, group);
+            w.seek(p.shape, begin - __ldcg(b.tile0 + group));
+            if (lane == 0) sh.walk = w;
+        }
+        if (lane == 0) sh.rounds = 0, sh.begin = begin, sh.end = end;
+    }
+    __syncthreads();
+    return sh.end > sh.begin;
+}
 
 // All threads of the block.  False: this CTA has nothing to do.  done: [kMaxSms] for the tiles of the units dealt to every CTA.
 template <class B>
@@ -217,7 +246,10 @@ struct Parts {
             tiles = w.range.tiles;
         } else {
             if (left == 0) return false;
-            if (!opened) {
+            if (!opened && p.batch.by_groups()) {
+                opened = true;
+                w = sh.walk;
+            } else if (!opened) {
                 opened = true;
                 w.open(shape, p.batch, p.cache.block_tokens, sh.begin_seq);
                 w.seek(shape, sh.begin_off);
@@ -522,12 +554,22 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
     while (part.next(p, share)) {
         const Walk& w = part.w;
         const bool in_turn = B::kShared && part.in_turn;
-        // a bad block anywhere in the part: its tokens are looked up one by one below
+        // A bad block anywhere in the part: its tokens are looked up one by one below.  The table is asked now and the answer looked at behind
+        // the wait for the first logits.
         const int32_t* table = p.batch.table + (int64_t)w.seq.row * p.batch.max_blocks;
-        int bad = 0;
         const int part_lo = max(w.range.lo, w.range.base + w.t * kManyTile), part_hi = min(w.range.hi, w.range.base + (w.t + part.tiles) * kManyTile);
-        for (int i = part_lo / p.cache.block_tokens + (int)threadIdx.x % 128; i * (int64_t)p.cache.block_tokens < part_hi; i += 128)
-            bad |= table[i] < 0 || table[i] >= p.cache.num_blocks;
+        const int first_block = part_lo / p.cache.block_tokens + (int)threadIdx.x % 128;
+        const int blocks_end = part_hi > part_lo ? (part_hi - 1) / p.cache.block_tokens + 1 : 0;
+        constexpr int kAsked = 4;
+        int asked[kAsked];
+#pragma unroll
+        for (int k = 0; k < kAsked; ++k) asked[k] = first_block + k * 128 < blocks_end ? table[first_block + k * 128] : 0;
+        int bad = 0;
+        for (int i = first_block + kAsked * 128; i < blocks_end; i += 128) bad |= table[i] < 0 || table[i] >= p.cache.num_blocks;
+        const bool takes_part = in_turn || t < part.q_tiles;
+        if (ok && takes_part) ok = wait(&b.s_full[t], s_phase);
+#pragma unroll
+        for (int k = 0; k < kAsked; ++k) bad |= asked[k] < 0 || asked[k] >= p.cache.num_blocks;
         asm volatile(
             "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %0, 0;\n\t"
             "barrier.cta.red.or.pred q, %1, 128, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
@@ -541,10 +583,10 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
                   see_lo = !there ? 0 : sh.window > 0 ? max(pos - sh.window + 1, 0) : B::kShared ? w.seq.first : 0;
         const int first_tile = in_turn ? t : 0, step = in_turn ? 2 : 1;
         float m_ref = -INFINITY, l = 0.f;
-        if (ok && (in_turn || t < part.q_tiles)) ok = [&] {
+        if (ok && takes_part) ok = [&] {
             for (int i = first_tile; i < part.tiles; i += step) {
                 const int key0 = w.range.base + (w.t + i) * kManyTile;
-                if (!wait(&b.s_full[t], s_phase)) return false;
+                if (i > first_tile && !wait(&b.s_full[t], s_phase)) return false;
                 s_phase ^= 1;
                 tmem_fence_after();
                 if (__any_sync(~0u, key0 + kManyTile > see_hi || key0 < see_lo) || bad)
@@ -595,27 +637,33 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
         }
         if (ok && t < part.q_tiles) {
             const bool direct = part.from_start && part.to_end;
-            // A row's sum is `keep` of its own O, `other` of the second warpgroup's, `take` of the carried one.
+            // A row's sum is `keep` of its own O, `other` of the second warpgroup's, and what is carried.
             const bool into = B::kShared && w.seq.level, takes = B::kShared && direct && there && w.seq.first > 0;
             const int64_t head = B::kShared && there ? head_of(p, w.seq, w.h, row) : 0;
-            float keep = 1.f, other = 0.f, take = 0.f;
+            float keep = 1.f, other = 0.f;
             if (in_turn) {
                 const float m2 = p.part_m[at + 128], up = fmaxf(m_ref, m2), ref = up == -INFINITY ? 0.f : up;
                 keep = fast_exp2(m_ref - ref), other = fast_exp2(m2 - ref);
                 l = l * keep + p.part_l[at + 128] * other;
                 m_ref = up;
             }
+            Own own{};
+            float ref = 0.f;
+            auto carried = [&](auto add) {
+                if constexpr (B::kShared) take_up<D>(p, w.seq, own, w.h, row, add);
+            };
             if (takes) {
-                const float m2 = p.carry.m[head], up = fmaxf(m_ref, m2), ref = up == -INFINITY ? 0.f : up, f = fast_exp2(m_ref - ref);
-                take = fast_exp2(m2 - ref);
-                l = l * f + p.carry.l[head] * take;
-                keep *= f, other *= f;
+                if constexpr (B::kShared) own = own_of(p, w.s);
+                float up = m_ref;
+                carried([&](float m2, float, const float*) { up = fmaxf(up, m2); });
+                ref = up == -INFINITY ? 0.f : up;
+                const float f = fast_exp2(m_ref - ref);
+                l *= f, keep *= f, other *= f;
+                carried([&](float m2, float l2, const float*) { l += l2 * fast_exp2(m2 - ref); });
                 m_ref = up;
             }
-            if (direct && !into) {
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                keep *= inv, other *= inv, take *= inv;
-            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            if (direct && !into) keep *= inv, other *= inv;
             char* out = there ? row_of<D>(p.out, p, w.seq, w.h, row) : nullptr;
             float* const raw = direct ? p.carry.o + head * D : p.part_o + at * D;
 #pragma unroll
@@ -637,14 +685,17 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
                 if (!there) continue;
                 if (direct && !into) {
                     if (takes)
+                        carried([&](float m2, float, const float* from) {
+                            const float f = fast_exp2(m2 - ref) * inv;
 #pragma unroll
-                        for (int k = 0; k < 32; k += 4) {
-                            const float4 c4 = *reinterpret_cast<const float4*>(p.carry.o + head * D + j * 32 + k);
-                            o[k] = __float_as_uint(__uint_as_float(o[k]) + c4.x * take);
-                            o[k + 1] = __float_as_uint(__uint_as_float(o[k + 1]) + c4.y * take);
-                            o[k + 2] = __float_as_uint(__uint_as_float(o[k + 2]) + c4.z * take);
-                            o[k + 3] = __float_as_uint(__uint_as_float(o[k + 3]) + c4.w * take);
-                        }
+                            for (int k = 0; k < 32; k += 4) {
+                                const float4 c4 = *reinterpret_cast<const float4*>(from + j * 32 + k);
+                                o[k] = __float_as_uint(__uint_as_float(o[k]) + c4.x * f);
+                                o[k + 1] = __float_as_uint(__uint_as_float(o[k + 1]) + c4.y * f);
+                                o[k + 2] = __float_as_uint(__uint_as_float(o[k + 2]) + c4.z * f);
+                                o[k + 3] = __float_as_uint(__uint_as_float(o[k + 3]) + c4.w * f);
+                            }
+                        });
 #pragma unroll
                     for (int k = 0; k < 32; k += 8) {
                         uint32_t x[4];
@@ -679,14 +730,6 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     char* smem = smem_raw + (1024 - smem_u32(smem_raw) % 1024) % 1024;
     const int warp = threadIdx.x / 32;
     __shared__ Share share;
-    if (B::kShared) grid_dependency_wait();  // the groups are there
-    const bool busy = make_share(p, share, reinterpret_cast<int32_t*>(smem));
-    grid_dependency_launch();
-    if (!busy) {
-        grid_dependency_wait();
-        return;
-    }
-    __syncthreads();
     if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&b.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -700,9 +743,22 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
+    if (B::kShared) {
+        grid_dependency_wait();  // the groups are there, or what is carried
+        grid_dependency_launch();
+    }
+    bool busy;
+    if constexpr (B::kShared) busy = p.batch.by_groups() ? make_group_share(p, share) : make_share(p, share, reinterpret_cast<int32_t*>(smem));
+    else busy = make_share(p, share, reinterpret_cast<int32_t*>(smem));
+    if (!B::kShared) grid_dependency_launch();
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
+    if (!busy) {
+        grid_dependency_wait();
+        if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(b.tmem));
+        return;
+    }
     RingPlace loaded;
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");

@@ -27,20 +27,28 @@ struct Batch {
     static constexpr bool kShared = false;
     const int32_t *table, *lens, *starts;
     int32_t num_seqs, max_blocks, num_rows, max_q_len;
-    bool by_groups() const { return false; }
+    __host__ __device__ bool by_groups() const { return false; }
 };
 
 // The rows of all sequences of a group, over the tokens [0, len) that these have in common; row: of the block table.
 struct Group {
     int32_t q0, qn, len, row;
 };
+// What a sequence has from its group: the tokens in front of `first` are the group's.  Where the groups' pass is attend_many's, also where
+// the sums of its rows are: the group's first row, its tiles of tokens and of rows, and its first tile in the end-to-end order
+// of all groups' tiles, of which every CTA has `even` (attend_many.cu).
+struct alignas(16) Own {
+    int32_t first, q0, tiles, row_tiles;
+    int64_t tile0, even;
+};
 // A batch whose sequences share prefixes, in one of two readings: the groups over their prefixes, every row of a group seeing all of
-// it (`groups` not null, num_seqs of them), or the sequences over the tokens behind `first`.
+// it (`groups` not null, num_seqs of them), or the sequences over the tokens behind those.
 struct SharedBatch : Batch {
     static constexpr bool kShared = true;
     const Group* groups;
-    const int32_t* first;  // [num_seqs]
-    bool by_groups() const { return groups != nullptr; }
+    const int64_t* tile0;  // [groups + 1]
+    const Own* own;        // [num_seqs]
+    __host__ __device__ bool by_groups() const { return groups != nullptr; }
 };
 
 // Cached tokens of a sequence at most: their indices, rounded up to tiles and blocks or moved by a window, stay below 2^31.
@@ -50,9 +58,9 @@ constexpr int32_t kMaxTokens = 1 << 30;
 struct Seq {
     int32_t q0, qn, len;
     bool ok;
-    int32_t row = 0;     // of the block table
-    int32_t first = 0;   // tokens in front of it are another pass's
-    bool level = false;  // every row sees all len tokens
+    int32_t row;    // of the block table
+    int32_t first;  // tokens in front of it are another pass's
+    bool level;     // every row sees all len tokens
 };
 // Cache index up to which the sequence's new token `tok` sees, itself included.
 __device__ __forceinline__ int last_seen(const Seq& q, int tok) { return q.level ? q.len - 1 : q.len - q.qn + tok; }
@@ -71,18 +79,18 @@ __device__ __forceinline__ Seq sequence(const Batch& b, int s, int block_tokens)
     q.ok = q.q0 >= 0 && q1 >= q.q0 && q1 <= b.num_rows && q1 - q.q0 <= b.max_q_len && q.len >= 0 &&
            q.len <= min((int64_t)b.max_blocks * block_tokens, (int64_t)kMaxTokens);
     q.qn = q.ok ? q1 - q.q0 : 0;
-    q.row = s;
+    q.row = s, q.first = 0, q.level = false;
     return q;
 }
 __device__ __forceinline__ Seq sequence(const SharedBatch& b, int s, int block_tokens) {
     if (!b.groups) {
         Seq q = sequence(static_cast<const Batch&>(b), s, block_tokens);
-        q.first = __ldcg(b.first + s);
+        q.first = __ldcg(&b.own[s].first);
         return q;
     }
     const int4 g = __ldcg(reinterpret_cast<const int4*>(b.groups) + s);
     Seq q;
-    q.q0 = g.x, q.qn = g.y, q.len = g.z, q.row = g.w;
+    q.q0 = g.x, q.qn = g.y, q.len = g.z, q.row = g.w, q.first = 0;
     q.ok = q.level = true;
     return q;
 }

@@ -51,6 +51,7 @@ __device__ __forceinline__ int row_tiles(const Shape& p, const Seq& q) {
 // Tiles of one head of a sequence.
 __device__ __forceinline__ int64_t head_tiles(const Shape& p, const Seq& q) {
     const int nm = row_tiles(p, q);
+    if (q.level) return (int64_t)nm * row_tile_range(p, q, 0).tiles;
     int64_t n = 0;
     for (int m = 0; m < nm; ++m) n += row_tile_range(p, q, m).tiles;
     return n;
@@ -76,6 +77,12 @@ struct Walk {
     }
     // To the tile `off` tiles into the (non-empty) sequence that is open.
     __device__ __forceinline__ void seek(const Shape& p, int64_t off) {
+        if (seq.level) {  // all units have as many
+            const int64_t unit = off >> 31 == 0 ? (uint32_t)off / (uint32_t)range.tiles : off / range.tiles;
+            t = (int)(off - unit * range.tiles);
+            h = (int)(unit / nm), m = (int)(unit - (int64_t)h * nm);
+            return;
+        }
         const int64_t per_head = head_tiles(p, seq);
         h = (off | per_head) >> 31 == 0 ? (int)((uint32_t)off / (uint32_t)per_head) : (int)(off / per_head);
         off -= h * per_head;
