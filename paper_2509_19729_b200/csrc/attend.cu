@@ -205,12 +205,6 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
         const int rows = min(R, walk.seq.qn * sh.group - walk.m * R);
         const bool direct = from_start && unit_ends;
         const int64_t part = (int64_t)(2 * blockIdx.x + (from_start ? 1 : 0)) * R;
-        Own own{};
-        if constexpr (B::kShared)
-            if (direct && walk.seq.first > 0) {
-                own = own_of(p, walk.s);
-                grid_dependency_wait();  // the groups' pass is done
-            }
         for (int i = tid; i < rows * (D / 4); i += kFewThreads) {
             const int r = i / (D / 4), d = i % (D / 4) * 4;
             float top = -INFINITY;
@@ -226,8 +220,11 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
                 j.l += f * s_l[w][r];
                 j.acc.x += f * x.x, j.acc.y += f * x.y, j.acc.z += f * x.z, j.acc.w += f * x.w;
             }
-            if (direct) {
-                finish<T, D>(p, walk.seq, own, walk.h, walk.m * R + r, d, j);
+            if (goes_on(p, walk.seq) && d == 0 && from_start && !direct) p.sums.l[head_of(p, walk.seq, walk.h, walk.m * R + r)] = kCutRow;
+            if (direct && goes_on(p, walk.seq)) {
+                write_sums<D>(p, walk.seq, walk.h, walk.m * R + r, d, j);
+            } else if (direct) {
+                write_row<T, D>(p, walk.seq, walk.h, walk.m * R + r, d, j);
             } else {
                 *reinterpret_cast<float4*>(p.part_o + (part + r) * D + d) = j.acc;
                 if (d == 0) p.part_m[part + r] = top, p.part_l[part + r] = j.l;
@@ -249,9 +246,10 @@ constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
 template <int kWarps, class B>
 constexpr int kJoinRows = kWarps > 1 ? 1 : B::kShared ? kJoinWarps : 4 * kJoinWarps;  // of a block
 
-// `groups` blocks to every share: the unit that it begins in is joined there, if that began in the share before.
-template <class T, int D, int kWarps, class B>
-__device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, int block, int groups) {
+// `groups` blocks to every share: the unit that it begins in is joined there, if that began in the share before; with what `prefix` adds
+// to a row.
+template <class T, int D, int kWarps, class B, class Prefix>
+__device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, int block, int groups, Prefix prefix) {
     constexpr int kRows = kJoinRows<kWarps, B>, kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes to a part's row, parts at once
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int mine = block / groups, first_row = block % groups * kRows, R = p.shape.rows;
@@ -259,9 +257,6 @@ __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, in
     if (cut.begin == cut.end || cut.t == 0 || first_row >= cut.rows) return;
     const int64_t first = cut.begin - cut.t, last = first + cut.tiles;
     const Seq q = sequence(p.batch, cut.s, p.cache.block_tokens);
-    Own own{};
-    if constexpr (B::kShared)
-        if (q.first > 0) own = own_of(p, cut.s);
     int c0 = mine - 1;
     while (p.cuts[c0].begin == p.cuts[c0].end) --c0;  // (empty shares)
     if (p.cuts[c0].begin > first) return;
@@ -282,6 +277,7 @@ __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, in
                 const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
                 j.add(p.part_m[part], p.part_l[part], *reinterpret_cast<const float4*>(p.part_o + part * D + lane % kLanes * 4));
             }
+            prefix(q, cut.h, cut.m * R + r, (kWarps == 1 ? 0 : warp) * kAtOnce + lane / kLanes, kWarps * kAtOnce, j);
         }
         if (kAtOnce == 2) {  // the second half of the warp has every other part
             const float4 x = make_float4(__shfl_down_sync(~0u, j.acc.x, 16), __shfl_down_sync(~0u, j.acc.y, 16),
@@ -299,7 +295,8 @@ __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, in
             for (int w = 1; w < kWarps; ++w) j.add(s_top[w], s_l[w], s_acc[w][lane % kLanes]);
         }
         if (r >= cut.rows || lane >= kLanes) continue;
-        finish<T, D>(p, q, own, cut.h, cut.m * R + r, lane * 4, j);
+        if (q.level) write_sums<D>(p, q, cut.h, cut.m * R + r, lane * 4, j);
+        else write_row<T, D>(p, q, cut.h, cut.m * R + r, lane * 4, j);
     }
 }
 // Blocks [0, few_ctas * few_rows) join what attend_few has cut, the others what attend_many has.
@@ -308,8 +305,80 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constan
                                                             const __grid_constant__ AttendParams<B> many, int many_ctas) {
     grid_dependency_wait();
     const int block = (int)blockIdx.x - few_ctas * few_rows;
-    if (block < 0) join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x, few_rows);
-    else join_rows<T, D, 1>(many, many_ctas, block, kManyRows / kJoinRows<1, B>);
+    auto none = [](const Seq&, int, int, int, int, Joined&) {};
+    if (block < 0) join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x, few_rows, none);
+    else join_rows<T, D, 1>(many, many_ctas, block, kManyRows / kJoinRows<1, B>, none);
+}
+
+// What the groups' pass has left: sums of whole rows, and where it was attend_many's (`ctas` of them) the parts of its cut units.
+struct PrefixSums {
+    Sums rows, parts;
+    const Group* groups;
+    const int64_t* tile0;
+    const int32_t* row_group;  // [num_rows] -1: none
+    int32_t num_groups, ctas, num_rows;
+    int32_t row_blocks;        // blocks of attend_finish to a row
+};
+// Adds the prefix's sums of a row (of a kv head's, from the first of the sequence) to j: every step-th part from `first` on.
+template <int D, class B>
+__device__ __forceinline__ void add_prefix(const AttendParams<B>& p, const PrefixSums& x, int g, const Seq& q, int kv_head, int row, int first, int step,
+                                           Joined& j) {
+    const int d = (int)threadIdx.x % 32 % (D / 4) * 4, tok = row / p.shape.group;
+    if (x.ctas > 0) {
+        const int4 group = __ldcg(reinterpret_cast<const int4*>(x.groups + g));
+        const int64_t total = __ldcg(x.tile0 + x.num_groups), even = divide(total + x.ctas - 1, x.ctas);
+        const int tiles = (group.z - 1) / kManyTile + 1, row_tiles = (int)(((int64_t)group.y * p.shape.group - 1) / kManyRows) + 1;
+        const int in_group = (q.q0 - group.x) * p.shape.group + row, m = in_group / kManyRows, r = in_group % kManyRows;
+        const int64_t begin = __ldcg(x.tile0 + g) + ((int64_t)kv_head * row_tiles + m) * tiles;
+        const int c0 = (int)divide(begin, even), c1 = (int)divide(begin + tiles - 1, even);
+        if (c0 < c1) {
+#pragma unroll 4
+            for (int c = c0 + first; c <= c1; c += step) {
+                const int64_t part = (int64_t)(2 * c + (c == c0)) * kManyRows + r;
+                j.add(x.parts.m[part], x.parts.l[part], *reinterpret_cast<const float4*>(x.parts.o + part * D + d));
+            }
+            return;
+        }
+    }
+    const int64_t at = (int64_t)(q.q0 + tok) * p.q_heads + kv_head * p.shape.group + row - tok * p.shape.group;
+    if (first == 0) j.add(x.rows.m[at], x.rows.l[at], *reinterpret_cast<const float4*>(x.rows.o + at * D + d));
+}
+// The end of both passes: as attend_join, with the prefixes' sums where there are any; then x.row_blocks blocks to a row for the rows with
+// a prefix whose own tokens were not cut, a warp to a query head.  Bound by four loads one after the other.
+template <class T, int D>
+__global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_constant__ AttendParams<SharedBatch> few, int few_ctas, int few_rows,
+                                                              const __grid_constant__ AttendParams<SharedBatch> many, int many_ctas,
+                                                              const __grid_constant__ PrefixSums x) {
+    constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;
+    grid_dependency_wait();
+    auto prefix = [&](const Seq& q, int kv_head, int row, int first, int step, Joined& j) {
+        if (q.first > 0) add_prefix<D>(few, x, x.row_group[q.q0], q, kv_head, row, first, step, j);
+    };
+    const int many_groups = kManyRows / kJoinRows<1, SharedBatch>;
+    int block = (int)blockIdx.x - few_ctas * few_rows;
+    if (block < 0) return join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x, few_rows, prefix);
+    if (block < many_ctas * many_groups) return join_rows<T, D, 1>(many, many_ctas, block, many_groups, prefix);
+    block -= many_ctas * many_groups;
+    const int row = block / x.row_blocks, g = x.row_group[row], lane = threadIdx.x % 32;
+    if (g < 0) return;
+    for (int head = block % x.row_blocks * kJoinWarps + (int)threadIdx.x / 32; head < few.q_heads; head += x.row_blocks * kJoinWarps) {
+        const int64_t at = (int64_t)row * few.q_heads + head;
+        const float l = few.sums.l[at];
+        if (l == kCutRow) continue;
+        const int kv_head = head / few.shape.group, r = head - kv_head * few.shape.group, half = lane / kLanes, d = lane % kLanes * 4;
+        Seq q{};
+        q.q0 = row;
+        Joined j;
+        if (half == 0) j.add(few.sums.m[at], l, *reinterpret_cast<const float4*>(few.sums.o + at * D + d));
+        add_prefix<D>(few, x, g, q, kv_head, r, half, kAtOnce, j);
+        if (kAtOnce == 2) {
+            const float4 o = make_float4(__shfl_down_sync(~0u, j.acc.x, 16), __shfl_down_sync(~0u, j.acc.y, 16),
+                                         __shfl_down_sync(~0u, j.acc.z, 16), __shfl_down_sync(~0u, j.acc.w, 16));
+            const float top = __shfl_down_sync(~0u, j.top, 16), l2 = __shfl_down_sync(~0u, j.l, 16);
+            j.add(top, l2, o);
+        }
+        if (half == 0) write_row<T, D>(few, q, kv_head, r, d, j);
+    }
 }
 
 // The workspace holds the parts of cut units, two for each CTA; these bound the grids without asking the device.
@@ -358,7 +427,7 @@ static amoeba_status run_few(AttendParams<B>& p, int sms, int* ctas, cudaStream_
 // before the kernel in front of it ends, and wait there for its results if they read them (attend_join) or end only after
 // it (attend_many).
 template <class T, int D, class B>
-static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
+static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char* ws, int sms, cudaStream_t stream, const PrefixSums* prefix) {
     const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
     const int64_t few_bytes = few_workspace(&p, ws, D);
     // In a batch with longer pieces attend_few gets the single tokens (and what has as few rows): its rows cost registers.  Groups
@@ -373,7 +442,7 @@ static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char*
                        : most == 8  ? run_few<T, D, 1>(p, sms, &few_ctas, stream)
                        : most == 16 ? run_few<T, D, 2>(p, sms, &few_ctas, stream)
                                     : run_few<T, D, 4>(p, sms, &few_ctas, stream);
-    if (st != AMOEBA_OK || (p.whole && few && rows <= kMaxFewRows)) return st;
+    if (st != AMOEBA_OK || (p.whole && few && rows <= kMaxFewRows && !prefix)) return st;
     if (p.whole) few_ctas = 0;  // nothing is cut
     const int few_most = (int)std::min<int64_t>(rows, most);
     AttendParams<B> many = p;
@@ -388,6 +457,13 @@ static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char*
         many_blocks = many_ctas * (kManyRows / kJoinRows<1, B>);
         if ((st = launch_attend_many(many, tp, dtype, D, many_ctas, stream)) != AMOEBA_OK || groups) return st;
     }
+    if constexpr (B::kShared)
+        if (prefix) {
+            const int64_t grid = few_ctas * few_most + many_blocks + (int64_t)prefix->num_rows * prefix->row_blocks;
+            return grid > INT32_MAX ? AMOEBA_ERR_UNSUPPORTED
+                                    : launch_kernel(attend_finish<T, D>, (int)grid, kJoinThreads, 0, stream, true, p, few_ctas, few_most, many,
+                                                    many_ctas, *prefix);
+        }
     return launch_kernel(attend_join<T, D, B>, few_ctas * few_most + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_most, many,
                          many_ctas);
 }
@@ -448,15 +524,16 @@ static bool units_fit(const amoeba_layout* l, int64_t num_seqs, int64_t rows) {
 // 9.5 cut; of 1024: 20.5 and 11.3; 32 sequences of 1024: 24 and 29; of 2048: 41 and 47, but there one long one would
 // hold up all).  With max_q_len 0 sequences are only looked at.
 template <class B>
-static amoeba_status attend_pass(const amoeba_layout* layout, int32_t dtype, AttendParams<B>& p, char* ws, int sms, cudaStream_t stream) {
+static amoeba_status attend_pass(const amoeba_layout* layout, int32_t dtype, AttendParams<B>& p, char* ws, int sms, cudaStream_t stream,
+                                 const PrefixSums* prefix = nullptr) {
     const amoeba_model& m = layout->model;
     const int64_t tokens = (int64_t)p.batch.max_blocks * layout->block_tokens;
     p.whole = rows_of(layout, p.batch.max_q_len) == 0 || tokens <= 512 || (tokens <= 1024 && p.batch.num_seqs * m.num_kv_heads >= sms);
     if (dtype == AMOEBA_FP16)
-        return m.head_dim == 64 ? run_attend<__half, 64>(p, layout->tp, dtype, ws, sms, stream)
-                                : run_attend<__half, 128>(p, layout->tp, dtype, ws, sms, stream);
-    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, layout->tp, dtype, ws, sms, stream)
-                            : run_attend<__nv_bfloat16, 128>(p, layout->tp, dtype, ws, sms, stream);
+        return m.head_dim == 64 ? run_attend<__half, 64>(p, layout->tp, dtype, ws, sms, stream, prefix)
+                                : run_attend<__half, 128>(p, layout->tp, dtype, ws, sms, stream, prefix);
+    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, layout->tp, dtype, ws, sms, stream, prefix)
+                            : run_attend<__nv_bfloat16, 128>(p, layout->tp, dtype, ws, sms, stream, prefix);
 }
 
 extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtype, int32_t layer,
@@ -490,11 +567,9 @@ struct PrefixParams {
     const int32_t *group_starts, *prefix_lens;
     Group* groups;
     int64_t* tile0;
-    Own* own;
-    int32_t* status;
+    int32_t *first, *row_group, *status;
     int32_t num_groups, max_group_rows, block_tokens;
     int32_t kv_heads, group;  // query heads per key head
-    int32_t many_ctas;        // of the groups' pass, if it is attend_many's
 };
 
 // What a group shares: no more than its shortest sequence has in front of its new tokens, and nothing where fewer than two have
@@ -503,108 +578,114 @@ struct PrefixParams {
 // Whether it pays is counted in tiles of 128 tokens (a tile of a sequence with few rows costs about as much as one of 256 rows): every
 // tile of rows reads the prefix, of each sequence by itself or of the group's rows together; a group's unit costs its start and end, about
 // four tiles, and taking up the sums half a tile for a few rows, six for 256.
-constexpr int kPrefixThreads = 1024;
+constexpr int kPrefixThreads = 1024, kPrefixWarps = kPrefixThreads / 32;
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_constant__ PrefixParams p) {
-    __shared__ int64_t s_warp[kPrefixThreads / 32];
-    const int tid = threadIdx.x, lane = tid % 32, S = p.batch.num_seqs, G = p.num_groups;
+    __shared__ int64_t s_tiles[kPrefixThreads], s_warp[kPrefixWarps];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.batch.num_seqs, G = p.num_groups;
     bool bad = false;
     for (int g = tid; g < G; g += kPrefixThreads) {
         const int a = p.group_starts[g], z = p.group_starts[g + 1];
         bad |= a < 0 || z < a || z > S;
     }
-    for (int s = tid; s < S; s += kPrefixThreads) p.own[s] = Own{};
+    for (int s = tid; s < S; s += kPrefixThreads) p.first[s] = 0;
+    for (int r = tid; r < p.batch.num_rows; r += kPrefixThreads) p.row_group[r] = -1;
     bad = __syncthreads_or(bad);
     if (bad && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
-    for (int g = tid / 32; g < G; g += kPrefixThreads / 32) {
-        const int a = bad ? 0 : p.group_starts[g], z = bad ? 0 : p.group_starts[g + 1];
-        int least = INT32_MAX, row = INT32_MAX, with_rows = 0, q0 = INT32_MAX, q1 = 0, alone = 0, taking = 0;
-        bool ok = true;
-        for (int s = a + lane; s < z; s += 32) {
-            const Seq q = sequence(p.batch, s, p.block_tokens);
-            ok &= q.ok;
-            if (q.qn == 0) continue;
-            const int tiles = (q.qn * p.group - 1) / kManyRows + 1;
-            least = min(least, q.len - q.qn);
-            row = min(row, s);
-            q0 = min(q0, q.q0);
-            q1 = max(q1, q.q0 + q.qn);
-            alone += tiles;
-            taking += q.qn * p.group <= kMaxFewRows ? 1 : 12 * tiles;  // half tiles
-            ++with_rows;
-        }
-        ok = __all_sync(~0u, ok);
-        least = __reduce_min_sync(~0u, least);
-        row = __reduce_min_sync(~0u, row);
-        with_rows = __reduce_add_sync(~0u, with_rows);
-        q0 = __reduce_min_sync(~0u, q0);
-        q1 = __reduce_max_sync(~0u, q1);
-        alone = __reduce_add_sync(~0u, alone);
-        taking = __reduce_add_sync(~0u, taking);
-        Group out{0, 0, 0, 0};
-        int64_t tiles = 0;
-        if (z > a) {
-            const int given = p.prefix_lens[g];
-            const bool wrong = given < 0 || (with_rows && q1 - q0 > p.max_group_rows);
-            if (wrong && lane == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
-            const int len = min(given, least), key_tiles = (len - 1) / kManyTile + 1;
-            if (!wrong && ok && with_rows > 1 && len > 0) {
-                const int row_tiles = (int)(((int64_t)(q1 - q0) * p.group - 1) / kManyRows) + 1;
-                if (2 * (int64_t)(alone - row_tiles) * key_tiles > 8 * (int64_t)row_tiles + taking) {
-                    out = Group{q0, q1 - q0, len, row};
-                    tiles = (int64_t)p.kv_heads * row_tiles * key_tiles;
-                    for (int s = a + lane; s < z; s += 32) p.own[s] = Own{len, q0, key_tiles, row_tiles, g, 0};
-                }
-            }
-        }
-        if (lane == 0) p.groups[g] = out, p.tile0[g] = tiles;
-    }
-    if (p.many_ctas == 0) return;
-    // the first tile of every group, and every CTA's share
-    __syncthreads();
     int64_t run = 0;
     for (int base = 0; base < G; base += kPrefixThreads) {
-        const int g = base + tid;
-        const int64_t own = g < G ? p.tile0[g] : 0;
+        for (int g = base + warp; g < min(G, base + kPrefixThreads); g += kPrefixWarps) {
+            const int a = bad ? 0 : p.group_starts[g], z = bad ? 0 : p.group_starts[g + 1];
+            int least = INT32_MAX, row = INT32_MAX, with_rows = 0, q0 = INT32_MAX, q1 = 0, alone = 0, taking = 0;
+            bool ok = true;
+            for (int s = a + lane; s < z; s += 32) {
+                const Seq q = sequence(p.batch, s, p.block_tokens);
+                ok &= q.ok;
+                if (q.qn == 0) continue;
+                const int tiles = (q.qn * p.group - 1) / kManyRows + 1;
+                least = min(least, q.len - q.qn);
+                row = min(row, s);
+                q0 = min(q0, q.q0);
+                q1 = max(q1, q.q0 + q.qn);
+                alone += tiles;
+                taking += q.qn * p.group <= kMaxFewRows ? 1 : 12 * tiles;  // half tiles
+                ++with_rows;
+            }
+            ok = __all_sync(~0u, ok);
+            least = __reduce_min_sync(~0u, least);
+            row = __reduce_min_sync(~0u, row);
+            with_rows = __reduce_add_sync(~0u, with_rows);
+            q0 = __reduce_min_sync(~0u, q0);
+            q1 = __reduce_max_sync(~0u, q1);
+            alone = __reduce_add_sync(~0u, alone);
+            taking = __reduce_add_sync(~0u, taking);
+            Group out{0, 0, 0, 0};
+            int64_t tiles = 0;
+            if (z > a) {
+                const int given = p.prefix_lens[g];
+                const bool wrong = given < 0 || (with_rows && q1 - q0 > p.max_group_rows);
+                if (wrong && lane == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
+                const int len = min(given, least), key_tiles = (len - 1) / kManyTile + 1;
+                if (!wrong && ok && with_rows > 1 && len > 0) {
+                    const int row_tiles = (int)(((int64_t)(q1 - q0) * p.group - 1) / kManyRows) + 1;
+                    if (2 * (int64_t)(alone - row_tiles) * key_tiles > 8 * (int64_t)row_tiles + taking) {
+                        out = Group{q0, q1 - q0, len, row};
+                        tiles = (int64_t)p.kv_heads * row_tiles * key_tiles;
+                        for (int s = a + lane; s < z; s += 32) p.first[s] = len;
+                        for (int r = q0 + lane; r < q1; r += 32) p.row_group[r] = g;
+                    }
+                }
+            }
+            if (lane == 0) p.groups[g] = out, s_tiles[g - base] = tiles;
+        }
+        __syncthreads();
+        // the first tile of every group
+        const int64_t own = base + tid < G ? s_tiles[tid] : 0;
         int64_t incl = own;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
             const int64_t up = __shfl_up_sync(~0u, incl, o);
             if (lane >= o) incl += up;
         }
-        if (lane == 31) s_warp[tid / 32] = incl;
+        if (lane == 31) s_warp[warp] = incl;
         __syncthreads();
-        int64_t before = run;
-        for (int w = 0; w < kPrefixThreads / 32; ++w) {
-            if (w < tid / 32) before += s_warp[w];
-            run += s_warp[w];
+        int64_t warps = s_warp[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t up = __shfl_up_sync(~0u, warps, o);
+            if (lane >= o) warps += up;
         }
-        if (g < G) p.tile0[g] = before + incl - own;
+        const int64_t total = __shfl_sync(~0u, warps, 31), before = __shfl_sync(~0u, warps, max(warp - 1, 0));
+        if (base + tid < G) p.tile0[base + tid] = run + (warp ? before : 0) + incl - own;
+        run += total;
         __syncthreads();
     }
     if (tid == 0) p.tile0[G] = run;
-    const int64_t even = divide(run + p.many_ctas - 1, p.many_ctas);
-    for (int s = tid; s < S; s += kPrefixThreads)
-        if (p.own[s].first > 0) p.own[s].tile0 = p.tile0[p.own[s].tile0], p.own[s].even = even;
 }
 
 // Where the parts of the workspace begin: both passes' own, the carry, the groups and the sequences' first tokens.
 struct SharedSpace {
-    int64_t groups_pass, rest_pass, carry_o, carry_m, carry_l, groups, tile0, own, end;
+    int64_t groups_pass, rest_pass, group_sums, rest_sums, groups, tile0, first, row_group, end;
 };
+// Sums of all rows and query heads.
+static int64_t sums_space(const amoeba_layout* l, int64_t rows, char* ws, Sums* out) {
+    const int64_t heads = (rows * l->model.num_q_heads + 3) / 4 * 4, o = heads * l->model.head_dim * 4;
+    if (out) *out = Sums{reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + o), reinterpret_cast<float*>(ws + o + heads * 4)};
+    return o + heads * 8;
+}
 static SharedSpace shared_space(const amoeba_layout* l, const amoeba_batch* b, const amoeba_prefixes* x) {
     const int D = l->model.head_dim;
     const int64_t few = few_workspace<Batch>(nullptr, nullptr, D), many = many_workspace<Batch>(nullptr, nullptr, D);
-    const int64_t heads = ((int64_t)b->num_rows * l->model.num_q_heads + 3) / 4 * 4;
+    auto ints = [](int64_t n) { return (n * 4 + 15) / 16 * 16; };
     SharedSpace s;
     s.groups_pass = 0;
     s.rest_pass = few + (rows_of(l, x->max_group_rows) > kMaxGroupRows ? many : 0);
-    s.carry_o = s.rest_pass + few + (rows_of(l, b->max_q_len) > kMaxFewRows ? many : 0);
-    s.carry_m = s.carry_o + heads * D * 4;
-    s.carry_l = s.carry_m + heads * 4;
-    s.groups = s.carry_l + heads * 4;
+    s.group_sums = s.rest_pass + few + (rows_of(l, b->max_q_len) > kMaxFewRows ? many : 0);
+    s.rest_sums = s.group_sums + sums_space(l, b->num_rows, nullptr, nullptr);
+    s.groups = s.rest_sums + sums_space(l, b->num_rows, nullptr, nullptr);
     s.tile0 = s.groups + (int64_t)x->num_groups * sizeof(Group);
-    s.own = s.tile0 + ((int64_t)x->num_groups / 2 + 1) * 16;
-    s.end = s.own + (int64_t)b->num_seqs * sizeof(Own);
+    s.first = s.tile0 + ((int64_t)x->num_groups / 2 + 1) * 16;
+    s.row_group = s.first + ints(b->num_seqs);
+    s.end = s.row_group + ints(b->num_rows);
     return s;
 }
 
@@ -642,29 +723,36 @@ extern "C" amoeba_status amoeba_attend_shared(const amoeba_layout* layout, int32
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(d_workspace);
     const SharedSpace at = shared_space(layout, batch, prefixes);
-    p.carry = Carry{reinterpret_cast<float*>(ws + at.carry_o), reinterpret_cast<float*>(ws + at.carry_m), reinterpret_cast<float*>(ws + at.carry_l)};
     const int32_t num_groups = group_rows ? prefixes->num_groups : 0;
-    const bool many = rows_of(layout, group_rows) > kMaxGroupRows;
     PrefixParams x{};
     x.batch = p.batch;
     x.group_starts = prefixes->d_group_starts, x.prefix_lens = prefixes->d_prefix_lens;
     x.groups = reinterpret_cast<Group*>(ws + at.groups), x.tile0 = reinterpret_cast<int64_t*>(ws + at.tile0);
-    x.own = reinterpret_cast<Own*>(ws + at.own);
+    x.first = reinterpret_cast<int32_t*>(ws + at.first), x.row_group = reinterpret_cast<int32_t*>(ws + at.row_group);
     x.status = d_status;
     x.num_groups = prefixes->num_groups, x.max_group_rows = group_rows, x.block_tokens = layout->block_tokens;
     x.kv_heads = p.shape.kv_heads, x.group = p.shape.group;
-    x.many_ctas = many ? std::min(dev.sms, kMaxSms) : 0;
     if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, false, x)) != AMOEBA_OK) return st;
-    p.batch.own = x.own;
-    if (num_groups) {
-        AttendParams<SharedBatch> g = p;
-        g.batch.groups = x.groups, g.batch.tile0 = x.tile0;
-        g.batch.num_seqs = num_groups;
-        g.batch.max_q_len = group_rows;
-        if ((st = attend_pass(layout, dtype, g, ws + at.groups_pass, dev.sms, stream)) != AMOEBA_OK) return st;
+    p.batch.first = x.first;
+    sums_space(layout, p.batch.num_rows, ws + at.rest_sums, &p.sums);
+    if (!num_groups) return attend_pass(layout, dtype, p, ws + at.rest_pass, dev.sms, stream);
+    AttendParams<SharedBatch> g = p;
+    g.batch.groups = x.groups, g.batch.tile0 = x.tile0;
+    g.batch.num_seqs = num_groups;
+    g.batch.max_q_len = group_rows;
+    sums_space(layout, p.batch.num_rows, ws + at.group_sums, &g.sums);
+    if ((st = attend_pass(layout, dtype, g, ws + at.groups_pass, dev.sms, stream)) != AMOEBA_OK) return st;
+    PrefixSums sums{};
+    sums.rows = g.sums;
+    if (rows_of(layout, group_rows) > kMaxGroupRows) {
         AttendParams<SharedBatch> cut{};  // where the parts of its units are
         many_workspace(&cut, ws + at.groups_pass + few_workspace<Batch>(nullptr, nullptr, layout->model.head_dim), layout->model.head_dim);
-        p.cut = Carry{cut.part_o, cut.part_m, cut.part_l};
+        sums.parts = Sums{cut.part_o, cut.part_m, cut.part_l};
+        sums.ctas = std::min(dev.sms, kMaxSms);
     }
-    return attend_pass(layout, dtype, p, ws + at.rest_pass, dev.sms, stream);
+    sums.groups = x.groups, sums.tile0 = x.tile0, sums.row_group = x.row_group;
+    sums.num_groups = num_groups, sums.num_rows = p.batch.num_rows;
+    // Enough blocks for a head to a warp, unless there are rows enough to fill the GPU as it is.
+    sums.row_blocks = p.batch.num_rows >= 1024 ? 1 : (p.q_heads + kJoinWarps - 1) / kJoinWarps;
+    return attend_pass(layout, dtype, p, ws + at.rest_pass, dev.sms, stream, &sums);
 }

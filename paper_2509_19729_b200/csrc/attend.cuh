@@ -7,13 +7,12 @@ namespace amoeba {
 // The kernel for many rows (attend_many.cu): 256 rows a unit, 128 tokens a tile.
 constexpr int kManyRows = 256, kManyTile = 128;
 constexpr int kMaxSms = 192;  // bounds the grids, and so the workspace, without asking the device
-// What a row has from its sequence's prefix, for every query head, before it is divided: sums of weights times values, the largest
-// logit in powers of two and the sum of the weights.
-struct Carry {
-    float *o, *m, *l;  // [num_rows][query heads][D], [num_rows][query heads]
+// Sums of rows and query heads that are not yet divided: weights times values, the largest logit in powers of two, the weights.
+struct Sums {
+    float *o, *m, *l;  // [rows][query heads][D], [rows][query heads]; or parts as below
 };
 
-// B: Batch, or SharedBatch: then the groups' pass writes the carry and the sequences' pass takes it up.
+// B: Batch, or SharedBatch: then rows with a prefix go to `sums`, by both passes, and are joined behind them.
 template <class B>
 struct AttendParams {
     CacheView cache;
@@ -27,7 +26,7 @@ struct AttendParams {
     float scale_log2;        // scale * log2(e): the softmax runs in powers of two
     int32_t q_heads;         // of all workers
     int32_t whole;           // 1: one CTA per unit, nothing is cut
-    Carry carry, cut;        // of a SharedBatch: whole rows of the groups' pass; the parts that attend_many's left, as part_o, ...
+    Sums sums;               // of a SharedBatch
 #ifdef AMOEBA_CHECK_ITEMS
     int32_t polls;           // of every wait in attend_many
 #endif
@@ -65,50 +64,23 @@ struct Joined {
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
     return (uint64_t)(a | b) >> 32 == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// Calls add(m, l, address of o) for the sums that the groups' pass has left for a row: one, or the parts of a unit that was cut.
-template <int D, class B, class Add>
-__device__ __forceinline__ void take_up(const AttendParams<B>& p, const Seq& q, const Own& own, int kv_head, int row, Add add) {
-    const int g = p.shape.group, tok = row / g;
-    if (own.even > 0) {
-        const int at = (q.q0 + tok - own.q0) * g + row - tok * g, m = at / kManyRows, r = at % kManyRows;
-        const int64_t begin = own.tile0 + ((int64_t)kv_head * own.row_tiles + m) * own.tiles;
-        const int c0 = (int)divide(begin, own.even), c1 = (int)divide(begin + own.tiles - 1, own.even);
-        if (c0 < c1) {
-#pragma unroll 4
-            for (int c = c0; c <= c1; ++c) {
-                const int64_t part = (int64_t)(2 * c + (c == c0)) * kManyRows + r;
-                add(p.cut.m[part], p.cut.l[part], p.cut.o + part * D);
-            }
-            return;
-        }
-    }
-    const int64_t at = head_of(p, q, kv_head, row);
-    add(p.carry.m[at], p.carry.l[at], p.carry.o + at * D);
-}
+// Whether a unit's rows are to be joined with sums over other tokens.
 template <class B>
-__device__ __forceinline__ Own own_of(const AttendParams<B>& p, int s) {
-    Own o;
-    const int4* from = reinterpret_cast<const int4*>(p.batch.own + s);
-    reinterpret_cast<int4*>(&o)[0] = __ldcg(from);
-    reinterpret_cast<int4*>(&o)[1] = __ldcg(from + 1);
-    return o;
-}
-// What a unit's row comes to, its values d .. d + 3: into the carry, or with what is carried to the output.  own: of a sequence with a
-// prefix.
+__device__ __forceinline__ bool goes_on(const AttendParams<B>&, const Seq& q) { return B::kShared && (q.level || q.first > 0); }
+constexpr float kCutRow = -1.f;  // in place of a row's sum of weights: the unit was cut, its parts are elsewhere
+// What a row comes to, its values d .. d + 3, to the output.
 template <class T, int D, class B>
-__device__ __forceinline__ void finish(const AttendParams<B>& p, const Seq& q, const Own& own, int kv_head, int row, int d, Joined& j) {
-    if (B::kShared && q.level) {
-        const int64_t at = head_of(p, q, kv_head, row);
-        *reinterpret_cast<float4*>(p.carry.o + at * D + d) = j.acc;
-        if (d == 0) p.carry.m[at] = j.top, p.carry.l[at] = j.l;
-        return;
-    }
-    if (B::kShared && q.first > 0)
-        take_up<D>(p, q, own, kv_head, row, [&](float m, float l, const float* o) { j.add(m, l, *reinterpret_cast<const float4*>(o + d)); });
+__device__ __forceinline__ void write_row(const AttendParams<B>& p, const Seq& q, int kv_head, int row, int d, const Joined& j) {
     const float inv = j.l == 0.f ? 0.f : 1.f / j.l;
     *reinterpret_cast<uint2*>(row_of<D>(p.out, p, q, kv_head, row) + d * 2) =
         make_uint2(Elem<T>::pack(j.acc.x * inv, j.acc.y * inv), Elem<T>::pack(j.acc.z * inv, j.acc.w * inv));
     if (d == 0 && p.lse) *lse_of(p, q, kv_head, row) = j.l == 0.f ? -INFINITY : (j.top + log2f(j.l)) * kLn2;
+}
+template <int D, class B>
+__device__ __forceinline__ void write_sums(const AttendParams<B>& p, const Seq& q, int kv_head, int row, int d, const Joined& j) {
+    const int64_t at = head_of(p, q, kv_head, row);
+    *reinterpret_cast<float4*>(p.sums.o + at * D + d) = j.acc;
+    if (d == 0) p.sums.m[at] = j.top, p.sums.l[at] = j.l;
 }
 
 template <class B>

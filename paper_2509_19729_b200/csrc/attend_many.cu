@@ -309,11 +309,15 @@ __device__ RingPlace load_loop(const AttendParams<B>& p, const CacheMaps& maps, 
         load.open(w, p.batch);
         int key0 = w.range.base + w.t * kManyTile;
         auto at = load.groups(w.range.lo, w.range.hi, key0), next = load.groups(w.range.lo, w.range.hi, key0 + kManyTile);
-        ok = load.queries(part, q_phase);
+        // (the first keys and values are on their way while the queries are gathered, which takes longer)
+        if (B::kShared) ok = load.tile(w.range, key0, at, 0) && load.tile(w.range, key0, at, 1);
+        if (ok) ok = load.queries(part, q_phase);
         q_phase ^= 1;
         for (int i = 0; ok && i < part.tiles; ++i, key0 += kManyTile) {
-            ok = load.tile(w.range, key0, at, 0);
-            if (ok) ok = load.tile(w.range, key0, at, 1);
+            if (!B::kShared || i > 0) {
+                ok = load.tile(w.range, key0, at, 0);
+                if (ok) ok = load.tile(w.range, key0, at, 1);
+            }
             at = next;
             if (i + 2 < part.tiles) next = load.groups(w.range.lo, w.range.hi, key0 + 2 * kManyTile);
         }
@@ -637,8 +641,8 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
         }
         if (ok && t < part.q_tiles) {
             const bool direct = part.from_start && part.to_end;
-            // A row's sum is `keep` of its own O, `other` of the second warpgroup's, and what is carried.
-            const bool into = B::kShared && w.seq.level, takes = B::kShared && direct && there && w.seq.first > 0;
+            // A row's sum is `keep` of its own O and `other` of the second warpgroup's.
+            const bool on = goes_on(p, w.seq);
             const int64_t head = B::kShared && there ? head_of(p, w.seq, w.h, row) : 0;
             float keep = 1.f, other = 0.f;
             if (in_turn) {
@@ -647,26 +651,13 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
                 l = l * keep + p.part_l[at + 128] * other;
                 m_ref = up;
             }
-            Own own{};
-            float ref = 0.f;
-            auto carried = [&](auto add) {
-                if constexpr (B::kShared) take_up<D>(p, w.seq, own, w.h, row, add);
-            };
-            if (takes) {
-                if constexpr (B::kShared) own = own_of(p, w.s);
-                float up = m_ref;
-                carried([&](float m2, float, const float*) { up = fmaxf(up, m2); });
-                ref = up == -INFINITY ? 0.f : up;
-                const float f = fast_exp2(m_ref - ref);
-                l *= f, keep *= f, other *= f;
-                carried([&](float m2, float l2, const float*) { l += l2 * fast_exp2(m2 - ref); });
-                m_ref = up;
+            if (direct && !on) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                keep *= inv, other *= inv;
             }
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            if (direct && !into) keep *= inv, other *= inv;
             char* out = there ? row_of<D>(p.out, p, w.seq, w.h, row) : nullptr;
-            float* const raw = direct ? p.carry.o + head * D : p.part_o + at * D;
-#pragma unroll
+            float* const raw = direct ? p.sums.o + head * D : p.part_o + at * D;
+#pragma unroll (B::kShared ? 1 : D / 32)  // (what runs once or twice waits for its instructions)
             for (int j = 0; j < D / 32; ++j) {
                 uint32_t o[32];
                 __syncwarp();  // (rows that are not there have parted from the others)
@@ -683,19 +674,7 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
                     for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
                 }
                 if (!there) continue;
-                if (direct && !into) {
-                    if (takes)
-                        carried([&](float m2, float, const float* from) {
-                            const float f = fast_exp2(m2 - ref) * inv;
-#pragma unroll
-                            for (int k = 0; k < 32; k += 4) {
-                                const float4 c4 = *reinterpret_cast<const float4*>(from + j * 32 + k);
-                                o[k] = __float_as_uint(__uint_as_float(o[k]) + c4.x * f);
-                                o[k + 1] = __float_as_uint(__uint_as_float(o[k + 1]) + c4.y * f);
-                                o[k + 2] = __float_as_uint(__uint_as_float(o[k + 2]) + c4.z * f);
-                                o[k + 3] = __float_as_uint(__uint_as_float(o[k + 3]) + c4.w * f);
-                            }
-                        });
+                if (direct && !on) {
 #pragma unroll
                     for (int k = 0; k < 32; k += 8) {
                         uint32_t x[4];
@@ -713,9 +692,14 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
             tmem_fence_before();
             mbar_arrive(&b.o_free[t]);
             if (in_turn) mbar_arrive(&b.o_free[1]);
-            if (there && !direct) p.part_m[at] = m_ref, p.part_l[at] = l;
-            else if (there && into) p.carry.m[head] = m_ref, p.carry.l[head] = l;
-            else if (there && p.lse) *lse_of(p, w.seq, w.h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
+            if (there && !direct) {
+                p.part_m[at] = m_ref, p.part_l[at] = l;
+                if (on && part.from_start && !w.seq.level) p.sums.l[head] = kCutRow;
+            } else if (there && on) {
+                p.sums.m[head] = m_ref, p.sums.l[head] = l;
+            } else if (there && p.lse) {
+                *lse_of(p, w.seq, w.h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
+            }
         }
         if (!ok) b.abort = 1;
     }

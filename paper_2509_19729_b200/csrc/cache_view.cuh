@@ -34,20 +34,13 @@ struct Batch {
 struct Group {
     int32_t q0, qn, len, row;
 };
-// What a sequence has from its group: the tokens in front of `first` are the group's.  Where the groups' pass is attend_many's, also where
-// the sums of its rows are: the group's first row, its tiles of tokens and of rows, and its first tile in the end-to-end order
-// of all groups' tiles, of which every CTA has `even` (attend_many.cu).
-struct alignas(16) Own {
-    int32_t first, q0, tiles, row_tiles;
-    int64_t tile0, even;
-};
 // A batch whose sequences share prefixes, in one of two readings: the groups over their prefixes, every row of a group seeing all of
 // it (`groups` not null, num_seqs of them), or the sequences over the tokens behind those.
 struct SharedBatch : Batch {
     static constexpr bool kShared = true;
     const Group* groups;
-    const int64_t* tile0;  // [groups + 1]
-    const Own* own;        // [num_seqs]
+    const int64_t* tile0;  // [groups + 1] first tile of every group in the end-to-end order of all groups' tiles
+    const int32_t* first;  // [num_seqs] tokens in front of it are the group's
     __host__ __device__ bool by_groups() const { return groups != nullptr; }
 };
 
@@ -85,7 +78,7 @@ __device__ __forceinline__ Seq sequence(const Batch& b, int s, int block_tokens)
 __device__ __forceinline__ Seq sequence(const SharedBatch& b, int s, int block_tokens) {
     if (!b.groups) {
         Seq q = sequence(static_cast<const Batch&>(b), s, block_tokens);
-        q.first = __ldcg(&b.own[s].first);
+        q.first = __ldcg(b.first + s);
         return q;
     }
     const int4 g = __ldcg(reinterpret_cast<const int4*>(b.groups) + s);

@@ -241,10 +241,15 @@ struct TileLoader {
         for (int first = warp * 32; first < 128; first += kWarps * 32) {
             const int r = row + (kRepeat ? min(first + lane, count - 1) : first + lane), tok = r / group;
             const int64_t mine = kRepeat || first + lane < count ? tok * q.stride + (r - tok * group) * (D * 2) : -1;
+            constexpr int kAtOnce = 8;  // the lanes' answers of so many rows are asked for before any load waits for its own
 #pragma unroll
-            for (int i = 0; i < 32; i += kStep) {
-                const int64_t off = __shfl_sync(~0u, mine, i + sub);
-                cp_async16(dst + tile_offset(first + i + sub, c), off >= 0 ? base + off : v.pools[0], off >= 0 ? 16 : 0);
+            for (int i0 = 0; i0 < 32 / kStep; i0 += kAtOnce) {
+                int64_t off[kAtOnce];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) off[i] = __shfl_sync(~0u, mine, (i0 + i) * kStep + sub);
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i)
+                    cp_async16(dst + tile_offset(first + (i0 + i) * kStep + sub, c), off[i] >= 0 ? base + off[i] : v.pools[0], off[i] >= 0 ? 16 : 0);
             }
         }
     }
