@@ -9,6 +9,64 @@
 
 namespace amoeba {
 
+constexpr int kMaxFewRows = 32;   // rows of a unit of attend_few
+constexpr int kMaxGroupRows = 8;  // of a group by attend_few
+constexpr int kUnitStart = 3;     // tiles of 64 tokens that a unit's start and end cost: 5000 clocks, 1660 a tile that is in flight already
+
+// ------------------------------------------------------------------------------------------------ groups' numbers
+// What the sequences of a group come to; the warp together.
+struct GroupSums {
+    int32_t first, end;        // sequences; none if the numbers are bad
+    int32_t q0, q1, row;       // rows, and the first sequence that has any
+    int32_t with_rows, least;  // sequences with rows, and the fewest tokens in front of the new ones
+    int32_t alone, taking;     // row tiles of all sequences, and what joining their sums costs, in half tiles
+    bool ok;
+};
+__device__ __forceinline__ GroupSums sum_group(const Batch& b, const int32_t* group_starts, int g, int block_tokens, int heads) {
+    GroupSums x{group_starts[g], group_starts[g + 1], INT32_MAX, 0, INT32_MAX, 0, INT32_MAX, 0, 0, true};
+    for (int s = x.first + (int)threadIdx.x % 32; s < x.end; s += 32) {
+        const Seq q = sequence(b, s, block_tokens);
+        x.ok &= q.ok;
+        if (q.qn == 0) continue;
+        const int tiles = (q.qn * heads - 1) / kManyRows + 1;
+        x.least = min(x.least, q.len - q.qn);
+        x.row = min(x.row, s);
+        x.q0 = min(x.q0, q.q0);
+        x.q1 = max(x.q1, q.q0 + q.qn);
+        x.alone += tiles;
+        x.taking += q.qn * heads <= kMaxFewRows ? 1 : 12 * tiles;
+        ++x.with_rows;
+    }
+    x.ok = __all_sync(~0u, x.ok);
+    x.least = __reduce_min_sync(~0u, x.least);
+    x.row = __reduce_min_sync(~0u, x.row);
+    x.with_rows = __reduce_add_sync(~0u, x.with_rows);
+    x.q0 = __reduce_min_sync(~0u, x.q0);
+    x.q1 = __reduce_max_sync(~0u, x.q1);
+    x.alone = __reduce_add_sync(~0u, x.alone);
+    x.taking = __reduce_add_sync(~0u, x.taking);
+    return x;
+}
+// Whether a group's numbers are refused.
+__device__ __forceinline__ bool refused(const GroupSums& x, int prefix, int max_group_rows) {
+    return x.end > x.first && (prefix < 0 || (x.with_rows > 0 && x.q1 - x.q0 > max_group_rows));
+}
+// Whether the groups' sequences are in order; the block together.
+__device__ __forceinline__ bool groups_in_order(const int32_t* starts, int groups, int num_seqs) {
+    bool bad = false;
+    for (int g = threadIdx.x; g < groups; g += blockDim.x) bad |= starts[g] < 0 || starts[g + 1] < starts[g] || starts[g + 1] > num_seqs;
+    return !__syncthreads_or(bad);
+}
+// All that is reported of groups, where nothing is shared.
+template <class B>
+__device__ void check_groups(const AttendParams<B>& p) {
+    const SharedBatch& b = p.batch;
+    bool bad = !groups_in_order(b.group_starts, b.num_groups, b.num_seqs);
+    for (int g = threadIdx.x / 32; !bad && g < b.num_groups; g += blockDim.x / 32)
+        bad = refused(sum_group(b, b.group_starts, g, p.cache.block_tokens, p.shape.group), b.prefix_lens[g], b.max_group_rows);
+    if (bad) report(p.status, AMOEBA_ERR_INVALID_ARG);
+}
+
 // ------------------------------------------------------------------------------------------------ few rows
 // Up to 8*NT rows a unit.  Bound by the bytes of the cache: 2 * 2 * D a token and key head against at most 32 rows of
 // arithmetic, which warp-level matrix instructions do in a fraction of the time.  Every warp works alone on every
@@ -44,7 +102,11 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
 
     Walk walk{};
     int64_t n;
-    if (B::kShared && p.batch.by_groups()) grid_dependency_wait();  // the groups are there
+    if constexpr (B::kShared) {
+        // The groups are there.  (Their own pass comes behind the sequences', whose blocks have all waited for them.)
+        if (!p.batch.by_groups()) grid_dependency_wait();
+        if (p.whole && !p.batch.own && !p.batch.by_groups() && (int)blockIdx.x == p.batch.num_seqs * sh.kv_heads) return check_groups(p);
+    }
     if (p.whole) {
         walk.open(sh, p.batch, p.cache.block_tokens, blockIdx.x / sh.kv_heads);
         if (!walk.seq.ok && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
@@ -52,7 +114,8 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
         n = walk.nm ? walk.range.tiles : 0;
     } else {
         int64_t begin, end;
-        take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
+        if (B::kShared) take_weighted_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status, smem);
+        else take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
         write_cut(sh, p.cuts, walk, begin, end);
         n = end - begin;
     }
@@ -279,12 +342,7 @@ __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, in
             }
             prefix(q, cut.h, cut.m * R + r, (kWarps == 1 ? 0 : warp) * kAtOnce + lane / kLanes, kWarps * kAtOnce, j);
         }
-        if (kAtOnce == 2) {  // the second half of the warp has every other part
-            const float4 x = make_float4(__shfl_down_sync(~0u, j.acc.x, 16), __shfl_down_sync(~0u, j.acc.y, 16),
-                                         __shfl_down_sync(~0u, j.acc.z, 16), __shfl_down_sync(~0u, j.acc.w, 16));
-            const float top = __shfl_down_sync(~0u, j.top, 16), l = __shfl_down_sync(~0u, j.l, 16);
-            j.add(top, l, x);
-        }
+        if (kAtOnce == 2) j.add_lower_half();  // the second half of the warp has every other part
         if (kWarps > 1) {
             __shared__ float4 s_acc[kWarps][kLanes];
             __shared__ float s_top[kWarps], s_l[kWarps];
@@ -343,20 +401,63 @@ __device__ __forceinline__ void add_prefix(const AttendParams<B>& p, const Prefi
     const int64_t at = (int64_t)(q.q0 + tok) * p.q_heads + kv_head * p.shape.group + row - tok * p.shape.group;
     if (first == 0) j.add(x.rows.m[at], x.rows.l[at], *reinterpret_cast<const float4*>(x.rows.o + at * D + d));
 }
-// The end of both passes: as attend_join, with the prefixes' sums where there are any; then x.row_blocks blocks to a row for the rows with
-// a prefix whose own tokens were not cut, a warp to a query head.  Bound by four loads one after the other.
+// The cut units of attend_few, a block to a share as in join_rows: a warp to a row if it is in few parts, else all of them.
+template <class T, int D, class Prefix>
+__device__ __forceinline__ void finish_cut(const AttendParams<SharedBatch>& p, int ctas, int mine, Prefix prefix) {
+    constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes, kMost = 32;  // parts of a row for one warp
+    __shared__ float4 s_acc[kJoinWarps][kLanes];
+    __shared__ float s_top[kJoinWarps], s_l[kJoinWarps];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, R = p.shape.rows;
+    const Cut cut = p.cuts[mine];
+    if (cut.begin == cut.end || cut.t == 0) return;
+    const int64_t first = cut.begin - cut.t, last = first + cut.tiles;
+    const Seq q = sequence(p.batch, cut.s, p.cache.block_tokens);
+    int c0 = mine - 1;
+    while (p.cuts[c0].begin == p.cuts[c0].end) --c0;  // (empty shares)
+    if (p.cuts[c0].begin > first) return;
+    int c1 = mine;  // behind the last part
+    for (bool more = true; more; c1 += 32) {
+        const unsigned in = __ballot_sync(~0u, c1 + lane < ctas && p.cuts[c1 + lane].begin < last);
+        more = in == ~0u;
+        if (!more) c1 += __popc(in) - 32;
+    }
+    const bool alone = c1 - c0 <= kMost;
+    const int begin = (alone ? 0 : warp) * kAtOnce + lane / kLanes, step = (alone ? 1 : kJoinWarps) * kAtOnce;
+    for (int r = alone ? warp : 0; r < cut.rows; r += alone ? kJoinWarps : 1) {
+        Joined j;
+#pragma unroll 4
+        for (int c = c0 + begin; c < c1; c += step) {
+            if (p.cuts[c].begin == p.cuts[c].end) continue;
+            const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
+            j.add(p.part_m[part], p.part_l[part], *reinterpret_cast<const float4*>(p.part_o + part * D + lane % kLanes * 4));
+        }
+        prefix(q, cut.h, cut.m * R + r, begin, step, j);
+        if (kAtOnce == 2) j.add_lower_half();
+        if (!alone) {
+            if (lane < kLanes) s_acc[warp][lane] = j.acc;
+            if (lane == 0) s_top[warp] = j.top, s_l[warp] = j.l;
+            __syncthreads();
+            for (int w = 1; warp == 0 && w < kJoinWarps; ++w) j.add(s_top[w], s_l[w], s_acc[w][lane % kLanes]);
+            __syncthreads();
+        }
+        if ((alone || warp == 0) && lane < kLanes) write_row<T, D>(p, q, cut.h, cut.m * R + r, lane * 4, j);
+    }
+}
+// The end of both passes: what was cut of the sequences', with the prefixes' sums where there are any; then x.row_blocks blocks to a row
+// for the rows with a prefix whose own tokens were not cut, a warp to a query head.  Bound by four or five loads one after the other.
 template <class T, int D>
-__global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_constant__ AttendParams<SharedBatch> few, int few_ctas, int few_rows,
+__global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_constant__ AttendParams<SharedBatch> few, int few_ctas,
                                                               const __grid_constant__ AttendParams<SharedBatch> many, int many_ctas,
                                                               const __grid_constant__ PrefixSums x) {
     constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;
     grid_dependency_wait();
     auto prefix = [&](const Seq& q, int kv_head, int row, int first, int step, Joined& j) {
-        if (q.first > 0) add_prefix<D>(few, x, x.row_group[q.q0], q, kv_head, row, first, step, j);
+        if (q.first > 0) add_prefix<D>(few, x, q.group, q, kv_head, row, first, step, j);
     };
     const int many_groups = kManyRows / kJoinRows<1, SharedBatch>;
-    int block = (int)blockIdx.x - few_ctas * few_rows;
-    if (block < 0) return join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x, few_rows, prefix);
+    int block = blockIdx.x;
+    if (block < few_ctas) return finish_cut<T, D>(few, few_ctas, block, prefix);
+    block -= few_ctas;
     if (block < many_ctas * many_groups) return join_rows<T, D, 1>(many, many_ctas, block, many_groups, prefix);
     block -= many_ctas * many_groups;
     const int row = block / x.row_blocks, g = x.row_group[row], lane = threadIdx.x % 32;
@@ -371,20 +472,13 @@ __global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_const
         Joined j;
         if (half == 0) j.add(few.sums.m[at], l, *reinterpret_cast<const float4*>(few.sums.o + at * D + d));
         add_prefix<D>(few, x, g, q, kv_head, r, half, kAtOnce, j);
-        if (kAtOnce == 2) {
-            const float4 o = make_float4(__shfl_down_sync(~0u, j.acc.x, 16), __shfl_down_sync(~0u, j.acc.y, 16),
-                                         __shfl_down_sync(~0u, j.acc.z, 16), __shfl_down_sync(~0u, j.acc.w, 16));
-            const float top = __shfl_down_sync(~0u, j.top, 16), l2 = __shfl_down_sync(~0u, j.l, 16);
-            j.add(top, l2, o);
-        }
+        if (kAtOnce == 2) j.add_lower_half();
         if (half == 0) write_row<T, D>(few, q, kv_head, r, d, j);
     }
 }
 
 // The workspace holds the parts of cut units, two for each CTA; these bound the grids without asking the device.
 constexpr int kMaxFewCtas = 2 * kMaxSms;
-constexpr int kMaxFewRows = 32;
-constexpr int kMaxGroupRows = 8;  // of a group by attend_few
 
 // One kernel's part of the workspace: where the shares begin, then the parts.
 template <class B>
@@ -415,11 +509,21 @@ static amoeba_status run_few(AttendParams<B>& p, int sms, int* ctas, cudaStream_
     using F = FewShape<D, NT>;
     p.shape.rows = 8 * NT;
     p.shape.tile = kFewTile;
+    p.shape.start = kUnitStart;
     if (ensure_dynamic_smem((const void*)attend_few<T, D, NT, B>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
     *ctas = std::min(F::kCtas * sms, kMaxFewCtas);
-    return launch_kernel(attend_few<T, D, NT, B>, p.whole ? p.batch.num_seqs * p.shape.kv_heads : *ctas, kFewThreads, F::kSmem, stream,
-                         B::kShared, p);
+    return launch_kernel(attend_few<T, D, NT, B>, p.whole ? p.batch.num_seqs * p.shape.kv_heads + p.batch.check_blocks() : *ctas, kFewThreads,
+                         F::kSmem, stream, B::kShared, p);
 }
+
+// The launches of a pass, and what is left for the join behind them.
+template <class B>
+struct Pass {
+    AttendParams<B> few, many;
+    int few_ctas = 0, few_rows = 0, many_ctas = 0;
+    bool cuts = false;  // something may be cut
+    int many_blocks() const { return many_ctas * (kManyRows / kJoinRows<1, B>); }
+};
 
 // Sequences with few rows (new tokens times query heads per key head) are read by attend_few, whose time is that of reading
 // the cache; the others by attend_many.  Which there are is known only on the device: a batch that may hold longer
@@ -427,7 +531,7 @@ static amoeba_status run_few(AttendParams<B>& p, int sms, int* ctas, cudaStream_
 // before the kernel in front of it ends, and wait there for its results if they read them (attend_join) or end only after
 // it (attend_many).
 template <class T, int D, class B>
-static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char* ws, int sms, cudaStream_t stream, const PrefixSums* prefix) {
+static amoeba_status run_pass(AttendParams<B>& p, int tp, int32_t dtype, char* ws, int sms, cudaStream_t stream, Pass<B>* pass) {
     const int64_t rows = (int64_t)p.batch.max_q_len * p.shape.group;
     const int64_t few_bytes = few_workspace(&p, ws, D);
     // In a batch with longer pieces attend_few gets the single tokens (and what has as few rows): its rows cost registers.  Groups
@@ -437,35 +541,46 @@ static amoeba_status run_attend(AttendParams<B>& p, int tp, int32_t dtype, char*
     const int most = !few ? 0 : few_rows <= 8 ? 8 : few_rows <= 16 ? 16 : kMaxFewRows;
     p.shape.min_rows = 0;
     p.shape.max_rows = most;
-    int few_ctas = 0;
     amoeba_status st = !few         ? AMOEBA_OK
-                       : most == 8  ? run_few<T, D, 1>(p, sms, &few_ctas, stream)
-                       : most == 16 ? run_few<T, D, 2>(p, sms, &few_ctas, stream)
-                                    : run_few<T, D, 4>(p, sms, &few_ctas, stream);
-    if (st != AMOEBA_OK || (p.whole && few && rows <= kMaxFewRows && !prefix)) return st;
-    if (p.whole) few_ctas = 0;  // nothing is cut
-    const int few_most = (int)std::min<int64_t>(rows, most);
-    AttendParams<B> many = p;
-    int many_ctas = 0, many_blocks = 0;
-    if (!few || rows > kMaxFewRows) {
-        many_workspace(&many, ws + few_bytes, D);
-        many.shape.min_rows = most + 1;
-        many.shape.max_rows = INT32_MAX;
-        many.shape.rows = kManyRows;
-        many.shape.tile = kManyTile;
-        many_ctas = std::min(sms, kMaxSms);
-        many_blocks = many_ctas * (kManyRows / kJoinRows<1, B>);
-        if ((st = launch_attend_many(many, tp, dtype, D, many_ctas, stream)) != AMOEBA_OK || groups) return st;
-    }
-    if constexpr (B::kShared)
-        if (prefix) {
-            const int64_t grid = few_ctas * few_most + many_blocks + (int64_t)prefix->num_rows * prefix->row_blocks;
-            return grid > INT32_MAX ? AMOEBA_ERR_UNSUPPORTED
-                                    : launch_kernel(attend_finish<T, D>, (int)grid, kJoinThreads, 0, stream, true, p, few_ctas, few_most, many,
-                                                    many_ctas, *prefix);
-        }
-    return launch_kernel(attend_join<T, D, B>, few_ctas * few_most + many_blocks, kJoinThreads, 0, stream, true, p, few_ctas, few_most, many,
-                         many_ctas);
+                       : most == 8  ? run_few<T, D, 1>(p, sms, &pass->few_ctas, stream)
+                       : most == 16 ? run_few<T, D, 2>(p, sms, &pass->few_ctas, stream)
+                                    : run_few<T, D, 4>(p, sms, &pass->few_ctas, stream);
+    if (st != AMOEBA_OK) return st;
+    if (p.whole) pass->few_ctas = 0;  // nothing is cut
+    pass->few_rows = (int)std::min<int64_t>(rows, most);
+    pass->cuts = !p.whole || rows > kMaxFewRows;
+    pass->few = pass->many = p;
+    if (few && rows <= kMaxFewRows) return AMOEBA_OK;
+    AttendParams<B>& many = pass->many;
+    many_workspace(&many, ws + few_bytes, D);
+    many.shape.min_rows = most + 1;
+    many.shape.max_rows = INT32_MAX;
+    many.shape.rows = kManyRows;
+    many.shape.tile = kManyTile;
+    pass->many_ctas = std::min(sms, kMaxSms);
+    return launch_attend_many(many, tp, dtype, D, pass->many_ctas, stream);
+}
+template <class T, int D, class B>
+static amoeba_status run_join(const Pass<B>& x, cudaStream_t stream) {
+    if (!x.cuts) return AMOEBA_OK;
+    return launch_kernel(attend_join<T, D, B>, x.few_ctas * x.few_rows + x.many_blocks(), kJoinThreads, 0, stream, true, x.few, x.few_ctas,
+                         x.few_rows, x.many, x.many_ctas);
+}
+// Short sequences are not worth cutting: what the shares and the join take, about 5 us, is what a CTA needs for 512
+// tokens, or for 1024 when there are units enough to fill the GPU (one sequence of 256 tokens, 8 key heads: 7.9 us whole,
+// 9.5 cut; of 1024: 20.5 and 11.3; 32 sequences of 1024: 24 and 29; of 2048: 41 and 47, but there one long one would
+// hold up all).  With max_q_len 0 sequences are only looked at.
+template <class B>
+static bool not_cut(const AttendParams<B>& p, int sms) {
+    const int64_t tokens = (int64_t)p.batch.max_blocks * p.cache.block_tokens;
+    return p.batch.max_q_len == 0 || tokens <= 512 || (tokens <= 1024 && (int64_t)p.batch.num_seqs * p.shape.kv_heads >= sms);
+}
+template <class T, int D>
+static amoeba_status run_attend(AttendParams<Batch>& p, int tp, int32_t dtype, char* ws, int sms, cudaStream_t stream) {
+    Pass<Batch> x;
+    p.whole = not_cut(p, sms);
+    const amoeba_status st = run_pass<T, D>(p, tp, dtype, ws, sms, stream, &x);
+    return st != AMOEBA_OK ? st : run_join<T, D>(x, stream);
 }
 
 }  // namespace amoeba
@@ -519,22 +634,10 @@ static bool units_fit(const amoeba_layout* l, int64_t num_seqs, int64_t rows) {
     return rows <= INT32_MAX && num_seqs * l->model.num_kv_heads <= INT32_MAX / (rows / kManyRows + 1);
 }
 
-// Short sequences are not worth cutting: what the shares and the join take, about 5 us, is what a CTA needs for 512
-// tokens, or for 1024 when there are units enough to fill the GPU (one sequence of 256 tokens, 8 key heads: 7.9 us whole,
-// 9.5 cut; of 1024: 20.5 and 11.3; 32 sequences of 1024: 24 and 29; of 2048: 41 and 47, but there one long one would
-// hold up all).  With max_q_len 0 sequences are only looked at.
-template <class B>
-static amoeba_status attend_pass(const amoeba_layout* layout, int32_t dtype, AttendParams<B>& p, char* ws, int sms, cudaStream_t stream,
-                                 const PrefixSums* prefix = nullptr) {
-    const amoeba_model& m = layout->model;
-    const int64_t tokens = (int64_t)p.batch.max_blocks * layout->block_tokens;
-    p.whole = rows_of(layout, p.batch.max_q_len) == 0 || tokens <= 512 || (tokens <= 1024 && p.batch.num_seqs * m.num_kv_heads >= sms);
-    if (dtype == AMOEBA_FP16)
-        return m.head_dim == 64 ? run_attend<__half, 64>(p, layout->tp, dtype, ws, sms, stream, prefix)
-                                : run_attend<__half, 128>(p, layout->tp, dtype, ws, sms, stream, prefix);
-    return m.head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, layout->tp, dtype, ws, sms, stream, prefix)
-                            : run_attend<__nv_bfloat16, 128>(p, layout->tp, dtype, ws, sms, stream, prefix);
-}
+// Calls run with the element type and head size as its template arguments.
+#define AMOEBA_BY_ELEMENT(run, ...)                                                                                   \
+    (dtype == AMOEBA_FP16 ? (layout->model.head_dim == 64 ? run<__half, 64>(__VA_ARGS__) : run<__half, 128>(__VA_ARGS__)) \
+                          : (layout->model.head_dim == 64 ? run<__nv_bfloat16, 64>(__VA_ARGS__) : run<__nv_bfloat16, 128>(__VA_ARGS__)))
 
 extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtype, int32_t layer,
                                        const void* const* pools, const amoeba_batch* batch, const void* const* q,
@@ -552,7 +655,7 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
     if (!units_fit(layout, p.batch.num_seqs, rows_of(layout, p.batch.max_q_len))) return AMOEBA_ERR_UNSUPPORTED;
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
-    return attend_pass(layout, dtype, p, static_cast<char*>(d_workspace), dev.sms, static_cast<cudaStream_t>(cuda_stream));
+    return AMOEBA_BY_ELEMENT(run_attend, p, layout->tp, dtype, static_cast<char*>(d_workspace), dev.sms, static_cast<cudaStream_t>(cuda_stream));
 }
 
 // ------------------------------------------------------------------------------------------------ shared prefixes
@@ -567,7 +670,8 @@ struct PrefixParams {
     const int32_t *group_starts, *prefix_lens;
     Group* groups;
     int64_t* tile0;
-    int32_t *first, *row_group, *status;
+    int2* own;
+    int32_t *row_group, *status;
     int32_t num_groups, max_group_rows, block_tokens;
     int32_t kv_heads, group;  // query heads per key head
 };
@@ -582,56 +686,27 @@ constexpr int kPrefixThreads = 1024, kPrefixWarps = kPrefixThreads / 32;
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_constant__ PrefixParams p) {
     __shared__ int64_t s_tiles[kPrefixThreads], s_warp[kPrefixWarps];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.batch.num_seqs, G = p.num_groups;
-    bool bad = false;
-    for (int g = tid; g < G; g += kPrefixThreads) {
-        const int a = p.group_starts[g], z = p.group_starts[g + 1];
-        bad |= a < 0 || z < a || z > S;
-    }
-    for (int s = tid; s < S; s += kPrefixThreads) p.first[s] = 0;
+    for (int s = tid; s < S; s += kPrefixThreads) p.own[s] = make_int2(0, -1);
     for (int r = tid; r < p.batch.num_rows; r += kPrefixThreads) p.row_group[r] = -1;
-    bad = __syncthreads_or(bad);
-    if (bad && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
+    const bool in_order = groups_in_order(p.group_starts, G, S);
+    if (!in_order && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
     int64_t run = 0;
     for (int base = 0; base < G; base += kPrefixThreads) {
         for (int g = base + warp; g < min(G, base + kPrefixThreads); g += kPrefixWarps) {
-            const int a = bad ? 0 : p.group_starts[g], z = bad ? 0 : p.group_starts[g + 1];
-            int least = INT32_MAX, row = INT32_MAX, with_rows = 0, q0 = INT32_MAX, q1 = 0, alone = 0, taking = 0;
-            bool ok = true;
-            for (int s = a + lane; s < z; s += 32) {
-                const Seq q = sequence(p.batch, s, p.block_tokens);
-                ok &= q.ok;
-                if (q.qn == 0) continue;
-                const int tiles = (q.qn * p.group - 1) / kManyRows + 1;
-                least = min(least, q.len - q.qn);
-                row = min(row, s);
-                q0 = min(q0, q.q0);
-                q1 = max(q1, q.q0 + q.qn);
-                alone += tiles;
-                taking += q.qn * p.group <= kMaxFewRows ? 1 : 12 * tiles;  // half tiles
-                ++with_rows;
-            }
-            ok = __all_sync(~0u, ok);
-            least = __reduce_min_sync(~0u, least);
-            row = __reduce_min_sync(~0u, row);
-            with_rows = __reduce_add_sync(~0u, with_rows);
-            q0 = __reduce_min_sync(~0u, q0);
-            q1 = __reduce_max_sync(~0u, q1);
-            alone = __reduce_add_sync(~0u, alone);
-            taking = __reduce_add_sync(~0u, taking);
             Group out{0, 0, 0, 0};
             int64_t tiles = 0;
-            if (z > a) {
-                const int given = p.prefix_lens[g];
-                const bool wrong = given < 0 || (with_rows && q1 - q0 > p.max_group_rows);
+            if (in_order) {
+                const GroupSums x = sum_group(p.batch, p.group_starts, g, p.block_tokens, p.group);
+                const int given = p.prefix_lens[g], len = min(given, x.least), key_tiles = (len - 1) / kManyTile + 1;
+                const bool wrong = refused(x, given, p.max_group_rows);
                 if (wrong && lane == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
-                const int len = min(given, least), key_tiles = (len - 1) / kManyTile + 1;
-                if (!wrong && ok && with_rows > 1 && len > 0) {
-                    const int row_tiles = (int)(((int64_t)(q1 - q0) * p.group - 1) / kManyRows) + 1;
-                    if (2 * (int64_t)(alone - row_tiles) * key_tiles > 8 * (int64_t)row_tiles + taking) {
-                        out = Group{q0, q1 - q0, len, row};
+                if (!wrong && x.ok && x.with_rows > 1 && len > 0) {
+                    const int row_tiles = (int)(((int64_t)(x.q1 - x.q0) * p.group - 1) / kManyRows) + 1;
+                    if (2 * (int64_t)(x.alone - row_tiles) * key_tiles > 8 * (int64_t)row_tiles + x.taking) {
+                        out = Group{x.q0, x.q1 - x.q0, len, x.row};
                         tiles = (int64_t)p.kv_heads * row_tiles * key_tiles;
-                        for (int s = a + lane; s < z; s += 32) p.first[s] = len;
-                        for (int r = q0 + lane; r < q1; r += 32) p.row_group[r] = g;
+                        for (int s = x.first + lane; s < x.end; s += 32) p.own[s] = make_int2(len, g);
+                        for (int r = x.q0 + lane; r < x.q1; r += 32) p.row_group[r] = g;
                     }
                 }
             }
@@ -664,7 +739,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_
 
 // Where the parts of the workspace begin: both passes' own, the carry, the groups and the sequences' first tokens.
 struct SharedSpace {
-    int64_t groups_pass, rest_pass, group_sums, rest_sums, groups, tile0, first, row_group, end;
+    int64_t groups_pass, rest_pass, group_sums, rest_sums, groups, tile0, own, row_group, end;
 };
 // Sums of all rows and query heads.
 static int64_t sums_space(const amoeba_layout* l, int64_t rows, char* ws, Sums* out) {
@@ -683,10 +758,65 @@ static SharedSpace shared_space(const amoeba_layout* l, const amoeba_batch* b, c
     s.rest_sums = s.group_sums + sums_space(l, b->num_rows, nullptr, nullptr);
     s.groups = s.rest_sums + sums_space(l, b->num_rows, nullptr, nullptr);
     s.tile0 = s.groups + (int64_t)x->num_groups * sizeof(Group);
-    s.first = s.tile0 + ((int64_t)x->num_groups / 2 + 1) * 16;
-    s.row_group = s.first + ints(b->num_seqs);
+    s.own = s.tile0 + ((int64_t)x->num_groups / 2 + 1) * 16;
+    s.row_group = s.own + ints(2 * (int64_t)b->num_seqs);
     s.end = s.row_group + ints(b->num_rows);
     return s;
+}
+
+template <class T, int D>
+static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layout* layout, int32_t dtype, const amoeba_batch* batch,
+                                const amoeba_prefixes* prefixes, char* ws, int sms, cudaStream_t stream) {
+    const SharedSpace at = shared_space(layout, batch, prefixes);
+    const int32_t group_rows = std::min(prefixes->max_group_rows, p.batch.num_rows);
+    amoeba_status st;
+    Pass<SharedBatch> rest;
+    p.whole = not_cut(p, sms);
+    p.batch.group_starts = prefixes->d_group_starts, p.batch.prefix_lens = prefixes->d_prefix_lens;
+    p.batch.num_groups = prefixes->num_groups, p.batch.max_group_rows = group_rows;
+    // Where all sequences together have less to read than the launches for the groups would take (a tile takes an SM about 1.5 us; 8
+    // sequences of 160 tokens: 13.6 us with them, 8 without), they attend by themselves, and the groups' numbers are only checked.
+    const int64_t tiles = ((int64_t)p.batch.max_blocks * p.cache.block_tokens + kManyTile - 1) / kManyTile;
+    if (p.whole && (int64_t)p.batch.num_seqs * p.shape.kv_heads * tiles <= 8 * sms) {
+        if ((st = run_pass<T, D>(p, layout->tp, dtype, ws + at.rest_pass, sms, stream, &rest)) != AMOEBA_OK) return st;
+        return run_join<T, D>(rest, stream);
+    }
+    PrefixParams x{};
+    x.batch = p.batch;
+    x.group_starts = prefixes->d_group_starts, x.prefix_lens = prefixes->d_prefix_lens;
+    x.groups = reinterpret_cast<Group*>(ws + at.groups), x.tile0 = reinterpret_cast<int64_t*>(ws + at.tile0);
+    x.own = reinterpret_cast<int2*>(ws + at.own), x.row_group = reinterpret_cast<int32_t*>(ws + at.row_group);
+    x.status = p.status;
+    x.num_groups = prefixes->num_groups, x.max_group_rows = group_rows, x.block_tokens = layout->block_tokens;
+    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group;
+    if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, false, x)) != AMOEBA_OK) return st;
+    p.batch.own = x.own;
+    sums_space(layout, p.batch.num_rows, ws + at.rest_sums, &p.sums);
+    if ((st = run_pass<T, D>(p, layout->tp, dtype, ws + at.rest_pass, sms, stream, &rest)) != AMOEBA_OK) return st;
+    if (prefixes->num_groups == 0 || group_rows == 0) return run_join<T, D>(rest, stream);
+    Pass<SharedBatch> groups;
+    AttendParams<SharedBatch> g = p;
+    g.batch.groups = x.groups, g.batch.tile0 = x.tile0;
+    g.batch.num_seqs = prefixes->num_groups;
+    g.batch.max_q_len = group_rows;
+    g.whole = not_cut(g, sms);
+    sums_space(layout, p.batch.num_rows, ws + at.group_sums, &g.sums);
+    if ((st = run_pass<T, D>(g, layout->tp, dtype, ws + at.groups_pass, sms, stream, &groups)) != AMOEBA_OK) return st;
+    PrefixSums sums{};
+    sums.rows = g.sums;
+    if (groups.many_ctas) {
+        sums.parts = Sums{groups.many.part_o, groups.many.part_m, groups.many.part_l};
+        sums.ctas = groups.many_ctas;
+    } else if ((st = run_join<T, D>(groups, stream)) != AMOEBA_OK) {
+        return st;
+    }
+    sums.groups = x.groups, sums.tile0 = x.tile0, sums.row_group = x.row_group;
+    sums.num_groups = prefixes->num_groups, sums.num_rows = p.batch.num_rows;
+    // Enough blocks for a head to a warp, unless there are rows enough to fill the GPU as it is.
+    sums.row_blocks = p.batch.num_rows >= 1024 ? 1 : (p.q_heads + kJoinWarps - 1) / kJoinWarps;
+    const int64_t grid = rest.few_ctas + rest.many_blocks() + (int64_t)sums.num_rows * sums.row_blocks;
+    if (grid > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
+    return launch_kernel(attend_finish<T, D>, (int)grid, kJoinThreads, 0, stream, true, rest.few, rest.few_ctas, rest.many, rest.many_ctas, sums);
 }
 
 extern "C" amoeba_status amoeba_attend_shared_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
@@ -720,39 +850,6 @@ extern "C" amoeba_status amoeba_attend_shared(const amoeba_layout* layout, int32
         return AMOEBA_ERR_UNSUPPORTED;
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
-    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    char* ws = static_cast<char*>(d_workspace);
-    const SharedSpace at = shared_space(layout, batch, prefixes);
-    const int32_t num_groups = group_rows ? prefixes->num_groups : 0;
-    PrefixParams x{};
-    x.batch = p.batch;
-    x.group_starts = prefixes->d_group_starts, x.prefix_lens = prefixes->d_prefix_lens;
-    x.groups = reinterpret_cast<Group*>(ws + at.groups), x.tile0 = reinterpret_cast<int64_t*>(ws + at.tile0);
-    x.first = reinterpret_cast<int32_t*>(ws + at.first), x.row_group = reinterpret_cast<int32_t*>(ws + at.row_group);
-    x.status = d_status;
-    x.num_groups = prefixes->num_groups, x.max_group_rows = group_rows, x.block_tokens = layout->block_tokens;
-    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group;
-    if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, false, x)) != AMOEBA_OK) return st;
-    p.batch.first = x.first;
-    sums_space(layout, p.batch.num_rows, ws + at.rest_sums, &p.sums);
-    if (!num_groups) return attend_pass(layout, dtype, p, ws + at.rest_pass, dev.sms, stream);
-    AttendParams<SharedBatch> g = p;
-    g.batch.groups = x.groups, g.batch.tile0 = x.tile0;
-    g.batch.num_seqs = num_groups;
-    g.batch.max_q_len = group_rows;
-    sums_space(layout, p.batch.num_rows, ws + at.group_sums, &g.sums);
-    if ((st = attend_pass(layout, dtype, g, ws + at.groups_pass, dev.sms, stream)) != AMOEBA_OK) return st;
-    PrefixSums sums{};
-    sums.rows = g.sums;
-    if (rows_of(layout, group_rows) > kMaxGroupRows) {
-        AttendParams<SharedBatch> cut{};  // where the parts of its units are
-        many_workspace(&cut, ws + at.groups_pass + few_workspace<Batch>(nullptr, nullptr, layout->model.head_dim), layout->model.head_dim);
-        sums.parts = Sums{cut.part_o, cut.part_m, cut.part_l};
-        sums.ctas = std::min(dev.sms, kMaxSms);
-    }
-    sums.groups = x.groups, sums.tile0 = x.tile0, sums.row_group = x.row_group;
-    sums.num_groups = num_groups, sums.num_rows = p.batch.num_rows;
-    // Enough blocks for a head to a warp, unless there are rows enough to fill the GPU as it is.
-    sums.row_blocks = p.batch.num_rows >= 1024 ? 1 : (p.q_heads + kJoinWarps - 1) / kJoinWarps;
-    return attend_pass(layout, dtype, p, ws + at.rest_pass, dev.sms, stream, &sums);
+    return AMOEBA_BY_ELEMENT(run_shared, p, layout, dtype, batch, prefixes, static_cast<char*>(d_workspace), dev.sms,
+                             static_cast<cudaStream_t>(cuda_stream));
 }

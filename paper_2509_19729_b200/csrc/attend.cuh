@@ -60,6 +60,13 @@ struct Joined {
         acc.x = acc.x * f + x.x * g, acc.y = acc.y * f + x.y * g, acc.z = acc.z * f + x.z * g, acc.w = acc.w * f + x.w * g;
         top = up;
     }
+    // For the first half of the warp: what the second has.
+    __device__ __forceinline__ void add_lower_half() {
+        const float4 x = make_float4(__shfl_down_sync(~0u, acc.x, 16), __shfl_down_sync(~0u, acc.y, 16), __shfl_down_sync(~0u, acc.z, 16),
+                                     __shfl_down_sync(~0u, acc.w, 16));
+        const float top2 = __shfl_down_sync(~0u, top, 16), l2 = __shfl_down_sync(~0u, l, 16);
+        add(top2, l2, x);
+    }
 };
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
     return (uint64_t)(a | b) >> 32 == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;

@@ -727,14 +727,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
-    if (B::kShared) {
-        grid_dependency_wait();  // the groups are there, or what is carried
-        grid_dependency_launch();
-    }
     bool busy;
     if constexpr (B::kShared) busy = p.batch.by_groups() ? make_group_share(p, share) : make_share(p, share, reinterpret_cast<int32_t*>(smem));
     else busy = make_share(p, share, reinterpret_cast<int32_t*>(smem));
-    if (!B::kShared) grid_dependency_launch();
+    grid_dependency_launch();
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();

@@ -28,6 +28,7 @@ struct Batch {
     const int32_t *table, *lens, *starts;
     int32_t num_seqs, max_blocks, num_rows, max_q_len;
     __host__ __device__ bool by_groups() const { return false; }
+    int check_blocks() const { return 0; }
 };
 
 // The rows of all sequences of a group, over the tokens [0, len) that these have in common; row: of the block table.
@@ -40,8 +41,12 @@ struct SharedBatch : Batch {
     static constexpr bool kShared = true;
     const Group* groups;
     const int64_t* tile0;  // [groups + 1] first tile of every group in the end-to-end order of all groups' tiles
-    const int32_t* first;  // [num_seqs] tokens in front of it are the group's
+    const int2* own;       // [num_seqs] tokens in front of x are those of group y; null: nothing is shared
+    // What there is to be checked where nothing is shared, because it would not pay.
+    const int32_t *group_starts, *prefix_lens;
+    int32_t num_groups, max_group_rows;
     __host__ __device__ bool by_groups() const { return groups != nullptr; }
+    int check_blocks() const { return !own && !groups; }  // blocks beside a launch's own that check the groups' numbers
 };
 
 // Cached tokens of a sequence at most: their indices, rounded up to tiles and blocks or moved by a window, stay below 2^31.
@@ -54,6 +59,7 @@ struct Seq {
     int32_t row;    // of the block table
     int32_t first;  // tokens in front of it are another pass's
     bool level;     // every row sees all len tokens
+    int32_t group;  // whose pass that is
 };
 // Cache index up to which the sequence's new token `tok` sees, itself included.
 __device__ __forceinline__ int last_seen(const Seq& q, int tok) { return q.level ? q.len - 1 : q.len - q.qn + tok; }
@@ -72,18 +78,21 @@ __device__ __forceinline__ Seq sequence(const Batch& b, int s, int block_tokens)
     q.ok = q.q0 >= 0 && q1 >= q.q0 && q1 <= b.num_rows && q1 - q.q0 <= b.max_q_len && q.len >= 0 &&
            q.len <= min((int64_t)b.max_blocks * block_tokens, (int64_t)kMaxTokens);
     q.qn = q.ok ? q1 - q.q0 : 0;
-    q.row = s, q.first = 0, q.level = false;
+    q.row = s, q.first = 0, q.level = false, q.group = -1;
     return q;
 }
 __device__ __forceinline__ Seq sequence(const SharedBatch& b, int s, int block_tokens) {
     if (!b.groups) {
         Seq q = sequence(static_cast<const Batch&>(b), s, block_tokens);
-        q.first = __ldcg(b.first + s);
+        if (b.own) {
+            const int2 own = __ldcg(b.own + s);
+            q.first = own.x, q.group = own.y;
+        }
         return q;
     }
     const int4 g = __ldcg(reinterpret_cast<const int4*>(b.groups) + s);
     Seq q;
-    q.q0 = g.x, q.qn = g.y, q.len = g.z, q.row = g.w, q.first = 0;
+    q.q0 = g.x, q.qn = g.y, q.len = g.z, q.row = g.w, q.first = 0, q.group = s;
     q.ok = q.level = true;
     return q;
 }

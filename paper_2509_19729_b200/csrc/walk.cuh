@@ -18,6 +18,7 @@ struct Shape {  // what the split depends on, besides the batch
     int32_t tile;       // tokens per tile, a power of two
     int32_t min_rows, max_rows;  // sequences with more or fewer rows (new tokens * group) are not this launch's
     int32_t rowless;    // 1: sequences without rows have one row tile all the same
+    int32_t start;      // what a unit's start and end cost, in tiles (take_weighted_share)
 };
 
 struct Range {
@@ -193,6 +194,91 @@ __device__ void take_share(const Shape& p, const B& b, int block_tokens, Walk* w
         walk->open(p, b, block_tokens, s_seq);
         walk->seek(p, s_off);
     }
+}
+
+// The same where units are short and what starting and ending one costs counts: every unit weighs p.start tiles more, and the CTAs' shares
+// are even by weight.  A border that falls into a unit's extra weight moves to its first tile.  [*begin, *end) are tiles as above.
+// scratch: shared memory that nothing else uses yet.
+struct ShareBorder {
+    int64_t off, before;  // weight in front of it in its sequence, tiles in front of the sequence
+    int64_t at;           // its tile
+    int32_t s;
+    Walk walk;
+};
+template <int kThreads, class B>
+__device__ void take_weighted_share(const Shape& p, const B& b, int block_tokens, Walk* walk, int64_t* begin_out, int64_t* end_out,
+                                    int32_t* status, char* scratch) {
+    constexpr int kWarps = kThreads / 32;
+    int64_t* const s_warp = reinterpret_cast<int64_t*>(scratch);  // [2][kWarps]
+    ShareBorder* const border = reinterpret_cast<ShareBorder*>(s_warp + 2 * kWarps);
+    const int tid = threadIdx.x, lane = tid % 32;
+    int64_t tiles = 0, weight = 0, sums[2] = {0, 0};
+    auto look = [&](int s) {
+        const Seq q = sequence(b, s, block_tokens);
+        tiles = p.kv_heads * head_tiles(p, q), weight = tiles + (int64_t)p.kv_heads * row_tiles(p, q) * p.start;
+        return q.ok;
+    };
+    for (int s = tid; s < b.num_seqs; s += kThreads) {
+        if (!look(s) && blockIdx.x == 0) report(status, AMOEBA_ERR_INVALID_ARG);
+        sums[0] += tiles, sums[1] += weight;
+    }
+    const int64_t all_tiles = block_sum<kThreads>(sums[0], s_warp), all = block_sum<kThreads>(sums[1], s_warp + kWarps);
+    const int ctas = (int)max((int64_t)1, min((int64_t)gridDim.x, all_tiles));
+    const int c = min((int)blockIdx.x, ctas);
+    const int64_t at[2] = {share_begin(all, ctas, c), share_begin(all, ctas, min(c + 1, ctas))};
+    int64_t run_tiles = 0, run = 0;
+    for (int base = 0; base < b.num_seqs; base += kThreads) {
+        const int s = base + tid;
+        if (b.num_seqs > kThreads) {
+            tiles = weight = 0;
+            if (s < b.num_seqs) look(s);
+        }
+        int64_t incl[2] = {tiles, weight};
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t up0 = __shfl_up_sync(~0u, incl[0], o), up1 = __shfl_up_sync(~0u, incl[1], o);
+            if (lane >= o) incl[0] += up0, incl[1] += up1;
+        }
+        __syncthreads();
+        if (lane == 31) s_warp[tid / 32] = incl[0], s_warp[kWarps + tid / 32] = incl[1];
+        __syncthreads();
+        int64_t before_tiles = run_tiles, before = run;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < tid / 32) before_tiles += s_warp[w], before += s_warp[kWarps + w];
+            run_tiles += s_warp[w], run += s_warp[kWarps + w];
+        }
+        const int64_t first = before + incl[1] - weight;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (at[i] >= first && at[i] < first + weight)
+                border[i].s = s, border[i].off = at[i] - first, border[i].before = before_tiles + incl[0] - tiles;
+        if (run > at[1]) break;  // block-uniform
+    }
+    __syncthreads();
+    if (tid < 64 && at[tid / 32] < all) {  // a warp to each border
+        ShareBorder& x = border[tid / 32];
+        Walk w{};
+        w.open(p, b, block_tokens, x.s);
+        const int64_t head = head_tiles(p, w.seq), heavy = head + (int64_t)w.nm * p.start;
+        int64_t off = x.off;
+        w.h = (off | heavy) >> 31 == 0 ? (int)((uint32_t)off / (uint32_t)heavy) : (int)(off / heavy);
+        off -= w.h * heavy;
+        int64_t tile = x.before + w.h * head;
+        for (w.m = 0;; ++w.m) {
+            w.range = row_tile_range(p, w.seq, w.m);
+            if (off < w.range.tiles + p.start) break;
+            off -= w.range.tiles + p.start, tile += w.range.tiles;
+        }
+        w.t = max((int)off - p.start, 0);
+        __syncwarp();
+        if (lane == 0) x.walk = w, x.at = tile + w.t;
+    }
+    __syncthreads();
+    *begin_out = at[0] < all ? border[0].at : all_tiles;
+    *end_out = at[1] < all ? border[1].at : all_tiles;
+    if (*end_out > *begin_out) *walk = border[0].walk;
+    __syncthreads();  // the scratch is free
 }
 
 }  // namespace amoeba
