@@ -24,6 +24,7 @@ struct GroupSums {
 };
 __device__ __forceinline__ GroupSums sum_group(const Batch& b, const int32_t* group_starts, int g, int block_tokens, int heads) {
     GroupSums x{group_starts[g], group_starts[g + 1], INT32_MAX, 0, INT32_MAX, 0, INT32_MAX, 0, 0, true};
+#pragma unroll 4
     for (int s = x.first + (int)threadIdx.x % 32; s < x.end; s += 32) {
         const Seq q = sequence(b, s, block_tokens);
         x.ok &= q.ok;
@@ -390,7 +391,7 @@ __device__ __forceinline__ void add_prefix(const AttendParams<B>& p, const Prefi
         const int64_t begin = __ldcg(x.tile0 + g) + ((int64_t)kv_head * row_tiles + m) * tiles;
         const int c0 = (int)divide(begin, even), c1 = (int)divide(begin + tiles - 1, even);
         if (c0 < c1) {
-#pragma unroll 4
+#pragma unroll 8
             for (int c = c0 + first; c <= c1; c += step) {
                 const int64_t part = (int64_t)(2 * c + (c == c0)) * kManyRows + r;
                 j.add(x.parts.m[part], x.parts.l[part], *reinterpret_cast<const float4*>(x.parts.o + part * D + d));
@@ -462,18 +463,29 @@ __global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_const
     block -= many_ctas * many_groups;
     const int row = block / x.row_blocks, g = x.row_group[row], lane = threadIdx.x % 32;
     if (g < 0) return;
-    for (int head = block % x.row_blocks * kJoinWarps + (int)threadIdx.x / 32; head < few.q_heads; head += x.row_blocks * kJoinWarps) {
-        const int64_t at = (int64_t)row * few.q_heads + head;
-        const float l = few.sums.l[at];
-        if (l == kCutRow) continue;
-        const int kv_head = head / few.shape.group, r = head - kv_head * few.shape.group, half = lane / kLanes, d = lane % kLanes * 4;
-        Seq q{};
-        q.q0 = row;
-        Joined j;
-        if (half == 0) j.add(few.sums.m[at], l, *reinterpret_cast<const float4*>(few.sums.o + at * D + d));
-        add_prefix<D>(few, x, g, q, kv_head, r, half, kAtOnce, j);
-        if (kAtOnce == 2) j.add_lower_half();
-        if (half == 0) write_row<T, D>(few, q, kv_head, r, d, j);
+    const int half = lane / kLanes, d = lane % kLanes * 4, stride = x.row_blocks * kJoinWarps;
+    constexpr int kHeads = 4;  // of a warp at a time, so that the loads of their own sums overlap
+    for (int head0 = block % x.row_blocks * kJoinWarps + (int)threadIdx.x / 32; head0 < few.q_heads; head0 += kHeads * stride) {
+        float l[kHeads], m[kHeads];
+        float4 o[kHeads];
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            const int64_t at = (int64_t)row * few.q_heads + min(head0 + i * stride, few.q_heads - 1);
+            l[i] = few.sums.l[at], m[i] = few.sums.m[at], o[i] = *reinterpret_cast<const float4*>(few.sums.o + at * D + d);
+        }
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            const int head = head0 + i * stride;
+            if (head >= few.q_heads || l[i] == kCutRow) continue;  // (of a cut row only l is there)
+            const int kv_head = head / few.shape.group, r = head - kv_head * few.shape.group;
+            Seq q{};
+            q.q0 = row;
+            Joined j;
+            if (half == 0) j.add(m[i], l[i], o[i]);
+            add_prefix<D>(few, x, g, q, kv_head, r, half, kAtOnce, j);
+            if (kAtOnce == 2) j.add_lower_half();
+            if (half == 0) write_row<T, D>(few, q, kv_head, r, d, j);
+        }
     }
 }
 
@@ -681,11 +693,13 @@ struct PrefixParams {
 //
 // Whether it pays is counted in tiles of 128 tokens (a tile of a sequence with few rows costs about as much as one of 256 rows): every
 // tile of rows reads the prefix, of each sequence by itself or of the group's rows together; a group's unit costs its start and end, about
-// four tiles, and taking up the sums half a tile for a few rows, six for 256.
+// four tiles, and joining its sums with the sequences' half a tile for a few rows, six for 256.
 constexpr int kPrefixThreads = 1024, kPrefixWarps = kPrefixThreads / 32;
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_constant__ PrefixParams p) {
     __shared__ int64_t s_tiles[kPrefixThreads], s_warp[kPrefixWarps];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.batch.num_seqs, G = p.num_groups;
+    grid_dependency_launch();
+    grid_dependency_wait();
     for (int s = tid; s < S; s += kPrefixThreads) p.own[s] = make_int2(0, -1);
     for (int r = tid; r < p.batch.num_rows; r += kPrefixThreads) p.row_group[r] = -1;
     const bool in_order = groups_in_order(p.group_starts, G, S);
@@ -789,7 +803,7 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     x.status = p.status;
     x.num_groups = prefixes->num_groups, x.max_group_rows = group_rows, x.block_tokens = layout->block_tokens;
     x.kv_heads = p.shape.kv_heads, x.group = p.shape.group;
-    if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, false, x)) != AMOEBA_OK) return st;
+    if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, true, x)) != AMOEBA_OK) return st;
     p.batch.own = x.own;
     sums_space(layout, p.batch.num_rows, ws + at.rest_sums, &p.sums);
     if ((st = run_pass<T, D>(p, layout->tp, dtype, ws + at.rest_pass, sms, stream, &rest)) != AMOEBA_OK) return st;

@@ -271,8 +271,8 @@ struct Parts {
 
 // ---- loading
 template <int D, class B>
-struct Loader : TileLoader<D, kLoadWarps> {
-    using Base = TileLoader<D, kLoadWarps>;
+struct Loader : TileLoader<D, kLoadWarps, B::kShared> {
+    using Base = TileLoader<D, kLoadWarps, B::kShared>;
     const AttendParams<B>& p;
     const uint32_t smem;  // two query tiles, then the ring
     ManyBarriers& b;
@@ -307,6 +307,7 @@ __device__ RingPlace load_loop(const AttendParams<B>& p, const CacheMaps& maps, 
     while (ok && part.next(p, share)) {
         const Walk& w = part.w;
         load.open(w, p.batch);
+        load.once = w.nm == 1;
         int key0 = w.range.base + w.t * kManyTile;
         auto at = load.groups(w.range.lo, w.range.hi, key0), next = load.groups(w.range.lo, w.range.hi, key0 + kManyTile);
         // (the first keys and values are on their way while the queries are gathered, which takes longer)

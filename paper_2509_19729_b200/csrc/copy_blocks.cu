@@ -69,6 +69,8 @@ struct BlockCopyItems {
 __global__ void __launch_bounds__(1024) copy_blocks(const __grid_constant__ BlockCopyParams p, const RingShape rs) {
     extern __shared__ __align__(128) char smem[];
     const PairRing r = pair_ring_setup(smem, rs);
+    grid_dependency_launch();
+    grid_dependency_wait();  // the pairs and blocks are there
     const BlockCopyItems items(p, (int)gridDim.x * r.nrings);
     const bool ok = pair_bulk_ring(r.role, items, items.count(), (int64_t)r.ring * gridDim.x + blockIdx.x,
                                    (int64_t)gridDim.x * r.nrings, r.stages, r.full, r.empty, r.abort, rs);
@@ -111,5 +113,5 @@ extern "C" amoeba_status amoeba_copy_blocks(const amoeba_layout* layout, void* c
     const int64_t most = (int64_t)pairs_cap * p.n_layers * p.workers * p.runs * ((p.run + kCopyLeast - 1) / kCopyLeast);
     const int grid = (int)std::min<int64_t>(most, dev.sms);
     if (ensure_dynamic_smem((const void*)copy_blocks, (int)bs.smem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    return launch_kernel(copy_blocks, grid, bs.threads, bs.smem, static_cast<cudaStream_t>(cuda_stream), false, p, bs.ring);
+    return launch_kernel(copy_blocks, grid, bs.threads, bs.smem, static_cast<cudaStream_t>(cuda_stream), true, p, bs.ring);
 }

@@ -130,6 +130,14 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
             "r"(dst), "l"(map), "r"(dim), "r"(token), "r"(kv), "r"(head), "r"(block), "r"(smem_u32(bar))
         : "memory");
 }
+// The same with an L2 policy.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int dim, int token, int kv, int head, int block,
+                                         uint64_t* bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], "
+        "%8;" ::"r"(dst), "l"(map), "r"(dim), "r"(token), "r"(kv), "r"(head), "r"(block), "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
 // Where a loading thread is in its ring of tiles: the next one, and the parity that it waits for at its `empty` (the first round
 // waits for nothing).
 struct RingPlace {
@@ -144,8 +152,8 @@ __device__ __forceinline__ void drain_ring(uint64_t* full, RingPlace at) {
         for (uint32_t n = 0; n < kDrainWaitTries && !mbar_test_wait(&full[i], i < at.slot ? at.phase ^ 1 : at.phase); ++n) __nanosleep(64);
 }
 // The tiles that kWarps warps load together: by boxes where all 128 tokens are wanted and the blocks have a box's shape, else
-// each lane 16 bytes at a time.
-template <int D, int kWarps>
+// each lane 16 bytes at a time.  kOnce: `once` says whether what is loaded is not read again soon; it is then the first to leave L2.
+template <int D, int kWarps, bool kOnce = false>
 struct TileLoader {
     const CacheView& v;
     const CacheMaps& maps;
@@ -154,10 +162,14 @@ struct TileLoader {
     const int32_t* table = nullptr;    // the sequence's blocks
     const CUtensorMap* map = nullptr;
     int hw = 0;                        // head of the worker
+    bool once = false;
+    uint64_t policy = 0;
     static constexpr int kChunks = D / 8, kStep = 32 / kChunks;  // a warp loads kStep rows at a time
 
     __device__ __forceinline__ TileLoader(const CacheView& v_, const CacheMaps& maps_, int box_rows_, int warp_, int lane_)
-        : v(v_), maps(maps_), box_rows(box_rows_), warp(warp_), lane(lane_) {}
+        : v(v_), maps(maps_), box_rows(box_rows_), warp(warp_), lane(lane_) {
+        if (kOnce) policy = policy_evict_first();
+    }
     __device__ __forceinline__ void open(const Walk& w, const Batch& b) {
         const int r = w.h / v.heads;
         hw = w.h - r * v.heads;
@@ -190,7 +202,8 @@ struct TileLoader {
             const int block = __shfl_sync(~0u, group.block, row / 8 & 15), token = __shfl_sync(~0u, group.in_block, row / 8 & 15);
             if (row < 128) {
                 mbar_arrive_expect_tx(bar, box_rows * 128);
-                load_box(dst + half * (128 * 128) + row * 128, map, half * 64, token, kv, hw, block, bar);
+                if (kOnce && once) load_box(dst + half * (128 * 128) + row * 128, map, half * 64, token, kv, hw, block, bar, policy);
+                else load_box(dst + half * (128 * 128) + row * 128, map, half * 64, token, kv, hw, block, bar);
             } else {
                 mbar_arrive(bar);
             }

@@ -1,6 +1,7 @@
 // Warp-level pieces shared by the operators that read the cache with few query rows: asynchronous 16-byte loads into
 // swizzled shared memory, 8x8 matrix loads and the 16x8x16 matrix instruction.
 #pragma once
+#include "copy_engine.cuh"
 #include "walk.cuh"
 
 namespace amoeba {
@@ -8,6 +9,10 @@ namespace amoeba {
 // 16 bytes global -> shared; src_bytes 0 writes zeros and reads nothing.
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int src_bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+// The same, for what is not read again soon: it is the first to leave L2.
+__device__ __forceinline__ void cp_async16_once(uint32_t dst, const void* src, int src_bytes, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(src_bytes), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -63,6 +68,7 @@ struct Ahead {
     int32_t* status;
     const int lane, offset;
     const bool one_block;  // 16 tokens lie in one block
+    uint64_t policy = 0;   // of a SharedBatch's loads
     Walk w;
     int64_t left;          // tiles to go
     const int32_t* table;
@@ -73,6 +79,7 @@ struct Ahead {
                                      int offset_)
         : v(v_), b(b_), shape(s_), status(status_), lane(threadIdx.x & 31), offset(offset_), one_block(v_.block_tokens % 16 == 0), w(w_),
           left(n) {
+        if (B::kShared) policy = policy_evict_first();
         if (left > 0) {
             open();
             look_up();
@@ -83,6 +90,10 @@ struct Ahead {
         const int r = w.h / v.heads;
         hw = w.h - r * v.heads;
         head = v.pools[r] + hw * v.head_stride;
+    }
+    __device__ __forceinline__ void start(uint32_t dst, const void* src, int src_bytes) const {
+        if (B::kShared) cp_async16_once(dst, src, src_bytes, policy);
+        else cp_async16(dst, src, src_bytes);
     }
     __device__ __forceinline__ int key0() const { return w.range.base + w.t * kTile + offset; }
     __device__ __forceinline__ void look_up() {
@@ -114,8 +125,8 @@ struct Ahead {
 #pragma unroll
                 for (int i = 0; i < kRows; ++i) {
                     const char* s = src + i * kStep * v.tok_stride;
-                    cp_async16(dst + swizzled<D>(r0 + i * kStep, c), s, 16);
-                    if (kValues) cp_async16(dst + 16 * D * 2 + swizzled<D>(r0 + i * kStep, c), s + v.kv_stride, 16);
+                    start(dst + swizzled<D>(r0 + i * kStep, c), s, 16);
+                    if (kValues) start(dst + 16 * D * 2 + swizzled<D>(r0 + i * kStep, c), s + v.kv_stride, 16);
                 }
             } else {
 #pragma unroll
@@ -123,8 +134,8 @@ struct Ahead {
                     const int r = r0 + i * kStep;
                     const bool in = mask >> r & 1u;
                     const char* s = in ? src + i * kStep * v.tok_stride : head;
-                    cp_async16(dst + swizzled<D>(r, c), s, in ? 16 : 0);
-                    if (kValues) cp_async16(dst + 16 * D * 2 + swizzled<D>(r, c), in ? s + v.kv_stride : s, in ? 16 : 0);
+                    start(dst + swizzled<D>(r, c), s, in ? 16 : 0);
+                    if (kValues) start(dst + 16 * D * 2 + swizzled<D>(r, c), in ? s + v.kv_stride : s, in ? 16 : 0);
                 }
             }
         } else {
@@ -139,8 +150,8 @@ struct Ahead {
                     bad |= !in;
                     if (in) s = head + own * v.block_stride + (key % v.block_tokens) * v.tok_stride + c * 16;
                 }
-                cp_async16(dst + swizzled<D>(r, c), s, in ? 16 : 0);
-                if (kValues) cp_async16(dst + 16 * D * 2 + swizzled<D>(r, c), in ? s + v.kv_stride : s, in ? 16 : 0);
+                start(dst + swizzled<D>(r, c), s, in ? 16 : 0);
+                if (kValues) start(dst + 16 * D * 2 + swizzled<D>(r, c), in ? s + v.kv_stride : s, in ? 16 : 0);
                 const uint32_t there = __ballot_sync(~0u, in);
 #pragma unroll
                 for (int j = 0; j < kStep; ++j) mask |= (there >> (j * kChunks) & 1u) << (i * kStep + j);
