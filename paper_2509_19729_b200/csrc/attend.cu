@@ -19,23 +19,25 @@ struct GroupSums {
     int32_t first, end;        // sequences; none if the numbers are bad
     int32_t q0, q1, row;       // rows, and the first sequence that has any
     int32_t with_rows, least;  // sequences with rows, and the fewest tokens in front of the new ones
-    int32_t alone, taking;     // row tiles of all sequences, and what joining their sums costs, in half tiles
+    int32_t alone, taking;     // what a tile of the prefix costs all sequences by themselves, and what joining their sums with the group's does
     bool ok;
 };
-__device__ __forceinline__ GroupSums sum_group(const Batch& b, const int32_t* group_starts, int g, int block_tokens, int heads) {
+// What a tile of 128 tokens costs so many rows of attend_many, in tiles of 128 rows: the last, of up to 128, is half as large.
+__device__ __forceinline__ int rows_cost(int rows) { return rows / kManyRows * 2 + (rows % kManyRows > 128 ? 2 : rows % kManyRows > 0); }
+__device__ __forceinline__ GroupSums sum_group(const Batch& b, const int32_t* group_starts, int g, int block_tokens, int heads, int few_cost) {
     GroupSums x{group_starts[g], group_starts[g + 1], INT32_MAX, 0, INT32_MAX, 0, INT32_MAX, 0, 0, true};
 #pragma unroll 4
     for (int s = x.first + (int)threadIdx.x % 32; s < x.end; s += 32) {
         const Seq q = sequence(b, s, block_tokens);
         x.ok &= q.ok;
         if (q.qn == 0) continue;
-        const int tiles = (q.qn * heads - 1) / kManyRows + 1;
+        const bool few = q.qn * heads <= kMaxFewRows;
         x.least = min(x.least, q.len - q.qn);
         x.row = min(x.row, s);
         x.q0 = min(x.q0, q.q0);
         x.q1 = max(x.q1, q.q0 + q.qn);
-        x.alone += tiles;
-        x.taking += q.qn * heads <= kMaxFewRows ? 1 : 12 * tiles;
+        x.alone += few ? few_cost : rows_cost(q.qn * heads);
+        x.taking += few ? 1 : 5 * rows_cost(q.qn * heads);
         ++x.with_rows;
     }
     x.ok = __all_sync(~0u, x.ok);
@@ -64,7 +66,7 @@ __device__ void check_groups(const AttendParams<B>& p) {
     const SharedBatch& b = p.batch;
     bool bad = !groups_in_order(b.group_starts, b.num_groups, b.num_seqs);
     for (int g = threadIdx.x / 32; !bad && g < b.num_groups; g += blockDim.x / 32)
-        bad = refused(sum_group(b, b.group_starts, g, p.cache.block_tokens, p.shape.group), b.prefix_lens[g], b.max_group_rows);
+        bad = refused(sum_group(b, b.group_starts, g, p.cache.block_tokens, p.shape.group, 0), b.prefix_lens[g], b.max_group_rows);
     if (bad) report(p.status, AMOEBA_ERR_INVALID_ARG);
 }
 
@@ -106,7 +108,7 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
     if constexpr (B::kShared) {
         // The groups are there.  (Their own pass comes behind the sequences', whose blocks have all waited for them.)
         if (!p.batch.by_groups()) grid_dependency_wait();
-        if (p.whole && !p.batch.own && !p.batch.by_groups() && (int)blockIdx.x == p.batch.num_seqs * sh.kv_heads) return check_groups(p);
+        if (p.batch.check_blocks() && blockIdx.x == gridDim.x - 1) return check_groups(p);
     }
     if (p.whole) {
         walk.open(sh, p.batch, p.cache.block_tokens, blockIdx.x / sh.kv_heads);
@@ -115,8 +117,11 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
         n = walk.nm ? walk.range.tiles : 0;
     } else {
         int64_t begin, end;
-        if (B::kShared) take_weighted_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status, smem);
-        else take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
+        if constexpr (B::kShared)
+            take_weighted_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status, smem,
+                                             gridDim.x - p.batch.check_blocks());
+        else
+            take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
         write_cut(sh, p.cuts, walk, begin, end);
         n = end - begin;
     }
@@ -307,14 +312,14 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
 // one for each CTA where a few units of many rows run over a long cache.  Bound by its few dependent loads: 9 us by itself for 296
 // shares of 8 rows, of which the launch in front hides a part.
 constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps;
-template <int kWarps, class B>
-constexpr int kJoinRows = kWarps > 1 ? 1 : B::kShared ? kJoinWarps : 4 * kJoinWarps;  // of a block
+template <int kWarps>
+constexpr int kJoinRows = kWarps == 1 ? 4 * kJoinWarps : 1;  // of a block
 
 // `groups` blocks to every share: the unit that it begins in is joined there, if that began in the share before; with what `prefix` adds
 // to a row.
 template <class T, int D, int kWarps, class B, class Prefix>
 __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, int block, int groups, Prefix prefix) {
-    constexpr int kRows = kJoinRows<kWarps, B>, kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes to a part's row, parts at once
+    constexpr int kRows = kJoinRows<kWarps>, kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes to a part's row, parts at once
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int mine = block / groups, first_row = block % groups * kRows, R = p.shape.rows;
     const Cut cut = p.cuts[mine];
@@ -335,7 +340,7 @@ __device__ __forceinline__ void join_rows(const AttendParams<B>& p, int ctas, in
         const int r = first_row + (kWarps == 1 ? i + warp : 0);
         Joined j;
         if (r < cut.rows) {
-#pragma unroll (kWarps > 1 ? 8 : B::kShared ? 6 : 2)
+#pragma unroll (kWarps == 1 ? 2 : 8)
             for (int c = c0 + (kWarps == 1 ? 0 : warp) * kAtOnce + lane / kLanes; c < c1; c += kWarps * kAtOnce) {
                 if (p.cuts[c].begin == p.cuts[c].end) continue;
                 const int64_t part = (int64_t)(2 * c + (c == c0)) * R + r;
@@ -366,7 +371,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constan
     const int block = (int)blockIdx.x - few_ctas * few_rows;
     auto none = [](const Seq&, int, int, int, int, Joined&) {};
     if (block < 0) join_rows<T, D, kJoinWarps>(few, few_ctas, blockIdx.x, few_rows, none);
-    else join_rows<T, D, 1>(many, many_ctas, block, kManyRows / kJoinRows<1, B>, none);
+    else join_rows<T, D, 1>(many, many_ctas, block, kManyRows / kJoinRows<1>, none);
 }
 
 // What the groups' pass has left: sums of whole rows, and where it was attend_many's (`ctas` of them) the parts of its cut units.
@@ -376,7 +381,7 @@ struct PrefixSums {
     const int64_t* tile0;
     const int32_t* row_group;  // [num_rows] -1: none
     int32_t num_groups, ctas, num_rows;
-    int32_t row_blocks;        // blocks of attend_finish to a row
+    int32_t row_warps;         // warps of attend_finish to a row
 };
 // Adds the prefix's sums of a row (of a kv head's, from the first of the sequence) to j: every step-th part from `first` on.
 template <int D, class B>
@@ -444,8 +449,8 @@ __device__ __forceinline__ void finish_cut(const AttendParams<SharedBatch>& p, i
         if ((alone || warp == 0) && lane < kLanes) write_row<T, D>(p, q, cut.h, cut.m * R + r, lane * 4, j);
     }
 }
-// The end of both passes: what was cut of the sequences', with the prefixes' sums where there are any; then x.row_blocks blocks to a row
-// for the rows with a prefix whose own tokens were not cut, a warp to a query head.  Bound by four or five loads one after the other.
+// The end of both passes: what was cut of the sequences', with the prefixes' sums where there are any; then x.row_warps warps to a row
+// for the rows with a prefix whose own tokens were not cut, a query head at a time.  Bound by four or five loads one after the other.
 template <class T, int D>
 __global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_constant__ AttendParams<SharedBatch> few, int few_ctas,
                                                               const __grid_constant__ AttendParams<SharedBatch> many, int many_ctas,
@@ -455,17 +460,19 @@ __global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_const
     auto prefix = [&](const Seq& q, int kv_head, int row, int first, int step, Joined& j) {
         if (q.first > 0) add_prefix<D>(few, x, q.group, q, kv_head, row, first, step, j);
     };
-    const int many_groups = kManyRows / kJoinRows<1, SharedBatch>;
+    const int many_groups = kManyRows / kJoinRows<1>;
     int block = blockIdx.x;
     if (block < few_ctas) return finish_cut<T, D>(few, few_ctas, block, prefix);
     block -= few_ctas;
     if (block < many_ctas * many_groups) return join_rows<T, D, 1>(many, many_ctas, block, many_groups, prefix);
     block -= many_ctas * many_groups;
-    const int row = block / x.row_blocks, g = x.row_group[row], lane = threadIdx.x % 32;
+    const int64_t warp = (int64_t)block * kJoinWarps + threadIdx.x / 32;
+    const int row = (int)(warp / x.row_warps), first = (int)(warp - (int64_t)row * x.row_warps), stride = x.row_warps;
+    const int lane = threadIdx.x % 32, half = lane / kLanes, d = lane % kLanes * 4;
+    const int g = row < x.num_rows ? x.row_group[row] : -1;
     if (g < 0) return;
-    const int half = lane / kLanes, d = lane % kLanes * 4, stride = x.row_blocks * kJoinWarps;
     constexpr int kHeads = 4;  // of a warp at a time, so that the loads of their own sums overlap
-    for (int head0 = block % x.row_blocks * kJoinWarps + (int)threadIdx.x / 32; head0 < few.q_heads; head0 += kHeads * stride) {
+    for (int head0 = first; head0 < few.q_heads; head0 += kHeads * stride) {
         float l[kHeads], m[kHeads];
         float4 o[kHeads];
 #pragma unroll
@@ -524,8 +531,8 @@ static amoeba_status run_few(AttendParams<B>& p, int sms, int* ctas, cudaStream_
     p.shape.start = kUnitStart;
     if (ensure_dynamic_smem((const void*)attend_few<T, D, NT, B>, F::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
     *ctas = std::min(F::kCtas * sms, kMaxFewCtas);
-    return launch_kernel(attend_few<T, D, NT, B>, p.whole ? p.batch.num_seqs * p.shape.kv_heads + p.batch.check_blocks() : *ctas, kFewThreads,
-                         F::kSmem, stream, B::kShared, p);
+    return launch_kernel(attend_few<T, D, NT, B>, (p.whole ? p.batch.num_seqs * p.shape.kv_heads : *ctas) + p.batch.check_blocks(),
+                         kFewThreads, F::kSmem, stream, B::kShared, p);
 }
 
 // The launches of a pass, and what is left for the join behind them.
@@ -534,7 +541,7 @@ struct Pass {
     AttendParams<B> few, many;
     int few_ctas = 0, few_rows = 0, many_ctas = 0;
     bool cuts = false;  // something may be cut
-    int many_blocks() const { return many_ctas * (kManyRows / kJoinRows<1, B>); }
+    int many_blocks() const { return many_ctas * (kManyRows / kJoinRows<1>); }
 };
 
 // Sequences with few rows (new tokens times query heads per key head) are read by attend_few, whose time is that of reading
@@ -686,17 +693,26 @@ struct PrefixParams {
     int32_t *row_group, *status;
     int32_t num_groups, max_group_rows, block_tokens;
     int32_t kv_heads, group;  // query heads per key head
+    int32_t sms, few_cost;    // few_cost: of a tile of attend_few
 };
 
 // What a group shares: no more than its shortest sequence has in front of its new tokens, and nothing where fewer than two have
 // rows, one is bad, or it does not pay; then its sequences attend by themselves.  One block, a warp to a group.
 //
-// Whether it pays is counted in tiles of 128 tokens (a tile of a sequence with few rows costs about as much as one of 256 rows): every
-// tile of rows reads the prefix, of each sequence by itself or of the group's rows together; a group's unit costs its start and end, about
-// four tiles, and joining its sums with the sequences' half a tile for a few rows, six for 256.
+// Whether it pays is counted in what 128 rows of attend_many cost over 128 tokens, 1650 clocks: every tile of the prefix costs 1 for up to
+// 128 rows of a sequence, 2 for up to 256, and 2 where the rows are few and it is the reading that counts, 4 where attend_few has 32.  A tile of the group's
+// rows costs 5 to start and end, joining its sums with a sequence's 1 for few rows and 5 for 128; and the launches for all groups
+// together as much as 28 on every SM, 25 us.  (2 groups of up to 5 sequences, 74 new tokens each behind up to 946: 89 us shared, 74 not; two of 7,
+// 230 new tokens behind 9000: 610 and 605.)
 constexpr int kPrefixThreads = 1024, kPrefixWarps = kPrefixThreads / 32;
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_constant__ PrefixParams p) {
+    struct Plan {
+        Group group;
+        int32_t first, end;  // sequences
+    };
+    __shared__ Plan s_plan[kPrefixThreads];
     __shared__ int64_t s_tiles[kPrefixThreads], s_warp[kPrefixWarps];
+    __shared__ unsigned long long s_gain;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.batch.num_seqs, G = p.num_groups;
     grid_dependency_launch();
     grid_dependency_wait();
@@ -706,25 +722,39 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_
     if (!in_order && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
     int64_t run = 0;
     for (int base = 0; base < G; base += kPrefixThreads) {
-        for (int g = base + warp; g < min(G, base + kPrefixThreads); g += kPrefixWarps) {
-            Group out{0, 0, 0, 0};
-            int64_t tiles = 0;
+        const int end = min(G, base + kPrefixThreads);
+        if (tid == 0) s_gain = 0;
+        __syncthreads();
+        for (int g = base + warp; g < end; g += kPrefixWarps) {
+            Plan out{{0, 0, 0, 0}, 0, 0};
             if (in_order) {
-                const GroupSums x = sum_group(p.batch, p.group_starts, g, p.block_tokens, p.group);
+                const GroupSums x = sum_group(p.batch, p.group_starts, g, p.block_tokens, p.group, p.few_cost);
                 const int given = p.prefix_lens[g], len = min(given, x.least), key_tiles = (len - 1) / kManyTile + 1;
                 const bool wrong = refused(x, given, p.max_group_rows);
                 if (wrong && lane == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
                 if (!wrong && x.ok && x.with_rows > 1 && len > 0) {
-                    const int row_tiles = (int)(((int64_t)(x.q1 - x.q0) * p.group - 1) / kManyRows) + 1;
-                    if (2 * (int64_t)(x.alone - row_tiles) * key_tiles > 8 * (int64_t)row_tiles + x.taking) {
-                        out = Group{x.q0, x.q1 - x.q0, len, x.row};
-                        tiles = (int64_t)p.kv_heads * row_tiles * key_tiles;
-                        for (int s = x.first + lane; s < x.end; s += 32) p.own[s] = make_int2(len, g);
-                        for (int r = x.q0 + lane; r < x.q1; r += 32) p.row_group[r] = g;
+                    const int rows = (x.q1 - x.q0) * p.group, row_tiles = (rows - 1) / kManyRows + 1;
+                    const int64_t gain = (int64_t)(x.alone - rows_cost(rows)) * key_tiles - 5 * row_tiles - x.taking;
+                    if (gain > 0) {
+                        out = Plan{{x.q0, x.q1 - x.q0, len, x.row}, x.first, x.end};
+                        if (lane == 0) atomicAdd(&s_gain, (unsigned long long)(gain * p.kv_heads));
                     }
                 }
             }
-            if (lane == 0) p.groups[g] = out, s_tiles[g - base] = tiles;
+            if (lane == 0) s_plan[g - base] = out;
+        }
+        __syncthreads();
+        const bool pays = s_gain > 28ull * p.sms;
+        for (int g = base + warp; g < end; g += kPrefixWarps) {
+            Plan x = s_plan[g - base];
+            if (!pays) x.group.qn = x.group.len = 0;
+            int64_t tiles = 0;
+            if (x.group.len > 0) {
+                for (int s = x.first + lane; s < x.end; s += 32) p.own[s] = make_int2(x.group.len, g);
+                for (int r = lane; r < x.group.qn; r += 32) p.row_group[x.group.q0 + r] = g;
+                tiles = (int64_t)p.kv_heads * ((x.group.qn * p.group - 1) / kManyRows + 1) * ((x.group.len - 1) / kManyTile + 1);
+            }
+            if (lane == 0) p.groups[g] = x.group, s_tiles[g - base] = tiles;
         }
         __syncthreads();
         // the first tile of every group
@@ -788,10 +818,13 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     p.whole = not_cut(p, sms);
     p.batch.group_starts = prefixes->d_group_starts, p.batch.prefix_lens = prefixes->d_prefix_lens;
     p.batch.num_groups = prefixes->num_groups, p.batch.max_group_rows = group_rows;
-    // Where all sequences together have less to read than the launches for the groups would take (a tile takes an SM about 1.5 us; 8
-    // sequences of 160 tokens: 13.6 us with them, 8 without), they attend by themselves, and the groups' numbers are only checked.
+    // Where all sequences by themselves take less than the launches for the groups would, they attend by themselves, and the groups' numbers
+    // are only checked.  A tile of 128 tokens takes an SM about 1.5 us, twice that with 17 to 32 rows, 1.7 us for 256 (8 sequences of 160
+    // tokens: 13.6 us with the launches, 5.5 without; 8 of up to 950 tokens, 32 key heads: 24.5 and 17).
+    const int64_t rows = rows_of(layout, p.batch.max_q_len);
+    const int few_cost = rows > 16 && rows <= kMaxFewRows ? 4 : 2;
     const int64_t tiles = ((int64_t)p.batch.max_blocks * p.cache.block_tokens + kManyTile - 1) / kManyTile;
-    if (p.whole && (int64_t)p.batch.num_seqs * p.shape.kv_heads * tiles <= 8 * sms) {
+    if ((int64_t)p.batch.num_seqs * p.shape.kv_heads * std::max<int64_t>(few_cost, (rows + 127) / 128) * tiles <= 32 * sms) {
         if ((st = run_pass<T, D>(p, layout->tp, dtype, ws + at.rest_pass, sms, stream, &rest)) != AMOEBA_OK) return st;
         return run_join<T, D>(rest, stream);
     }
@@ -802,7 +835,7 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     x.own = reinterpret_cast<int2*>(ws + at.own), x.row_group = reinterpret_cast<int32_t*>(ws + at.row_group);
     x.status = p.status;
     x.num_groups = prefixes->num_groups, x.max_group_rows = group_rows, x.block_tokens = layout->block_tokens;
-    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group;
+    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group, x.sms = sms, x.few_cost = few_cost;
     if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, true, x)) != AMOEBA_OK) return st;
     p.batch.own = x.own;
     sums_space(layout, p.batch.num_rows, ws + at.rest_sums, &p.sums);
@@ -826,9 +859,9 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     }
     sums.groups = x.groups, sums.tile0 = x.tile0, sums.row_group = x.row_group;
     sums.num_groups = prefixes->num_groups, sums.num_rows = p.batch.num_rows;
-    // Enough blocks for a head to a warp, unless there are rows enough to fill the GPU as it is.
-    sums.row_blocks = p.batch.num_rows >= 1024 ? 1 : (p.q_heads + kJoinWarps - 1) / kJoinWarps;
-    const int64_t grid = rest.few_ctas + rest.many_blocks() + (int64_t)sums.num_rows * sums.row_blocks;
+    // A warp to a head, unless there are rows enough to fill the GPU as it is.
+    sums.row_warps = p.batch.num_rows >= 1024 ? 1 : p.q_heads;
+    const int64_t grid = rest.few_ctas + rest.many_blocks() + ((int64_t)sums.num_rows * sums.row_warps + kJoinWarps - 1) / kJoinWarps;
     if (grid > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
     return launch_kernel(attend_finish<T, D>, (int)grid, kJoinThreads, 0, stream, true, rest.few, rest.few_ctas, rest.many, rest.many_ctas, sums);
 }

@@ -28,7 +28,7 @@ struct Batch {
     const int32_t *table, *lens, *starts;
     int32_t num_seqs, max_blocks, num_rows, max_q_len;
     __host__ __device__ bool by_groups() const { return false; }
-    int check_blocks() const { return 0; }
+    __host__ __device__ int check_blocks() const { return 0; }
 };
 
 // The rows of all sequences of a group, over the tokens [0, len) that these have in common; row: of the block table.
@@ -46,7 +46,7 @@ struct SharedBatch : Batch {
     const int32_t *group_starts, *prefix_lens;
     int32_t num_groups, max_group_rows;
     __host__ __device__ bool by_groups() const { return groups != nullptr; }
-    int check_blocks() const { return !own && !groups; }  // blocks beside a launch's own that check the groups' numbers
+    __host__ __device__ int check_blocks() const { return !own && !groups; }  // blocks beside a launch's own that check the groups' numbers
 };
 
 // Cached tokens of a sequence at most: their indices, rounded up to tiles and blocks or moved by a window, stay below 2^31.

@@ -207,7 +207,7 @@ struct ShareBorder {
 };
 template <int kThreads, class B>
 __device__ void take_weighted_share(const Shape& p, const B& b, int block_tokens, Walk* walk, int64_t* begin_out, int64_t* end_out,
-                                    int32_t* status, char* scratch) {
+                                    int32_t* status, char* scratch, int most_ctas) {
     constexpr int kWarps = kThreads / 32;
     int64_t* const s_warp = reinterpret_cast<int64_t*>(scratch);  // [2][kWarps]
     ShareBorder* const border = reinterpret_cast<ShareBorder*>(s_warp + 2 * kWarps);
@@ -223,7 +223,7 @@ __device__ void take_weighted_share(const Shape& p, const B& b, int block_tokens
         sums[0] += tiles, sums[1] += weight;
     }
     const int64_t all_tiles = block_sum<kThreads>(sums[0], s_warp), all = block_sum<kThreads>(sums[1], s_warp + kWarps);
-    const int ctas = (int)max((int64_t)1, min((int64_t)gridDim.x, all_tiles));
+    const int ctas = (int)max((int64_t)1, min((int64_t)most_ctas, all_tiles));
     const int c = min((int)blockIdx.x, ctas);
     const int64_t at[2] = {share_begin(all, ctas, c), share_begin(all, ctas, min(c + 1, ctas))};
     int64_t run_tiles = 0, run = 0;
