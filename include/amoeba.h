@@ -597,23 +597,25 @@ AMOEBA_API amoeba_status amoeba_evict_kv(const amoeba_layout* layout, int32_t la
  * amoeba_attend_shared
  *
  * amoeba_attend (without a window) for sequences that share prefixes: group g is the sequences d_group_starts[g] ...
- * d_group_starts[g + 1] - 1 of the batch, whose caches hold the same first d_prefix_lens[g] tokens - in the same blocks or in
- * copies: the prefix is read once for the group, through the block table of its first sequence with rows, and not looked at in the
- * others' blocks.  Which tokens are the same is the caller's to know; a length need not be a multiple of block_tokens.  The results
- * are amoeba_attend's but for the order of the sums.
+ * d_group_starts[g + 1] - 1 of the batch, whose caches hold the same first d_prefix_lens[g] tokens, in the same blocks or in
+ * copies.  Which tokens are the same is the caller's to know; a length need not be a multiple of block_tokens.  Where it pays, or
+ * `always` is 1, the prefix is read once for the group, through the block table of its first sequence with rows; where it does not, every
+ * sequence's own.  The results are amoeba_attend's but for the order of the sums.
  * A group shares at most as many tokens as its shortest sequence has cached in front of its new ones.  It shares nothing, and its
  * sequences attend by themselves, if fewer than two have rows, if one is bad (reported as by amoeba_attend), if d_prefix_lens[g] is
  * negative or if it has more than max_group_rows rows (INVALID_ARG is reported).  So do sequences in front of the first group and
  * behind the last, and all of them if d_group_starts decreases or leaves [0, num_seqs] (INVALID_ARG).
- * The rows of the prefix's bad blocks are left out for the whole group.
- * d_workspace: amoeba_attend_shared_workspace_bytes(...) bytes, as in amoeba_attend; it grows with num_rows (32-bit sums of every row and
- * query head).
+ * Bad blocks of a prefix that is shared are left out for the whole group.
+ * d_workspace: amoeba_attend_shared_workspace_bytes(...) bytes, as in amoeba_attend; it grows with num_rows by 8 * (head_dim + 2) bytes for
+ * each row and query head.
  */
 typedef struct {
     const int32_t* d_group_starts; /* [num_groups + 1] sequences */
     const int32_t* d_prefix_lens;  /* [num_groups] tokens */
     int32_t num_groups;
     int32_t max_group_rows;        /* no group has more new tokens than this (it sizes the launch) */
+    int32_t always;                /* 1: groups are shared whether it pays or not */
+    int32_t reserved;
 } amoeba_prefixes;
 AMOEBA_API amoeba_status amoeba_attend_shared_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
                                                    const amoeba_prefixes* prefixes, int64_t* bytes);
@@ -650,7 +652,7 @@ AMOEBA_API amoeba_status amoeba_attend_shared(const amoeba_layout* layout, int32
  * pairs_cap.  BAD_BLOCK_ID: a block id outside the pool, or one counted 0, that was to be shared, copied or given back; such an id
  * is shared as it is, its pair's source is -1, and nothing is counted for it.  One code is reported, the first of these in this order.
  * What is in the counts is the caller's to keep right: with wrong ones blocks may be handed out twice.
- * TOO_LARGE: 20 bytes for each sequence and 0.26 for every eighth of the pool's blocks do not fit in the 201 KiB of shared memory that
+ * UNSUPPORTED: more than 2^30 table entries or rows.  TOO_LARGE: 20 bytes for each sequence and 0.26 for every eighth of the pool's blocks do not fit in the 201 KiB of shared memory that
  * there are for them (10 000 sequences with 30 000 blocks, 1 000 with 5 million).
  */
 typedef struct {

@@ -87,7 +87,7 @@ class Batch(C.Structure):
 
 class Prefixes(C.Structure):
     _fields_ = [("d_group_starts", C.c_void_p), ("d_prefix_lens", C.c_void_p), ("num_groups", C.c_int32),
-                ("max_group_rows", C.c_int32)]
+                ("max_group_rows", C.c_int32), ("always", C.c_int32), ("reserved", C.c_int32)]
 
 
 class TableStep(C.Structure):
@@ -621,15 +621,15 @@ def amoeba_evict_kv(layout: Layout, layer_begin: int, layer_end: int, pools: Seq
           dst_bt, budget, recent, new_lens, status, workspace, _handle(stream))
 
 
-def make_prefixes(group_starts, prefix_lens, max_group_rows: int) -> Prefixes:
+def make_prefixes(group_starts, prefix_lens, max_group_rows: int, always: bool = False) -> Prefixes:
     """What groups of a batch's sequences share: group g is the sequences group_starts[g] .. group_starts[g + 1] - 1 (int32
-    [groups + 1]) and shares its first prefix_lens[g] tokens (int32 [groups]); max_group_rows: no group has more new tokens.
-    Keeps the tensors."""
+    [groups + 1]) and shares its first prefix_lens[g] tokens (int32 [groups]); max_group_rows: no group has more new tokens;
+    always: share whether it pays or not.  Keeps the tensors."""
     import torch
 
     dev, G = prefix_lens.device, prefix_lens.numel()
     x = Prefixes(_tensor(group_starts, "make_prefixes", torch.int32, G + 1, dev), _tensor(prefix_lens, "make_prefixes", torch.int32, G, dev),
-                 G, max_group_rows)
+                 G, max_group_rows, int(always), 0)
     x.index = dev.index if dev.type == "cuda" else -1
     x.address, x.keep = C.addressof(x), (group_starts, prefix_lens)
     return x

@@ -435,6 +435,8 @@ extern "C" amoeba_status amoeba_advance_tables(const amoeba_layout* layout, cons
     if (a.d_first_positions && !a.d_positions) return AMOEBA_ERR_INVALID_ARG;
     if (a.pairs_cap && (!a.d_pairs || !a.d_num_pairs)) return AMOEBA_ERR_INVALID_ARG;
     if ((uintptr_t)a.d_pairs % 8 || (uintptr_t)a.d_slots % 8) return AMOEBA_ERR_ALIGNMENT;
+    // (entries and rows are numbered in 32 bits, and counted on past the last one)
+    if ((int64_t)a.num_seqs * a.max_blocks_per_seq > (1 << 30) || a.num_rows > (1 << 30)) return AMOEBA_ERR_UNSUPPORTED;
     StepParams p{};
     p.table = a.d_block_table, p.refs = a.d_block_refs;
     p.lens = a.d_seq_lens, p.new_lens = a.d_new_lens, p.parents = a.d_parents, p.shared = a.d_shared_lens;

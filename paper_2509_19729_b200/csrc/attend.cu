@@ -694,6 +694,7 @@ struct PrefixParams {
     int32_t num_groups, max_group_rows, block_tokens;
     int32_t kv_heads, group;  // query heads per key head
     int32_t sms, few_cost;    // few_cost: of a tile of attend_few
+    int32_t always;
 };
 
 // What a group shares: no more than its shortest sequence has in front of its new tokens, and nothing where fewer than two have
@@ -735,16 +736,16 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_
                 if (!wrong && x.ok && x.with_rows > 1 && len > 0) {
                     const int rows = (x.q1 - x.q0) * p.group, row_tiles = (rows - 1) / kManyRows + 1;
                     const int64_t gain = (int64_t)(x.alone - rows_cost(rows)) * key_tiles - 5 * row_tiles - x.taking;
-                    if (gain > 0) {
+                    if (gain > 0 || p.always) {
                         out = Plan{{x.q0, x.q1 - x.q0, len, x.row}, x.first, x.end};
-                        if (lane == 0) atomicAdd(&s_gain, (unsigned long long)(gain * p.kv_heads));
+                        if (lane == 0 && gain > 0) atomicAdd(&s_gain, (unsigned long long)(gain * p.kv_heads));
                     }
                 }
             }
             if (lane == 0) s_plan[g - base] = out;
         }
         __syncthreads();
-        const bool pays = s_gain > 28ull * p.sms;
+        const bool pays = p.always || s_gain > 28ull * p.sms;
         for (int g = base + warp; g < end; g += kPrefixWarps) {
             Plan x = s_plan[g - base];
             if (!pays) x.group.qn = x.group.len = 0;
@@ -824,7 +825,7 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     const int64_t rows = rows_of(layout, p.batch.max_q_len);
     const int few_cost = rows > 16 && rows <= kMaxFewRows ? 4 : 2;
     const int64_t tiles = ((int64_t)p.batch.max_blocks * p.cache.block_tokens + kManyTile - 1) / kManyTile;
-    if ((int64_t)p.batch.num_seqs * p.shape.kv_heads * std::max<int64_t>(few_cost, (rows + 127) / 128) * tiles <= 32 * sms) {
+    if (!prefixes->always && (int64_t)p.batch.num_seqs * p.shape.kv_heads * std::max<int64_t>(few_cost, (rows + 127) / 128) * tiles <= 32 * sms) {
         if ((st = run_pass<T, D>(p, layout->tp, dtype, ws + at.rest_pass, sms, stream, &rest)) != AMOEBA_OK) return st;
         return run_join<T, D>(rest, stream);
     }
@@ -835,7 +836,7 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     x.own = reinterpret_cast<int2*>(ws + at.own), x.row_group = reinterpret_cast<int32_t*>(ws + at.row_group);
     x.status = p.status;
     x.num_groups = prefixes->num_groups, x.max_group_rows = group_rows, x.block_tokens = layout->block_tokens;
-    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group, x.sms = sms, x.few_cost = few_cost;
+    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group, x.sms = sms, x.few_cost = few_cost, x.always = prefixes->always;
     if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, true, x)) != AMOEBA_OK) return st;
     p.batch.own = x.own;
     sums_space(layout, p.batch.num_rows, ws + at.rest_sums, &p.sums);
@@ -888,6 +889,7 @@ extern "C" amoeba_status amoeba_attend_shared(const amoeba_layout* layout, int32
     int64_t need = 0;
     if ((st = amoeba_attend_shared_workspace_bytes(layout, batch, prefixes, &need)) != AMOEBA_OK) return st;
     if (prefixes->num_groups && (!prefixes->d_group_starts || !prefixes->d_prefix_lens)) return AMOEBA_ERR_INVALID_ARG;
+    if (prefixes->always != 0 && prefixes->always != 1) return AMOEBA_ERR_INVALID_ARG;
     if (!d_workspace || workspace_bytes < need) return AMOEBA_ERR_INVALID_ARG;
     if ((uintptr_t)d_workspace % 16) return AMOEBA_ERR_ALIGNMENT;
     if (p.batch.num_seqs == 0 || p.batch.num_rows == 0) return AMOEBA_OK;

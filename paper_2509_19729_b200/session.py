@@ -354,8 +354,11 @@ class CacheSession:
 
     dtype: "fp16" or "bf16"; kv_layers: layers the pools hold (None = all); scores: hold score pools too.  set_tables()
     and set_rows() describe the batch of a step; the row buffers q, k, v, out are the caller's, one tensor per worker.
+    Or the tables are kept on the GPU: advance() takes the sequences to new lengths, with blocks that block_refs counts, and describes
+    the step's batch; copy_forks() then copies the blocks that forks begin inside.  attend_shared() is attend() for sequences whose
+    prefixes set_prefixes() names.
     All calls share one workspace, so they run one after another, on one stream or on streams that wait for each other;
-    set_tables() and set_rows() work on the current stream."""
+    set_tables(), set_rows(), set_prefixes() and advance()'s host arguments work on the current stream."""
 
     def __init__(self, model: dict, tp: int, NB: int, num_seqs: int, max_blocks_per_seq: int, dtype: str = "bf16",
                  kv_layers: Optional[int] = None, block_tokens: int = 16, kv_order: int = A.KV_HEAD_MAJOR,
@@ -374,6 +377,13 @@ class CacheSession:
         self.seq_lens = torch.zeros(num_seqs, **i32)
         self.new_lens = torch.zeros(num_seqs, **i32)
         self.q_starts = torch.zeros(num_seqs + 1, **i32)
+        self.block_refs = torch.zeros(NB, **i32)  # table entries that name a block
+        self.next_lens = torch.zeros(num_seqs, **i32)
+        self.parents, self.shared_lens = torch.full((num_seqs,), -1, **i32), torch.zeros(num_seqs, **i32)
+        self.positions, self.slots = torch.empty(0, **i32), torch.empty(0, dtype=torch.int64, device=dev)
+        self.copies, self.num_copies = torch.full((num_seqs, 2), -1, **i32), torch.zeros(1, **i32)
+        self.free_blocks = torch.zeros(1, **i32)
+        self.prefixes = None
         self.status = torch.zeros(1, **i32)
         self.workspace, self._outgrown = torch.empty(0, dtype=torch.uint8, device=dev), []
         self.set_rows(None, num_seqs, 1)
@@ -382,6 +392,14 @@ class CacheSession:
         self.seq_lens.copy_(torch.as_tensor(seq_lens, dtype=torch.int32))
         self.block_table.copy_(torch.as_tensor(block_table, dtype=torch.int32))
 
+    def count_blocks(self) -> None:
+        """Counts anew which blocks the tables name: after tables that come from elsewhere (set_tables, a transformation, an eviction),
+        in front of advance()."""
+        T = self.layout.block_tokens
+        column = torch.arange(self.block_table.shape[1], device=self.device)
+        named = self.block_table[column < ((self.seq_lens + T - 1) // T)[:, None]].long()
+        self.block_refs.copy_(torch.bincount(named, minlength=self.block_refs.numel()))
+
     def set_rows(self, q_starts, num_rows: int, max_q_len: int) -> None:
         """q_starts: first row of every sequence's new tokens and the end, or None for one token each."""
         if q_starts is not None:
@@ -389,6 +407,44 @@ class CacheSession:
         self.batch = A.make_batch(self.block_table, self.seq_lens, None if q_starts is None else self.q_starts, num_rows,
                                   max_q_len)
         self._room(A.amoeba_attend_workspace_bytes(self.layout, self.batch))
+
+    def set_prefixes(self, group_starts, prefix_lens, max_group_rows: int, always: bool = False) -> None:
+        """Group g, the sequences group_starts[g] .. group_starts[g + 1] - 1, shares its first prefix_lens[g] tokens; max_group_rows:
+        no group has more new tokens; always: share whether it pays or not.  Of the batch that is described now."""
+        as_i32 = lambda x: torch.as_tensor(x, dtype=torch.int32).to(self.device)  # noqa: E731
+        self._outgrown.append(self.prefixes)  # (captured calls may still read them)
+        self.prefixes = A.make_prefixes(as_i32(group_starts), as_i32(prefix_lens), max_group_rows, always)
+
+    def advance(self, new_lens, num_rows: int, max_q_len: int, parents=None, shared_lens=None, first_positions=None, stream=None) -> None:
+        """Takes the sequences from seq_lens to new_lens: blocks are handed out, given back (shorter lengths; 0: finished) and shared
+        (parents[s] >= 0: sequence s begins with the first shared_lens[s] tokens of that one).  Afterwards seq_lens has what they
+        have, and the batch is that of the new tokens, with positions and slots; free_blocks is what is left.  num_rows,
+        max_q_len: no more new tokens in all and of a sequence."""
+        self.next_lens.copy_(torch.as_tensor(new_lens, dtype=torch.int32))
+        forks = parents is not None
+        if forks:
+            self.parents.copy_(torch.as_tensor(parents, dtype=torch.int32))
+            self.shared_lens.copy_(torch.as_tensor(shared_lens, dtype=torch.int32))
+        if self.positions.numel() < num_rows:
+            self._outgrown += [self.positions, self.slots]
+            with _on(stream, self.device):
+                self.positions = torch.empty(num_rows, dtype=torch.int32, device=self.device)
+                self.slots = torch.empty(num_rows, dtype=torch.int64, device=self.device)
+        A.amoeba_advance_tables(self.layout, self.block_table, self.block_refs, self.seq_lens, self.next_lens, self.parents if forks else None,
+                                self.shared_lens if forks else None, self.seq_lens, self.q_starts, num_rows, first_positions,
+                                self.positions, self.slots, self.copies, self.num_copies, self.free_blocks, self.status, stream)
+        self.batch = A.make_batch(self.block_table, self.seq_lens, self.q_starts, num_rows, max_q_len)
+        self._room(A.amoeba_attend_workspace_bytes(self.layout, self.batch), stream)
+
+    def copy_forks(self, layer_begin: int = 0, layer_end: Optional[int] = None, stream=None) -> None:
+        """The copies that the last advance() asked for; in front of append()."""
+        A.amoeba_copy_blocks(self.layout, self.pools, self.copies, self.num_copies, layer_begin,
+                             self.kv_layers if layer_end is None else layer_end, self.status, stream)
+
+    def attend_shared(self, layer: int, q, out, lse=None, scale: Optional[float] = None, stream=None) -> None:
+        self._room(A.amoeba_attend_shared_workspace_bytes(self.layout, self.batch, self.prefixes), stream)
+        A.amoeba_attend_shared(self.layout, self.dtype, layer, self.pools, self.batch, self.prefixes, q,
+                               self.model["D"] ** -0.5 if scale is None else scale, out, lse, self.status, self.workspace, stream)
 
     def _room(self, nbytes: int, stream=None) -> None:
         """A workspace of nbytes, for calls on `stream` (None: the current one) and on what waits for it."""

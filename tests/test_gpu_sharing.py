@@ -253,14 +253,14 @@ class Case:
         self.scale = D ** -0.5
         self.layout = A().make_layout(self.m, tp, self.NB, T, kv_order=order)
 
-    def up(self, max_group_rows=None):
+    def up(self, always=True, max_group_rows=None):
         a = A()
         self.dpools = [p.to(DEV) for p in self.cache.pools]
         self.dq = [x.contiguous().flatten(1) for x in self.q.to(DEV).chunk(self.tp, 1)]
         self.batch = a.make_batch(dev(self.bt), dev(self.lens), dev(self.starts), self.rows, int(max(1, self.qlens.max(initial=1))))
         gs, S = self.group_starts.clip(0, len(self.lens)), self.starts
         most = int((S[gs[1:]] - S[gs[:-1]]).max(initial=0)) if max_group_rows is None else max_group_rows
-        self.prefixes = a.make_prefixes(dev(self.group_starts), dev(self.prefix), most)
+        self.prefixes = a.make_prefixes(dev(self.group_starts), dev(self.prefix), most, always)
         self.status = torch.zeros(1, dtype=torch.int32, device=DEV)
         self.ws = torch.full((a.amoeba_attend_shared_workspace_bytes(self.layout, self.batch, self.prefixes),), 0x7F, dtype=torch.uint8, device=DEV)
         self.out = [torch.full((self.rows, x.shape[1]), 7.0, dtype=DT[self.dtype], device=DEV) for x in self.dq]
@@ -303,10 +303,11 @@ HEADS = [(4, 4, 64, 1), (4, 2, 128, 2), (12, 4, 64, 2), (8, 1, 128, 1), (16, 1, 
 @pytest.mark.parametrize("Hq,Hkv,D,tp", HEADS)
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("order", [0, 1])
-def test_single_tokens_behind_a_prefix(Hq, Hkv, D, tp, dtype, order):
+@pytest.mark.parametrize("always", [True, False])
+def test_single_tokens_behind_a_prefix(Hq, Hkv, D, tp, dtype, order, always):
     own = [(n, 1) for n in (1, 2, 15, 16, 17, 63, 65, 1)]
     Case([(70, own), (1, own[:2]), (129, own[3:])], Hq, Hkv, D, tp, order=order, dtype=dtype, lead=[(33, 1)], loose=[(5, 1), (90, 1)],
-         seed=Hq).up().run().check()
+         seed=Hq).up(always).run().check()
 
 
 @pytest.mark.parametrize("T", [1, 5, 8, 16, 24, 64, 100, 256])
@@ -320,3 +321,236 @@ def test_block_sizes(T, D, order):
 @pytest.mark.parametrize("members,q", [(2, 1), (9, 1), (40, 1), (3, 5), (2, 70), (5, 130)])
 def test_prefix_lengths(prefix, members, q):
     Case([(prefix, [(q + s % 3, q) for s in range(members)])], 8, 2, 128, dtype="fp16", seed=prefix, extra_rows=2).up().run().check()
+
+
+def test_a_group_shares_no_more_than_its_shortest_sequence_has():
+    """A prefix that reaches into the new tokens of some sequence, or behind its end."""
+    for given in (40, 64, 200, 2 ** 31 - 1):
+        c = Case([(40, [(1 + s, 1) for s in range(30)] + [(60, 50)])], 8, 2, 128)
+        c.prefix[0] = given
+        c.up().run().check()
+
+
+def test_a_group_through_its_first_sequence_with_rows():
+    """Sequences without new tokens, empty ones in front among them, are in the way of nothing."""
+    c = Case([(300, [(0, 0), (9, 0)] + [(5 + s % 7, 1) for s in range(50)] + [(2, 0)])], 4, 2, 64)
+    c.lens[c.group_starts[0]] = 0
+    c.up().run().check()
+
+
+@pytest.mark.parametrize("members,q", [(40, 1), (3, 70)])
+def test_what_nobody_sees_may_be_anything(members, q):
+    """NaN in free blocks, behind the last tokens and, as the prefix is read through the first sequence's table, in the others' copies of
+    the block that it ends in."""
+    c = Case([(150, [(q + 3 + s % 9, q) for s in range(members)])], 8, 4, 128, spare=5, seed=q)
+    used = np.zeros((c.NB, c.T), bool)
+    for s, n in enumerate(c.lens):
+        for i in range(int(n)):
+            if i >= 150 or s == 0:  # the first sequence's table is the group's
+                used[c.bt[s, i // c.T], i % c.T] = True
+    c.up()
+    for p, mine in zip(c.cache.pools, c.dpools):
+        mine[:] = torch.where(torch.from_numpy(used)[None, :, None, None, :, None], p, float("nan")).to(DEV)
+    c.run().check()
+
+
+@pytest.mark.parametrize("members", [6, 50])
+@pytest.mark.parametrize("where", ["prefix", "own"])
+@pytest.mark.parametrize("always", [True, False])
+def test_bad_blocks_of_a_prefix_and_of_a_sequence(members, where, always):
+    c = Case([(600, [(40 + s % 5, 1) for s in range(members)])], 16, 4, 128)
+    if where == "prefix":
+        c.bt[:, [0, 7, 30]] = [-1, c.NB, 2 ** 31 - 1]
+    else:
+        c.bt[2, 38], c.bt[5, 39] = -5, c.NB
+    c.up(always).run().check(status=share.BAD_BLOCK_ID)
+
+
+@pytest.mark.parametrize("members", [3, 40])
+@pytest.mark.parametrize("always", [True, False])
+def test_bad_groups_attend_by_themselves(members, always):
+    def case():
+        return Case([(150, [(3 + s % 4, 1) for s in range(members)]), (210, [(2, 1)] * members)], 4, 2, 128, lead=[(9, 1)], loose=[(30, 2)])
+
+    n = 2 * members + 2
+    for starts in ([1, members + 1, members], [-1, members + 1, n], [1, members + 1, n + 1], [5, 3, n], [2 ** 31 - 1, 0, 1]):
+        c = case()
+        c.group_starts[:] = starts
+        c.up(always, 99).run().check(status=share.INVALID_ARG)
+    c = case()
+    c.prefix[0] = -1
+    c.up(always).run().check(status=share.INVALID_ARG)
+    case().up(always, members - 1).run().check(status=share.INVALID_ARG)
+    case().up(always, 0).run().check(status=share.INVALID_ARG)
+
+
+@pytest.mark.parametrize("members,q", [(40, 1), (3, 90)])
+@pytest.mark.parametrize("always", [True, False])
+def test_bad_sequences_of_a_group_are_left_out(members, q, always):
+    c = Case([(500, [(q + s % 4, q) for s in range(members)]), (300, [(q, q)] * members)], 8, 2, 128, extra_rows=1)
+    c.up(always)
+    lens = c.lens.copy()
+    lens[1], lens[members + 2] = -1, c.bt.shape[1] * c.T + 1
+    c.batch.keep[1].copy_(dev(lens))
+    c.run().check(status=share.INVALID_ARG, left_out=(1, members + 2))
+
+
+@pytest.mark.parametrize("always", [True, False])
+def test_groups_beyond_what_a_block_plans_at_once(always):
+    """1100 groups of two."""
+    Case([(33, [(2, 1), (1 + k % 3, 1)]) for k in range(1100)], 2, 1, 64, T=8).up(always).run().check()
+
+
+def test_what_pays_is_shared_and_what_does_not_is_not():
+    """One group worth it beside one of two short sequences, by what is read: the others' copies of the block that the prefix ends in
+    hold other values."""
+    c = Case([(1500, [(2 + s % 5, 1) for s in range(60)]), (40, [(3, 1), (4, 1)])], 8, 8, 128, seed=2)
+    for s in range(1, 60):  # (in the oracle's tables too: they name the first sequence's block, as far as the prefix goes)
+        for p in c.cache.pools:
+            p[:, int(c.bt[s, 93]), :, :, :1500 % 16] = 5.0
+    c.up(False).run()
+    want = c.bt.copy()
+    got, _ = c.result()
+    alone = Case([(1500, [(2 + s % 5, 1) for s in range(60)]), (40, [(3, 1), (4, 1)])], 8, 8, 128, seed=2).up(False).run()
+    same, _ = alone.result()
+    assert np.array_equal(got, same) and np.array_equal(want, c.bt)  # what differs is not read
+
+
+@pytest.mark.parametrize("members,prefix", [(40, 700), (6, 9000), (120, 150)])
+def test_the_same_call_gives_the_same_bits(members, prefix):
+    c = Case([(prefix, [(5 + s % 30, 1) for s in range(members)])], 16, 2, 128).up().run()
+    first = [x.clone() for x in c.out] + [c.lse.clone()]
+    for _ in range(3):
+        c.ws.fill_(0x7F)
+        c.run()
+        assert all(torch.equal(a, b) for a, b in zip(first, c.out + [c.lse]))
+
+
+def test_without_lse_and_in_wider_rows():
+    c = Case([(300, [(4, 1)] * 40)], 8, 4, 128, tp=2).up().run()
+    want = [x.clone() for x in c.out]
+    wide = [torch.full((c.rows, 1024), 7.0, dtype=DT[c.dtype], device=DEV) for _ in range(2)]
+    for w, x in zip(wide, c.dq):
+        w[:, :512] = x
+    A().amoeba_attend_shared(c.layout, code(c.dtype), 0, c.dpools, c.batch, c.prefixes, [w[:, :512] for w in wide], c.scale,
+                             [w[:, 512:] for w in wide], None, c.status, c.ws)
+    for w, x, y in zip(wide, c.dq, want):
+        assert torch.equal(w[:, 512:], y) and torch.equal(w[:, :512], x)
+
+
+def test_long_prefix_and_one_long_rest():
+    """A rest that is cut into many parts beside short ones."""
+    Case([(5000, [(3, 1)] * 20 + [(6000, 1)] + [(1, 1)] * 12)], 8, 1, 128, seed=3).up().run().check()
+
+
+def test_two_streams_at_once():
+    cases = [Case([(400 + 100 * k, [(9, 1)] * 40)], 8, 2, 128, seed=k).up() for k in range(2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, st in zip(cases, streams):
+            c.run(st)
+    for c in cases:
+        c.check()
+
+
+def test_captured_calls_follow_lengths_and_groups():
+    """A step of tables, copies and attention is captured once and replayed as the sequences grow."""
+    c = Case([(320, [(8, 1)] * 30), (64, [(8, 1)] * 10)], 8, 2, 128).up().run()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            c.run()
+    for own, prefix in ((3, (320, 64)), (8, (17, 0)), (5, (0, 60)), (8, (300, 63))):
+        lens = np.concatenate([np.full(30, 320 + own), np.full(10, 64 + own)]).astype(np.int32)
+        c.lens[:] = lens
+        c.batch.keep[1].copy_(dev(lens))
+        c.prefixes.keep[1].copy_(dev(prefix))
+        for o in c.out:
+            o.fill_(7.0)
+        torch.cuda.synchronize()
+        g.replay()
+        c.check()
+
+
+# ---------------------------------------------------------------------------------------------------- a run of them
+
+@pytest.mark.parametrize("order,tp", [(0, 1), (1, 2)])
+def test_answers_to_prompts(order, tp):
+    """Prompts come in, are forked inside a block, answers grow and end, blocks come back: captured and replayed, the attention by groups
+    the same as by sequences, and the same as over a cache that nothing shares."""
+    from paper_2509_19729_b200.session import CacheSession
+
+    m, T, S, NB, dt = model(8, 4, 64, 2), 16, 24, 300, torch.bfloat16
+    s = CacheSession(m, tp, NB, S, 20, block_tokens=T, kv_order=order)
+    flat = CacheSession(m, tp, S * 20, S, 20, block_tokens=T, kv_order=order)  # sequence b has blocks 20 b ...
+    flat.block_table.copy_(torch.arange(S * 20, device=DEV).view(S, 20))
+    g = torch.Generator(device=DEV).manual_seed(order)
+    randn = lambda *n: torch.randn(*n, generator=g, device=DEV).to(dt)  # noqa: E731
+    workers = lambda x: list(x.chunk(tp, 1))  # noqa: E731
+    keys = [[[None] * 320 for _ in range(S)] for _ in range(2)]  # what every sequence should hold
+    lens = np.zeros(S, int)
+
+    def step(new, rows, longest, groups=None, prefix=None, parents=None, shared=None):
+        s.advance(new, rows, longest, parents, shared)
+        s.copy_forks()
+        torch.cuda.synchronize()
+        assert int(s.status.item()) == 0
+        starts, now = s.q_starts.tolist(), s.seq_lens.tolist()
+        assert now == list(new)
+        k, v, q = randn(rows, 256), randn(rows, 256), randn(rows, 512)
+        for layer in range(2):
+            s.append(layer, None, workers(k), workers(v), None, None)
+        for b in range(S):
+            if parents is not None and parents[b] >= 0:
+                for x in keys:
+                    x[b][:shared[b]] = x[parents[b]][:shared[b]]
+            for j, r in enumerate(range(starts[b], starts[b + 1])):
+                i = now[b] - (starts[b + 1] - starts[b]) + j
+                keys[0][b][i], keys[1][b][i] = k[r], v[r]
+                assert int(s.positions[r]) == i
+        if groups is None:
+            return
+        s.set_prefixes(groups, prefix, rows, always=True)
+        shared_out, alone = ([torch.empty(rows, 512 // tp, dtype=dt, device=DEV) for _ in range(tp)] for _ in range(2))
+        s.attend_shared(1, workers(q.clone()), shared_out)
+        s.attend(1, workers(q.clone()), alone)
+        # the flat cache: every sequence's tokens anew
+        flat.set_tables(now, flat.block_table.cpu())
+        flat.set_rows(np.concatenate([[0], np.cumsum(now)]), int(sum(now)), max(now))
+        kk = torch.stack([keys[0][b][i] for b in range(S) for i in range(now[b])])
+        vv = torch.stack([keys[1][b][i] for b in range(S) for i in range(now[b])])
+        flat.append(1, None, workers(kk), workers(vv), None, None)
+        flat.set_rows(starts, rows, longest)
+        third = [torch.empty_like(x) for x in alone]
+        flat.attend(1, workers(q.clone()), third)
+        torch.cuda.synchronize()
+        assert int(s.status.item()) == 0 and int(flat.status.item()) == 0
+        n = starts[-1]
+        for a, b, c in zip(shared_out, alone, third):
+            assert torch.equal(b[:n], c[:n])  # the same tokens, read in the same order
+            # both are within half a step of bf16 twice (weights and outputs) of the same value, which is an average of the values
+            bound = 4 * 2.0 ** -8 * (c[:n].float().abs() + vv.float().abs().max())
+            assert ((a[:n].float() - c[:n].float()).abs() <= bound).all()
+
+    new = lens.copy()
+    new[[0, 10]] = 200, 77
+    step(new, 300, 200)
+    parents, shared = np.full(S, -1), np.zeros(S, int)
+    parents[1:10], shared[1:10] = 0, 150 + np.arange(9)
+    parents[11:20], shared[11:20] = 10, 77
+    lens = new.copy()
+    new = lens + 1
+    new[1:10], new[11:20] = shared[1:10] + 2, 78 + np.arange(9) % 3
+    new[20:] = 0
+    step(new, 60, 3, [0, 10, 20], [150, 77], parents, shared)
+    for k in range(20):
+        new = new + (new > 0)
+        step(new, 24, 1, [0, 10, 20], [150, 77])
+    left = int(s.free_blocks.item())
+    held = s.block_refs.clone()
+    s.count_blocks()
+    assert torch.equal(s.block_refs, held) and left == int((held == 0).sum())
+    step(np.zeros(S, int), 0, 1)
+    assert int(s.free_blocks.item()) == NB and (s.block_refs == 0).all() and (s.block_table == -1).all()
