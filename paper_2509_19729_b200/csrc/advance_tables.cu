@@ -23,7 +23,8 @@ struct StepParams {
     int32_t num_seqs, max_blocks, num_rows, pairs_cap, num_blocks, block_tokens;
     int32_t shift;          // block_tokens = 2^shift, or -1
     int32_t max_len;        // tokens that a row of the table has room for
-    int32_t tiles;          // of kTileBlocks blocks, in the pool
+    int32_t tiles;          // in the pool (large launches)
+    int32_t words;          // of 32 blocks, of a CTA (others)
 
     __device__ __forceinline__ int whole(int tokens) const { return shift >= 0 ? tokens >> shift : tokens / block_tokens; }
     __device__ __forceinline__ int blocks_of(int tokens) const { return whole(tokens + block_tokens - 1); }
@@ -35,33 +36,34 @@ constexpr int kStepCluster = 16;   // CTAs
 constexpr uint32_t kBadArg = 1, kBadBlock = 2;
 
 // In dynamic shared memory: sums over the sequences in front of every one, and at [num_seqs] over all; then what the CTA knows of
-// its tiles, every size-th of the pool's.  A tile has a word of 32 blocks for each warp.
+// its part of the pool.  In large launches that is every size-th tile, which has a word of 32 blocks for each warp, so that all CTAs have
+// blocks to hand out; in others a run of words, no more than there are threads.
 struct StepShared {
     int32_t* sums[4];   // blocks, rows, copies; entries of the table that are shared with a parent's or given back
     int32_t* first;     // cache index of the first new token; -1: refused
-    int32_t* count;     // free blocks of a tile,
-    int32_t* start;     // and of all tiles of the pool in front of it
-    uint32_t* free;     // [warps] a tile: the free blocks' bits
-    int32_t* before;    // [warps] a tile: free blocks of the tile in front of a word
+    uint32_t* free;     // the free blocks' bits, by words
+    int32_t* before;    // free blocks in front of a word, of its tile or of the CTA
+    int32_t* count;     // of a tile: free blocks in it,
+    int32_t* start;     // and in all tiles of the pool in front of it
 
-    __device__ __forceinline__ StepShared(char* smem, const StepParams& p, int tiles, int warps) {
+    __device__ __forceinline__ StepShared(char* smem, const StepParams& p, int words, int tiles) {
         const int n = p.num_seqs + 1;
         sums[0] = reinterpret_cast<int32_t*>(smem);
         sums[1] = sums[0] + n, sums[2] = sums[1] + n, sums[3] = sums[2] + n, first = sums[3] + n;
-        count = first + n, start = count + tiles;
-        free = reinterpret_cast<uint32_t*>(start + tiles);
-        before = reinterpret_cast<int32_t*>(free + warps * tiles);
+        free = reinterpret_cast<uint32_t*>(first + n);
+        before = reinterpret_cast<int32_t*>(free + words);
+        count = before + words, start = count + tiles;
     }
 };
-static int64_t step_smem(int64_t num_seqs, int64_t tiles, int warps) { return (5 * (num_seqs + 1) + (2 + 2 * warps) * tiles) * 4; }
+static int64_t step_smem(int64_t num_seqs, int64_t words, int64_t tiles) { return (5 * (num_seqs + 1) + 2 * words + 2 * tiles) * 4; }
 constexpr int kStepStatic = 26 * 1024;  // bytes of shared memory beside those
 
-// What a sequence asks for.  The loads come in two steps, so that others can be started in between.
+// What a sequence asks for.  The loads come in three steps, so that others can be started in between.
 struct Need {
     int32_t blocks = 0, rows = 0, copies = 0, entries = 0, first = -1;
 };
 struct Ask {
-    int32_t old = 0, now = 0, parent = -1, share = 0, from = 0, last = -1;
+    int32_t old = 0, now = 0, parent = -1, share = 0, from = 0, last = -1, count = 0;
     bool ok = false;
 
     __device__ __forceinline__ void lengths(const StepParams& p, int s) {
@@ -73,6 +75,9 @@ struct Ask {
         if (!ok) return;
         if (parent >= 0) share = p.shared[s], from = p.lens[parent];
         else if (now > old && p.whole(old) * p.block_tokens != old) last = p.table[(int64_t)s * p.max_blocks + p.whole(old)];
+    }
+    __device__ __forceinline__ void counts(const StepParams& p) {
+        if (p.inside(last)) count = p.refs[last];
     }
     __device__ __forceinline__ Need need(const StepParams& p, uint32_t* bad) const {
         Need n;
@@ -91,7 +96,6 @@ struct Ask {
             // The last block is not full: a fork gets a copy of its parent's, and a sequence one of a block that others name too.
             n.copies = parent >= 0;
             if (parent < 0 && now > old) {
-                const int count = p.inside(last) ? p.refs[last] : 0;
                 if (count < 1) *bad |= kBadBlock;
                 n.copies = count > 1;
             }
@@ -125,7 +129,7 @@ __device__ __forceinline__ void step_sync(uint32_t size) {
 // Sums over the block in front of every thread of N values a thread, none above 2^31 - 1; total: of all.  Only the first `busy` warps
 // have any.  shared: [N][32], not in use since the last barrier.
 template <int N, int kWarps>
-__device__ __forceinline__ void sum_before(uint32_t (&v)[N], uint32_t (&total)[N], uint32_t (*shared)[32], int busy) {
+__device__ __forceinline__ void sum_before(uint32_t* v, uint32_t* total, uint32_t (*shared)[32], int busy) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (warp < busy) {
 #pragma unroll
@@ -175,15 +179,17 @@ template <int kThreads>
 __global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_constant__ StepParams p) {
     constexpr int kWarps = kThreads / 32;
     extern __shared__ __align__(16) char smem[];
-    __shared__ uint32_t s_sum[4][32];
+    constexpr bool kLarge = kThreads == kStepMost;
+    __shared__ uint32_t s_sum[5][32];
     __shared__ Handed s_block[kWarps][32];
-    __shared__ int32_t s_freed;
+    __shared__ int32_t s_freed, s_count;
     __shared__ uint32_t s_bad;
     __shared__ int32_t s_all_bad[kStepCluster], s_all_freed[kStepCluster];  // in the first CTA
     const uint32_t rank = cluster_rank(), size = cluster_size();
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.num_seqs, T = p.block_tokens;
-    const int tiles = (p.tiles + (int)size - 1) / (int)size;  // of this CTA; the last may lie behind the pool
-    const StepShared sh(smem, p, tiles, kWarps);
+    const int tiles = kLarge ? (p.tiles + (int)size - 1) / (int)size : 0;  // of this CTA; the last may lie behind the pool
+    const int words = kLarge ? tiles * kWarps : p.words;
+    const StepShared sh(smem, p, words, tiles);
     const int32_t *const blocks = sh.sums[0], *const rows = sh.sums[1], *const copied = sh.sums[2], *const entries = sh.sums[3];
     if (tid == 0) s_freed = 0, s_bad = 0;
     grid_dependency_launch();
@@ -192,76 +198,93 @@ __global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_const
     // ---- the free blocks, and what the first sequences ask for
     Ask ask;
     if (tid < S) ask.lengths(p, tid);
-    auto first_block = [&](int tile) { return ((uint32_t)tile * size + rank) * kThreads + warp * 32; };  // of this warp's word
-    constexpr int kAtOnce = kThreads == kStepMost ? 16 : 8;
-    for (int t0 = 0; t0 < tiles || t0 == 0; t0 += kAtOnce) {
+    // First block of this warp's i-th word, the (warp + i * kWarps)-th of the CTA.
+    const uint32_t step = (kLarge ? size : 1) * kThreads, own_block = kLarge ? rank * kThreads + warp * 32 : (rank * p.words + warp) * 32;
+    auto first_block = [&](int i) { return own_block + (uint32_t)i * step; };
+    const int own_words = kLarge ? tiles : (words - warp + kWarps - 1) / kWarps;
+    constexpr int kAtOnce = 16;
+    for (int i0 = 0; i0 < own_words || i0 == 0; i0 += kAtOnce) {
         int count[kAtOnce];  // loaded without a question, so that the loads overlap
-        const uint32_t b0 = first_block(t0) + lane, step = size * kThreads, last = (uint32_t)p.num_blocks - 1;
+        const uint32_t b0 = first_block(i0) + lane, last = (uint32_t)p.num_blocks - 1;
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) count[i] = p.refs[min(b0 + i * step, last)];
-        if (t0 == 0 && tid < S) ask.more(p, tid);
+        if (i0 == 0 && tid < S) ask.more(p, tid), ask.counts(p);
         uint32_t mine = 0;  // lane i keeps word i
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
             const uint32_t word = __ballot_sync(~0u, count[i] == 0 && b0 + i * step <= last);
             if (lane == i) mine = word;
         }
-        if (lane < min(kAtOnce, tiles - t0)) sh.free[(t0 + lane) * kWarps + warp] = mine;
+        if (lane < min(kAtOnce, own_words - i0)) sh.free[(i0 + lane) * kWarps + warp] = mine;
     }
+    if (!kLarge) __syncthreads();
 
-    // ---- the sums in front of every sequence
+    // ---- the sums in front of every sequence (and, in launches that are not large, of every word)
     uint32_t bad = 0, run[4] = {0, 0, 0, 0};
-    for (int base = 0; base < S; base += kThreads) {
+    for (int base = 0; base < S || base == 0; base += kThreads) {
         const int s = base + tid;
         Need n;
         if (s < S) {
+            Ask a = ask;
             if (base > 0) {
-                ask = Ask();
-                ask.lengths(p, s);
-                ask.more(p, s);
+                a = Ask();
+                a.lengths(p, s), a.more(p, s), a.counts(p);
             }
-            n = ask.need(p, &bad);
+            n = a.need(p, &bad);
             sh.first[s] = n.first;
         }
-        uint32_t v[4] = {(uint32_t)n.blocks, (uint32_t)n.rows, (uint32_t)n.copies, (uint32_t)n.entries}, total[4];
+        uint32_t v[5] = {(uint32_t)n.blocks, (uint32_t)n.rows, (uint32_t)n.copies, (uint32_t)n.entries, 0}, total[5];
+        const bool counts = !kLarge && base == 0;
+        if (counts && tid < words) v[4] = __popc(sh.free[tid]);
         if (base > 0) __syncthreads();
-        sum_before<4, kWarps>(v, total, s_sum, min(kWarps, (S - base + 31) / 32));
+        sum_before<kLarge ? 4 : 5, kWarps>(v, total, s_sum, min(kWarps, (max(S - base, counts ? words : 1) + 31) / 32));
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (s < S) sh.sums[k][s] = (int32_t)add_up(run[k], v[k]);
             run[k] = add_up(run[k], total[k]);
         }
+        if (counts && tid < words) sh.before[tid] = (int32_t)v[4];
+        if (counts && tid == 0) s_count = (int32_t)total[4];
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
         if (tid == 0) sh.sums[k][S] = (int32_t)run[k];
     if (bad) atomicOr(&s_bad, bad);
-    __syncthreads();
-    for (int t = warp; t < tiles; t += kWarps) {  // words of a tile
-        const int own = lane < kWarps ? __popc(sh.free[t * kWarps + lane]) : 0;
-        int sum = own;
+    if (kLarge) {
+        __syncthreads();
+        for (int t = warp; t < tiles; t += kWarps) {  // words of a tile
+            const int own = __popc(sh.free[t * kWarps + lane]);
+            int sum = own;
 #pragma unroll
-        for (int o = 1; o < kWarps; o *= 2) {
-            const int up = __shfl_up_sync(~0u, sum, o);
-            if (lane >= o) sum += up;
+            for (int o = 1; o < 32; o *= 2) {
+                const int up = __shfl_up_sync(~0u, sum, o);
+                if (lane >= o) sum += up;
+            }
+            sh.before[t * kWarps + lane] = sum - own;
+            if (lane == 31) sh.count[t] = sum;
         }
-        if (lane < kWarps) sh.before[t * kWarps + lane] = sum - own;
-        if (lane == kWarps - 1) sh.count[t] = sum;
     }
     step_sync(size);
 
-    // ---- the tiles of all CTAs, and who gets what: the sequences in front of the first that does not fit
+    // ---- the free blocks of all CTAs, and who gets what: the sequences in front of the first that does not fit
     uint32_t n_free = 0;
-    for (int base = 0; base < p.tiles; base += kThreads) {
-        const int t = base + tid;
-        uint32_t v[1] = {t >= p.tiles ? 0u : (uint32_t)(size > 1 ? load_remote(&sh.count[(uint32_t)t / size], (uint32_t)t % size) : sh.count[t])}, total[1];
-        if (base > 0) __syncthreads();
-        sum_before<1, kWarps>(v, total, s_sum, min(kWarps, (p.tiles - base + 31) / 32));
-        if (t < p.tiles && (uint32_t)t % size == rank) sh.start[(uint32_t)t / size] = (int32_t)(n_free + v[0]);
-        n_free += total[0];
+    int in_front = 0;  // free blocks in front of this CTA's run of words
+    if (kLarge) {
+        for (int base = 0; base < p.tiles; base += kThreads) {
+            const int t = base + tid;
+            uint32_t v[1] = {t >= p.tiles ? 0u : (uint32_t)load_remote(&sh.count[(uint32_t)t / size], (uint32_t)t % size)}, total[1];
+            if (base > 0) __syncthreads();
+            sum_before<1, kWarps>(v, total, s_sum, min(kWarps, (p.tiles - base + 31) / 32));
+            if (t < p.tiles && (uint32_t)t % size == rank) sh.start[(uint32_t)t / size] = (int32_t)(n_free + v[0]);
+            n_free += total[0];
+        }
+        for (int t = tid; t < tiles; t += kThreads)
+            if ((int64_t)t * size + rank >= p.tiles) sh.start[t] = INT32_MAX;
+    } else {
+        const int own = lane >= (int)size ? 0 : size > 1 ? load_remote(&s_count, lane) : s_count;
+        n_free = __reduce_add_sync(~0u, (uint32_t)own);
+        in_front = (int)__reduce_add_sync(~0u, lane < (int)rank ? (uint32_t)own : 0u);
     }
-    for (int t = tid; t < tiles; t += kThreads)
-        if ((int64_t)t * size + rank >= p.tiles) sh.start[t] = INT32_MAX;
     // No CTA ends while another reads its counts: the barrier that all arrive at here, or behind the reads of other sequences' rows.
     const bool reads_others = p.parents || p.pairs_cap > 0;
     if (size > 1 && !reads_others) cluster_arrive();
@@ -319,13 +342,15 @@ __global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_const
         if (p.slots) p.slots[row] = slot;
     };
     auto end_of = [&](int s) { return sh.first[s] + rows[s + 1] - rows[s]; };
-    for (int t = 0; t < tiles && sh.start[t] < n_taken; ++t) {
-        const uint32_t word = sh.free[t * kWarps + warp];
-        const int r0 = sh.start[t] + sh.before[t * kWarps + warp], n = min(__popc(word), n_taken - r0);
+    for (int i = 0; i < own_words; ++i) {
+        const int w = i * kWarps + warp, front = kLarge ? sh.start[i] : in_front;
+        if (front >= n_taken) break;
+        const uint32_t word = sh.free[w];
+        const int r0 = front + sh.before[w], n = min(__popc(word), n_taken - r0);
         const int k = __popc(word & ((1u << lane) - 1)), r = r0 + k;
         if (n <= 0) continue;
         if (word >> lane & 1u && k < n) {
-            const int b = (int)(first_block(t) + lane), s = last_at_most(blocks, fits, r), j = r - blocks[s], first = sh.first[s];
+            const int b = (int)(first_block(i) + lane), s = last_at_most(blocks, fits, r), j = r - blocks[s], first = sh.first[s];
             const bool copy = copies(s);
             const int column = (copy ? p.whole(first) : p.blocks_of(first)) + j;
             p.table[(int64_t)s * p.max_blocks + column] = b;
@@ -359,16 +384,19 @@ __global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_const
     }
 
     // ---- lengths, row starts, and the rows in blocks that were there: what is left of a last block
-    for (int base = (warp * size + rank) * 32; base <= S; base += all) {
+    for (int base = warp * 32; base <= S; base += kThreads) {
         const int s = base + lane;
+        if (base / 32 % (int)size != (int)rank) continue;
         Handed x{0, 0, 0, 0, 0};
         if (s < S) {
-            const int old = p.lens[s], now = p.new_lens[s], first = sh.first[s];
-            const bool grows = now > old || parent_of(s) >= 0, stays = first < 0 || (grows && s >= fits);
+            Ask a = ask;  // (of the first sequences)
+            if (base >= kThreads) a.lengths(p, s);
+            const int old = a.old, now = a.now, first = sh.first[s];
+            const bool grows = now > old || a.parent >= 0, stays = first < 0 || (grows && s >= fits);
             p.lens_out[s] = stays ? old : now;
             const int n = stays ? 0 : p.whole(first);
             if (writes_rows && !stays && n * T != first && !copies(s) && rows[s + 1] > rows[s]) {
-                const int b = p.table[(int64_t)s * p.max_blocks + n];
+                const int b = base >= kThreads ? p.table[(int64_t)s * p.max_blocks + n] : a.last;
                 x = Handed{p.inside(b) ? ((int64_t)b - n) * T : kNoSlot, first, (int)min((int64_t)end_of(s), ((int64_t)n + 1) * T), rows[s] - first,
                            p.first_pos ? p.first_pos[s] - first : 0};
                 if (T < 128)
@@ -450,11 +478,12 @@ extern "C" amoeba_status amoeba_advance_tables(const amoeba_layout* layout, cons
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
     // A few sequences and blocks are soonest done by one small CTA; then a cluster's loads and stores count, then its bytes.
-    const bool large = p.num_blocks > 131072 || p.num_seqs > 512 || p.num_rows > 8192;
+    const bool large = p.num_blocks > 65536 || p.num_seqs > 512 || p.num_rows > 8192;
     const bool small = p.num_blocks <= 8192 && p.num_seqs <= 256 && p.num_rows <= 1024;
     const int cluster = small ? 1 : large ? kStepCluster : kMaxCluster, threads = large ? kStepMost : 256;
-    p.tiles = (int32_t)(((int64_t)p.num_blocks + threads - 1) / threads);
-    const int64_t smem = step_smem(p.num_seqs, (p.tiles + cluster - 1) / cluster, threads / 32);
+    p.tiles = large ? (int32_t)(((int64_t)p.num_blocks + threads - 1) / threads) : 0;
+    p.words = large ? 0 : (p.num_blocks + 32 * cluster - 1) / (32 * cluster);
+    const int64_t tiles = (p.tiles + cluster - 1) / cluster, smem = step_smem(p.num_seqs, large ? tiles * (threads / 32) : p.words, tiles);
     if (smem > dev.smem_optin - kStepStatic) return AMOEBA_ERR_TOO_LARGE;
     if (large && allow_large_clusters((const void*)advance_tables<kStepMost>) != cudaSuccess) return AMOEBA_ERR_CUDA;
     return launch_clusters(large ? advance_tables<kStepMost> : advance_tables<256>, cluster, threads, (size_t)smem, cluster, true,
