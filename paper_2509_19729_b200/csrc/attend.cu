@@ -106,8 +106,7 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
     Walk walk{};
     int64_t n;
     if constexpr (B::kShared) {
-        // The groups are there.  (Their own pass comes behind the sequences', whose blocks have all waited for them.)
-        if (!p.batch.by_groups()) grid_dependency_wait();
+        if (p.batch.waits) grid_dependency_wait();
         if (p.batch.check_blocks() && blockIdx.x == gridDim.x - 1) return check_groups(p);
     }
     if (p.whole) {
@@ -119,7 +118,7 @@ attend_few(const __grid_constant__ AttendParams<B> p) {
         int64_t begin, end;
         if constexpr (B::kShared)
             take_weighted_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status, smem,
-                                             gridDim.x - p.batch.check_blocks());
+                                             p.batch.split && !p.batch.by_groups() ? __ldcg(p.batch.split + 1) : (int)gridDim.x - p.batch.check_blocks());
         else
             take_share<kFewThreads>(sh, p.batch, p.cache.block_tokens, &walk, &begin, &end, p.status);
         write_cut(sh, p.cuts, walk, begin, end);
@@ -374,13 +373,14 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constan
     else join_rows<T, D, 1>(many, many_ctas, block, kManyRows / kJoinRows<1>, none);
 }
 
-// What the groups' pass has left: sums of whole rows, and where it was attend_many's (`ctas` of them) the parts of its cut units.
+// What the groups' pass has left: sums of whole rows, and where it was attend_many's the parts of its cut units.
 struct PrefixSums {
     Sums rows, parts;
     const Group* groups;
     const int64_t* tile0;
     const int32_t* row_group;  // [num_rows] -1: none
-    int32_t num_groups, ctas, num_rows;
+    const int32_t* split;      // where the groups' pass was attend_many's: its CTAs
+    int32_t num_groups, num_rows;
     int32_t row_warps;         // warps of attend_finish to a row
 };
 // Adds the prefix's sums of a row (of a kv head's, from the first of the sequence) to j: every step-th part from `first` on.
@@ -388,9 +388,10 @@ template <int D, class B>
 __device__ __forceinline__ void add_prefix(const AttendParams<B>& p, const PrefixSums& x, int g, const Seq& q, int kv_head, int row, int first, int step,
                                            Joined& j) {
     const int d = (int)threadIdx.x % 32 % (D / 4) * 4, tok = row / p.shape.group;
-    if (x.ctas > 0) {
+    if (x.split) {
+        const int ctas = __ldcg(x.split);
         const int4 group = __ldcg(reinterpret_cast<const int4*>(x.groups + g));
-        const int64_t total = __ldcg(x.tile0 + x.num_groups), even = divide(total + x.ctas - 1, x.ctas);
+        const int64_t total = __ldcg(x.tile0 + x.num_groups), even = divide(total + ctas - 1, ctas);
         const int tiles = (group.z - 1) / kManyTile + 1, row_tiles = (int)(((int64_t)group.y * p.shape.group - 1) / kManyRows) + 1;
         const int in_group = (q.q0 - group.x) * p.shape.group + row, m = in_group / kManyRows, r = in_group % kManyRows;
         const int64_t begin = __ldcg(x.tile0 + g) + ((int64_t)kv_head * row_tiles + m) * tiles;
@@ -690,11 +691,13 @@ struct PrefixParams {
     Group* groups;
     int64_t* tile0;
     int2* own;
-    int32_t *row_group, *status;
+    int32_t *row_group, *split, *status;
     int32_t num_groups, max_group_rows, block_tokens;
     int32_t kv_heads, group;  // query heads per key head
     int32_t sms, few_cost;    // few_cost: of a tile of attend_few
     int32_t always;
+    int32_t tile_bytes;       // keys and values of 64 tokens and a key head
+    int32_t few_ctas;         // to an SM, of the sequences' pass; 0: the passes do not run side by side
 };
 
 // What a group shares: no more than its shortest sequence has in front of its new tokens, and nothing where fewer than two have
@@ -705,6 +708,14 @@ struct PrefixParams {
 // rows costs 5 to start and end, joining its sums with a sequence's 1 for few rows and 5 for 128; and the launches for all groups
 // together as much as 28 on every SM, 25 us.  (2 groups of up to 5 sequences, 74 new tokens each behind up to 946: 89 us shared, 74 not; two of 7,
 // 230 new tokens behind 9000: 610 and 605.)
+//
+// The two passes run side by side where the sequences' is attend_few's, whose time is that of reading: the groups' CTAs, one to an SM, take
+// long to start and are bound by their products, and would leave the memory idle in front of it and behind.  The SMs are shared out
+// by the clocks that each is known to take: a tile of 128 tokens and 256 rows 3300, of up to 128 rows 2600, a unit's begin and end 20 000
+// beside the other pass, the kernel's 35 000; a tile of 64 tokens of attend_few 1000 (two CTAs to an SM), but all together no less than
+// 6.3 TB/s.  (128 sequences behind 8192 tokens: 142 us one after the other, 120 with 32 SMs for the group, 129 with 24 or 48; chosen: 28.)
+constexpr int kTileClocks = 3300, kTurnClocks = 2600, kSwitchClocks = 20000, kFewClocks = 1000;
+constexpr float kStartClocks = 35000.f, kBytesPerClock = 3300.f;
 constexpr int kPrefixThreads = 1024, kPrefixWarps = kPrefixThreads / 32;
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_constant__ PrefixParams p) {
     struct Plan {
@@ -713,12 +724,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_
     };
     __shared__ Plan s_plan[kPrefixThreads];
     __shared__ int64_t s_tiles[kPrefixThreads], s_warp[kPrefixWarps];
-    __shared__ unsigned long long s_gain;
+    __shared__ unsigned long long s_gain, s_groups, s_rest, s_tiles64;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, S = p.batch.num_seqs, G = p.num_groups;
     grid_dependency_launch();
     grid_dependency_wait();
     for (int s = tid; s < S; s += kPrefixThreads) p.own[s] = make_int2(0, -1);
     for (int r = tid; r < p.batch.num_rows; r += kPrefixThreads) p.row_group[r] = -1;
+    if (tid == 0) s_groups = s_rest = s_tiles64 = 0;
     const bool in_order = groups_in_order(p.group_starts, G, S);
     if (!in_order && tid == 0) report(p.status, AMOEBA_ERR_INVALID_ARG);
     int64_t run = 0;
@@ -753,7 +765,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_
             if (x.group.len > 0) {
                 for (int s = x.first + lane; s < x.end; s += 32) p.own[s] = make_int2(x.group.len, g);
                 for (int r = lane; r < x.group.qn; r += 32) p.row_group[x.group.q0 + r] = g;
-                tiles = (int64_t)p.kv_heads * ((x.group.qn * p.group - 1) / kManyRows + 1) * ((x.group.len - 1) / kManyTile + 1);
+                const int rows = x.group.qn * p.group, units = p.kv_heads * ((rows - 1) / kManyRows + 1);
+                tiles = (int64_t)units * ((x.group.len - 1) / kManyTile + 1);
+                if (lane == 0) atomicAdd(&s_groups, (unsigned long long)(tiles * (rows > 128 ? kTileClocks : kTurnClocks) + units * (int64_t)kSwitchClocks));
             }
             if (lane == 0) p.groups[g] = x.group, s_tiles[g - base] = tiles;
         }
@@ -780,11 +794,44 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_groups(const __grid_
         __syncthreads();
     }
     if (tid == 0) p.tile0[G] = run;
+    if (!p.few_ctas) {
+        if (tid == 0) p.split[0] = p.sms, p.split[1] = 0;
+        return;
+    }
+    // How many SMs the groups' pass gets, so that both end together.
+    unsigned long long clocks = 0, tiles64 = 0;
+    for (int s = tid; s < S; s += kPrefixThreads) {
+        const Seq q = sequence(p.batch, s, p.block_tokens);
+        if (q.qn == 0) continue;
+        const int64_t n = (int64_t)p.kv_heads * ((q.len - p.own[s].x + 63) / 64);
+        clocks += (n + kUnitStart * p.kv_heads) * kFewClocks, tiles64 += n;
+    }
+    if (warp * 32 < S) {
+#pragma unroll
+        for (int o = 16; o; o /= 2) clocks += __shfl_xor_sync(~0u, clocks, o), tiles64 += __shfl_xor_sync(~0u, tiles64, o);
+        if (lane == 0) atomicAdd(&s_rest, clocks), atomicAdd(&s_tiles64, tiles64);
+    }
+    __syncthreads();
+    if (warp) return;
+    const float groups = (float)s_groups, rest = (float)s_rest, reading = (float)s_tiles64 * p.tile_bytes / kBytesPerClock;
+    float best = INFINITY;
+    int sms = 0;
+    for (int m = 1 + lane; groups > 0.f && m < p.sms; m += 32) {
+        const float t = fmaxf(kStartClocks + groups / m, fmaxf(rest / (p.sms - m), reading));
+        if (t < best) best = t, sms = m;
+    }
+#pragma unroll
+    for (int o = 16; o; o /= 2) {
+        const float t = __shfl_xor_sync(~0u, best, o);
+        const int m = __shfl_xor_sync(~0u, sms, o);
+        if (t < best || (t == best && m < sms)) best = t, sms = m;
+    }
+    if (lane == 0) p.split[0] = sms, p.split[1] = (p.sms - sms) * p.few_ctas;
 }
 
 // Where the parts of the workspace begin: both passes' own, the carry, the groups and the sequences' first tokens.
 struct SharedSpace {
-    int64_t groups_pass, rest_pass, group_sums, rest_sums, groups, tile0, own, row_group, end;
+    int64_t groups_pass, rest_pass, group_sums, rest_sums, groups, tile0, own, row_group, split, end;
 };
 // Sums of all rows and query heads.
 static int64_t sums_space(const amoeba_layout* l, int64_t rows, char* ws, Sums* out) {
@@ -805,7 +852,8 @@ static SharedSpace shared_space(const amoeba_layout* l, const amoeba_batch* b, c
     s.tile0 = s.groups + (int64_t)x->num_groups * sizeof(Group);
     s.own = s.tile0 + ((int64_t)x->num_groups / 2 + 1) * 16;
     s.row_group = s.own + ints(2 * (int64_t)b->num_seqs);
-    s.end = s.row_group + ints(b->num_rows);
+    s.split = s.row_group + ints(b->num_rows);
+    s.end = s.split + 16;
     return s;
 }
 
@@ -819,6 +867,7 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     p.whole = not_cut(p, sms);
     p.batch.group_starts = prefixes->d_group_starts, p.batch.prefix_lens = prefixes->d_prefix_lens;
     p.batch.num_groups = prefixes->num_groups, p.batch.max_group_rows = group_rows;
+    p.batch.waits = 1;
     // Where all sequences by themselves take less than the launches for the groups would, they attend by themselves, and the groups' numbers
     // are only checked.  A tile of 128 tokens takes an SM about 1.5 us, twice that with 17 to 32 rows, 1.7 us for 256 (8 sequences of 160
     // tokens: 13.6 us with the launches, 5.5 without; 8 of up to 950 tokens, 32 key heads: 24.5 and 17).
@@ -836,27 +885,38 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     x.own = reinterpret_cast<int2*>(ws + at.own), x.row_group = reinterpret_cast<int32_t*>(ws + at.row_group);
     x.status = p.status;
     x.num_groups = prefixes->num_groups, x.max_group_rows = group_rows, x.block_tokens = layout->block_tokens;
-    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group, x.sms = sms, x.few_cost = few_cost, x.always = prefixes->always;
+    x.kv_heads = p.shape.kv_heads, x.group = p.shape.group, x.sms = std::min(sms, kMaxSms), x.few_cost = few_cost, x.always = prefixes->always;
+    x.split = reinterpret_cast<int32_t*>(ws + at.split);
+    // Side by side: groups of attend_many, sequences of attend_few alone.
+    const bool many_groups = prefixes->num_groups && rows_of(layout, group_rows) > kMaxGroupRows, side_by_side = many_groups && rows <= kMaxFewRows;
+    const int few_ctas = rows <= 8 ? FewShape<D, 1>::kCtas : rows <= 16 ? FewShape<D, 2>::kCtas : FewShape<D, 4>::kCtas;
+    x.tile_bytes = 64 * 2 * D * 2, x.few_ctas = side_by_side ? few_ctas : 0;
     if ((st = launch_kernel(prefix_groups, 1, kPrefixThreads, 0, stream, true, x)) != AMOEBA_OK) return st;
     p.batch.own = x.own;
     sums_space(layout, p.batch.num_rows, ws + at.rest_sums, &p.sums);
-    if ((st = run_pass<T, D>(p, layout->tp, dtype, ws + at.rest_pass, sms, stream, &rest)) != AMOEBA_OK) return st;
-    if (prefixes->num_groups == 0 || group_rows == 0) return run_join<T, D>(rest, stream);
     Pass<SharedBatch> groups;
     AttendParams<SharedBatch> g = p;
-    g.batch.groups = x.groups, g.batch.tile0 = x.tile0;
+    g.batch.groups = x.groups, g.batch.tile0 = x.tile0, g.batch.split = x.split;
     g.batch.num_seqs = prefixes->num_groups;
     g.batch.max_q_len = group_rows;
     g.whole = not_cut(g, sms);
     sums_space(layout, p.batch.num_rows, ws + at.group_sums, &g.sums);
-    if ((st = run_pass<T, D>(g, layout->tp, dtype, ws + at.groups_pass, sms, stream, &groups)) != AMOEBA_OK) return st;
+    if (many_groups) {
+        if ((st = run_pass<T, D>(g, layout->tp, dtype, ws + at.groups_pass, sms, stream, &groups)) != AMOEBA_OK) return st;
+        p.batch.waits = 0;
+        if (side_by_side) p.batch.split = x.split;
+    }
+    if ((st = run_pass<T, D>(p, layout->tp, dtype, ws + at.rest_pass, sms, stream, &rest)) != AMOEBA_OK) return st;
+    if (prefixes->num_groups == 0 || group_rows == 0) return run_join<T, D>(rest, stream);
     PrefixSums sums{};
     sums.rows = g.sums;
-    if (groups.many_ctas) {
+    if (many_groups) {
         sums.parts = Sums{groups.many.part_o, groups.many.part_m, groups.many.part_l};
-        sums.ctas = groups.many_ctas;
-    } else if ((st = run_join<T, D>(groups, stream)) != AMOEBA_OK) {
-        return st;
+        sums.split = x.split;
+    } else {
+        g.batch.waits = 0;
+        if ((st = run_pass<T, D>(g, layout->tp, dtype, ws + at.groups_pass, sms, stream, &groups)) != AMOEBA_OK) return st;
+        if ((st = run_join<T, D>(groups, stream)) != AMOEBA_OK) return st;
     }
     sums.groups = x.groups, sums.tile0 = x.tile0, sums.row_group = x.row_group;
     sums.num_groups = prefixes->num_groups, sums.num_rows = p.batch.num_rows;

@@ -66,14 +66,15 @@ struct Share {
 };
 
 // Groups: all rows of one see the same tokens, so a unit's place in the end-to-end order of all tiles is a product, and the first tile of
-// every group is in memory.  Every CTA has `even` of them, the last ones fewer, without a look at the others; what is cut is joined where
-// it is taken up (attend.cuh).
+// every group is in memory.  Every CTA has `even` of them, the last ones fewer, without a look at the others; what is cut is joined behind
+// both passes (attend.cu).  CTAs behind split[0] leave their SMs to the sequences' pass.
 template <class B>
 __device__ bool make_group_share(const AttendParams<B>& p, Share& sh) {
     const B& b = p.batch;
     if (threadIdx.x < 32) {
         const int lane = threadIdx.x;
-        const int64_t all = __ldcg(b.tile0 + b.num_seqs), even = divide(all + gridDim.x - 1, gridDim.x);
+        const int ctas = max(__ldcg(b.split), 1);
+        const int64_t all = __ldcg(b.tile0 + b.num_seqs), even = divide(all + ctas - 1, ctas);
         const int64_t begin = min(blockIdx.x * even, all), end = min(begin + even, all);
         int group = 0;  // the last that does not begin behind
         for (int base = 0; base < b.num_seqs; base += 32) {
@@ -729,6 +730,12 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
         fence_async_smem();
     }
     bool busy;
+    if constexpr (B::kShared) {
+        if (p.batch.waits) {
+            grid_dependency_wait();
+            grid_dependency_launch();
+        }
+    }
     if constexpr (B::kShared) busy = p.batch.by_groups() ? make_group_share(p, share) : make_share(p, share, reinterpret_cast<int32_t*>(smem));
     else busy = make_share(p, share, reinterpret_cast<int32_t*>(smem));
     grid_dependency_launch();

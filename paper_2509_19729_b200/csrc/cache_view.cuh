@@ -42,6 +42,8 @@ struct SharedBatch : Batch {
     const Group* groups;
     const int64_t* tile0;  // [groups + 1] first tile of every group in the end-to-end order of all groups' tiles
     const int2* own;       // [num_seqs] tokens in front of x are those of group y; null: nothing is shared
+    const int32_t* split;  // CTAs of the groups' pass and of the sequences', which run side by side; null: all of a launch's
+    int32_t waits;         // 1: what is read here is written by the kernel in front; 0: that one has waited for it
     // What there is to be checked where nothing is shared, because it would not pay.
     const int32_t *group_starts, *prefix_lens;
     int32_t num_groups, max_group_rows;
