@@ -43,7 +43,7 @@ struct ManyShape {
 
 struct ManyBarriers {
     uint64_t full[8], empty[8];  // ring of tiles: K, V, K, V, ...
-    uint64_t q_full, q_empty;
+    uint64_t q_full[2], q_empty[2];  // the second where units of one query tile take the two places in turn
     uint64_t s_full[2], p_half[2], p_full[2], o_full[2], o_free[2];
     uint64_t drain;
     uint32_t tmem;
@@ -227,6 +227,7 @@ __device__ bool make_share(const AttendParams<B>& p, Share& sh, int32_t* done) {
 struct Parts {
     Walk w;
     int32_t round = 0, tiles = 0, q_tiles, rows;  // rows of the unit, 1 .. 256
+    int32_t place = 0, places = 0;  // of the queries of a unit with one tile of them: the next unit's are loaded beside them
     bool from_start, to_end, in_turn, opened = false;  // in_turn: the warpgroups take the tiles in turn
     int64_t left;
 
@@ -264,6 +265,7 @@ struct Parts {
         rows = min(kManyRows, w.seq.qn * shape.group - w.m * kManyRows);
         q_tiles = rows > 128 ? 2 : 1;
         in_turn = B::kShared && q_tiles == 1 && tiles > 1;
+        if (B::kShared) place = q_tiles == 1 ? places++ & 1 : 0;
         from_start = w.t == 0;
         to_end = w.t + tiles == w.range.tiles;
         return true;
@@ -290,11 +292,20 @@ struct Loader : TileLoader<D, kLoadWarps, B::kShared> {
         if (++at.slot == ManyShape<D>::kStages) at.slot = 0, at.phase ^= 1;
         return true;
     }
-    __device__ __forceinline__ bool queries(const Parts& part, uint32_t q_phase) {
-        if (!__all_sync(~0u, mbar_wait_bounded(&b.q_empty, q_phase, polls(p), &b.abort))) return false;
+    uint32_t q_phase[2] = {1, 1};
+    template <int kPlace>
+    __device__ __forceinline__ bool place_free() {
+        const uint32_t parity = q_phase[kPlace];
+        q_phase[kPlace] ^= 1;
+        return __all_sync(~0u, mbar_wait_bounded(&b.q_empty[kPlace], parity, polls(p), &b.abort));
+    }
+    __device__ __forceinline__ bool queries(const Parts& part) {
+        const int place = B::kShared ? part.place : 0;
+        if (!(place ? place_free<1>() : place_free<0>())) return false;
+        if (B::kShared && part.q_tiles == 2 && !place_free<1>()) return false;
         for (int t = 0; t < part.q_tiles; ++t)
-            Base::queries(p.q, part.w, p.shape.group, part.w.m * kManyRows + t * 128, min(128, part.rows - t * 128), smem + t * kTile);
-        arrive_when_loaded(&b.q_full);
+            Base::queries(p.q, part.w, p.shape.group, part.w.m * kManyRows + t * 128, min(128, part.rows - t * 128), smem + (place + t) * kTile);
+        arrive_when_loaded(&b.q_full[place]);
         return true;
     }
 };
@@ -302,7 +313,6 @@ struct Loader : TileLoader<D, kLoadWarps, B::kShared> {
 template <int D, class B>
 __device__ RingPlace load_loop(const AttendParams<B>& p, const CacheMaps& maps, int box_rows, const Share& share, char* smem, ManyBarriers& b) {
     Loader<D, B> load(p, maps, box_rows, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32);
-    uint32_t q_phase = 1;
     bool ok = true;
     Parts part(share);
     while (ok && part.next(p, share)) {
@@ -313,8 +323,7 @@ __device__ RingPlace load_loop(const AttendParams<B>& p, const CacheMaps& maps, 
         auto at = load.groups(w.range.lo, w.range.hi, key0), next = load.groups(w.range.lo, w.range.hi, key0 + kManyTile);
         // (the first keys and values are on their way while the queries are gathered, which takes longer)
         if (B::kShared) ok = load.tile(w.range, key0, at, 0) && load.tile(w.range, key0, at, 1);
-        if (ok) ok = load.queries(part, q_phase);
-        q_phase ^= 1;
+        if (ok) ok = load.queries(part);
         for (int i = 0; ok && i < part.tiles; ++i, key0 += kManyTile) {
             if (!B::kShared || i > 0) {
                 ok = load.tile(w.range, key0, at, 0);
@@ -337,7 +346,7 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
     constexpr uint32_t kS = product<T>(128, false), kO = product<T>(D, true);
     const uint32_t tmem = __shfl_sync(~0u, b.tmem, 0), leader = elect_one();
     int slot = 0;  // of the next K; V is the one behind
-    uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
+    uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort)); };
     const uint64_t q_op = operand(smem, 16);
     auto logits = [&](int q_tile, int t, int k_slot) {
@@ -354,6 +363,11 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
         for (int k = half * 4; k < half * 4 + 4; ++k)
             umma_tmem(leader, tmem + 256 + t * D, tmem + t * 128 + k * 8, v_op + (k * 2048 >> 4), kO, accumulate || k > 0);
     };
+    // The queries of a part have been read when the products issued so far are done.
+    auto free_queries = [&](const Parts& part) {
+        umma_commit(leader, &b.q_empty[B::kShared ? part.place : 0]);
+        if (B::kShared && part.q_tiles == 2) umma_commit(leader, &b.q_empty[1]);
+    };
     // The place `n` slots on in the ring.
     auto onward = [&](int n, int& at, uint32_t& parity) {
         at = slot + n, parity = phase;
@@ -368,11 +382,11 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
             if (!wait(&b.full[at], parity)) return false;
             fence_async_smem();
             tmem_fence_after();
-            logits(0, t, at);
+            logits(part.place, t, at);
             umma_commit(leader, &b.s_full[t]);
             umma_commit(leader, &b.empty[at]);
         }
-        if (part.tiles == 2) umma_commit(leader, &b.q_empty);
+        if (part.tiles == 2) free_queries(part);
         for (int i = 0; i < part.tiles; ++i) {
             const int t = i % 2;
             onward(1, at, parity);
@@ -395,19 +409,21 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
                 onward(4, at, parity);
                 if (!wait(&b.full[at], parity)) return false;
                 fence_async_smem();
-                logits(0, t, at);
+                logits(part.place, t, at);
                 umma_commit(leader, &b.s_full[t]);
                 umma_commit(leader, &b.empty[at]);
             }
-            if (i + 3 == part.tiles) umma_commit(leader, &b.q_empty);
+            if (i + 3 == part.tiles) free_queries(part);
             onward(2, slot, phase);
         }
         return true;
     };
     Parts part(share);
     while (part.next(p, share)) {
-        if (!wait(&b.q_full, q_phase)) return false;
-        q_phase ^= 1;
+        const int place = B::kShared ? part.place : 0;
+        if (!wait(&b.q_full[place], place ? q_phase[1] : q_phase[0])) return false;
+        if (place) q_phase[1] ^= 1;
+        else q_phase[0] ^= 1;
         if (B::kShared && part.in_turn) {
             if (!in_turn(part)) return false;
             continue;
@@ -418,11 +434,11 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
         #pragma unroll
         for (int t = 0; t < 2; ++t) {
             if (t >= part.q_tiles) break;
-            logits(t, t, slot);
+            logits(place + t, t, slot);
             umma_commit(leader, &b.s_full[t]);
         }
         umma_commit(leader, &b.empty[slot]);
-        if (part.tiles == 1) umma_commit(leader, &b.q_empty);
+        if (part.tiles == 1) free_queries(part);
         for (int i = 0; i < part.tiles; ++i) {
             int v_slot = slot + 1, k_slot = slot + 2;
             uint32_t v_phase = phase, k_phase = phase;
@@ -451,13 +467,13 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
                         if (!wait(&b.full[k_slot], k_phase)) return false;
                         fence_async_smem();
                     }
-                    logits(t, t, k_slot);
+                    logits(place + t, t, k_slot);
                     umma_commit(leader, &b.s_full[t]);
                 }
             }
             umma_commit(leader, &b.empty[v_slot]);
             if (i + 1 < part.tiles) umma_commit(leader, &b.empty[k_slot]);
-            if (i + 2 == part.tiles) umma_commit(leader, &b.q_empty);
+            if (i + 2 == part.tiles) free_queries(part);
             slot = k_slot, phase = k_phase;
         }
     }
@@ -722,9 +738,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     }
     if (threadIdx.x == 0) {
         for (int i = 0; i < ManyShape<D>::kStages; ++i) mbar_init(&b.full[i], kLoadThreads), mbar_init(&b.empty[i], 1);
-        mbar_init(&b.q_full, kLoadThreads), mbar_init(&b.q_empty, 1), mbar_init(&b.drain, 1);
+        mbar_init(&b.drain, 1);
         for (int t = 0; t < 2; ++t)
-            mbar_init(&b.s_full[t], 1), mbar_init(&b.p_half[t], 128), mbar_init(&b.p_full[t], 128), mbar_init(&b.o_full[t], 1), mbar_init(&b.o_free[t], 128);
+            mbar_init(&b.q_full[t], kLoadThreads), mbar_init(&b.q_empty[t], 1), mbar_init(&b.s_full[t], 1), mbar_init(&b.p_half[t], 128), mbar_init(&b.p_full[t], 128), mbar_init(&b.o_full[t], 1), mbar_init(&b.o_free[t], 128);
         b.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
