@@ -652,8 +652,10 @@ AMOEBA_API amoeba_status amoeba_attend_shared(const amoeba_layout* layout, int32
  * pairs_cap.  BAD_BLOCK_ID: a block id outside the pool, or one counted 0, that was to be shared, copied or given back; such an id
  * is shared as it is, its pair's source is -1, and nothing is counted for it.  One code is reported, the first of these in this order.
  * What is in the counts is the caller's to keep right: with wrong ones blocks may be handed out twice.
- * UNSUPPORTED: more than 2^30 table entries or rows.  TOO_LARGE: 20 bytes for each sequence and 0.26 for every eighth of the pool's blocks do not fit in the 201 KiB of shared memory that
- * there are for them (10 000 sequences with 30 000 blocks, 1 000 with 5 million).
+ * Blocks that several sequences name are for reading: amoeba_accumulate_scores and amoeba_evict_kv in place want sequences that share
+ * none, a transformation into other pools gives every sequence its own, and amoeba_merge_block_tables reports an id that is named twice.
+ * UNSUPPORTED: more than 2^30 table entries or rows.  TOO_LARGE: 20 bytes for each sequence and 1/60 for each block of the pool are
+ * more than 200 000 (10 000 sequences with 30 000 blocks fit, and 1 000 with 10 million).
  */
 typedef struct {
     int32_t* d_block_table;           /* [num_seqs][max_blocks_per_seq], in and out */

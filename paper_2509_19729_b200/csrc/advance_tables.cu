@@ -287,9 +287,10 @@ __global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_const
         n_free = __reduce_add_sync(~0u, (uint32_t)own);
         in_front = (int)__reduce_add_sync(~0u, lane < (int)rank ? (uint32_t)own : 0u);
     }
-    // No CTA ends while another reads its counts: the barrier that all arrive at here, or behind the reads of other sequences' rows.
-    const bool reads_others = p.parents || p.pairs_cap > 0;
-    if (size > 1 && !reads_others) cluster_arrive();
+    // No CTA ends while another reads its counts: the barrier that all arrive at here, or, where there is something to share, to copy or
+    // to give back, behind that: free blocks are handed out when it is done.
+    const bool in_turn = entries[S] > 0 || copied[S] > 0;  // (the same in all CTAs)
+    if (size > 1 && !in_turn) cluster_arrive();
     int fits = S;
     if (blocks[S] > (int)n_free || rows[S] > p.num_rows || copied[S] > p.pairs_cap) {
         fits = 0;
@@ -313,6 +314,15 @@ __global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_const
         bad |= kBadBlock;  // no count left: it was not this table's to give back
         if (p.inside(b)) atomicAdd(&p.refs[b], 1);
     };
+    auto can_share = [&](int b) {  // in the pool, and counted in front of the call
+        if (p.inside(b)) {
+            const uint32_t word = (uint32_t)b / 32, tile = word / kWarps, of = kLarge ? tile % size : word / p.words;
+            const int32_t* const at = reinterpret_cast<const int32_t*>(sh.free) + (kLarge ? tile / size * kWarps + word % kWarps : word - of * p.words);
+            if (!((uint32_t)(size > 1 ? load_remote(at, of) : *at) >> (b % 32) & 1u)) return true;
+        }
+        bad |= kBadBlock;
+        return false;
+    };
 
     // ---- shared and given back blocks, sources of copies: everything that reads other sequences' rows of the table
     for (int e = me; e < n_entries; e += all) {
@@ -323,18 +333,16 @@ __global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_const
         } else if (s < fits) {
             const int b = p.table[(int64_t)parent * p.max_blocks + j];
             row[j] = b;
-            if (!p.inside(b)) bad |= kBadBlock;
-            else freed -= atomicAdd(&p.refs[b], 1) == 0;  // (its last other user has just given it back)
+            if (can_share(b)) freed -= atomicAdd(&p.refs[b], 1) == 0;  // (its last other user has just given it back)
         }
     }
     for (int s = me; n_copies > 0 && s < fits; s += all) {
         if (!copies(s)) continue;
         const int parent = parent_of(s), b = p.table[(int64_t)(parent >= 0 ? parent : s) * p.max_blocks + p.whole(sh.first[s])];
-        p.pairs[copied[s]].x = p.inside(b) ? b : -1;
+        p.pairs[copied[s]].x = parent < 0 || can_share(b) ? b : -1;
         if (parent < 0) give_back(b);
-        else if (!p.inside(b)) bad |= kBadBlock;
     }
-    if (size > 1 && reads_others) cluster_sync();
+    if (size > 1 && in_turn) cluster_sync();
     else __syncthreads();
 
     // ---- the free blocks to their sequences, a warp's word of every tile; rows, positions and slots of the tokens in them
@@ -423,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) advance_tables(const __grid_const
     if (bad) atomicOr(&s_bad, bad);
     if (freed) atomicAdd(&s_freed, freed);
     __syncthreads();
-    if (size > 1 && !reads_others) cluster_wait();
+    if (size > 1 && !in_turn) cluster_wait();
     if (tid == 0) {
         if (size > 1) store_remote(&s_all_bad[rank], 0, (int32_t)s_bad), store_remote(&s_all_freed[rank], 0, s_freed);
         else s_all_bad[0] = (int32_t)s_bad, s_all_freed[0] = s_freed;

@@ -71,7 +71,7 @@ def advance(T, table, refs, old, new, parents=None, shared=None, num_rows=None, 
             for j in range(at // T):
                 b = int(was[t, j])
                 table[s, j] = b
-                if good(b):
+                if good(b) and count[b] > 0:
                     refs[b] += 1
                 else:
                     codes.add(BAD_BLOCK_ID)
@@ -79,15 +79,16 @@ def advance(T, table, refs, old, new, parents=None, shared=None, num_rows=None, 
             for j in range(-(-n // T), -(-o // T)):
                 b = int(was[s, j])
                 table[s, j] = -1
-                if good(b) and refs[b] > 0:
+                if good(b) and count[b] > 0 and refs[b] > 0:
                     refs[b] -= 1
                 else:
                     codes.add(BAD_BLOCK_ID)
         if copy:
             b = int(was[t if t >= 0 else s, at // T])
-            pairs[k] = (b if good(b) else -1, free[taken])
+            known = good(b) and count[b] > 0
+            pairs[k] = (b if known else -1, free[taken])
             k += 1
-            if not good(b):
+            if not known:
                 codes.add(BAD_BLOCK_ID)
             elif t < 0:
                 refs[b] -= 1

@@ -182,6 +182,25 @@ def test_bad_blocks(bad):
         Step(T, t, refs, old, [9, 8, 12, 1], parents, shared, num_rows=30, pairs_cap=4).run().check()
 
 
+@pytest.mark.parametrize("T,NB,S", [(4, 60, 8), (4, 12000, 300), (2, 70000, 600)])
+def test_blocks_that_are_counted_free(T, NB, S):
+    """Named in a table, counted 0: neither shared, copied from, nor given back, and handed out to somebody."""
+    g = np.random.default_rng(S)
+    old = np.where(np.arange(S) % 4 < 2, 0, g.integers(2, 4 * T, S))
+    table, refs = state(old, T, NB, seed=S)
+    parents, shared, new = np.full(S, -1), np.zeros(S, int), old + 3
+    parents[1::4] = np.arange(2, S, 4)
+    shared[1::4] = old[2::4] - g.integers(0, 2, S // 4)
+    new[1::4] = shared[1::4] + 2
+    new[3::4] = g.integers(0, old[3::4] + 1)
+    for s in range(2, S, 8):
+        refs[table[s, 0]] = 0
+        refs[table[s + 1, -(-old[s + 1] // T) - 1]] = 0
+    refs[table[6, (old[6] - 1) // T]] = 0
+    want = Step(T, table, refs, old, new, parents, shared, num_rows=12 * S, pairs_cap=S).run().check()
+    assert want["status"] == share.BAD_BLOCK_ID
+
+
 def test_no_sequences_and_no_blocks():
     for S, NB in ((0, 5), (3, 1)):
         refs = np.zeros(NB, np.int32)
