@@ -356,7 +356,7 @@ class CacheSession:
     and set_rows() describe the batch of a step; the row buffers q, k, v, out are the caller's, one tensor per worker.
     Or the tables are kept on the GPU: advance() takes the sequences to new lengths, with blocks that block_refs counts, and describes
     the step's batch; copy_forks() then copies the blocks that forks begin inside.  attend_shared() is attend() for sequences whose
-    prefixes set_prefixes() names.
+    prefixes set_prefixes() names.  Scores, and evictions in place, are for sequences that share no blocks.
     All calls share one workspace, so they run one after another, on one stream or on streams that wait for each other;
     set_tables(), set_rows(), set_prefixes() and advance()'s host arguments work on the current stream."""
 
@@ -383,6 +383,7 @@ class CacheSession:
         self.positions, self.slots = torch.empty(0, **i32), torch.empty(0, dtype=torch.int64, device=dev)
         self.copies, self.num_copies = torch.full((num_seqs, 2), -1, **i32), torch.zeros(1, **i32)
         self.free_blocks = torch.zeros(1, **i32)
+        self.group_starts, self.prefix_lens = torch.zeros(num_seqs + 1, **i32), torch.zeros(num_seqs, **i32)
         self.prefixes = None
         self.status = torch.zeros(1, **i32)
         self.workspace, self._outgrown = torch.empty(0, dtype=torch.uint8, device=dev), []
@@ -410,10 +411,18 @@ class CacheSession:
 
     def set_prefixes(self, group_starts, prefix_lens, max_group_rows: int, always: bool = False) -> None:
         """Group g, the sequences group_starts[g] .. group_starts[g + 1] - 1, shares its first prefix_lens[g] tokens; max_group_rows:
-        no group has more new tokens; always: share whether it pays or not.  Of the batch that is described now."""
-        as_i32 = lambda x: torch.as_tensor(x, dtype=torch.int32).to(self.device)  # noqa: E731
-        self._outgrown.append(self.prefixes)  # (captured calls may still read them)
-        self.prefixes = A.make_prefixes(as_i32(group_starts), as_i32(prefix_lens), max_group_rows, always)
+        no group has more new tokens; always: share whether it pays or not.  Of the batch that is described now.  Captured calls
+        read what is set last, of as many groups as there were."""
+        starts, lens = torch.as_tensor(group_starts, dtype=torch.int32), torch.as_tensor(prefix_lens, dtype=torch.int32)
+        groups = lens.numel()
+        if starts.numel() != groups + 1:
+            raise ValueError("groups begin at [groups + 1] sequences")
+        if self.prefix_lens.numel() < groups:
+            self._outgrown += [self.group_starts, self.prefix_lens]  # captured calls may still read them
+            self.group_starts, self.prefix_lens = (torch.empty(n, dtype=torch.int32, device=self.device) for n in (groups + 1, groups))
+        self.group_starts[:groups + 1].copy_(starts)
+        self.prefix_lens[:groups].copy_(lens)
+        self.prefixes = A.make_prefixes(self.group_starts[:groups + 1], self.prefix_lens[:groups], max_group_rows, always)
 
     def advance(self, new_lens, num_rows: int, max_q_len: int, parents=None, shared_lens=None, first_positions=None, stream=None) -> None:
         """Takes the sequences from seq_lens to new_lens: blocks are handed out, given back (shorter lengths; 0: finished) and shared

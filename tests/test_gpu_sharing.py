@@ -514,6 +514,26 @@ def test_captured_calls_follow_lengths_and_groups():
         c.check()
 
 
+def test_prefixes_of_a_session_are_set_in_place():
+    """Step after step without new memory; a captured call reads what was set last; more groups than sequences have room all the same."""
+    from paper_2509_19729_b200.session import CacheSession
+
+    s = CacheSession(model(2, 2, 64), 1, 10, 4, 4, scores=False)
+    s.set_prefixes([0, 2, 4], [5, 6], 4)
+    first, kept, held = s.prefixes, len(s._outgrown), torch.cuda.memory_allocated()
+    for n in range(50):
+        s.set_prefixes([0, n % 4, 4], [n, 6], 4, always=n % 2 == 1)
+    assert len(s._outgrown) == kept and torch.cuda.memory_allocated() == held
+    assert (s.prefixes.d_group_starts, s.prefixes.d_prefix_lens) == (first.d_group_starts, first.d_prefix_lens)
+    assert first.keep[0].tolist() == [0, 1, 4] and first.keep[1].tolist() == [49, 6]
+    s.set_prefixes([0] * 9 + [4], list(range(9)), 4)
+    assert s.prefixes.num_groups == 9 and s.prefixes.keep[1].tolist() == list(range(9)) and first.keep[1].tolist() == [49, 6]
+    s.set_prefixes([0], [], 4)
+    assert s.prefixes.num_groups == 0
+    with pytest.raises(ValueError):
+        s.set_prefixes([0, 4], [1, 2], 4)
+
+
 # ---------------------------------------------------------------------------------------------------- a run of them
 
 @pytest.mark.parametrize("order,tp", [(0, 1), (1, 2)])
