@@ -383,21 +383,33 @@ struct PrefixSums {
     int32_t num_groups, num_rows;
     int32_t row_warps;         // warps of attend_finish to a row
 };
+// What is to be known of a group to find its parts; the loads in two steps.
+struct PrefixPlace {
+    int32_t ctas = 0;
+    int64_t total = 0, tile0 = 0;
+    int4 group = {0, 0, 0, 0};
+
+    __device__ __forceinline__ void all(const PrefixSums& x) {
+        if (x.split) ctas = __ldcg(x.split), total = __ldcg(x.tile0 + x.num_groups);
+    }
+    __device__ __forceinline__ void of(const PrefixSums& x, int g) {
+        if (x.split) group = __ldcg(reinterpret_cast<const int4*>(x.groups + g)), tile0 = __ldcg(x.tile0 + g);
+    }
+};
 // Adds the prefix's sums of a row (of a kv head's, from the first of the sequence) to j: every step-th part from `first` on.
 template <int D, class B>
-__device__ __forceinline__ void add_prefix(const AttendParams<B>& p, const PrefixSums& x, int g, const Seq& q, int kv_head, int row, int first, int step,
-                                           Joined& j) {
+__device__ __forceinline__ void add_prefix(const AttendParams<B>& p, const PrefixSums& x, const PrefixPlace& at_group, const Seq& q, int kv_head, int row,
+                                           int first, int step, Joined& j) {
     const int d = (int)threadIdx.x % 32 % (D / 4) * 4, tok = row / p.shape.group;
     if (x.split) {
-        const int ctas = __ldcg(x.split);
-        const int4 group = __ldcg(reinterpret_cast<const int4*>(x.groups + g));
-        const int64_t total = __ldcg(x.tile0 + x.num_groups), even = divide(total + ctas - 1, ctas);
+        const int4 group = at_group.group;
+        const int64_t even = divide(at_group.total + at_group.ctas - 1, at_group.ctas);
         const int tiles = (group.z - 1) / kManyTile + 1, row_tiles = (int)(((int64_t)group.y * p.shape.group - 1) / kManyRows) + 1;
         const int in_group = (q.q0 - group.x) * p.shape.group + row, m = in_group / kManyRows, r = in_group % kManyRows;
-        const int64_t begin = __ldcg(x.tile0 + g) + ((int64_t)kv_head * row_tiles + m) * tiles;
+        const int64_t begin = at_group.tile0 + ((int64_t)kv_head * row_tiles + m) * tiles;
         const int c0 = (int)divide(begin, even), c1 = (int)divide(begin + tiles - 1, even);
         if (c0 < c1) {
-#pragma unroll 8
+#pragma unroll 4
             for (int c = c0 + first; c <= c1; c += step) {
                 const int64_t part = (int64_t)(2 * c + (c == c0)) * kManyRows + r;
                 j.add(x.parts.m[part], x.parts.l[part], *reinterpret_cast<const float4*>(x.parts.o + part * D + d));
@@ -451,16 +463,20 @@ __device__ __forceinline__ void finish_cut(const AttendParams<SharedBatch>& p, i
     }
 }
 // The end of both passes: what was cut of the sequences', with the prefixes' sums where there are any; then x.row_warps warps to a row
-// for the rows with a prefix whose own tokens were not cut, a query head at a time.  Bound by four or five loads one after the other: 13 us
+// for the rows with a prefix whose own tokens were not cut, kHeads query heads at a time, whose loads of their own sums overlap.  Bound by four or five loads one after the other: 13 us
 // by itself for 128 rows of 32 heads, whose prefixes are in 5 to 10 parts, of which the launch in front hides some.
-template <class T, int D>
-__global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_constant__ AttendParams<SharedBatch> few, int few_ctas,
+// Four blocks to an SM, 64 registers (the whole call 115.4 us; three 116.5, five and six, which spill, 116.3 and 117.2).
+template <class T, int D, int kHeads>
+__global__ void __launch_bounds__(kJoinThreads, kHeads == 1 ? 4 : 3) attend_finish(const __grid_constant__ AttendParams<SharedBatch> few, int few_ctas,
                                                               const __grid_constant__ AttendParams<SharedBatch> many, int many_ctas,
                                                               const __grid_constant__ PrefixSums x) {
     constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;
     grid_dependency_wait();
     auto prefix = [&](const Seq& q, int kv_head, int row, int first, int step, Joined& j) {
-        if (q.first > 0) add_prefix<D>(few, x, q.group, q, kv_head, row, first, step, j);
+        if (q.first <= 0) return;
+        PrefixPlace at;
+        at.all(x), at.of(x, q.group);
+        add_prefix<D>(few, x, at, q, kv_head, row, first, step, j);
     };
     const int many_groups = kManyRows / kJoinRows<1>;
     int block = blockIdx.x;
@@ -471,9 +487,11 @@ __global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_const
     const int64_t warp = (int64_t)block * kJoinWarps + threadIdx.x / 32;
     const int row = (int)(warp / x.row_warps), first = (int)(warp - (int64_t)row * x.row_warps), stride = x.row_warps;
     const int lane = threadIdx.x % 32, half = lane / kLanes, d = lane % kLanes * 4;
+    PrefixPlace place;
+    place.all(x);
     const int g = row < x.num_rows ? x.row_group[row] : -1;
     if (g < 0) return;
-    constexpr int kHeads = 4;  // of a warp at a time, so that the loads of their own sums overlap
+    place.of(x, g);
     for (int head0 = first; head0 < few.q_heads; head0 += kHeads * stride) {
         float l[kHeads], m[kHeads];
         float4 o[kHeads];
@@ -491,7 +509,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_finish(const __grid_const
             q.q0 = row;
             Joined j;
             if (half == 0) j.add(m[i], l[i], o[i]);
-            add_prefix<D>(few, x, g, q, kv_head, r, half, kAtOnce, j);
+            add_prefix<D>(few, x, place, q, kv_head, r, half, kAtOnce, j);
             if (kAtOnce == 2) j.add_lower_half();
             if (half == 0) write_row<T, D>(few, q, kv_head, r, d, j);
         }
@@ -928,7 +946,8 @@ static amoeba_status run_shared(AttendParams<SharedBatch>& p, const amoeba_layou
     sums.row_warps = p.batch.num_rows >= 1024 ? 1 : p.q_heads;
     const int64_t grid = rest.few_ctas + rest.many_blocks() + ((int64_t)sums.num_rows * sums.row_warps + kJoinWarps - 1) / kJoinWarps;
     if (grid > INT32_MAX) return AMOEBA_ERR_UNSUPPORTED;
-    return launch_kernel(attend_finish<T, D>, (int)grid, kJoinThreads, 0, stream, true, rest.few, rest.few_ctas, rest.many, rest.many_ctas, sums);
+    return launch_kernel(sums.row_warps > 1 ? attend_finish<T, D, 1> : attend_finish<T, D, 4>, (int)grid, kJoinThreads, 0, stream, true, rest.few,
+                         rest.few_ctas, rest.many, rest.many_ctas, sums);
 }
 
 extern "C" amoeba_status amoeba_attend_shared_workspace_bytes(const amoeba_layout* layout, const amoeba_batch* batch,
