@@ -8,8 +8,8 @@
 // to the CTAs in tiles of 1024, whose free blocks are exchanged once.
 //
 // What bounds it is latency: a launch, the dependent loads of a look at a sequence's last block, one or two barriers of the
-// cluster, a search for every block.  The counts (4 bytes a block) are read once.  Measured, a step and the way back: 8 sequences 9.1 us,
-// 128 in 36 500 blocks 15, 256 with prompts of 50 000 tokens and 60 forks 26, 1024 in 750 000 blocks 35.  (A warp to a sequence's
+// cluster, a search for every block.  The counts (4 bytes a block) are read once.  Measured, a step and the way back: 8 sequences 9.3 us,
+// 128 in 36 500 blocks 15, 256 with prompts of 50 000 tokens and 60 forks 27, 1024 in 750 000 blocks 36.  (A warp to a sequence's
 // entries and the blocks dealt by warps took 20, 85, 188 and 651.)
 #include "cache_view.cuh"
 #include "cluster.cuh"

@@ -704,8 +704,8 @@ extern "C" amoeba_status amoeba_attend(const amoeba_layout* layout, int32_t dtyp
 // prefix once, and has rows enough for the tensor cores where a sequence by itself has a few.  The sequences attend over their own tokens.
 // Both leave the sums of rows with a prefix in the workspace, in 32 bits and not yet divided, and attend_finish joins them.
 //
-// Measured (one B200): 128 sequences of 64 to 2048 tokens of their own behind 8192, 32 query heads on 8 key heads of 128, a token each: 116 us
-// (569 MB once each: 88), 477 if every sequence reads its prefix; 16 behind 131 072, 64 query heads: 129 us (98), 918 by themselves.
+// Measured (one B200): 128 sequences of 64 to 2048 tokens of their own behind 8192, 32 query heads on 8 key heads of 128, a token each: 115 us
+// (569 MB once each: 88), 477 if every sequence reads its prefix; 16 behind 131 072, 64 query heads: 126 us (98), 918 by themselves.
 
 struct PrefixParams {
     Batch batch;
