@@ -21,7 +21,7 @@
 // stay below 2^8 until then and the result is the same, as numerator and sum have the same factor.  That makes the
 // scaling of O, a pass through tensor memory, rare.
 //
-// Units of at most 128 rows (of a SharedBatch, whose groups are often that small) would leave one warpgroup idle and every product
+// Units of at most 128 rows (kTurns: those of a SharedBatch, whose groups are often that small) would leave one warpgroup idle and every product
 // waiting for a softmax.  There both warpgroups have the same rows and take the tiles in turn, each with its own maximum, sum and O;
 // the first reads the other's O from tensor memory, whose lanes both reach, and joins the two.
 //
@@ -224,6 +224,8 @@ __device__ bool make_share(const AttendParams<B>& p, Share& sh, int32_t* done) {
 }
 
 // The parts of units in a CTA's share, one after the other: tiles [w.t, w.t + tiles) of w's unit.
+// kTurns: units of at most 128 rows are taken in turn by the warpgroups, and their queries by the two places.
+template <bool kTurns>
 struct Parts {
     Walk w;
     int32_t round = 0, tiles = 0, q_tiles, rows;  // rows of the unit, 1 .. 256
@@ -248,7 +250,7 @@ struct Parts {
             tiles = w.range.tiles;
         } else {
             if (left == 0) return false;
-            if (!opened && p.batch.by_groups()) {
+            if (kTurns && !opened && p.batch.by_groups()) {
                 opened = true;
                 w = sh.walk;
             } else if (!opened) {
@@ -264,8 +266,8 @@ struct Parts {
         }
         rows = min(kManyRows, w.seq.qn * shape.group - w.m * kManyRows);
         q_tiles = rows > 128 ? 2 : 1;
-        in_turn = B::kShared && q_tiles == 1 && tiles > 1;
-        if (B::kShared) place = q_tiles == 1 ? places++ & 1 : 0;
+        in_turn = kTurns && q_tiles == 1 && tiles > 1;
+        if (kTurns) place = q_tiles == 1 ? places++ & 1 : 0;
         from_start = w.t == 0;
         to_end = w.t + tiles == w.range.tiles;
         return true;
@@ -273,9 +275,9 @@ struct Parts {
 };
 
 // ---- loading
-template <int D, class B>
-struct Loader : TileLoader<D, kLoadWarps, B::kShared> {
-    using Base = TileLoader<D, kLoadWarps, B::kShared>;
+template <int D, bool kTurns, class B>
+struct Loader : TileLoader<D, kLoadWarps, kTurns> {
+    using Base = TileLoader<D, kLoadWarps, kTurns>;
     const AttendParams<B>& p;
     const uint32_t smem;  // two query tiles, then the ring
     ManyBarriers& b;
@@ -299,10 +301,10 @@ struct Loader : TileLoader<D, kLoadWarps, B::kShared> {
         q_phase[kPlace] ^= 1;
         return __all_sync(~0u, mbar_wait_bounded(&b.q_empty[kPlace], parity, polls(p), &b.abort));
     }
-    __device__ __forceinline__ bool queries(const Parts& part) {
-        const int place = B::kShared ? part.place : 0;
+    __device__ __forceinline__ bool queries(const Parts<kTurns>& part) {
+        const int place = kTurns ? part.place : 0;
         if (!(place ? place_free<1>() : place_free<0>())) return false;
-        if (B::kShared && part.q_tiles == 2 && !place_free<1>()) return false;
+        if (kTurns && part.q_tiles == 2 && !place_free<1>()) return false;
         for (int t = 0; t < part.q_tiles; ++t)
             Base::queries(p.q, part.w, p.shape.group, part.w.m * kManyRows + t * 128, min(128, part.rows - t * 128), smem + (place + t) * kTile);
         arrive_when_loaded(&b.q_full[place]);
@@ -310,11 +312,11 @@ struct Loader : TileLoader<D, kLoadWarps, B::kShared> {
     }
 };
 
-template <int D, class B>
+template <int D, bool kTurns, class B>
 __device__ RingPlace load_loop(const AttendParams<B>& p, const CacheMaps& maps, int box_rows, const Share& share, char* smem, ManyBarriers& b) {
-    Loader<D, B> load(p, maps, box_rows, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32);
+    Loader<D, kTurns, B> load(p, maps, box_rows, smem_u32(smem), b, (int)(threadIdx.x - kManyThreads + kLoadThreads) / 32, (int)threadIdx.x % 32);
     bool ok = true;
-    Parts part(share);
+    Parts<kTurns> part(share);
     while (ok && part.next(p, share)) {
         const Walk& w = part.w;
         load.open(w, p.batch);
@@ -322,10 +324,10 @@ __device__ RingPlace load_loop(const AttendParams<B>& p, const CacheMaps& maps, 
         int key0 = w.range.base + w.t * kManyTile;
         auto at = load.groups(w.range.lo, w.range.hi, key0), next = load.groups(w.range.lo, w.range.hi, key0 + kManyTile);
         // (the first keys and values are on their way while the queries are gathered, which takes longer)
-        if (B::kShared) ok = load.tile(w.range, key0, at, 0) && load.tile(w.range, key0, at, 1);
+        if (kTurns) ok = load.tile(w.range, key0, at, 0) && load.tile(w.range, key0, at, 1);
         if (ok) ok = load.queries(part);
         for (int i = 0; ok && i < part.tiles; ++i, key0 += kManyTile) {
-            if (!B::kShared || i > 0) {
+            if (!kTurns || i > 0) {
                 ok = load.tile(w.range, key0, at, 0);
                 if (ok) ok = load.tile(w.range, key0, at, 1);
             }
@@ -340,7 +342,7 @@ __device__ RingPlace load_loop(const AttendParams<B>& p, const CacheMaps& maps, 
 }
 
 // ---- products: one warp, one of its lanes issues
-template <class T, int D, class B>
+template <class T, int D, bool kTurns, class B>
 __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t smem, ManyBarriers& b) {
     constexpr int kTile = ManyShape<D>::kTileBytes, kStages = ManyShape<D>::kStages;
     constexpr uint32_t kS = product<T>(128, false), kO = product<T>(D, true);
@@ -364,9 +366,9 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
             umma_tmem(leader, tmem + 256 + t * D, tmem + t * 128 + k * 8, v_op + (k * 2048 >> 4), kO, accumulate || k > 0);
     };
     // The queries of a part have been read when the products issued so far are done.
-    auto free_queries = [&](const Parts& part) {
-        umma_commit(leader, &b.q_empty[B::kShared ? part.place : 0]);
-        if (B::kShared && part.q_tiles == 2) umma_commit(leader, &b.q_empty[1]);
+    auto free_queries = [&](const Parts<kTurns>& part) {
+        umma_commit(leader, &b.q_empty[kTurns ? part.place : 0]);
+        if (kTurns && part.q_tiles == 2) umma_commit(leader, &b.q_empty[1]);
     };
     // The place `n` slots on in the ring.
     auto onward = [&](int n, int& at, uint32_t& parity) {
@@ -374,7 +376,7 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
         if (at >= kStages) at -= kStages, parity ^= 1;
     };
     // The products of a part whose tiles the warpgroups take in turn: the logits run two tiles ahead of the weights.
-    auto in_turn = [&](const Parts& part) {
+    auto in_turn = [&](const Parts<kTurns>& part) {
         int at;
         uint32_t parity;
         for (int t = 0; t < 2; ++t) {
@@ -418,13 +420,13 @@ __device__ bool multiply(const AttendParams<B>& p, const Share& share, uint32_t 
         }
         return true;
     };
-    Parts part(share);
+    Parts<kTurns> part(share);
     while (part.next(p, share)) {
-        const int place = B::kShared ? part.place : 0;
+        const int place = kTurns ? part.place : 0;
         if (!wait(&b.q_full[place], place ? q_phase[1] : q_phase[0])) return false;
         if (place) q_phase[1] ^= 1;
         else q_phase[0] ^= 1;
-        if (B::kShared && part.in_turn) {
+        if (kTurns && part.in_turn) {
             if (!in_turn(part)) return false;
             continue;
         }
@@ -560,7 +562,7 @@ __device__ __forceinline__ float row_weights(uint32_t s_tmem, float c, float ref
     return a + b;
 }
 
-template <class T, int D, class B>
+template <class T, int D, bool kTurns, class B>
 __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarriers& b) {
     const Shape& sh = p.shape;
     const int t = threadIdx.x / 128;
@@ -572,10 +574,10 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
         return __all_sync(~0u, mbar_wait_bounded(bar, parity, polls(p), &b.abort));  // and the warp is together again
     };
     bool ok = true;  // a warp that gives up goes on to the barriers below, where the others of its warpgroup wait for it
-    Parts part(share);
+    Parts<kTurns> part(share);
     while (part.next(p, share)) {
         const Walk& w = part.w;
-        const bool in_turn = B::kShared && part.in_turn;
+        const bool in_turn = kTurns && part.in_turn;
         // A bad block anywhere in the part: its tokens are looked up one by one below.  The table is asked now and the answer looked at behind
         // the wait for the first logits.
         const int32_t* table = p.batch.table + (int64_t)w.seq.row * p.batch.max_blocks;
@@ -675,7 +677,7 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
             }
             char* out = there ? row_of<D>(p.out, p, w.seq, w.h, row) : nullptr;
             float* const raw = direct ? p.sums.o + head * D : p.part_o + at * D;
-#pragma unroll (B::kShared ? 1 : D / 32)  // (what runs once or twice waits for its instructions)
+#pragma unroll (kTurns ? 1 : D / 32)  // (what runs once or twice waits for its instructions)
             for (int j = 0; j < D / 32; ++j) {
                 uint32_t o[32];
                 __syncwarp();  // (rows that are not there have parted from the others)
@@ -724,7 +726,7 @@ __device__ bool softmax(const AttendParams<B>& p, const Share& share, ManyBarrie
     return ok;
 }
 
-template <class T, int D, class B>
+template <class T, int D, bool kTurns, class B>
 __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_constant__ AttendParams<B> p, const __grid_constant__ CacheMaps maps,
                                                             int box_rows) {
     extern __shared__ char smem_raw[];
@@ -752,7 +754,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
             grid_dependency_launch();
         }
     }
-    if constexpr (B::kShared) busy = p.batch.by_groups() ? make_group_share(p, share) : make_share(p, share, reinterpret_cast<int32_t*>(smem));
+    if constexpr (kTurns) busy = p.batch.by_groups() ? make_group_share(p, share) : make_share(p, share, reinterpret_cast<int32_t*>(smem));
     else busy = make_share(p, share, reinterpret_cast<int32_t*>(smem));
     grid_dependency_launch();
     tmem_fence_before();
@@ -767,15 +769,15 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == 8) {
-            if (!multiply<T, D>(p, share, smem_u32(smem), b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+            if (!multiply<T, D, kTurns>(p, share, smem_u32(smem), b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
             __syncwarp();
             drain_products(b);
         } else {
-            loaded = load_loop<D>(p, maps, box_rows, share, smem, b);
+            loaded = load_loop<D, kTurns>(p, maps, box_rows, share, smem, b);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        if (!softmax<T, D>(p, share, b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
+        if (!softmax<T, D, kTurns>(p, share, b)) b.abort = 1, report(p.status, AMOEBA_ERR_TIMEOUT);
     }
     grid_dependency_wait();  // attend_few in front is done when this kernel is
     tmem_fence_before();
@@ -787,10 +789,18 @@ __global__ void __launch_bounds__(kManyThreads, 1) attend_many(const __grid_cons
     if (warp > 8 && b.abort) drain_ring<ManyShape<D>::kStages>(b.full, loaded);
 }
 
+template <class T, int D, bool kTurns, class B>
+static amoeba_status launch_one(const AttendParams<B>& p, const CacheMaps& maps, int box_rows, int ctas, cudaStream_t stream) {
+    if (ensure_dynamic_smem((const void*)attend_many<T, D, kTurns, B>, ManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
+    return launch_kernel(attend_many<T, D, kTurns, B>, ctas, kManyThreads, ManyShape<D>::kSmem, stream, true, p, maps, box_rows);
+}
+// In turn where units are small: groups, and sequences that have no unit of more than 128 rows.  What it takes costs large units 4 % (16
+// sequences of 500 new tokens behind 6000 to 12288, the whole call: 621 us, 595 without).
 template <class T, int D, class B>
 static amoeba_status launch(const AttendParams<B>& p, const CacheMaps& maps, int box_rows, int ctas, cudaStream_t stream) {
-    if (ensure_dynamic_smem((const void*)attend_many<T, D, B>, ManyShape<D>::kSmem) != cudaSuccess) return AMOEBA_ERR_CUDA;
-    return launch_kernel(attend_many<T, D, B>, ctas, kManyThreads, ManyShape<D>::kSmem, stream, true, p, maps, box_rows);
+    if constexpr (B::kShared)
+        if (p.batch.by_groups() || (int64_t)p.batch.max_q_len * p.shape.group <= 128) return launch_one<T, D, true>(p, maps, box_rows, ctas, stream);
+    return launch_one<T, D, false>(p, maps, box_rows, ctas, stream);
 }
 
 template <class B>
