@@ -463,7 +463,7 @@ __device__ __forceinline__ void finish_cut(const AttendParams<SharedBatch>& p, i
     }
 }
 // The end of both passes: what was cut of the sequences', with the prefixes' sums where there are any; then x.row_warps warps to a row
-// for the rows with a prefix whose own tokens were not cut, kHeads query heads at a time, whose loads of their own sums overlap.  Bound by four or five loads one after the other: 13 us
+// for the rows with a prefix whose own tokens were not cut, kHeads query heads at a time, whose loads of their own sums overlap.  Bound by four or five loads one after the other: 12 us
 // by itself for 128 rows of 32 heads, whose prefixes are in 5 to 10 parts, of which the launch in front hides some.
 // Four blocks to an SM, 64 registers (the whole call 115.4 us; three 116.5, five and six, which spill, 116.3 and 117.2).
 template <class T, int D, int kHeads>
